@@ -371,7 +371,7 @@ def _prepare_pages(case, g, s):
                             dst=torch.empty(cap, dtype=torch.int32, device=DEVICE),
                             counts=torch.empty(2, dtype=torch.int32, device=DEVICE),
                             granted=torch.empty(B2, dtype=torch.int32, device=DEVICE))
-            s["ws"] = s["spec"].cache_workspace(B2, case["K"], ps, P, DEVICE)
+            s["ws"] = s["spec"].cache_workspace(B2, case["K"], ps, DEVICE)
         return
     accepted = [k - p - 1 for k, p in zip(_kept(case), ctx)]
     # a finished request keeps nothing: position -1 and nothing accepted
@@ -383,7 +383,6 @@ def _prepare_pages(case, g, s):
                         dst=torch.empty(cap, dtype=torch.int32, device=DEVICE),
                         map=torch.empty(P, dtype=torch.int32, device=DEVICE),
                         counts=torch.empty(2, dtype=torch.int32, device=DEVICE))
-        s["ws"] = s["spec"].cache_workspace(B, case["K"], ps, P, DEVICE)
 
 
 # ---------------------------------------------------------------------------
@@ -500,7 +499,7 @@ def _sweep(s):
         spec, o = s["spec"], s["out"]
         spec.spec_cache_release(table, refs, s["pos_now"], ps, accepted_len=s["accepted"], window=W, sinks=S,
                                 status=s["status"])
-        spec.spec_cache_compact(table, refs, o["src"], o["dst"], o["map"], o["counts"], s["ws"], status=s["status"])
+        spec.spec_cache_compact(table, refs, o["src"], o["dst"], o["map"], o["counts"], status=s["status"])
         spec.spec_cache_copy(s["k"], s["v"], o["src"], o["dst"], o["counts"], status=s["status"])
         return dict(o, table=table, refs=refs, k=s["k"], v=s["v"])
     # release: pages past the kept tokens, and those that no later row sees
