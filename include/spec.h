@@ -78,8 +78,9 @@ typedef enum {
   SPEC_ERR_CUDA = 3,        /* a CUDA runtime call failed (e.g. launch) */
   SPEC_ERR_BAD_INPUT = 4,   /* device-detected data error (via *status) */
   SPEC_ERR_TIMEOUT = 5,     /* a bounded device wait gave up (via *status) */
-  SPEC_ERR_TOO_LARGE = 6    /* shape needs more than the static scratch of
+  SPEC_ERR_TOO_LARGE = 6,   /* shape needs more than the static scratch of
                                spec_verify_static; nothing launched */
+  SPEC_ERR_CACHE_FULL = 7   /* too few free pages for a request (via *status) */
 } spec_err;
 
 typedef enum { SPEC_BF16 = 0, SPEC_F32 = 1 } spec_dtype;
@@ -508,6 +509,214 @@ int spec_select_round(const int32_t* chosen_T, int M, const int32_t* cand_T, voi
  * A row whose offset within its request exceeds K sets SPEC_ERR_BAD_INPUT. */
 int spec_pack_rows(const void* src, size_t row_bytes, int B, int K, const int32_t* row_offsets,
                    void* dst, int R_dst, int32_t* status, cudaStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * The paged key-value cache.  The target forward between spec_allocate and
+ * spec_verify runs over the packed rows (request i's rows row_offsets[i] ..
+ * row_offsets[i] + n_i, at positions pos_base[i] + j); its attention reads
+ * the keys and values of every earlier position, and a rejected draft's keys
+ * have to leave the cache again.  The paper leaves this to the serving engine
+ * (Section 4.3); the entry points below do it on the device, on the arrays
+ * the round already has, with no host round trip.
+ *
+ * Pages.  A cache holds `pages` pages of page_size consecutive positions of
+ * one request.  page_table (device int32 [B, max_pages]) maps request i's
+ * slot s (positions s * page_size ...) to a page, -1 for none.  page_refs
+ * (device int32 [pages]) counts the holders of each page: table entries, and
+ * whoever else keeps one (a prefix store); 0 means free.  One table serves
+ * every layer.
+ *
+ * Element (layer l, page p, token t, head h, d) of K lies at
+ *   k + l * layer_stride + p * page_stride + t * token_stride
+ *     + h * head_stride + d   (strides in elements), and of V likewise.
+ * So [pages, page_size, kv_heads, head_dim], [pages, kv_heads, page_size,
+ * head_dim] and K/V interleaved layouts are all expressible.  k and v are
+ * 16-byte aligned, every stride and head_dim * element size a multiple of
+ * 16 bytes, strides are positive and the elements do not overlap.
+ * ---------------------------------------------------------------------- */
+typedef struct spec_cache {
+  void* k;                /* device */
+  void* v;                /* device */
+  int32_t dtype;          /* spec_dtype of both */
+  int32_t layers;         /* >= 1 */
+  int32_t pages;          /* >= 1 */
+  int32_t page_size;      /* >= 1 positions */
+  int32_t kv_heads;       /* >= 1 */
+  int32_t head_dim;       /* <= SPEC_MAX_HEAD_DIM */
+  int64_t layer_stride, page_stride, token_stride, head_stride;
+} spec_cache;
+
+#define SPEC_MAX_HEAD_DIM 256
+#define SPEC_MAX_GROUP 64 /* query heads per key-value head */
+
+/* ------------------------------------------------------------------------
+ * spec_attend -- attention of the packed verification rows over the paged
+ * cache (K = 0: one new token per request).  For row j of request i, at
+ * position P = pos_base[i] + j, and query head h (key-value head
+ * h / (q_heads / kv_heads)):
+ *   x_t = scale * <q, k_t> over the visible positions t: t <= P and
+ *         (window == 0, or t > P - window, or t < sinks);
+ *   out = sum_t exp(x_t - m) v_t / sum_t exp(x_t - m),  m = max_t x_t;
+ *   lse = m + ln sum_t exp(x_t - m).
+ * A row that sees no position (P < 0: pos_base = -1 marks an idle request of
+ * a captured graph) gets out = 0 and lse = -inf.  The row's own key and value
+ * are read from the cache (spec_cache_append comes first).  Keys and values
+ * of invisible positions do not reach the result, whatever they hold.
+ * Sums are held in fp32; with a bf16 cache of head_dim 64 or 128 the products
+ * run on the tensor cores, the weights exp(x - m) rounded to bf16 for the
+ * second one (the sum in the denominator is taken before that rounding).
+ * The result does not depend on the run: partial results of a request that
+ * is split over CTAs are joined in a fixed order.
+ * Arguments
+ *   q               device [R, q_heads, head_dim] of cache->dtype, rows
+ *                   q_row_stride elements apart (a multiple of 16 bytes,
+ *                   16-byte aligned): a view of a fused projection will do.
+ *   layer           in [0, cache->layers).
+ *   row_offsets, depth, pos_base  as spec_verify.
+ *   page_table      device int32 [B, max_pages].
+ *   scale           finite, > 0.
+ *   window          0 (none) or the number of positions a row sees up to its
+ *                   own; sinks: the first positions that stay visible (>= 0,
+ *                   of no effect without a window).  Table entries of
+ *                   positions that no row sees may be -1.
+ *   out             device [R, q_heads, head_dim] of cache->dtype, 16-byte
+ *                   aligned; rows that belong to no request are not written.
+ *   lse_out         device fp32 [R, q_heads] or NULL.
+ *   status          device int32 [1]: a visible position without a page (its
+ *                   keys count as invisible), a position past the table (its
+ *                   request's rows are treated as seeing nothing), or
+ *                   inconsistent offsets or depths (the request's rows are
+ *                   not written) set SPEC_ERR_BAD_INPUT.
+ *   ws, ws_bytes    spec_attend_workspace(...) bytes, 256-byte aligned,
+ *                   zero-filled once before the first use; left ready for the
+ *                   next call.  Calls that may overlap need separate ones.
+ * Limits: 1 <= B, 0 <= K <= SPEC_MAX_DRAFTS, q_heads a multiple of kv_heads
+ * and at most SPEC_MAX_GROUP times it, max_pages * page_size < 2^31.  A longer
+ * prompt is fed in chunks of up to K + 1 = 256 rows.
+ * ---------------------------------------------------------------------- */
+size_t spec_attend_workspace(int B, int K, int q_heads, int kv_heads, int head_dim, int dtype);
+int spec_attend(const void* q, int64_t q_row_stride, int q_heads, const spec_cache* cache, int layer,
+                const int32_t* row_offsets, const int32_t* depth, const int64_t* pos_base,
+                const int32_t* page_table, int max_pages, int B, int K, float scale, int window,
+                int sinks, void* out, float* lse_out, int32_t* status, void* ws, size_t ws_bytes,
+                cudaStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * spec_cache_append -- writes the round's new keys and values to their pages:
+ * row j of request i goes to position pos_base[i] + j of `layer`.
+ *   k_new, v_new    device [R, kv_heads, head_dim] of cache->dtype, rows
+ *                   k_row_stride / v_row_stride elements apart (multiples of
+ *                   16 bytes, 16-byte aligned).
+ *   row_offsets, depth, pos_base, page_table: as spec_attend.  A row at a
+ *                   negative position is skipped; one at a position past the
+ *                   table or without a page is skipped and sets
+ *                   SPEC_ERR_BAD_INPUT.
+ * Positions of different requests must lie in different pages (spec_cache_
+ * reserve sees to that), else the rows overwrite one another.
+ * ---------------------------------------------------------------------- */
+int spec_cache_append(const spec_cache* cache, int layer, const void* k_new, int64_t k_row_stride,
+                      const void* v_new, int64_t v_row_stride, const int32_t* row_offsets,
+                      const int32_t* depth, const int64_t* pos_base, const int32_t* page_table,
+                      int max_pages, int B, int K, int32_t* status, cudaStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * spec_cache_fork -- request i of the new table takes the pages of request
+ * parent[i] of the old one (several may take the same: parallel samples of a
+ * prompt; none: a request that ends; -1: a new, empty request).
+ *   page_table      device int32 [B_in, max_pages]; page_refs device int32
+ *                   [pages]; parent device int32 [B], each in [-1, B_in).
+ *   table_out       device int32 [B, max_pages], not overlapping page_table.
+ *   refs_out        device int32 [pages]: page_refs plus the new table's
+ *                   entries less the old table's; may be page_refs itself.
+ * A parent or an entry out of range counts as -1 and sets SPEC_ERR_BAD_INPUT.
+ * ---------------------------------------------------------------------- */
+int spec_cache_fork(const int32_t* page_table, const int32_t* page_refs, const int32_t* parent,
+                    int B_in, int B, int max_pages, int pages, int32_t* table_out,
+                    int32_t* refs_out, int32_t* status, cudaStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * spec_cache_reserve -- every request gets pages of its own for the positions
+ * pos_base[i] .. pos_base[i] + n_i of its next rows (negative ones need
+ * none).  A slot they touch that is empty takes a free page; one whose page
+ * has other holders takes a free page and is listed to be copied (copy on
+ * write; spec_cache_copy does the copying).  Reference counts are read as
+ * they were before the call.
+ *   The needed slots, in order of (request, slot), take the free pages in
+ *   order of their index.  A request is granted if the slots needed up to and
+ *   including its own do not exceed the free pages, or if it needs none;
+ *   otherwise its entries stay as they are and SPEC_ERR_CACHE_FULL is set.
+ *   page_table      device int32 [B, max_pages], updated; page_refs device
+ *                   int32 [pages], updated.
+ *   row_offsets, depth, pos_base  as spec_attend (row_offsets is only checked
+ *                   against depth).
+ *   cow_src_out, cow_dst_out  device int32 [B * (K / page_size + 2)]: the
+ *                   pages to copy, in the same order; -1 past the last pair.
+ *   counts_out      device int32 [2]: pairs to copy, pages taken.
+ *   granted_out     device int32 [B]: 1 or 0.
+ *   status          a position past the table, an entry out of range or
+ *                   inconsistent depths set SPEC_ERR_BAD_INPUT; that request
+ *                   is not granted and needs nothing.
+ *   ws, ws_bytes    spec_cache_workspace(...) bytes, 256-byte aligned; no
+ *                   zeroing needed.
+ * ---------------------------------------------------------------------- */
+size_t spec_cache_workspace(int B, int K, int page_size);
+int spec_cache_reserve(int32_t* page_table, int32_t* page_refs, const int32_t* row_offsets,
+                       const int32_t* depth, const int64_t* pos_base, int B, int K, int max_pages,
+                       int pages, int page_size, int32_t* cow_src_out, int32_t* cow_dst_out,
+                       int32_t* counts_out, int32_t* granted_out, int32_t* status, void* ws,
+                       size_t ws_bytes, cudaStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * spec_cache_copy -- copies page src[x] to page dst[x] for x < *count, keys
+ * and values of every layer.  No page may be a destination twice, or both a
+ * source and a destination (the lists of spec_cache_reserve and
+ * spec_cache_compact satisfy this).
+ *   src, dst        device int32 [max_count]; count device int32 [1] (the
+ *                   first entry of either counts_out).
+ * A page out of range is skipped and sets SPEC_ERR_BAD_INPUT; a count outside
+ * [0, max_count] sets it too and is clamped.
+ * ---------------------------------------------------------------------- */
+int spec_cache_copy(const spec_cache* cache, const int32_t* src, const int32_t* dst,
+                    const int32_t* count, int max_count, int32_t* status, cudaStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * spec_cache_release -- gives back the pages that request i no longer needs
+ * once it keeps its first keep = pos_base[i] + accepted_len[i] + 1 positions
+ * (accepted_len from spec_verify: the rejected drafts' positions go), or
+ * keep = max(0, pos_base[i]) with accepted_len NULL (0 gives back the whole
+ * request).  With a window, pages that neither a later row's window nor the
+ * sinks reach go back too.  A slot s is dropped if
+ *   s * page_size >= keep, or window > 0 and (s + 1) * page_size <=
+ *   keep - window + 1 and s * page_size >= sinks:
+ * its entry becomes -1 and its page's count goes down by one.
+ *   page_table      device int32 [B, max_pages], page_refs device int32
+ *                   [pages]: updated.
+ *   status          an entry out of range (dropped all the same), an accepted
+ *                   length < 0 (counts as 0) or a count that was not positive
+ *                   sets SPEC_ERR_BAD_INPUT.
+ * ---------------------------------------------------------------------- */
+int spec_cache_release(int32_t* page_table, int32_t* page_refs, const int64_t* pos_base,
+                       const int32_t* accepted_len, int B, int max_pages, int pages, int page_size,
+                       int window, int sinks, int32_t* status, cudaStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * spec_cache_compact -- moves the live pages (page_refs > 0) to the indices
+ * below their number n: the live pages at or past n, in order of index, take
+ * the free indices below n, in order of index.  Table and counts are updated;
+ * spec_cache_copy moves the contents (call it next, on the same stream).
+ *   page_table      device int32 [B, max_pages], page_refs device int32
+ *                   [pages]: updated.  An entry whose page is not live
+ *                   becomes -1, one out of range too; both set
+ *                   SPEC_ERR_BAD_INPUT.
+ *   move_src_out, move_dst_out  device int32 [max(1, pages / 2)]: the moves;
+ *                   -1 past the last.
+ *   page_map_out    device int32 [pages]: a live page's new index, -1 for a
+ *                   free one (for holders outside the table).
+ *   counts_out      device int32 [2]: moves, live pages.
+ * ---------------------------------------------------------------------- */
+int spec_cache_compact(int32_t* page_table, int32_t* page_refs, int B, int max_pages, int pages,
+                       int32_t* move_src_out, int32_t* move_dst_out, int32_t* page_map_out,
+                       int32_t* counts_out, int32_t* status, cudaStream_t stream);
 
 /* ------------------------------------------------------------------------
  * spec_profile_stream_pass -- measurement aid.  The next spec_verify call

@@ -25,10 +25,13 @@ ERR_CUDA = 3
 ERR_BAD_INPUT = 4
 ERR_TIMEOUT = 5
 ERR_TOO_LARGE = 6
+ERR_CACHE_FULL = 7
 
 MAX_DRAFTS = 255
 MAX_ALLOC_POSITIONS = 8192
 MAX_CANDIDATES = 64
+MAX_HEAD_DIM = 256
+MAX_GROUP = 64
 
 SHARD_STAT_BYTES = 32
 SHARD_DECISION_BYTES = 32
@@ -42,7 +45,9 @@ __all__ = [
     "spec_shard_finish", "shard_workspace", "spec_draft_workspace", "spec_draft", "draft_workspace",
     "spec_graph_begin_capture", "spec_graph_end_capture", "spec_graph_launch", "spec_graph_destroy",
     "spec_select_round", "spec_pack_rows", "spec_markov_workspace", "spec_markov_draft", "markov_workspace",
-    "spec_pointer_device_readable", "spec_check_bounded_wait",
+    "spec_pointer_device_readable", "spec_check_bounded_wait", "spec_attend_workspace", "spec_attend",
+    "attend_workspace", "spec_cache_append", "spec_cache_fork", "spec_cache_workspace", "cache_workspace",
+    "spec_cache_reserve", "spec_cache_copy", "spec_cache_release", "spec_cache_compact",
 ]
 
 
@@ -335,6 +340,164 @@ def spec_shard_finish(races, S, decisions, B, K, V, temperature, seeds, request_
         _ptr(races), S, _ptr(decisions), B, K, V, float(temperature), _ptr(seeds), _ptr(request_ids),
         _ptr(accepted_len_out), _ptr(out_tokens), _ptr(status), _stream(stream))
     _check(code, "spec_shard_finish")
+
+
+def _cache(k, v):
+    """struct spec_cache of K and V tensors [layers, pages, page_size, kv_heads, head_dim] (or without the first
+    dimension), any strides but a contiguous last dimension."""
+    if k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.dim() not in (4, 5):
+        raise ValueError("k_cache and v_cache: 4 or 5 dimensions, the same shape, strides and dtype")
+    if k.stride(-1) != 1:
+        raise ValueError("the head dimension of a cache must be contiguous")
+    shape = (1,) * (5 - k.dim()) + tuple(k.shape)
+    stride = (0,) * (5 - k.dim()) + tuple(k.stride())
+    return _native.Cache(k.data_ptr(), v.data_ptr(), _dtype(k), *shape[:5], *stride[:4])
+
+
+def _rows(t, heads, head_dim, like, what):
+    """Pointer and row stride of packed rows [R, heads, head_dim]; rows may lie apart (a fused projection's view)."""
+    if t.dtype != like.dtype:
+        raise TypeError(f"{what}: the cache's dtype is {like.dtype}, not {t.dtype}")
+    if t.dim() != 3 or t.shape[1:] != (heads, head_dim):
+        raise ValueError(f"{what}: expected [rows, {heads}, {head_dim}]")
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != head_dim):
+        raise ValueError(f"{what}: a row's heads must be contiguous")
+    return ctypes.c_void_p(t.data_ptr()), (t.stride(0) if t.shape[0] > 1 else heads * head_dim)
+
+
+def _table(page_table, B):
+    if page_table.dim() != 2 or page_table.shape[0] < B or page_table.dtype != torch.int32:
+        raise ValueError("page_table: expected int32 [B, max_pages]")
+    return _ptr(page_table), page_table.shape[1]
+
+
+def _ints(t, n, what, dtype=torch.int32):
+    """Pointer of an integer tensor (or None) of at least n entries."""
+    if t is not None and (t.dtype != dtype or t.numel() < n):
+        raise ValueError(f"{what}: expected {dtype} with at least {n} entries")
+    return _ptr(t)
+
+
+def spec_attend_workspace(B: int, K: int, q_heads: int, kv_heads: int, head_dim: int, dtype=torch.bfloat16) -> int:
+    return library().spec_attend_workspace(B, K, q_heads, kv_heads, head_dim, F32 if dtype == torch.float32 else BF16)
+
+
+def attend_workspace(B: int, K: int, q_heads: int, kv_heads: int, head_dim: int, dtype=torch.bfloat16, device="cuda"):
+    """A zero-filled workspace for spec_attend."""
+    n = spec_attend_workspace(B, K, q_heads, kv_heads, head_dim, dtype)
+    if n == 0:
+        raise SpecError(ERR_INVALID_ARG, "spec_attend_workspace")
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+def spec_attend(q, k_cache, v_cache, page_table, pos_base, B, K, out, ws, row_offsets=None, depth=None, scale=None,
+                window=0, sinks=0, lse_out=None, layer=0, status=None, stream=None):
+    """q and out [R, q_heads, head_dim]; k_cache and v_cache [layers, pages, page_size, kv_heads, head_dim] (or one
+    layer, 4 dimensions); page_table int32 [B, max_pages]; scale 1 / sqrt(head_dim) if None; see spec.h."""
+    cache = _cache(k_cache, v_cache)
+    Hq, D = q.shape[1], cache.head_dim
+    q_ptr, q_row = _rows(q, Hq, D, k_cache, "q")
+    rows = B * (K + 1) if row_offsets is None else 0  # packed rows: their number is on the device
+    if q.shape[0] < rows or out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError("out: expected q's shape and dtype, and rows for every request")
+    if lse_out is not None and (lse_out.dtype != torch.float32 or lse_out.numel() < q.shape[0] * Hq):
+        raise ValueError("lse_out: expected fp32 [R, q_heads]")
+    table, max_pages = _table(page_table, B)
+    code = library().spec_attend(
+        q_ptr, q_row, Hq, ctypes.byref(cache), layer, _ints(row_offsets, B + 1, "row_offsets"),
+        _ints(depth, B, "depth"), _ints(pos_base, B, "pos_base", torch.int64), table, max_pages, B, K,
+        D ** -0.5 if scale is None else float(scale), window, sinks, _ptr(out), _ptr(lse_out), _ptr(status), _ptr(ws),
+        _nbytes(ws), _stream(stream))
+    _check(code, "spec_attend")
+
+
+def spec_cache_append(k_new, v_new, k_cache, v_cache, page_table, pos_base, B, K, row_offsets=None, depth=None,
+                      layer=0, status=None, stream=None):
+    """k_new and v_new [R, kv_heads, head_dim], written to their pages; see spec.h."""
+    cache = _cache(k_cache, v_cache)
+    k_ptr, k_row = _rows(k_new, cache.kv_heads, cache.head_dim, k_cache, "k_new")
+    v_ptr, v_row = _rows(v_new, cache.kv_heads, cache.head_dim, k_cache, "v_new")
+    if row_offsets is None and min(k_new.shape[0], v_new.shape[0]) < B * (K + 1):
+        raise ValueError("k_new, v_new: rows for every request")
+    table, max_pages = _table(page_table, B)
+    code = library().spec_cache_append(
+        ctypes.byref(cache), layer, k_ptr, k_row, v_ptr, v_row, _ints(row_offsets, B + 1, "row_offsets"),
+        _ints(depth, B, "depth"), _ints(pos_base, B, "pos_base", torch.int64), table, max_pages, B, K, _ptr(status),
+        _stream(stream))
+    _check(code, "spec_cache_append")
+
+
+def spec_cache_fork(page_table, page_refs, parent, table_out, refs_out, status=None, stream=None):
+    """table_out [B, max_pages]: row i takes page_table's row parent[i] (-1: empty); see spec.h."""
+    B, pages = table_out.shape[0], page_refs.numel()
+    table, max_pages = _table(page_table, 1)
+    out, max_out = _table(table_out, 1)
+    if max_out != max_pages:
+        raise ValueError("table_out: expected page_table's max_pages")
+    code = library().spec_cache_fork(
+        table, _ints(page_refs, pages, "page_refs"), _ints(parent, B, "parent"), page_table.shape[0], B, max_pages,
+        pages, out, _ints(refs_out, pages, "refs_out"), _ptr(status), _stream(stream))
+    _check(code, "spec_cache_fork")
+
+
+def spec_cache_workspace(B: int, K: int, page_size: int) -> int:
+    return library().spec_cache_workspace(B, K, page_size)
+
+
+def cache_workspace(B: int, K: int, page_size: int, device="cuda"):
+    """A workspace for spec_cache_reserve."""
+    n = spec_cache_workspace(B, K, page_size)
+    if n == 0:
+        raise SpecError(ERR_INVALID_ARG, "spec_cache_workspace")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def spec_cache_reserve(page_table, page_refs, pos_base, B, K, page_size, cow_src_out, cow_dst_out, counts_out,
+                       granted_out, ws, row_offsets=None, depth=None, status=None, stream=None):
+    """cow_src_out, cow_dst_out int32 [B * (K // page_size + 2)]; counts_out int32 [2]; granted_out int32 [B]."""
+    table, max_pages = _table(page_table, B)
+    cap = B * (K // page_size + 2) if page_size > 0 else 0
+    code = library().spec_cache_reserve(
+        table, _ints(page_refs, 1, "page_refs"), _ints(row_offsets, B + 1, "row_offsets"), _ints(depth, B, "depth"),
+        _ints(pos_base, B, "pos_base", torch.int64), B, K, max_pages, page_refs.numel(), page_size,
+        _ints(cow_src_out, cap, "cow_src_out"), _ints(cow_dst_out, cap, "cow_dst_out"),
+        _ints(counts_out, 2, "counts_out"), _ints(granted_out, B, "granted_out"), _ptr(status), _ptr(ws), _nbytes(ws),
+        _stream(stream))
+    _check(code, "spec_cache_reserve")
+
+
+def spec_cache_copy(k_cache, v_cache, src, dst, count, status=None, stream=None):
+    """Pages src[x] to dst[x] for x < count[0] (a device tensor), every layer of both caches."""
+    cache = _cache(k_cache, v_cache)
+    n = min(src.numel(), dst.numel())
+    code = library().spec_cache_copy(ctypes.byref(cache), _ints(src, n, "src"), _ints(dst, n, "dst"),
+                                     _ints(count, 1, "count"), n, _ptr(status), _stream(stream))
+    _check(code, "spec_cache_copy")
+
+
+def spec_cache_release(page_table, page_refs, pos_base, page_size, accepted_len=None, window=0, sinks=0, status=None,
+                       stream=None):
+    """Drops what lies past pos_base + accepted_len + 1 kept positions (past pos_base without accepted_len)."""
+    B = page_table.shape[0]
+    table, max_pages = _table(page_table, B)
+    code = library().spec_cache_release(
+        table, _ints(page_refs, 1, "page_refs"), _ints(pos_base, B, "pos_base", torch.int64),
+        _ints(accepted_len, B, "accepted_len"), B, max_pages, page_refs.numel(), page_size, window, sinks, _ptr(status),
+        _stream(stream))
+    _check(code, "spec_cache_release")
+
+
+def spec_cache_compact(page_table, page_refs, move_src_out, move_dst_out, page_map_out, counts_out, status=None,
+                       stream=None):
+    """Live pages to the low indices; move_src_out, move_dst_out int32 [max(1, pages // 2)] for spec_cache_copy."""
+    B, pages = page_table.shape[0], page_refs.numel()
+    table, max_pages = _table(page_table, B)
+    cap = max(1, pages // 2)
+    code = library().spec_cache_compact(
+        table, _ints(page_refs, 1, "page_refs"), B, max_pages, pages, _ints(move_src_out, cap, "move_src_out"),
+        _ints(move_dst_out, cap, "move_dst_out"), _ints(page_map_out, pages, "page_map_out"),
+        _ints(counts_out, 2, "counts_out"), _ptr(status), _stream(stream))
+    _check(code, "spec_cache_compact")
 
 
 def spec_check_bounded_wait(status):

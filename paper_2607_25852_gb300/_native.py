@@ -12,6 +12,7 @@ LIBRARY = os.path.join(HERE, "libspec.so")
 _P = ctypes.c_void_p
 _I = ctypes.c_int
 _SZ = ctypes.c_size_t
+_L = ctypes.c_int64
 
 # name -> (restype, argtypes); the exported surface of include/spec.h
 SIGNATURES = {
@@ -48,7 +49,25 @@ SIGNATURES = {
     "spec_shard_sample": (_I, [_P, _I, _P, _I, _P, _I, _I, _I, _I, _I, ctypes.c_float, _P, _P, _P,
                                _P, _P, _SZ, _P]),
     "spec_shard_finish": (_I, [_P, _I, _P, _I, _I, _I, ctypes.c_float, _P, _P, _P, _P, _P, _P]),
+    "spec_attend_workspace": (_SZ, [_I, _I, _I, _I, _I, _I]),
+    "spec_attend": (_I, [_P, _L, _I, _P, _I, _P, _P, _P, _P, _I, _I, _I, ctypes.c_float, _I, _I, _P, _P, _P, _P, _SZ,
+                         _P]),
+    "spec_cache_append": (_I, [_P, _I, _P, _L, _P, _L, _P, _P, _P, _P, _I, _I, _I, _P, _P]),
+    "spec_cache_fork": (_I, [_P, _P, _P, _I, _I, _I, _I, _P, _P, _P, _P]),
+    "spec_cache_workspace": (_SZ, [_I, _I, _I]),
+    "spec_cache_reserve": (_I, [_P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "spec_cache_copy": (_I, [_P, _P, _P, _P, _I, _P, _P]),
+    "spec_cache_release": (_I, [_P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _P, _P]),
+    "spec_cache_compact": (_I, [_P, _P, _I, _I, _I, _P, _P, _P, _P, _P, _P]),
 }
+
+
+class Cache(ctypes.Structure):
+    """struct spec_cache of include/spec.h."""
+    _fields_ = [("k", _P), ("v", _P)] + [
+        (n, ctypes.c_int32) for n in ("dtype", "layers", "pages", "page_size", "kv_heads", "head_dim")] + [
+        (n, _L) for n in ("layer_stride", "page_stride", "token_stride", "head_stride")]
+
 
 _lib = None
 

@@ -1,0 +1,313 @@
+// attend.cuh -- how spec_attend divides its work, and how a divided item is
+// joined (shared by its kernels).
+//
+// An item is one key-value head of one request with up to NT of its (row,
+// query head) columns; it is done in tiles of TT positions.  The lengths are
+// on the device, so the division is too: the tiles of all items, one after
+// another, are cut into equal ranges, one per CTA of a persistent grid.  A
+// CTA's range covers whole items and at most two parts of items (its first
+// and its last), so a fixed workspace of two partial results per CTA serves
+// any batch, a single long request fills the GPU, and ragged batches balance.
+// The last CTA to finish a part of an item adds the parts up, in CTA order.
+#pragma once
+
+#include "paged.cuh"
+
+namespace spec {
+
+constexpr int kAttendMaxCtas = 160;  // partial results in the workspace: two per CTA
+
+struct AttendLaunch {
+  const void* q;
+  int64_t q_row;  // elements between rows
+  const char *k, *v;  // of the layer
+  int64_t page_b, token_b, head_b;
+  int pages, page_size, max_pages;
+  int Hq, Hkv, G, D;
+  const int32_t* table;
+  RowLayout rows;
+  float c2;    // scale * log2(e)
+  int window, sinks;
+  void* out;
+  float* lse;
+  int32_t* status;
+  float* part;        // [2 * ctas][NT][D] sums relative to the part's maximum
+  float2* part_stat;  // [2 * ctas][NT] (maximum in log2 units, sum)
+  uint32_t* arrived;  // [ctas], zero between calls
+  int ctas, min_tiles;
+};
+
+// The tiles of positions that rows at positions p_first..p_last see: the
+// sinks' (ns tiles from 0), then the window's from tile w0.  A request that
+// sees nothing has one (masked) tile, so that its rows are written.
+struct ItemTiles {
+  int ns, w0, count;
+};
+template <int TT>
+__device__ __forceinline__ ItemTiles item_tiles(const AttendLaunch& a, int p_first, int p_last) {
+  ItemTiles t{0, 0, 1};
+  if (p_last < 0) return t;
+  if (a.window > 0 && p_first >= a.window) {
+    const int lo = p_first - a.window + 1;
+    t.w0 = lo / TT;
+    const int sink_end = a.sinks < lo ? a.sinks : lo;
+    t.ns = (sink_end + TT - 1) / TT;
+    if (t.ns > t.w0) t.ns = t.w0;
+  }
+  t.count = t.ns + p_last / TT - t.w0 + 1;
+  return t;
+}
+template <int TT>
+__device__ __forceinline__ int tile_start(const ItemTiles& t, int x) {
+  return (x < t.ns ? x : t.w0 + x - t.ns) * TT;
+}
+
+constexpr int kNowhere = -(1 << 30);  // the position of rows that see nothing
+
+// A request's rows as spec_attend takes them: p is kNowhere where its rows see
+// nothing (idle, or positions past the table), count 0 where nothing of it
+// is written.
+struct AttendRows {
+  int row0, count, p;
+  bool bad;
+};
+__device__ __forceinline__ AttendRows attend_rows(const AttendLaunch& a, int i) {
+  const RequestRows r = request_rows(a.rows, i);
+  AttendRows o{r.row0, r.ok ? r.count : 0, kNowhere, !r.ok};
+  if (r.ok && r.p > -(int64_t)(1 << 20)) {
+    if (r.p + r.count > (int64_t)a.max_pages * a.page_size) o.bad = true;
+    else o.p = (int)r.p;
+  }
+  return o;
+}
+
+// Tiles of one key-value head of a request, over its column tiles of NT.
+template <int NT, int TT>
+__device__ __forceinline__ int head_units(const AttendLaunch& a, const AttendRows& r) {
+  const int cols = r.count * a.G;
+  int n = 0;
+  for (int c0 = 0; c0 < cols; c0 += NT) {
+    const int c1 = min(cols, c0 + NT) - 1;
+    n += item_tiles<TT>(a, r.p + c0 / a.G, r.p + c1 / a.G).count;
+  }
+  return n;
+}
+
+// A CTA's share: units [u0, u1) of `units`, starting in request `request`
+// whose first unit is `base`.
+struct Share {
+  long long units, u0, u1, base;
+  int ctas, request;
+};
+
+// All threads of the CTA (a multiple of 32, at most 1024).
+template <int NT, int TT>
+__device__ void find_share(const AttendLaunch& a, Share* sh, long long* sums) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  const int B = a.rows.B, step = blockDim.x;
+  if (threadIdx.x == 0) sh->request = -1;
+  // pass 0: the total; pass 1: the request in which this CTA's range starts.
+  // A batch of at most one request per thread does both with one scan.
+  long long carry = 0;
+  const int passes = B <= step ? 1 : 2;
+  for (int pass = 0; pass < passes; ++pass) {
+    carry = 0;
+    for (int i0 = 0; i0 < B; i0 += step) {
+      const int i = i0 + threadIdx.x;
+      long long mine = 0;
+      if (i < B) {
+        const AttendRows r = attend_rows(a, i);
+        mine = (long long)head_units<NT, TT>(a, r) * a.Hkv;
+        if (r.bad && pass == 0 && blockIdx.x == 0) report(a.status, SPEC_ERR_BAD_INPUT);
+      }
+      long long incl = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long y = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+        if (lane >= o) incl += y;
+      }
+      if (lane == 31) sums[warp] = incl;
+      __syncthreads();
+      long long before = carry, total = carry;
+      for (int w = 0; w < warps; ++w) {
+        if (w < warp) before += sums[w];
+        total += sums[w];
+      }
+      incl += before;
+      carry = total;
+      __syncthreads();
+      if (pass == passes - 1) {
+        if (passes == 1 && threadIdx.x == 0) {
+          sh->units = total;
+          const long long most = (total + a.min_tiles - 1) / a.min_tiles;
+          sh->ctas = (int)(most < a.ctas ? most : a.ctas);
+          const int g = blockIdx.x;
+          sh->u0 = g < sh->ctas ? g * total / sh->ctas : 0;
+          sh->u1 = g < sh->ctas ? (g + 1) * total / sh->ctas : 0;
+        }
+        __syncthreads();
+        if (mine > 0 && incl - mine <= sh->u0 && sh->u0 < incl) {
+          sh->request = i;
+          sh->base = incl - mine;
+        }
+      }
+    }
+    if (passes == 2 && pass == 0) {
+      if (threadIdx.x == 0) {
+        sh->units = carry;
+        const long long most = (carry + a.min_tiles - 1) / a.min_tiles;
+        sh->ctas = (int)(most < a.ctas ? most : a.ctas);
+        const int g = blockIdx.x;
+        sh->u0 = g < sh->ctas ? g * carry / sh->ctas : 0;
+        sh->u1 = g < sh->ctas ? (g + 1) * carry / sh->ctas : 0;
+      }
+      __syncthreads();
+    }
+  }
+  __syncthreads();
+}
+
+// A run of tiles of one item.
+struct Segment {
+  int request, head;   // key-value head
+  int row0;            // packed row of the request's first row
+  int col0, cols;      // columns (row, query head) of the item: col0 .. col0 + cols - 1
+  int p;               // position of the request's first row
+  ItemTiles tiles;
+  int tile0, ntiles;   // the run
+  int slot;            // where its partial result goes; -1: it is the whole item
+  int first_cta, parts;
+};
+
+// Walks the segments of a CTA's share, one thread.
+template <int NT, int TT>
+struct Walk {
+  const AttendLaunch& a;
+  const Share& sh;
+  long long u, base;  // next unit; first unit of the item's request
+  int i, h, c0;
+  AttendRows r;
+  long long item;     // first unit of the item (i, h, c0)
+  ItemTiles t;
+
+  __device__ Walk(const AttendLaunch& a_, const Share& s_) : a(a_), sh(s_), u(s_.u0), i(s_.request) {
+    if (u >= sh.u1) return;
+    r = attend_rows(a, i);
+    const int per = head_units<NT, TT>(a, r);
+    h = (int)((u - sh.base) / per);
+    item = sh.base + (long long)h * per;
+    c0 = 0;
+    set_tiles();
+    while (item + t.count <= u) {
+      item += t.count;
+      c0 += NT;
+      set_tiles();
+    }
+  }
+  __device__ __forceinline__ void set_tiles() {
+    const int c1 = min(r.count * a.G, c0 + NT) - 1;
+    t = item_tiles<TT>(a, r.p + c0 / a.G, r.p + c1 / a.G);
+  }
+  // The CTA whose range holds unit x.
+  __device__ __forceinline__ int owner(long long x) const { return (int)(((x + 1) * sh.ctas - 1) / sh.units); }
+
+  __device__ bool next(Segment* s) {
+    if (u >= sh.u1) return false;
+    s->request = i;
+    s->head = h;
+    s->row0 = r.row0;
+    s->col0 = c0;
+    s->cols = min(r.count * a.G, c0 + NT) - c0;
+    s->p = r.p;
+    s->tiles = t;
+    s->tile0 = (int)(u - item);
+    const long long end = item + t.count;
+    s->ntiles = (int)((end < sh.u1 ? end : sh.u1) - u);
+    s->slot = -1;
+    s->first_cta = blockIdx.x;
+    s->parts = 1;
+    if (s->ntiles < t.count) {
+      const int f = owner(item), l = owner(end - 1);
+      s->first_cta = f;
+      s->parts = l - f + 1;
+      s->slot = 2 * (int)blockIdx.x + ((int)blockIdx.x == f ? 1 : 0);
+    }
+    u += s->ntiles;
+    if (u < sh.u1) {  // the next item
+      item = end;
+      c0 += NT;
+      if (c0 >= r.count * a.G) {
+        c0 = 0;
+        if (++h == a.Hkv) {
+          h = 0;
+          do {
+            r = attend_rows(a, ++i);
+          } while (r.count == 0);
+        }
+      }
+      set_tiles();
+    }
+    return true;
+  }
+};
+
+// Slot of the x-th part of a divided item: the first CTA's part is the tail of
+// its range, every other's the head.
+__device__ __forceinline__ int part_slot(const Segment& s, int x) { return 2 * (s.first_cta + x) + (x == 0 ? 1 : 0); }
+
+// Where column c of a segment goes: packed row * Hq + query head.
+__device__ __forceinline__ long long out_index(const AttendLaunch& a, const Segment& s, int c) {
+  const int col = s.col0 + c, j = col / a.G;
+  return (long long)(s.row0 + j) * a.Hq + s.head * a.G + (col - j * a.G);
+}
+
+constexpr float kLn2 = 0.69314718055994531f;
+
+// A row's log-sum-exp from its maximum (log2 units) and sum; -inf where it saw
+// nothing.
+__device__ __forceinline__ float row_lse(float m2, float l) { return l == 0.0f ? -INFINITY : (m2 + log2f(l)) * kLn2; }
+
+template <typename T>
+__device__ __forceinline__ T from_float(float x);
+template <>
+__device__ __forceinline__ float from_float<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16(x); }
+
+// The weight of a part in its row's sum.
+__device__ __forceinline__ float part_weight(float2 st, float m) {
+  return st.x == -INFINITY ? 0.0f : exp2f(st.x - m);
+}
+
+// Adds the parts of a divided item up: `threads` threads, `tid` of them, all of
+// them past the arrival of the last part.  Two consecutive columns d per step.
+template <int NT, typename T>
+__device__ void join_parts(const AttendLaunch& a, const Segment& s, int tid, int threads) {
+  const int half = a.D / 2;
+  for (int e = tid; e < s.cols * half; e += threads) {
+    const int c = e / half, d = 2 * (e - c * half);
+    float m = -INFINITY;
+    for (int x = 0; x < s.parts; ++x) m = fmaxf(m, __ldcg(&a.part_stat[(size_t)part_slot(s, x) * NT + c].x));
+    float l = 0.0f, o0 = 0.0f, o1 = 0.0f;
+    for (int x = 0; x < s.parts; ++x) {
+      const size_t at = (size_t)part_slot(s, x) * NT + c;
+      const float2 st = __ldcg(a.part_stat + at);
+      const float2 o = __ldcg(reinterpret_cast<const float2*>(a.part + at * a.D + d));
+      const float w = part_weight(st, m);
+      l = fmaf(st.y, w, l);
+      // a part that saw nothing adds nothing
+      if (w != 0.0f) {
+        o0 = fmaf(o.x, w, o0);
+        o1 = fmaf(o.y, w, o1);
+      }
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const long long at = out_index(a, s, c);
+    T* out = static_cast<T*>(a.out) + at * a.D + d;
+    out[0] = from_float<T>(o0 * inv);
+    out[1] = from_float<T>(o1 * inv);
+    if (d == 0 && a.lse) a.lse[at] = row_lse(m, l);
+  }
+}
+
+}  // namespace spec
