@@ -563,8 +563,8 @@ typedef struct spec_cache {
  * are read from the cache (spec_cache_append comes first).  Keys and values
  * of invisible positions do not reach the result, whatever they hold.
  * Sums are held in fp32; with a bf16 cache of head_dim 64 or 128 the products
- * run on the tensor cores, the weights exp(x - m) rounded to bf16 for the
- * second one (the sum in the denominator is taken before that rounding).
+ * run on the tensor cores, with each weight exp(x - m) as a sum of two bf16
+ * numbers (2^-17 relative) in the second one.
  * The result does not depend on the run: partial results of a request that
  * is split over CTAs are joined in a fixed order.
  * Arguments

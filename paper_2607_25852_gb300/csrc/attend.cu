@@ -14,6 +14,7 @@
 #include <algorithm>
 
 #include "attend.cuh"
+#include "attend_tc.cuh"
 #include "tensor_core.cuh"
 
 namespace spec {
@@ -68,8 +69,8 @@ __global__ void __launch_bounds__(kGenThreads, 1) attend_general_kernel(const At
   float* sS = sQ + kGenCols * a.D;  // [col][token]
 
   pdl_wait_prerequisites();
-  find_share<kGenCols, kGenTile>(a, &share, sums);
-  Walk<kGenCols, kGenTile> walk(a, share);
+  find_share<kGenTile>(a, &share, sums);
+  Walk<kGenTile> walk(a, share);
   const int vecs = a.D * (int)sizeof(T) / 16;
   // outputs of a thread: 4 consecutive d of up to 4 columns
   const int dv = a.D / 4;
@@ -262,7 +263,7 @@ __global__ void __launch_bounds__(kGenThreads, 1) attend_general_kernel(const At
       __syncthreads();
       if (last) {
         __threadfence();
-        join_parts<kGenCols, T>(a, s, tid, kGenThreads);
+        join_parts<T>(a, s, tid, kGenThreads);
       }
     }
     __syncthreads();
@@ -272,21 +273,19 @@ __global__ void __launch_bounds__(kGenThreads, 1) attend_general_kernel(const At
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
-// Columns per item of the kernel that serves a shape.
-static int attend_columns(int, int, int, int) { return kGenCols; }
-
 struct AttendGeometry {
-  int NT;
-  size_t stat_off, arrived_off, bytes;
+  int ct;  // columns per item, the most of the kernels that may serve the shape
+  size_t part_off, stat_off, bytes;
 };
 
+// The counters come first, so that their place does not depend on the kernel.
 static AttendGeometry attend_geometry(int cols, int D, int dtype) {
   AttendGeometry g{};
-  g.NT = attend_columns(cols, D, dtype, 0);
+  g.ct = dtype == SPEC_BF16 ? std::max(kGenCols, attend_tc_columns(cols)) : kGenCols;
   const size_t slots = 2 * kAttendMaxCtas;
-  g.stat_off = (slots * g.NT * D * 4 + 255) / 256 * 256;
-  g.arrived_off = g.stat_off + (slots * g.NT * 8 + 255) / 256 * 256;
-  g.bytes = g.arrived_off + (kAttendMaxCtas * 4 + 255) / 256 * 256;
+  g.part_off = (kAttendMaxCtas * 4 + 255) / 256 * 256;
+  g.stat_off = g.part_off + (slots * g.ct * D * 4 + 255) / 256 * 256;
+  g.bytes = g.stat_off + (slots * g.ct * 8 + 255) / 256 * 256;
   return g;
 }
 
@@ -357,12 +356,18 @@ extern "C" int spec_attend(const void* q, int64_t q_row_stride, int q_heads, con
   a.lse = lse_out;
   a.status = status;
   char* base = static_cast<char*>(ws);
-  a.part = reinterpret_cast<float*>(base);
+  a.arrived = reinterpret_cast<uint32_t*>(base);
+  a.part = reinterpret_cast<float*>(base + g.part_off);
   a.part_stat = reinterpret_cast<float2*>(base + g.stat_off);
-  a.arrived = reinterpret_cast<uint32_t*>(base + g.arrived_off);
   a.ctas = std::min(device_sms(), kAttendMaxCtas);
   a.min_tiles = 1;
-  const cudaError_t err = cache->dtype == SPEC_F32 ? launch_general<float>(a, stream)
-                                                   : launch_general<__nv_bfloat16>(a, stream);
+  cudaError_t err;
+  if (attend_tc_serves(a.D, cache->dtype, a.page_size, a.head_b, a.token_b, a.page_b)) {
+    a.ct = attend_tc_columns((K + 1) * a.G);
+    err = launch_attend_tc(a, stream);
+  } else {
+    a.ct = kGenCols;
+    err = cache->dtype == SPEC_F32 ? launch_general<float>(a, stream) : launch_general<__nv_bfloat16>(a, stream);
+  }
   return err == cudaSuccess && cudaGetLastError() == cudaSuccess ? SPEC_OK : SPEC_ERR_CUDA;
 }

@@ -1,7 +1,7 @@
 // attend.cuh -- how spec_attend divides its work, and how a divided item is
 // joined (shared by its kernels).
 //
-// An item is one key-value head of one request with up to NT of its (row,
+// An item is one key-value head of one request with up to ct of its (row,
 // query head) columns; it is done in tiles of TT positions.  The lengths are
 // on the device, so the division is too: the tiles of all items, one after
 // another, are cut into equal ranges, one per CTA of a persistent grid.  A
@@ -31,8 +31,9 @@ struct AttendLaunch {
   void* out;
   float* lse;
   int32_t* status;
-  float* part;        // [2 * ctas][NT][D] sums relative to the part's maximum
-  float2* part_stat;  // [2 * ctas][NT] (maximum in log2 units, sum)
+  int ct;             // columns per item
+  float* part;        // [2 * ctas][ct][D] sums relative to the part's maximum
+  float2* part_stat;  // [2 * ctas][ct] (maximum in log2 units, sum)
   uint32_t* arrived;  // [ctas], zero between calls
   int ctas, min_tiles;
 };
@@ -81,13 +82,13 @@ __device__ __forceinline__ AttendRows attend_rows(const AttendLaunch& a, int i) 
   return o;
 }
 
-// Tiles of one key-value head of a request, over its column tiles of NT.
-template <int NT, int TT>
+// Tiles of one key-value head of a request, over its column tiles.
+template <int TT>
 __device__ __forceinline__ int head_units(const AttendLaunch& a, const AttendRows& r) {
   const int cols = r.count * a.G;
   int n = 0;
-  for (int c0 = 0; c0 < cols; c0 += NT) {
-    const int c1 = min(cols, c0 + NT) - 1;
+  for (int c0 = 0; c0 < cols; c0 += a.ct) {
+    const int c1 = min(cols, c0 + a.ct) - 1;
     n += item_tiles<TT>(a, r.p + c0 / a.G, r.p + c1 / a.G).count;
   }
   return n;
@@ -101,7 +102,7 @@ struct Share {
 };
 
 // All threads of the CTA (a multiple of 32, at most 1024).
-template <int NT, int TT>
+template <int TT>
 __device__ void find_share(const AttendLaunch& a, Share* sh, long long* sums) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
   const int B = a.rows.B, step = blockDim.x;
@@ -117,7 +118,7 @@ __device__ void find_share(const AttendLaunch& a, Share* sh, long long* sums) {
       long long mine = 0;
       if (i < B) {
         const AttendRows r = attend_rows(a, i);
-        mine = (long long)head_units<NT, TT>(a, r) * a.Hkv;
+        mine = (long long)head_units<TT>(a, r) * a.Hkv;
         if (r.bad && pass == 0 && blockIdx.x == 0) report(a.status, SPEC_ERR_BAD_INPUT);
       }
       long long incl = mine;
@@ -180,7 +181,7 @@ struct Segment {
 };
 
 // Walks the segments of a CTA's share, one thread.
-template <int NT, int TT>
+template <int TT>
 struct Walk {
   const AttendLaunch& a;
   const Share& sh;
@@ -193,19 +194,19 @@ struct Walk {
   __device__ Walk(const AttendLaunch& a_, const Share& s_) : a(a_), sh(s_), u(s_.u0), i(s_.request) {
     if (u >= sh.u1) return;
     r = attend_rows(a, i);
-    const int per = head_units<NT, TT>(a, r);
+    const int per = head_units<TT>(a, r);
     h = (int)((u - sh.base) / per);
     item = sh.base + (long long)h * per;
     c0 = 0;
     set_tiles();
     while (item + t.count <= u) {
       item += t.count;
-      c0 += NT;
+      c0 += a.ct;
       set_tiles();
     }
   }
   __device__ __forceinline__ void set_tiles() {
-    const int c1 = min(r.count * a.G, c0 + NT) - 1;
+    const int c1 = min(r.count * a.G, c0 + a.ct) - 1;
     t = item_tiles<TT>(a, r.p + c0 / a.G, r.p + c1 / a.G);
   }
   // The CTA whose range holds unit x.
@@ -217,7 +218,7 @@ struct Walk {
     s->head = h;
     s->row0 = r.row0;
     s->col0 = c0;
-    s->cols = min(r.count * a.G, c0 + NT) - c0;
+    s->cols = min(r.count * a.G, c0 + a.ct) - c0;
     s->p = r.p;
     s->tiles = t;
     s->tile0 = (int)(u - item);
@@ -235,7 +236,7 @@ struct Walk {
     u += s->ntiles;
     if (u < sh.u1) {  // the next item
       item = end;
-      c0 += NT;
+      c0 += a.ct;
       if (c0 >= r.count * a.G) {
         c0 = 0;
         if (++h == a.Hkv) {
@@ -281,16 +282,16 @@ __device__ __forceinline__ float part_weight(float2 st, float m) {
 
 // Adds the parts of a divided item up: `threads` threads, `tid` of them, all of
 // them past the arrival of the last part.  Two consecutive columns d per step.
-template <int NT, typename T>
+template <typename T>
 __device__ void join_parts(const AttendLaunch& a, const Segment& s, int tid, int threads) {
   const int half = a.D / 2;
   for (int e = tid; e < s.cols * half; e += threads) {
     const int c = e / half, d = 2 * (e - c * half);
     float m = -INFINITY;
-    for (int x = 0; x < s.parts; ++x) m = fmaxf(m, __ldcg(&a.part_stat[(size_t)part_slot(s, x) * NT + c].x));
+    for (int x = 0; x < s.parts; ++x) m = fmaxf(m, __ldcg(&a.part_stat[(size_t)part_slot(s, x) * a.ct + c].x));
     float l = 0.0f, o0 = 0.0f, o1 = 0.0f;
     for (int x = 0; x < s.parts; ++x) {
-      const size_t at = (size_t)part_slot(s, x) * NT + c;
+      const size_t at = (size_t)part_slot(s, x) * a.ct + c;
       const float2 st = __ldcg(a.part_stat + at);
       const float2 o = __ldcg(reinterpret_cast<const float2*>(a.part + at * a.D + d));
       const float w = part_weight(st, m);

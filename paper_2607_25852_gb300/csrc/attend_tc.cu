@@ -1,0 +1,840 @@
+// attend_tc.cu -- spec_attend on the 5th-generation tensor cores: bf16 caches
+// of head dimension 64 or 128 whose pages are a multiple of 8 positions.
+//
+// The few columns (row, query head) that share a key-value head are the N
+// dimension of both products, so their cost follows their number, and the
+// positions of the cache fill the 128 rows of the tensor cores:
+//   S^T [128 positions x N] = K Q^T        K from shared memory as it lies
+//   O^T [D x N]            += V^T P^T      V as it lies, read transposed
+// S^T and O^T live in TMEM, a position (or a d) per lane, a column per TMEM
+// column.  A thread of the softmax holds one position's scores: the weights
+// are elementwise, and the maximum over positions is looked at only for a
+// bound: as long as no score exceeds its column's reference maximum by more
+// than 2^8 (in the exponent's base), the old reference serves (weights stay
+// below 2^8, exact in range and in relative precision), so most tiles need one
+// vote and no reduction, no rescaling of O^T and no exchange between warps.
+// The sum of the weights is kept per thread, in fp32, and reduced once per
+// item.  For the second product a weight is the sum of two bf16 numbers, its
+// upper 8 bits and the rounded rest (2^-17 relative): one bf16 number would
+// put an error of the size of the result's own rounding on top of it, and the
+// second product is a small part of the time while the cache is read.
+//
+// Warps: 0 loads pages by TMA into a ring of K and V tiles; 1 issues the MMAs
+// (the scores of tile t + 1 before the second product of tile t); 2 loads
+// queries; 3 walks the CTA's share of the work; the rest are the softmax, one
+// TMEM lane quarter per warp, in one or two sets that halve the columns.
+//
+// Positions that no row sees must not reach the result whatever they hold: a
+// weight of 0 does not cancel an infinite or NaN value, so in tiles at an edge
+// of the mask such values are cleared in shared memory before the product
+// (a value that some rows see and others do not is added back, row by row, in
+// the item's epilogue: only if it is not finite).
+//
+// Every mbarrier wait is bounded (about a second): a wait that gives up sets
+// SPEC_ERR_TIMEOUT and the kernel ends; the softmax warps, which meet at
+// barriers, leave together by a vote.
+#include <algorithm>
+
+#include "attend.cuh"
+#include "attend_tc.cuh"
+#include "tensor_core.cuh"
+
+namespace spec {
+
+namespace {
+
+constexpr int kTile = 128;        // positions per tile: the M of S^T
+constexpr int kHalfBytes = kTile * 128;  // 64 elements of 128 positions
+constexpr int kMaxSlots = 12;
+constexpr int kSegRing = 4;
+constexpr int kBadRing = 32;      // tiles between the loader and the softmax: fewer than 2 kMaxSlots
+constexpr float kNoMax = -3.0e38f;  // the reference of a column that has seen nothing
+constexpr float kGrowth = 8.0f;   // log2 of how far weights may exceed 1
+
+struct TcPlan {
+  int chunk, nchunk;    // positions per TMA box, boxes per tile and half
+  int slots;            // ring slots (a K or V tile each)
+  int q_off, p_off;     // bytes from the start of shared memory
+  int qb, pb;           // buffers of Q and P
+};
+
+// ---- PTX ----
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w,
+                                            uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], "
+      "[%6];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
+      : "memory");
+}
+__device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void named_sync(int id, int threads) {
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+__device__ __forceinline__ bool named_or(int id, int threads, bool x) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %1, 0;\n\t"
+      "bar.red.or.pred q, %2, %3, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(r)
+      : "r"((uint32_t)x), "r"(id), "r"(threads)
+      : "memory");
+  return r != 0;
+}
+__device__ __forceinline__ float warp_max(float x) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ void tmem_ld8(uint32_t addr, float* v) {
+  uint32_t r[8];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+      : "r"(addr)
+      : "memory");
+#pragma unroll
+  for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(r[k]);
+}
+__device__ __forceinline__ void tmem_ld24(uint32_t addr, float* v) {
+  uint32_t r[24];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%24];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%16,%17,%18,%19,%20,%21,%22,%23}, [%25];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23])
+      : "r"(addr), "r"(addr + 16)
+      : "memory");
+#pragma unroll
+  for (int k = 0; k < 24; ++k) v[k] = __uint_as_float(r[k]);
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, float* v) {
+  uint32_t r[16];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(addr)
+      : "memory");
+#pragma unroll
+  for (int k = 0; k < 16; ++k) v[k] = __uint_as_float(r[k]);
+}
+__device__ __forceinline__ void tmem_st8(uint32_t addr, const float* v) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(addr),
+               "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])),
+               "r"(__float_as_uint(v[3])), "r"(__float_as_uint(v[4])), "r"(__float_as_uint(v[5])),
+               "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7]))
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// V as the A operand, read transposed (its d is contiguous): 128-byte swizzled
+// atoms of 64 d x 8 positions; `lbo` bytes to the next 64 d, 1024 to the next
+// 8 positions.
+__device__ __forceinline__ uint64_t desc_v(uint32_t saddr, uint32_t lbo) {
+  return (uint64_t)((saddr >> 4) & 0x3FFFu) | (uint64_t)(lbo >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 |
+         (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+// P^T as the B operand, a position's columns contiguous: 32-byte swizzled atoms
+// of 16 columns x 8 positions; 4096 bytes to the next 16 columns, 256 to the
+// next 8 positions.
+constexpr int kPChunkBytes = kTile * 32;
+__device__ __forceinline__ uint64_t desc_p(uint32_t saddr) {
+  return (uint64_t)((saddr >> 4) & 0x3FFFu) | (uint64_t)(kPChunkBytes >> 4) << 16 | (uint64_t)(256 >> 4) << 32 |
+         (uint64_t)1 << 46 | (uint64_t)6 << 61;
+}
+constexpr uint32_t kTransposeA = 1u << 15, kTransposeB = 1u << 16;
+
+// Two weights as pairs of bf16 numbers: their upper halves, and the rest rounded.
+__device__ __forceinline__ void split_bf16(float x, float y, uint32_t* hi, uint32_t* lo) {
+  const uint32_t xb = __float_as_uint(x), yb = __float_as_uint(y);
+  *hi = __byte_perm(xb, yb, 0x7632);
+  const float xr = x - __uint_as_float(xb & 0xFFFF0000u), yr = y - __uint_as_float(yb & 0xFFFF0000u);
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(*lo) : "f"(yr), "f"(xr));
+}
+__device__ __forceinline__ void st_shared16(uint32_t at, const uint32_t (&w)[4]) {
+  asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+}
+__device__ __forceinline__ bool bf16_not_finite(uint32_t h) { return (h & 0x7F80u) == 0x7F80u; }
+
+// Column sums over a warp's lanes of 8 values per lane: afterwards lanes 4k
+// hold the sum of column k.
+__device__ __forceinline__ float column_sum8(float (&v)[8], int lane) {
+#pragma unroll
+  for (int n = 8, o = 16; n > 1; n >>= 1, o >>= 1) {
+    const bool hi = (lane & o) != 0;
+#pragma unroll
+    for (int j = 0; j < n / 2; ++j) {
+      const float send = hi ? v[j] : v[j + n / 2];
+      const float keep = hi ? v[j + n / 2] : v[j];
+      v[j] = keep + __shfl_xor_sync(0xFFFFFFFFu, send, o);
+    }
+  }
+  v[0] += __shfl_xor_sync(0xFFFFFFFFu, v[0], 2);
+  v[0] += __shfl_xor_sync(0xFFFFFFFFu, v[0], 1);
+  return v[0];  // column 4 * bit4 + 2 * bit3 + bit2 = lane / 4
+}
+
+// ---------------------------------------------------------------------------
+// D: head dimension.  CG: groups of 8 columns per softmax thread.  H: sets of
+// four softmax warps (they split the columns).
+// ---------------------------------------------------------------------------
+template <int D, int CG, int H>
+__global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
+    attend_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                     const __grid_constant__ AttendLaunch a, const __grid_constant__ TcPlan t) {
+  constexpr int kCols = CG * 8 * H;             // most columns of an item
+  constexpr int kSlotBytes = (D / 64) * kHalfBytes;
+  constexpr int kTmemStep = (kCols + 31) / 32 * 32;
+  constexpr int kTmemCols = 3 * kTmemStep <= 128 ? 128 : 3 * kTmemStep <= 256 ? 256 : 512;
+  static_assert(3 * kTmemStep <= kTmemCols, "two score buffers and the output fit TMEM");
+  constexpr int kSoftThreads = 128 * H;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  __shared__ uint64_t full[kMaxSlots], empty[kMaxSlots], s_full[2], s_free[2], p_full[2], p_free[2], o_free, drained, q_full[2],
+      q_free[2], seg_full[kSegRing], seg_free[kSegRing];
+  __shared__ Segment segs[kSegRing];
+  __shared__ Share share;
+  __shared__ long long sums[32];
+  __shared__ int tile_bad[kBadRing];
+  __shared__ __align__(16) float sM[kCols], red[4][kCols];
+  __shared__ int sRow[kCols];        // position of the column's row
+  __shared__ long long sOut[kCols];  // where the column goes
+  __shared__ uint32_t tmem_sh;
+  __shared__ int abort_flag, poison, last_sh;
+  volatile int& aborted = abort_flag;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+  if (tid == 0) {
+    for (int k = 0; k < t.slots; ++k) {
+      mbar_init(&full[k], 1);
+      mbar_init(&empty[k], 1);
+    }
+    for (int k = 0; k < 2; ++k) {
+      mbar_init(&s_full[k], 1);
+      mbar_init(&s_free[k], 4 * H);
+      mbar_init(&p_full[k], 4 * H);
+      mbar_init(&p_free[k], 1);
+      mbar_init(&q_full[k], 1);
+      mbar_init(&q_free[k], 1);
+    }
+    mbar_init(&o_free, 4 * H);
+    mbar_init(&drained, 1);
+    for (int k = 0; k < kSegRing; ++k) {
+      mbar_init(&seg_full[k], 1);
+      mbar_init(&seg_free[k], 3 + 4 * H);
+    }
+    abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_sh)),
+                 "r"(kTmemCols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  if (warp == 0 && lane == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmK)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmV)) : "memory");
+  }
+  pdl_wait_prerequisites();
+  tc_fence_before();
+  find_share<kTile>(a, &share, sums);  // ends with a barrier
+  tc_fence_after();
+  const uint32_t tmem = tmem_sh;
+  const uint32_t tS[2] = {tmem, tmem + kTmemStep}, tO = tmem + 2 * kTmemStep;
+  const uint32_t ring = smem_u32(smem);
+
+  // The next segment of the share, for a reading warp (n counts segments).
+  auto take = [&](int n, Segment* s) -> bool {
+    const int k = n % kSegRing;
+    const bool ok = __all_sync(0xFFFFFFFFu, mbar_wait(&seg_full[k], (uint32_t)((n / kSegRing) & 1), a.status));
+    *s = segs[k];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&seg_free[k]);
+    return ok;
+  };
+
+  if (warp == 0) {
+    // ---- pages into the ring ----
+    const int c = lane % t.nchunk, hf = lane / t.nchunk;
+    const bool mine = hf < D / 64;
+    int tiles = 0, issued = 0;  // tiles done, ring slots filled
+    for (int n = 0;; ++n) {
+      Segment s;
+      if (!take(n, &s)) {
+        aborted = 1;
+        break;
+      }
+      if (s.request < 0) break;
+      const int p_first = s.p + s.col0 / a.G, p_last = s.p + (s.col0 + s.cols - 1) / a.G;
+      const int32_t* row = a.table + (size_t)s.request * a.max_pages;
+      // does some row see this lane's positions of tile x?
+      auto seen = [&](int x) {
+        const int pos = tile_start<kTile>(s.tiles, x) + c * t.chunk;
+        return mine && pos <= p_last && (a.window == 0 || pos + t.chunk - 1 > p_first - a.window || pos < a.sinks);
+      };
+      auto lookup = [&](int x) {
+        return __ldg(row + (tile_start<kTile>(s.tiles, x) + c * t.chunk) / a.page_size);
+      };
+      bool wanted_next = seen(s.tile0);
+      int next = wanted_next ? lookup(s.tile0) : 0;
+      bool ok = true;
+      for (int x = 0; x < s.ntiles && ok; ++x) {
+        int page = next;
+        const bool wanted = wanted_next;
+        if (x + 1 < s.ntiles) {  // the next tile's page, a tile ahead
+          wanted_next = seen(s.tile0 + x + 1);
+          next = wanted_next ? lookup(s.tile0 + x + 1) : 0;
+        }
+        const bool bad = wanted && (page < 0 || page >= a.pages);
+        const uint32_t bads = __ballot_sync(0xFFFFFFFFu, bad && hf == 0);
+        if (bad) report(a.status, SPEC_ERR_BAD_INPUT);
+        if (bad || !wanted) page = a.pages;  // past the map's last page: zeros are written, nothing is read
+        if (lane == 0) tile_bad[tiles % kBadRing] = (int)bads;
+        const int tok = (tile_start<kTile>(s.tiles, s.tile0 + x) + c * t.chunk) % a.page_size;
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+          const int u = 2 * tiles + kv, slot = u % t.slots, use = u / t.slots;
+          ok = __all_sync(0xFFFFFFFFu, !aborted && (use == 0 || mbar_wait(&empty[slot], (uint32_t)((use - 1) & 1),
+                                                                           a.status)));
+          if (!ok) break;
+          if (lane == 0) mbar_expect_tx(&full[slot], kSlotBytes);
+          __syncwarp();
+          if (mine)
+            tma_load_4d(ring + slot * kSlotBytes + hf * kHalfBytes + c * t.chunk * 128, kv ? &tmV : &tmK, hf * 64, s.head,
+                        tok, page, &full[slot]);
+          ++issued;
+        }
+        if (ok) ++tiles;
+      }
+      if (!ok) {
+        aborted = 1;
+        break;
+      }
+    }
+    // what was issued has landed before the CTA ends
+    if (aborted)
+      for (int u = max(0, issued - t.slots); u < issued; ++u)
+        mbar_wait(&full[u % t.slots], (uint32_t)((u / t.slots) & 1), a.status);
+  } else if (warp == 1) {
+    // ---- MMAs ----
+    int T = 0, prev_n = 0;
+    bool prev_first = false, ok = true;
+    uint32_t prev_idesc = 0;
+    // O^T of tile u; `first` of its segment n
+    auto second = [&](int u, bool first, int n, uint32_t idesc) -> bool {
+      const int v = 2 * u + 1, slot = v % t.slots, b = u % t.pb;
+      if (first && n > 0 && !mbar_wait(&o_free, (uint32_t)((n - 1) & 1), a.status)) return false;
+      if (!mbar_wait(&full[slot], (uint32_t)((v / t.slots) & 1), a.status)) return false;
+      if (!mbar_wait(&p_full[b], (uint32_t)((u / t.pb) & 1), a.status)) return false;
+      tc_fence_after();
+      const uint32_t va = ring + slot * kSlotBytes, p_part = (a.ct / 16) * kPChunkBytes;
+      const uint32_t pa = ring + t.p_off + b * 2 * p_part;
+      for (int kk = 0; kk < kTile / 16; ++kk) {
+        const uint64_t dv = desc_v(va + kk * 2048, D == 128 ? kHalfBytes : 0);
+        umma_bf16(tO, dv, desc_p(pa + kk * 512), idesc, first && kk == 0 ? 0u : 1u);
+        umma_bf16(tO, dv, desc_p(pa + p_part + kk * 512), idesc, 1u);
+      }
+      umma_commit(&empty[slot]);
+      umma_commit(&p_free[b]);
+      return true;
+    };
+    for (int n = 0; ok; ++n) {
+      Segment s;
+      ok = take(n, &s);
+      if (!ok || s.request < 0) break;
+      if (lane == 0) {
+        const int N = (s.cols + 15) / 16 * 16, qb = n % t.qb;
+        const uint32_t idesc_s = umma_idesc_bf16(kTile, N);
+        ok = mbar_wait(&q_full[qb], (uint32_t)((n / t.qb) & 1), a.status);
+        const uint32_t qa = ring + t.q_off + qb * a.ct * D * 2;
+        for (int x = 0; x < s.ntiles && ok && !aborted; ++x, ++T) {
+          const int u = 2 * T, slot = u % t.slots, b = T & 1;
+          ok = mbar_wait(&full[slot], (uint32_t)((u / t.slots) & 1), a.status);
+          if (ok && T >= 2) ok = mbar_wait(&s_free[b], (uint32_t)(((T >> 1) - 1) & 1), a.status);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t ka = ring + slot * kSlotBytes;
+          for (int kk = 0; kk < D / 16; ++kk)
+            umma_bf16(tS[b], umma_desc_sw128(ka + (kk >> 2) * kHalfBytes + (kk & 3) * 32),
+                      umma_desc_sw128(qa + (kk >> 2) * a.ct * 128 + (kk & 3) * 32), idesc_s, kk > 0 ? 1u : 0u);
+          umma_commit(&empty[slot]);
+          umma_commit(&s_full[b]);
+          if (x == s.ntiles - 1) umma_commit(&q_free[qb]);
+          if (T > 0) ok = second(T - 1, prev_first, prev_n, prev_idesc);
+          prev_first = x == 0;
+          prev_n = n;
+          prev_idesc = umma_idesc_bf16(kTile, N) | kTransposeA | kTransposeB;
+        }
+        if (aborted) ok = false;
+      }
+      ok = __shfl_sync(0xFFFFFFFFu, (int)ok, 0) != 0;
+    }
+    if (lane == 0) {
+      if (ok && T > 0) ok = second(T - 1, prev_first, prev_n, prev_idesc);
+      if (!ok) aborted = 1;
+      // everything issued has completed before the TMEM goes
+      umma_commit(&drained);
+      mbar_wait(&drained, 0u, a.status);
+    }
+    __syncwarp();
+  } else if (warp == 2) {
+    // ---- queries: [64-element halves][column][128 bytes], 128-byte swizzle ----
+    constexpr int kVecs = D / 8;
+    for (int n = 0;; ++n) {
+      Segment s;
+      if (!take(n, &s)) {
+        aborted = 1;
+        break;
+      }
+      if (s.request < 0 || __any_sync(0xFFFFFFFFu, aborted)) break;
+      const int b = n % t.qb;
+      if (n >= t.qb && !__all_sync(0xFFFFFFFFu, mbar_wait(&q_free[b], (uint32_t)(((n / t.qb) - 1) & 1), a.status))) {
+        aborted = 1;
+        break;
+      }
+      const int N = (s.cols + 15) / 16 * 16;
+      uint8_t* dst = smem + t.q_off + b * a.ct * D * 2;
+      const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q);
+      for (int e0 = 0; e0 < N * kVecs; e0 += 256) {  // N is a multiple of 16: whole rounds of 8 vectors a lane
+        uint4 w[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int e = e0 + 32 * k + lane, c = e / kVecs, v = e % kVecs;
+          w[k] = make_uint4(0u, 0u, 0u, 0u);
+          if (c < s.cols) {
+            const int col = s.col0 + c, j = col / a.G;
+            w[k] = __ldg(reinterpret_cast<const uint4*>(q + (int64_t)(s.row0 + j) * a.q_row +
+                                                        (int64_t)(s.head * a.G + col - j * a.G) * D) +
+                         v);
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int e = e0 + 32 * k + lane, c = e / kVecs, v = e % kVecs;
+          if (c < N)
+            *reinterpret_cast<uint4*>(dst + (v >> 3) * a.ct * 128 + c * 128 + (((v & 7) ^ (c & 7)) << 4)) = w[k];
+        }
+      }
+      proxy_fence();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&q_full[b]);
+    }
+  } else if (warp == 3) {
+    // ---- the CTA's segments ----
+    if (lane == 0) {
+      Walk<kTile> walk(a, share);
+      for (int n = 0; !aborted; ++n) {
+        const int k = n % kSegRing;
+        if (n >= kSegRing && !mbar_wait(&seg_free[k], (uint32_t)(((n / kSegRing) - 1) & 1), a.status)) {
+          aborted = 1;
+          break;
+        }
+        const bool more = walk.next(&segs[k]);
+        if (!more) segs[k].request = -1;
+        mbar_arrive(&seg_full[k]);
+        if (!more) break;
+      }
+    }
+    __syncwarp();
+  } else {
+    // ---- softmax ----
+    const int quad = warp & 3, hf = (warp - 4) >> 2;  // TMEM lanes 32 quad .. + 31; column set
+    const int st = tid - 128;                         // of kSoftThreads
+    const int tl = quad * 32 + lane;                  // this thread's position in a tile, and its d of O^T
+    const uint32_t lanes = (uint32_t)(32 * quad) << 16;
+    constexpr bool kKeep = CG <= 4;  // the scores stay in registers between the vote and the weights
+    constexpr int kStep = kKeep ? CG : 3;
+    bool failed = false;
+    int T = 0;
+    auto wait = [&](uint64_t* bar, int use) {
+      if (!failed && !__all_sync(0xFFFFFFFFu, mbar_wait(bar, (uint32_t)(use & 1), a.status))) failed = true;
+    };
+    for (int n = 0;; ++n) {
+      Segment s;
+      if (!take(n, &s)) failed = true;
+      if (named_or(1, kSoftThreads, failed)) {  // no one has left the last segment's epilogue behind
+        aborted = 1;
+        break;
+      }
+      if (s.request < 0) break;
+      const int p_first = s.p + s.col0 / a.G, p_last = s.p + (s.col0 + s.cols - 1) / a.G;
+      const int NG = (s.cols + 15) / 16 * 2;        // groups of 8 columns
+      const int gc = NG / H, gb = hf * gc;          // this set's
+      for (int c = st; c < NG * 8; c += kSoftThreads) {
+        const int cc = min(c, s.cols - 1);
+        sRow[c] = s.p + (s.col0 + cc) / a.G;
+        sOut[c] = out_index(a, s, cc);
+        sM[c] = kNoMax;
+      }
+      if (st == 0) poison = 0;
+      named_sync(1, kSoftThreads);
+      float l[CG][8];
+#pragma unroll
+      for (int g = 0; g < CG; ++g)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) l[g][j] = 0.0f;
+
+      for (int x = 0; x < s.ntiles; ++x, ++T) {
+        const int t0 = tile_start<kTile>(s.tiles, s.tile0 + x), b = T & 1, pb = T % t.pb;
+        wait(&s_full[b], T >> 1);
+        tc_fence_after();
+        const uint32_t sS = tS[b] + lanes + gb * 8;
+        const int bads = tile_bad[T % kBadRing];
+        const bool edge = !(t0 + kTile - 1 <= p_first &&
+                            (a.window == 0 || t0 > p_last - a.window || t0 + kTile <= a.sinks)) ||
+                          bads != 0;
+        const int pos = t0 + tl;
+        const bool gone = (bads >> (tl / t.chunk)) & 1;
+        float v[kStep][8];
+        // scores of groups g0 .. g0 + kStep - 1 in log2 units, -inf where masked
+        auto load = [&](int g0) {
+          if constexpr (kKeep) {
+            float w[32];
+            if constexpr (CG == 2) tmem_ld16(sS, w);
+            else tmem_ld32(sS, w);
+#pragma unroll
+            for (int g = 0; g < CG; ++g)
+#pragma unroll
+              for (int j = 0; j < 8; ++j) v[g][j] = w[8 * g + j];
+          } else {
+            tmem_ld24(sS + g0 * 8, &v[0][0]);
+          }
+        };
+        auto mask = [&](int g0) {
+          if (!edge) return;
+#pragma unroll
+          for (int g = 0; g < kStep; ++g) {
+            if (g0 + g >= gc) continue;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const int r = sRow[(gb + g0 + g) * 8 + j];
+              const bool seen = pos <= r && (a.window == 0 || pos > r - a.window || pos < a.sinks) && !gone;
+              if (!seen) v[g][j] = -INFINITY;
+            }
+          }
+        };
+        // v := v * c2 - reference
+        auto relative = [&](int g0) {
+#pragma unroll
+          for (int g = 0; g < kStep; ++g) {
+            if (g0 + g >= gc) continue;
+            const float4 m0 = *reinterpret_cast<const float4*>(sM + (gb + g0 + g) * 8);
+            const float4 m1 = *reinterpret_cast<const float4*>(sM + (gb + g0 + g) * 8 + 4);
+            v[g][0] = fmaf(v[g][0], a.c2, -m0.x);
+            v[g][1] = fmaf(v[g][1], a.c2, -m0.y);
+            v[g][2] = fmaf(v[g][2], a.c2, -m0.z);
+            v[g][3] = fmaf(v[g][3], a.c2, -m0.w);
+            v[g][4] = fmaf(v[g][4], a.c2, -m1.x);
+            v[g][5] = fmaf(v[g][5], a.c2, -m1.y);
+            v[g][6] = fmaf(v[g][6], a.c2, -m1.z);
+            v[g][7] = fmaf(v[g][7], a.c2, -m1.w);
+          }
+        };
+        // ---- does a score exceed its column's reference by too much? ----
+        bool grow = x == 0;
+        if (x > 0) {
+          float top = -INFINITY;
+#pragma unroll
+          for (int g0 = 0; g0 < CG; g0 += kStep) {
+            if (g0 >= gc) continue;
+            load(g0);
+            mask(g0);
+            relative(g0);
+#pragma unroll
+            for (int g = 0; g < kStep; ++g) {
+              if (g0 + g >= gc) continue;
+#pragma unroll
+              for (int j = 0; j < 8; ++j) top = fmaxf(top, v[g][j]);
+            }
+          }
+          grow = named_or(2 + hf, 128, top > kGrowth || failed);
+        }
+        if (grow) {
+          // new references: the columns' maxima so far
+#pragma unroll
+          for (int g0 = 0; g0 < CG; g0 += kStep) {
+            if (g0 >= gc) continue;
+            load(g0);
+            mask(g0);
+#pragma unroll
+            for (int g = 0; g < kStep; ++g) {
+              if (g0 + g >= gc) continue;
+              float mine = 0.0f;
+#pragma unroll
+              for (int j = 0; j < 8; ++j) {
+                const float r = warp_max(v[g][j]);
+                if (lane == j) mine = r * a.c2;
+              }
+              if (lane < 8) red[quad][(gb + g0 + g) * 8 + lane] = mine;
+            }
+          }
+          named_sync(2 + hf, 128);
+          if (x > 0) wait(&p_free[(T - 1) % t.pb], (T - 1) / t.pb);  // O^T is complete up to tile T - 1
+          tc_fence_after();
+#pragma unroll
+          for (int g = 0; g < CG; ++g) {
+            if (g >= gc) continue;
+            float alpha[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const int c = (gb + g) * 8 + j;
+              const float m = fmaxf(fmaxf(red[0][c], red[1][c]), fmaxf(red[2][c], red[3][c]));
+              const float old = sM[c];
+              alpha[j] = ex2_approx(old - fmaxf(old, m));
+              l[g][j] *= alpha[j];
+            }
+            if (x > 0) {
+              float o[8];
+              tmem_ld8(tO + lanes + (gb + g) * 8, o);
+#pragma unroll
+              for (int j = 0; j < 8; ++j) o[j] *= alpha[j];
+              tmem_st8(tO + lanes + (gb + g) * 8, o);
+            }
+          }
+          if (x > 0) tmem_st_wait();
+          failed = named_or(2 + hf, 128, failed);  // everyone has read the old references
+          for (int c = tl; c < gc * 8; c += 128) {
+            const int cc = gb * 8 + c;
+            sM[cc] = fmaxf(sM[cc], fmaxf(fmaxf(red[0][cc], red[1][cc]), fmaxf(red[2][cc], red[3][cc])));
+          }
+          named_sync(2 + hf, 128);
+        }
+        // ---- weights ----
+        if (T >= t.pb) wait(&p_free[pb], T / t.pb - 1);
+        const uint32_t p_part = (a.ct / 16) * kPChunkBytes;
+        const uint32_t pw = ring + t.p_off + pb * 2 * p_part + tl * 32;
+#pragma unroll
+        for (int g0 = 0; g0 < CG; g0 += kStep) {
+          if (g0 >= gc) continue;
+          if (!kKeep || grow) {
+            load(g0);
+            mask(g0);
+            relative(g0);
+          }
+#pragma unroll
+          for (int g = 0; g < kStep; ++g) {
+            if (g0 + g >= gc) continue;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              v[g][j] = ex2_approx(v[g][j]);
+              l[g0 + g][j] += v[g][j];
+            }
+            const int gg = gb + g0 + g;
+            const uint32_t at = pw + (gg >> 1) * kPChunkBytes + ((((uint32_t)gg & 1) ^ ((tl >> 2) & 1)) << 4);
+            uint32_t hi[4], lo[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) split_bf16(v[g][2 * j], v[g][2 * j + 1], &hi[j], &lo[j]);
+            st_shared16(at, hi);
+            st_shared16(at + p_part, lo);
+          }
+        }
+        if (edge && hf == 0) {
+          // ---- values that rows must not see ----
+          // seen by the last row alone or by the first alone: between the two
+          const bool any = !gone && pos <= p_last && (a.window == 0 || pos > p_first - a.window || pos < a.sinks);
+          const bool all = !gone && pos <= p_first && (a.window == 0 || pos > p_last - a.window || pos < a.sinks);
+          if (!__all_sync(0xFFFFFFFFu, all)) {
+            const int u = 2 * T + 1;
+            wait(&full[u % t.slots], u / t.slots);
+            uint8_t* row = smem + (u % t.slots) * kSlotBytes + tl * 128;
+            if (!any) {
+#pragma unroll
+              for (int k = 0; k < D / 8; ++k)
+                *reinterpret_cast<uint4*>(row + (k >> 3) * kHalfBytes + (((k & 7) ^ (tl & 7)) << 4)) =
+                    make_uint4(0u, 0u, 0u, 0u);
+            } else if (!all) {
+              for (int k = 0; k < D / 8; ++k) {
+                uint4* at = reinterpret_cast<uint4*>(row + (k >> 3) * kHalfBytes + (((k & 7) ^ (tl & 7)) << 4));
+                uint4 w = *at;
+                uint32_t e[4] = {w.x, w.y, w.z, w.w};
+                bool found = false;
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                  const bool lo = bf16_not_finite(e[y]), hi = bf16_not_finite(e[y] >> 16);
+                  found |= lo || hi;
+                  e[y] &= (lo ? 0xFFFF0000u : 0xFFFFFFFFu) & (hi ? 0x0000FFFFu : 0xFFFFFFFFu);
+                }
+                if (found) {
+                  poison = 1;
+                  *at = make_uint4(e[0], e[1], e[2], e[3]);
+                }
+              }
+            }
+          }
+        }
+        tc_fence_before();
+        proxy_fence();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(&s_free[b]);
+          mbar_arrive(&p_full[pb]);
+        }
+      }
+
+      // ---- the item's result, or this part's ----
+#pragma unroll
+      for (int g = 0; g < CG; ++g) {
+        if (g >= gc) continue;
+        const float sum = column_sum8(l[g], lane);
+        if ((lane & 3) == 0) red[quad][(gb + g) * 8 + (lane >> 2)] = sum;
+      }
+      wait(&p_free[(T - 1) % t.pb], (T - 1) / t.pb);
+      tc_fence_after();
+      named_sync(1, kSoftThreads);
+      const bool whole = s.slot < 0;
+      const bool poisoned = poison != 0;
+#pragma unroll
+      for (int g = 0; g < CG; ++g) {
+        if (g >= gc) continue;
+        float o[8];
+        tmem_ld8(tO + lanes + (gb + g) * 8, o);
+        if (tl < D) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int c = (gb + g) * 8 + j;
+            if (c >= s.cols) continue;
+            if (poisoned) {
+              // what was cleared for some rows' sake, added for those that see it
+              const int r = sRow[c];
+              for (int x = 0; x < s.ntiles; ++x) {
+                const int t0 = tile_start<kTile>(s.tiles, s.tile0 + x);
+                for (int y = 0; y < kTile; ++y) {
+                  const int pos = t0 + y;
+                  const bool any = pos <= p_last && (a.window == 0 || pos > p_first - a.window || pos < a.sinks);
+                  const bool all = pos <= p_first && (a.window == 0 || pos > p_last - a.window || pos < a.sinks);
+                  const bool seen = pos <= r && (a.window == 0 || pos > r - a.window || pos < a.sinks);
+                  if (!any || all || !seen) continue;
+                  const int page = a.table[(size_t)s.request * a.max_pages + pos / a.page_size];
+                  if (page < 0 || page >= a.pages) continue;
+                  const float val = load_elem(reinterpret_cast<const __nv_bfloat16*>(
+                                                  a.v + (int64_t)page * a.page_b +
+                                                  (int64_t)(pos % a.page_size) * a.token_b + s.head * a.head_b) +
+                                              tl);
+                  if (!isfinite(val)) o[j] += val;
+                }
+              }
+            }
+            if (whole) {
+              const float sum = (red[0][c] + red[1][c]) + (red[2][c] + red[3][c]);
+              const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+              static_cast<__nv_bfloat16*>(a.out)[sOut[c] * D + tl] = __float2bfloat16(o[j] * inv);
+            } else {
+              a.part[((size_t)s.slot * a.ct + c) * D + tl] = o[j];
+            }
+          }
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&o_free);
+      for (int c = st; c < s.cols; c += kSoftThreads) {
+        const float sum = (red[0][c] + red[1][c]) + (red[2][c] + red[3][c]);
+        const float m = sum == 0.0f ? -INFINITY : sM[c];
+        if (!whole) a.part_stat[(size_t)s.slot * a.ct + c] = make_float2(m, sum);
+        else if (a.lse) a.lse[sOut[c]] = row_lse(m, sum);
+      }
+      if (!whole) {
+        __threadfence();
+        named_sync(1, kSoftThreads);
+        if (st == 0) {
+          last_sh = atomicAdd(a.arrived + s.first_cta, 1u) == (uint32_t)s.parts - 1 ? 1 : 0;
+          if (last_sh) a.arrived[s.first_cta] = 0;
+        }
+        named_sync(1, kSoftThreads);
+        if (last_sh) {
+          __threadfence();
+          join_parts<__nv_bfloat16>(a, s, st, kSoftThreads);
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------
+constexpr int kSmemLimit = 227 * 1024;
+
+// One layer of K or V as [page][token][head][d], in boxes of `chunk` tokens
+// of 64 elements of one head.
+bool make_cache_map(CUtensorMap* map, const char* base, const AttendLaunch& a, int chunk) {
+  auto enc = tensor_map_encoder();
+  if (!enc) return false;
+  cuuint64_t dims[4] = {(cuuint64_t)a.D, (cuuint64_t)a.Hkv, (cuuint64_t)a.page_size, (cuuint64_t)a.pages};
+  // the stride of an extent of one is never used: any valid one
+  const cuuint64_t any = (cuuint64_t)a.D * 2;
+  cuuint64_t strides[3] = {a.Hkv > 1 ? (cuuint64_t)a.head_b : any, a.page_size > 1 ? (cuuint64_t)a.token_b : any,
+                           a.pages > 1 ? (cuuint64_t)a.page_b : any};
+  cuuint32_t box[4] = {64u, 1u, (cuuint32_t)chunk, 1u};
+  cuuint32_t estr[4] = {1u, 1u, 1u, 1u};
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<char*>(base), dims, strides, box, estr,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, int CG, int H>
+cudaError_t launch_variant(const AttendLaunch& a, cudaStream_t stream) {
+  TcPlan t{};
+  t.chunk = a.page_size & -a.page_size;
+  if (t.chunk > kTile) t.chunk = kTile;
+  t.nchunk = kTile / t.chunk;
+  const int q_bytes = a.ct * D * 2, p_bytes = 2 * (a.ct / 16) * kPChunkBytes, slot = (D / 64) * kHalfBytes;
+  // two buffers of Q and P while they leave room for enough tiles in flight
+  t.qb = t.pb = a.ct <= 32 ? 2 : 1;
+  t.p_off = 0;
+  // what the kernel's static shared memory takes, read once
+  static int static_smem = -1;
+  if (static_smem < 0) {
+    cudaFuncAttributes fa{};
+    const cudaError_t err = cudaFuncGetAttributes(&fa, attend_tc_kernel<D, CG, H>);
+    if (err != cudaSuccess) return err;
+    static_smem = (int)fa.sharedSizeBytes;
+  }
+  // dynamic shared memory starts behind the static one, on a 1024-byte boundary
+  const int room = kSmemLimit - (static_smem + 1023) / 1024 * 1024;
+  t.slots = (room - t.qb * q_bytes - t.pb * p_bytes) / slot;
+  if (t.slots > kMaxSlots) t.slots = kMaxSlots;
+  t.q_off = t.slots * slot;
+  t.p_off = t.q_off + t.qb * q_bytes;
+  const int smem = t.p_off + t.pb * p_bytes + kSmemLimit - room - static_smem;  // and the gap before it
+  CUtensorMap tmK, tmV;
+  if (!make_cache_map(&tmK, a.k, a, t.chunk) || !make_cache_map(&tmV, a.v, a, t.chunk)) return cudaErrorInvalidValue;
+  const cudaError_t err =
+      cudaFuncSetAttribute(attend_tc_kernel<D, CG, H>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (err != cudaSuccess) return err;
+  return launch_after_previous(attend_tc_kernel<D, CG, H>, dim3(a.ctas), dim3((4 + 4 * H) * 32), (size_t)smem, stream,
+                               tmK, tmV, a, t);
+}
+
+}  // namespace
+
+bool attend_tc_serves(int D, int dtype, int page_size, int64_t head_b, int64_t token_b, int64_t page_b) {
+  const int64_t far = 1LL << 40;  // a tensor map's strides end there
+  return dtype == SPEC_BF16 && (D == 64 || D == 128) && page_size % 8 == 0 && head_b < far && token_b < far && page_b < far;
+}
+
+int attend_tc_columns(int cols) {
+  const int n = (cols + kTcMaxCols - 1) / kTcMaxCols;  // column tiles, of equal width
+  return ((cols + n - 1) / n + 15) / 16 * 16;
+}
+
+cudaError_t launch_attend_tc(const AttendLaunch& a, cudaStream_t stream) {
+  if (a.ct <= 32) return a.D == 64 ? launch_variant<64, 4, 1>(a, stream) : launch_variant<128, 4, 1>(a, stream);
+  return a.D == 64 ? launch_variant<64, 9, 2>(a, stream) : launch_variant<128, 9, 2>(a, stream);
+}
+
+}  // namespace spec

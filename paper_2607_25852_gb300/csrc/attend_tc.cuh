@@ -1,0 +1,18 @@
+// attend_tc.cuh -- the tensor-core kernel of spec_attend (attend_tc.cu).
+#pragma once
+
+#include "attend.cuh"
+
+namespace spec {
+
+constexpr int kTcMaxCols = 144;  // columns per item: 17 rows of 8 heads, and three such accumulators fit TMEM
+
+// Whether the tensor-core kernel takes a cache of this geometry (strides in bytes).
+bool attend_tc_serves(int D, int dtype, int page_size, int64_t head_b, int64_t token_b, int64_t page_b);
+
+// Columns per item for requests of up to `cols` columns.
+int attend_tc_columns(int cols);
+
+cudaError_t launch_attend_tc(const AttendLaunch& a, cudaStream_t stream);
+
+}  // namespace spec
