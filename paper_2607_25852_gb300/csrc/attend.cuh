@@ -275,38 +275,63 @@ __device__ __forceinline__ float from_float<float>(float x) { return x; }
 template <>
 __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16(x); }
 
+__device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
+__device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v) {
+  const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x, v.y), hi = __floats2bfloat162_rn(v.z, v.w);
+  *reinterpret_cast<uint2*>(p) =
+      make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+}
+
 // The weight of a part in its row's sum.
 __device__ __forceinline__ float part_weight(float2 st, float m) {
   return st.x == -INFINITY ? 0.0f : exp2f(st.x - m);
 }
 
-// Adds the parts of a divided item up: `threads` threads, `tid` of them, all of
-// them past the arrival of the last part.  Two consecutive columns d per step.
+// Adds the parts of a divided item up, in order: `threads` threads, `tid` of
+// them, all of them past the arrival of the last part.  A thread takes four
+// consecutive d of a column and eight parts at a time, whose loads are all in
+// flight together: it is the latency of these loads that a join costs.
 template <typename T>
 __device__ void join_parts(const AttendLaunch& a, const Segment& s, int tid, int threads) {
-  const int half = a.D / 2;
-  for (int e = tid; e < s.cols * half; e += threads) {
-    const int c = e / half, d = 2 * (e - c * half);
-    float m = -INFINITY;
-    for (int x = 0; x < s.parts; ++x) m = fmaxf(m, __ldcg(&a.part_stat[(size_t)part_slot(s, x) * a.ct + c].x));
-    float l = 0.0f, o0 = 0.0f, o1 = 0.0f;
-    for (int x = 0; x < s.parts; ++x) {
-      const size_t at = (size_t)part_slot(s, x) * a.ct + c;
-      const float2 st = __ldcg(a.part_stat + at);
-      const float2 o = __ldcg(reinterpret_cast<const float2*>(a.part + at * a.D + d));
-      const float w = part_weight(st, m);
-      l = fmaf(st.y, w, l);
-      // a part that saw nothing adds nothing
-      if (w != 0.0f) {
-        o0 = fmaf(o.x, w, o0);
-        o1 = fmaf(o.y, w, o1);
+  constexpr int kBatch = 8;
+  const int dv = a.D / 4;
+  for (int e = tid; e < s.cols * dv; e += threads) {
+    const int c = e / dv, d = 4 * (e - c * dv);
+    float m = -INFINITY, l = 0.0f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int x0 = 0; x0 < s.parts; x0 += kBatch) {
+      float2 st[kBatch];
+      float4 w[kBatch];
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        st[k] = make_float2(-INFINITY, 0.0f);
+        if (x0 + k < s.parts) {
+          const size_t at = (size_t)part_slot(s, x0 + k) * a.ct + c;
+          st[k] = __ldcg(a.part_stat + at);
+          w[k] = __ldcg(reinterpret_cast<const float4*>(a.part + at * a.D + d));
+        }
       }
+      float mb = m;
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) mb = fmaxf(mb, st[k].x);
+      const float old = part_weight(make_float2(m, l), mb);
+      l *= old;
+      o = make_float4(o.x * old, o.y * old, o.z * old, o.w * old);
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const float f = part_weight(st[k], mb);
+        if (f == 0.0f) continue;  // a part that saw nothing (or does not exist) adds nothing
+        l = fmaf(st[k].y, f, l);
+        o.x = fmaf(w[k].x, f, o.x);
+        o.y = fmaf(w[k].y, f, o.y);
+        o.z = fmaf(w[k].z, f, o.z);
+        o.w = fmaf(w[k].w, f, o.w);
+      }
+      m = mb;
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     const long long at = out_index(a, s, c);
-    T* out = static_cast<T*>(a.out) + at * a.D + d;
-    out[0] = from_float<T>(o0 * inv);
-    out[1] = from_float<T>(o1 * inv);
+    store4(static_cast<T*>(a.out) + at * a.D + d, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
     if (d == 0 && a.lse) a.lse[at] = row_lse(m, l);
   }
 }

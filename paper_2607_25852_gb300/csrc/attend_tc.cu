@@ -55,7 +55,19 @@ struct TcPlan {
   int chunk, nchunk;    // positions per TMA box, boxes per tile and half
   int slots;            // ring slots (a K or V tile each)
   int q_off, p_off;     // bytes from the start of shared memory
-  int qb, pb;           // buffers of Q and P
+};
+
+// A place in a ring and the parity of its current use, stepped without a division.
+struct RingPos {
+  int slot;
+  uint32_t use;
+  __device__ __forceinline__ void step(int n, int slots) {
+    slot += n;
+    if (slot >= slots) {
+      slot -= slots;
+      use ^= 1u;
+    }
+  }
 };
 
 // ---- PTX ----
@@ -66,6 +78,19 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
       "[%6];" ::"r"(dst),
       "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
       : "memory");
+}
+// mbar_wait with its loop inline: a call would cost the softmax its registers
+// around every wait.
+__device__ __forceinline__ bool wait_phase(uint64_t* bar, uint32_t parity, int32_t* status) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const uint64_t t0 = global_ns();
+  for (uint32_t it = 1; !mbar_try_wait(bar, parity); ++it) {
+    if ((it & 255u) == 0u && global_ns() - t0 > 1000000000ull) {
+      report(status, SPEC_ERR_TIMEOUT);
+      return false;
+    }
+  }
+  return true;
 }
 __device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void named_sync(int id, int threads) {
@@ -99,31 +124,17 @@ __device__ __forceinline__ void tmem_ld8(uint32_t addr, float* v) {
 #pragma unroll
   for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(r[k]);
 }
-__device__ __forceinline__ void tmem_ld24(uint32_t addr, float* v) {
-  uint32_t r[24];
+__device__ __forceinline__ void tmem_ld48(uint32_t addr, float* v) {
+  uint32_t r[48];
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%24];\n\t"
-      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%16,%17,%18,%19,%20,%21,%22,%23}, [%25];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%48];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47}, [%49];\n\t"
       "tcgen05.wait::ld.sync.aligned;"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23])
-      : "r"(addr), "r"(addr + 16)
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]), "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47])
+      : "r"(addr), "r"(addr + 32)
       : "memory");
 #pragma unroll
-  for (int k = 0; k < 24; ++k) v[k] = __uint_as_float(r[k]);
-}
-__device__ __forceinline__ void tmem_ld16(uint32_t addr, float* v) {
-  uint32_t r[16];
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
-      "tcgen05.wait::ld.sync.aligned;"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(addr)
-      : "memory");
-#pragma unroll
-  for (int k = 0; k < 16; ++k) v[k] = __uint_as_float(r[k]);
+  for (int k = 0; k < 48; ++k) v[k] = __uint_as_float(r[k]);
 }
 __device__ __forceinline__ void tmem_st8(uint32_t addr, const float* v) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(addr),
@@ -134,21 +145,28 @@ __device__ __forceinline__ void tmem_st8(uint32_t addr, const float* v) {
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// V as the A operand, read transposed (its d is contiguous): 128-byte swizzled
-// atoms of 64 d x 8 positions; `lbo` bytes to the next 64 d, 1024 to the next
-// 8 positions.
-__device__ __forceinline__ uint64_t desc_v(uint32_t saddr, uint32_t lbo) {
-  return (uint64_t)((saddr >> 4) & 0x3FFFu) | (uint64_t)(lbo >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 |
-         (uint64_t)1 << 46 | (uint64_t)2 << 61;
+// Matrix descriptors: the address (in 16-byte units) in the low word, to which
+// offsets are added, above it the strides and the swizzle.
+constexpr uint32_t kDescVersion = 1u << 14;
+__device__ __forceinline__ uint64_t desc(uint32_t lo, uint32_t hi) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(lo), "r"(hi));
+  return d;
 }
+// K and Q: K-major, 128-byte swizzle, 1024 bytes to the next 8 rows.
+constexpr uint32_t kHiKQ = (1024u >> 4) | kDescVersion | 2u << 29;
+__device__ __forceinline__ uint32_t lo_kq(uint32_t saddr) { return (saddr >> 4) | 1u << 16; }
+// V as the A operand, read transposed (its d is contiguous): 128-byte swizzled
+// atoms of 64 d x 8 positions; `next` bytes to the next 64 d, 1024 to the next
+// 8 positions.
+constexpr uint32_t kHiV = (1024u >> 4) | kDescVersion | 2u << 29;
+__device__ __forceinline__ uint32_t lo_v(uint32_t saddr, uint32_t next) { return (saddr >> 4) | (next >> 4) << 16; }
 // P^T as the B operand, a position's columns contiguous: 32-byte swizzled atoms
 // of 16 columns x 8 positions; 4096 bytes to the next 16 columns, 256 to the
 // next 8 positions.
 constexpr int kPChunkBytes = kTile * 32;
-__device__ __forceinline__ uint64_t desc_p(uint32_t saddr) {
-  return (uint64_t)((saddr >> 4) & 0x3FFFu) | (uint64_t)(kPChunkBytes >> 4) << 16 | (uint64_t)(256 >> 4) << 32 |
-         (uint64_t)1 << 46 | (uint64_t)6 << 61;
-}
+constexpr uint32_t kHiP = (256u >> 4) | kDescVersion | 6u << 29;
+__device__ __forceinline__ uint32_t lo_p(uint32_t saddr) { return (saddr >> 4) | (uint32_t)(kPChunkBytes >> 4) << 16; }
 constexpr uint32_t kTransposeA = 1u << 15, kTransposeB = 1u << 16;
 
 // Two weights as pairs of bf16 numbers: their upper halves, and the rest rounded.
@@ -160,6 +178,12 @@ __device__ __forceinline__ void split_bf16(float x, float y, uint32_t* hi, uint3
 }
 __device__ __forceinline__ void st_shared16(uint32_t at, const uint32_t (&w)[4]) {
   asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+}
+// The references of 8 columns.
+__device__ __forceinline__ void load_ref(float (&m)[8], const float* ref) {
+  const float4 a = *reinterpret_cast<const float4*>(ref), b = *reinterpret_cast<const float4*>(ref + 4);
+  m[0] = a.x; m[1] = a.y; m[2] = a.z; m[3] = a.w;
+  m[4] = b.x; m[5] = b.y; m[6] = b.z; m[7] = b.w;
 }
 __device__ __forceinline__ bool bf16_not_finite(uint32_t h) { return (h & 0x7F80u) == 0x7F80u; }
 
@@ -181,6 +205,31 @@ __device__ __forceinline__ float column_sum8(float (&v)[8], int lane) {
   return v[0];  // column 4 * bit4 + 2 * bit3 + bit2 = lane / 4
 }
 
+// What was cleared in shared memory for the sake of rows that must not see it,
+// for a row (at position r) that does: the values at d, of the positions that
+// some of the item's rows see and some do not, that are not finite.  Rare, so a
+// plain loop over the cache.
+template <int D>
+__device__ __noinline__ float cleared_values(const AttendLaunch& a, const Segment& s, int r, int d) {
+  const int p_first = s.p + s.col0 / a.G, p_last = s.p + (s.col0 + s.cols - 1) / a.G;
+  float sum = 0.0f;
+  for (int x = 0; x < s.ntiles; ++x) {
+    const int t0 = tile_start<kTile>(s.tiles, s.tile0 + x);
+    for (int pos = t0; pos < t0 + kTile; ++pos) {
+      const bool any = pos <= p_last && (a.window == 0 || pos > p_first - a.window || pos < a.sinks);
+      const bool all = pos <= p_first && (a.window == 0 || pos > p_last - a.window || pos < a.sinks);
+      const bool seen = pos <= r && (a.window == 0 || pos > r - a.window || pos < a.sinks);
+      if (!any || all || !seen) continue;
+      const int page = a.table[(size_t)s.request * a.max_pages + pos / a.page_size];
+      if (page < 0 || page >= a.pages) continue;
+      const char* at = a.v + (int64_t)page * a.page_b + (int64_t)(pos % a.page_size) * a.token_b + s.head * a.head_b;
+      const float v = load_elem(reinterpret_cast<const __nv_bfloat16*>(at) + d);
+      if (!isfinite(v)) sum += v;
+    }
+  }
+  return sum;
+}
+
 // ---------------------------------------------------------------------------
 // D: head dimension.  CG: groups of 8 columns per softmax thread.  H: sets of
 // four softmax warps (they split the columns).
@@ -191,9 +240,14 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
                      const __grid_constant__ AttendLaunch a, const __grid_constant__ TcPlan t) {
   constexpr int kCols = CG * 8 * H;             // most columns of an item
   constexpr int kSlotBytes = (D / 64) * kHalfBytes;
+  // Few columns: the two halves of the weights are one product of twice the
+  // width, whose two results the epilogue adds (V is read once, and its reading
+  // is what such a product costs).  Many: two products into the same result.
+  constexpr bool kWide = H > 1;
+  constexpr int PB = kWide ? 1 : 2, QB = kWide ? 1 : 2;  // buffers of P and Q
   constexpr int kTmemStep = (kCols + 31) / 32 * 32;
-  constexpr int kTmemCols = 3 * kTmemStep <= 128 ? 128 : 3 * kTmemStep <= 256 ? 256 : 512;
-  static_assert(3 * kTmemStep <= kTmemCols, "two score buffers and the output fit TMEM");
+  constexpr int kTmemCols = kWide ? 512 : 128;
+  static_assert((kWide ? 3 : 4) * kTmemStep <= kTmemCols, "two score buffers and the output fit TMEM");
   constexpr int kSoftThreads = 128 * H;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -248,226 +302,46 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
   find_share<kTile>(a, &share, sums);  // ends with a barrier
   tc_fence_after();
   const uint32_t tmem = tmem_sh;
-  const uint32_t tS[2] = {tmem, tmem + kTmemStep}, tO = tmem + 2 * kTmemStep;
+  const uint32_t tS0 = tmem, tS1 = tmem + kTmemStep, tO = tmem + 2 * kTmemStep;
   const uint32_t ring = smem_u32(smem);
 
   // The next segment of the share, for a reading warp (n counts segments).
   auto take = [&](int n, Segment* s) -> bool {
     const int k = n % kSegRing;
-    const bool ok = __all_sync(0xFFFFFFFFu, mbar_wait(&seg_full[k], (uint32_t)((n / kSegRing) & 1), a.status));
+    const bool ok = __all_sync(0xFFFFFFFFu, wait_phase(&seg_full[k], (uint32_t)((n / kSegRing) & 1), a.status));
     *s = segs[k];
     __syncwarp();
     if (lane == 0) mbar_arrive(&seg_free[k]);
     return ok;
   };
 
-  if (warp == 0) {
-    // ---- pages into the ring ----
-    const int c = lane % t.nchunk, hf = lane / t.nchunk;
-    const bool mine = hf < D / 64;
-    int tiles = 0, issued = 0;  // tiles done, ring slots filled
-    for (int n = 0;; ++n) {
-      Segment s;
-      if (!take(n, &s)) {
-        aborted = 1;
-        break;
-      }
-      if (s.request < 0) break;
-      const int p_first = s.p + s.col0 / a.G, p_last = s.p + (s.col0 + s.cols - 1) / a.G;
-      const int32_t* row = a.table + (size_t)s.request * a.max_pages;
-      // does some row see this lane's positions of tile x?
-      auto seen = [&](int x) {
-        const int pos = tile_start<kTile>(s.tiles, x) + c * t.chunk;
-        return mine && pos <= p_last && (a.window == 0 || pos + t.chunk - 1 > p_first - a.window || pos < a.sinks);
-      };
-      auto lookup = [&](int x) {
-        return __ldg(row + (tile_start<kTile>(s.tiles, x) + c * t.chunk) / a.page_size);
-      };
-      bool wanted_next = seen(s.tile0);
-      int next = wanted_next ? lookup(s.tile0) : 0;
-      bool ok = true;
-      for (int x = 0; x < s.ntiles && ok; ++x) {
-        int page = next;
-        const bool wanted = wanted_next;
-        if (x + 1 < s.ntiles) {  // the next tile's page, a tile ahead
-          wanted_next = seen(s.tile0 + x + 1);
-          next = wanted_next ? lookup(s.tile0 + x + 1) : 0;
-        }
-        const bool bad = wanted && (page < 0 || page >= a.pages);
-        const uint32_t bads = __ballot_sync(0xFFFFFFFFu, bad && hf == 0);
-        if (bad) report(a.status, SPEC_ERR_BAD_INPUT);
-        if (bad || !wanted) page = a.pages;  // past the map's last page: zeros are written, nothing is read
-        if (lane == 0) tile_bad[tiles % kBadRing] = (int)bads;
-        const int tok = (tile_start<kTile>(s.tiles, s.tile0 + x) + c * t.chunk) % a.page_size;
-#pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-          const int u = 2 * tiles + kv, slot = u % t.slots, use = u / t.slots;
-          ok = __all_sync(0xFFFFFFFFu, !aborted && (use == 0 || mbar_wait(&empty[slot], (uint32_t)((use - 1) & 1),
-                                                                           a.status)));
-          if (!ok) break;
-          if (lane == 0) mbar_expect_tx(&full[slot], kSlotBytes);
-          __syncwarp();
-          if (mine)
-            tma_load_4d(ring + slot * kSlotBytes + hf * kHalfBytes + c * t.chunk * 128, kv ? &tmV : &tmK, hf * 64, s.head,
-                        tok, page, &full[slot]);
-          ++issued;
-        }
-        if (ok) ++tiles;
-      }
-      if (!ok) {
-        aborted = 1;
-        break;
-      }
-    }
-    // what was issued has landed before the CTA ends
-    if (aborted)
-      for (int u = max(0, issued - t.slots); u < issued; ++u)
-        mbar_wait(&full[u % t.slots], (uint32_t)((u / t.slots) & 1), a.status);
-  } else if (warp == 1) {
-    // ---- MMAs ----
-    int T = 0, prev_n = 0;
-    bool prev_first = false, ok = true;
-    uint32_t prev_idesc = 0;
-    // O^T of tile u; `first` of its segment n
-    auto second = [&](int u, bool first, int n, uint32_t idesc) -> bool {
-      const int v = 2 * u + 1, slot = v % t.slots, b = u % t.pb;
-      if (first && n > 0 && !mbar_wait(&o_free, (uint32_t)((n - 1) & 1), a.status)) return false;
-      if (!mbar_wait(&full[slot], (uint32_t)((v / t.slots) & 1), a.status)) return false;
-      if (!mbar_wait(&p_full[b], (uint32_t)((u / t.pb) & 1), a.status)) return false;
-      tc_fence_after();
-      const uint32_t va = ring + slot * kSlotBytes, p_part = (a.ct / 16) * kPChunkBytes;
-      const uint32_t pa = ring + t.p_off + b * 2 * p_part;
-      for (int kk = 0; kk < kTile / 16; ++kk) {
-        const uint64_t dv = desc_v(va + kk * 2048, D == 128 ? kHalfBytes : 0);
-        umma_bf16(tO, dv, desc_p(pa + kk * 512), idesc, first && kk == 0 ? 0u : 1u);
-        umma_bf16(tO, dv, desc_p(pa + p_part + kk * 512), idesc, 1u);
-      }
-      umma_commit(&empty[slot]);
-      umma_commit(&p_free[b]);
-      return true;
-    };
-    for (int n = 0; ok; ++n) {
-      Segment s;
-      ok = take(n, &s);
-      if (!ok || s.request < 0) break;
-      if (lane == 0) {
-        const int N = (s.cols + 15) / 16 * 16, qb = n % t.qb;
-        const uint32_t idesc_s = umma_idesc_bf16(kTile, N);
-        ok = mbar_wait(&q_full[qb], (uint32_t)((n / t.qb) & 1), a.status);
-        const uint32_t qa = ring + t.q_off + qb * a.ct * D * 2;
-        for (int x = 0; x < s.ntiles && ok && !aborted; ++x, ++T) {
-          const int u = 2 * T, slot = u % t.slots, b = T & 1;
-          ok = mbar_wait(&full[slot], (uint32_t)((u / t.slots) & 1), a.status);
-          if (ok && T >= 2) ok = mbar_wait(&s_free[b], (uint32_t)(((T >> 1) - 1) & 1), a.status);
-          if (!ok) break;
-          tc_fence_after();
-          const uint32_t ka = ring + slot * kSlotBytes;
-          for (int kk = 0; kk < D / 16; ++kk)
-            umma_bf16(tS[b], umma_desc_sw128(ka + (kk >> 2) * kHalfBytes + (kk & 3) * 32),
-                      umma_desc_sw128(qa + (kk >> 2) * a.ct * 128 + (kk & 3) * 32), idesc_s, kk > 0 ? 1u : 0u);
-          umma_commit(&empty[slot]);
-          umma_commit(&s_full[b]);
-          if (x == s.ntiles - 1) umma_commit(&q_free[qb]);
-          if (T > 0) ok = second(T - 1, prev_first, prev_n, prev_idesc);
-          prev_first = x == 0;
-          prev_n = n;
-          prev_idesc = umma_idesc_bf16(kTile, N) | kTransposeA | kTransposeB;
-        }
-        if (aborted) ok = false;
-      }
-      ok = __shfl_sync(0xFFFFFFFFu, (int)ok, 0) != 0;
-    }
-    if (lane == 0) {
-      if (ok && T > 0) ok = second(T - 1, prev_first, prev_n, prev_idesc);
-      if (!ok) aborted = 1;
-      // everything issued has completed before the TMEM goes
-      umma_commit(&drained);
-      mbar_wait(&drained, 0u, a.status);
-    }
-    __syncwarp();
-  } else if (warp == 2) {
-    // ---- queries: [64-element halves][column][128 bytes], 128-byte swizzle ----
-    constexpr int kVecs = D / 8;
-    for (int n = 0;; ++n) {
-      Segment s;
-      if (!take(n, &s)) {
-        aborted = 1;
-        break;
-      }
-      if (s.request < 0 || __any_sync(0xFFFFFFFFu, aborted)) break;
-      const int b = n % t.qb;
-      if (n >= t.qb && !__all_sync(0xFFFFFFFFu, mbar_wait(&q_free[b], (uint32_t)(((n / t.qb) - 1) & 1), a.status))) {
-        aborted = 1;
-        break;
-      }
-      const int N = (s.cols + 15) / 16 * 16;
-      uint8_t* dst = smem + t.q_off + b * a.ct * D * 2;
-      const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q);
-      for (int e0 = 0; e0 < N * kVecs; e0 += 256) {  // N is a multiple of 16: whole rounds of 8 vectors a lane
-        uint4 w[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int e = e0 + 32 * k + lane, c = e / kVecs, v = e % kVecs;
-          w[k] = make_uint4(0u, 0u, 0u, 0u);
-          if (c < s.cols) {
-            const int col = s.col0 + c, j = col / a.G;
-            w[k] = __ldg(reinterpret_cast<const uint4*>(q + (int64_t)(s.row0 + j) * a.q_row +
-                                                        (int64_t)(s.head * a.G + col - j * a.G) * D) +
-                         v);
-          }
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int e = e0 + 32 * k + lane, c = e / kVecs, v = e % kVecs;
-          if (c < N)
-            *reinterpret_cast<uint4*>(dst + (v >> 3) * a.ct * 128 + c * 128 + (((v & 7) ^ (c & 7)) << 4)) = w[k];
-        }
-      }
-      proxy_fence();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&q_full[b]);
-    }
-  } else if (warp == 3) {
-    // ---- the CTA's segments ----
-    if (lane == 0) {
-      Walk<kTile> walk(a, share);
-      for (int n = 0; !aborted; ++n) {
-        const int k = n % kSegRing;
-        if (n >= kSegRing && !mbar_wait(&seg_free[k], (uint32_t)(((n / kSegRing) - 1) & 1), a.status)) {
-          aborted = 1;
-          break;
-        }
-        const bool more = walk.next(&segs[k]);
-        if (!more) segs[k].request = -1;
-        mbar_arrive(&seg_full[k]);
-        if (!more) break;
-      }
-    }
-    __syncwarp();
-  } else {
+  // Three softmax sets need more than the 128 registers a thread that 512
+  // threads get: 4 warps x 32 x 56 + 12 x 32 x 152 = 65,536 = 512 x 128.
+  if (warp >= 4) {
+    if constexpr (H == 3) asm volatile("setmaxnreg.inc.sync.aligned.u32 152;");
     // ---- softmax ----
     const int quad = warp & 3, hf = (warp - 4) >> 2;  // TMEM lanes 32 quad .. + 31; column set
     const int st = tid - 128;                         // of kSoftThreads
     const int tl = quad * 32 + lane;                  // this thread's position in a tile, and its d of O^T
     const uint32_t lanes = (uint32_t)(32 * quad) << 16;
-    constexpr bool kKeep = CG <= 4;  // the scores stay in registers between the vote and the weights
-    constexpr int kStep = kKeep ? CG : 3;
     bool failed = false;
     int T = 0;
-    auto wait = [&](uint64_t* bar, int use) {
-      if (!failed && !__all_sync(0xFFFFFFFFu, mbar_wait(bar, (uint32_t)(use & 1), a.status))) failed = true;
+    RingPos vp{1, 0u};
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      if (!failed && !__all_sync(0xFFFFFFFFu, wait_phase(bar, parity & 1u, a.status))) failed = true;
     };
     for (int n = 0;; ++n) {
-      Segment s;
-      if (!take(n, &s)) failed = true;
+      const Segment& s = segs[n % kSegRing];  // given back at the segment's end
+      wait(&seg_full[n % kSegRing], n / kSegRing);
       if (named_or(1, kSoftThreads, failed)) {  // no one has left the last segment's epilogue behind
         aborted = 1;
         break;
       }
       if (s.request < 0) break;
-      const int p_first = s.p + s.col0 / a.G, p_last = s.p + (s.col0 + s.cols - 1) / a.G;
+      const int p_first = s.p + s.col0 / a.G, p_last = s.p + (s.col0 + s.cols - 1) / a.G, ntiles = s.ntiles;
       const int NG = (s.cols + 15) / 16 * 2;        // groups of 8 columns
-      const int gc = NG / H, gb = hf * gc;          // this set's
+      const int per = (NG + H - 1) / H, gb = hf * per;  // this set's: gb .. gb + gc - 1
+      const int gc = max(0, min(NG - gb, per));
       for (int c = st; c < NG * 8; c += kSoftThreads) {
         const int cc = min(c, s.cols - 1);
         sRow[c] = s.p + (s.col0 + cc) / a.G;
@@ -476,108 +350,68 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
       }
       if (st == 0) poison = 0;
       named_sync(1, kSoftThreads);
-      float l[CG][8];
+      float l[CG * 8];
 #pragma unroll
-      for (int g = 0; g < CG; ++g)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) l[g][j] = 0.0f;
+      for (int j = 0; j < CG * 8; ++j) l[j] = 0.0f;
 
-      for (int x = 0; x < s.ntiles; ++x, ++T) {
-        const int t0 = tile_start<kTile>(s.tiles, s.tile0 + x), b = T & 1, pb = T % t.pb;
+      for (int x = 0; x < ntiles; ++x, ++T) {
+        const int t0 = tile_start<kTile>(s.tiles, s.tile0 + x), b = T & 1, pb = T % PB;
         wait(&s_full[b], T >> 1);
         tc_fence_after();
-        const uint32_t sS = tS[b] + lanes + gb * 8;
         const int bads = tile_bad[T % kBadRing];
         const bool edge = !(t0 + kTile - 1 <= p_first &&
                             (a.window == 0 || t0 > p_last - a.window || t0 + kTile <= a.sinks)) ||
                           bads != 0;
         const int pos = t0 + tl;
-        const bool gone = (bads >> (tl / t.chunk)) & 1;
-        float v[kStep][8];
-        // scores of groups g0 .. g0 + kStep - 1 in log2 units, -inf where masked
-        auto load = [&](int g0) {
-          if constexpr (kKeep) {
-            float w[32];
-            if constexpr (CG == 2) tmem_ld16(sS, w);
-            else tmem_ld32(sS, w);
+        const bool gone = edge && (bads >> (tl / t.chunk)) & 1;
+        // scores; -inf where masked
+        float v[CG * 8];
+        {
+          const uint32_t at = (b ? tS1 : tS0) + lanes + gb * 8;
+          if constexpr (CG == 4) tmem_ld32(at, v);
+          else tmem_ld48(at, v);
+        }
+        if (edge) {
 #pragma unroll
-            for (int g = 0; g < CG; ++g)
-#pragma unroll
-              for (int j = 0; j < 8; ++j) v[g][j] = w[8 * g + j];
-          } else {
-            tmem_ld24(sS + g0 * 8, &v[0][0]);
-          }
-        };
-        auto mask = [&](int g0) {
-          if (!edge) return;
-#pragma unroll
-          for (int g = 0; g < kStep; ++g) {
-            if (g0 + g >= gc) continue;
+          for (int g = 0; g < CG; ++g) {
+            if (g >= gc) continue;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-              const int r = sRow[(gb + g0 + g) * 8 + j];
+              const int r = sRow[(gb + g) * 8 + j];
               const bool seen = pos <= r && (a.window == 0 || pos > r - a.window || pos < a.sinks) && !gone;
-              if (!seen) v[g][j] = -INFINITY;
+              if (!seen) v[8 * g + j] = -INFINITY;
             }
           }
-        };
-        // v := v * c2 - reference
-        auto relative = [&](int g0) {
-#pragma unroll
-          for (int g = 0; g < kStep; ++g) {
-            if (g0 + g >= gc) continue;
-            const float4 m0 = *reinterpret_cast<const float4*>(sM + (gb + g0 + g) * 8);
-            const float4 m1 = *reinterpret_cast<const float4*>(sM + (gb + g0 + g) * 8 + 4);
-            v[g][0] = fmaf(v[g][0], a.c2, -m0.x);
-            v[g][1] = fmaf(v[g][1], a.c2, -m0.y);
-            v[g][2] = fmaf(v[g][2], a.c2, -m0.z);
-            v[g][3] = fmaf(v[g][3], a.c2, -m0.w);
-            v[g][4] = fmaf(v[g][4], a.c2, -m1.x);
-            v[g][5] = fmaf(v[g][5], a.c2, -m1.y);
-            v[g][6] = fmaf(v[g][6], a.c2, -m1.z);
-            v[g][7] = fmaf(v[g][7], a.c2, -m1.w);
-          }
-        };
+        }
         // ---- does a score exceed its column's reference by too much? ----
         bool grow = x == 0;
         if (x > 0) {
           float top = -INFINITY;
 #pragma unroll
-          for (int g0 = 0; g0 < CG; g0 += kStep) {
-            if (g0 >= gc) continue;
-            load(g0);
-            mask(g0);
-            relative(g0);
+          for (int g = 0; g < CG; ++g) {
+            if (g >= gc) continue;
+            float m[8];
+            load_ref(m, sM + (gb + g) * 8);
 #pragma unroll
-            for (int g = 0; g < kStep; ++g) {
-              if (g0 + g >= gc) continue;
-#pragma unroll
-              for (int j = 0; j < 8; ++j) top = fmaxf(top, v[g][j]);
-            }
+            for (int j = 0; j < 8; ++j) top = fmaxf(top, fmaf(v[8 * g + j], a.c2, -m[j]));
           }
           grow = named_or(2 + hf, 128, top > kGrowth || failed);
         }
         if (grow) {
           // new references: the columns' maxima so far
 #pragma unroll
-          for (int g0 = 0; g0 < CG; g0 += kStep) {
-            if (g0 >= gc) continue;
-            load(g0);
-            mask(g0);
+          for (int g = 0; g < CG; ++g) {
+            if (g >= gc) continue;
+            float mine = 0.0f;
 #pragma unroll
-            for (int g = 0; g < kStep; ++g) {
-              if (g0 + g >= gc) continue;
-              float mine = 0.0f;
-#pragma unroll
-              for (int j = 0; j < 8; ++j) {
-                const float r = warp_max(v[g][j]);
-                if (lane == j) mine = r * a.c2;
-              }
-              if (lane < 8) red[quad][(gb + g0 + g) * 8 + lane] = mine;
+            for (int j = 0; j < 8; ++j) {
+              const float r = warp_max(v[8 * g + j]);
+              if (lane == j) mine = r * a.c2;
             }
+            if (lane < 8) red[quad][(gb + g) * 8 + lane] = mine;
           }
           named_sync(2 + hf, 128);
-          if (x > 0) wait(&p_free[(T - 1) % t.pb], (T - 1) / t.pb);  // O^T is complete up to tile T - 1
+          if (x > 0) wait(&p_free[(T - 1) % PB], (T - 1) / PB);  // O^T is complete up to tile T - 1
           tc_fence_after();
 #pragma unroll
           for (int g = 0; g < CG; ++g) {
@@ -589,14 +423,18 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
               const float m = fmaxf(fmaxf(red[0][c], red[1][c]), fmaxf(red[2][c], red[3][c]));
               const float old = sM[c];
               alpha[j] = ex2_approx(old - fmaxf(old, m));
-              l[g][j] *= alpha[j];
+              l[8 * g + j] *= alpha[j];
             }
             if (x > 0) {
-              float o[8];
-              tmem_ld8(tO + lanes + (gb + g) * 8, o);
 #pragma unroll
-              for (int j = 0; j < 8; ++j) o[j] *= alpha[j];
-              tmem_st8(tO + lanes + (gb + g) * 8, o);
+              for (int part = 0; part < (kWide ? 1 : 2); ++part) {
+                const uint32_t at = tO + lanes + (gb + g) * 8 + part * NG * 8;
+                float o[8];
+                tmem_ld8(at, o);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[j] *= alpha[j];
+                tmem_st8(at, o);
+              }
             }
           }
           if (x > 0) tmem_st_wait();
@@ -608,33 +446,26 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
           named_sync(2 + hf, 128);
         }
         // ---- weights ----
-        if (T >= t.pb) wait(&p_free[pb], T / t.pb - 1);
-        const uint32_t p_part = (a.ct / 16) * kPChunkBytes;
-        const uint32_t pw = ring + t.p_off + pb * 2 * p_part + tl * 32;
+        if (T >= PB) wait(&p_free[pb], T / PB - 1);
+        const uint32_t p_part = NG * (kPChunkBytes / 2);
+        const uint32_t pw = ring + t.p_off + pb * 2 * (a.ct / 16) * kPChunkBytes + tl * 32;
 #pragma unroll
-        for (int g0 = 0; g0 < CG; g0 += kStep) {
-          if (g0 >= gc) continue;
-          if (!kKeep || grow) {
-            load(g0);
-            mask(g0);
-            relative(g0);
+        for (int g = 0; g < CG; ++g) {
+          if (g >= gc) continue;
+          float m[8];
+          load_ref(m, sM + (gb + g) * 8);
+          uint32_t hi[4], lo[4];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            v[8 * g + j] = ex2_approx(fmaf(v[8 * g + j], a.c2, -m[j]));
+            l[8 * g + j] += v[8 * g + j];
           }
 #pragma unroll
-          for (int g = 0; g < kStep; ++g) {
-            if (g0 + g >= gc) continue;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              v[g][j] = ex2_approx(v[g][j]);
-              l[g0 + g][j] += v[g][j];
-            }
-            const int gg = gb + g0 + g;
-            const uint32_t at = pw + (gg >> 1) * kPChunkBytes + ((((uint32_t)gg & 1) ^ ((tl >> 2) & 1)) << 4);
-            uint32_t hi[4], lo[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) split_bf16(v[g][2 * j], v[g][2 * j + 1], &hi[j], &lo[j]);
-            st_shared16(at, hi);
-            st_shared16(at + p_part, lo);
-          }
+          for (int j = 0; j < 4; ++j) split_bf16(v[8 * g + 2 * j], v[8 * g + 2 * j + 1], &hi[j], &lo[j]);
+          const uint32_t gg = (uint32_t)(gb + g);
+          const uint32_t at = pw + (gg >> 1) * kPChunkBytes + (((gg & 1) ^ ((tl >> 2) & 1)) << 4);
+          st_shared16(at, hi);
+          st_shared16(at + p_part, lo);
         }
         if (edge && hf == 0) {
           // ---- values that rows must not see ----
@@ -642,9 +473,8 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
           const bool any = !gone && pos <= p_last && (a.window == 0 || pos > p_first - a.window || pos < a.sinks);
           const bool all = !gone && pos <= p_first && (a.window == 0 || pos > p_last - a.window || pos < a.sinks);
           if (!__all_sync(0xFFFFFFFFu, all)) {
-            const int u = 2 * T + 1;
-            wait(&full[u % t.slots], u / t.slots);
-            uint8_t* row = smem + (u % t.slots) * kSlotBytes + tl * 128;
+            wait(&full[vp.slot], vp.use);
+            uint8_t* row = smem + vp.slot * kSlotBytes + tl * 128;
             if (!any) {
 #pragma unroll
               for (int k = 0; k < D / 8; ++k)
@@ -670,6 +500,7 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
             }
           }
         }
+        vp.step(2, t.slots);
         tc_fence_before();
         proxy_fence();
         __syncwarp();
@@ -683,45 +514,33 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
 #pragma unroll
       for (int g = 0; g < CG; ++g) {
         if (g >= gc) continue;
-        const float sum = column_sum8(l[g], lane);
+        float mine[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) mine[j] = l[8 * g + j];
+        const float sum = column_sum8(mine, lane);
         if ((lane & 3) == 0) red[quad][(gb + g) * 8 + (lane >> 2)] = sum;
       }
-      wait(&p_free[(T - 1) % t.pb], (T - 1) / t.pb);
+      wait(&p_free[(T - 1) % PB], (T - 1) / PB);
       tc_fence_after();
       named_sync(1, kSoftThreads);
       const bool whole = s.slot < 0;
       const bool poisoned = poison != 0;
-#pragma unroll
-      for (int g = 0; g < CG; ++g) {
-        if (g >= gc) continue;
+#pragma unroll 1
+      for (int g = 0; g < gc; ++g) {
         float o[8];
         tmem_ld8(tO + lanes + (gb + g) * 8, o);
+        if (!kWide) {
+          float rest[8];
+          tmem_ld8(tO + lanes + (NG + gb + g) * 8, rest);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) o[j] += rest[j];
+        }
         if (tl < D) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             const int c = (gb + g) * 8 + j;
             if (c >= s.cols) continue;
-            if (poisoned) {
-              // what was cleared for some rows' sake, added for those that see it
-              const int r = sRow[c];
-              for (int x = 0; x < s.ntiles; ++x) {
-                const int t0 = tile_start<kTile>(s.tiles, s.tile0 + x);
-                for (int y = 0; y < kTile; ++y) {
-                  const int pos = t0 + y;
-                  const bool any = pos <= p_last && (a.window == 0 || pos > p_first - a.window || pos < a.sinks);
-                  const bool all = pos <= p_first && (a.window == 0 || pos > p_last - a.window || pos < a.sinks);
-                  const bool seen = pos <= r && (a.window == 0 || pos > r - a.window || pos < a.sinks);
-                  if (!any || all || !seen) continue;
-                  const int page = a.table[(size_t)s.request * a.max_pages + pos / a.page_size];
-                  if (page < 0 || page >= a.pages) continue;
-                  const float val = load_elem(reinterpret_cast<const __nv_bfloat16*>(
-                                                  a.v + (int64_t)page * a.page_b +
-                                                  (int64_t)(pos % a.page_size) * a.token_b + s.head * a.head_b) +
-                                              tl);
-                  if (!isfinite(val)) o[j] += val;
-                }
-              }
-            }
+            if (poisoned) o[j] += cleared_values<D>(a, s, sRow[c], tl);
             if (whole) {
               const float sum = (red[0][c] + red[1][c]) + (red[2][c] + red[3][c]);
               const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
@@ -754,6 +573,205 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
           join_parts<__nv_bfloat16>(a, s, st, kSoftThreads);
         }
       }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&seg_free[n % kSegRing]);
+    }
+  } else {
+    if constexpr (H == 3) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    if (warp == 0) {
+      // ---- pages into the ring ----
+      const int c = lane % t.nchunk, hf = lane / t.nchunk;
+      const bool mine = hf < D / 64;
+      int tiles = 0, issued = 0;  // tiles done, ring slots filled
+      RingPos rp{0, 1u};          // the parity of the slot's previous use
+      for (int n = 0;; ++n) {
+        Segment s;
+        if (!take(n, &s)) {
+          aborted = 1;
+          break;
+        }
+        if (s.request < 0) break;
+        const int p_first = s.p + s.col0 / a.G, p_last = s.p + (s.col0 + s.cols - 1) / a.G;
+        const int32_t* row = a.table + (size_t)s.request * a.max_pages;
+        // does some row see this lane's positions of tile x?
+        auto seen = [&](int x) {
+          const int pos = tile_start<kTile>(s.tiles, x) + c * t.chunk;
+          return mine && pos <= p_last && (a.window == 0 || pos + t.chunk - 1 > p_first - a.window || pos < a.sinks);
+        };
+        int tok_next = 0;  // its first position in the page
+        auto lookup = [&](int x) {
+          const int pos = tile_start<kTile>(s.tiles, x) + c * t.chunk, slot = pos / a.page_size;
+          tok_next = pos - slot * a.page_size;
+          return __ldg(row + slot);
+        };
+        bool wanted_next = seen(s.tile0);
+        int next = wanted_next ? lookup(s.tile0) : 0;
+        bool ok = true;
+        for (int x = 0; x < s.ntiles && ok; ++x) {
+          int page = next;
+          const int tok = tok_next;
+          const bool wanted = wanted_next;
+          if (x + 1 < s.ntiles) {  // the next tile's page, a tile ahead
+            wanted_next = seen(s.tile0 + x + 1);
+            next = wanted_next ? lookup(s.tile0 + x + 1) : 0;
+          }
+          const bool bad = wanted && (page < 0 || page >= a.pages);
+          const uint32_t bads = __ballot_sync(0xFFFFFFFFu, bad && hf == 0);
+          if (bad) report(a.status, SPEC_ERR_BAD_INPUT);
+          if (bad || !wanted) page = a.pages;  // past the map's last page: zeros are written, nothing is read
+          if (lane == 0) tile_bad[tiles % kBadRing] = (int)bads;
+  #pragma unroll
+          for (int kv = 0; kv < 2; ++kv) {
+            const int slot = rp.slot;
+            ok = __all_sync(0xFFFFFFFFu, !aborted && (issued < t.slots || wait_phase(&empty[slot], rp.use, a.status)));
+            if (!ok) break;
+            rp.step(1, t.slots);
+            if (lane == 0) mbar_expect_tx(&full[slot], kSlotBytes);
+            __syncwarp();
+            if (mine)
+              tma_load_4d(ring + slot * kSlotBytes + hf * kHalfBytes + c * t.chunk * 128, kv ? &tmV : &tmK, hf * 64, s.head,
+                          tok, page, &full[slot]);
+            ++issued;
+          }
+          if (ok) ++tiles;
+        }
+        if (!ok) {
+          aborted = 1;
+          break;
+        }
+      }
+      // what was issued has landed before the CTA ends
+      if (aborted)
+        for (int u = max(0, issued - t.slots); u < issued; ++u)
+          wait_phase(&full[u % t.slots], (uint32_t)((u / t.slots) & 1), a.status);
+    } else if (warp == 1) {
+      // ---- MMAs ----
+      int T = 0, prev_n = 0;
+      bool prev_first = false, ok = true;
+      int prev_N = 0;
+      RingPos kp{0, 0u}, vp{1, 0u};
+      // O^T of tile u, of width N; `first` of its segment n
+      auto second = [&](int u, bool first, int n, int N) -> bool {
+        const int b = u % PB;
+        if (first && n > 0 && !wait_phase(&o_free, (uint32_t)((n - 1) & 1), a.status)) return false;
+        if (!wait_phase(&full[vp.slot], vp.use, a.status)) return false;
+        if (!wait_phase(&p_full[b], (uint32_t)((u / PB) & 1), a.status)) return false;
+        tc_fence_after();
+        const uint32_t idesc = umma_idesc_bf16(kTile, kWide ? N : 2 * N) | kTransposeA | kTransposeB;
+        const uint32_t v = lo_v(ring + vp.slot * kSlotBytes, D == 128 ? kHalfBytes : 0);
+        const uint32_t part = (uint32_t)((N / 16) * kPChunkBytes) >> 4;
+        const uint32_t pw = lo_p(ring + t.p_off + b * 2 * (a.ct / 16) * kPChunkBytes);
+  #pragma unroll
+        for (int kk = 0; kk < kTile / 16; ++kk) {
+          const uint64_t dv = desc(v + kk * (2048 >> 4), kHiV);
+          umma_bf16(tO, dv, desc(pw + kk * (512 >> 4), kHiP), idesc, kk > 0 || !first ? 1u : 0u);
+          if (kWide) umma_bf16(tO, dv, desc(pw + part + kk * (512 >> 4), kHiP), idesc, 1u);
+        }
+        umma_commit(&empty[vp.slot]);
+        umma_commit(&p_free[b]);
+        vp.step(2, t.slots);
+        return true;
+      };
+      for (int n = 0; ok; ++n) {
+        Segment s;
+        ok = take(n, &s);
+        if (!ok || s.request < 0) break;
+        if (lane == 0) {
+          const int N = (s.cols + 15) / 16 * 16, qb = n % QB;
+          const uint32_t idesc = umma_idesc_bf16(kTile, N);
+          ok = wait_phase(&q_full[qb], (uint32_t)((n / QB) & 1), a.status);
+          const uint32_t q = lo_kq(ring + t.q_off + qb * a.ct * D * 2), q_half = (uint32_t)(a.ct * 128) >> 4;
+          for (int x = 0; x < s.ntiles && ok && !aborted; ++x, ++T) {
+            const int b = T & 1;
+            ok = wait_phase(&full[kp.slot], kp.use, a.status);
+            if (ok && T >= 2) ok = wait_phase(&s_free[b], (uint32_t)(((T >> 1) - 1) & 1), a.status);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t k = lo_kq(ring + kp.slot * kSlotBytes), tD = b ? tS1 : tS0;
+  #pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk)
+              umma_bf16(tD, desc(k + (((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4), kHiKQ),
+                        desc(q + (kk >> 2) * q_half + (((kk & 3) * 32) >> 4), kHiKQ), idesc, kk > 0 ? 1u : 0u);
+            umma_commit(&empty[kp.slot]);
+            umma_commit(&s_full[b]);
+            kp.step(2, t.slots);
+            if (x == s.ntiles - 1) umma_commit(&q_free[qb]);
+            if (T > 0) ok = second(T - 1, prev_first, prev_n, prev_N);
+            prev_first = x == 0;
+            prev_n = n;
+            prev_N = N;
+          }
+          if (aborted) ok = false;
+        }
+        ok = __shfl_sync(0xFFFFFFFFu, (int)ok, 0) != 0;
+      }
+      if (lane == 0) {
+        if (ok && T > 0) ok = second(T - 1, prev_first, prev_n, prev_N);
+        if (!ok) aborted = 1;
+        // everything issued has completed before the TMEM goes
+        umma_commit(&drained);
+        wait_phase(&drained, 0u, a.status);
+      }
+      __syncwarp();
+    } else if (warp == 2) {
+      // ---- queries: [64-element halves][column][128 bytes], 128-byte swizzle ----
+      constexpr int kVecs = D / 8;
+      for (int n = 0;; ++n) {
+        Segment s;
+        if (!take(n, &s)) {
+          aborted = 1;
+          break;
+        }
+        if (s.request < 0 || __any_sync(0xFFFFFFFFu, aborted)) break;
+        const int b = n % QB;
+        if (n >= QB && !__all_sync(0xFFFFFFFFu, wait_phase(&q_free[b], (uint32_t)(((n / QB) - 1) & 1), a.status))) {
+          aborted = 1;
+          break;
+        }
+        const int N = (s.cols + 15) / 16 * 16;
+        uint8_t* dst = smem + t.q_off + b * a.ct * D * 2;
+        const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q);
+        for (int e0 = 0; e0 < N * kVecs; e0 += 256) {  // N is a multiple of 16: whole rounds of 8 vectors a lane
+          uint4 w[8];
+  #pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const int e = e0 + 32 * k + lane, c = e / kVecs, v = e % kVecs;
+            w[k] = make_uint4(0u, 0u, 0u, 0u);
+            if (c < s.cols) {
+              const int col = s.col0 + c, j = col / a.G;
+              w[k] = __ldg(reinterpret_cast<const uint4*>(q + (int64_t)(s.row0 + j) * a.q_row +
+                                                          (int64_t)(s.head * a.G + col - j * a.G) * D) +
+                           v);
+            }
+          }
+  #pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const int e = e0 + 32 * k + lane, c = e / kVecs, v = e % kVecs;
+            if (c < N)
+              *reinterpret_cast<uint4*>(dst + (v >> 3) * a.ct * 128 + c * 128 + (((v & 7) ^ (c & 7)) << 4)) = w[k];
+          }
+        }
+        proxy_fence();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&q_full[b]);
+      }
+    } else if (warp == 3) {
+      // ---- the CTA's segments ----
+      if (lane == 0) {
+        Walk<kTile> walk(a, share);
+        for (int n = 0; !aborted; ++n) {
+          const int k = n % kSegRing;
+          if (n >= kSegRing && !wait_phase(&seg_free[k], (uint32_t)(((n / kSegRing) - 1) & 1), a.status)) {
+            aborted = 1;
+            break;
+          }
+          const bool more = walk.next(&segs[k]);
+          if (!more) segs[k].request = -1;
+          mbar_arrive(&seg_full[k]);
+          if (!more) break;
+        }
+      }
+      __syncwarp();
     }
   }
   tc_fence_before();
@@ -793,9 +811,7 @@ cudaError_t launch_variant(const AttendLaunch& a, cudaStream_t stream) {
   if (t.chunk > kTile) t.chunk = kTile;
   t.nchunk = kTile / t.chunk;
   const int q_bytes = a.ct * D * 2, p_bytes = 2 * (a.ct / 16) * kPChunkBytes, slot = (D / 64) * kHalfBytes;
-  // two buffers of Q and P while they leave room for enough tiles in flight
-  t.qb = t.pb = a.ct <= 32 ? 2 : 1;
-  t.p_off = 0;
+  constexpr int QB = H > 1 ? 1 : 2, PB = QB;
   // what the kernel's static shared memory takes, read once
   static int static_smem = -1;
   if (static_smem < 0) {
@@ -806,11 +822,11 @@ cudaError_t launch_variant(const AttendLaunch& a, cudaStream_t stream) {
   }
   // dynamic shared memory starts behind the static one, on a 1024-byte boundary
   const int room = kSmemLimit - (static_smem + 1023) / 1024 * 1024;
-  t.slots = (room - t.qb * q_bytes - t.pb * p_bytes) / slot;
+  t.slots = (room - QB * q_bytes - PB * p_bytes) / slot;
   if (t.slots > kMaxSlots) t.slots = kMaxSlots;
   t.q_off = t.slots * slot;
-  t.p_off = t.q_off + t.qb * q_bytes;
-  const int smem = t.p_off + t.pb * p_bytes + kSmemLimit - room - static_smem;  // and the gap before it
+  t.p_off = t.q_off + QB * q_bytes;
+  const int smem = t.p_off + PB * p_bytes + kSmemLimit - room - static_smem;  // and the gap before it
   CUtensorMap tmK, tmV;
   if (!make_cache_map(&tmK, a.k, a, t.chunk) || !make_cache_map(&tmV, a.v, a, t.chunk)) return cudaErrorInvalidValue;
   const cudaError_t err =
@@ -834,7 +850,7 @@ int attend_tc_columns(int cols) {
 
 cudaError_t launch_attend_tc(const AttendLaunch& a, cudaStream_t stream) {
   if (a.ct <= 32) return a.D == 64 ? launch_variant<64, 4, 1>(a, stream) : launch_variant<128, 4, 1>(a, stream);
-  return a.D == 64 ? launch_variant<64, 9, 2>(a, stream) : launch_variant<128, 9, 2>(a, stream);
+  return a.D == 64 ? launch_variant<64, 6, 3>(a, stream) : launch_variant<128, 6, 3>(a, stream);
 }
 
 }  // namespace spec
