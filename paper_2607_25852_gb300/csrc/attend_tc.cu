@@ -16,13 +16,17 @@
 // The sum of the weights is kept per thread, in fp32, and reduced once per
 // item.  For the second product a weight is the sum of two bf16 numbers, its
 // upper 8 bits and the rounded rest (2^-17 relative): one bf16 number would
-// put an error of the size of the result's own rounding on top of it, and the
-// second product is a small part of the time while the cache is read.
+// put an error of the size of the result's own rounding on top of it.  The two
+// are columns of one product of twice the width, whose two results the item's
+// end adds: a product of 128 rows and 16 steps costs 65 cycles up to N = 32 and
+// 79 at N = 144 (it is the reading of V that it costs), so the width is free
+// where few columns share a head.
 //
 // Warps: 0 loads pages by TMA into a ring of K and V tiles; 1 issues the MMAs
 // (the scores of tile t + 1 before the second product of tile t); 2 loads
 // queries; 3 walks the CTA's share of the work; the rest are the softmax, one
-// TMEM lane quarter per warp, in one or two sets that halve the columns.
+// TMEM lane quarter per warp, in one set or in two that halve the columns and
+// take turns at the buffer of the weights.
 //
 // Positions that no row sees must not reach the result whatever they hold: a
 // weight of 0 does not cancel an infinite or NaN value, so in tiles at an edge
@@ -55,6 +59,7 @@ struct TcPlan {
   int chunk, nchunk;    // positions per TMA box, boxes per tile and half
   int slots;            // ring slots (a K or V tile each)
   int q_off, p_off;     // bytes from the start of shared memory
+  int p_bytes;          // of one buffer of weights
 };
 
 // A place in a ring and the parity of its current use, stepped without a division.
@@ -93,6 +98,22 @@ __device__ __forceinline__ bool wait_phase(uint64_t* bar, uint32_t parity, int32
   return true;
 }
 __device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+// One lane of a converged warp.  The compiler knows elect.sync: descriptors and
+// coordinates under it go to the uniform registers that MMAs and TMA take (an
+// MMA issued by `lane == 0` costs 138 cycles instead).
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(r));
+  return r != 0;
+}
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool real) {
+  // nothing is read where `real` is false: 16 zero bytes are written
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+}
 __device__ __forceinline__ void named_sync(int id, int threads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
@@ -124,17 +145,29 @@ __device__ __forceinline__ void tmem_ld8(uint32_t addr, float* v) {
 #pragma unroll
   for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(r[k]);
 }
-__device__ __forceinline__ void tmem_ld48(uint32_t addr, float* v) {
-  uint32_t r[48];
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, float* v) {
+  uint32_t r[16];
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%48];\n\t"
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47}, [%49];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
       "tcgen05.wait::ld.sync.aligned;"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]), "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47])
-      : "r"(addr), "r"(addr + 32)
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(addr)
       : "memory");
 #pragma unroll
-  for (int k = 0; k < 48; ++k) v[k] = __uint_as_float(r[k]);
+  for (int k = 0; k < 16; ++k) v[k] = __uint_as_float(r[k]);
+}
+__device__ __forceinline__ void tmem_ld80(uint32_t addr, float* v) {
+  uint32_t r[80];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%80];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%64,%65,%66,%67,%68,%69,%70,%71,%72,%73,%74,%75,%76,%77,%78,%79}, [%81];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]), "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]), "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63]), "=r"(r[64]), "=r"(r[65]), "=r"(r[66]), "=r"(r[67]), "=r"(r[68]), "=r"(r[69]), "=r"(r[70]), "=r"(r[71]), "=r"(r[72]), "=r"(r[73]), "=r"(r[74]), "=r"(r[75]), "=r"(r[76]), "=r"(r[77]), "=r"(r[78]), "=r"(r[79])
+      : "r"(addr), "r"(addr + 64)
+      : "memory");
+#pragma unroll
+  for (int k = 0; k < 80; ++k) v[k] = __uint_as_float(r[k]);
 }
 __device__ __forceinline__ void tmem_st8(uint32_t addr, const float* v) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(addr),
@@ -184,6 +217,16 @@ __device__ __forceinline__ void load_ref(float (&m)[8], const float* ref) {
   const float4 a = *reinterpret_cast<const float4*>(ref), b = *reinterpret_cast<const float4*>(ref + 4);
   m[0] = a.x; m[1] = a.y; m[2] = a.z; m[3] = a.w;
   m[4] = b.x; m[5] = b.y; m[6] = b.z; m[7] = b.w;
+}
+__device__ __forceinline__ void load_rows(int (&r)[8], const int* rows) {
+  const int4 a = *reinterpret_cast<const int4*>(rows), b = *reinterpret_cast<const int4*>(rows + 4);
+  r[0] = a.x; r[1] = a.y; r[2] = a.z; r[3] = a.w;
+  r[4] = b.x; r[5] = b.y; r[6] = b.z; r[7] = b.w;
+}
+// Columns of each softmax set but the last, for an item of N (a multiple of 16).
+template <int H>
+__device__ __forceinline__ int set_cols(int N) {
+  return H == 1 ? N : (N / 16 + 1) / 2 * 16;
 }
 __device__ __forceinline__ bool bf16_not_finite(uint32_t h) { return (h & 0x7F80u) == 0x7F80u; }
 
@@ -238,27 +281,28 @@ template <int D, int CG, int H>
 __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
     attend_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                      const __grid_constant__ AttendLaunch a, const __grid_constant__ TcPlan t) {
-  constexpr int kCols = CG * 8 * H;             // most columns of an item
+  constexpr int kCols = H == 1 ? 32 : kTcMaxCols;  // most columns of an item
   constexpr int kSlotBytes = (D / 64) * kHalfBytes;
-  // Few columns: the two halves of the weights are one product of twice the
-  // width, whose two results the epilogue adds (V is read once, and its reading
-  // is what such a product costs).  Many: two products into the same result.
-  constexpr bool kWide = H > 1;
-  constexpr int PB = kWide ? 1 : 2, QB = kWide ? 1 : 2;  // buffers of P and Q
-  constexpr int kTmemStep = (kCols + 31) / 32 * 32;
-  constexpr int kTmemCols = kWide ? 512 : 128;
-  static_assert((kWide ? 3 : 4) * kTmemStep <= kTmemCols, "two score buffers and the output fit TMEM");
+  // One set: two buffers of scores, of weights and of queries.  Two sets: one of
+  // each (the scores are in registers before the next tile's are due, and the
+  // sets take turns at the weights), which leaves room for tiles in flight.
+  constexpr int SB = H == 1 ? 2 : 1, PB = SB, QB = SB;
+  constexpr int kSetCols = CG * 8;                      // most columns of a set
+  constexpr int kOut = SB * ((kCols + 31) / 32 * 32);   // TMEM columns of the scores; then per set 2 kSetCols of O^T
+  constexpr int kTmemCols = H == 1 ? 128 : 512;
+  static_assert(kOut + 2 * kSetCols * H <= kTmemCols, "scores and outputs fit TMEM");
   constexpr int kSoftThreads = 128 * H;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  __shared__ uint64_t full[kMaxSlots], empty[kMaxSlots], s_full[2], s_free[2], p_full[2], p_free[2], o_free, drained, q_full[2],
+  __shared__ uint64_t full[kMaxSlots], empty[kMaxSlots], s_full[2], s_free[2], p_full[2], p_free[2], o_done[2], o_free, drained, q_full[2],
       q_free[2], seg_full[kSegRing], seg_free[kSegRing];
   __shared__ Segment segs[kSegRing];
   __shared__ Share share;
   __shared__ long long sums[32];
   __shared__ int tile_bad[kBadRing];
-  __shared__ __align__(16) float sM[kCols], red[4][kCols];
-  __shared__ int sRow[kCols];        // position of the column's row
+  __shared__ __align__(16) float sM[kCols + 16], sF[kCols], red[4][kCols];
+  __shared__ int2 sPage[2][16];      // a tile's boxes: page, first position in it
+  __shared__ __align__(16) int sRow[kCols];        // position of the column's row
   __shared__ long long sOut[kCols];  // where the column goes
   __shared__ uint32_t tmem_sh;
   __shared__ int abort_flag, poison, last_sh;
@@ -273,8 +317,9 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
     for (int k = 0; k < 2; ++k) {
       mbar_init(&s_full[k], 1);
       mbar_init(&s_free[k], 4 * H);
-      mbar_init(&p_full[k], 4 * H);
+      mbar_init(&p_full[k], 4);
       mbar_init(&p_free[k], 1);
+      mbar_init(&o_done[k], 1);
       mbar_init(&q_full[k], 1);
       mbar_init(&q_free[k], 1);
     }
@@ -302,7 +347,7 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
   find_share<kTile>(a, &share, sums);  // ends with a barrier
   tc_fence_after();
   const uint32_t tmem = tmem_sh;
-  const uint32_t tS0 = tmem, tS1 = tmem + kTmemStep, tO = tmem + 2 * kTmemStep;
+  const uint32_t tO = tmem + kOut;
   const uint32_t ring = smem_u32(smem);
 
   // The next segment of the share, for a reading warp (n counts segments).
@@ -315,10 +360,10 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
     return ok;
   };
 
-  // Three softmax sets need more than the 128 registers a thread that 512
-  // threads get: 4 warps x 32 x 56 + 12 x 32 x 152 = 65,536 = 512 x 128.
+  // Two softmax sets need more than the 168 registers a thread that 384 threads
+  // get: 4 warps x 32 x 56 + 8 x 32 x 224 = 64,512 = 384 x 168.
   if (warp >= 4) {
-    if constexpr (H == 3) asm volatile("setmaxnreg.inc.sync.aligned.u32 152;");
+    if constexpr (H == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
     // ---- softmax ----
     const int quad = warp & 3, hf = (warp - 4) >> 2;  // TMEM lanes 32 quad .. + 31; column set
     const int st = tid - 128;                         // of kSoftThreads
@@ -326,9 +371,20 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
     const uint32_t lanes = (uint32_t)(32 * quad) << 16;
     bool failed = false;
     int T = 0;
+    int U = 0;       // units (tile, set) before this tile
+    int done = 0;    // of this set
     RingPos vp{1, 0u};
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       if (!failed && !__all_sync(0xFFFFFFFFu, wait_phase(bar, parity & 1u, a.status))) failed = true;
+    };
+    // The second product of this set's last unit.  A wait by parity must not
+    // come two phases late: with one set, p_free of the unit's own buffer, whose
+    // phase before was waited for when the buffer was taken; with two, o_done,
+    // waited for before every unit, after which p_free, too, is at most one
+    // phase (the other set's) behind the one the unit needs.
+    auto wait_output = [&]() {
+      if constexpr (H == 1) wait(&p_free[(done - 1) & 1], (done - 1) >> 1);
+      else wait(&o_done[hf], done - 1);
     };
     for (int n = 0;; ++n) {
       const Segment& s = segs[n % kSegRing];  // given back at the segment's end
@@ -339,14 +395,13 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
       }
       if (s.request < 0) break;
       const int p_first = s.p + s.col0 / a.G, p_last = s.p + (s.col0 + s.cols - 1) / a.G, ntiles = s.ntiles;
-      const int NG = (s.cols + 15) / 16 * 2;        // groups of 8 columns
-      const int per = (NG + H - 1) / H, gb = hf * per;  // this set's: gb .. gb + gc - 1
-      const int gc = max(0, min(NG - gb, per));
-      for (int c = st; c < NG * 8; c += kSoftThreads) {
+      const int N = (s.cols + 15) / 16 * 16, wide = set_cols<H>(N);
+      const int cb = hf * wide, gc = max(0, min(wide, N - cb)) / 8;  // this set's columns: gc groups of 8 from cb
+      const int sets = (N + wide - 1) / wide;
+      for (int c = st; c < N; c += kSoftThreads) {
         const int cc = min(c, s.cols - 1);
         sRow[c] = s.p + (s.col0 + cc) / a.G;
         sOut[c] = out_index(a, s, cc);
-        sM[c] = kNoMax;
       }
       if (st == 0) poison = 0;
       named_sync(1, kSoftThreads);
@@ -355,8 +410,8 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
       for (int j = 0; j < CG * 8; ++j) l[j] = 0.0f;
 
       for (int x = 0; x < ntiles; ++x, ++T) {
-        const int t0 = tile_start<kTile>(s.tiles, s.tile0 + x), b = T & 1, pb = T % PB;
-        wait(&s_full[b], T >> 1);
+        const int t0 = tile_start<kTile>(s.tiles, s.tile0 + x), b = T % SB;
+        wait(&s_full[b], T / SB);
         tc_fence_after();
         const int bads = tile_bad[T % kBadRing];
         const bool edge = !(t0 + kTile - 1 <= p_first &&
@@ -366,19 +421,20 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
         const bool gone = edge && (bads >> (tl / t.chunk)) & 1;
         // scores; -inf where masked
         float v[CG * 8];
-        {
-          const uint32_t at = (b ? tS1 : tS0) + lanes + gb * 8;
-          if constexpr (CG == 4) tmem_ld32(at, v);
-          else tmem_ld48(at, v);
-        }
+        if constexpr (H == 1) tmem_ld32(tmem + b * (kOut / SB) + lanes + cb, v);
+        else tmem_ld80(tmem + lanes + cb, v);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&s_free[b]);
         if (edge) {
 #pragma unroll
           for (int g = 0; g < CG; ++g) {
-            if (g >= gc) continue;
+            if (g >= gc) break;
+            int r[8];
+            load_rows(r, sRow + cb + g * 8);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-              const int r = sRow[(gb + g) * 8 + j];
-              const bool seen = pos <= r && (a.window == 0 || pos > r - a.window || pos < a.sinks) && !gone;
+              const bool seen = pos <= r[j] && (a.window == 0 || pos > r[j] - a.window || pos < a.sinks) && !gone;
               if (!seen) v[8 * g + j] = -INFINITY;
             }
           }
@@ -389,9 +445,9 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
           float top = -INFINITY;
 #pragma unroll
           for (int g = 0; g < CG; ++g) {
-            if (g >= gc) continue;
+            if (g >= gc) break;
             float m[8];
-            load_ref(m, sM + (gb + g) * 8);
+            load_ref(m, sM + cb + g * 8);
 #pragma unroll
             for (int j = 0; j < 8; ++j) top = fmaxf(top, fmaf(v[8 * g + j], a.c2, -m[j]));
           }
@@ -401,72 +457,78 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
           // new references: the columns' maxima so far
 #pragma unroll
           for (int g = 0; g < CG; ++g) {
-            if (g >= gc) continue;
+            if (g >= gc) break;
             float mine = 0.0f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
               const float r = warp_max(v[8 * g + j]);
               if (lane == j) mine = r * a.c2;
             }
-            if (lane < 8) red[quad][(gb + g) * 8 + lane] = mine;
+            if (lane < 8) red[quad][cb + g * 8 + lane] = mine;
           }
           named_sync(2 + hf, 128);
-          if (x > 0) wait(&p_free[(T - 1) % PB], (T - 1) / PB);  // O^T is complete up to tile T - 1
-          tc_fence_after();
+          if (tl < gc * 8) {
+            const int c = cb + tl;
+            const float old = x == 0 ? kNoMax : sM[c];
+            const float m = fmaxf(old, fmaxf(fmaxf(red[0][c], red[1][c]), fmaxf(red[2][c], red[3][c])));
+            sF[c] = ex2_approx(old - m);
+            sM[c] = m;
+          }
+          if (x > 0 && gc > 0) wait_output();  // O^T is complete up to the last tile
+          failed = named_or(2 + hf, 128, failed);
+          if (x > 0) {
+            tc_fence_after();
 #pragma unroll
-          for (int g = 0; g < CG; ++g) {
-            if (g >= gc) continue;
-            float alpha[8];
+            for (int g = 0; g < CG; ++g) {
+              if (g >= gc) break;
+              float f[8], o[8];
+              load_ref(f, sF + cb + g * 8);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const int c = (gb + g) * 8 + j;
-              const float m = fmaxf(fmaxf(red[0][c], red[1][c]), fmaxf(red[2][c], red[3][c]));
-              const float old = sM[c];
-              alpha[j] = ex2_approx(old - fmaxf(old, m));
-              l[8 * g + j] *= alpha[j];
-            }
-            if (x > 0) {
+              for (int j = 0; j < 8; ++j) l[8 * g + j] *= f[j];
 #pragma unroll
-              for (int part = 0; part < (kWide ? 1 : 2); ++part) {
-                const uint32_t at = tO + lanes + (gb + g) * 8 + part * NG * 8;
-                float o[8];
+              for (int part = 0; part < 2; ++part) {
+                const uint32_t at = tO + lanes + hf * 2 * kSetCols + part * gc * 8 + g * 8;
                 tmem_ld8(at, o);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) o[j] *= alpha[j];
+                for (int j = 0; j < 8; ++j) o[j] *= f[j];
                 tmem_st8(at, o);
               }
             }
+            tmem_st_wait();
           }
-          if (x > 0) tmem_st_wait();
-          failed = named_or(2 + hf, 128, failed);  // everyone has read the old references
-          for (int c = tl; c < gc * 8; c += 128) {
-            const int cc = gb * 8 + c;
-            sM[cc] = fmaxf(sM[cc], fmaxf(fmaxf(red[0][cc], red[1][cc]), fmaxf(red[2][cc], red[3][cc])));
-          }
-          named_sync(2 + hf, 128);
         }
         // ---- weights ----
-        if (T >= PB) wait(&p_free[pb], T / PB - 1);
-        const uint32_t p_part = NG * (kPChunkBytes / 2);
-        const uint32_t pw = ring + t.p_off + pb * 2 * (a.ct / 16) * kPChunkBytes + tl * 32;
+        const int u = U + hf, pb = u % PB;
 #pragma unroll
         for (int g = 0; g < CG; ++g) {
-          if (g >= gc) continue;
+          if (g >= gc) break;
           float m[8];
-          load_ref(m, sM + (gb + g) * 8);
-          uint32_t hi[4], lo[4];
+          load_ref(m, sM + cb + g * 8);
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             v[8 * g + j] = ex2_approx(fmaf(v[8 * g + j], a.c2, -m[j]));
             l[8 * g + j] += v[8 * g + j];
           }
-#pragma unroll
-          for (int j = 0; j < 4; ++j) split_bf16(v[8 * g + 2 * j], v[8 * g + 2 * j + 1], &hi[j], &lo[j]);
-          const uint32_t gg = (uint32_t)(gb + g);
-          const uint32_t at = pw + (gg >> 1) * kPChunkBytes + (((gg & 1) ^ ((tl >> 2) & 1)) << 4);
-          st_shared16(at, hi);
-          st_shared16(at + p_part, lo);
         }
+        if (gc > 0) {
+          if (H > 1 && done > 0) wait_output();
+          if (u >= PB) wait(&p_free[pb], u / PB - 1);
+          const uint32_t p_part = gc * (kPChunkBytes / 2);  // the upper halves' bytes; then the rest's
+          const uint32_t pw = ring + t.p_off + pb * t.p_bytes + tl * 32;
+          const uint32_t swap = (uint32_t)((tl >> 2) & 1) << 4;
+#pragma unroll
+          for (int g = 0; g < CG; ++g) {
+            if (g >= gc) break;
+            uint32_t hi[4], lo[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) split_bf16(v[8 * g + 2 * j], v[8 * g + 2 * j + 1], &hi[j], &lo[j]);
+            const uint32_t at = pw + (g >> 1) * kPChunkBytes + (((uint32_t)(g & 1) << 4) ^ swap);
+            st_shared16(at, hi);
+            st_shared16(at + p_part, lo);
+          }
+        }
+        U += sets;
+        if (gc > 0) ++done;
         if (edge && hf == 0) {
           // ---- values that rows must not see ----
           // seen by the last row alone or by the first alone: between the two
@@ -504,62 +566,56 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
         tc_fence_before();
         proxy_fence();
         __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(&s_free[b]);
-          mbar_arrive(&p_full[pb]);
-        }
+        if (lane == 0 && gc > 0) mbar_arrive(&p_full[pb]);
       }
 
       // ---- the item's result, or this part's ----
 #pragma unroll
       for (int g = 0; g < CG; ++g) {
-        if (g >= gc) continue;
+        if (g >= gc) break;
         float mine[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) mine[j] = l[8 * g + j];
         const float sum = column_sum8(mine, lane);
-        if ((lane & 3) == 0) red[quad][(gb + g) * 8 + (lane >> 2)] = sum;
+        if ((lane & 3) == 0) red[quad][cb + g * 8 + (lane >> 2)] = sum;
       }
-      wait(&p_free[(T - 1) % PB], (T - 1) / PB);
-      tc_fence_after();
-      named_sync(1, kSoftThreads);
       const bool whole = s.slot < 0;
+      named_sync(1, kSoftThreads);
+      for (int c = st; c < s.cols; c += kSoftThreads) {
+        const float sum = (red[0][c] + red[1][c]) + (red[2][c] + red[3][c]);
+        const float m = sum == 0.0f ? -INFINITY : sM[c];
+        sF[c] = whole ? (sum == 0.0f ? 0.0f : 1.0f / sum) : 1.0f;
+        if (!whole) a.part_stat[(size_t)s.slot * a.ct + c] = make_float2(m, sum);
+        else if (a.lse) a.lse[sOut[c]] = row_lse(m, sum);
+      }
+      if (gc > 0) wait_output();
+      tc_fence_after();
       const bool poisoned = poison != 0;
+      named_sync(1, kSoftThreads);
+      // two groups at a time: a thread has d = tl of 16 columns
 #pragma unroll 1
-      for (int g = 0; g < gc; ++g) {
-        float o[8];
-        tmem_ld8(tO + lanes + (gb + g) * 8, o);
-        if (!kWide) {
-          float rest[8];
-          tmem_ld8(tO + lanes + (NG + gb + g) * 8, rest);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) o[j] += rest[j];
-        }
+      for (int g = 0; g < gc; g += 2) {
+        float o[16], rest[16];
+        const uint32_t at = tO + lanes + hf * 2 * kSetCols + g * 8;
+        tmem_ld16(at, o);
+        tmem_ld16(at + gc * 8, rest);
         if (tl < D) {
+          const int c0 = cb + g * 8;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int c = (gb + g) * 8 + j;
-            if (c >= s.cols) continue;
+          for (int j = 0; j < 16; ++j) {
+            const int c = c0 + j;
+            if (c >= s.cols) break;
+            o[j] += rest[j];
             if (poisoned) o[j] += cleared_values<D>(a, s, sRow[c], tl);
-            if (whole) {
-              const float sum = (red[0][c] + red[1][c]) + (red[2][c] + red[3][c]);
-              const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-              static_cast<__nv_bfloat16*>(a.out)[sOut[c] * D + tl] = __float2bfloat16(o[j] * inv);
-            } else {
-              a.part[((size_t)s.slot * a.ct + c) * D + tl] = o[j];
-            }
+            o[j] *= sF[c];
+            if (whole) static_cast<__nv_bfloat16*>(a.out)[sOut[c] * D + tl] = __float2bfloat16(o[j]);
+            else a.part[((size_t)s.slot * a.ct + c) * D + tl] = o[j];
           }
         }
       }
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&o_free);
-      for (int c = st; c < s.cols; c += kSoftThreads) {
-        const float sum = (red[0][c] + red[1][c]) + (red[2][c] + red[3][c]);
-        const float m = sum == 0.0f ? -INFINITY : sM[c];
-        if (!whole) a.part_stat[(size_t)s.slot * a.ct + c] = make_float2(m, sum);
-        else if (a.lse) a.lse[sOut[c]] = row_lse(m, sum);
-      }
       if (!whole) {
         __threadfence();
         named_sync(1, kSoftThreads);
@@ -577,20 +633,18 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
       if (lane == 0) mbar_arrive(&seg_free[n % kSegRing]);
     }
   } else {
-    if constexpr (H == 3) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    if constexpr (H == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     if (warp == 0) {
       // ---- pages into the ring ----
-      const int c = lane % t.nchunk, hf = lane / t.nchunk;
-      const bool mine = hf < D / 64;
-      int tiles = 0, issued = 0;  // tiles done, ring slots filled
+      const int c = lane;  // the box of this lane: positions c chunk .. of a tile
+      const bool mine = c < t.nchunk;
+      int tiles = 0, issued = 0;  // tiles done, ring slots filled (by the lane that issues)
       RingPos rp{0, 1u};          // the parity of the slot's previous use
-      for (int n = 0;; ++n) {
+      bool ok = true;
+      for (int n = 0; ok; ++n) {
         Segment s;
-        if (!take(n, &s)) {
-          aborted = 1;
-          break;
-        }
-        if (s.request < 0) break;
+        ok = take(n, &s);
+        if (!ok || s.request < 0) break;
         const int p_first = s.p + s.col0 / a.G, p_last = s.p + (s.col0 + s.cols - 1) / a.G;
         const int32_t* row = a.table + (size_t)s.request * a.max_pages;
         // does some row see this lane's positions of tile x?
@@ -606,107 +660,113 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
         };
         bool wanted_next = seen(s.tile0);
         int next = wanted_next ? lookup(s.tile0) : 0;
-        bool ok = true;
-        for (int x = 0; x < s.ntiles && ok; ++x) {
+        for (int x = 0; x < s.ntiles && ok; ++x, ++tiles) {
           int page = next;
-          const int tok = tok_next;
+          const int tok = wanted_next ? tok_next : 0;
           const bool wanted = wanted_next;
           if (x + 1 < s.ntiles) {  // the next tile's page, a tile ahead
             wanted_next = seen(s.tile0 + x + 1);
             next = wanted_next ? lookup(s.tile0 + x + 1) : 0;
           }
           const bool bad = wanted && (page < 0 || page >= a.pages);
-          const uint32_t bads = __ballot_sync(0xFFFFFFFFu, bad && hf == 0);
+          const uint32_t bads = __ballot_sync(0xFFFFFFFFu, bad);
           if (bad) report(a.status, SPEC_ERR_BAD_INPUT);
           if (bad || !wanted) page = a.pages;  // past the map's last page: zeros are written, nothing is read
           if (lane == 0) tile_bad[tiles % kBadRing] = (int)bads;
-  #pragma unroll
-          for (int kv = 0; kv < 2; ++kv) {
-            const int slot = rp.slot;
-            ok = __all_sync(0xFFFFFFFFu, !aborted && (issued < t.slots || wait_phase(&empty[slot], rp.use, a.status)));
-            if (!ok) break;
-            rp.step(1, t.slots);
-            if (lane == 0) mbar_expect_tx(&full[slot], kSlotBytes);
-            __syncwarp();
-            if (mine)
-              tma_load_4d(ring + slot * kSlotBytes + hf * kHalfBytes + c * t.chunk * 128, kv ? &tmV : &tmK, hf * 64, s.head,
-                          tok, page, &full[slot]);
-            ++issued;
+          if (mine) sPage[tiles & 1][c] = make_int2(page, tok);
+          __syncwarp();
+          if (elect_one()) {
+            for (int kv = 0; kv < 2 && ok; ++kv) {
+              ok = !aborted && (issued < t.slots || wait_phase(&empty[rp.slot], rp.use, a.status));
+              if (!ok) break;
+              mbar_expect_tx(&full[rp.slot], kSlotBytes);
+              const CUtensorMap* map = kv ? &tmV : &tmK;
+              uint32_t dst = ring + rp.slot * kSlotBytes;
+              for (int b = 0; b < t.nchunk; ++b, dst += t.chunk * 128) {
+                const int2 pt = sPage[tiles & 1][b];
+                tma_load_4d(dst, map, 0, s.head, pt.y, pt.x, &full[rp.slot]);
+                if (D == 128) tma_load_4d(dst + kHalfBytes, map, 64, s.head, pt.y, pt.x, &full[rp.slot]);
+              }
+              ++issued;
+              rp.step(1, t.slots);
+            }
           }
-          if (ok) ++tiles;
-        }
-        if (!ok) {
-          aborted = 1;
-          break;
+          ok = __all_sync(0xFFFFFFFFu, ok);
         }
       }
-      // what was issued has landed before the CTA ends
-      if (aborted)
+      if (!ok) {
+        aborted = 1;
+        // what was issued has landed before the CTA ends
+        issued = (int)__reduce_max_sync(0xFFFFFFFFu, (unsigned)issued);
         for (int u = max(0, issued - t.slots); u < issued; ++u)
           wait_phase(&full[u % t.slots], (uint32_t)((u / t.slots) & 1), a.status);
+      }
     } else if (warp == 1) {
       // ---- MMAs ----
-      int T = 0, prev_n = 0;
-      bool prev_first = false, ok = true;
-      int prev_N = 0;
-      RingPos kp{0, 0u}, vp{1, 0u};
-      // O^T of tile u, of width N; `first` of its segment n
-      auto second = [&](int u, bool first, int n, int N) -> bool {
-        const int b = u % PB;
-        if (first && n > 0 && !wait_phase(&o_free, (uint32_t)((n - 1) & 1), a.status)) return false;
-        if (!wait_phase(&full[vp.slot], vp.use, a.status)) return false;
-        if (!wait_phase(&p_full[b], (uint32_t)((u / PB) & 1), a.status)) return false;
-        tc_fence_after();
-        const uint32_t idesc = umma_idesc_bf16(kTile, kWide ? N : 2 * N) | kTransposeA | kTransposeB;
-        const uint32_t v = lo_v(ring + vp.slot * kSlotBytes, D == 128 ? kHalfBytes : 0);
-        const uint32_t part = (uint32_t)((N / 16) * kPChunkBytes) >> 4;
-        const uint32_t pw = lo_p(ring + t.p_off + b * 2 * (a.ct / 16) * kPChunkBytes);
-  #pragma unroll
-        for (int kk = 0; kk < kTile / 16; ++kk) {
-          const uint64_t dv = desc(v + kk * (2048 >> 4), kHiV);
-          umma_bf16(tO, dv, desc(pw + kk * (512 >> 4), kHiP), idesc, kk > 0 || !first ? 1u : 0u);
-          if (kWide) umma_bf16(tO, dv, desc(pw + part + kk * (512 >> 4), kHiP), idesc, 1u);
-        }
-        umma_commit(&empty[vp.slot]);
-        umma_commit(&p_free[b]);
-        vp.step(2, t.slots);
-        return true;
-      };
-      for (int n = 0; ok; ++n) {
-        Segment s;
-        ok = take(n, &s);
-        if (!ok || s.request < 0) break;
-        if (lane == 0) {
-          const int N = (s.cols + 15) / 16 * 16, qb = n % QB;
+      if (elect_one()) {
+        int T = 0, U = 0;  // tiles whose scores, units (tile, set) whose second product is issued
+        int prev_n = 0, prev_N = 0;
+        bool prev_first = false, ok = true;
+        RingPos kp{0, 0u}, vp{1, 0u};
+        // O^T of a tile of width N, set by set; `first` of its segment n
+        auto second = [&](bool first, int n, int N) -> bool {
+          if (first && n > 0 && !wait_phase(&o_free, (uint32_t)((n - 1) & 1), a.status)) return false;
+          if (!wait_phase(&full[vp.slot], vp.use, a.status)) return false;
+          const uint32_t v = lo_v(ring + vp.slot * kSlotBytes, D == 128 ? kHalfBytes : 0);
+          const int wide = set_cols<H>(N);
+#pragma unroll
+          for (int h = 0; h < H; ++h) {
+            const int Nh = min(wide, N - h * wide);
+            if (Nh <= 0) break;
+            const int b = U % PB;
+            if (!wait_phase(&p_full[b], (uint32_t)((U / PB) & 1), a.status)) return false;
+            tc_fence_after();
+            const uint32_t idesc = umma_idesc_bf16(kTile, 2 * Nh) | kTransposeA | kTransposeB;
+            const uint32_t w = lo_p(ring + t.p_off + b * t.p_bytes), tD = tO + h * 2 * kSetCols;
+#pragma unroll
+            for (int kk = 0; kk < kTile / 16; ++kk)
+              umma_bf16(tD, desc(v + kk * (2048 >> 4), kHiV), desc(w + kk * (512 >> 4), kHiP), idesc,
+                        kk > 0 || !first ? 1u : 0u);
+            umma_commit(&p_free[b]);
+            umma_commit(&o_done[h]);
+            ++U;
+          }
+          umma_commit(&empty[vp.slot]);
+          vp.step(2, t.slots);
+          return true;
+        };
+        for (int n = 0; ok; ++n) {
+          const int k = n % kSegRing;
+          ok = wait_phase(&seg_full[k], (uint32_t)((n / kSegRing) & 1), a.status);
+          const int request = segs[k].request, cols = segs[k].cols, ntiles = segs[k].ntiles;
+          mbar_arrive(&seg_free[k]);
+          if (!ok || request < 0) break;
+          const int N = (cols + 15) / 16 * 16, qb = n % QB;
           const uint32_t idesc = umma_idesc_bf16(kTile, N);
           ok = wait_phase(&q_full[qb], (uint32_t)((n / QB) & 1), a.status);
           const uint32_t q = lo_kq(ring + t.q_off + qb * a.ct * D * 2), q_half = (uint32_t)(a.ct * 128) >> 4;
-          for (int x = 0; x < s.ntiles && ok && !aborted; ++x, ++T) {
-            const int b = T & 1;
-            ok = wait_phase(&full[kp.slot], kp.use, a.status);
-            if (ok && T >= 2) ok = wait_phase(&s_free[b], (uint32_t)(((T >> 1) - 1) & 1), a.status);
+          for (int x = 0; x < ntiles && ok; ++x, ++T) {
+            const int b = T % SB;
+            ok = !aborted && wait_phase(&full[kp.slot], kp.use, a.status);
+            if (ok && T >= SB) ok = wait_phase(&s_free[b], (uint32_t)((T / SB - 1) & 1), a.status);
             if (!ok) break;
             tc_fence_after();
-            const uint32_t k = lo_kq(ring + kp.slot * kSlotBytes), tD = b ? tS1 : tS0;
-  #pragma unroll
+            const uint32_t key = lo_kq(ring + kp.slot * kSlotBytes), tD = tmem + b * (kOut / SB);
+#pragma unroll
             for (int kk = 0; kk < D / 16; ++kk)
-              umma_bf16(tD, desc(k + (((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4), kHiKQ),
+              umma_bf16(tD, desc(key + (((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4), kHiKQ),
                         desc(q + (kk >> 2) * q_half + (((kk & 3) * 32) >> 4), kHiKQ), idesc, kk > 0 ? 1u : 0u);
-            umma_commit(&empty[kp.slot]);
             umma_commit(&s_full[b]);
+            umma_commit(&empty[kp.slot]);
             kp.step(2, t.slots);
-            if (x == s.ntiles - 1) umma_commit(&q_free[qb]);
-            if (T > 0) ok = second(T - 1, prev_first, prev_n, prev_N);
+            if (x == ntiles - 1) umma_commit(&q_free[qb]);
+            if (T > 0) ok = second(prev_first, prev_n, prev_N);
             prev_first = x == 0;
             prev_n = n;
             prev_N = N;
           }
-          if (aborted) ok = false;
         }
-        ok = __shfl_sync(0xFFFFFFFFu, (int)ok, 0) != 0;
-      }
-      if (lane == 0) {
-        if (ok && T > 0) ok = second(T - 1, prev_first, prev_n, prev_N);
+        if (ok && T > 0) ok = second(prev_first, prev_n, prev_N);
         if (!ok) aborted = 1;
         // everything issued has completed before the TMEM goes
         umma_commit(&drained);
@@ -729,28 +789,25 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
           break;
         }
         const int N = (s.cols + 15) / 16 * 16;
-        uint8_t* dst = smem + t.q_off + b * a.ct * D * 2;
-        const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q);
-        for (int e0 = 0; e0 < N * kVecs; e0 += 256) {  // N is a multiple of 16: whole rounds of 8 vectors a lane
-          uint4 w[8];
-  #pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const int e = e0 + 32 * k + lane, c = e / kVecs, v = e % kVecs;
-            w[k] = make_uint4(0u, 0u, 0u, 0u);
-            if (c < s.cols) {
-              const int col = s.col0 + c, j = col / a.G;
-              w[k] = __ldg(reinterpret_cast<const uint4*>(q + (int64_t)(s.row0 + j) * a.q_row +
-                                                          (int64_t)(s.head * a.G + col - j * a.G) * D) +
-                           v);
-            }
-          }
-  #pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const int e = e0 + 32 * k + lane, c = e / kVecs, v = e % kVecs;
-            if (c < N)
-              *reinterpret_cast<uint4*>(dst + (v >> 3) * a.ct * 128 + c * 128 + (((v & 7) ^ (c & 7)) << 4)) = w[k];
+        const uint32_t dst = ring + t.q_off + b * a.ct * D * 2;
+        // a lane takes vector v of every kStep-th column; the column's row j and
+        // head g move along without divisions
+        constexpr int kStep = 32 / kVecs;
+        const int v = lane % kVecs;
+        int c = lane / kVecs, j = (s.col0 + c) / a.G, g = s.col0 + c - j * a.G;
+        const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q) + (int64_t)s.row0 * a.q_row +
+                                 (int64_t)s.head * a.G * D + v * 8;
+        for (; c < N; c += kStep) {
+          const bool real = c < s.cols;
+          cp_async16(dst + (v >> 3) * a.ct * 128 + c * 128 + (((v & 7) ^ (c & 7)) << 4),
+                     real ? q + (int64_t)j * a.q_row + g * D : q, real);
+          g += kStep;
+          while (g >= a.G) {
+            g -= a.G;
+            ++j;
           }
         }
+        asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
         proxy_fence();
         __syncwarp();
         if (lane == 0) mbar_arrive(&q_full[b]);
@@ -810,8 +867,10 @@ cudaError_t launch_variant(const AttendLaunch& a, cudaStream_t stream) {
   t.chunk = a.page_size & -a.page_size;
   if (t.chunk > kTile) t.chunk = kTile;
   t.nchunk = kTile / t.chunk;
-  const int q_bytes = a.ct * D * 2, p_bytes = 2 * (a.ct / 16) * kPChunkBytes, slot = (D / 64) * kHalfBytes;
-  constexpr int QB = H > 1 ? 1 : 2, PB = QB;
+  constexpr int QB = H == 1 ? 2 : 1, PB = QB;
+  const int set = H == 1 ? a.ct : (a.ct / 16 + 1) / 2 * 16;
+  const int q_bytes = a.ct * D * 2, p_bytes = 2 * (set / 16) * kPChunkBytes, slot = (D / 64) * kHalfBytes;
+  t.p_bytes = p_bytes;
   // what the kernel's static shared memory takes, read once
   static int static_smem = -1;
   if (static_smem < 0) {
@@ -850,7 +909,7 @@ int attend_tc_columns(int cols) {
 
 cudaError_t launch_attend_tc(const AttendLaunch& a, cudaStream_t stream) {
   if (a.ct <= 32) return a.D == 64 ? launch_variant<64, 4, 1>(a, stream) : launch_variant<128, 4, 1>(a, stream);
-  return a.D == 64 ? launch_variant<64, 6, 3>(a, stream) : launch_variant<128, 6, 3>(a, stream);
+  return a.D == 64 ? launch_variant<64, 10, 2>(a, stream) : launch_variant<128, 10, 2>(a, stream);
 }
 
 }  // namespace spec

@@ -5,7 +5,7 @@
 
 namespace spec {
 
-constexpr int kTcMaxCols = 144;  // columns per item: 17 rows of 8 heads, and three such accumulators fit TMEM
+constexpr int kTcMaxCols = 144;  // columns per item: 17 rows of 8 heads; scores and two halves of the output fit TMEM
 
 // Whether the tensor-core kernel takes a cache of this geometry (strides in bytes).
 bool attend_tc_serves(int D, int dtype, int page_size, int64_t head_b, int64_t token_b, int64_t page_b);
