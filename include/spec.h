@@ -591,7 +591,7 @@ typedef struct spec_cache {
  *                   zero-filled once before the first use; left ready for the
  *                   next call.  Calls that may overlap need separate ones.
  * Limits: 1 <= B, 0 <= K <= SPEC_MAX_DRAFTS, q_heads a multiple of kv_heads
- * and at most SPEC_MAX_GROUP times it, max_pages * page_size < 2^31.  A longer
+ * and at most SPEC_MAX_GROUP times it, max_pages * page_size <= 2^30.  A longer
  * prompt is fed in chunks of up to K + 1 = 256 rows.
  * ---------------------------------------------------------------------- */
 size_t spec_attend_workspace(int B, int K, int q_heads, int kv_heads, int head_dim, int dtype);

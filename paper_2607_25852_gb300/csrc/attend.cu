@@ -275,6 +275,7 @@ __global__ void __launch_bounds__(kGenThreads, 1) attend_general_kernel(const At
 // ---------------------------------------------------------------------------
 struct AttendGeometry {
   int ct;  // columns per item, the most of the kernels that may serve the shape
+  int ctas;  // most CTAs: two parts each
   size_t part_off, stat_off, bytes;
 };
 
@@ -282,8 +283,9 @@ struct AttendGeometry {
 static AttendGeometry attend_geometry(int cols, int D, int dtype) {
   AttendGeometry g{};
   g.ct = dtype == SPEC_BF16 ? std::max(kGenCols, attend_tc_columns(cols)) : kGenCols;
-  const size_t slots = 2 * kAttendMaxCtas;
-  g.part_off = (kAttendMaxCtas * 4 + 255) / 256 * 256;
+  g.ctas = kAttendMaxSms * (dtype == SPEC_BF16 ? attend_tc_ctas_per_sm(D, g.ct) : 1);
+  const size_t slots = 2 * (size_t)g.ctas;
+  g.part_off = ((size_t)g.ctas * 4 + 255) / 256 * 256;
   g.stat_off = g.part_off + (slots * g.ct * D * 4 + 255) / 256 * 256;
   g.bytes = g.stat_off + (slots * g.ct * 8 + 255) / 256 * 256;
   return g;
@@ -350,7 +352,8 @@ extern "C" int spec_attend(const void* q, int64_t q_row_stride, int q_heads, con
   a.table = page_table;
   a.rows = RowLayout{row_offsets, depth, pos_base, B, K};
   a.c2 = (float)(1.4426950408889634 * (double)scale);
-  a.window = window;
+  // a window longer than the table hides nothing
+  a.window = (long long)window > (long long)max_pages * cache->page_size ? 0 : window;
   a.sinks = sinks;
   a.out = out;
   a.lse = lse_out;
@@ -359,14 +362,16 @@ extern "C" int spec_attend(const void* q, int64_t q_row_stride, int q_heads, con
   a.arrived = reinterpret_cast<uint32_t*>(base);
   a.part = reinterpret_cast<float*>(base + g.part_off);
   a.part_stat = reinterpret_cast<float2*>(base + g.stat_off);
-  a.ctas = std::min(device_sms(), kAttendMaxCtas);
+  const int sms = std::min(device_sms(), kAttendMaxSms);
   a.min_tiles = 1;
   cudaError_t err;
   if (attend_tc_serves(a.D, cache->dtype, a.page_size, a.head_b, a.token_b, a.page_b)) {
     a.ct = attend_tc_columns((K + 1) * a.G);
+    a.ctas = sms * attend_tc_ctas_per_sm(a.D, a.ct);
     err = launch_attend_tc(a, stream);
   } else {
     a.ct = kGenCols;
+    a.ctas = sms;
     err = cache->dtype == SPEC_F32 ? launch_general<float>(a, stream) : launch_general<__nv_bfloat16>(a, stream);
   }
   return err == cudaSuccess && cudaGetLastError() == cudaSuccess ? SPEC_OK : SPEC_ERR_CUDA;

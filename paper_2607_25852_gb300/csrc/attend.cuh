@@ -15,7 +15,7 @@
 
 namespace spec {
 
-constexpr int kAttendMaxCtas = 160;  // partial results in the workspace: two per CTA
+constexpr int kAttendMaxSms = 160;  // SMs a grid uses at most; the workspace is sized for them
 
 struct AttendLaunch {
   const void* q;
@@ -63,7 +63,7 @@ __device__ __forceinline__ int tile_start(const ItemTiles& t, int x) {
   return (x < t.ns ? x : t.w0 + x - t.ns) * TT;
 }
 
-constexpr int kNowhere = -(1 << 30);  // the position of rows that see nothing
+constexpr int kNowhere = -(1 << 28);  // the position of rows that see nothing
 
 // A request's rows as spec_attend takes them: p is kNowhere where its rows see
 // nothing (idle, or positions past the table), count 0 where nothing of it

@@ -52,6 +52,12 @@ constexpr int kHalfBytes = kTile * 128;  // 64 elements of 128 positions
 constexpr int kMaxSlots = 12;
 constexpr int kSegRing = 4;
 constexpr int kBadRing = 32;      // tiles between the loader and the softmax: fewer than 2 kMaxSlots
+// Items of few columns and small tiles go two CTAs to an SM: a CTA's chain from
+// scores to weights to output is longer than the time its tile takes to arrive,
+// and the ends of its items leave the loads idle.  (With D = 128 the tiles are
+// twice as large: one CTA's chain keeps up, and two would not have three tiles'
+// room each.)
+constexpr bool two_per_sm(int D, int CG) { return D == 64 && CG == 2; }
 constexpr float kNoMax = -3.0e38f;  // the reference of a column that has seen nothing
 constexpr float kGrowth = 8.0f;   // log2 of how far weights may exceed 1
 
@@ -157,6 +163,18 @@ __device__ __forceinline__ void tmem_ld16(uint32_t addr, float* v) {
 #pragma unroll
   for (int k = 0; k < 16; ++k) v[k] = __uint_as_float(r[k]);
 }
+__device__ __forceinline__ void tmem_ld48(uint32_t addr, float* v) {
+  uint32_t r[48];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%48];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47}, [%49];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]), "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47])
+      : "r"(addr), "r"(addr + 32)
+      : "memory");
+#pragma unroll
+  for (int k = 0; k < 48; ++k) v[k] = __uint_as_float(r[k]);
+}
 __device__ __forceinline__ void tmem_ld80(uint32_t addr, float* v) {
   uint32_t r[80];
   asm volatile(
@@ -202,26 +220,63 @@ constexpr uint32_t kHiP = (256u >> 4) | kDescVersion | 6u << 29;
 __device__ __forceinline__ uint32_t lo_p(uint32_t saddr) { return (saddr >> 4) | (uint32_t)(kPChunkBytes >> 4) << 16; }
 constexpr uint32_t kTransposeA = 1u << 15, kTransposeB = 1u << 16;
 
-// Two weights as pairs of bf16 numbers: their upper halves, and the rest rounded.
-__device__ __forceinline__ void split_bf16(float x, float y, uint32_t* hi, uint32_t* lo) {
-  const uint32_t xb = __float_as_uint(x), yb = __float_as_uint(y);
-  *hi = __byte_perm(xb, yb, 0x7632);
-  const float xr = x - __uint_as_float(xb & 0xFFFF0000u), yr = y - __uint_as_float(yb & 0xFFFF0000u);
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(*lo) : "f"(yr), "f"(xr));
+// Two fp32 numbers in one register pair, for the packed instructions.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair(float x, float y) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+  return r;
 }
-__device__ __forceinline__ void st_shared16(uint32_t at, const uint32_t (&w)[4]) {
-  asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+__device__ __forceinline__ float2 unpair(f32x2 p) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(p));
+  return r;
 }
-// The references of 8 columns.
-__device__ __forceinline__ void load_ref(float (&m)[8], const float* ref) {
-  const float4 a = *reinterpret_cast<const float4*>(ref), b = *reinterpret_cast<const float4*>(ref + 4);
-  m[0] = a.x; m[1] = a.y; m[2] = a.z; m[3] = a.w;
-  m[4] = b.x; m[5] = b.y; m[6] = b.z; m[7] = b.w;
+__device__ __forceinline__ f32x2 fma2(f32x2 x, f32x2 y, f32x2 z) {
+  f32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(x), "l"(y), "l"(z));
+  return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 x, f32x2 y) {
+  f32x2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
+  return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 x, f32x2 y) {
+  f32x2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
+  return r;
+}
+__device__ __forceinline__ float max3(float x, float y, float z) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
+  return r;
+}
+// Four pairs of shared memory.
+__device__ __forceinline__ void load_pairs(f32x2 (&p)[4], const float* at) {
+  const ulonglong2 a = *reinterpret_cast<const ulonglong2*>(at), b = *reinterpret_cast<const ulonglong2*>(at + 4);
+  p[0] = a.x; p[1] = a.y; p[2] = b.x; p[3] = b.y;
 }
 __device__ __forceinline__ void load_rows(int (&r)[8], const int* rows) {
   const int4 a = *reinterpret_cast<const int4*>(rows), b = *reinterpret_cast<const int4*>(rows + 4);
   r[0] = a.x; r[1] = a.y; r[2] = a.z; r[3] = a.w;
   r[4] = b.x; r[5] = b.y; r[6] = b.z; r[7] = b.w;
+}
+// Two weights as pairs of bf16 numbers: their upper halves, and the rest rounded.
+__device__ __forceinline__ void split_bf16(float x, float y, uint32_t* hi, uint32_t* lo) {
+  const uint32_t xb = __float_as_uint(x), yb = __float_as_uint(y);
+  *hi = __byte_perm(xb, yb, 0x7632);
+  const f32x2 upper = pair(__uint_as_float(xb & 0xFFFF0000u), __uint_as_float(yb & 0xFFFF0000u));
+  const float2 rest = unpair(fma2(upper, pair(-1.0f, -1.0f), pair(x, y)));
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(*lo) : "f"(rest.y), "f"(rest.x));
+}
+__device__ __forceinline__ void st_shared16_if(bool yes, uint32_t at, const uint32_t (&w)[4]) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.u32 p, %0, 0;\n\t"
+      "@p st.shared.v4.b32 [%1], {%2,%3,%4,%5};\n\t}" ::"r"((uint32_t)yes),
+      "r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
+      : "memory");
 }
 // Columns of each softmax set but the last, for an item of N (a multiple of 16).
 template <int H>
@@ -273,34 +328,119 @@ __device__ __noinline__ float cleared_values(const AttendLaunch& a, const Segmen
   return sum;
 }
 
+// An item's queries into shared memory, [64-element halves][column][128 bytes]
+// with the 128-byte swizzle, columns past the last zero: `threads` threads (a
+// multiple of 32), thread i a vector of every (threads / vectors)-th column.
+// The column's row and head move along without divisions.
+template <int D>
+__device__ __forceinline__ void load_queries(const AttendLaunch& a, const Segment& s, uint32_t dst, int i, int threads) {
+  constexpr int kVecs = D / 8;
+  const int N = (s.cols + 15) / 16 * 16, step = threads / kVecs, v = i % kVecs;
+  int c = i / kVecs, j = (s.col0 + c) / a.G, g = s.col0 + c - j * a.G;
+  const __nv_bfloat16* row = static_cast<const __nv_bfloat16*>(a.q) + (int64_t)(s.row0 + j) * a.q_row +
+                             (int64_t)s.head * a.G * D + v * 8;
+  uint32_t at = dst + (v >> 3) * a.ct * 128 + c * 128;
+  for (; c < N; c += step, at += step * 128) {
+    const bool real = c < s.cols;
+    cp_async16(at + (((v & 7) ^ (c & 7)) << 4), real ? row + g * D : static_cast<const __nv_bfloat16*>(a.q), real);
+    g += step;
+    while (g >= a.G) {
+      g -= a.G;
+      row += a.q_row;
+    }
+  }
+  asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
+  proxy_fence();
+}
+
+// Adds the parts of a divided item up, in order, with `threads` threads past the
+// arrival of the last part.  The parts' weights go to `scratch` (`room` floats
+// of shared memory) once, for as many columns at a time as fit; then a thread
+// adds four consecutive d of up to four columns at a time, whose loads are in
+// flight together.  What a join costs is the latency of these loads.
+template <int D>
+__device__ void join_tc(const AttendLaunch& a, const Segment& s, const long long* where, float* scratch, int room,
+                        int tid, int threads) {
+  constexpr int kQ = D / 4, kE = 4;
+  const int parts = s.parts, most = max(1, room / parts);
+  for (int c0 = 0; c0 < s.cols; c0 += most) {
+    const int nc = min(most, s.cols - c0);
+    for (int c = tid; c < nc; c += threads) {
+      float m = -INFINITY, l = 0.0f;
+#pragma unroll 8
+      for (int x = 0; x < parts; ++x) {
+        const float2 st = __ldcg(a.part_stat + (size_t)part_slot(s, x) * a.ct + c0 + c);
+        const float mn = fmaxf(m, st.x);
+        l = l * part_weight(make_float2(m, l), mn) + st.y * part_weight(st, mn);
+        m = mn;
+        scratch[x * nc + c] = st.x;
+      }
+      const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+      for (int x = 0; x < parts; ++x)
+        scratch[x * nc + c] = part_weight(make_float2(scratch[x * nc + c], 0.0f), m) * inv;
+      if (a.lse) a.lse[where[c0 + c]] = row_lse(m, l);
+    }
+    named_sync(1, threads);
+    for (int e0 = tid; e0 < nc * kQ; e0 += threads * kE) {
+      float4 o[kE];
+#pragma unroll
+      for (int k = 0; k < kE; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+      for (int x = 0; x < parts; ++x) {
+        const float* from = a.part + (size_t)part_slot(s, x) * a.ct * D;
+#pragma unroll
+        for (int k = 0; k < kE; ++k) {
+          const int e = e0 + k * threads, c = e / kQ;
+          if (c >= nc) continue;
+          const float4 w = __ldcg(reinterpret_cast<const float4*>(from + (size_t)c0 * D) + e);
+          const float f = scratch[x * nc + c];
+          if (f != 0.0f) {  // a part that saw nothing adds nothing
+            o[k].x = fmaf(w.x, f, o[k].x);
+            o[k].y = fmaf(w.y, f, o[k].y);
+            o[k].z = fmaf(w.z, f, o[k].z);
+            o[k].w = fmaf(w.w, f, o[k].w);
+          }
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kE; ++k) {
+        const int e = e0 + k * threads, c = e / kQ;
+        if (c < nc) store4(static_cast<__nv_bfloat16*>(a.out) + where[c0 + c] * D + 4 * (e % kQ), o[k]);
+      }
+    }
+    named_sync(1, threads);
+  }
+}
+
 // ---------------------------------------------------------------------------
 // D: head dimension.  CG: groups of 8 columns per softmax thread.  H: sets of
 // four softmax warps (they split the columns).
 // ---------------------------------------------------------------------------
 template <int D, int CG, int H>
-__global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
+__global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
     attend_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                      const __grid_constant__ AttendLaunch a, const __grid_constant__ TcPlan t) {
-  constexpr int kCols = H == 1 ? 32 : kTcMaxCols;  // most columns of an item
+  constexpr int kSetCols = CG * 8;          // most columns of a set
+  constexpr int kCols = H * kSetCols;       // and of an item
   constexpr int kSlotBytes = (D / 64) * kHalfBytes;
-  // One set: two buffers of scores, of weights and of queries.  Two sets: one of
-  // each (the scores are in registers before the next tile's are due, and the
-  // sets take turns at the weights), which leaves room for tiles in flight.
-  constexpr int SB = H == 1 ? 2 : 1, PB = SB, QB = SB;
-  constexpr int kSetCols = CG * 8;                      // most columns of a set
-  constexpr int kOut = SB * ((kCols + 31) / 32 * 32);   // TMEM columns of the scores; then per set 2 kSetCols of O^T
+  // One set: two buffers of scores and two of weights.  Two sets: one of each
+  // (the scores are in registers before the next tile's are due, and the sets
+  // take turns at the weights), which leaves room for tiles in flight.
+  constexpr int SB = H == 1 ? 2 : 1, PB = SB, QB = H == 1 && !two_per_sm(D, CG) ? 2 : 1;
+  constexpr int kScores = (kCols + 31) / 32 * 32, kOut = SB * kScores;  // TMEM columns; then per set 2 kSetCols of O^T
   constexpr int kTmemCols = H == 1 ? 128 : 512;
-  static_assert(kOut + 2 * kSetCols * H <= kTmemCols, "scores and outputs fit TMEM");
+  static_assert(kOut + 2 * kCols <= kTmemCols, "scores and outputs fit TMEM");
   constexpr int kSoftThreads = 128 * H;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  __shared__ uint64_t full[kMaxSlots], empty[kMaxSlots], s_full[2], s_free[2], p_full[2], p_free[2], o_done[2], o_free, drained, q_full[2],
+  __shared__ uint64_t full[kMaxSlots], empty[kMaxSlots], s_full[2], s_free[2], p_full[2], p_free[2], o_free, drained, q_full[2],
       q_free[2], seg_full[kSegRing], seg_free[kSegRing];
   __shared__ Segment segs[kSegRing];
   __shared__ Share share;
   __shared__ long long sums[32];
   __shared__ int tile_bad[kBadRing];
-  __shared__ __align__(16) float sM[kCols + 16], sF[kCols], red[4][kCols];
+  // per set and column: the reference's negative (-inf: no column), a factor, maxima and sums per warp
+  __shared__ __align__(16) float sN[kCols], sF[kCols], red[4][kCols];
   __shared__ int2 sPage[2][16];      // a tile's boxes: page, first position in it
   __shared__ __align__(16) int sRow[kCols];        // position of the column's row
   __shared__ long long sOut[kCols];  // where the column goes
@@ -319,7 +459,6 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
       mbar_init(&s_free[k], 4 * H);
       mbar_init(&p_full[k], 4);
       mbar_init(&p_free[k], 1);
-      mbar_init(&o_done[k], 1);
       mbar_init(&q_full[k], 1);
       mbar_init(&q_free[k], 1);
     }
@@ -369,48 +508,51 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
     const int st = tid - 128;                         // of kSoftThreads
     const int tl = quad * 32 + lane;                  // this thread's position in a tile, and its d of O^T
     const uint32_t lanes = (uint32_t)(32 * quad) << 16;
+    const f32x2 c2 = pair(a.c2, a.c2);
+    float *const ref = sN + hf * kSetCols, *const factor = sF + hf * kSetCols;  // this set's
     bool failed = false;
     int T = 0;
     int U = 0;       // units (tile, set) before this tile
-    int done = 0;    // of this set
+    int mine_u = 0;  // this set's last unit
     RingPos vp{1, 0u};
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       if (!failed && !__all_sync(0xFFFFFFFFu, wait_phase(bar, parity & 1u, a.status))) failed = true;
     };
-    // The second product of this set's last unit.  A wait by parity must not
-    // come two phases late: with one set, p_free of the unit's own buffer, whose
-    // phase before was waited for when the buffer was taken; with two, o_done,
-    // waited for before every unit, after which p_free, too, is at most one
-    // phase (the other set's) behind the one the unit needs.
-    auto wait_output = [&]() {
-      if constexpr (H == 1) wait(&p_free[(done - 1) & 1], (done - 1) >> 1);
-      else wait(&o_done[hf], done - 1);
-    };
+    // The second product of unit u.  Units alternate between two barriers, so
+    // that a wait (by parity) is never two phases early: whoever waits for u has
+    // waited for u - 2, or for something after it.
+    auto wait_unit = [&](int u) { wait(&p_free[u & 1], (uint32_t)u >> 1); };
     for (int n = 0;; ++n) {
       const Segment& s = segs[n % kSegRing];  // given back at the segment's end
       wait(&seg_full[n % kSegRing], n / kSegRing);
-      if (named_or(1, kSoftThreads, failed)) {  // no one has left the last segment's epilogue behind
+      if (named_or(1, kSoftThreads, failed)) {  // no one has left the last segment's end behind
         aborted = 1;
         break;
       }
       if (s.request < 0) break;
       const int p_first = s.p + s.col0 / a.G, p_last = s.p + (s.col0 + s.cols - 1) / a.G, ntiles = s.ntiles;
-      const int N = (s.cols + 15) / 16 * 16, wide = set_cols<H>(N);
+      const int cols = s.cols, N = (cols + 15) / 16 * 16, wide = set_cols<H>(N);
       const int cb = hf * wide, gc = max(0, min(wide, N - cb)) / 8;  // this set's columns: gc groups of 8 from cb
       const int sets = (N + wide - 1) / wide;
+      const ItemTiles tiles = s.tiles;
+      const int tile0 = s.tile0;
+      if (n == 0) load_queries<D>(a, s, ring + t.q_off, st, kSoftThreads);
       for (int c = st; c < N; c += kSoftThreads) {
-        const int cc = min(c, s.cols - 1);
-        sRow[c] = s.p + (s.col0 + cc) / a.G;
+        const int cc = min(c, cols - 1);
+        const int at = (c < wide ? c : kSetCols + c - wide);
+        sRow[at] = s.p + (s.col0 + cc) / a.G;
         sOut[c] = out_index(a, s, cc);
       }
+      if (tl < kSetCols) ref[tl] = tl < gc * 8 ? -kNoMax : -INFINITY;
       if (st == 0) poison = 0;
       named_sync(1, kSoftThreads);
-      float l[CG * 8];
+      if (n == 0 && st == 0) mbar_arrive(&q_full[0]);
+      f32x2 l[CG * 4];
 #pragma unroll
-      for (int j = 0; j < CG * 8; ++j) l[j] = 0.0f;
+      for (int j = 0; j < CG * 4; ++j) l[j] = 0ull;
 
       for (int x = 0; x < ntiles; ++x, ++T) {
-        const int t0 = tile_start<kTile>(s.tiles, s.tile0 + x), b = T % SB;
+        const int t0 = tile_start<kTile>(tiles, tile0 + x), b = T % SB;
         wait(&s_full[b], T / SB);
         tc_fence_after();
         const int bads = tile_bad[T % kBadRing];
@@ -419,19 +561,25 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
                           bads != 0;
         const int pos = t0 + tl;
         const bool gone = edge && (bads >> (tl / t.chunk)) & 1;
-        // scores; -inf where masked
+        // scores; -inf where masked.  Columns past this set's are whatever TMEM
+        // holds: their reference makes every weight of theirs 0 (or NaN), and
+        // nothing of it is stored.
         float v[CG * 8];
-        if constexpr (H == 1) tmem_ld32(tmem + b * (kOut / SB) + lanes + cb, v);
-        else tmem_ld80(tmem + lanes + cb, v);
+        {
+          const uint32_t at = tmem + b * kScores + lanes + cb;
+          if constexpr (CG == 2) tmem_ld16(at, v);
+          else if constexpr (CG == 4) tmem_ld32(at, v);
+          else if constexpr (CG == 6) tmem_ld48(at, v);
+          else tmem_ld80(at, v);
+        }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&s_free[b]);
         if (edge) {
 #pragma unroll
           for (int g = 0; g < CG; ++g) {
-            if (g >= gc) break;
             int r[8];
-            load_rows(r, sRow + cb + g * 8);
+            load_rows(r, sRow + hf * kSetCols + g * 8);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
               const bool seen = pos <= r[j] && (a.window == 0 || pos > r[j] - a.window || pos < a.sinks) && !gone;
@@ -442,55 +590,57 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
         // ---- does a score exceed its column's reference by too much? ----
         bool grow = x == 0;
         if (x > 0) {
-          float top = -INFINITY;
+          float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
           for (int g = 0; g < CG; ++g) {
-            if (g >= gc) break;
-            float m[8];
-            load_ref(m, sM + cb + g * 8);
+            f32x2 m[4];
+            load_pairs(m, ref + g * 8);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) top = fmaxf(top, fmaf(v[8 * g + j], a.c2, -m[j]));
+            for (int j = 0; j < 4; ++j) {
+              const float2 d = unpair(fma2(pair(v[8 * g + 2 * j], v[8 * g + 2 * j + 1]), c2, m[j]));
+              top[j & 1] = max3(top[j & 1], d.x, d.y);
+            }
           }
-          grow = named_or(2 + hf, 128, top > kGrowth || failed);
+          grow = named_or(2 + hf, 128, fmaxf(top[0], top[1]) > kGrowth || failed);
         }
         if (grow) {
           // new references: the columns' maxima so far
 #pragma unroll
           for (int g = 0; g < CG; ++g) {
-            if (g >= gc) break;
             float mine = 0.0f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
               const float r = warp_max(v[8 * g + j]);
               if (lane == j) mine = r * a.c2;
             }
-            if (lane < 8) red[quad][cb + g * 8 + lane] = mine;
+            if (lane < 8) red[quad][hf * kSetCols + g * 8 + lane] = mine;
           }
           named_sync(2 + hf, 128);
           if (tl < gc * 8) {
-            const int c = cb + tl;
-            const float old = x == 0 ? kNoMax : sM[c];
+            const int c = hf * kSetCols + tl;
+            const float old = -ref[tl];
             const float m = fmaxf(old, fmaxf(fmaxf(red[0][c], red[1][c]), fmaxf(red[2][c], red[3][c])));
-            sF[c] = ex2_approx(old - m);
-            sM[c] = m;
+            factor[tl] = ex2_approx(old - m);
+            ref[tl] = -m;
           }
-          if (x > 0 && gc > 0) wait_output();  // O^T is complete up to the last tile
+          if (x > 0 && gc > 0) wait_unit(mine_u);  // O^T is complete up to the last tile
           failed = named_or(2 + hf, 128, failed);
           if (x > 0) {
             tc_fence_after();
 #pragma unroll
             for (int g = 0; g < CG; ++g) {
               if (g >= gc) break;
-              float f[8], o[8];
-              load_ref(f, sF + cb + g * 8);
+              f32x2 f[4];
+              float o[8];
+              load_pairs(f, factor + g * 8);
 #pragma unroll
-              for (int j = 0; j < 8; ++j) l[8 * g + j] *= f[j];
+              for (int j = 0; j < 4; ++j) l[4 * g + j] = mul2(l[4 * g + j], f[j]);
 #pragma unroll
               for (int part = 0; part < 2; ++part) {
                 const uint32_t at = tO + lanes + hf * 2 * kSetCols + part * gc * 8 + g * 8;
                 tmem_ld8(at, o);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) o[j] *= f[j];
+                for (int j = 0; j < 8; ++j) o[j] *= factor[g * 8 + j];
                 tmem_st8(at, o);
               }
             }
@@ -498,37 +648,38 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
           }
         }
         // ---- weights ----
-        const int u = U + hf, pb = u % PB;
 #pragma unroll
         for (int g = 0; g < CG; ++g) {
-          if (g >= gc) break;
-          float m[8];
-          load_ref(m, sM + cb + g * 8);
+          f32x2 m[4];
+          load_pairs(m, ref + g * 8);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            v[8 * g + j] = ex2_approx(fmaf(v[8 * g + j], a.c2, -m[j]));
-            l[8 * g + j] += v[8 * g + j];
+          for (int j = 0; j < 4; ++j) {
+            const float2 d = unpair(fma2(pair(v[8 * g + 2 * j], v[8 * g + 2 * j + 1]), c2, m[j]));
+            v[8 * g + 2 * j] = ex2_approx(d.x);
+            v[8 * g + 2 * j + 1] = ex2_approx(d.y);
+            l[4 * g + j] = add2(l[4 * g + j], pair(v[8 * g + 2 * j], v[8 * g + 2 * j + 1]));
           }
         }
+        const int u = U + hf;
         if (gc > 0) {
-          if (H > 1 && done > 0) wait_output();
-          if (u >= PB) wait(&p_free[pb], u / PB - 1);
+          mine_u = u;
+          if (u >= PB) wait_unit(u - PB);  // the buffer's last reader
+        }
+        {
           const uint32_t p_part = gc * (kPChunkBytes / 2);  // the upper halves' bytes; then the rest's
-          const uint32_t pw = ring + t.p_off + pb * t.p_bytes + tl * 32;
+          const uint32_t pw = ring + t.p_off + (u % PB) * t.p_bytes + tl * 32;
           const uint32_t swap = (uint32_t)((tl >> 2) & 1) << 4;
 #pragma unroll
           for (int g = 0; g < CG; ++g) {
-            if (g >= gc) break;
             uint32_t hi[4], lo[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) split_bf16(v[8 * g + 2 * j], v[8 * g + 2 * j + 1], &hi[j], &lo[j]);
             const uint32_t at = pw + (g >> 1) * kPChunkBytes + (((uint32_t)(g & 1) << 4) ^ swap);
-            st_shared16(at, hi);
-            st_shared16(at + p_part, lo);
+            st_shared16_if(g < gc, at, hi);
+            st_shared16_if(g < gc, at + p_part, lo);
           }
         }
         U += sets;
-        if (gc > 0) ++done;
         if (edge && hf == 0) {
           // ---- values that rows must not see ----
           // seen by the last row alone or by the first alone: between the two
@@ -566,51 +717,65 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
         tc_fence_before();
         proxy_fence();
         __syncwarp();
-        if (lane == 0 && gc > 0) mbar_arrive(&p_full[pb]);
+        if (lane == 0 && gc > 0) mbar_arrive(&p_full[u & 1]);
       }
 
       // ---- the item's result, or this part's ----
 #pragma unroll
       for (int g = 0; g < CG; ++g) {
-        if (g >= gc) break;
         float mine[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) mine[j] = l[8 * g + j];
+        for (int j = 0; j < 4; ++j) {
+          const float2 w = unpair(l[4 * g + j]);
+          mine[2 * j] = w.x;
+          mine[2 * j + 1] = w.y;
+        }
         const float sum = column_sum8(mine, lane);
-        if ((lane & 3) == 0) red[quad][cb + g * 8 + (lane >> 2)] = sum;
+        if ((lane & 3) == 0) red[quad][hf * kSetCols + g * 8 + (lane >> 2)] = sum;
       }
-      const bool whole = s.slot < 0;
-      named_sync(1, kSoftThreads);
-      for (int c = st; c < s.cols; c += kSoftThreads) {
+      const int slot = s.slot;
+      const bool whole = slot < 0;
+      named_sync(2 + hf, 128);
+      if (tl < gc * 8 && cb + tl < cols) {
+        const int c = hf * kSetCols + tl;
         const float sum = (red[0][c] + red[1][c]) + (red[2][c] + red[3][c]);
-        const float m = sum == 0.0f ? -INFINITY : sM[c];
-        sF[c] = whole ? (sum == 0.0f ? 0.0f : 1.0f / sum) : 1.0f;
-        if (!whole) a.part_stat[(size_t)s.slot * a.ct + c] = make_float2(m, sum);
-        else if (a.lse) a.lse[sOut[c]] = row_lse(m, sum);
+        const float m = sum == 0.0f ? -INFINITY : -ref[tl];
+        factor[tl] = whole ? (sum == 0.0f ? 0.0f : 1.0f / sum) : 1.0f;
+        if (!whole) a.part_stat[(size_t)slot * a.ct + cb + tl] = make_float2(m, sum);
+        else if (a.lse) a.lse[sOut[cb + tl]] = row_lse(m, sum);
       }
-      if (gc > 0) wait_output();
+      if (gc > 0) wait_unit(mine_u);
       tc_fence_after();
-      const bool poisoned = poison != 0;
       named_sync(1, kSoftThreads);
-      // two groups at a time: a thread has d = tl of 16 columns
+      const bool poisoned = poison != 0;
+      // sixteen columns at a time, this thread's d = tl of each
 #pragma unroll 1
       for (int g = 0; g < gc; g += 2) {
         float o[16], rest[16];
         const uint32_t at = tO + lanes + hf * 2 * kSetCols + g * 8;
         tmem_ld16(at, o);
         tmem_ld16(at + gc * 8, rest);
-        if (tl < D) {
-          const int c0 = cb + g * 8;
+        if (D < 128 && tl >= D) continue;
+        const int c0 = cb + g * 8, nc = cols - c0;
 #pragma unroll
+        for (int j = 0; j < 16; ++j) o[j] += rest[j];
+        if (poisoned) {
           for (int j = 0; j < 16; ++j) {
-            const int c = c0 + j;
-            if (c >= s.cols) break;
-            o[j] += rest[j];
-            if (poisoned) o[j] += cleared_values<D>(a, s, sRow[c], tl);
-            o[j] *= sF[c];
-            if (whole) static_cast<__nv_bfloat16*>(a.out)[sOut[c] * D + tl] = __float2bfloat16(o[j]);
-            else a.part[((size_t)s.slot * a.ct + c) * D + tl] = o[j];
+            const float add = j < nc ? cleared_values<D>(a, s, sRow[hf * kSetCols + g * 8 + j], tl) : 0.0f;
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+              if (k == j) o[k] += add;
           }
+        }
+        if (whole) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            if (j < nc) static_cast<__nv_bfloat16*>(a.out)[sOut[c0 + j] * D + tl] = __float2bfloat16(o[j] * factor[g * 8 + j]);
+        } else {
+          float* part = a.part + ((size_t)slot * a.ct + c0) * D + tl;
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            if (j < nc) part[j * D] = o[j];
         }
       }
       tc_fence_before();
@@ -626,7 +791,8 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
         named_sync(1, kSoftThreads);
         if (last_sh) {
           __threadfence();
-          join_parts<__nv_bfloat16>(a, s, st, kSoftThreads);
+          // the weights' buffer is free: every product of the segment is complete
+          join_tc<D>(a, s, sOut, reinterpret_cast<float*>(smem + t.p_off), PB * t.p_bytes / 4, st, kSoftThreads);
         }
       }
       __syncwarp();
@@ -719,7 +885,7 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
             const int Nh = min(wide, N - h * wide);
             if (Nh <= 0) break;
             const int b = U % PB;
-            if (!wait_phase(&p_full[b], (uint32_t)((U / PB) & 1), a.status)) return false;
+            if (!wait_phase(&p_full[U & 1], (uint32_t)((U >> 1) & 1), a.status)) return false;
             tc_fence_after();
             const uint32_t idesc = umma_idesc_bf16(kTile, 2 * Nh) | kTransposeA | kTransposeB;
             const uint32_t w = lo_p(ring + t.p_off + b * t.p_bytes), tD = tO + h * 2 * kSetCols;
@@ -727,8 +893,7 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
             for (int kk = 0; kk < kTile / 16; ++kk)
               umma_bf16(tD, desc(v + kk * (2048 >> 4), kHiV), desc(w + kk * (512 >> 4), kHiP), idesc,
                         kk > 0 || !first ? 1u : 0u);
-            umma_commit(&p_free[b]);
-            umma_commit(&o_done[h]);
+            umma_commit(&p_free[U & 1]);
             ++U;
           }
           umma_commit(&empty[vp.slot]);
@@ -751,7 +916,7 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
             if (ok && T >= SB) ok = wait_phase(&s_free[b], (uint32_t)((T / SB - 1) & 1), a.status);
             if (!ok) break;
             tc_fence_after();
-            const uint32_t key = lo_kq(ring + kp.slot * kSlotBytes), tD = tmem + b * (kOut / SB);
+            const uint32_t key = lo_kq(ring + kp.slot * kSlotBytes), tD = tmem + b * kScores;
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk)
               umma_bf16(tD, desc(key + (((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4), kHiKQ),
@@ -775,7 +940,6 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
       __syncwarp();
     } else if (warp == 2) {
       // ---- queries: [64-element halves][column][128 bytes], 128-byte swizzle ----
-      constexpr int kVecs = D / 8;
       for (int n = 0;; ++n) {
         Segment s;
         if (!take(n, &s)) {
@@ -788,27 +952,8 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
           aborted = 1;
           break;
         }
-        const int N = (s.cols + 15) / 16 * 16;
-        const uint32_t dst = ring + t.q_off + b * a.ct * D * 2;
-        // a lane takes vector v of every kStep-th column; the column's row j and
-        // head g move along without divisions
-        constexpr int kStep = 32 / kVecs;
-        const int v = lane % kVecs;
-        int c = lane / kVecs, j = (s.col0 + c) / a.G, g = s.col0 + c - j * a.G;
-        const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q) + (int64_t)s.row0 * a.q_row +
-                                 (int64_t)s.head * a.G * D + v * 8;
-        for (; c < N; c += kStep) {
-          const bool real = c < s.cols;
-          cp_async16(dst + (v >> 3) * a.ct * 128 + c * 128 + (((v & 7) ^ (c & 7)) << 4),
-                     real ? q + (int64_t)j * a.q_row + g * D : q, real);
-          g += kStep;
-          while (g >= a.G) {
-            g -= a.G;
-            ++j;
-          }
-        }
-        asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
-        proxy_fence();
+        if (n == 0) continue;  // the softmax warps, idle then, load the first
+        load_queries<D>(a, s, ring + t.q_off + b * a.ct * D * 2, lane, 32);
         __syncwarp();
         if (lane == 0) mbar_arrive(&q_full[b]);
       }
@@ -842,8 +987,6 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, 1)
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
-constexpr int kSmemLimit = 227 * 1024;
-
 // One layer of K or V as [page][token][head][d], in boxes of `chunk` tokens
 // of 64 elements of one head.
 bool make_cache_map(CUtensorMap* map, const char* base, const AttendLaunch& a, int chunk) {
@@ -867,7 +1010,8 @@ cudaError_t launch_variant(const AttendLaunch& a, cudaStream_t stream) {
   t.chunk = a.page_size & -a.page_size;
   if (t.chunk > kTile) t.chunk = kTile;
   t.nchunk = kTile / t.chunk;
-  constexpr int QB = H == 1 ? 2 : 1, PB = QB;
+  constexpr int QB = H == 1 && !two_per_sm(D, CG) ? 2 : 1, PB = H == 1 ? 2 : 1;
+  constexpr int kPerSm = two_per_sm(D, CG) ? 2 : 1;
   const int set = H == 1 ? a.ct : (a.ct / 16 + 1) / 2 * 16;
   const int q_bytes = a.ct * D * 2, p_bytes = 2 * (set / 16) * kPChunkBytes, slot = (D / 64) * kHalfBytes;
   t.p_bytes = p_bytes;
@@ -880,12 +1024,14 @@ cudaError_t launch_variant(const AttendLaunch& a, cudaStream_t stream) {
     static_smem = (int)fa.sharedSizeBytes;
   }
   // dynamic shared memory starts behind the static one, on a 1024-byte boundary
-  const int room = kSmemLimit - (static_smem + 1023) / 1024 * 1024;
+  // (1 KB of an SM's 228 KB is reserved per CTA)
+  const int limit = 228 * 1024 / kPerSm - 1024;
+  const int room = limit - (static_smem + 1023) / 1024 * 1024;
   t.slots = (room - QB * q_bytes - PB * p_bytes) / slot;
   if (t.slots > kMaxSlots) t.slots = kMaxSlots;
   t.q_off = t.slots * slot;
   t.p_off = t.q_off + QB * q_bytes;
-  const int smem = t.p_off + PB * p_bytes + kSmemLimit - room - static_smem;  // and the gap before it
+  const int smem = t.p_off + PB * p_bytes + limit - room - static_smem;  // and the gap before it
   CUtensorMap tmK, tmV;
   if (!make_cache_map(&tmK, a.k, a, t.chunk) || !make_cache_map(&tmV, a.v, a, t.chunk)) return cudaErrorInvalidValue;
   const cudaError_t err =
@@ -902,13 +1048,17 @@ bool attend_tc_serves(int D, int dtype, int page_size, int64_t head_b, int64_t t
   return dtype == SPEC_BF16 && (D == 64 || D == 128) && page_size % 8 == 0 && head_b < far && token_b < far && page_b < far;
 }
 
+int attend_tc_ctas_per_sm(int D, int ct) { return two_per_sm(D, ct <= 16 ? 2 : 4) ? 2 : 1; }
+
 int attend_tc_columns(int cols) {
   const int n = (cols + kTcMaxCols - 1) / kTcMaxCols;  // column tiles, of equal width
   return ((cols + n - 1) / n + 15) / 16 * 16;
 }
 
 cudaError_t launch_attend_tc(const AttendLaunch& a, cudaStream_t stream) {
+  if (a.ct <= 16) return a.D == 64 ? launch_variant<64, 2, 1>(a, stream) : launch_variant<128, 2, 1>(a, stream);
   if (a.ct <= 32) return a.D == 64 ? launch_variant<64, 4, 1>(a, stream) : launch_variant<128, 4, 1>(a, stream);
+  if (a.ct <= 96) return a.D == 64 ? launch_variant<64, 6, 2>(a, stream) : launch_variant<128, 6, 2>(a, stream);
   return a.D == 64 ? launch_variant<64, 10, 2>(a, stream) : launch_variant<128, 10, 2>(a, stream);
 }
 

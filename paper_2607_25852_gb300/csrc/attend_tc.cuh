@@ -13,6 +13,9 @@ bool attend_tc_serves(int D, int dtype, int page_size, int64_t head_b, int64_t t
 // Columns per item for requests of up to `cols` columns.
 int attend_tc_columns(int cols);
 
+// CTAs of its grid per SM, for ct columns per item.
+int attend_tc_ctas_per_sm(int D, int ct);
+
 cudaError_t launch_attend_tc(const AttendLaunch& a, cudaStream_t stream);
 
 }  // namespace spec

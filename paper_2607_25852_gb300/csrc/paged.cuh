@@ -66,7 +66,7 @@ inline bool rows_shape_ok(int B, int K) {
 }
 
 inline bool table_shape_ok(int B, int max_pages, int pages, int page_size) {
-  return B >= 1 && max_pages >= 1 && pages >= 1 && page_size >= 1 && (long long)max_pages * page_size < (1LL << 31) &&
+  return B >= 1 && max_pages >= 1 && pages >= 1 && page_size >= 1 && (long long)max_pages * page_size <= (1LL << 30) &&
          (long long)B * max_pages < (1LL << 31);
 }
 

@@ -331,3 +331,32 @@ def test_writes_stay_inside(dtype, D, ps):
     c.call(ws=ws.t, out=out.t, lse=lse.t)
     assert_intact(ws=ws, out=out, lse=lse)
     assert torch.equal(out.t, want[0]) and torch.equal(lse.t, want[1])
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("K,G", [(0, 8), (3, 8), (5, 8), (7, 8), (10, 8), (11, 8), (15, 8), (16, 8), (31, 4)])
+def test_long_runs_of_every_width(D, K, G):
+    """Many tiles per CTA at every number of columns: a pipeline that mixes up
+    two uses of a buffer shows in runs longer than the buffers are deep.  Equal
+    requests must get equal results, whatever share of the work they fall into."""
+    B, p, Hkv = 40, 2900, 4
+    g = torch.Generator().manual_seed(K)
+    slots = (p + K) // 64 + 1
+    k = torch.randn((slots, 64, Hkv, D), generator=g).to(BF16).to(DEV)
+    v = torch.randn((slots, 64, Hkv, D), generator=g).to(BF16).to(DEV)
+    q1 = torch.randn((K + 1, Hkv * G, D), generator=g).to(BF16)
+    table = torch.arange(slots, dtype=torch.int32, device=DEV).repeat(B, 1)
+    q = q1.repeat(B, 1, 1).to(DEV)
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device=DEV)
+    ws = spec.attend_workspace(B, K, Hkv * G, Hkv, D, BF16, DEV)
+    st = torch.zeros(1, dtype=torch.int32, device=DEV)
+    pos = torch.full((B,), p, dtype=torch.int64, device=DEV)
+    want, want_lse, mass, big = ref.attend(q1, k, v, table, [p], ref.Rows([K], K), ref.sqrt_scale(D))
+    tol, tol_lse = ref.bounds(want, mass, big, p + K + 1, D, True)
+    for _ in range(10):
+        out.fill_(7.0)
+        spec.spec_attend(q, k, v, table, pos, B, K, out, ws, lse_out=lse, status=st)
+        assert int(st.item()) == 0
+        got = out.view(B, K + 1, -1, D).cpu().double()
+        assert ((got - want).abs() <= tol).all()
+        assert ((lse.view(B, K + 1, -1).cpu().double() - want_lse).abs() <= tol_lse).all()
