@@ -426,7 +426,7 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
   // One set: two buffers of scores and two of weights.  Two sets: one of each
   // (the scores are in registers before the next tile's are due, and the sets
   // take turns at the weights), which leaves room for tiles in flight.
-  constexpr int SB = H == 1 ? 2 : 1, PB = SB, QB = H == 1 && !two_per_sm(D, CG) ? 2 : 1;
+  constexpr int SB = H == 1 ? 2 : 1, PB = 2, QB = H == 1 && !two_per_sm(D, CG) ? 2 : 1;
   constexpr int kScores = (kCols + 31) / 32 * 32, kOut = SB * kScores;  // TMEM columns; then per set 2 kSetCols of O^T
   constexpr int kTmemCols = H == 1 ? 128 : 512;
   static_assert(kOut + 2 * kCols <= kTmemCols, "scores and outputs fit TMEM");
@@ -647,7 +647,8 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
             tmem_st_wait();
           }
         }
-        // ---- weights ----
+        // ---- weights, split in two, in registers: they take the scores' place ----
+        uint32_t w[CG][2][4];
 #pragma unroll
         for (int g = 0; g < CG; ++g) {
           f32x2 m[4];
@@ -655,9 +656,9 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const float2 d = unpair(fma2(pair(v[8 * g + 2 * j], v[8 * g + 2 * j + 1]), c2, m[j]));
-            v[8 * g + 2 * j] = ex2_approx(d.x);
-            v[8 * g + 2 * j + 1] = ex2_approx(d.y);
-            l[4 * g + j] = add2(l[4 * g + j], pair(v[8 * g + 2 * j], v[8 * g + 2 * j + 1]));
+            const float x0 = ex2_approx(d.x), x1 = ex2_approx(d.y);
+            l[4 * g + j] = add2(l[4 * g + j], pair(x0, x1));
+            split_bf16(x0, x1, &w[g][0][j], &w[g][1][j]);
           }
         }
         const int u = U + hf;
@@ -671,12 +672,9 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
           const uint32_t swap = (uint32_t)((tl >> 2) & 1) << 4;
 #pragma unroll
           for (int g = 0; g < CG; ++g) {
-            uint32_t hi[4], lo[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) split_bf16(v[8 * g + 2 * j], v[8 * g + 2 * j + 1], &hi[j], &lo[j]);
             const uint32_t at = pw + (g >> 1) * kPChunkBytes + (((uint32_t)(g & 1) << 4) ^ swap);
-            st_shared16_if(g < gc, at, hi);
-            st_shared16_if(g < gc, at + p_part, lo);
+            st_shared16_if(g < gc, at, w[g][0]);
+            st_shared16_if(g < gc, at + p_part, w[g][1]);
           }
         }
         U += sets;
@@ -1000,7 +998,9 @@ bool make_cache_map(CUtensorMap* map, const char* base, const AttendLaunch& a, i
   cuuint32_t box[4] = {64u, 1u, (cuuint32_t)chunk, 1u};
   cuuint32_t estr[4] = {1u, 1u, 1u, 1u};
   return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<char*>(base), dims, strides, box, estr,
-             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             // a head's row is 2 D bytes: fetching more would bring in another head's
+             a.D == 64 ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B : CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -1010,7 +1010,7 @@ cudaError_t launch_variant(const AttendLaunch& a, cudaStream_t stream) {
   t.chunk = a.page_size & -a.page_size;
   if (t.chunk > kTile) t.chunk = kTile;
   t.nchunk = kTile / t.chunk;
-  constexpr int QB = H == 1 && !two_per_sm(D, CG) ? 2 : 1, PB = H == 1 ? 2 : 1;
+  constexpr int QB = H == 1 && !two_per_sm(D, CG) ? 2 : 1, PB = 2;
   constexpr int kPerSm = two_per_sm(D, CG) ? 2 : 1;
   const int set = H == 1 ? a.ct : (a.ct / 16 + 1) / 2 * 16;
   const int q_bytes = a.ct * D * 2, p_bytes = 2 * (set / 16) * kPChunkBytes, slot = (D / 64) * kHalfBytes;
