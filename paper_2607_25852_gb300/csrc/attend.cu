@@ -364,10 +364,16 @@ extern "C" int spec_attend(const void* q, int64_t q_row_stride, int q_heads, con
   a.part_stat = reinterpret_cast<float2*>(base + g.stat_off);
   const int sms = std::min(device_sms(), kAttendMaxSms);
   a.min_tiles = 1;
+  a.lists = 1;
   cudaError_t err;
   if (attend_tc_serves(a.D, cache->dtype, a.page_size, a.head_b, a.token_b, a.page_b)) {
     a.ct = attend_tc_columns((K + 1) * a.G);
     a.ctas = sms * attend_tc_ctas_per_sm(a.D, a.ct);
+    // a list per head, if that leaves no more than one CTA in sixteen idle
+    if (a.ctas % a.Hkv <= a.ctas / 16) {
+      a.lists = a.Hkv;
+      a.ctas -= a.ctas % a.Hkv;
+    }
     err = launch_attend_tc(a, stream);
   } else {
     a.ct = kGenCols;

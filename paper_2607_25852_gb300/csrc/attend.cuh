@@ -9,6 +9,13 @@
 // and its last), so a fixed workspace of two partial results per CTA serves
 // any batch, a single long request fills the GPU, and ragged batches balance.
 // The last CTA to finish a part of an item adds the parts up, in CTA order.
+//
+// Lists.  Every key-value head has the same tiles, and the heads of a position
+// lie side by side in the usual cache.  So where the CTAs divide evenly enough
+// among the heads, each head is a list of its own: consecutive CTAs take
+// different heads of the same positions at the same time, and the pieces they
+// read make whole DRAM pages.  Otherwise one list holds the heads one after
+// another.
 #pragma once
 
 #include "paged.cuh"
@@ -36,6 +43,7 @@ struct AttendLaunch {
   float2* part_stat;  // [2 * ctas][ct] (maximum in log2 units, sum)
   uint32_t* arrived;  // [ctas], zero between calls
   int ctas, min_tiles;
+  int lists;          // 1, or one per key-value head
 };
 
 // The tiles of positions that rows at positions p_first..p_last see: the
@@ -94,33 +102,43 @@ __device__ __forceinline__ int head_units(const AttendLaunch& a, const AttendRow
   return n;
 }
 
-// A CTA's share: units [u0, u1) of `units`, starting in request `request`
-// whose first unit is `base`.
+// A CTA's share: units [u0, u1) of its list's `units`, starting in request
+// `request`, whose first unit is `base`.
 struct Share {
   long long units, u0, u1, base;
-  int ctas, request;
+  int ctas, cta;   // of the list, and this one's place among them
+  int per;         // units of one head of the request
+  int request;
+  AttendRows rows; // of the request
 };
+
+// x * y / z for 0 <= x < z, without a 64-bit division where 32 bits hold it.
+__device__ __forceinline__ long long scale_floor(long long x, long long y, int z) {
+  const long long p = x * y;
+  return p < (1LL << 31) ? (long long)((uint32_t)p / (uint32_t)z) : p / z;
+}
 
 // All threads of the CTA (a multiple of 32, at most 1024).
 template <int TT>
 __device__ void find_share(const AttendLaunch& a, Share* sh, long long* sums) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
   const int B = a.rows.B, step = blockDim.x;
-  if (threadIdx.x == 0) sh->request = -1;
+  const int heads = a.lists > 1 ? 1 : a.Hkv;  // of a list
   // pass 0: the total; pass 1: the request in which this CTA's range starts.
   // A batch of at most one request per thread does both with one scan.
-  long long carry = 0;
   const int passes = B <= step ? 1 : 2;
   for (int pass = 0; pass < passes; ++pass) {
-    carry = 0;
+    long long carry = 0;
     for (int i0 = 0; i0 < B; i0 += step) {
       const int i = i0 + threadIdx.x;
-      long long mine = 0;
+      AttendRows r{0, 0, 0, false};
+      int per = 0;
       if (i < B) {
-        const AttendRows r = attend_rows(a, i);
-        mine = (long long)head_units<TT>(a, r) * a.Hkv;
+        r = attend_rows(a, i);
+        per = head_units<TT>(a, r);
         if (r.bad && pass == 0 && blockIdx.x == 0) report(a.status, SPEC_ERR_BAD_INPUT);
       }
+      const long long mine = (long long)per * heads;
       long long incl = mine;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -131,37 +149,40 @@ __device__ void find_share(const AttendLaunch& a, Share* sh, long long* sums) {
       __syncthreads();
       long long before = carry, total = carry;
       for (int w = 0; w < warps; ++w) {
-        if (w < warp) before += sums[w];
-        total += sums[w];
+        const long long x = sums[w];
+        if (w < warp) before += x;
+        total += x;
       }
       incl += before;
       carry = total;
-      __syncthreads();
-      if (pass == passes - 1) {
-        if (passes == 1 && threadIdx.x == 0) {
-          sh->units = total;
-          const long long most = (total + a.min_tiles - 1) / a.min_tiles;
-          sh->ctas = (int)(most < a.ctas ? most : a.ctas);
-          const int g = blockIdx.x;
-          sh->u0 = g < sh->ctas ? g * total / sh->ctas : 0;
-          sh->u1 = g < sh->ctas ? (g + 1) * total / sh->ctas : 0;
-        }
-        __syncthreads();
-        if (mine > 0 && incl - mine <= sh->u0 && sh->u0 < incl) {
-          sh->request = i;
-          sh->base = incl - mine;
-        }
+      if (passes == 2) __syncthreads();  // the sums may be written again
+      if (pass < passes - 1) continue;
+      if (passes == 2) total = sh->units;
+      // this CTA's range: every thread that may hold its start works it out
+      const int most = a.ctas / a.lists;
+      const long long want = (total + a.min_tiles - 1) / a.min_tiles;
+      const int ctas = (int)(want < most ? want : most), c = (int)blockIdx.x / a.lists;
+      long long u0 = 0, u1 = 0;
+      if (c < ctas) {
+        u0 = scale_floor(c, total, ctas);
+        u1 = scale_floor(c + 1, total, ctas);
+      }
+      if (mine > 0 && incl - mine <= u0 && u0 < incl) {
+        sh->request = i;
+        sh->base = incl - mine;
+        sh->per = per;
+        sh->rows = r;
+      }
+      if (threadIdx.x == 0) {
+        sh->units = total;
+        sh->ctas = ctas;
+        sh->cta = c;
+        sh->u0 = u0;
+        sh->u1 = u1;
       }
     }
     if (passes == 2 && pass == 0) {
-      if (threadIdx.x == 0) {
-        sh->units = carry;
-        const long long most = (carry + a.min_tiles - 1) / a.min_tiles;
-        sh->ctas = (int)(most < a.ctas ? most : a.ctas);
-        const int g = blockIdx.x;
-        sh->u0 = g < sh->ctas ? g * carry / sh->ctas : 0;
-        sh->u1 = g < sh->ctas ? (g + 1) * carry / sh->ctas : 0;
-      }
+      if (threadIdx.x == 0) sh->units = carry;
       __syncthreads();
     }
   }
@@ -177,7 +198,7 @@ struct Segment {
   ItemTiles tiles;
   int tile0, ntiles;   // the run
   int slot;            // where its partial result goes; -1: it is the whole item
-  int first_cta, parts;
+  int first_cta, step, parts;  // the CTAs that share the item: first_cta, first_cta + step, ...
 };
 
 // Walks the segments of a CTA's share, one thread.
@@ -185,18 +206,24 @@ template <int TT>
 struct Walk {
   const AttendLaunch& a;
   const Share& sh;
-  long long u, base;  // next unit; first unit of the item's request
-  int i, h, c0;
+  long long u;        // next unit
+  int i, h, c0, heads, list;
   AttendRows r;
   long long item;     // first unit of the item (i, h, c0)
   ItemTiles t;
 
-  __device__ Walk(const AttendLaunch& a_, const Share& s_) : a(a_), sh(s_), u(s_.u0), i(s_.request) {
+  __device__ Walk(const AttendLaunch& a_, const Share& s_) : a(a_), sh(s_), u(s_.u0) {
     if (u >= sh.u1) return;
-    r = attend_rows(a, i);
-    const int per = head_units<TT>(a, r);
-    h = (int)((u - sh.base) / per);
-    item = sh.base + (long long)h * per;
+    heads = a.lists > 1 ? 1 : a.Hkv;
+    list = a.lists > 1 ? (int)blockIdx.x % a.lists : 0;
+    i = sh.request;
+    r = sh.rows;
+    h = 0;
+    item = sh.base;
+    while (item + sh.per <= u) {
+      item += sh.per;
+      ++h;
+    }
     c0 = 0;
     set_tiles();
     while (item + t.count <= u) {
@@ -209,13 +236,17 @@ struct Walk {
     const int c1 = min(r.count * a.G, c0 + a.ct) - 1;
     t = item_tiles<TT>(a, r.p + c0 / a.G, r.p + c1 / a.G);
   }
-  // The CTA whose range holds unit x.
-  __device__ __forceinline__ int owner(long long x) const { return (int)(((x + 1) * sh.ctas - 1) / sh.units); }
+  // The CTA (of the list) whose range holds unit x, found from a CTA that starts
+  // at or after it, or before it: ranges differ by at most one unit in length.
+  __device__ __forceinline__ int owner(long long x) const {
+    const long long p = (x + 1) * sh.ctas - 1;
+    return p < (1LL << 31) && sh.units < (1LL << 31) ? (int)((uint32_t)p / (uint32_t)sh.units) : (int)(p / sh.units);
+  }
 
   __device__ bool next(Segment* s) {
     if (u >= sh.u1) return false;
     s->request = i;
-    s->head = h;
+    s->head = a.lists > 1 ? list : h;
     s->row0 = r.row0;
     s->col0 = c0;
     s->cols = min(r.count * a.G, c0 + a.ct) - c0;
@@ -226,12 +257,13 @@ struct Walk {
     s->ntiles = (int)((end < sh.u1 ? end : sh.u1) - u);
     s->slot = -1;
     s->first_cta = blockIdx.x;
+    s->step = a.lists;
     s->parts = 1;
     if (s->ntiles < t.count) {
-      const int f = owner(item), l = owner(end - 1);
-      s->first_cta = f;
+      const int f = u > item ? owner(item) : sh.cta, l = end > sh.u1 ? owner(end - 1) : sh.cta;
+      s->first_cta = f * a.lists + list;
       s->parts = l - f + 1;
-      s->slot = 2 * (int)blockIdx.x + ((int)blockIdx.x == f ? 1 : 0);
+      s->slot = 2 * (int)blockIdx.x + (sh.cta == f ? 1 : 0);
     }
     u += s->ntiles;
     if (u < sh.u1) {  // the next item
@@ -239,7 +271,7 @@ struct Walk {
       c0 += a.ct;
       if (c0 >= r.count * a.G) {
         c0 = 0;
-        if (++h == a.Hkv) {
+        if (++h == heads) {
           h = 0;
           do {
             r = attend_rows(a, ++i);
@@ -254,7 +286,9 @@ struct Walk {
 
 // Slot of the x-th part of a divided item: the first CTA's part is the tail of
 // its range, every other's the head.
-__device__ __forceinline__ int part_slot(const Segment& s, int x) { return 2 * (s.first_cta + x) + (x == 0 ? 1 : 0); }
+__device__ __forceinline__ int part_slot(const Segment& s, int x) {
+  return 2 * (s.first_cta + x * s.step) + (x == 0 ? 1 : 0);
+}
 
 // Where column c of a segment goes: packed row * Hq + query head.
 __device__ __forceinline__ long long out_index(const AttendLaunch& a, const Segment& s, int c) {

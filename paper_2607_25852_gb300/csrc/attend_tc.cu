@@ -26,7 +26,7 @@
 // (the scores of tile t + 1 before the second product of tile t); 2 loads
 // queries; 3 walks the CTA's share of the work; the rest are the softmax, one
 // TMEM lane quarter per warp, in one set or in two that halve the columns and
-// take turns at the buffer of the weights.
+// take turns at two buffers of the weights.
 //
 // Positions that no row sees must not reach the result whatever they hold: a
 // weight of 0 does not cancel an infinite or NaN value, so in tiles at an edge
@@ -175,17 +175,17 @@ __device__ __forceinline__ void tmem_ld48(uint32_t addr, float* v) {
 #pragma unroll
   for (int k = 0; k < 48; ++k) v[k] = __uint_as_float(r[k]);
 }
-__device__ __forceinline__ void tmem_ld80(uint32_t addr, float* v) {
-  uint32_t r[80];
+__device__ __forceinline__ void tmem_ld72(uint32_t addr, float* v) {
+  uint32_t r[72];
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%80];\n\t"
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%64,%65,%66,%67,%68,%69,%70,%71,%72,%73,%74,%75,%76,%77,%78,%79}, [%81];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%72];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%64,%65,%66,%67,%68,%69,%70,%71}, [%73];\n\t"
       "tcgen05.wait::ld.sync.aligned;"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]), "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]), "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63]), "=r"(r[64]), "=r"(r[65]), "=r"(r[66]), "=r"(r[67]), "=r"(r[68]), "=r"(r[69]), "=r"(r[70]), "=r"(r[71]), "=r"(r[72]), "=r"(r[73]), "=r"(r[74]), "=r"(r[75]), "=r"(r[76]), "=r"(r[77]), "=r"(r[78]), "=r"(r[79])
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]), "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]), "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63]), "=r"(r[64]), "=r"(r[65]), "=r"(r[66]), "=r"(r[67]), "=r"(r[68]), "=r"(r[69]), "=r"(r[70]), "=r"(r[71])
       : "r"(addr), "r"(addr + 64)
       : "memory");
 #pragma unroll
-  for (int k = 0; k < 80; ++k) v[k] = __uint_as_float(r[k]);
+  for (int k = 0; k < 72; ++k) v[k] = __uint_as_float(r[k]);
 }
 __device__ __forceinline__ void tmem_st8(uint32_t addr, const float* v) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(addr),
@@ -278,10 +278,10 @@ __device__ __forceinline__ void st_shared16_if(bool yes, uint32_t at, const uint
       "r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
       : "memory");
 }
-// Columns of each softmax set but the last, for an item of N (a multiple of 16).
+// Columns of each softmax set, for an item of N (a multiple of 16).
 template <int H>
 __device__ __forceinline__ int set_cols(int N) {
-  return H == 1 ? N : (N / 16 + 1) / 2 * 16;
+  return N / H;
 }
 __device__ __forceinline__ bool bf16_not_finite(uint32_t h) { return (h & 0x7F80u) == 0x7F80u; }
 
@@ -359,21 +359,31 @@ __device__ __forceinline__ void load_queries(const AttendLaunch& a, const Segmen
 // adds four consecutive d of up to four columns at a time, whose loads are in
 // flight together.  What a join costs is the latency of these loads.
 template <int D>
-__device__ void join_tc(const AttendLaunch& a, const Segment& s, const long long* where, float* scratch, int room,
+__device__ __noinline__ void join_tc(const AttendLaunch& a, const Segment& s, const long long* where, float* scratch, int room,
                         int tid, int threads) {
-  constexpr int kQ = D / 4, kE = 4;
+  constexpr int kQ = D / 4, kE = 4, kX = 4;
   const int parts = s.parts, most = max(1, room / parts);
   for (int c0 = 0; c0 < s.cols; c0 += most) {
     const int nc = min(most, s.cols - c0);
     for (int c = tid; c < nc; c += threads) {
+      constexpr int kBatch = 8;
       float m = -INFINITY, l = 0.0f;
-#pragma unroll 8
-      for (int x = 0; x < parts; ++x) {
-        const float2 st = __ldcg(a.part_stat + (size_t)part_slot(s, x) * a.ct + c0 + c);
-        const float mn = fmaxf(m, st.x);
-        l = l * part_weight(make_float2(m, l), mn) + st.y * part_weight(st, mn);
+      for (int x0 = 0; x0 < parts; x0 += kBatch) {
+        float2 st[kBatch];
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k)
+          st[k] = x0 + k < parts ? __ldcg(a.part_stat + (size_t)part_slot(s, x0 + k) * a.ct + c0 + c)
+                                 : make_float2(-INFINITY, 0.0f);
+        float mn = m;
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) mn = fmaxf(mn, st[k].x);
+        l *= part_weight(make_float2(m, l), mn);
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+          l = fmaf(st[k].y, part_weight(st[k], mn), l);
+          if (x0 + k < parts) scratch[(x0 + k) * nc + c] = st[k].x;
+        }
         m = mn;
-        scratch[x * nc + c] = st.x;
       }
       const float inv = l == 0.0f ? 0.0f : 1.0f / l;
       for (int x = 0; x < parts; ++x)
@@ -385,20 +395,31 @@ __device__ void join_tc(const AttendLaunch& a, const Segment& s, const long long
       float4 o[kE];
 #pragma unroll
       for (int k = 0; k < kE; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-      for (int x = 0; x < parts; ++x) {
-        const float* from = a.part + (size_t)part_slot(s, x) * a.ct * D;
+      for (int x0 = 0; x0 < parts; x0 += kX) {
+        float4 w[kX][kE];
 #pragma unroll
-        for (int k = 0; k < kE; ++k) {
-          const int e = e0 + k * threads, c = e / kQ;
-          if (c >= nc) continue;
-          const float4 w = __ldcg(reinterpret_cast<const float4*>(from + (size_t)c0 * D) + e);
-          const float f = scratch[x * nc + c];
-          if (f != 0.0f) {  // a part that saw nothing adds nothing
-            o[k].x = fmaf(w.x, f, o[k].x);
-            o[k].y = fmaf(w.y, f, o[k].y);
-            o[k].z = fmaf(w.z, f, o[k].z);
-            o[k].w = fmaf(w.w, f, o[k].w);
+        for (int y = 0; y < kX; ++y) {
+          if (x0 + y >= parts) break;
+          const float4* from = reinterpret_cast<const float4*>(a.part + ((size_t)part_slot(s, x0 + y) * a.ct + c0) * D);
+#pragma unroll
+          for (int k = 0; k < kE; ++k) {
+            const int e = e0 + k * threads;
+            w[y][k] = __ldcg(from + (e < nc * kQ ? e : tid));
+          }
+        }
+#pragma unroll
+        for (int y = 0; y < kX; ++y) {
+          if (x0 + y >= parts) break;
+#pragma unroll
+          for (int k = 0; k < kE; ++k) {
+            const int c = min((e0 + k * threads) / kQ, nc - 1);
+            const float f = scratch[(x0 + y) * nc + c];
+            if (f != 0.0f) {  // a part that saw nothing adds nothing
+              o[k].x = fmaf(w[y][k].x, f, o[k].x);
+              o[k].y = fmaf(w[y][k].y, f, o[k].y);
+              o[k].z = fmaf(w[y][k].z, f, o[k].z);
+              o[k].w = fmaf(w[y][k].w, f, o[k].w);
+            }
           }
         }
       }
@@ -423,17 +444,16 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
   constexpr int kSetCols = CG * 8;          // most columns of a set
   constexpr int kCols = H * kSetCols;       // and of an item
   constexpr int kSlotBytes = (D / 64) * kHalfBytes;
-  // One set: two buffers of scores and two of weights.  Two sets: one of each
-  // (the scores are in registers before the next tile's are due, and the sets
-  // take turns at the weights), which leaves room for tiles in flight.
-  constexpr int SB = H == 1 ? 2 : 1, PB = 2, QB = H == 1 && !two_per_sm(D, CG) ? 2 : 1;
+  // Two buffers of scores where they fit (else one: the scores are in registers
+  // before the next tile's are due), two of weights.
+  constexpr int SB = CG <= 6 ? 2 : 1, PB = 2, QB = H == 1 && !two_per_sm(D, CG) ? 2 : 1;
   constexpr int kScores = (kCols + 31) / 32 * 32, kOut = SB * kScores;  // TMEM columns; then per set 2 kSetCols of O^T
   constexpr int kTmemCols = H == 1 ? 128 : 512;
   static_assert(kOut + 2 * kCols <= kTmemCols, "scores and outputs fit TMEM");
   constexpr int kSoftThreads = 128 * H;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  __shared__ uint64_t full[kMaxSlots], empty[kMaxSlots], s_full[2], s_free[2], p_full[2], p_free[2], o_free, drained, q_full[2],
+  __shared__ uint64_t full[kMaxSlots], empty[kMaxSlots], s_full[2], s_free[2], p_full[2], p_free[4], o_free, drained, q_full[2],
       q_free[2], seg_full[kSegRing], seg_free[kSegRing];
   __shared__ Segment segs[kSegRing];
   __shared__ Share share;
@@ -459,6 +479,7 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
       mbar_init(&s_free[k], 4 * H);
       mbar_init(&p_full[k], 4);
       mbar_init(&p_free[k], 1);
+      mbar_init(&p_free[2 + k], 1);
       mbar_init(&q_full[k], 1);
       mbar_init(&q_free[k], 1);
     }
@@ -516,12 +537,13 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
     int mine_u = 0;  // this set's last unit
     RingPos vp{1, 0u};
     auto wait = [&](uint64_t* bar, uint32_t parity) {
-      if (!failed && !__all_sync(0xFFFFFFFFu, wait_phase(bar, parity & 1u, a.status))) failed = true;
+      // a lane's own finding until the next vote
+      if (!failed) failed = !wait_phase(bar, parity & 1u, a.status);
     };
-    // The second product of unit u.  Units alternate between two barriers, so
-    // that a wait (by parity) is never two phases early: whoever waits for u has
-    // waited for u - 2, or for something after it.
-    auto wait_unit = [&](int u) { wait(&p_free[u & 1], (uint32_t)u >> 1); };
+    // The second product of unit u.  A wait by parity must not come two phases
+    // early: with four barriers in turn that would be before unit u - 4 is done,
+    // and who waits for u knows of u - 2 H or later.
+    auto wait_unit = [&](int u) { wait(&p_free[u & 3], (uint32_t)u >> 2); };
     for (int n = 0;; ++n) {
       const Segment& s = segs[n % kSegRing];  // given back at the segment's end
       wait(&seg_full[n % kSegRing], n / kSegRing);
@@ -532,15 +554,13 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
       if (s.request < 0) break;
       const int p_first = s.p + s.col0 / a.G, p_last = s.p + (s.col0 + s.cols - 1) / a.G, ntiles = s.ntiles;
       const int cols = s.cols, N = (cols + 15) / 16 * 16, wide = set_cols<H>(N);
-      const int cb = hf * wide, gc = max(0, min(wide, N - cb)) / 8;  // this set's columns: gc groups of 8 from cb
-      const int sets = (N + wide - 1) / wide;
+      const int cb = hf * wide, gc = wide / 8;  // this set's columns: gc groups of 8 from cb
       const ItemTiles tiles = s.tiles;
       const int tile0 = s.tile0;
       if (n == 0) load_queries<D>(a, s, ring + t.q_off, st, kSoftThreads);
       for (int c = st; c < N; c += kSoftThreads) {
         const int cc = min(c, cols - 1);
-        const int at = (c < wide ? c : kSetCols + c - wide);
-        sRow[at] = s.p + (s.col0 + cc) / a.G;
+        sRow[c + (c >= wide ? kSetCols - wide : 0)] = s.p + (s.col0 + cc) / a.G;
         sOut[c] = out_index(a, s, cc);
       }
       if (tl < kSetCols) ref[tl] = tl < gc * 8 ? -kNoMax : -INFINITY;
@@ -570,7 +590,7 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
           if constexpr (CG == 2) tmem_ld16(at, v);
           else if constexpr (CG == 4) tmem_ld32(at, v);
           else if constexpr (CG == 6) tmem_ld48(at, v);
-          else tmem_ld80(at, v);
+          else tmem_ld72(at, v);
         }
         tc_fence_before();
         __syncwarp();
@@ -623,7 +643,7 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
             factor[tl] = ex2_approx(old - m);
             ref[tl] = -m;
           }
-          if (x > 0 && gc > 0) wait_unit(mine_u);  // O^T is complete up to the last tile
+          if (x > 0) wait_unit(mine_u);  // O^T is complete up to the last tile
           failed = named_or(2 + hf, 128, failed);
           if (x > 0) {
             tc_fence_after();
@@ -645,39 +665,45 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
               }
             }
             tmem_st_wait();
+            tc_fence_before();
           }
         }
-        // ---- weights, split in two, in registers: they take the scores' place ----
-        uint32_t w[CG][2][4];
+        // ---- weights, split in two.  With few columns a thread they stay in
+        // registers until their buffer is free, with many they are stored as they
+        // come.  The buffer's last reader is unit u - 2; with one set its product
+        // was issued before this tile's scores, so those say that it is done ----
+        const int u = U + hf;
+        mine_u = u;
+        constexpr bool kStoreNow = CG > 6;
+        const uint32_t pw = ring + t.p_off + (u % PB) * t.p_bytes + tl * 32;
+        const uint32_t swap = (uint32_t)((tl >> 2) & 1) << 4;
+        auto store = [&](int g, const uint32_t (&x)[2][4]) {
+          const int lo = gc + g;  // the rests' groups follow the upper halves'
+          st_shared16_if(g < gc, pw + (g >> 1) * kPChunkBytes + (((uint32_t)(g & 1) << 4) ^ swap), x[0]);
+          st_shared16_if(g < gc, pw + (lo >> 1) * kPChunkBytes + (((uint32_t)(lo & 1) << 4) ^ swap), x[1]);
+        };
+        uint32_t w[kStoreNow ? 1 : CG][2][4];
+        if (kStoreNow && H > 1 && u >= PB) wait_unit(u - PB);
 #pragma unroll
         for (int g = 0; g < CG; ++g) {
           f32x2 m[4];
           load_pairs(m, ref + g * 8);
+          uint32_t(&x)[2][4] = w[kStoreNow ? 0 : g];
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const float2 d = unpair(fma2(pair(v[8 * g + 2 * j], v[8 * g + 2 * j + 1]), c2, m[j]));
             const float x0 = ex2_approx(d.x), x1 = ex2_approx(d.y);
             l[4 * g + j] = add2(l[4 * g + j], pair(x0, x1));
-            split_bf16(x0, x1, &w[g][0][j], &w[g][1][j]);
+            split_bf16(x0, x1, &x[0][j], &x[1][j]);
           }
+          if (kStoreNow) store(g, x);
         }
-        const int u = U + hf;
-        if (gc > 0) {
-          mine_u = u;
-          if (u >= PB) wait_unit(u - PB);  // the buffer's last reader
-        }
-        {
-          const uint32_t p_part = gc * (kPChunkBytes / 2);  // the upper halves' bytes; then the rest's
-          const uint32_t pw = ring + t.p_off + (u % PB) * t.p_bytes + tl * 32;
-          const uint32_t swap = (uint32_t)((tl >> 2) & 1) << 4;
+        if (!kStoreNow) {
+          if (H > 1 && u >= PB) wait_unit(u - PB);
 #pragma unroll
-          for (int g = 0; g < CG; ++g) {
-            const uint32_t at = pw + (g >> 1) * kPChunkBytes + (((uint32_t)(g & 1) << 4) ^ swap);
-            st_shared16_if(g < gc, at, w[g][0]);
-            st_shared16_if(g < gc, at + p_part, w[g][1]);
-          }
+          for (int g = 0; g < CG; ++g) store(g, w[kStoreNow ? 0 : g]);
         }
-        U += sets;
+        U += H;
         if (edge && hf == 0) {
           // ---- values that rows must not see ----
           // seen by the last row alone or by the first alone: between the two
@@ -712,10 +738,9 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
           }
         }
         vp.step(2, t.slots);
-        tc_fence_before();
         proxy_fence();
         __syncwarp();
-        if (lane == 0 && gc > 0) mbar_arrive(&p_full[u & 1]);
+        if (lane == 0) mbar_arrive(&p_full[u & 1]);
       }
 
       // ---- the item's result, or this part's ----
@@ -742,7 +767,7 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
         if (!whole) a.part_stat[(size_t)slot * a.ct + cb + tl] = make_float2(m, sum);
         else if (a.lse) a.lse[sOut[cb + tl]] = row_lse(m, sum);
       }
-      if (gc > 0) wait_unit(mine_u);
+      wait_unit(mine_u);
       tc_fence_after();
       named_sync(1, kSoftThreads);
       const bool poisoned = poison != 0;
@@ -754,7 +779,7 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
         tmem_ld16(at, o);
         tmem_ld16(at + gc * 8, rest);
         if (D < 128 && tl >= D) continue;
-        const int c0 = cb + g * 8, nc = cols - c0;
+        const int c0 = cb + g * 8, nc = min(cols, cb + gc * 8) - c0;
 #pragma unroll
         for (int j = 0; j < 16; ++j) o[j] += rest[j];
         if (poisoned) {
@@ -780,9 +805,9 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(&o_free);
       if (!whole) {
-        __threadfence();
         named_sync(1, kSoftThreads);
         if (st == 0) {
+          __threadfence();
           last_sh = atomicAdd(a.arrived + s.first_cta, 1u) == (uint32_t)s.parts - 1 ? 1 : 0;
           if (last_sh) a.arrived[s.first_cta] = 0;
         }
@@ -880,18 +905,16 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
           const int wide = set_cols<H>(N);
 #pragma unroll
           for (int h = 0; h < H; ++h) {
-            const int Nh = min(wide, N - h * wide);
-            if (Nh <= 0) break;
             const int b = U % PB;
             if (!wait_phase(&p_full[U & 1], (uint32_t)((U >> 1) & 1), a.status)) return false;
             tc_fence_after();
-            const uint32_t idesc = umma_idesc_bf16(kTile, 2 * Nh) | kTransposeA | kTransposeB;
+            const uint32_t idesc = umma_idesc_bf16(kTile, 2 * wide) | kTransposeA | kTransposeB;
             const uint32_t w = lo_p(ring + t.p_off + b * t.p_bytes), tD = tO + h * 2 * kSetCols;
 #pragma unroll
             for (int kk = 0; kk < kTile / 16; ++kk)
               umma_bf16(tD, desc(v + kk * (2048 >> 4), kHiV), desc(w + kk * (512 >> 4), kHiP), idesc,
                         kk > 0 || !first ? 1u : 0u);
-            umma_commit(&p_free[U & 1]);
+            umma_commit(&p_free[U & 3]);
             ++U;
           }
           umma_commit(&empty[vp.slot]);
@@ -1012,8 +1035,7 @@ cudaError_t launch_variant(const AttendLaunch& a, cudaStream_t stream) {
   t.nchunk = kTile / t.chunk;
   constexpr int QB = H == 1 && !two_per_sm(D, CG) ? 2 : 1, PB = 2;
   constexpr int kPerSm = two_per_sm(D, CG) ? 2 : 1;
-  const int set = H == 1 ? a.ct : (a.ct / 16 + 1) / 2 * 16;
-  const int q_bytes = a.ct * D * 2, p_bytes = 2 * (set / 16) * kPChunkBytes, slot = (D / 64) * kHalfBytes;
+  const int q_bytes = a.ct * D * 2, p_bytes = a.ct / 8 / H * kPChunkBytes, slot = (D / 64) * kHalfBytes;
   t.p_bytes = p_bytes;
   // what the kernel's static shared memory takes, read once
   static int static_smem = -1;
@@ -1059,7 +1081,7 @@ cudaError_t launch_attend_tc(const AttendLaunch& a, cudaStream_t stream) {
   if (a.ct <= 16) return a.D == 64 ? launch_variant<64, 2, 1>(a, stream) : launch_variant<128, 2, 1>(a, stream);
   if (a.ct <= 32) return a.D == 64 ? launch_variant<64, 4, 1>(a, stream) : launch_variant<128, 4, 1>(a, stream);
   if (a.ct <= 96) return a.D == 64 ? launch_variant<64, 6, 2>(a, stream) : launch_variant<128, 6, 2>(a, stream);
-  return a.D == 64 ? launch_variant<64, 10, 2>(a, stream) : launch_variant<128, 10, 2>(a, stream);
+  return a.D == 64 ? launch_variant<64, 9, 2>(a, stream) : launch_variant<128, 9, 2>(a, stream);
 }
 
 }  // namespace spec
