@@ -342,40 +342,60 @@ def spec_shard_finish(races, S, decisions, B, K, V, temperature, seeds, request_
     _check(code, "spec_shard_finish")
 
 
+# The calls around a round's forward are made many times per token, so what they
+# do on the host counts: pointers go to ctypes as integers, and the current
+# stream comes from torch's own accessor where it has one.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream_handle(stream):
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is None:
+        return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(torch.cuda.current_device())
+
+
 def _cache(k, v):
     """struct spec_cache of K and V tensors [layers, pages, page_size, kv_heads, head_dim] (or without the first
     dimension), any strides but a contiguous last dimension."""
-    if k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.dim() not in (4, 5):
+    shape, stride, dtype = k.shape, k.stride(), k.dtype
+    if shape != v.shape or stride != v.stride() or dtype != v.dtype or len(shape) not in (4, 5):
         raise ValueError("k_cache and v_cache: 4 or 5 dimensions, the same shape, strides and dtype")
-    if k.stride(-1) != 1:
+    if stride[-1] != 1:
         raise ValueError("the head dimension of a cache must be contiguous")
-    shape = (1,) * (5 - k.dim()) + tuple(k.shape)
-    stride = (0,) * (5 - k.dim()) + tuple(k.stride())
-    return _native.Cache(k.data_ptr(), v.data_ptr(), _dtype(k), *shape[:5], *stride[:4])
+    if len(shape) == 4:
+        return _native.Cache(k.data_ptr(), v.data_ptr(), _dtype(k), 1, *shape, 0, *stride[:3])
+    return _native.Cache(k.data_ptr(), v.data_ptr(), _dtype(k), *shape, *stride[:4])
 
 
-def _rows(t, heads, head_dim, like, what):
+def _rows(t, heads, head_dim, dtype, what):
     """Pointer and row stride of packed rows [R, heads, head_dim]; rows may lie apart (a fused projection's view)."""
-    if t.dtype != like.dtype:
-        raise TypeError(f"{what}: the cache's dtype is {like.dtype}, not {t.dtype}")
-    if t.dim() != 3 or t.shape[1:] != (heads, head_dim):
+    if t.dtype != dtype:
+        raise TypeError(f"{what}: the cache's dtype is {dtype}, not {t.dtype}")
+    shape = t.shape
+    if len(shape) != 3 or shape[1] != heads or shape[2] != head_dim:
         raise ValueError(f"{what}: expected [rows, {heads}, {head_dim}]")
-    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != head_dim):
+    stride = t.stride()
+    if stride[2] != 1 or (heads > 1 and stride[1] != head_dim):
         raise ValueError(f"{what}: a row's heads must be contiguous")
-    return ctypes.c_void_p(t.data_ptr()), (t.stride(0) if t.shape[0] > 1 else heads * head_dim)
+    return t.data_ptr(), (stride[0] if shape[0] > 1 else heads * head_dim)
 
 
 def _table(page_table, B):
-    if page_table.dim() != 2 or page_table.shape[0] < B or page_table.dtype != torch.int32:
-        raise ValueError("page_table: expected int32 [B, max_pages]")
-    return _ptr(page_table), page_table.shape[1]
+    shape = page_table.shape
+    if len(shape) != 2 or shape[0] < B or page_table.dtype != torch.int32 or not page_table.is_contiguous():
+        raise ValueError("page_table: expected contiguous int32 [B, max_pages]")
+    return page_table.data_ptr(), shape[1]
 
 
 def _ints(t, n, what, dtype=torch.int32):
-    """Pointer of an integer tensor (or None) of at least n entries."""
-    if t is not None and (t.dtype != dtype or t.numel() < n):
-        raise ValueError(f"{what}: expected {dtype} with at least {n} entries")
-    return _ptr(t)
+    """Pointer of a contiguous integer tensor of at least n entries (or of None)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() < n or not t.is_contiguous():
+        raise ValueError(f"{what}: expected contiguous {dtype} with at least {n} entries")
+    return t.data_ptr()
 
 
 def spec_attend_workspace(B: int, K: int, q_heads: int, kv_heads: int, head_dim: int, dtype=torch.bfloat16) -> int:
@@ -395,36 +415,44 @@ def spec_attend(q, k_cache, v_cache, page_table, pos_base, B, K, out, ws, row_of
     """q and out [R, q_heads, head_dim]; k_cache and v_cache [layers, pages, page_size, kv_heads, head_dim] (or one
     layer, 4 dimensions); page_table int32 [B, max_pages]; scale 1 / sqrt(head_dim) if None; see spec.h."""
     cache = _cache(k_cache, v_cache)
-    Hq, D = q.shape[1], cache.head_dim
-    q_ptr, q_row = _rows(q, Hq, D, k_cache, "q")
-    rows = B * (K + 1) if row_offsets is None else 0  # packed rows: their number is on the device
-    if q.shape[0] < rows or out.shape != q.shape or out.dtype != q.dtype:
-        raise ValueError("out: expected q's shape and dtype, and rows for every request")
-    if lse_out is not None and (lse_out.dtype != torch.float32 or lse_out.numel() < q.shape[0] * Hq):
-        raise ValueError("lse_out: expected fp32 [R, q_heads]")
+    shape = q.shape
+    Hq, D = shape[1], cache.head_dim
+    q_ptr, q_row = _rows(q, Hq, D, k_cache.dtype, "q")
+    # with row_offsets the number of packed rows is on the device
+    if out.shape != shape or out.dtype != q.dtype or not out.is_contiguous() or (
+            row_offsets is None and shape[0] < B * (K + 1)):
+        raise ValueError("out: expected q's shape and dtype, contiguous, and rows for every request")
+    lse = None
+    if lse_out is not None:
+        if lse_out.dtype != torch.float32 or lse_out.numel() < shape[0] * Hq or not lse_out.is_contiguous():
+            raise ValueError("lse_out: expected contiguous fp32 [R, q_heads]")
+        lse = lse_out.data_ptr()
     table, max_pages = _table(page_table, B)
     code = library().spec_attend(
         q_ptr, q_row, Hq, ctypes.byref(cache), layer, _ints(row_offsets, B + 1, "row_offsets"),
         _ints(depth, B, "depth"), _ints(pos_base, B, "pos_base", torch.int64), table, max_pages, B, K,
-        D ** -0.5 if scale is None else float(scale), window, sinks, _ptr(out), _ptr(lse_out), _ptr(status), _ptr(ws),
-        _nbytes(ws), _stream(stream))
-    _check(code, "spec_attend")
+        D ** -0.5 if scale is None else scale, window, sinks, out.data_ptr(), lse, _ints(status, 1, "status"),
+        ws.data_ptr(), ws.nbytes, _stream_handle(stream))
+    if code:
+        raise SpecError(code, "spec_attend")
 
 
 def spec_cache_append(k_new, v_new, k_cache, v_cache, page_table, pos_base, B, K, row_offsets=None, depth=None,
                       layer=0, status=None, stream=None):
     """k_new and v_new [R, kv_heads, head_dim], written to their pages; see spec.h."""
     cache = _cache(k_cache, v_cache)
-    k_ptr, k_row = _rows(k_new, cache.kv_heads, cache.head_dim, k_cache, "k_new")
-    v_ptr, v_row = _rows(v_new, cache.kv_heads, cache.head_dim, k_cache, "v_new")
+    H, D, dtype = cache.kv_heads, cache.head_dim, k_cache.dtype
+    k_ptr, k_row = _rows(k_new, H, D, dtype, "k_new")
+    v_ptr, v_row = _rows(v_new, H, D, dtype, "v_new")
     if row_offsets is None and min(k_new.shape[0], v_new.shape[0]) < B * (K + 1):
         raise ValueError("k_new, v_new: rows for every request")
     table, max_pages = _table(page_table, B)
     code = library().spec_cache_append(
         ctypes.byref(cache), layer, k_ptr, k_row, v_ptr, v_row, _ints(row_offsets, B + 1, "row_offsets"),
-        _ints(depth, B, "depth"), _ints(pos_base, B, "pos_base", torch.int64), table, max_pages, B, K, _ptr(status),
-        _stream(stream))
-    _check(code, "spec_cache_append")
+        _ints(depth, B, "depth"), _ints(pos_base, B, "pos_base", torch.int64), table, max_pages, B, K,
+        _ints(status, 1, "status"), _stream_handle(stream))
+    if code:
+        raise SpecError(code, "spec_cache_append")
 
 
 def spec_cache_fork(page_table, page_refs, parent, table_out, refs_out, status=None, stream=None):
@@ -436,8 +464,9 @@ def spec_cache_fork(page_table, page_refs, parent, table_out, refs_out, status=N
         raise ValueError("table_out: expected page_table's max_pages")
     code = library().spec_cache_fork(
         table, _ints(page_refs, pages, "page_refs"), _ints(parent, B, "parent"), page_table.shape[0], B, max_pages,
-        pages, out, _ints(refs_out, pages, "refs_out"), _ptr(status), _stream(stream))
-    _check(code, "spec_cache_fork")
+        pages, out, _ints(refs_out, pages, "refs_out"), _ints(status, 1, "status"), _stream_handle(stream))
+    if code:
+        raise SpecError(code, "spec_cache_fork")
 
 
 def spec_cache_workspace(B: int, K: int, page_size: int) -> int:
@@ -461,9 +490,10 @@ def spec_cache_reserve(page_table, page_refs, pos_base, B, K, page_size, cow_src
         table, _ints(page_refs, 1, "page_refs"), _ints(row_offsets, B + 1, "row_offsets"), _ints(depth, B, "depth"),
         _ints(pos_base, B, "pos_base", torch.int64), B, K, max_pages, page_refs.numel(), page_size,
         _ints(cow_src_out, cap, "cow_src_out"), _ints(cow_dst_out, cap, "cow_dst_out"),
-        _ints(counts_out, 2, "counts_out"), _ints(granted_out, B, "granted_out"), _ptr(status), _ptr(ws), _nbytes(ws),
-        _stream(stream))
-    _check(code, "spec_cache_reserve")
+        _ints(counts_out, 2, "counts_out"), _ints(granted_out, B, "granted_out"), _ints(status, 1, "status"),
+        ws.data_ptr(), ws.nbytes, _stream_handle(stream))
+    if code:
+        raise SpecError(code, "spec_cache_reserve")
 
 
 def spec_cache_copy(k_cache, v_cache, src, dst, count, status=None, stream=None):
@@ -471,8 +501,9 @@ def spec_cache_copy(k_cache, v_cache, src, dst, count, status=None, stream=None)
     cache = _cache(k_cache, v_cache)
     n = min(src.numel(), dst.numel())
     code = library().spec_cache_copy(ctypes.byref(cache), _ints(src, n, "src"), _ints(dst, n, "dst"),
-                                     _ints(count, 1, "count"), n, _ptr(status), _stream(stream))
-    _check(code, "spec_cache_copy")
+                                     _ints(count, 1, "count"), n, _ints(status, 1, "status"), _stream_handle(stream))
+    if code:
+        raise SpecError(code, "spec_cache_copy")
 
 
 def spec_cache_release(page_table, page_refs, pos_base, page_size, accepted_len=None, window=0, sinks=0, status=None,
@@ -482,9 +513,10 @@ def spec_cache_release(page_table, page_refs, pos_base, page_size, accepted_len=
     table, max_pages = _table(page_table, B)
     code = library().spec_cache_release(
         table, _ints(page_refs, 1, "page_refs"), _ints(pos_base, B, "pos_base", torch.int64),
-        _ints(accepted_len, B, "accepted_len"), B, max_pages, page_refs.numel(), page_size, window, sinks, _ptr(status),
-        _stream(stream))
-    _check(code, "spec_cache_release")
+        _ints(accepted_len, B, "accepted_len"), B, max_pages, page_refs.numel(), page_size, window, sinks,
+        _ints(status, 1, "status"), _stream_handle(stream))
+    if code:
+        raise SpecError(code, "spec_cache_release")
 
 
 def spec_cache_compact(page_table, page_refs, move_src_out, move_dst_out, page_map_out, counts_out, status=None,
@@ -496,8 +528,9 @@ def spec_cache_compact(page_table, page_refs, move_src_out, move_dst_out, page_m
     code = library().spec_cache_compact(
         table, _ints(page_refs, 1, "page_refs"), B, max_pages, pages, _ints(move_src_out, cap, "move_src_out"),
         _ints(move_dst_out, cap, "move_dst_out"), _ints(page_map_out, pages, "page_map_out"),
-        _ints(counts_out, 2, "counts_out"), _ptr(status), _stream(stream))
-    _check(code, "spec_cache_compact")
+        _ints(counts_out, 2, "counts_out"), _ints(status, 1, "status"), _stream_handle(stream))
+    if code:
+        raise SpecError(code, "spec_cache_compact")
 
 
 def spec_check_bounded_wait(status):

@@ -303,8 +303,8 @@ static cudaError_t launch_general(const AttendLaunch& a, cudaStream_t stream) {
   // two stages where they fit (228 KB an SM, 1 KB of it reserved per CTA)
   const int stages = general_smem(a.D, esize, 2) <= 220 * 1024 ? 2 : 1;
   const size_t smem = general_smem(a.D, esize, stages);
-  cudaError_t err =
-      cudaFuncSetAttribute(attend_general_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  static std::atomic<size_t> raised[kMaxDevices];
+  const cudaError_t err = raise_smem(attend_general_kernel<T>, smem, raised);
   if (err != cudaSuccess) return err;
   return launch_after_previous(attend_general_kernel<T>, dim3(a.ctas), dim3(kGenThreads), smem, stream, a, stages);
 }

@@ -94,6 +94,7 @@ __device__ __forceinline__ AttendRows attend_rows(const AttendLaunch& a, int i) 
 template <int TT>
 __device__ __forceinline__ int head_units(const AttendLaunch& a, const AttendRows& r) {
   const int cols = r.count * a.G;
+  if (cols <= a.ct) return cols == 0 ? 0 : item_tiles<TT>(a, r.p, r.p + r.count - 1).count;
   int n = 0;
   for (int c0 = 0; c0 < cols; c0 += a.ct) {
     const int c1 = min(cols, c0 + a.ct) - 1;
@@ -233,11 +234,11 @@ struct Walk {
     }
   }
   __device__ __forceinline__ void set_tiles() {
-    const int c1 = min(r.count * a.G, c0 + a.ct) - 1;
-    t = item_tiles<TT>(a, r.p + c0 / a.G, r.p + c1 / a.G);
+    const int cols = r.count * a.G;
+    t = cols <= a.ct ? item_tiles<TT>(a, r.p, r.p + r.count - 1)
+                     : item_tiles<TT>(a, r.p + c0 / a.G, r.p + (min(cols, c0 + a.ct) - 1) / a.G);
   }
-  // The CTA (of the list) whose range holds unit x, found from a CTA that starts
-  // at or after it, or before it: ranges differ by at most one unit in length.
+  // The CTA (of the list) whose range holds unit x.
   __device__ __forceinline__ int owner(long long x) const {
     const long long p = (x + 1) * sh.ctas - 1;
     return p < (1LL << 31) && sh.units < (1LL << 31) ? (int)((uint32_t)p / (uint32_t)sh.units) : (int)(p / sh.units);

@@ -353,82 +353,96 @@ __device__ __forceinline__ void load_queries(const AttendLaunch& a, const Segmen
   proxy_fence();
 }
 
+// Adds up E vectors of four consecutive d, X parts at a time, whose loads are all
+// in flight together: what a join costs is the latency of its loads, and, as it
+// runs once a CTA, of fetching its instructions, so its loops are short.
+template <int D, int E, int X>
+__device__ __forceinline__ void add_parts(const AttendLaunch& a, const Segment& s, const long long* where,
+                                          const float* weights, int c0, int nc, int tid, int threads) {
+  constexpr int kQ = D / 4;
+#pragma unroll 1
+  for (int e0 = tid; e0 < nc * kQ; e0 += threads * E) {
+    float4 o[E];
+#pragma unroll
+    for (int k = 0; k < E; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+    for (int x0 = 0; x0 < s.parts; x0 += X) {
+      float4 w[X][E];
+      float f[X][E];
+#pragma unroll
+      for (int y = 0; y < X; ++y) {
+        const int x = min(x0 + y, s.parts - 1);
+        const float4* from = reinterpret_cast<const float4*>(a.part + ((size_t)part_slot(s, x) * a.ct + c0) * D);
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+          const int e = min(e0 + k * threads, nc * kQ - 1);
+          w[y][k] = __ldcg(from + e);
+          f[y][k] = x0 + y < s.parts ? weights[x * nc + e / kQ] : 0.0f;
+        }
+      }
+#pragma unroll
+      for (int y = 0; y < X; ++y)
+#pragma unroll
+        for (int k = 0; k < E; ++k)
+          if (f[y][k] != 0.0f) {  // a part that saw nothing adds nothing
+            o[k].x = fmaf(w[y][k].x, f[y][k], o[k].x);
+            o[k].y = fmaf(w[y][k].y, f[y][k], o[k].y);
+            o[k].z = fmaf(w[y][k].z, f[y][k], o[k].z);
+            o[k].w = fmaf(w[y][k].w, f[y][k], o[k].w);
+          }
+    }
+#pragma unroll
+    for (int k = 0; k < E; ++k) {
+      const int e = e0 + k * threads, c = e / kQ;
+      if (c < nc) store4(static_cast<__nv_bfloat16*>(a.out) + where[c0 + c] * D + 4 * (e % kQ), o[k]);
+    }
+  }
+}
+
 // Adds the parts of a divided item up, in order, with `threads` threads past the
-// arrival of the last part.  The parts' weights go to `scratch` (`room` floats
-// of shared memory) once, for as many columns at a time as fit; then a thread
-// adds four consecutive d of up to four columns at a time, whose loads are in
-// flight together.  What a join costs is the latency of these loads.
+// arrival of the last part.  Groups of lanes find the weights of a column's
+// parts, a part per lane; they go to `weights` (`room` floats of shared memory),
+// for as many columns at a time as fit.
 template <int D>
-__device__ __noinline__ void join_tc(const AttendLaunch& a, const Segment& s, const long long* where, float* scratch, int room,
-                        int tid, int threads) {
-  constexpr int kQ = D / 4, kE = 4, kX = 4;
+__device__ __noinline__ void join_tc(const AttendLaunch& a, const Segment& s, const long long* where, float* weights,
+                                     int room, int tid, int threads) {
   const int parts = s.parts, most = max(1, room / parts);
+  int group = 2;  // lanes per column: a power of two
+  while (group < parts && group < 32) group *= 2;
+  const int first = tid & (group - 1);
+#pragma unroll 1
   for (int c0 = 0; c0 < s.cols; c0 += most) {
     const int nc = min(most, s.cols - c0);
-    for (int c = tid; c < nc; c += threads) {
-      constexpr int kBatch = 8;
+#pragma unroll 1
+    for (int b = 0; b < nc; b += threads / group) {  // all lanes stay for the shuffles
+      const int c = b + tid / group;
       float m = -INFINITY, l = 0.0f;
-      for (int x0 = 0; x0 < parts; x0 += kBatch) {
-        float2 st[kBatch];
-#pragma unroll
-        for (int k = 0; k < kBatch; ++k)
-          st[k] = x0 + k < parts ? __ldcg(a.part_stat + (size_t)part_slot(s, x0 + k) * a.ct + c0 + c)
-                                 : make_float2(-INFINITY, 0.0f);
-        float mn = m;
-#pragma unroll
-        for (int k = 0; k < kBatch; ++k) mn = fmaxf(mn, st[k].x);
-        l *= part_weight(make_float2(m, l), mn);
-#pragma unroll
-        for (int k = 0; k < kBatch; ++k) {
-          l = fmaf(st[k].y, part_weight(st[k], mn), l);
-          if (x0 + k < parts) scratch[(x0 + k) * nc + c] = st[k].x;
-        }
+#pragma unroll 1
+      for (int x0 = 0; x0 < parts; x0 += group) {  // one round but for more than 32 parts
+        const int x = x0 + first;
+        const bool mine = x < parts && c < nc;
+        const float2 st = mine ? __ldcg(a.part_stat + (size_t)part_slot(s, x) * a.ct + c0 + c)
+                               : make_float2(-INFINITY, 0.0f);
+        float mn = fmaxf(m, st.x);
+#pragma unroll 1
+        for (int o = group / 2; o > 0; o >>= 1) mn = fmaxf(mn, __shfl_xor_sync(0xFFFFFFFFu, mn, o));
+        float sum = st.y * part_weight(st, mn);
+#pragma unroll 1
+        for (int o = group / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+        l = fmaf(l, part_weight(make_float2(m, l), mn), sum);
         m = mn;
+        if (mine) weights[x * nc + c] = st.x;
       }
+      if (c >= nc) continue;
       const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-      for (int x = 0; x < parts; ++x)
-        scratch[x * nc + c] = part_weight(make_float2(scratch[x * nc + c], 0.0f), m) * inv;
-      if (a.lse) a.lse[where[c0 + c]] = row_lse(m, l);
+#pragma unroll 1
+      for (int x = first; x < parts; x += group)
+        weights[x * nc + c] = part_weight(make_float2(weights[x * nc + c], 0.0f), m) * inv;
+      if (first == 0 && a.lse) a.lse[where[c0 + c]] = row_lse(m, l);
     }
     named_sync(1, threads);
-    for (int e0 = tid; e0 < nc * kQ; e0 += threads * kE) {
-      float4 o[kE];
-#pragma unroll
-      for (int k = 0; k < kE; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int x0 = 0; x0 < parts; x0 += kX) {
-        float4 w[kX][kE];
-#pragma unroll
-        for (int y = 0; y < kX; ++y) {
-          if (x0 + y >= parts) break;
-          const float4* from = reinterpret_cast<const float4*>(a.part + ((size_t)part_slot(s, x0 + y) * a.ct + c0) * D);
-#pragma unroll
-          for (int k = 0; k < kE; ++k) {
-            const int e = e0 + k * threads;
-            w[y][k] = __ldcg(from + (e < nc * kQ ? e : tid));
-          }
-        }
-#pragma unroll
-        for (int y = 0; y < kX; ++y) {
-          if (x0 + y >= parts) break;
-#pragma unroll
-          for (int k = 0; k < kE; ++k) {
-            const int c = min((e0 + k * threads) / kQ, nc - 1);
-            const float f = scratch[(x0 + y) * nc + c];
-            if (f != 0.0f) {  // a part that saw nothing adds nothing
-              o[k].x = fmaf(w[y][k].x, f, o[k].x);
-              o[k].y = fmaf(w[y][k].y, f, o[k].y);
-              o[k].z = fmaf(w[y][k].z, f, o[k].z);
-              o[k].w = fmaf(w[y][k].w, f, o[k].w);
-            }
-          }
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < kE; ++k) {
-        const int e = e0 + k * threads, c = e / kQ;
-        if (c < nc) store4(static_cast<__nv_bfloat16*>(a.out) + where[c0 + c] * D + 4 * (e % kQ), o[k]);
-      }
-    }
+    if (nc * (D / 4) <= threads) add_parts<D, 1, 8>(a, s, where, weights, c0, nc, tid, threads);
+    else add_parts<D, 4, 4>(a, s, where, weights, c0, nc, tid, threads);
     named_sync(1, threads);
   }
 }
@@ -1056,8 +1070,8 @@ cudaError_t launch_variant(const AttendLaunch& a, cudaStream_t stream) {
   const int smem = t.p_off + PB * p_bytes + limit - room - static_smem;  // and the gap before it
   CUtensorMap tmK, tmV;
   if (!make_cache_map(&tmK, a.k, a, t.chunk) || !make_cache_map(&tmV, a.v, a, t.chunk)) return cudaErrorInvalidValue;
-  const cudaError_t err =
-      cudaFuncSetAttribute(attend_tc_kernel<D, CG, H>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  static std::atomic<size_t> raised[kMaxDevices];
+  const cudaError_t err = raise_smem(attend_tc_kernel<D, CG, H>, (size_t)smem, raised);
   if (err != cudaSuccess) return err;
   return launch_after_previous(attend_tc_kernel<D, CG, H>, dim3(a.ctas), dim3((4 + 4 * H) * 32), (size_t)smem, stream,
                                tmK, tmV, a, t);

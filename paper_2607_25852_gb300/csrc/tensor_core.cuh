@@ -6,6 +6,8 @@
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
+#include <atomic>
+
 #include "spec_internal.cuh"
 
 namespace spec {
@@ -130,11 +132,35 @@ inline PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() {
   return fn;
 }
 
+constexpr int kMaxDevices = 64;
+
+// SMs of the current device, asked for once per device.
 inline int device_sms() {
-  int dev = 0, sms = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-    return 1;
+  static std::atomic<int> known[kMaxDevices];
+  int dev = -1, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return 1;
+  const bool kept = dev >= 0 && dev < kMaxDevices;
+  if (kept && (sms = known[dev].load(std::memory_order_relaxed)) > 0) return sms;
+  if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 1;
+  if (kept) known[dev].store(sms, std::memory_order_relaxed);
   return sms;
+}
+
+// Raises a kernel's dynamic shared memory limit, once per device and size:
+// `raised` is the kernel's own, the largest so far per device.
+template <typename Kernel>
+inline cudaError_t raise_smem(Kernel kernel, size_t smem, std::atomic<size_t> (&raised)[kMaxDevices]) {
+  int dev = -1;
+  cudaError_t err = cudaGetDevice(&dev);
+  if (err != cudaSuccess) return err;
+  const bool kept = dev >= 0 && dev < kMaxDevices;
+  if (kept && raised[dev].load(std::memory_order_relaxed) >= smem) return cudaSuccess;
+  err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (err != cudaSuccess || !kept) return err;
+  size_t cur = raised[dev].load(std::memory_order_relaxed);
+  while (cur < smem && !raised[dev].compare_exchange_weak(cur, smem)) {
+  }
+  return cudaSuccess;
 }
 
 }  // namespace spec
