@@ -23,9 +23,10 @@ namespace spec {
 // The general kernel
 // ---------------------------------------------------------------------------
 constexpr int kGenThreads = 256;
-constexpr int kGenCols = 16;   // columns per item
+constexpr int kGenCols = 32;   // columns per item
 constexpr int kGenTile = 64;   // positions per tile
 constexpr int kGenPitchS = kGenTile + 4;
+constexpr int kGenQuarter = kGenCols / 4;  // columns of a thread's scores, and of a warp's softmax x 2
 
 __device__ __forceinline__ void cp_async16(void* dst, const void* src, bool real) {
   // nothing is read where `real` is false: 16 zero bytes are written
@@ -52,8 +53,16 @@ static size_t general_smem(int D, int esize, int stages) {
   return (size_t)stages * 2 * kGenTile * (D * esize + 16) + (size_t)kGenCols * D * 4 + (size_t)kGenCols * kGenPitchS * 4;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kGenThreads, 1) attend_general_kernel(const AttendLaunch a, int stages) {
+// C: columns of a thread's outputs (4 consecutive d of each).
+//
+// Scores: a token and eight columns per thread, from a K row of its own and Q
+// rows that the warp shares (12 shared-memory wavefronts for 32 products a
+// lane).  Weights: four columns per warp, the sums kept per lane.  Output: four
+// d of C columns per thread over all tokens.  The running time is that of
+// shared memory and of the four barriers a tile, not of the cache's bytes; two
+// CTAs share an SM where two fit.
+template <typename T, int C>
+__global__ void __launch_bounds__(kGenThreads, C <= 2 ? 2 : 1) attend_general_kernel(const AttendLaunch a, int stages) {
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ Share share;
   __shared__ Segment seg;
@@ -72,12 +81,9 @@ __global__ void __launch_bounds__(kGenThreads, 1) attend_general_kernel(const At
   find_share<kGenTile>(a, &share, sums);
   Walk<kGenTile> walk(a, share);
   const int vecs = a.D * (int)sizeof(T) / 16;
-  // outputs of a thread: 4 consecutive d of up to 4 columns
   const int dv = a.D / 4;
-  const int groups = kGenThreads / dv;  // >= 4 (D <= 256)
-  const int cpg = (kGenCols + groups - 1) / groups;
-  const int my_d = (tid % dv) * 4, my_c = (tid / dv) * cpg;
-  const bool pv_active = tid / dv < groups && my_c < kGenCols;
+  const int my_d = (tid % dv) * 4, my_c = (tid / dv) * C;
+  const bool pv_active = my_c < kGenCols && my_c + C <= (kGenThreads / dv) * C;
 
   for (;;) {
     if (tid == 0) more = walk.next(&seg) ? 1 : 0;
@@ -107,17 +113,18 @@ __global__ void __launch_bounds__(kGenThreads, 1) attend_general_kernel(const At
       const int tok = tid >> 2, pos = tile_start<kGenTile>(s.tiles, x) + tok;
       const bool wanted =
           pos <= p_last && (a.window == 0 || pos > p_first - a.window || pos < a.sinks);  // some row sees it
-      int page = -1;
+      int page = -1, in_page = 0;
       if (wanted) {
-        page = __ldg(a.table + (size_t)s.request * a.max_pages + pos / a.page_size);
+        const int slot = pos / a.page_size;
+        in_page = pos - slot * a.page_size;
+        page = __ldg(a.table + (size_t)s.request * a.max_pages + slot);
         if (page < 0 || page >= a.pages) {
           page = -1;
           if ((tid & 3) == 0) report(a.status, SPEC_ERR_BAD_INPUT);
         }
       }
       if ((tid & 3) == 0) sh_tok[stage][tok] = page >= 0 ? pos : -1;
-      const int64_t off = (page >= 0 ? (int64_t)page * a.page_b + (int64_t)(pos % a.page_size) * a.token_b : 0) +
-                          s.head * a.head_b;
+      const int64_t off = (page >= 0 ? (int64_t)page * a.page_b + (int64_t)in_page * a.token_b : 0) + s.head * a.head_b;
       uint8_t* dk = sK + ((size_t)stage * kGenTile + tok) * pitch;
       uint8_t* dvv = sV + ((size_t)stage * kGenTile + tok) * pitch;
       for (int w = tid & 3; w < vecs; w += 4) {
@@ -126,10 +133,15 @@ __global__ void __launch_bounds__(kGenThreads, 1) attend_general_kernel(const At
       }
       cp_async_commit();
     };
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};  // columns 2 warp, 2 warp + 1 (all lanes alike)
-    float acc[4][4];
+    // columns 4 warp .. 4 warp + 3: the maximum (all lanes alike), a lane's part of the sum
+    float m[4], l[4], acc[C][4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
+    for (int k = 0; k < 4; ++k) {
+      m[k] = -INFINITY;
+      l[k] = 0.0f;
+    }
+#pragma unroll
+    for (int k = 0; k < C; ++k)
 #pragma unroll
       for (int d = 0; d < 4; ++d) acc[k][d] = 0.0f;
     load_tile(s.tile0, 0);
@@ -142,15 +154,21 @@ __global__ void __launch_bounds__(kGenThreads, 1) attend_general_kernel(const At
         cp_async_wait<0>();
       }
       __syncthreads();
-      {  // ---- scores: a token and 4 columns per thread ----
-        const int tok = tid & (kGenTile - 1), c0 = (tid / kGenTile) * 4;
+      // ---- scores ----
+      bool masked = false;
+      {
+        const int tok = tid & (kGenTile - 1), c0 = (tid / kGenTile) * kGenQuarter;
+        const int pos = sh_tok[stage][tok];
         if (c0 < s.cols) {
           const T* kr = reinterpret_cast<const T*>(sK + ((size_t)stage * kGenTile + tok) * pitch);
-          float dot[4] = {0.f, 0.f, 0.f, 0.f};
+          float dot[kGenQuarter];
+#pragma unroll
+          for (int c = 0; c < kGenQuarter; ++c) dot[c] = 0.0f;
+#pragma unroll 2
           for (int d = 0; d < a.D; d += 4) {
             const float4 k4 = load4(kr + d);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < kGenQuarter; ++c) {
               const float4 q4 = load4(sQ + (c0 + c) * a.D + d);
               dot[c] = fmaf(k4.x, q4.x, dot[c]);
               dot[c] = fmaf(k4.y, q4.y, dot[c]);
@@ -158,61 +176,61 @@ __global__ void __launch_bounds__(kGenThreads, 1) attend_general_kernel(const At
               dot[c] = fmaf(k4.w, q4.w, dot[c]);
             }
           }
-          const int pos = sh_tok[stage][tok];
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            const int row = s.p + (s.col0 + c0 + c) / a.G;
+          for (int c = 0; c < kGenQuarter; ++c) {
+            const int row = s.p + (s.col0 + min(c0 + c, s.cols - 1)) / a.G;
             const bool seen = pos >= 0 && pos <= row && (a.window == 0 || pos > row - a.window || pos < a.sinks);
+            masked |= !seen;
             sS[(c0 + c) * kGenPitchS + tok] = seen ? dot[c] * a.c2 : -INFINITY;
           }
         }
       }
-      __syncthreads();
-      // ---- the running maximum and sum: two columns per warp ----
+      const bool edge = __syncthreads_or(masked);
+      // ---- weights ----
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int c = 2 * warp + k;
-        if (c >= s.cols) continue;
+      for (int k = 0; k < 4; ++k) {
+        const int c = 4 * warp + k;
+        if (c >= s.cols) break;
         float* row = sS + c * kGenPitchS;
         const float x0 = row[lane], x1 = row[lane + 32];
-        float t = fmaxf(x0, x1);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) t = fmaxf(t, __shfl_xor_sync(0xFFFFFFFFu, t, o));
-        const float mn = fmaxf(m[k], t);
+        const float mn = fmaxf(m[k], warp_max(fmaxf(x0, x1)));
         const float alpha = m[k] == -INFINITY ? 0.0f : exp2f(m[k] - mn);
         // a masked score is -inf and weighs 0; a NaN score stays NaN
         const float p0 = x0 == -INFINITY ? 0.0f : exp2f(x0 - mn), p1 = x1 == -INFINITY ? 0.0f : exp2f(x1 - mn);
         row[lane] = p0;
         row[lane + 32] = p1;
-        float sum = p0 + p1;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-        l[k] = fmaf(l[k], alpha, sum);
+        l[k] = fmaf(l[k], alpha, p0 + p1);
         m[k] = mn;
         if (lane == 0) sh_alpha[c] = alpha;
       }
       __syncthreads();
-      // ---- out += P V ----
+      // ---- output ----
       if (pv_active && my_c < s.cols) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          if (k >= cpg) break;
+        for (int k = 0; k < C; ++k) {
           const float alpha = sh_alpha[min(my_c + k, s.cols - 1)];
 #pragma unroll
           for (int d = 0; d < 4; ++d) acc[k][d] *= alpha;
         }
         const uint8_t* vr = sV + (size_t)stage * kGenTile * pitch + my_d * sizeof(T);
-        for (int tok = 0; tok < kGenTile; ++tok) {
-          const float4 v4 = load4(reinterpret_cast<const T*>(vr + (size_t)tok * pitch));
+        const float* wr = sS + my_c * kGenPitchS;
+#pragma unroll 2
+        for (int tok = 0; tok < kGenTile; tok += 4) {
+          float4 v4[4];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            if (k >= cpg) break;
-            const float w = my_c + k < s.cols ? sS[(my_c + k) * kGenPitchS + tok] : 0.0f;
-            if (w != 0.0f) {  // what a masked token holds does not reach the sum
-              acc[k][0] = fmaf(w, v4.x, acc[k][0]);
-              acc[k][1] = fmaf(w, v4.y, acc[k][1]);
-              acc[k][2] = fmaf(w, v4.z, acc[k][2]);
-              acc[k][3] = fmaf(w, v4.w, acc[k][3]);
+          for (int y = 0; y < 4; ++y) v4[y] = load4(reinterpret_cast<const T*>(vr + (size_t)(tok + y) * pitch));
+#pragma unroll
+          for (int k = 0; k < C; ++k) {
+            // (columns past the item's hold old weights: their sums are not written)
+            const float4 w4 = load4(wr + k * kGenPitchS + tok);
+            const float w[4] = {w4.x, w4.y, w4.z, w4.w};
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              if (edge && w[y] == 0.0f) continue;  // what a masked token holds does not reach the sum
+              acc[k][0] = fmaf(w[y], v4[y].x, acc[k][0]);
+              acc[k][1] = fmaf(w[y], v4[y].y, acc[k][1]);
+              acc[k][2] = fmaf(w[y], v4[y].z, acc[k][2]);
+              acc[k][3] = fmaf(w[y], v4[y].w, acc[k][3]);
             }
           }
         }
@@ -221,9 +239,12 @@ __global__ void __launch_bounds__(kGenThreads, 1) attend_general_kernel(const At
       if (stages == 1 && x + 1 < s.ntiles) load_tile(s.tile0 + x + 1, 0);
     }
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const int c = 2 * warp + k;
-      if (lane == 0 && c < s.cols) {
+    for (int k = 0; k < 4; ++k) {
+      const int c = 4 * warp + k;
+      if (c >= s.cols) break;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) l[k] += __shfl_xor_sync(0xFFFFFFFFu, l[k], o);
+      if (lane == 0) {
         sh_l[c] = l[k];
         sh_m[c] = m[k];
       }
@@ -232,16 +253,15 @@ __global__ void __launch_bounds__(kGenThreads, 1) attend_general_kernel(const At
     // ---- the item's result, or this part's ----
     if (pv_active) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < C; ++k) {
         const int c = my_c + k;
-        if (k >= cpg || c >= s.cols) break;
+        if (c >= s.cols) break;
         if (s.slot < 0) {
           const float inv = sh_l[c] == 0.0f ? 0.0f : 1.0f / sh_l[c];
-          T* o = static_cast<T*>(a.out) + out_index(a, s, c) * a.D + my_d;
-#pragma unroll
-          for (int d = 0; d < 4; ++d) o[d] = from_float<T>(acc[k][d] * inv);
+          store4(static_cast<T*>(a.out) + out_index(a, s, c) * a.D + my_d,
+                 make_float4(acc[k][0] * inv, acc[k][1] * inv, acc[k][2] * inv, acc[k][3] * inv));
         } else {
-          *reinterpret_cast<float4*>(a.part + ((size_t)s.slot * kGenCols + c) * a.D + my_d) =
+          *reinterpret_cast<float4*>(a.part + ((size_t)s.slot * a.ct + c) * a.D + my_d) =
               make_float4(acc[k][0], acc[k][1], acc[k][2], acc[k][3]);
         }
       }
@@ -250,13 +270,13 @@ __global__ void __launch_bounds__(kGenThreads, 1) attend_general_kernel(const At
       if (s.slot < 0) {
         if (a.lse) a.lse[out_index(a, s, tid)] = row_lse(sh_m[tid], sh_l[tid]);
       } else {
-        a.part_stat[(size_t)s.slot * kGenCols + tid] = make_float2(sh_m[tid], sh_l[tid]);
+        a.part_stat[(size_t)s.slot * a.ct + tid] = make_float2(sh_m[tid], sh_l[tid]);
       }
     }
     if (s.slot >= 0) {
-      __threadfence();
       __syncthreads();
       if (tid == 0) {
+        __threadfence();
         last = atomicAdd(a.arrived + s.first_cta, 1u) == (uint32_t)s.parts - 1 ? 1 : 0;
         if (last) a.arrived[s.first_cta] = 0;
       }
@@ -273,8 +293,14 @@ __global__ void __launch_bounds__(kGenThreads, 1) attend_general_kernel(const At
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
+// The general kernel's CTAs per SM (228 KB, 1 KB of it reserved per CTA and some
+// for its static arrays).
+static int general_ctas_per_sm(int D, int dtype) {
+  return D <= 64 && general_smem(D, element_size(dtype), 2) <= 112 * 1024 ? 2 : 1;
+}
+
 struct AttendGeometry {
-  int ct;  // columns per item, the most of the kernels that may serve the shape
+  int ct;    // columns per item, the most of the kernels that may serve the shape
   int ctas;  // most CTAs: two parts each
   size_t part_off, stat_off, bytes;
 };
@@ -283,7 +309,7 @@ struct AttendGeometry {
 static AttendGeometry attend_geometry(int cols, int D, int dtype) {
   AttendGeometry g{};
   g.ct = dtype == SPEC_BF16 ? std::max(kGenCols, attend_tc_columns(cols)) : kGenCols;
-  g.ctas = kAttendMaxSms * (dtype == SPEC_BF16 ? attend_tc_ctas_per_sm(D, g.ct) : 1);
+  g.ctas = kAttendMaxSms * 2;
   const size_t slots = 2 * (size_t)g.ctas;
   g.part_off = ((size_t)g.ctas * 4 + 255) / 256 * 256;
   g.stat_off = g.part_off + (slots * g.ct * D * 4 + 255) / 256 * 256;
@@ -297,16 +323,22 @@ static bool attend_shape_ok(int B, int K, int q_heads, int kv_heads, int D, int 
          (dtype == SPEC_BF16 || dtype == SPEC_F32) && D * element_size(dtype) % 16 == 0;
 }
 
-template <typename T>
+template <typename T, int C>
 static cudaError_t launch_general(const AttendLaunch& a, cudaStream_t stream) {
   const int esize = (int)sizeof(T);
-  // two stages where they fit (228 KB an SM, 1 KB of it reserved per CTA)
-  const int stages = general_smem(a.D, esize, 2) <= 220 * 1024 ? 2 : 1;
+  const int stages = general_smem(a.D, esize, 2) <= 220 * 1024 ? 2 : 1;  // two where they fit
   const size_t smem = general_smem(a.D, esize, stages);
   static std::atomic<size_t> raised[kMaxDevices];
-  const cudaError_t err = raise_smem(attend_general_kernel<T>, smem, raised);
+  const cudaError_t err = raise_smem(attend_general_kernel<T, C>, smem, raised);
   if (err != cudaSuccess) return err;
-  return launch_after_previous(attend_general_kernel<T>, dim3(a.ctas), dim3(kGenThreads), smem, stream, a, stages);
+  return launch_after_previous(attend_general_kernel<T, C>, dim3(a.ctas), dim3(kGenThreads), smem, stream, a, stages);
+}
+
+// A thread's columns: kGenThreads / (D / 4) threads share the item's.
+template <typename T>
+static cudaError_t launch_general(const AttendLaunch& a, cudaStream_t stream) {
+  return a.D <= 64 ? launch_general<T, 2>(a, stream)
+                   : a.D <= 128 ? launch_general<T, 4>(a, stream) : launch_general<T, 8>(a, stream);
 }
 
 }  // namespace spec
@@ -364,21 +396,17 @@ extern "C" int spec_attend(const void* q, int64_t q_row_stride, int q_heads, con
   a.part_stat = reinterpret_cast<float2*>(base + g.stat_off);
   const int sms = std::min(device_sms(), kAttendMaxSms);
   a.min_tiles = 1;
+  const bool tc = attend_tc_serves(a.D, cache->dtype, a.page_size, a.head_b, a.token_b, a.page_b);
+  a.ct = tc ? attend_tc_columns((K + 1) * a.G) : kGenCols;
+  a.ctas = sms * (tc ? attend_tc_ctas_per_sm(a.D, a.ct) : general_ctas_per_sm(a.D, cache->dtype));
+  // a list per head, if that leaves no more than one CTA in sixteen idle
   a.lists = 1;
-  cudaError_t err;
-  if (attend_tc_serves(a.D, cache->dtype, a.page_size, a.head_b, a.token_b, a.page_b)) {
-    a.ct = attend_tc_columns((K + 1) * a.G);
-    a.ctas = sms * attend_tc_ctas_per_sm(a.D, a.ct);
-    // a list per head, if that leaves no more than one CTA in sixteen idle
-    if (a.ctas % a.Hkv <= a.ctas / 16) {
-      a.lists = a.Hkv;
-      a.ctas -= a.ctas % a.Hkv;
-    }
-    err = launch_attend_tc(a, stream);
-  } else {
-    a.ct = kGenCols;
-    a.ctas = sms;
-    err = cache->dtype == SPEC_F32 ? launch_general<float>(a, stream) : launch_general<__nv_bfloat16>(a, stream);
+  if (a.ctas % a.Hkv <= a.ctas / 16) {
+    a.lists = a.Hkv;
+    a.ctas -= a.ctas % a.Hkv;
   }
+  const cudaError_t err = tc                              ? launch_attend_tc(a, stream)
+                          : cache->dtype == SPEC_F32      ? launch_general<float>(a, stream)
+                                                          : launch_general<__nv_bfloat16>(a, stream);
   return err == cudaSuccess && cudaGetLastError() == cudaSuccess ? SPEC_OK : SPEC_ERR_CUDA;
 }

@@ -135,11 +135,6 @@ __device__ __forceinline__ bool named_or(int id, int threads, bool x) {
       : "memory");
   return r != 0;
 }
-__device__ __forceinline__ float warp_max(float x) {
-  float r;
-  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
-  return r;
-}
 __device__ __forceinline__ void tmem_ld8(uint32_t addr, float* v) {
   uint32_t r[8];
   asm volatile(
