@@ -544,7 +544,7 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
     int T = 0;
     int U = 0;       // units (tile, set) before this tile
     int mine_u = 0;  // this set's last unit
-    RingPos vp{1, 0u};
+    RingPos vp{2, 0u};  // the place of a tile's values
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       // a lane's own finding until the next vote
       if (!failed) failed = !wait_phase(bar, parity & 1u, a.status);
@@ -836,8 +836,25 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
       // ---- pages into the ring ----
       const int c = lane;  // the box of this lane: positions c chunk .. of a tile
       const bool mine = c < t.nchunk;
-      int tiles = 0, issued = 0;  // tiles done, ring slots filled (by the lane that issues)
       RingPos rp{0, 1u};          // the parity of the slot's previous use
+      // The ring's order is K0 K1 V0 K2 V1 ...: a tile's keys are loaded a tile
+      // ahead of its values, into the place of values that are done two tiles
+      // before, so that with three places the scores do not wait for the output.
+      int tiles = 0, issued = 0;  // tiles whose keys, places filled (by the lane that issues)
+      int v_head = 0;             // head of the tile whose values are due
+      auto fill = [&](const CUtensorMap* map, int head, const int2* pages) -> bool {
+        if (issued >= t.slots && !wait_phase(&empty[rp.slot], rp.use, a.status)) return false;
+        mbar_expect_tx(&full[rp.slot], kSlotBytes);
+        uint32_t dst = ring + rp.slot * kSlotBytes;
+        for (int b = 0; b < t.nchunk; ++b, dst += t.chunk * 128) {
+          const int2 pt = pages[b];
+          tma_load_4d(dst, map, 0, head, pt.y, pt.x, &full[rp.slot]);
+          if (D == 128) tma_load_4d(dst + kHalfBytes, map, 64, head, pt.y, pt.x, &full[rp.slot]);
+        }
+        ++issued;
+        rp.step(1, t.slots);
+        return true;
+      };
       bool ok = true;
       for (int n = 0; ok; ++n) {
         Segment s;
@@ -873,24 +890,21 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
           if (lane == 0) tile_bad[tiles % kBadRing] = (int)bads;
           if (mine) sPage[tiles & 1][c] = make_int2(page, tok);
           __syncwarp();
-          if (elect_one()) {
-            for (int kv = 0; kv < 2 && ok; ++kv) {
-              ok = !aborted && (issued < t.slots || wait_phase(&empty[rp.slot], rp.use, a.status));
-              if (!ok) break;
-              mbar_expect_tx(&full[rp.slot], kSlotBytes);
-              const CUtensorMap* map = kv ? &tmV : &tmK;
-              uint32_t dst = ring + rp.slot * kSlotBytes;
-              for (int b = 0; b < t.nchunk; ++b, dst += t.chunk * 128) {
-                const int2 pt = sPage[tiles & 1][b];
-                tma_load_4d(dst, map, 0, s.head, pt.y, pt.x, &full[rp.slot]);
-                if (D == 128) tma_load_4d(dst + kHalfBytes, map, 64, s.head, pt.y, pt.x, &full[rp.slot]);
-              }
-              ++issued;
-              rp.step(1, t.slots);
-            }
-          }
+          if (elect_one())
+            ok = !aborted && fill(&tmK, s.head, sPage[tiles & 1]) &&
+                 (tiles == 0 || fill(&tmV, v_head, sPage[(tiles - 1) & 1]));
+          v_head = s.head;
           ok = __all_sync(0xFFFFFFFFu, ok);
         }
+      }
+      if (ok && tiles > 0) {  // the last values; no keys go before them
+        if (elect_one()) {
+          ok = issued < t.slots || wait_phase(&empty[rp.slot], rp.use, a.status);
+          ++issued;
+          rp.step(1, t.slots);
+          ok = ok && fill(&tmV, v_head, sPage[(tiles - 1) & 1]);
+        }
+        ok = __all_sync(0xFFFFFFFFu, ok);
       }
       if (!ok) {
         aborted = 1;
@@ -905,12 +919,12 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
         int T = 0, U = 0;  // tiles whose scores, units (tile, set) whose second product is issued
         int prev_n = 0, prev_N = 0;
         bool prev_first = false, ok = true;
-        RingPos kp{0, 0u}, vp{1, 0u};
+        RingPos rp{0, 0u};  // K0 K1 V0 K2 V1 ...: the order of the products
         // O^T of a tile of width N, set by set; `first` of its segment n
         auto second = [&](bool first, int n, int N) -> bool {
           if (first && n > 0 && !wait_phase(&o_free, (uint32_t)((n - 1) & 1), a.status)) return false;
-          if (!wait_phase(&full[vp.slot], vp.use, a.status)) return false;
-          const uint32_t v = lo_v(ring + vp.slot * kSlotBytes, D == 128 ? kHalfBytes : 0);
+          if (!wait_phase(&full[rp.slot], rp.use, a.status)) return false;
+          const uint32_t v = lo_v(ring + rp.slot * kSlotBytes, D == 128 ? kHalfBytes : 0);
           const int wide = set_cols<H>(N);
 #pragma unroll
           for (int h = 0; h < H; ++h) {
@@ -926,8 +940,8 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
             umma_commit(&p_free[U & 3]);
             ++U;
           }
-          umma_commit(&empty[vp.slot]);
-          vp.step(2, t.slots);
+          umma_commit(&empty[rp.slot]);
+          rp.step(1, t.slots);
           return true;
         };
         for (int n = 0; ok; ++n) {
@@ -942,18 +956,18 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
           const uint32_t q = lo_kq(ring + t.q_off + qb * a.ct * D * 2), q_half = (uint32_t)(a.ct * 128) >> 4;
           for (int x = 0; x < ntiles && ok; ++x, ++T) {
             const int b = T % SB;
-            ok = !aborted && wait_phase(&full[kp.slot], kp.use, a.status);
+            ok = !aborted && wait_phase(&full[rp.slot], rp.use, a.status);
             if (ok && T >= SB) ok = wait_phase(&s_free[b], (uint32_t)((T / SB - 1) & 1), a.status);
             if (!ok) break;
             tc_fence_after();
-            const uint32_t key = lo_kq(ring + kp.slot * kSlotBytes), tD = tmem + b * kScores;
+            const uint32_t key = lo_kq(ring + rp.slot * kSlotBytes), tD = tmem + b * kScores;
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk)
               umma_bf16(tD, desc(key + (((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4), kHiKQ),
                         desc(q + (kk >> 2) * q_half + (((kk & 3) * 32) >> 4), kHiKQ), idesc, kk > 0 ? 1u : 0u);
             umma_commit(&s_full[b]);
-            umma_commit(&empty[kp.slot]);
-            kp.step(2, t.slots);
+            umma_commit(&empty[rp.slot]);
+            rp.step(1, t.slots);
             if (x == ntiles - 1) umma_commit(&q_free[qb]);
             if (T > 0) ok = second(prev_first, prev_n, prev_N);
             prev_first = x == 0;
@@ -961,6 +975,7 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
             prev_N = N;
           }
         }
+        rp.step(1, t.slots);  // the place of keys that do not come
         if (ok && T > 0) ok = second(prev_first, prev_n, prev_N);
         if (!ok) aborted = 1;
         // everything issued has completed before the TMEM goes
