@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(kGenThreads, C <= 2 ? 2 : 1) attend_general_ke
     const int p_first = s.p + s.col0 / a.G, p_last = s.p + (s.col0 + s.cols - 1) / a.G;
     // four threads per token
     auto load_tile = [&](int x, int stage) {
-      const int tok = tid >> 2, pos = tile_start<kGenTile>(s.tiles, x) + tok;
+      const int tok = tid >> 2, pos = place_position(s.tiles, x * kGenTile + tok);
       const bool wanted =
           pos <= p_last && (a.window == 0 || pos > p_first - a.window || pos < a.sinks);  // some row sees it
       int page = -1, in_page = 0;
@@ -395,10 +395,10 @@ extern "C" int spec_attend(const void* q, int64_t q_row_stride, int q_heads, con
   a.part = reinterpret_cast<float*>(base + g.part_off);
   a.part_stat = reinterpret_cast<float2*>(base + g.stat_off);
   const int sms = std::min(device_sms(), kAttendMaxSms);
-  a.min_tiles = 1;
   const bool tc = attend_tc_serves(a.D, cache->dtype, a.page_size, a.head_b, a.token_b, a.page_b);
   a.ct = tc ? attend_tc_columns((K + 1) * a.G) : kGenCols;
   a.ctas = sms * (tc ? attend_tc_ctas_per_sm(a.D, a.ct) : general_ctas_per_sm(a.D, cache->dtype));
+  a.grain = tc ? attend_tc_grain(a.page_size) : 1;
   // a list per head, if that leaves no more than one CTA in sixteen idle
   a.lists = 1;
   if (a.ctas % a.Hkv <= a.ctas / 16) {

@@ -35,6 +35,7 @@ struct AttendLaunch {
   RowLayout rows;
   float c2;    // scale * log2(e)
   int window, sinks;
+  int grain;          // positions of a load: a power of two that divides the page size
   void* out;
   float* lse;
   int32_t* status;
@@ -42,13 +43,14 @@ struct AttendLaunch {
   float* part;        // [2 * ctas][ct][D] sums relative to the part's maximum
   float2* part_stat;  // [2 * ctas][ct] (maximum in log2 units, sum)
   uint32_t* arrived;  // [ctas], zero between calls
-  int ctas, min_tiles;
+  int ctas;
   int lists;          // 1, or one per key-value head
 };
 
-// The tiles of positions that rows at positions p_first..p_last see: the
-// sinks' (ns tiles from 0), then the window's from tile w0.  A request that
-// sees nothing has one (masked) tile, so that its rows are written.
+// What rows at positions p_first..p_last see, as one run of places: the sinks'
+// positions 0 .. ns - 1, then the window's from w0, both in whole grains (what a
+// load takes together), cut into tiles of TT.  A request that sees nothing has
+// one (masked) tile, so that its rows are written.
 struct ItemTiles {
   int ns, w0, count;
 };
@@ -58,17 +60,16 @@ __device__ __forceinline__ ItemTiles item_tiles(const AttendLaunch& a, int p_fir
   if (p_last < 0) return t;
   if (a.window > 0 && p_first >= a.window) {
     const int lo = p_first - a.window + 1;
-    t.w0 = lo / TT;
-    const int sink_end = a.sinks < lo ? a.sinks : lo;
-    t.ns = (sink_end + TT - 1) / TT;
-    if (t.ns > t.w0) t.ns = t.w0;
+    t.w0 = lo & -a.grain;
+    t.ns = ((a.sinks < lo ? a.sinks : lo) + a.grain - 1) & -a.grain;
+    if (t.ns >= t.w0) t.ns = t.w0 = 0;  // they meet: one run from 0
   }
-  t.count = t.ns + p_last / TT - t.w0 + 1;
+  t.count = (t.ns + p_last - t.w0) / TT + 1;
   return t;
 }
-template <int TT>
-__device__ __forceinline__ int tile_start(const ItemTiles& t, int x) {
-  return (x < t.ns ? x : t.w0 + x - t.ns) * TT;
+// The position at a place.
+__device__ __forceinline__ int place_position(const ItemTiles& t, int place) {
+  return place < t.ns ? place : place - t.ns + t.w0;
 }
 
 constexpr int kNowhere = -(1 << 28);  // the position of rows that see nothing
@@ -161,8 +162,7 @@ __device__ void find_share(const AttendLaunch& a, Share* sh, long long* sums) {
       if (passes == 2) total = sh->units;
       // this CTA's range: every thread that may hold its start works it out
       const int most = a.ctas / a.lists;
-      const long long want = (total + a.min_tiles - 1) / a.min_tiles;
-      const int ctas = (int)(want < most ? want : most), c = (int)blockIdx.x / a.lists;
+      const int ctas = (int)(total < most ? total : most), c = (int)blockIdx.x / a.lists;
       long long u0 = 0, u1 = 0;
       if (c < ctas) {
         u0 = scale_floor(c, total, ctas);

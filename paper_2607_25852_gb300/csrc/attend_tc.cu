@@ -10,9 +10,10 @@
 // column.  A thread of the softmax holds one position's scores: the weights
 // are elementwise, and the maximum over positions is looked at only for a
 // bound: as long as no score exceeds its column's reference maximum by more
-// than 2^8 (in the exponent's base), the old reference serves (weights stay
-// below 2^8, exact in range and in relative precision), so most tiles need one
-// vote and no reduction, no rescaling of O^T and no exchange between warps.
+// than 24 binary orders, the old reference serves (weights stay below 2^24,
+// far from any overflow and with the same relative precision), so most tiles
+// need one vote and no reduction, no rescaling of O^T and no exchange between
+// warps.
 // The sum of the weights is kept per thread, in fp32, and reduced once per
 // item.  For the second product a weight is the sum of two bf16 numbers, its
 // upper 8 bits and the rounded rest (2^-17 relative): one bf16 number would
@@ -59,7 +60,7 @@ constexpr int kBadRing = 32;      // tiles between the loader and the softmax: f
 // room each.)
 constexpr bool two_per_sm(int D, int CG) { return D == 64 && CG == 2; }
 constexpr float kNoMax = -3.0e38f;  // the reference of a column that has seen nothing
-constexpr float kGrowth = 8.0f;   // log2 of how far weights may exceed 1
+constexpr float kGrowth = 24.0f;  // log2 of how far weights may exceed 1
 
 struct TcPlan {
   int chunk, nchunk;    // positions per TMA box, boxes per tile and half
@@ -307,8 +308,8 @@ __device__ __noinline__ float cleared_values(const AttendLaunch& a, const Segmen
   const int p_first = s.p + s.col0 / a.G, p_last = s.p + (s.col0 + s.cols - 1) / a.G;
   float sum = 0.0f;
   for (int x = 0; x < s.ntiles; ++x) {
-    const int t0 = tile_start<kTile>(s.tiles, s.tile0 + x);
-    for (int pos = t0; pos < t0 + kTile; ++pos) {
+    for (int y = 0; y < kTile; ++y) {
+      const int pos = place_position(s.tiles, (s.tile0 + x) * kTile + y);
       const bool any = pos <= p_last && (a.window == 0 || pos > p_first - a.window || pos < a.sinks);
       const bool all = pos <= p_first && (a.window == 0 || pos > p_last - a.window || pos < a.sinks);
       const bool seen = pos <= r && (a.window == 0 || pos > r - a.window || pos < a.sinks);
@@ -544,6 +545,7 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
     int T = 0;
     int U = 0;       // units (tile, set) before this tile
     int mine_u = 0;  // this set's last unit
+    float neg_lowest = 0.0f;  // the negative of this set's lowest reference
     RingPos vp{2, 0u};  // the place of a tile's values
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       // a lane's own finding until the next vote
@@ -581,14 +583,15 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
       for (int j = 0; j < CG * 4; ++j) l[j] = 0ull;
 
       for (int x = 0; x < ntiles; ++x, ++T) {
-        const int t0 = tile_start<kTile>(tiles, tile0 + x), b = T % SB;
+        const int b = T % SB, first = (tile0 + x) * kTile, t0 = place_position(tiles, first);
         wait(&s_full[b], T / SB);
         tc_fence_after();
         const int bads = tile_bad[T % kBadRing];
-        const bool edge = !(t0 + kTile - 1 <= p_first &&
+        // do all rows see all of the tile's positions (t0 .. t0 + kTile - 1, or some sinks and some others)?
+        const bool edge = !(t0 + kTile - 1 <= p_first && (first >= tiles.ns || first + kTile <= tiles.ns) &&
                             (a.window == 0 || t0 > p_last - a.window || t0 + kTile <= a.sinks)) ||
                           bads != 0;
-        const int pos = t0 + tl;
+        const int pos = place_position(tiles, first + tl);
         const bool gone = edge && (bads >> (tl / t.chunk)) & 1;
         // scores; -inf where masked.  Columns past this set's are whatever TMEM
         // holds: their reference makes every weight of theirs 0 (or NaN), and
@@ -616,21 +619,29 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
             }
           }
         }
-        // ---- does a score exceed its column's reference by too much? ----
+        // ---- does a score exceed its column's reference by too much?  First the
+        // largest of the thread's scores against the lowest reference, which
+        // nearly always says no; then each against its own ----
         bool grow = x == 0;
         if (x > 0) {
-          float top[2] = {-INFINITY, -INFINITY};
+          float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int g = 0; g < CG; ++g) {
-            f32x2 m[4];
-            load_pairs(m, ref + g * 8);
+          for (int k = 0; k < CG * 4; ++k) top[k & 3] = max3(top[k & 3], v[2 * k], v[2 * k + 1]);
+          const float most = fmaxf(max3(top[0], top[1], top[2]), top[3]);
+          if (named_or(2 + hf, 128, fmaf(most, a.c2, neg_lowest) > kGrowth || failed)) {
+            float far = -INFINITY;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float2 d = unpair(fma2(pair(v[8 * g + 2 * j], v[8 * g + 2 * j + 1]), c2, m[j]));
-              top[j & 1] = max3(top[j & 1], d.x, d.y);
+            for (int g = 0; g < CG; ++g) {
+              f32x2 m[4];
+              load_pairs(m, ref + g * 8);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const float2 d = unpair(fma2(pair(v[8 * g + 2 * j], v[8 * g + 2 * j + 1]), c2, m[j]));
+                far = max3(far, d.x, d.y);
+              }
             }
+            grow = named_or(2 + hf, 128, far > kGrowth || failed);
           }
-          grow = named_or(2 + hf, 128, fmaxf(top[0], top[1]) > kGrowth || failed);
         }
         if (grow) {
           // new references: the columns' maxima so far
@@ -654,6 +665,8 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
           }
           if (x > 0) wait_unit(mine_u);  // O^T is complete up to the last tile
           failed = named_or(2 + hf, 128, failed);
+          neg_lowest = -INFINITY;
+          for (int c = 0; c < gc * 8; ++c) neg_lowest = fmaxf(neg_lowest, ref[c]);
           if (x > 0) {
             tc_fence_after();
 #pragma unroll
@@ -864,12 +877,12 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
         const int32_t* row = a.table + (size_t)s.request * a.max_pages;
         // does some row see this lane's positions of tile x?
         auto seen = [&](int x) {
-          const int pos = tile_start<kTile>(s.tiles, x) + c * t.chunk;
+          const int pos = place_position(s.tiles, x * kTile + c * t.chunk);
           return mine && pos <= p_last && (a.window == 0 || pos + t.chunk - 1 > p_first - a.window || pos < a.sinks);
         };
         int tok_next = 0;  // its first position in the page
         auto lookup = [&](int x) {
-          const int pos = tile_start<kTile>(s.tiles, x) + c * t.chunk, slot = pos / a.page_size;
+          const int pos = place_position(s.tiles, x * kTile + c * t.chunk), slot = pos / a.page_size;
           tok_next = pos - slot * a.page_size;
           return __ldg(row + slot);
         };
@@ -1054,8 +1067,7 @@ bool make_cache_map(CUtensorMap* map, const char* base, const AttendLaunch& a, i
 template <int D, int CG, int H>
 cudaError_t launch_variant(const AttendLaunch& a, cudaStream_t stream) {
   TcPlan t{};
-  t.chunk = a.page_size & -a.page_size;
-  if (t.chunk > kTile) t.chunk = kTile;
+  t.chunk = a.grain;
   t.nchunk = kTile / t.chunk;
   constexpr int QB = H == 1 && !two_per_sm(D, CG) ? 2 : 1, PB = 2;
   constexpr int kPerSm = two_per_sm(D, CG) ? 2 : 1;
@@ -1093,6 +1105,8 @@ bool attend_tc_serves(int D, int dtype, int page_size, int64_t head_b, int64_t t
   const int64_t far = 1LL << 40;  // a tensor map's strides end there
   return dtype == SPEC_BF16 && (D == 64 || D == 128) && page_size % 8 == 0 && head_b < far && token_b < far && page_b < far;
 }
+
+int attend_tc_grain(int page_size) { return std::min(page_size & -page_size, kTile); }
 
 int attend_tc_ctas_per_sm(int D, int ct) { return two_per_sm(D, ct <= 16 ? 2 : 4) ? 2 : 1; }
 
