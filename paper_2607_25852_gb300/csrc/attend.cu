@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(kGenThreads, C <= 2 ? 2 : 1) attend_general_ke
       const int c = x / dv, d = (x - c * dv) * 4;
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
       if (c < s.cols) {
-        const int col = s.col0 + c, j = col / a.G;
+        const int col = s.col0 + c, j = group_row(a, col);
         const T* src = static_cast<const T*>(a.q) + (int64_t)(s.row0 + j) * a.q_row +
                        (int64_t)(s.head * a.G + col - j * a.G) * a.D + d;
         if (sizeof(T) == 4) {
@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(kGenThreads, C <= 2 ? 2 : 1) attend_general_ke
       }
       *reinterpret_cast<float4*>(sQ + c * a.D + d) = v;
     }
-    const int p_first = s.p + s.col0 / a.G, p_last = s.p + (s.col0 + s.cols - 1) / a.G;
+    const int p_first = s.p + group_row(a, s.col0), p_last = s.p + group_row(a, s.col0 + s.cols - 1);
     // four threads per token
     auto load_tile = [&](int x, int stage) {
       const int tok = tid >> 2, pos = place_position(s.tiles, x * kGenTile + tok);
@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(kGenThreads, C <= 2 ? 2 : 1) attend_general_ke
           }
 #pragma unroll
           for (int c = 0; c < kGenQuarter; ++c) {
-            const int row = s.p + (s.col0 + min(c0 + c, s.cols - 1)) / a.G;
+            const int row = s.p + group_row(a, s.col0 + min(c0 + c, s.cols - 1));
             const bool seen = pos >= 0 && pos <= row && (a.window == 0 || pos > row - a.window || pos < a.sinks);
             masked |= !seen;
             sS[(c0 + c) * kGenPitchS + tok] = seen ? dot[c] * a.c2 : -INFINITY;
@@ -380,6 +380,7 @@ extern "C" int spec_attend(const void* q, int64_t q_row_stride, int q_heads, con
   a.Hq = q_heads;
   a.Hkv = cache->kv_heads;
   a.G = q_heads / cache->kv_heads;
+  a.g_inverse = (uint32_t)(((1ull << 32) + a.G - 1) / a.G);
   a.D = cache->head_dim;
   a.table = page_table;
   a.rows = RowLayout{row_offsets, depth, pos_base, B, K};

@@ -31,6 +31,7 @@ struct AttendLaunch {
   int64_t page_b, token_b, head_b;
   int pages, page_size, max_pages;
   int Hq, Hkv, G, D;
+  uint32_t g_inverse;  // 2^32 / G, rounded up
   const int32_t* table;
   RowLayout rows;
   float c2;    // scale * log2(e)
@@ -46,6 +47,12 @@ struct AttendLaunch {
   int ctas;
   int lists;          // 1, or one per key-value head
 };
+
+// The row of a column: column / G, exact for the fewer than 2^15 columns of a
+// request and G <= 64 (the reciprocal is rounded up by less than G / 2^32).
+__device__ __forceinline__ int group_row(const AttendLaunch& a, int column) {
+  return a.G == 1 ? column : (int)__umulhi((uint32_t)column, a.g_inverse);
+}
 
 // What rows at positions p_first..p_last see, as one run of places: the sinks'
 // positions 0 .. ns - 1, then the window's from w0, both in whole grains (what a
@@ -99,7 +106,7 @@ __device__ __forceinline__ int head_units(const AttendLaunch& a, const AttendRow
   int n = 0;
   for (int c0 = 0; c0 < cols; c0 += a.ct) {
     const int c1 = min(cols, c0 + a.ct) - 1;
-    n += item_tiles<TT>(a, r.p + c0 / a.G, r.p + c1 / a.G).count;
+    n += item_tiles<TT>(a, r.p + group_row(a, c0), r.p + group_row(a, c1)).count;
   }
   return n;
 }
@@ -236,7 +243,7 @@ struct Walk {
   __device__ __forceinline__ void set_tiles() {
     const int cols = r.count * a.G;
     t = cols <= a.ct ? item_tiles<TT>(a, r.p, r.p + r.count - 1)
-                     : item_tiles<TT>(a, r.p + c0 / a.G, r.p + (min(cols, c0 + a.ct) - 1) / a.G);
+                     : item_tiles<TT>(a, r.p + group_row(a, c0), r.p + group_row(a, min(cols, c0 + a.ct) - 1));
   }
   // The CTA (of the list) whose range holds unit x.
   __device__ __forceinline__ int owner(long long x) const {
@@ -293,7 +300,7 @@ __device__ __forceinline__ int part_slot(const Segment& s, int x) {
 
 // Where column c of a segment goes: packed row * Hq + query head.
 __device__ __forceinline__ long long out_index(const AttendLaunch& a, const Segment& s, int c) {
-  const int col = s.col0 + c, j = col / a.G;
+  const int col = s.col0 + c, j = group_row(a, col);
   return (long long)(s.row0 + j) * a.Hq + s.head * a.G + (col - j * a.G);
 }
 

@@ -305,7 +305,7 @@ __device__ __forceinline__ float column_sum8(float (&v)[8], int lane) {
 // plain loop over the cache.
 template <int D>
 __device__ __noinline__ float cleared_values(const AttendLaunch& a, const Segment& s, int r, int d) {
-  const int p_first = s.p + s.col0 / a.G, p_last = s.p + (s.col0 + s.cols - 1) / a.G;
+  const int p_first = s.p + group_row(a, s.col0), p_last = s.p + group_row(a, s.col0 + s.cols - 1);
   float sum = 0.0f;
   for (int x = 0; x < s.ntiles; ++x) {
     for (int y = 0; y < kTile; ++y) {
@@ -332,7 +332,7 @@ template <int D>
 __device__ __forceinline__ void load_queries(const AttendLaunch& a, const Segment& s, uint32_t dst, int i, int threads) {
   constexpr int kVecs = D / 8;
   const int N = (s.cols + 15) / 16 * 16, step = threads / kVecs, v = i % kVecs;
-  int c = i / kVecs, j = (s.col0 + c) / a.G, g = s.col0 + c - j * a.G;
+  int c = i / kVecs, j = group_row(a, s.col0 + c), g = s.col0 + c - j * a.G;
   const __nv_bfloat16* row = static_cast<const __nv_bfloat16*>(a.q) + (int64_t)(s.row0 + j) * a.q_row +
                              (int64_t)s.head * a.G * D + v * 8;
   uint32_t at = dst + (v >> 3) * a.ct * 128 + c * 128;
@@ -438,6 +438,7 @@ __device__ __noinline__ void join_tc(const AttendLaunch& a, const Segment& s, co
     }
     named_sync(1, threads);
     if (nc * (D / 4) <= threads) add_parts<D, 1, 8>(a, s, where, weights, c0, nc, tid, threads);
+    else if (parts <= 2) add_parts<D, 8, 2>(a, s, where, weights, c0, nc, tid, threads);
     else add_parts<D, 4, 4>(a, s, where, weights, c0, nc, tid, threads);
     named_sync(1, threads);
   }
@@ -563,7 +564,7 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
         break;
       }
       if (s.request < 0) break;
-      const int p_first = s.p + s.col0 / a.G, p_last = s.p + (s.col0 + s.cols - 1) / a.G, ntiles = s.ntiles;
+      const int p_first = s.p + group_row(a, s.col0), p_last = s.p + group_row(a, s.col0 + s.cols - 1), ntiles = s.ntiles;
       const int cols = s.cols, N = (cols + 15) / 16 * 16, wide = set_cols<H>(N);
       const int cb = hf * wide, gc = wide / 8;  // this set's columns: gc groups of 8 from cb
       const ItemTiles tiles = s.tiles;
@@ -571,7 +572,7 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
       if (n == 0) load_queries<D>(a, s, ring + t.q_off, st, kSoftThreads);
       for (int c = st; c < N; c += kSoftThreads) {
         const int cc = min(c, cols - 1);
-        sRow[c + (c >= wide ? kSetCols - wide : 0)] = s.p + (s.col0 + cc) / a.G;
+        sRow[c + (c >= wide ? kSetCols - wide : 0)] = s.p + group_row(a, s.col0 + cc);
         sOut[c] = out_index(a, s, cc);
       }
       if (tl < kSetCols) ref[tl] = tl < gc * 8 ? -kNoMax : -INFINITY;
@@ -793,7 +794,10 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
       tc_fence_after();
       named_sync(1, kSoftThreads);
       const bool poisoned = poison != 0;
-      // sixteen columns at a time, this thread's d = tl of each
+      // sixteen columns at a time, this thread's d = tl of each; a whole item's rows
+      // go through the weights' buffer (every product of the segment is complete),
+      // so that they are stored 16 bytes a thread
+      __nv_bfloat16* staged = reinterpret_cast<__nv_bfloat16*>(smem + t.p_off + hf * t.p_bytes);
 #pragma unroll 1
       for (int g = 0; g < gc; g += 2) {
         float o[16], rest[16];
@@ -813,9 +817,10 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
           }
         }
         if (whole) {
+          __nv_bfloat16* row = staged + g * 8 * D + tl;
 #pragma unroll
           for (int j = 0; j < 16; ++j)
-            if (j < nc) static_cast<__nv_bfloat16*>(a.out)[sOut[c0 + j] * D + tl] = __float2bfloat16(o[j] * factor[g * 8 + j]);
+            if (j < nc) row[j * D] = __float2bfloat16(o[j] * factor[g * 8 + j]);
         } else {
           float* part = a.part + ((size_t)slot * a.ct + c0) * D + tl;
 #pragma unroll
@@ -826,6 +831,15 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&o_free);
+      if (whole) {
+        named_sync(2 + hf, 128);
+        const int nv = max(0, min(cols - cb, gc * 8)) * (D / 8);
+#pragma unroll 4
+        for (int e = tl; e < nv; e += 128) {
+          const int c = e / (D / 8);
+          static_cast<uint4*>(a.out)[sOut[cb + c] * (D / 8) + e % (D / 8)] = reinterpret_cast<const uint4*>(staged)[e];
+        }
+      }
       if (!whole) {
         named_sync(1, kSoftThreads);
         if (st == 0) {
@@ -873,7 +887,7 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
         Segment s;
         ok = take(n, &s);
         if (!ok || s.request < 0) break;
-        const int p_first = s.p + s.col0 / a.G, p_last = s.p + (s.col0 + s.cols - 1) / a.G;
+        const int p_first = s.p + group_row(a, s.col0), p_last = s.p + group_row(a, s.col0 + s.cols - 1);
         const int32_t* row = a.table + (size_t)s.request * a.max_pages;
         // does some row see this lane's positions of tile x?
         auto seen = [&](int x) {

@@ -41,6 +41,7 @@ __global__ void __launch_bounds__(32 * kAppendWarps) append_kernel(const AppendL
   const long long r = (long long)blockIdx.x * kAppendWarps + (threadIdx.x >> 5);
   const int K1 = p.rows.K + 1;
   pdl_wait_prerequisites();
+  pdl_launch_dependents();
   if (r >= (long long)p.rows.B * K1) return;
   const int i = (int)(r / K1), j = (int)(r - (long long)i * K1);
   const RequestRows q = request_rows(p.rows, i);
@@ -115,6 +116,7 @@ __global__ void __launch_bounds__(32 * kCopyWarps) copy_pages_kernel(const CopyL
   const long long warp = (long long)blockIdx.x * kCopyWarps + (threadIdx.x >> 5);
   const long long warps = (long long)gridDim.x * kCopyWarps;
   pdl_wait_prerequisites();
+  pdl_launch_dependents();
   int n = *p.count;
   if (n < 0 || n > p.max_count) {
     if (warp == 0 && lane == 0) report(p.status, SPEC_ERR_BAD_INPUT);
@@ -228,6 +230,7 @@ __global__ void __launch_bounds__(kForkThreads) fork_refs_kernel(const ForkLaunc
   __syncthreads();
   const int change = children - 1;
   pdl_wait_prerequisites();  // the counts' copy
+  pdl_launch_dependents();
   if (change == 0) return;
 #pragma unroll
   for (int k = 0; k < kForkPer; ++k)
@@ -345,6 +348,7 @@ __global__ void __cluster_dims__(kPageCluster, 1, 1) __launch_bounds__(kPageThre
   __shared__ int sums[33], slot;
   cg::cluster_group cluster = cg::this_cluster();
   pdl_wait_prerequisites();
+  pdl_launch_dependents();
   int begin, end, total;
   page_range(p.pages, &begin, &end);
   int mine = 0;
@@ -444,6 +448,7 @@ constexpr int kReleasePer = 4;
 __global__ void __launch_bounds__(kReleaseThreads) release_kernel(const ReleaseLaunch p, int segs) {
   const int i = (int)(blockIdx.x / segs), seg = (int)(blockIdx.x - (long long)i * segs);
   pdl_wait_prerequisites();
+  pdl_launch_dependents();
   const long long pos = __ldg(reinterpret_cast<const long long*>(p.pos_base) + i), far = 1LL << 40;
   int64_t keep = pos > far ? far : pos < -far ? -far : pos;
   int e[kReleasePer];
@@ -551,6 +556,7 @@ __global__ void __launch_bounds__(kForkThreads) remap_kernel(const CompactLaunch
     e[k] = x < n ? p.table[x] : -1;
   }
   pdl_wait_prerequisites();  // the map
+  pdl_launch_dependents();
 #pragma unroll
   for (int k = 0; k < kForkPer; ++k) {
     if (e[k] == -1) continue;
