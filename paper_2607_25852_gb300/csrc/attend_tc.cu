@@ -266,13 +266,14 @@ __device__ __forceinline__ void split_bf16(float x, float y, uint32_t* hi, uint3
   const float2 rest = unpair(fma2(upper, pair(-1.0f, -1.0f), pair(x, y)));
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(*lo) : "f"(rest.y), "f"(rest.x));
 }
+// Not ordered with loads from other places (nothing reads the weights' buffer
+// back): only with other volatile statements, the fence among them.
 __device__ __forceinline__ void st_shared16_if(bool yes, uint32_t at, const uint32_t (&w)[4]) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
       "setp.ne.u32 p, %0, 0;\n\t"
       "@p st.shared.v4.b32 [%1], {%2,%3,%4,%5};\n\t}" ::"r"((uint32_t)yes),
-      "r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
-      : "memory");
+      "r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]));
 }
 // Columns of each softmax set, for an item of N (a multiple of 16).
 template <int H>
@@ -691,40 +692,30 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
             tc_fence_before();
           }
         }
-        // ---- weights, split in two.  With few columns a thread they stay in
-        // registers until their buffer is free, with many they are stored as they
-        // come.  The buffer's last reader is unit u - 2; with one set its product
-        // was issued before this tile's scores, so those say that it is done ----
+        // ---- weights, split in two, stored as they come.  Their buffer's last reader
+        // is unit u - 2; with one set its product was issued before this tile's
+        // scores, so those say that it is done.  (Keeping the weights in registers
+        // until the buffer is free cost 6 % at 48 columns a thread.) ----
         const int u = U + hf;
         mine_u = u;
-        constexpr bool kStoreNow = CG > 6;
+        if (H > 1 && u >= PB) wait_unit(u - PB);
         const uint32_t pw = ring + t.p_off + (u % PB) * t.p_bytes + tl * 32;
         const uint32_t swap = (uint32_t)((tl >> 2) & 1) << 4;
-        auto store = [&](int g, const uint32_t (&x)[2][4]) {
-          const int lo = gc + g;  // the rests' groups follow the upper halves'
-          st_shared16_if(g < gc, pw + (g >> 1) * kPChunkBytes + (((uint32_t)(g & 1) << 4) ^ swap), x[0]);
-          st_shared16_if(g < gc, pw + (lo >> 1) * kPChunkBytes + (((uint32_t)(lo & 1) << 4) ^ swap), x[1]);
-        };
-        uint32_t w[kStoreNow ? 1 : CG][2][4];
-        if (kStoreNow && H > 1 && u >= PB) wait_unit(u - PB);
 #pragma unroll
         for (int g = 0; g < CG; ++g) {
           f32x2 m[4];
           load_pairs(m, ref + g * 8);
-          uint32_t(&x)[2][4] = w[kStoreNow ? 0 : g];
+          uint32_t hi[4], lo[4];
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const float2 d = unpair(fma2(pair(v[8 * g + 2 * j], v[8 * g + 2 * j + 1]), c2, m[j]));
             const float x0 = ex2_approx(d.x), x1 = ex2_approx(d.y);
             l[4 * g + j] = add2(l[4 * g + j], pair(x0, x1));
-            split_bf16(x0, x1, &x[0][j], &x[1][j]);
+            split_bf16(x0, x1, &hi[j], &lo[j]);
           }
-          if (kStoreNow) store(g, x);
-        }
-        if (!kStoreNow) {
-          if (H > 1 && u >= PB) wait_unit(u - PB);
-#pragma unroll
-          for (int g = 0; g < CG; ++g) store(g, w[kStoreNow ? 0 : g]);
+          const int r = gc + g;  // the rests' groups follow the upper halves'
+          st_shared16_if(g < gc, pw + (g >> 1) * kPChunkBytes + (((uint32_t)(g & 1) << 4) ^ swap), hi);
+          st_shared16_if(g < gc, pw + (r >> 1) * kPChunkBytes + (((uint32_t)(r & 1) << 4) ^ swap), lo);
         }
         U += H;
         if (edge && hf == 0) {
