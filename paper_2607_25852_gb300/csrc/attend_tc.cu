@@ -38,104 +38,18 @@
 // Every mbarrier wait is bounded (about a second): a wait that gives up sets
 // SPEC_ERR_TIMEOUT and the kernel ends; the softmax warps, which meet at
 // barriers, leave together by a vote.
-#include <algorithm>
-
-#include "attend.cuh"
-#include "attend_tc.cuh"
-#include "tensor_core.cuh"
+#include "attend_ring.cuh"
 
 namespace spec {
 
 namespace {
 
-constexpr int kTile = 128;        // positions per tile: the M of S^T
-constexpr int kHalfBytes = kTile * 128;  // 64 elements of 128 positions
-constexpr int kMaxSlots = 12;
-constexpr int kSegRing = 4;
-constexpr int kBadRing = 32;      // tiles between the loader and the softmax: fewer than 2 kMaxSlots
 // Items of few columns and small tiles go two CTAs to an SM: a CTA's chain from
 // scores to weights to output is longer than the time its tile takes to arrive,
 // and the ends of its items leave the loads idle.  (With D = 128 the tiles are
 // twice as large: one CTA's chain keeps up, and two would not have three tiles'
 // room each.)
 constexpr bool two_per_sm(int D, int CG) { return D == 64 && CG == 2; }
-constexpr float kNoMax = -3.0e38f;  // the reference of a column that has seen nothing
-constexpr float kGrowth = 24.0f;  // log2 of how far weights may exceed 1
-
-struct TcPlan {
-  int chunk, nchunk;    // positions per TMA box, boxes per tile and half
-  int slots;            // ring slots (a K or V tile each)
-  int q_off, p_off;     // bytes from the start of shared memory
-  int p_bytes;          // of one buffer of weights
-};
-
-// A place in a ring and the parity of its current use, stepped without a division.
-struct RingPos {
-  int slot;
-  uint32_t use;
-  __device__ __forceinline__ void step(int n, int slots) {
-    slot += n;
-    if (slot >= slots) {
-      slot -= slots;
-      use ^= 1u;
-    }
-  }
-};
-
-// ---- PTX ----
-__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w,
-                                            uint64_t* bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], "
-      "[%6];" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
-      : "memory");
-}
-// mbar_wait with its loop inline: a call would cost the softmax its registers
-// around every wait.
-__device__ __forceinline__ bool wait_phase(uint64_t* bar, uint32_t parity, int32_t* status) {
-  if (mbar_try_wait(bar, parity)) return true;
-  const uint64_t t0 = global_ns();
-  for (uint32_t it = 1; !mbar_try_wait(bar, parity); ++it) {
-    if ((it & 255u) == 0u && global_ns() - t0 > 1000000000ull) {
-      report(status, SPEC_ERR_TIMEOUT);
-      return false;
-    }
-  }
-  return true;
-}
-__device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-// One lane of a converged warp.  The compiler knows elect.sync: descriptors and
-// coordinates under it go to the uniform registers that MMAs and TMA take (an
-// MMA issued by `lane == 0` costs 138 cycles instead).
-__device__ __forceinline__ bool elect_one() {
-  uint32_t r;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "elect.sync _|p, 0xffffffff;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(r));
-  return r != 0;
-}
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool real) {
-  // nothing is read where `real` is false: 16 zero bytes are written
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void named_sync(int id, int threads) {
-  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
-}
-__device__ __forceinline__ bool named_or(int id, int threads, bool x) {
-  uint32_t r;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t"
-      "setp.ne.u32 p, %1, 0;\n\t"
-      "bar.red.or.pred q, %2, %3, p;\n\t"
-      "selp.u32 %0, 1, 0, q;\n\t}"
-      : "=r"(r)
-      : "r"((uint32_t)x), "r"(id), "r"(threads)
-      : "memory");
-  return r != 0;
-}
 __device__ __forceinline__ void tmem_ld8(uint32_t addr, float* v) {
   uint32_t r[8];
   asm volatile(
@@ -190,64 +104,12 @@ __device__ __forceinline__ void tmem_st8(uint32_t addr, const float* v) {
                "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7]))
                : "memory");
 }
-__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
-// Matrix descriptors: the address (in 16-byte units) in the low word, to which
-// offsets are added, above it the strides and the swizzle.
-constexpr uint32_t kDescVersion = 1u << 14;
-__device__ __forceinline__ uint64_t desc(uint32_t lo, uint32_t hi) {
-  uint64_t d;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(lo), "r"(hi));
-  return d;
-}
-// K and Q: K-major, 128-byte swizzle, 1024 bytes to the next 8 rows.
-constexpr uint32_t kHiKQ = (1024u >> 4) | kDescVersion | 2u << 29;
-__device__ __forceinline__ uint32_t lo_kq(uint32_t saddr) { return (saddr >> 4) | 1u << 16; }
-// V as the A operand, read transposed (its d is contiguous): 128-byte swizzled
-// atoms of 64 d x 8 positions; `next` bytes to the next 64 d, 1024 to the next
-// 8 positions.
-constexpr uint32_t kHiV = (1024u >> 4) | kDescVersion | 2u << 29;
-__device__ __forceinline__ uint32_t lo_v(uint32_t saddr, uint32_t next) { return (saddr >> 4) | (next >> 4) << 16; }
 // P^T as the B operand, a position's columns contiguous: 32-byte swizzled atoms
 // of 16 columns x 8 positions; 4096 bytes to the next 16 columns, 256 to the
 // next 8 positions.
 constexpr int kPChunkBytes = kTile * 32;
 constexpr uint32_t kHiP = (256u >> 4) | kDescVersion | 6u << 29;
 __device__ __forceinline__ uint32_t lo_p(uint32_t saddr) { return (saddr >> 4) | (uint32_t)(kPChunkBytes >> 4) << 16; }
-constexpr uint32_t kTransposeA = 1u << 15, kTransposeB = 1u << 16;
-
-// Two fp32 numbers in one register pair, for the packed instructions.
-typedef unsigned long long f32x2;
-__device__ __forceinline__ f32x2 pair(float x, float y) {
-  f32x2 r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
-  return r;
-}
-__device__ __forceinline__ float2 unpair(f32x2 p) {
-  float2 r;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(p));
-  return r;
-}
-__device__ __forceinline__ f32x2 fma2(f32x2 x, f32x2 y, f32x2 z) {
-  f32x2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(x), "l"(y), "l"(z));
-  return r;
-}
-__device__ __forceinline__ f32x2 add2(f32x2 x, f32x2 y) {
-  f32x2 r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
-  return r;
-}
-__device__ __forceinline__ f32x2 mul2(f32x2 x, f32x2 y) {
-  f32x2 r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
-  return r;
-}
-__device__ __forceinline__ float max3(float x, float y, float z) {
-  float r;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
-  return r;
-}
 // Four pairs of shared memory.
 __device__ __forceinline__ void load_pairs(f32x2 (&p)[4], const float* at) {
   const ulonglong2 a = *reinterpret_cast<const ulonglong2*>(at), b = *reinterpret_cast<const ulonglong2*>(at + 4);
@@ -257,14 +119,6 @@ __device__ __forceinline__ void load_rows(int (&r)[8], const int* rows) {
   const int4 a = *reinterpret_cast<const int4*>(rows), b = *reinterpret_cast<const int4*>(rows + 4);
   r[0] = a.x; r[1] = a.y; r[2] = a.z; r[3] = a.w;
   r[4] = b.x; r[5] = b.y; r[6] = b.z; r[7] = b.w;
-}
-// Two weights as pairs of bf16 numbers: their upper halves, and the rest rounded.
-__device__ __forceinline__ void split_bf16(float x, float y, uint32_t* hi, uint32_t* lo) {
-  const uint32_t xb = __float_as_uint(x), yb = __float_as_uint(y);
-  *hi = __byte_perm(xb, yb, 0x7632);
-  const f32x2 upper = pair(__uint_as_float(xb & 0xFFFF0000u), __uint_as_float(yb & 0xFFFF0000u));
-  const float2 rest = unpair(fma2(upper, pair(-1.0f, -1.0f), pair(x, y)));
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(*lo) : "f"(rest.y), "f"(rest.x));
 }
 // Not ordered with loads from other places (nothing reads the weights' buffer
 // back): only with other volatile statements, the fence among them.
@@ -280,8 +134,6 @@ template <int H>
 __device__ __forceinline__ int set_cols(int N) {
   return N / H;
 }
-__device__ __forceinline__ bool bf16_not_finite(uint32_t h) { return (h & 0x7F80u) == 0x7F80u; }
-
 // Column sums over a warp's lanes of 8 values per lane: afterwards lanes 4k
 // hold the sum of column k.
 __device__ __forceinline__ float column_sum8(float (&v)[8], int lane) {
@@ -300,150 +152,6 @@ __device__ __forceinline__ float column_sum8(float (&v)[8], int lane) {
   return v[0];  // column 4 * bit4 + 2 * bit3 + bit2 = lane / 4
 }
 
-// What was cleared in shared memory for the sake of rows that must not see it,
-// for a row (at position r) that does: the values at d, of the positions that
-// some of the item's rows see and some do not, that are not finite.  Rare, so a
-// plain loop over the cache.
-template <int D>
-__device__ __noinline__ float cleared_values(const AttendLaunch& a, const Segment& s, int r, int d) {
-  const int p_first = s.p + group_row(a, s.col0), p_last = s.p + group_row(a, s.col0 + s.cols - 1);
-  float sum = 0.0f;
-  for (int x = 0; x < s.ntiles; ++x) {
-    for (int y = 0; y < kTile; ++y) {
-      const int pos = place_position(s.tiles, (s.tile0 + x) * kTile + y);
-      const bool any = pos <= p_last && (a.window == 0 || pos > p_first - a.window || pos < a.sinks);
-      const bool all = pos <= p_first && (a.window == 0 || pos > p_last - a.window || pos < a.sinks);
-      const bool seen = pos <= r && (a.window == 0 || pos > r - a.window || pos < a.sinks);
-      if (!any || all || !seen) continue;
-      const int page = a.table[(size_t)s.request * a.max_pages + pos / a.page_size];
-      if (page < 0 || page >= a.pages) continue;
-      const char* at = a.v + (int64_t)page * a.page_b + (int64_t)(pos % a.page_size) * a.token_b + s.head * a.head_b;
-      const float v = load_elem(reinterpret_cast<const __nv_bfloat16*>(at) + d);
-      if (!isfinite(v)) sum += v;
-    }
-  }
-  return sum;
-}
-
-// An item's queries into shared memory, [64-element halves][column][128 bytes]
-// with the 128-byte swizzle, columns past the last zero: `threads` threads (a
-// multiple of 32), thread i a vector of every (threads / vectors)-th column.
-// The column's row and head move along without divisions.
-template <int D>
-__device__ __forceinline__ void load_queries(const AttendLaunch& a, const Segment& s, uint32_t dst, int i, int threads) {
-  constexpr int kVecs = D / 8;
-  const int N = (s.cols + 15) / 16 * 16, step = threads / kVecs, v = i % kVecs;
-  int c = i / kVecs, j = group_row(a, s.col0 + c), g = s.col0 + c - j * a.G;
-  const __nv_bfloat16* row = static_cast<const __nv_bfloat16*>(a.q) + (int64_t)(s.row0 + j) * a.q_row +
-                             (int64_t)s.head * a.G * D + v * 8;
-  uint32_t at = dst + (v >> 3) * a.ct * 128 + c * 128;
-  for (; c < N; c += step, at += step * 128) {
-    const bool real = c < s.cols;
-    cp_async16(at + (((v & 7) ^ (c & 7)) << 4), real ? row + g * D : static_cast<const __nv_bfloat16*>(a.q), real);
-    g += step;
-    while (g >= a.G) {
-      g -= a.G;
-      row += a.q_row;
-    }
-  }
-  asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
-  proxy_fence();
-}
-
-// Adds up E vectors of four consecutive d, X parts at a time, whose loads are all
-// in flight together: what a join costs is the latency of its loads, and, as it
-// runs once a CTA, of fetching its instructions, so its loops are short.
-template <int D, int E, int X>
-__device__ __forceinline__ void add_parts(const AttendLaunch& a, const Segment& s, const long long* where,
-                                          const float* weights, int c0, int nc, int tid, int threads) {
-  constexpr int kQ = D / 4;
-#pragma unroll 1
-  for (int e0 = tid; e0 < nc * kQ; e0 += threads * E) {
-    float4 o[E];
-#pragma unroll
-    for (int k = 0; k < E; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 1
-    for (int x0 = 0; x0 < s.parts; x0 += X) {
-      float4 w[X][E];
-      float f[X][E];
-#pragma unroll
-      for (int y = 0; y < X; ++y) {
-        const int x = min(x0 + y, s.parts - 1);
-        const float4* from = reinterpret_cast<const float4*>(a.part + ((size_t)part_slot(s, x) * a.ct + c0) * D);
-#pragma unroll
-        for (int k = 0; k < E; ++k) {
-          const int e = min(e0 + k * threads, nc * kQ - 1);
-          w[y][k] = __ldcg(from + e);
-          f[y][k] = x0 + y < s.parts ? weights[x * nc + e / kQ] : 0.0f;
-        }
-      }
-#pragma unroll
-      for (int y = 0; y < X; ++y)
-#pragma unroll
-        for (int k = 0; k < E; ++k)
-          if (f[y][k] != 0.0f) {  // a part that saw nothing adds nothing
-            o[k].x = fmaf(w[y][k].x, f[y][k], o[k].x);
-            o[k].y = fmaf(w[y][k].y, f[y][k], o[k].y);
-            o[k].z = fmaf(w[y][k].z, f[y][k], o[k].z);
-            o[k].w = fmaf(w[y][k].w, f[y][k], o[k].w);
-          }
-    }
-#pragma unroll
-    for (int k = 0; k < E; ++k) {
-      const int e = e0 + k * threads, c = e / kQ;
-      if (c < nc) store4(static_cast<__nv_bfloat16*>(a.out) + where[c0 + c] * D + 4 * (e % kQ), o[k]);
-    }
-  }
-}
-
-// Adds the parts of a divided item up, in order, with `threads` threads past the
-// arrival of the last part.  Groups of lanes find the weights of a column's
-// parts, a part per lane; they go to `weights` (`room` floats of shared memory),
-// for as many columns at a time as fit.
-template <int D>
-__device__ __noinline__ void join_tc(const AttendLaunch& a, const Segment& s, const long long* where, float* weights,
-                                     int room, int tid, int threads) {
-  const int parts = s.parts, most = max(1, room / parts);
-  int group = 2;  // lanes per column: a power of two
-  while (group < parts && group < 32) group *= 2;
-  const int first = tid & (group - 1);
-#pragma unroll 1
-  for (int c0 = 0; c0 < s.cols; c0 += most) {
-    const int nc = min(most, s.cols - c0);
-#pragma unroll 1
-    for (int b = 0; b < nc; b += threads / group) {  // all lanes stay for the shuffles
-      const int c = b + tid / group;
-      float m = -INFINITY, l = 0.0f;
-#pragma unroll 1
-      for (int x0 = 0; x0 < parts; x0 += group) {  // one round but for more than 32 parts
-        const int x = x0 + first;
-        const bool mine = x < parts && c < nc;
-        const float2 st = mine ? __ldcg(a.part_stat + (size_t)part_slot(s, x) * a.ct + c0 + c)
-                               : make_float2(-INFINITY, 0.0f);
-        float mn = fmaxf(m, st.x);
-#pragma unroll 1
-        for (int o = group / 2; o > 0; o >>= 1) mn = fmaxf(mn, __shfl_xor_sync(0xFFFFFFFFu, mn, o));
-        float sum = st.y * part_weight(st, mn);
-#pragma unroll 1
-        for (int o = group / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-        l = fmaf(l, part_weight(make_float2(m, l), mn), sum);
-        m = mn;
-        if (mine) weights[x * nc + c] = st.x;
-      }
-      if (c >= nc) continue;
-      const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-#pragma unroll 1
-      for (int x = first; x < parts; x += group)
-        weights[x * nc + c] = part_weight(make_float2(weights[x * nc + c], 0.0f), m) * inv;
-      if (first == 0 && a.lse) a.lse[where[c0 + c]] = row_lse(m, l);
-    }
-    named_sync(1, threads);
-    if (nc * (D / 4) <= threads) add_parts<D, 1, 8>(a, s, where, weights, c0, nc, tid, threads);
-    else if (parts <= 2) add_parts<D, 8, 2>(a, s, where, weights, c0, nc, tid, threads);
-    else add_parts<D, 4, 4>(a, s, where, weights, c0, nc, tid, threads);
-    named_sync(1, threads);
-  }
-}
 
 // ---------------------------------------------------------------------------
 // D: head dimension.  CG: groups of 8 columns per softmax thread.  H: sets of
@@ -465,43 +173,28 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
   constexpr int kSoftThreads = 128 * H;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  __shared__ uint64_t full[kMaxSlots], empty[kMaxSlots], s_full[2], s_free[2], p_full[2], p_free[4], o_free, drained, q_full[2],
-      q_free[2], seg_full[kSegRing], seg_free[kSegRing];
-  __shared__ Segment segs[kSegRing];
+  __shared__ Control ctl;
+  __shared__ uint64_t s_full[2], s_free[2], p_full[2], p_free[4], o_free;
   __shared__ Share share;
   __shared__ long long sums[32];
-  __shared__ int tile_bad[kBadRing];
   // per set and column: the reference's negative (-inf: no column), a factor, maxima and sums per warp
   __shared__ __align__(16) float sN[kCols], sF[kCols], red[4][kCols];
-  __shared__ int2 sPage[2][16];      // a tile's boxes: page, first position in it
   __shared__ __align__(16) int sRow[kCols];        // position of the column's row
   __shared__ long long sOut[kCols];  // where the column goes
   __shared__ uint32_t tmem_sh;
-  __shared__ int abort_flag, poison, last_sh;
-  volatile int& aborted = abort_flag;
+  __shared__ int poison, last_sh;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
   if (tid == 0) {
-    for (int k = 0; k < t.slots; ++k) {
-      mbar_init(&full[k], 1);
-      mbar_init(&empty[k], 1);
-    }
+    init_control(ctl, t.slots, 3 + 4 * H);
     for (int k = 0; k < 2; ++k) {
       mbar_init(&s_full[k], 1);
       mbar_init(&s_free[k], 4 * H);
       mbar_init(&p_full[k], 4);
       mbar_init(&p_free[k], 1);
       mbar_init(&p_free[2 + k], 1);
-      mbar_init(&q_full[k], 1);
-      mbar_init(&q_free[k], 1);
     }
     mbar_init(&o_free, 4 * H);
-    mbar_init(&drained, 1);
-    for (int k = 0; k < kSegRing; ++k) {
-      mbar_init(&seg_full[k], 1);
-      mbar_init(&seg_free[k], 3 + 4 * H);
-    }
-    abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
@@ -521,16 +214,6 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
   const uint32_t tmem = tmem_sh;
   const uint32_t tO = tmem + kOut;
   const uint32_t ring = smem_u32(smem);
-
-  // The next segment of the share, for a reading warp (n counts segments).
-  auto take = [&](int n, Segment* s) -> bool {
-    const int k = n % kSegRing;
-    const bool ok = __all_sync(0xFFFFFFFFu, wait_phase(&seg_full[k], (uint32_t)((n / kSegRing) & 1), a.status));
-    *s = segs[k];
-    __syncwarp();
-    if (lane == 0) mbar_arrive(&seg_free[k]);
-    return ok;
-  };
 
   // Two softmax sets need more than the 168 registers a thread that 384 threads
   // get: 4 warps x 32 x 56 + 8 x 32 x 224 = 64,512 = 384 x 168.
@@ -558,10 +241,10 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
     // and who waits for u knows of u - 2 H or later.
     auto wait_unit = [&](int u) { wait(&p_free[u & 3], (uint32_t)u >> 2); };
     for (int n = 0;; ++n) {
-      const Segment& s = segs[n % kSegRing];  // given back at the segment's end
-      wait(&seg_full[n % kSegRing], n / kSegRing);
+      const Segment& s = ctl.segs[n % kSegRing];  // given back at the segment's end
+      wait(&ctl.seg_full[n % kSegRing], n / kSegRing);
       if (named_or(1, kSoftThreads, failed)) {  // no one has left the last segment's end behind
-        aborted = 1;
+        ctl.aborted = 1;
         break;
       }
       if (s.request < 0) break;
@@ -570,7 +253,7 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
       const int cb = hf * wide, gc = wide / 8;  // this set's columns: gc groups of 8 from cb
       const ItemTiles tiles = s.tiles;
       const int tile0 = s.tile0;
-      if (n == 0) load_queries<D>(a, s, ring + t.q_off, st, kSoftThreads);
+      if (n == 0) load_queries<D>(a, s, ring + t.q_off, a.ct, st, kSoftThreads);
       for (int c = st; c < N; c += kSoftThreads) {
         const int cc = min(c, cols - 1);
         sRow[c + (c >= wide ? kSetCols - wide : 0)] = s.p + group_row(a, s.col0 + cc);
@@ -579,7 +262,7 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
       if (tl < kSetCols) ref[tl] = tl < gc * 8 ? -kNoMax : -INFINITY;
       if (st == 0) poison = 0;
       named_sync(1, kSoftThreads);
-      if (n == 0 && st == 0) mbar_arrive(&q_full[0]);
+      if (n == 0 && st == 0) mbar_arrive(&ctl.q_full[0]);
       f32x2 l[CG * 4];
 #pragma unroll
       for (int j = 0; j < CG * 4; ++j) l[j] = 0ull;
@@ -588,7 +271,7 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
         const int b = T % SB, first = (tile0 + x) * kTile, t0 = place_position(tiles, first);
         wait(&s_full[b], T / SB);
         tc_fence_after();
-        const int bads = tile_bad[T % kBadRing];
+        const int bads = ctl.tile_bad[T % kBadRing];
         // do all rows see all of the tile's positions (t0 .. t0 + kTile - 1, or some sinks and some others)?
         const bool edge = !(t0 + kTile - 1 <= p_first && (first >= tiles.ns || first + kTile <= tiles.ns) &&
                             (a.window == 0 || t0 > p_last - a.window || t0 + kTile <= a.sinks)) ||
@@ -724,31 +407,8 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
           const bool any = !gone && pos <= p_last && (a.window == 0 || pos > p_first - a.window || pos < a.sinks);
           const bool all = !gone && pos <= p_first && (a.window == 0 || pos > p_last - a.window || pos < a.sinks);
           if (!__all_sync(0xFFFFFFFFu, all)) {
-            wait(&full[vp.slot], vp.use);
-            uint8_t* row = smem + vp.slot * kSlotBytes + tl * 128;
-            if (!any) {
-#pragma unroll
-              for (int k = 0; k < D / 8; ++k)
-                *reinterpret_cast<uint4*>(row + (k >> 3) * kHalfBytes + (((k & 7) ^ (tl & 7)) << 4)) =
-                    make_uint4(0u, 0u, 0u, 0u);
-            } else if (!all) {
-              for (int k = 0; k < D / 8; ++k) {
-                uint4* at = reinterpret_cast<uint4*>(row + (k >> 3) * kHalfBytes + (((k & 7) ^ (tl & 7)) << 4));
-                uint4 w = *at;
-                uint32_t e[4] = {w.x, w.y, w.z, w.w};
-                bool found = false;
-#pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                  const bool lo = bf16_not_finite(e[y]), hi = bf16_not_finite(e[y] >> 16);
-                  found |= lo || hi;
-                  e[y] &= (lo ? 0xFFFF0000u : 0xFFFFFFFFu) & (hi ? 0x0000FFFFu : 0xFFFFFFFFu);
-                }
-                if (found) {
-                  poison = 1;
-                  *at = make_uint4(e[0], e[1], e[2], e[3]);
-                }
-              }
-            }
+            wait(&ctl.full[vp.slot], vp.use);
+            hide_values<D>(smem + vp.slot * kSlotBytes, tl, any, all, &poison);
           }
         }
         vp.step(2, t.slots);
@@ -846,91 +506,12 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
         }
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(&seg_free[n % kSegRing]);
+      if (lane == 0) mbar_arrive(&ctl.seg_free[n % kSegRing]);
     }
   } else {
     if constexpr (H == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     if (warp == 0) {
-      // ---- pages into the ring ----
-      const int c = lane;  // the box of this lane: positions c chunk .. of a tile
-      const bool mine = c < t.nchunk;
-      RingPos rp{0, 1u};          // the parity of the slot's previous use
-      // The ring's order is K0 K1 V0 K2 V1 ...: a tile's keys are loaded a tile
-      // ahead of its values, into the place of values that are done two tiles
-      // before, so that with three places the scores do not wait for the output.
-      int tiles = 0, issued = 0;  // tiles whose keys, places filled (by the lane that issues)
-      int v_head = 0;             // head of the tile whose values are due
-      auto fill = [&](const CUtensorMap* map, int head, const int2* pages) -> bool {
-        if (issued >= t.slots && !wait_phase(&empty[rp.slot], rp.use, a.status)) return false;
-        mbar_expect_tx(&full[rp.slot], kSlotBytes);
-        uint32_t dst = ring + rp.slot * kSlotBytes;
-        for (int b = 0; b < t.nchunk; ++b, dst += t.chunk * 128) {
-          const int2 pt = pages[b];
-          tma_load_4d(dst, map, 0, head, pt.y, pt.x, &full[rp.slot]);
-          if (D == 128) tma_load_4d(dst + kHalfBytes, map, 64, head, pt.y, pt.x, &full[rp.slot]);
-        }
-        ++issued;
-        rp.step(1, t.slots);
-        return true;
-      };
-      bool ok = true;
-      for (int n = 0; ok; ++n) {
-        Segment s;
-        ok = take(n, &s);
-        if (!ok || s.request < 0) break;
-        const int p_first = s.p + group_row(a, s.col0), p_last = s.p + group_row(a, s.col0 + s.cols - 1);
-        const int32_t* row = a.table + (size_t)s.request * a.max_pages;
-        // does some row see this lane's positions of tile x?
-        auto seen = [&](int x) {
-          const int pos = place_position(s.tiles, x * kTile + c * t.chunk);
-          return mine && pos <= p_last && (a.window == 0 || pos + t.chunk - 1 > p_first - a.window || pos < a.sinks);
-        };
-        int tok_next = 0;  // its first position in the page
-        auto lookup = [&](int x) {
-          const int pos = place_position(s.tiles, x * kTile + c * t.chunk), slot = pos / a.page_size;
-          tok_next = pos - slot * a.page_size;
-          return __ldg(row + slot);
-        };
-        bool wanted_next = seen(s.tile0);
-        int next = wanted_next ? lookup(s.tile0) : 0;
-        for (int x = 0; x < s.ntiles && ok; ++x, ++tiles) {
-          int page = next;
-          const int tok = wanted_next ? tok_next : 0;
-          const bool wanted = wanted_next;
-          if (x + 1 < s.ntiles) {  // the next tile's page, a tile ahead
-            wanted_next = seen(s.tile0 + x + 1);
-            next = wanted_next ? lookup(s.tile0 + x + 1) : 0;
-          }
-          const bool bad = wanted && (page < 0 || page >= a.pages);
-          const uint32_t bads = __ballot_sync(0xFFFFFFFFu, bad);
-          if (bad) report(a.status, SPEC_ERR_BAD_INPUT);
-          if (bad || !wanted) page = a.pages;  // past the map's last page: zeros are written, nothing is read
-          if (lane == 0) tile_bad[tiles % kBadRing] = (int)bads;
-          if (mine) sPage[tiles & 1][c] = make_int2(page, tok);
-          __syncwarp();
-          if (elect_one())
-            ok = !aborted && fill(&tmK, s.head, sPage[tiles & 1]) &&
-                 (tiles == 0 || fill(&tmV, v_head, sPage[(tiles - 1) & 1]));
-          v_head = s.head;
-          ok = __all_sync(0xFFFFFFFFu, ok);
-        }
-      }
-      if (ok && tiles > 0) {  // the last values; no keys go before them
-        if (elect_one()) {
-          ok = issued < t.slots || wait_phase(&empty[rp.slot], rp.use, a.status);
-          ++issued;
-          rp.step(1, t.slots);
-          ok = ok && fill(&tmV, v_head, sPage[(tiles - 1) & 1]);
-        }
-        ok = __all_sync(0xFFFFFFFFu, ok);
-      }
-      if (!ok) {
-        aborted = 1;
-        // what was issued has landed before the CTA ends
-        issued = (int)__reduce_max_sync(0xFFFFFFFFu, (unsigned)issued);
-        for (int u = max(0, issued - t.slots); u < issued; ++u)
-          wait_phase(&full[u % t.slots], (uint32_t)((u / t.slots) & 1), a.status);
-      }
+      load_pages<D>(a, t, ctl, &tmK, &tmV, ring, lane);
     } else if (warp == 1) {
       // ---- MMAs ----
       if (elect_one()) {
@@ -941,7 +522,7 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
         // O^T of a tile of width N, set by set; `first` of its segment n
         auto second = [&](bool first, int n, int N) -> bool {
           if (first && n > 0 && !wait_phase(&o_free, (uint32_t)((n - 1) & 1), a.status)) return false;
-          if (!wait_phase(&full[rp.slot], rp.use, a.status)) return false;
+          if (!wait_phase(&ctl.full[rp.slot], rp.use, a.status)) return false;
           const uint32_t v = lo_v(ring + rp.slot * kSlotBytes, D == 128 ? kHalfBytes : 0);
           const int wide = set_cols<H>(N);
 #pragma unroll
@@ -958,23 +539,23 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
             umma_commit(&p_free[U & 3]);
             ++U;
           }
-          umma_commit(&empty[rp.slot]);
+          umma_commit(&ctl.empty[rp.slot]);
           rp.step(1, t.slots);
           return true;
         };
         for (int n = 0; ok; ++n) {
           const int k = n % kSegRing;
-          ok = wait_phase(&seg_full[k], (uint32_t)((n / kSegRing) & 1), a.status);
-          const int request = segs[k].request, cols = segs[k].cols, ntiles = segs[k].ntiles;
-          mbar_arrive(&seg_free[k]);
+          ok = wait_phase(&ctl.seg_full[k], (uint32_t)((n / kSegRing) & 1), a.status);
+          const int request = ctl.segs[k].request, cols = ctl.segs[k].cols, ntiles = ctl.segs[k].ntiles;
+          mbar_arrive(&ctl.seg_free[k]);
           if (!ok || request < 0) break;
           const int N = (cols + 15) / 16 * 16, qb = n % QB;
           const uint32_t idesc = umma_idesc_bf16(kTile, N);
-          ok = wait_phase(&q_full[qb], (uint32_t)((n / QB) & 1), a.status);
+          ok = wait_phase(&ctl.q_full[qb], (uint32_t)((n / QB) & 1), a.status);
           const uint32_t q = lo_kq(ring + t.q_off + qb * a.ct * D * 2), q_half = (uint32_t)(a.ct * 128) >> 4;
           for (int x = 0; x < ntiles && ok; ++x, ++T) {
             const int b = T % SB;
-            ok = !aborted && wait_phase(&full[rp.slot], rp.use, a.status);
+            ok = !ctl.aborted && wait_phase(&ctl.full[rp.slot], rp.use, a.status);
             if (ok && T >= SB) ok = wait_phase(&s_free[b], (uint32_t)((T / SB - 1) & 1), a.status);
             if (!ok) break;
             tc_fence_after();
@@ -984,9 +565,9 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
               umma_bf16(tD, desc(key + (((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4), kHiKQ),
                         desc(q + (kk >> 2) * q_half + (((kk & 3) * 32) >> 4), kHiKQ), idesc, kk > 0 ? 1u : 0u);
             umma_commit(&s_full[b]);
-            umma_commit(&empty[rp.slot]);
+            umma_commit(&ctl.empty[rp.slot]);
             rp.step(1, t.slots);
-            if (x == ntiles - 1) umma_commit(&q_free[qb]);
+            if (x == ntiles - 1) umma_commit(&ctl.q_free[qb]);
             if (T > 0) ok = second(prev_first, prev_n, prev_N);
             prev_first = x == 0;
             prev_n = n;
@@ -995,47 +576,16 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
         }
         rp.step(1, t.slots);  // the place of keys that do not come
         if (ok && T > 0) ok = second(prev_first, prev_n, prev_N);
-        if (!ok) aborted = 1;
+        if (!ok) ctl.aborted = 1;
         // everything issued has completed before the TMEM goes
-        umma_commit(&drained);
-        wait_phase(&drained, 0u, a.status);
+        umma_commit(&ctl.drained);
+        wait_phase(&ctl.drained, 0u, a.status);
       }
       __syncwarp();
     } else if (warp == 2) {
-      // ---- queries: [64-element halves][column][128 bytes], 128-byte swizzle ----
-      for (int n = 0;; ++n) {
-        Segment s;
-        if (!take(n, &s)) {
-          aborted = 1;
-          break;
-        }
-        if (s.request < 0 || __any_sync(0xFFFFFFFFu, aborted)) break;
-        const int b = n % QB;
-        if (n >= QB && !__all_sync(0xFFFFFFFFu, wait_phase(&q_free[b], (uint32_t)(((n / QB) - 1) & 1), a.status))) {
-          aborted = 1;
-          break;
-        }
-        if (n == 0) continue;  // the softmax warps, idle then, load the first
-        load_queries<D>(a, s, ring + t.q_off + b * a.ct * D * 2, lane, 32);
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&q_full[b]);
-      }
+      stage_queries<D, QB>(a, ctl, ring + t.q_off, a.ct, lane);
     } else if (warp == 3) {
-      // ---- the CTA's segments ----
-      if (lane == 0) {
-        Walk<kTile> walk(a, share);
-        for (int n = 0; !aborted; ++n) {
-          const int k = n % kSegRing;
-          if (n >= kSegRing && !wait_phase(&seg_free[k], (uint32_t)(((n / kSegRing) - 1) & 1), a.status)) {
-            aborted = 1;
-            break;
-          }
-          const bool more = walk.next(&segs[k]);
-          if (!more) segs[k].request = -1;
-          mbar_arrive(&seg_full[k]);
-          if (!more) break;
-        }
-      }
+      if (lane == 0) list_segments(a, share, ctl);
       __syncwarp();
     }
   }
@@ -1050,25 +600,6 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
-// One layer of K or V as [page][token][head][d], in boxes of `chunk` tokens
-// of 64 elements of one head.
-bool make_cache_map(CUtensorMap* map, const char* base, const AttendLaunch& a, int chunk) {
-  auto enc = tensor_map_encoder();
-  if (!enc) return false;
-  cuuint64_t dims[4] = {(cuuint64_t)a.D, (cuuint64_t)a.Hkv, (cuuint64_t)a.page_size, (cuuint64_t)a.pages};
-  // the stride of an extent of one is never used: any valid one
-  const cuuint64_t any = (cuuint64_t)a.D * 2;
-  cuuint64_t strides[3] = {a.Hkv > 1 ? (cuuint64_t)a.head_b : any, a.page_size > 1 ? (cuuint64_t)a.token_b : any,
-                           a.pages > 1 ? (cuuint64_t)a.page_b : any};
-  cuuint32_t box[4] = {64u, 1u, (cuuint32_t)chunk, 1u};
-  cuuint32_t estr[4] = {1u, 1u, 1u, 1u};
-  return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<char*>(base), dims, strides, box, estr,
-             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-             // a head's row is 2 D bytes: fetching more would bring in another head's
-             a.D == 64 ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B : CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 template <int D, int CG, int H>
 cudaError_t launch_variant(const AttendLaunch& a, cudaStream_t stream) {
   TcPlan t{};
@@ -1116,11 +647,13 @@ int attend_tc_grain(int page_size) { return std::min(page_size & -page_size, kTi
 int attend_tc_ctas_per_sm(int D, int ct) { return two_per_sm(D, ct <= 16 ? 2 : 4) ? 2 : 1; }
 
 int attend_tc_columns(int cols) {
-  const int n = (cols + kTcMaxCols - 1) / kTcMaxCols;  // column tiles, of equal width
-  return ((cols + n - 1) / n + 15) / 16 * 16;
+  if (cols <= kTcMaxCols) return (cols + 15) / 16 * 16;
+  const int n = (cols + kRowsMaxCols - 1) / kRowsMaxCols;  // column tiles, of equal width
+  return std::max(kTcMaxCols + 16, ((cols + n - 1) / n + 15) / 16 * 16);
 }
 
 cudaError_t launch_attend_tc(const AttendLaunch& a, cudaStream_t stream) {
+  if (a.ct > kTcMaxCols) return launch_attend_rows(a, stream);
   if (a.ct <= 16) return a.D == 64 ? launch_variant<64, 2, 1>(a, stream) : launch_variant<128, 2, 1>(a, stream);
   if (a.ct <= 32) return a.D == 64 ? launch_variant<64, 4, 1>(a, stream) : launch_variant<128, 4, 1>(a, stream);
   if (a.ct <= 96) return a.D == 64 ? launch_variant<64, 6, 2>(a, stream) : launch_variant<128, 6, 2>(a, stream);
