@@ -66,7 +66,7 @@ __global__ void __launch_bounds__(kGenThreads, C <= 2 ? 2 : 1) attend_general_ke
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ Share share;
   __shared__ Segment seg;
-  __shared__ long long sums[32];
+  __shared__ ShareSums sums;
   __shared__ float sh_alpha[kGenCols], sh_l[kGenCols], sh_m[kGenCols];
   __shared__ int sh_tok[2][kGenTile];  // position of a loaded token, -1: none or without a page
   __shared__ int more, last;
@@ -78,7 +78,7 @@ __global__ void __launch_bounds__(kGenThreads, C <= 2 ? 2 : 1) attend_general_ke
   float* sS = sQ + kGenCols * a.D;  // [col][token]
 
   pdl_wait_prerequisites();
-  find_share<kGenTile>(a, &share, sums);
+  find_share<kGenTile>(a, &share, &sums);
   Walk<kGenTile> walk(a, share);
   const int vecs = a.D * (int)sizeof(T) / 16;
   const int dv = a.D / 4;
@@ -406,6 +406,14 @@ extern "C" int spec_attend(const void* q, int64_t q_row_stride, int q_heads, con
     a.lists = a.Hkv;
     a.ctas -= a.ctas % a.Hkv;
   }
+  // What dividing an item costs, in tiles of its kernel (a tile takes 1 to 2 us): a
+  // part's writing and its share of the join grow with the columns.  Measured with
+  // these rules / without them, us: a token of 8 heads over 1, 16,384 positions, D =
+  // 128: 22 / 37; 17 rows of it, 8,192: 45 / 110; 32 rows, 16,384: 60 / 265; 8
+  // requests of 17 rows, 64 heads over 8, 1,024: 31 / 46; 4 of 256 rows, 32 over 8,
+  // 4,096: 94 / 100; in fp32, 4 of 8 rows, 8 over 2, D = 64, 3,000: 31 / 35.
+  a.whole_tiles = tc ? 7 : 3;
+  a.part_tiles = (tc ? 200.0f : 400.0f) / (float)(tc ? a.ct : std::min(a.ct, (K + 1) * a.G));
   const cudaError_t err = tc                              ? launch_attend_tc(a, stream)
                           : cache->dtype == SPEC_F32      ? launch_general<float>(a, stream)
                                                           : launch_general<__nv_bfloat16>(a, stream);

@@ -9,6 +9,11 @@
 // and its last), so a fixed workspace of two partial results per CTA serves
 // any batch, a single long request fills the GPU, and ragged batches balance.
 // The last CTA to finish a part of an item adds the parts up, in CTA order.
+// Two things bound how far items are divided, as a division costs the writing
+// and the joining of parts: where there are no more items than CTAs, and the
+// longest is little longer than an equal share, each CTA takes one item; and
+// no more CTAs take part than make an item's share and its join together
+// shortest.
 //
 // Lists.  Every key-value head has the same tiles, and the heads of a position
 // lie side by side in the usual cache.  So where the CTAs divide evenly enough
@@ -46,6 +51,8 @@ struct AttendLaunch {
   uint32_t* arrived;  // [ctas], zero between calls
   int ctas;
   int lists;          // 1, or one per key-value head
+  int whole_tiles;    // tiles that dividing an item costs
+  float part_tiles;   // tiles in the time that the join of one more part takes
 };
 
 // The row of a column: column / G, exact for the fewer than 2^15 columns of a
@@ -99,14 +106,22 @@ __device__ __forceinline__ AttendRows attend_rows(const AttendLaunch& a, int i) 
 }
 
 // Tiles of one key-value head of a request, over its column tiles.
+struct HeadUnits {
+  int all, items, longest;  // tiles, column tiles, tiles of the longest
+};
 template <int TT>
-__device__ __forceinline__ int head_units(const AttendLaunch& a, const AttendRows& r) {
-  const int cols = r.count * a.G;
-  if (cols <= a.ct) return cols == 0 ? 0 : item_tiles<TT>(a, r.p, r.p + r.count - 1).count;
-  int n = 0;
-  for (int c0 = 0; c0 < cols; c0 += a.ct) {
-    const int c1 = min(cols, c0 + a.ct) - 1;
-    n += item_tiles<TT>(a, r.p + group_row(a, c0), r.p + group_row(a, c1)).count;
+__device__ __forceinline__ int item_units(const AttendLaunch& a, const AttendRows& r, int c0) {
+  const int c1 = min(r.count * a.G, c0 + a.ct) - 1;
+  return item_tiles<TT>(a, r.p + group_row(a, c0), r.p + group_row(a, c1)).count;
+}
+template <int TT>
+__device__ __forceinline__ HeadUnits head_units(const AttendLaunch& a, const AttendRows& r) {
+  HeadUnits n{0, 0, 0};
+  for (int c0 = 0; c0 < r.count * a.G; c0 += a.ct) {
+    const int tiles = item_units<TT>(a, r, c0);
+    n.all += tiles;
+    n.longest = max(n.longest, tiles);
+    ++n.items;
   }
   return n;
 }
@@ -127,9 +142,15 @@ __device__ __forceinline__ long long scale_floor(long long x, long long y, int z
   return p < (1LL << 31) ? (long long)((uint32_t)p / (uint32_t)z) : p / z;
 }
 
+// Per warp, of its threads' requests.
+struct ShareSums {
+  long long units[32];
+  int items[32], longest[32];
+};
+
 // All threads of the CTA (a multiple of 32, at most 1024).
 template <int TT>
-__device__ void find_share(const AttendLaunch& a, Share* sh, long long* sums) {
+__device__ void find_share(const AttendLaunch& a, Share* sh, ShareSums* sums) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
   const int B = a.rows.B, step = blockDim.x;
   const int heads = a.lists > 1 ? 1 : a.Hkv;  // of a list
@@ -141,36 +162,86 @@ __device__ void find_share(const AttendLaunch& a, Share* sh, long long* sums) {
     for (int i0 = 0; i0 < B; i0 += step) {
       const int i = i0 + threadIdx.x;
       AttendRows r{0, 0, 0, false};
-      int per = 0;
+      HeadUnits per{0, 0, 0};
       if (i < B) {
         r = attend_rows(a, i);
         per = head_units<TT>(a, r);
         if (r.bad && pass == 0 && blockIdx.x == 0) report(a.status, SPEC_ERR_BAD_INPUT);
       }
-      const long long mine = (long long)per * heads;
+      const long long mine = (long long)per.all * heads;
+      // items are counted up to 4096 per request: exact where they are few
+      const int my_items = min(per.items * heads, 4096);
       long long incl = mine;
+      int incl_items = my_items;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const long long y = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-        if (lane >= o) incl += y;
+        const int z = __shfl_up_sync(0xFFFFFFFFu, incl_items, o);
+        if (lane >= o) {
+          incl += y;
+          incl_items += z;
+        }
       }
-      if (lane == 31) sums[warp] = incl;
+      const int longest_here = (int)__reduce_max_sync(0xFFFFFFFFu, (unsigned)per.longest);
+      if (lane == 31) {
+        sums->units[warp] = incl;
+        sums->items[warp] = incl_items;
+        sums->longest[warp] = longest_here;
+      }
       __syncthreads();
       long long before = carry, total = carry;
+      int items_before = 0, items = 0, longest = 0;
       for (int w = 0; w < warps; ++w) {
-        const long long x = sums[w];
-        if (w < warp) before += x;
-        total += x;
+        if (w < warp) {
+          before += sums->units[w];
+          items_before += sums->items[w];
+        }
+        total += sums->units[w];
+        items += sums->items[w];
+        longest = max(longest, sums->longest[w]);
       }
       incl += before;
+      incl_items += items_before;
       carry = total;
       if (passes == 2) __syncthreads();  // the sums may be written again
       if (pass < passes - 1) continue;
       if (passes == 2) total = sh->units;
       // this CTA's range: every thread that may hold its start works it out
-      const int most = a.ctas / a.lists;
-      const int ctas = (int)(total < most ? total : most), c = (int)blockIdx.x / a.lists;
+      const int most = a.ctas / a.lists, c = (int)blockIdx.x / a.lists;
+      int ctas = (int)(total < most ? total : most);
       long long u0 = 0, u1 = 0;
+      if (passes == 1 && items > 0 && items <= most) {
+        if ((longest - a.whole_tiles) * (long long)ctas <= total) {
+          ctas = items;  // an item each
+          const int k = c - (incl_items - my_items);  // the item's place in this thread's request
+          if (k >= 0 && k < my_items) {
+            const int h = k / per.items;
+            u0 = incl - mine + (long long)h * per.all;
+            int c0 = 0;
+            for (int x = h * per.items; x < k; ++x, c0 += a.ct) u0 += item_units<TT>(a, r, c0);
+            sh->u0 = u0;
+            sh->u1 = u0 + item_units<TT>(a, r, c0);
+            sh->request = i;
+            sh->base = incl - mine;
+            sh->per = per.all;
+            sh->rows = r;
+          }
+          if (threadIdx.x == 0) {
+            sh->units = total;
+            sh->ctas = ctas;
+            sh->cta = c;
+            if (c >= items) sh->u0 = sh->u1 = 0;
+          }
+          break;
+        }
+        // an item of W tiles in p parts takes W / p tiles and a join of p parts, so p
+        // is at best the root of W part_tiles; then no more CTAs than the longest
+        // share leaves work for
+        const int few = (int)ceilf(sqrtf((float)total * (float)items * a.part_tiles));
+        ctas = max(1, min(ctas, few));
+        const int share = (int)((total + ctas - 1) / ctas);
+        ctas = (int)((total + share - 1) / share);
+      }
       if (c < ctas) {
         u0 = scale_floor(c, total, ctas);
         u1 = scale_floor(c + 1, total, ctas);
@@ -178,7 +249,7 @@ __device__ void find_share(const AttendLaunch& a, Share* sh, long long* sums) {
       if (mine > 0 && incl - mine <= u0 && u0 < incl) {
         sh->request = i;
         sh->base = incl - mine;
-        sh->per = per;
+        sh->per = per.all;
         sh->rows = r;
       }
       if (threadIdx.x == 0) {

@@ -143,7 +143,7 @@ __global__ void __launch_bounds__((4 + 4 * kSets) * 32, 1)
   __shared__ Control ctl;
   __shared__ uint64_t s_full[kSets], p_full[kSets], o_full[kSets], o_free[kSets];
   __shared__ Share share;
-  __shared__ long long sums[32];
+  __shared__ ShareSums sums;
   __shared__ uint32_t tmem_sh;
   __shared__ int poison, last_sh;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -170,7 +170,7 @@ __global__ void __launch_bounds__((4 + 4 * kSets) * 32, 1)
   }
   pdl_wait_prerequisites();
   tc_fence_before();
-  find_share<kTile>(a, &share, sums);  // ends with a barrier
+  find_share<kTile>(a, &share, &sums);  // ends with a barrier
   tc_fence_after();
   const uint32_t tmem = tmem_sh, tO = tmem + kSets * kTile;
   const uint32_t ring = smem_u32(smem);

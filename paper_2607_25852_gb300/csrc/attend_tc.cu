@@ -176,7 +176,7 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
   __shared__ Control ctl;
   __shared__ uint64_t s_full[2], s_free[2], p_full[2], p_free[4], o_free;
   __shared__ Share share;
-  __shared__ long long sums[32];
+  __shared__ ShareSums sums;
   // per set and column: the reference's negative (-inf: no column), a factor, maxima and sums per warp
   __shared__ __align__(16) float sN[kCols], sF[kCols], red[4][kCols];
   __shared__ __align__(16) int sRow[kCols];        // position of the column's row
@@ -209,7 +209,7 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
   }
   pdl_wait_prerequisites();
   tc_fence_before();
-  find_share<kTile>(a, &share, sums);  // ends with a barrier
+  find_share<kTile>(a, &share, &sums);  // ends with a barrier
   tc_fence_after();
   const uint32_t tmem = tmem_sh;
   const uint32_t tO = tmem + kOut;
