@@ -90,23 +90,6 @@ __global__ void __launch_bounds__(kGenThreads, C <= 2 ? 2 : 1) attend_general_ke
     __syncthreads();
     if (!more) break;
     const Segment s = seg;
-    // ---- Q, in fp32; unused columns zero ----
-    for (int x = tid; x < kGenCols * dv; x += kGenThreads) {
-      const int c = x / dv, d = (x - c * dv) * 4;
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (c < s.cols) {
-        const int col = s.col0 + c, j = group_row(a, col);
-        const T* src = static_cast<const T*>(a.q) + (int64_t)(s.row0 + j) * a.q_row +
-                       (int64_t)(s.head * a.G + col - j * a.G) * a.D + d;
-        if (sizeof(T) == 4) {
-          v = __ldg(reinterpret_cast<const float4*>(src));
-        } else {
-          const uint2 w = __ldg(reinterpret_cast<const uint2*>(src));
-          v = make_float4(bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y));
-        }
-      }
-      *reinterpret_cast<float4*>(sQ + c * a.D + d) = v;
-    }
     const int p_first = s.p + group_row(a, s.col0), p_last = s.p + group_row(a, s.col0 + s.cols - 1);
     // four threads per token
     auto load_tile = [&](int x, int stage) {
@@ -133,6 +116,25 @@ __global__ void __launch_bounds__(kGenThreads, C <= 2 ? 2 : 1) attend_general_ke
       }
       cp_async_commit();
     };
+    load_tile(s.tile0, 0);
+    if (tid == 0) walk.advance();
+    // ---- Q, in fp32; unused columns zero ----
+    for (int x = tid; x < kGenCols * dv; x += kGenThreads) {
+      const int c = x / dv, d = (x - c * dv) * 4;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (c < s.cols) {
+        const int col = s.col0 + c, j = group_row(a, col);
+        const T* src = static_cast<const T*>(a.q) + (int64_t)(s.row0 + j) * a.q_row +
+                       (int64_t)(s.head * a.G + col - j * a.G) * a.D + d;
+        if (sizeof(T) == 4) {
+          v = __ldg(reinterpret_cast<const float4*>(src));
+        } else {
+          const uint2 w = __ldg(reinterpret_cast<const uint2*>(src));
+          v = make_float4(bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y));
+        }
+      }
+      *reinterpret_cast<float4*>(sQ + c * a.D + d) = v;
+    }
     // columns 4 warp .. 4 warp + 3: the maximum (all lanes alike), a lane's part of the sum
     float m[4], l[4], acc[C][4];
 #pragma unroll
@@ -144,7 +146,6 @@ __global__ void __launch_bounds__(kGenThreads, C <= 2 ? 2 : 1) attend_general_ke
     for (int k = 0; k < C; ++k)
 #pragma unroll
       for (int d = 0; d < 4; ++d) acc[k][d] = 0.0f;
-    load_tile(s.tile0, 0);
     for (int x = 0; x < s.ntiles; ++x) {
       const int stage = stages == 2 ? x & 1 : 0;
       if (stages == 2 && x + 1 < s.ntiles) {
@@ -406,13 +407,14 @@ extern "C" int spec_attend(const void* q, int64_t q_row_stride, int q_heads, con
     a.lists = a.Hkv;
     a.ctas -= a.ctas % a.Hkv;
   }
-  // What dividing an item costs, in tiles of its kernel (a tile takes 1 to 2 us): a
+  // What dividing the items costs, in tiles of the kernel (a tile takes 1 to 2 us): a
   // part's writing and its share of the join grow with the columns.  Measured with
   // these rules / without them, us: a token of 8 heads over 1, 16,384 positions, D =
-  // 128: 22 / 37; 17 rows of it, 8,192: 45 / 110; 32 rows, 16,384: 60 / 265; 8
-  // requests of 17 rows, 64 heads over 8, 1,024: 31 / 46; 4 of 256 rows, 32 over 8,
+  // 128: 22 / 37; 17 rows of it, 8,192: 45 / 111; 32 rows, 16,384: 60 / 265; 8
+  // requests of 17 rows, 64 heads over 8, 1,024: 31 / 47; 4 of 256 rows, 32 over 8,
   // 4,096: 94 / 100; in fp32, 4 of 8 rows, 8 over 2, D = 64, 3,000: 31 / 35.
-  a.whole_tiles = tc ? 7 : 3;
+  a.part_cost = tc ? 4 : 2;
+  a.item_cost = tc ? 4 : 1;
   a.part_tiles = (tc ? 200.0f : 400.0f) / (float)(tc ? a.ct : std::min(a.ct, (K + 1) * a.G));
   const cudaError_t err = tc                              ? launch_attend_tc(a, stream)
                           : cache->dtype == SPEC_F32      ? launch_general<float>(a, stream)

@@ -51,7 +51,7 @@ struct AttendLaunch {
   uint32_t* arrived;  // [ctas], zero between calls
   int ctas;
   int lists;          // 1, or one per key-value head
-  int whole_tiles;    // tiles that dividing an item costs
+  int part_cost, item_cost;  // tiles that dividing the items costs each CTA, and besides all CTAs per item
   float part_tiles;   // tiles in the time that the join of one more part takes
 };
 
@@ -211,7 +211,7 @@ __device__ void find_share(const AttendLaunch& a, Share* sh, ShareSums* sums) {
       int ctas = (int)(total < most ? total : most);
       long long u0 = 0, u1 = 0;
       if (passes == 1 && items > 0 && items <= most) {
-        if ((longest - a.whole_tiles) * (long long)ctas <= total) {
+        if ((longest - a.part_cost) * (long long)ctas <= total + (long long)a.item_cost * items) {
           ctas = items;  // an item each
           const int k = c - (incl_items - my_items);  // the item's place in this thread's request
           if (k >= 0 && k < my_items) {
@@ -345,8 +345,14 @@ struct Walk {
       s->slot = 2 * (int)blockIdx.x + (sh.cta == f ? 1 : 0);
     }
     u += s->ntiles;
-    if (u < sh.u1) {  // the next item
-      item = end;
+    return true;
+  }
+
+  // On to the next item, past a segment that `next` gave: apart from it, so that
+  // the segment can be passed on before the next request's lengths are read.
+  __device__ void advance() {
+    if (u < sh.u1) {
+      item += t.count;
       c0 += a.ct;
       if (c0 >= r.count * a.G) {
         c0 = 0;
@@ -359,7 +365,6 @@ struct Walk {
       }
       set_tiles();
     }
-    return true;
   }
 };
 

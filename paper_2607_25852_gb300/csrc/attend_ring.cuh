@@ -334,10 +334,10 @@ __device__ __noinline__ void join_tc(const AttendLaunch& a, const Segment& s, co
 // What the warps of a CTA share beside the ring itself.
 struct Control {
   uint64_t full[kMaxSlots], empty[kMaxSlots], q_full[2], q_free[2], seg_full[kSegRing], seg_free[kSegRing], drained;
-  Segment segs[kSegRing];
+  volatile int aborted;
   int tile_bad[kBadRing];  // per tile: the boxes whose page is not one
   int2 page[2][16];        // a tile's boxes: page, first position in it
-  volatile int aborted;
+  Segment segs[kSegRing];
 };
 // One thread; `readers` warps read a segment.
 __device__ __forceinline__ void init_control(Control& ctl, int slots, int readers) {
@@ -489,6 +489,7 @@ __device__ __forceinline__ void list_segments(const AttendLaunch& a, const Share
     if (!more) ctl.segs[k].request = -1;
     mbar_arrive(&ctl.seg_full[k]);
     if (!more) break;
+    walk.advance();
   }
 }
 
