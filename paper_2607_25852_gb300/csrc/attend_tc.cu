@@ -1,5 +1,6 @@
 // attend_tc.cu -- spec_attend on the 5th-generation tensor cores: bf16 caches
-// of head dimension 64 or 128 whose pages are a multiple of 8 positions.
+// of head dimension 64 or 128 whose pages are a multiple of 8 positions, for up
+// to 144 (row, query head) columns per key-value head (attend_rows.cu: more).
 //
 // The few columns (row, query head) that share a key-value head are the N
 // dimension of both products, so their cost follows their number, and the
@@ -25,7 +26,7 @@
 //
 // Warps: 0 loads pages by TMA into a ring of K and V tiles; 1 issues the MMAs
 // (the scores of tile t + 1 before the second product of tile t); 2 loads
-// queries; 3 walks the CTA's share of the work; the rest are the softmax, one
+// queries; 3 lists the CTA's share of the work; the rest are the softmax, one
 // TMEM lane quarter per warp, in one set or in two that halve the columns and
 // take turns at two buffers of the weights.
 //
@@ -38,6 +39,15 @@
 // Every mbarrier wait is bounded (about a second): a wait that gives up sets
 // SPEC_ERR_TIMEOUT and the kernel ends; the softmax warps, which meet at
 // barriers, leave together by a vote.
+//
+// What it measures, 64 requests of 64 query heads over 8, D = 128, 4,096
+// positions each: 1 row 166 us (6.5 TB/s, 0.95 of the measured copy peak), 4 rows
+// 170, 8 rows 181, 12 rows 192 (5.6 TB/s), 17 rows 250 us (4.3 TB/s).  Up to 12
+// rows HBM bounds it; at 17 the chain from scores to weights to output: a tile
+// takes 2.1 us where its bytes take 1.5, shared memory is 76 % busy (the MMAs'
+// operands 33, the softmax 31, arriving tiles 12) and two softmax warps per
+// scheduler issue 38 % of the time.  Short runs are bound by what comes before
+// the first tile (8 us) and after the last (4 to 10 with a join).
 #include "attend_ring.cuh"
 
 namespace spec {
@@ -48,7 +58,8 @@ namespace {
 // scores to weights to output is longer than the time its tile takes to arrive,
 // and the ends of its items leave the loads idle.  (With D = 128 the tiles are
 // twice as large: one CTA's chain keeps up, and two would not have three tiles'
-// room each.)
+// room each.)  Two / one, us: a token of 128 requests, 64 heads over 8, window of
+// 1,024: 70 / 89; of 64 requests over 4,096 positions: 94 / 122.
 constexpr bool two_per_sm(int D, int CG) { return D == 64 && CG == 2; }
 __device__ __forceinline__ void tmem_ld8(uint32_t addr, float* v) {
   uint32_t r[8];
@@ -652,6 +663,12 @@ int attend_tc_columns(int cols) {
   return std::max(kTcMaxCols + 16, ((cols + n - 1) / n + 15) / 16 * 16);
 }
 
+// The narrowest variant that holds an item: wider ones spend their softmax on
+// columns that are not there.  64 requests of 64 heads over 8, 4,096 positions, us
+// in the variants of 16 / 32 / 96 / 144 columns: a token, D = 128: 166 / 165 / 168 /
+// 213; D = 64: 94 / 122 / 151 / 194; 8 rows, D = 128: - / - / 181 / 224.  17 rows (136
+// columns): 250 here, 328 in the kernel for many rows, whose second set holds 8
+// columns; 21 rows: 362 here as two items of 84, 323 there.
 cudaError_t launch_attend_tc(const AttendLaunch& a, cudaStream_t stream) {
   if (a.ct > kTcMaxCols) return launch_attend_rows(a, stream);
   if (a.ct <= 16) return a.D == 64 ? launch_variant<64, 2, 1>(a, stream) : launch_variant<128, 2, 1>(a, stream);
