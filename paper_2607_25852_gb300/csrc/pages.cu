@@ -41,7 +41,7 @@ constexpr int kAppendWarps = 4;
 
 // One warp per (request, row j): the row's vectors of K and V are loaded while
 // the row's page is looked up, so that the two round trips overlap.  Bound by
-// those round trips (600 rows of 8 heads of 128 in bf16: 2.6 us) and, for large
+// those round trips (578 rows of 8 heads of 128 in bf16, 4.7 MB: 2.6 us) and, for large
 // calls, by HBM (1,536 rows of 12 heads of 96 in fp32, 28 MB: 4.7 us, 6.0 TB/s).
 __global__ void __launch_bounds__(32 * kAppendWarps) append_kernel(const AppendLaunch p) {
   const int lane = threadIdx.x & 31;
