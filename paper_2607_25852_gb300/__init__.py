@@ -357,16 +357,16 @@ def _stream_handle(stream):
 
 
 def _cache(k, v):
-    """struct spec_cache of K and V tensors [layers, pages, page_size, kv_heads, head_dim] (or without the first
-    dimension), any strides but a contiguous last dimension."""
+    """struct spec_cache (its bytes) of K and V tensors [layers, pages, page_size, kv_heads, head_dim] (or without the
+    first dimension), any strides but a contiguous last dimension."""
     shape, stride, dtype = k.shape, k.stride(), k.dtype
     if shape != v.shape or stride != v.stride() or dtype != v.dtype or len(shape) not in (4, 5):
         raise ValueError("k_cache and v_cache: 4 or 5 dimensions, the same shape, strides and dtype")
     if stride[-1] != 1:
         raise ValueError("the head dimension of a cache must be contiguous")
     if len(shape) == 4:
-        return _native.Cache(k.data_ptr(), v.data_ptr(), _dtype(k), 1, *shape, 0, *stride[:3])
-    return _native.Cache(k.data_ptr(), v.data_ptr(), _dtype(k), *shape, *stride[:4])
+        return _native.pack_cache(k.data_ptr(), v.data_ptr(), _dtype(k), 1, *shape, 0, *stride[:3])
+    return _native.pack_cache(k.data_ptr(), v.data_ptr(), _dtype(k), *shape, *stride[:4])
 
 
 def _rows(t, heads, head_dim, dtype, what):
@@ -416,7 +416,7 @@ def spec_attend(q, k_cache, v_cache, page_table, pos_base, B, K, out, ws, row_of
     layer, 4 dimensions); page_table int32 [B, max_pages]; scale 1 / sqrt(head_dim) if None; see spec.h."""
     cache = _cache(k_cache, v_cache)
     shape = q.shape
-    Hq, D = shape[1], cache.head_dim
+    Hq, D = shape[1], k_cache.shape[-1]
     q_ptr, q_row = _rows(q, Hq, D, k_cache.dtype, "q")
     # with row_offsets the number of packed rows is on the device
     if out.shape != shape or out.dtype != q.dtype or not out.is_contiguous() or (
@@ -429,7 +429,7 @@ def spec_attend(q, k_cache, v_cache, page_table, pos_base, B, K, out, ws, row_of
         lse = lse_out.data_ptr()
     table, max_pages = _table(page_table, B)
     code = library().spec_attend(
-        q_ptr, q_row, Hq, ctypes.byref(cache), layer, _ints(row_offsets, B + 1, "row_offsets"),
+        q_ptr, q_row, Hq, cache, layer, _ints(row_offsets, B + 1, "row_offsets"),
         _ints(depth, B, "depth"), _ints(pos_base, B, "pos_base", torch.int64), table, max_pages, B, K,
         D ** -0.5 if scale is None else scale, window, sinks, out.data_ptr(), lse, _ints(status, 1, "status"),
         ws.data_ptr(), ws.nbytes, _stream_handle(stream))
@@ -441,14 +441,14 @@ def spec_cache_append(k_new, v_new, k_cache, v_cache, page_table, pos_base, B, K
                       layer=0, status=None, stream=None):
     """k_new and v_new [R, kv_heads, head_dim], written to their pages; see spec.h."""
     cache = _cache(k_cache, v_cache)
-    H, D, dtype = cache.kv_heads, cache.head_dim, k_cache.dtype
+    (H, D), dtype = k_cache.shape[-2:], k_cache.dtype
     k_ptr, k_row = _rows(k_new, H, D, dtype, "k_new")
     v_ptr, v_row = _rows(v_new, H, D, dtype, "v_new")
     if row_offsets is None and min(k_new.shape[0], v_new.shape[0]) < B * (K + 1):
         raise ValueError("k_new, v_new: rows for every request")
     table, max_pages = _table(page_table, B)
     code = library().spec_cache_append(
-        ctypes.byref(cache), layer, k_ptr, k_row, v_ptr, v_row, _ints(row_offsets, B + 1, "row_offsets"),
+        cache, layer, k_ptr, k_row, v_ptr, v_row, _ints(row_offsets, B + 1, "row_offsets"),
         _ints(depth, B, "depth"), _ints(pos_base, B, "pos_base", torch.int64), table, max_pages, B, K,
         _ints(status, 1, "status"), _stream_handle(stream))
     if code:
@@ -500,7 +500,7 @@ def spec_cache_copy(k_cache, v_cache, src, dst, count, status=None, stream=None)
     """Pages src[x] to dst[x] for x < count[0] (a device tensor), every layer of both caches."""
     cache = _cache(k_cache, v_cache)
     n = min(src.numel(), dst.numel())
-    code = library().spec_cache_copy(ctypes.byref(cache), _ints(src, n, "src"), _ints(dst, n, "dst"),
+    code = library().spec_cache_copy(cache, _ints(src, n, "src"), _ints(dst, n, "dst"),
                                      _ints(count, 1, "count"), n, _ints(status, 1, "status"), _stream_handle(stream))
     if code:
         raise SpecError(code, "spec_cache_copy")

@@ -476,10 +476,22 @@ __device__ __forceinline__ void stage_queries(const AttendLaunch& a, Control& ct
   }
 }
 
-// A thread: the share's segments.
+// A thread: the share's first segment.
+__device__ __forceinline__ void list_first(const AttendLaunch& a, const Share& share, Control& ctl) {
+  Walk<kTile> walk(a, share);
+  if (!walk.next(&ctl.segs[0])) ctl.segs[0].request = -1;
+  mbar_arrive(&ctl.seg_full[0]);
+}
+// A thread: the share's segments, from the first (N0 = 0) or past it (N0 = 1).
+template <int N0>
 __device__ __forceinline__ void list_segments(const AttendLaunch& a, const Share& share, Control& ctl) {
   Walk<kTile> walk(a, share);
-  for (int n = 0; !ctl.aborted; ++n) {
+  if (N0 == 1) {
+    Segment first;
+    if (!walk.next(&first)) return;
+    walk.advance();
+  }
+  for (int n = N0; !ctl.aborted; ++n) {
     const int k = n % kSegRing;
     if (n >= kSegRing && !wait_phase(&ctl.seg_free[k], (uint32_t)(((n / kSegRing) - 1) & 1), a.status)) {
       ctl.aborted = 1;

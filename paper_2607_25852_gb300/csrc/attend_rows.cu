@@ -391,6 +391,11 @@ __global__ void __launch_bounds__((4 + 4 * kSets) * 32, 1)
       if (lane == 0) mbar_arrive(&ctl.seg_free[n % kSegRing]);
     }
   } else {
+    // The first segment goes out before the registers move, for which the softmax
+    // waits: 64 requests of 32 rows of 64 heads 338 -> 327 us (in the kernel for few
+    // columns the same cost 3 % at 17 rows).
+    if (warp == 3 && lane == 0) list_first(a, share, ctl);
+    __syncwarp();
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 0) {
       load_pages<D>(a, t, ctl, &tmK, &tmV, ring, lane);
@@ -471,7 +476,7 @@ __global__ void __launch_bounds__((4 + 4 * kSets) * 32, 1)
     } else if (warp == 2) {
       stage_queries<D, 1>(a, ctl, ring + t.q_off, kItemCols, lane);
     } else {
-      if (lane == 0) list_segments(a, share, ctl);
+      if (lane == 0) list_segments<1>(a, share, ctl);
       __syncwarp();
     }
   }

@@ -596,7 +596,7 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
     } else if (warp == 2) {
       stage_queries<D, QB>(a, ctl, ring + t.q_off, a.ct, lane);
     } else if (warp == 3) {
-      if (lane == 0) list_segments(a, share, ctl);
+      if (lane == 0) list_segments<0>(a, share, ctl);
       __syncwarp();
     }
   }
