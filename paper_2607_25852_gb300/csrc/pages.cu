@@ -180,52 +180,22 @@ struct ForkLaunch {
 
 constexpr int kForkThreads = 256;
 constexpr int kForkPer = 4;  // entries per thread
+// The most entries (of tables and counts) and rows of a call that one cluster does.
+constexpr int kForkHere = 1 << 15, kForkRows = 256;
 
-// The new rows, a CTA per (row, segment); the last CTAs copy the counts when
-// they go to a new array, which has to be complete before fork_refs_kernel adds
-// to it: two launches.  Both together: 2.0 us (12 rows of 128 slots) and 2.4 us
-// (256 rows of 320); three round trips to L2 bound them.
-__global__ void __launch_bounds__(kForkThreads) fork_table_kernel(const ForkLaunch p, int segs) {
-  pdl_wait_prerequisites();
-  pdl_launch_dependents();  // only now: the next kernel reads this call's inputs before its own wait
-  const long long rows = (long long)p.B * segs;
-  if (blockIdx.x >= rows) {
-    const long long at = ((long long)blockIdx.x - rows) * kForkThreads * kForkPer + threadIdx.x;
-#pragma unroll
-    for (int k = 0; k < kForkPer; ++k) {
-      const long long e = at + k * kForkThreads;
-      if (e < p.pages) p.refs_out[e] = p.refs[e];
-    }
-    return;
-  }
-  const int i = (int)(blockIdx.x / segs), seg = (int)(blockIdx.x - (long long)i * segs);
-  const int par = __ldg(p.parent + i);
-  const bool has = par >= 0 && par < p.B_in;
-  if (!has && par != -1 && seg == 0 && threadIdx.x == 0) report(p.status, SPEC_ERR_BAD_INPUT);
-  int e[kForkPer];
-#pragma unroll
-  for (int k = 0; k < kForkPer; ++k) {
-    const int s = (seg * kForkPer + k) * kForkThreads + threadIdx.x;
-    e[k] = has && s < p.max_pages ? p.table[(size_t)par * p.max_pages + s] : -1;
-  }
-#pragma unroll
-  for (int k = 0; k < kForkPer; ++k) {
-    const int s = (seg * kForkPer + k) * kForkThreads + threadIdx.x;
-    if (s >= p.max_pages) continue;
-    if (e[k] < -1 || e[k] >= p.pages) {
-      report(p.status, SPEC_ERR_BAD_INPUT);
-      e[k] = -1;
-    }
-    p.table_out[(size_t)i * p.max_pages + s] = e[k];
-  }
-}
-
-// A CTA per (old row, segment): its entries' counts change by the row's
-// children less one, so a row that one child takes over touches no count.
-__global__ void __launch_bounds__(kForkThreads) fork_refs_kernel(const ForkLaunch p, int segs) {
-  const int r = (int)(blockIdx.x / segs), seg = (int)(blockIdx.x - (long long)r * segs);
+// Counts that stay in place need nothing of the new rows: one launch.  Counts that
+// go to a new array have to be copied there before they change: small calls do
+// both in one cluster (fork_cluster_kernel), large ones in two launches.  12 rows
+// of 128 slots: one cluster 5.9 us of the host and 3.5 of the GPU, two launches 7.4
+// and 2.0; 256 rows of 320 in two launches 7.4 and 2.4.  Round trips to L2 bound
+// the kernels.
+// A block per (old row, segment): its entries' counts change by the row's
+// children less one, so a row that one child takes over touches no count.  The
+// inputs are read before `wait`.
+template <typename Wait>
+__device__ __forceinline__ void fork_counts(const ForkLaunch& p, int segs, long long block, Wait wait) {
+  const int r = (int)(block / segs), seg = (int)(block - (long long)r * segs);
   int mine = 0;
-  // inputs: complete before this call's first kernel started
   for (int i = threadIdx.x; i < p.B; i += kForkThreads) mine += __ldg(p.parent + i) == r ? 1 : 0;
   __shared__ int children;
   if (threadIdx.x == 0) children = 0;
@@ -240,12 +210,63 @@ __global__ void __launch_bounds__(kForkThreads) fork_refs_kernel(const ForkLaunc
   }
   __syncthreads();
   const int change = children - 1;
-  pdl_wait_prerequisites();  // the counts' copy
-  pdl_launch_dependents();
+  wait();
   if (change == 0) return;
 #pragma unroll
   for (int k = 0; k < kForkPer; ++k)
     if (e[k] >= 0 && e[k] < p.pages) atomicAdd(p.refs_out + e[k], change);
+}
+
+// Row i's entry at slot s.
+__device__ __forceinline__ int fork_entry(const ForkLaunch& p, int par, int s) {
+  const int e = par >= 0 && par < p.B_in && s < p.max_pages ? __ldg(p.table + (size_t)par * p.max_pages + s) : -1;
+  if (e >= -1 && e < p.pages) return e;
+  report(p.status, SPEC_ERR_BAD_INPUT);
+  return -1;
+}
+
+// Blocks of kForkThreads threads: first the new rows, one per (row, segment of
+// its slots), then `extra` that copy the counts when they go to a new array, then,
+// where they stay in place, the counts' changes.
+__global__ void __launch_bounds__(kForkThreads) fork_kernel(const ForkLaunch p, int segs, int extra) {
+  pdl_wait_prerequisites();
+  pdl_launch_dependents();  // only now: the next kernel reads this call's inputs before its own wait
+  long long block = blockIdx.x;
+  if (block >= (long long)p.B * segs) {
+    block -= (long long)p.B * segs;
+    if (block >= extra) {
+      fork_counts(p, segs, block - extra, [] {});
+      return;
+    }
+    const long long at = block * kForkThreads * kForkPer + threadIdx.x;
+#pragma unroll
+    for (int k = 0; k < kForkPer; ++k) {
+      const long long e = at + k * kForkThreads;
+      if (e < p.pages) p.refs_out[e] = p.refs[e];
+    }
+    return;
+  }
+  const int i = (int)(block / segs), seg = (int)(block - (long long)i * segs);
+  const int par = __ldg(p.parent + i);
+  if (par < -1 || par >= p.B_in) {
+    if (seg == 0 && threadIdx.x == 0) report(p.status, SPEC_ERR_BAD_INPUT);
+  }
+  int e[kForkPer];
+#pragma unroll
+  for (int k = 0; k < kForkPer; ++k) e[k] = fork_entry(p, par, (seg * kForkPer + k) * kForkThreads + threadIdx.x);
+#pragma unroll
+  for (int k = 0; k < kForkPer; ++k) {
+    const int s = (seg * kForkPer + k) * kForkThreads + threadIdx.x;
+    if (s < p.max_pages) p.table_out[(size_t)i * p.max_pages + s] = e[k];
+  }
+}
+
+// The counts' changes, past the copy of a larger call.
+__global__ void __launch_bounds__(kForkThreads) fork_refs_kernel(const ForkLaunch p, int segs) {
+  fork_counts(p, segs, blockIdx.x, [] {
+    pdl_wait_prerequisites();  // the counts' copy
+    pdl_launch_dependents();
+  });
 }
 
 // ---------------------------------------------------------------------------
@@ -309,6 +330,35 @@ __device__ __forceinline__ void page_range(int pages, int* begin, int* end) {
   const int per = (pages + size - 1) / size;
   *begin = min(pages, rank * per);
   *end = min(pages, *begin + per);
+}
+
+// A small call with counts in a new array: one cluster.
+__global__ void __cluster_dims__(kPageCluster, 1, 1) __launch_bounds__(kPageThreads)
+    fork_cluster_kernel(const ForkLaunch p) {
+  cg::cluster_group cluster = cg::this_cluster();
+  pdl_wait_prerequisites();
+  pdl_launch_dependents();
+  const int threads = kPageThreads * (int)cluster.num_blocks();
+  const int at = (int)cluster.block_rank() * kPageThreads + (int)threadIdx.x;
+  for (int e = at; e < p.pages; e += threads) p.refs_out[e] = p.refs[e];
+  for (int x = at; x < p.B * p.max_pages; x += threads) {
+    const int i = x / p.max_pages, s = x - i * p.max_pages, par = __ldg(p.parent + i);
+    if (s == 0 && (par < -1 || par >= p.B_in)) report(p.status, SPEC_ERR_BAD_INPUT);
+    p.table_out[x] = fork_entry(p, par, s);
+  }
+  __threadfence();
+  cluster.sync();
+  const int lane = threadIdx.x & 31;
+  for (int r = at / 32; r < p.B_in; r += threads / 32) {  // a warp per old row
+    int mine = 0;
+    for (int i = lane; i < p.B; i += 32) mine += __ldg(p.parent + i) == r ? 1 : 0;
+    const int change = __reduce_add_sync(0xFFFFFFFFu, mine) - 1;
+    if (change == 0) continue;
+    for (int s = lane; s < p.max_pages; s += 32) {
+      const int e = __ldg(p.table + (size_t)r * p.max_pages + s);
+      if (e >= 0 && e < p.pages) atomicAdd(p.refs_out + e, change);
+    }
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -502,12 +552,26 @@ struct CompactLaunch {
   int32_t *src, *dst, *map, *counts;
   int cap;
   int32_t* status;
+  bool tables;  // the tables too, in compact_kernel
 };
 
+// The most entries of tables that compact_kernel rewrites: a launch less (1.7 us of
+// the host; 6 tables of 64 slots take the GPU 7.2 us so, 6.6 with the launch; 96 of
+// 384 slots 11.0 and 10.0).
+constexpr int kRemapHere = 1 << 14;
+
+// An entry through the map of moved pages.
+__device__ __forceinline__ void remap_entry(const CompactLaunch& p, long long x, int e) {
+  if (e == -1) return;
+  const int to = e >= 0 && e < p.pages ? __ldcg(p.map + e) : -1;
+  if (to < 0) report(p.status, SPEC_ERR_BAD_INPUT);
+  if (to != e) p.table[x] = to;
+}
+
 // One cluster of 8 CTAs: count the live pages (n), rank those at or past n and
-// the holes below n, pair them by rank, then move the counts; remap_kernel then
-// rewrites the tables.  Both together: 6.6 us (509 pages), 10 us (32,768 pages, 96
-// tables of 384 slots); barriers and round trips bound them.
+// the holes below n, pair them by rank, move the counts, then rewrite the tables
+// (large ones in remap_kernel).  7.2 us (509 pages), 10 us (32,768 pages, 96 tables
+// of 384 slots); barriers and round trips bound it.
 __global__ void __cluster_dims__(kPageCluster, 1, 1) __launch_bounds__(kPageThreads)
     compact_kernel(const CompactLaunch p) {
   __shared__ int sums[33], slot;
@@ -562,6 +626,17 @@ __global__ void __cluster_dims__(kPageCluster, 1, 1) __launch_bounds__(kPageThre
     p.counts[0] = moves;
     p.counts[1] = n;
   }
+  if (!p.tables) return;
+  __threadfence();
+  cluster.sync();
+  const int entries = p.B * p.max_pages;
+  for (int x0 = (int)cluster.block_rank() * kPageThreads + threadIdx.x; x0 < entries; x0 += kForkPer * threads) {
+    int e[kForkPer];
+#pragma unroll
+    for (int k = 0; k < kForkPer; ++k) e[k] = x0 + k * threads < entries ? p.table[x0 + k * threads] : -1;
+#pragma unroll
+    for (int k = 0; k < kForkPer; ++k) remap_entry(p, x0 + k * threads, e[k]);
+  }
 }
 
 // The tables' entries through the map of moved pages.
@@ -577,12 +652,7 @@ __global__ void __launch_bounds__(kForkThreads) remap_kernel(const CompactLaunch
   pdl_wait_prerequisites();  // the map
   pdl_launch_dependents();
 #pragma unroll
-  for (int k = 0; k < kForkPer; ++k) {
-    if (e[k] == -1) continue;
-    const int to = e[k] >= 0 && e[k] < p.pages ? __ldcg(p.map + e[k]) : -1;
-    if (to < 0) report(p.status, SPEC_ERR_BAD_INPUT);
-    if (to != e[k]) p.table[at + k * kForkThreads] = to;
-  }
+  for (int k = 0; k < kForkPer; ++k) remap_entry(p, at + k * kForkThreads, e[k]);
 }
 
 }  // namespace spec
@@ -693,10 +763,13 @@ extern "C" int spec_cache_fork(const int32_t* page_table, const int32_t* page_re
   ForkLaunch p{page_table, page_refs, parent, B_in, B, max_pages, pages, table_out, refs_out, status};
   const int per = kForkThreads * kForkPer;
   const int segs = (max_pages + per - 1) / per;
+  if (page_refs != refs_out && (long long)(B + B_in) * max_pages + pages <= kForkHere && B <= kForkRows)
+    return done(launch_after_previous(fork_cluster_kernel, dim3(kPageCluster), dim3(kPageThreads), 0, stream, p));
   const long long extra = page_refs == refs_out ? 0 : ((long long)pages + per - 1) / per;
-  cudaError_t err = launch_after_previous(fork_table_kernel, dim3((unsigned)((long long)B * segs + extra)),
-                                          dim3(kForkThreads), 0, stream, p, segs);
-  if (err == cudaSuccess)
+  const long long here = page_refs == refs_out ? (long long)B_in * segs : 0;
+  cudaError_t err = launch_after_previous(fork_kernel, dim3((unsigned)((long long)B * segs + extra + here)),
+                                          dim3(kForkThreads), 0, stream, p, segs, (int)extra);
+  if (err == cudaSuccess && here == 0)
     err = launch_after_previous(fork_refs_kernel, dim3((unsigned)((long long)B_in * segs)), dim3(kForkThreads), 0,
                                 stream, p, segs);
   return done(err);
@@ -761,9 +834,10 @@ extern "C" int spec_cache_compact(int32_t* page_table, int32_t* page_refs, int B
       !page_map_out || !counts_out)
     return SPEC_ERR_INVALID_ARG;
   CompactLaunch p{page_table,   page_refs,    B,          max_pages, pages, move_src_out,
-                  move_dst_out, page_map_out, counts_out, std::max(1, pages / 2), status};
+                  move_dst_out, page_map_out, counts_out, std::max(1, pages / 2), status,
+                  (long long)B * max_pages <= kRemapHere};
   cudaError_t err = launch_after_previous(compact_kernel, dim3(kPageCluster), dim3(kPageThreads), 0, stream, p);
-  if (err == cudaSuccess) {
+  if (err == cudaSuccess && !p.tables) {
     const long long per = kForkThreads * kForkPer, n = (long long)B * max_pages;
     err = launch_after_previous(remap_kernel, dim3((unsigned)((n + per - 1) / per)), dim3(kForkThreads), 0, stream, p);
   }
