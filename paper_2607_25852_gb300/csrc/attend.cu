@@ -57,14 +57,19 @@ static size_t general_smem(int D, int esize, int stages) {
 //
 // Scores: a token and eight columns per thread, from a K row of its own and Q
 // rows that the warp shares (12 shared-memory wavefronts for 32 products a
-// lane).  Weights: four columns per warp, the sums kept per lane.  Output: four
-// d of C columns per thread over all tokens.  The running time is that of
+// lane).  Weights: up to four columns per warp, the sums kept per lane.  Output:
+// four d of C columns per thread.  Threads that few columns leave over split the
+// sums: the scores' over d (the weights add their parts up), the output's over the
+// tile's tokens (added up, in order, at the item's end).  The running time is that of
 // shared memory and of the four barriers a tile, not of the cache's bytes; two
 // CTAs share an SM where two fit.  Measured in fp32: 8 requests of 5 rows, 16 heads
-// over 4, D = 64, 1,500 positions each 30 us (0.4 TB/s); 4 requests of 8 rows, 8
+// over 4, D = 64, 1,500 positions each 29 us (0.4 TB/s); 4 requests of 8 rows, 8
 // heads over 2, 3,000 positions 30 us; one of 256 rows of 8 heads over 1, D = 128,
-// 4,096 positions 217 us (19.8 TFLOP/s); 16 of one row, 16 heads over 8, 2,000
-// positions 131 us (1.0 TB/s: two columns of the 32).
+// 4,096 positions 218 us (19.7 TFLOP/s); 64 of one row, 32 heads over 8, 4,096
+// positions 668 us (3.2 TB/s; 1,013 without the split sums, at 4 columns of 32).
+// bf16, D = 96, 16 of one row, 16 heads over 4, 4,000 positions 74 us (without 108).
+// Bringing the tiles by a bulk copy per row instead of 16-byte copies of all
+// threads made it a quarter slower.
 template <typename T, int C>
 __global__ void __launch_bounds__(kGenThreads, C <= 2 ? 2 : 1) attend_general_kernel(const AttendLaunch a, int stages) {
   extern __shared__ __align__(16) uint8_t smem[];
@@ -86,14 +91,22 @@ __global__ void __launch_bounds__(kGenThreads, C <= 2 ? 2 : 1) attend_general_ke
   Walk<kGenTile> walk(a, share);
   const int vecs = a.D * (int)sizeof(T) / 16;
   const int dv = a.D / 4;
-  const int my_d = (tid % dv) * 4, my_c = (tid / dv) * C;
-  const bool pv_active = my_c < kGenCols && my_c + C <= (kGenThreads / dv) * C;
+  const int my_d = (tid % dv) * 4;
 
   for (;;) {
     if (tid == 0) more = walk.next(&seg) ? 1 : 0;
     __syncthreads();
     if (!more) break;
     const Segment s = seg;
+    // scores: quarters of columns, and how many ways d is split; output: groups of C
+    // columns, and how many ways the tokens are (a power of two)
+    const int quarters = (s.cols + kGenQuarter - 1) / kGenQuarter, d_ways = 4 / quarters;
+    const int part = tid / kGenTile / quarters, c0 = (tid / kGenTile - part * quarters) * kGenQuarter;
+    const int groups = (s.cols + C - 1) / C;
+    int t_ways = 1;
+    while (t_ways < kGenTile / 4 && 2 * t_ways * groups <= kGenThreads / dv) t_ways *= 2;
+    const int my_part = tid / dv / groups, my_c = (tid / dv - my_part * groups) * C;
+    const bool pv_active = my_part < t_ways;
     const int p_first = s.p + group_row(a, s.col0), p_last = s.p + group_row(a, s.col0 + s.cols - 1);
     // four threads per token
     auto load_tile = [&](int x, int stage) {
@@ -139,7 +152,7 @@ __global__ void __launch_bounds__(kGenThreads, C <= 2 ? 2 : 1) attend_general_ke
       }
       *reinterpret_cast<float4*>(sQ + c * a.D + d) = v;
     }
-    // columns 4 warp .. 4 warp + 3: the maximum (all lanes alike), a lane's part of the sum
+    // columns warp, warp + 8, ..: the maximum (all lanes alike), a lane's part of the sum
     float m[4], l[4], acc[C][4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -162,31 +175,35 @@ __global__ void __launch_bounds__(kGenThreads, C <= 2 ? 2 : 1) attend_general_ke
       // ---- scores ----
       bool masked = false;
       {
-        const int tok = tid & (kGenTile - 1), c0 = (tid / kGenTile) * kGenQuarter;
+        const int tok = tid & (kGenTile - 1);
         const int pos = sh_tok[stage][tok];
-        if (c0 < s.cols) {
+        if (part < d_ways) {
           const T* kr = reinterpret_cast<const T*>(sK + ((size_t)stage * kGenTile + tok) * pitch);
           float dot[kGenQuarter];
 #pragma unroll
           for (int c = 0; c < kGenQuarter; ++c) dot[c] = 0.0f;
+          auto add = [&](int first, int step) {
 #pragma unroll 2
-          for (int d = 0; d < a.D; d += 4) {
-            const float4 k4 = load4(kr + d);
+            for (int d = first; d < a.D; d += step) {
+              const float4 k4 = load4(kr + d);
 #pragma unroll
-            for (int c = 0; c < kGenQuarter; ++c) {
-              const float4 q4 = load4(sQ + (c0 + c) * a.D + d);
-              dot[c] = fmaf(k4.x, q4.x, dot[c]);
-              dot[c] = fmaf(k4.y, q4.y, dot[c]);
-              dot[c] = fmaf(k4.z, q4.z, dot[c]);
-              dot[c] = fmaf(k4.w, q4.w, dot[c]);
+              for (int c = 0; c < kGenQuarter; ++c) {
+                const float4 q4 = load4(sQ + (c0 + c) * a.D + d);
+                dot[c] = fmaf(k4.x, q4.x, dot[c]);
+                dot[c] = fmaf(k4.y, q4.y, dot[c]);
+                dot[c] = fmaf(k4.z, q4.z, dot[c]);
+                dot[c] = fmaf(k4.w, q4.w, dot[c]);
+              }
             }
-          }
+          };
+          if (d_ways == 1) add(0, 4);  // apart, for its addresses without arithmetic
+          else add(4 * part, 4 * d_ways);
 #pragma unroll
           for (int c = 0; c < kGenQuarter; ++c) {
             const int row = s.p + group_row(a, s.col0 + min(c0 + c, s.cols - 1));
             const bool seen = pos >= 0 && pos <= row && (a.window == 0 || pos > row - a.window || pos < a.sinks);
             masked |= !seen;
-            sS[(c0 + c) * kGenPitchS + tok] = seen ? dot[c] * a.c2 : -INFINITY;
+            sS[(part * quarters * kGenQuarter + c0 + c) * kGenPitchS + tok] = seen ? dot[c] * a.c2 : -INFINITY;
           }
         }
       }
@@ -194,10 +211,15 @@ __global__ void __launch_bounds__(kGenThreads, C <= 2 ? 2 : 1) attend_general_ke
       // ---- weights ----
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const int c = 4 * warp + k;
+        const int c = warp + kGenThreads / 32 * k;
         if (c >= s.cols) break;
         float* row = sS + c * kGenPitchS;
-        const float x0 = row[lane], x1 = row[lane + 32];
+        float x0 = row[lane], x1 = row[lane + 32];
+        for (int y = 1; y < d_ways; ++y) {
+          const float* more_d = row + y * quarters * kGenQuarter * kGenPitchS;
+          x0 += more_d[lane];
+          x1 += more_d[lane + 32];
+        }
         const float mn = fmaxf(m[k], warp_max(fmaxf(x0, x1)));
         const float alpha = m[k] == -INFINITY ? 0.0f : exp2f(m[k] - mn);
         // a masked score is -inf and weighs 0; a NaN score stays NaN
@@ -210,7 +232,7 @@ __global__ void __launch_bounds__(kGenThreads, C <= 2 ? 2 : 1) attend_general_ke
       }
       __syncthreads();
       // ---- output ----
-      if (pv_active && my_c < s.cols) {
+      if (pv_active) {
 #pragma unroll
         for (int k = 0; k < C; ++k) {
           const float alpha = sh_alpha[min(my_c + k, s.cols - 1)];
@@ -219,33 +241,37 @@ __global__ void __launch_bounds__(kGenThreads, C <= 2 ? 2 : 1) attend_general_ke
         }
         const uint8_t* vr = sV + (size_t)stage * kGenTile * pitch + my_d * sizeof(T);
         const float* wr = sS + my_c * kGenPitchS;
+        auto add = [&](int begin, int end) {
 #pragma unroll 2
-        for (int tok = 0; tok < kGenTile; tok += 4) {
-          float4 v4[4];
+          for (int tok = begin; tok < end; tok += 4) {
+            float4 v4[4];
 #pragma unroll
-          for (int y = 0; y < 4; ++y) v4[y] = load4(reinterpret_cast<const T*>(vr + (size_t)(tok + y) * pitch));
+            for (int y = 0; y < 4; ++y) v4[y] = load4(reinterpret_cast<const T*>(vr + (size_t)(tok + y) * pitch));
 #pragma unroll
-          for (int k = 0; k < C; ++k) {
-            // (columns past the item's hold old weights: their sums are not written)
-            const float4 w4 = load4(wr + k * kGenPitchS + tok);
-            const float w[4] = {w4.x, w4.y, w4.z, w4.w};
+            for (int k = 0; k < C; ++k) {
+              // (columns past the item's hold old weights: their sums are not written)
+              const float4 w4 = load4(wr + k * kGenPitchS + tok);
+              const float w[4] = {w4.x, w4.y, w4.z, w4.w};
 #pragma unroll
-            for (int y = 0; y < 4; ++y) {
-              if (edge && w[y] == 0.0f) continue;  // what a masked token holds does not reach the sum
-              acc[k][0] = fmaf(w[y], v4[y].x, acc[k][0]);
-              acc[k][1] = fmaf(w[y], v4[y].y, acc[k][1]);
-              acc[k][2] = fmaf(w[y], v4[y].z, acc[k][2]);
-              acc[k][3] = fmaf(w[y], v4[y].w, acc[k][3]);
+              for (int y = 0; y < 4; ++y) {
+                if (edge && w[y] == 0.0f) continue;  // what a masked token holds does not reach the sum
+                acc[k][0] = fmaf(w[y], v4[y].x, acc[k][0]);
+                acc[k][1] = fmaf(w[y], v4[y].y, acc[k][1]);
+                acc[k][2] = fmaf(w[y], v4[y].z, acc[k][2]);
+                acc[k][3] = fmaf(w[y], v4[y].w, acc[k][3]);
+              }
             }
           }
-        }
+        };
+        if (t_ways == 1) add(0, kGenTile);
+        else add(my_part * (kGenTile / t_ways), (my_part + 1) * (kGenTile / t_ways));
       }
       __syncthreads();
       if (stages == 1 && x + 1 < s.ntiles) load_tile(s.tile0 + x + 1, 0);
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const int c = 4 * warp + k;
+      const int c = warp + kGenThreads / 32 * k;
       if (c >= s.cols) break;
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) l[k] += __shfl_xor_sync(0xFFFFFFFFu, l[k], o);
@@ -254,9 +280,31 @@ __global__ void __launch_bounds__(kGenThreads, C <= 2 ? 2 : 1) attend_general_ke
         sh_m[c] = m[k];
       }
     }
+    if (t_ways > 1) {  // the tokens' parts of the output, through the tiles' place
+      float4* sums_at = reinterpret_cast<float4*>(smem);
+      if (pv_active && my_part > 0) {
+#pragma unroll
+        for (int k = 0; k < C; ++k)
+          sums_at[((my_part - 1) * groups * C + my_c + k) * dv + my_d / 4] =
+              make_float4(acc[k][0], acc[k][1], acc[k][2], acc[k][3]);
+      }
+      __syncthreads();
+      if (my_part == 0) {
+        for (int y = 0; y < t_ways - 1; ++y) {
+#pragma unroll
+          for (int k = 0; k < C; ++k) {
+            const float4 w = sums_at[(y * groups * C + my_c + k) * dv + my_d / 4];
+            acc[k][0] += w.x;
+            acc[k][1] += w.y;
+            acc[k][2] += w.z;
+            acc[k][3] += w.w;
+          }
+        }
+      }
+    }
     __syncthreads();
     // ---- the item's result, or this part's ----
-    if (pv_active) {
+    if (my_part == 0) {
 #pragma unroll
       for (int k = 0; k < C; ++k) {
         const int c = my_c + k;
