@@ -305,31 +305,36 @@ __device__ __forceinline__ int cta_exclusive(int x, int* sums, int* total) {
   return before + incl - x;
 }
 
-// Sum of one int per CTA over the cluster's CTAs before this one and over all.
-struct ClusterSum {
-  int before, all;
+// A thread's run of pages, in index order over the cluster's threads: one prefix
+// sum ranks them all.
+struct PageRun {
+  int begin, end;
 };
-__device__ __forceinline__ ClusterSum cluster_sum(int mine, int* slot) {
-  cg::cluster_group cluster = cg::this_cluster();
-  if (threadIdx.x == 0) *slot = mine;
-  cluster.sync();
-  const int rank = (int)cluster.block_rank(), size = (int)cluster.num_blocks();
-  ClusterSum r{0, 0};
-  for (int c = 0; c < size; ++c) {
-    const int x = *cluster.map_shared_rank(slot, c);
-    r.all += x;
-    if (c < rank) r.before += x;
-  }
-  cluster.sync();  // the slot may be written again, and no CTA leaves while it is read
-  return r;
+__device__ __forceinline__ int pages_per_thread(int pages) {
+  return (pages - 1) / (kPageCluster * kPageThreads) + 1;
+}
+__device__ __forceinline__ PageRun page_run(int pages) {
+  const int run = pages_per_thread(pages);
+  const long long at = (long long)((int)cg::this_cluster().block_rank() * kPageThreads + (int)threadIdx.x) * run;
+  const int begin = (int)min((long long)pages, at);
+  return PageRun{begin, begin + min(run, pages - begin)};
 }
 
-// The cluster's pages, a contiguous range per CTA in index order.
-__device__ __forceinline__ void page_range(int pages, int* begin, int* end) {
-  const int rank = (int)cg::this_cluster().block_rank(), size = (int)cg::this_cluster().num_blocks();
-  const int per = (pages + size - 1) / size;
-  *begin = min(pages, rank * per);
-  *end = min(pages, *begin + per);
+// Exclusive prefix sum of x over the cluster's threads; *total: the sum.  `slot` is
+// an int of shared memory, which the CTA keeps until the cluster's next barrier.
+__device__ __forceinline__ int cluster_exclusive(int x, int* sums, int* slot, int* total) {
+  cg::cluster_group cluster = cg::this_cluster();
+  int all;
+  int before = cta_exclusive(x, sums, &all);
+  if (threadIdx.x == 0) *slot = all;
+  cluster.sync();
+  *total = 0;
+  for (int c = 0; c < kPageCluster; ++c) {
+    const int y = *cluster.map_shared_rank(slot, c);
+    *total += y;
+    if (c < (int)cluster.block_rank()) before += y;
+  }
+  return before;
 }
 
 // A small call with counts in a new array: one cluster.
@@ -400,32 +405,24 @@ __device__ __forceinline__ int slot_need(const ReserveLaunch& p, int entry) {
   return p.refs[entry] > 1 ? 2 : 0;
 }
 
-// One cluster of 8 CTAs.  Each lists the free pages of its eighth of the cache
-// by rank (as far as the request's need can reach); CTA 0 then walks the
-// requests, a thread each: a prefix sum of the needs gives every needed slot
-// its rank.  One cluster, because the ranks need every CTA's counts: a barrier of
-// the cluster costs less than a second launch.  6.4 us (12 requests, 1,024 pages),
-// 7.4 us (256 requests, 32,768 pages); barriers and round trips bound it.
+// One cluster of 8 CTAs lists the free pages by rank (as far as the requests' need
+// can reach); CTA 0 then walks the requests, a thread each: a prefix sum of the
+// needs gives every needed slot its rank.  One cluster, because the ranks need
+// every CTA's counts: a barrier of the cluster costs less than a second launch.
+// 5.4 us (12 requests, 1,024 pages), 6.8 us (256 requests, 32,768 pages); barriers
+// and round trips bound it.
 __global__ void __cluster_dims__(kPageCluster, 1, 1) __launch_bounds__(kPageThreads)
     reserve_kernel(const ReserveLaunch p) {
   __shared__ int sums[33], slot;
   cg::cluster_group cluster = cg::this_cluster();
   pdl_wait_prerequisites();
   pdl_launch_dependents();
-  int begin, end, total;
-  page_range(p.pages, &begin, &end);
-  int mine = 0;
-  for (int e = begin + threadIdx.x; e < end; e += kPageThreads) mine += p.refs[e] == 0 ? 1 : 0;
-  cta_exclusive(mine, sums, &total);
-  const ClusterSum f = cluster_sum(total, &slot);
-  int rank = f.before;
-  for (int e0 = begin; e0 < end && rank < p.cap; e0 += kPageThreads) {
-    const int e = e0 + threadIdx.x;
-    const bool is_free = e < end && p.refs[e] == 0;
-    const int at = rank + cta_exclusive(is_free ? 1 : 0, sums, &total);
-    if (is_free && at < p.cap) p.free_list[at] = e;
-    rank += total;
-  }
+  const PageRun run = page_run(p.pages);
+  int mine = 0, all_free;
+  for (int e = run.begin; e < run.end; ++e) mine += p.refs[e] == 0 ? 1 : 0;
+  int rank = cluster_exclusive(mine, sums, &slot, &all_free);
+  for (int e = run.begin; e < run.end && rank < p.cap; ++e)
+    if (p.refs[e] == 0) p.free_list[rank++] = e;
   __threadfence();
   cluster.sync();
   if (cluster.block_rank() != 0) return;
@@ -450,7 +447,7 @@ __global__ void __cluster_dims__(kPageCluster, 1, 1) __launch_bounds__(kPageThre
     }
     int all_need, all_cow, all_taken;
     const int at = needed + cta_exclusive(need, sums, &all_need);
-    const bool grant = s.ok && (need == 0 || at + need <= f.all);
+    const bool grant = s.ok && (need == 0 || at + need <= all_free);
     if (i < p.rows.B) {
       p.granted[i] = grant ? 1 : 0;
       if (s.ok && !grant) report(p.status, SPEC_ERR_CACHE_FULL);
@@ -556,8 +553,7 @@ struct CompactLaunch {
 };
 
 // The most entries of tables that compact_kernel rewrites: a launch less (1.7 us of
-// the host; 6 tables of 64 slots take the GPU 7.2 us so, 6.6 with the launch; 96 of
-// 384 slots 11.0 and 10.0).
+// the host), 0.6 us more of the GPU for 6 tables of 64 slots, 1.0 for 96 of 384.
 constexpr int kRemapHere = 1 << 14;
 
 // An entry through the map of moved pages.
@@ -570,43 +566,35 @@ __device__ __forceinline__ void remap_entry(const CompactLaunch& p, long long x,
 
 // One cluster of 8 CTAs: count the live pages (n), rank those at or past n and
 // the holes below n, pair them by rank, move the counts, then rewrite the tables
-// (large ones in remap_kernel).  7.2 us (509 pages), 10 us (32,768 pages, 96 tables
+// (large ones in remap_kernel).  5.2 us (509 pages), 7.5 us (32,768 pages, 96 tables
 // of 384 slots); barriers and round trips bound it.
 __global__ void __cluster_dims__(kPageCluster, 1, 1) __launch_bounds__(kPageThreads)
     compact_kernel(const CompactLaunch p) {
-  __shared__ int sums[33], slot;
+  __shared__ int sums[33], slot, low;
   cg::cluster_group cluster = cg::this_cluster();
   pdl_wait_prerequisites();
   pdl_launch_dependents();  // only now: the next kernel reads the table before its own wait
-  int begin, end, total;
-  page_range(p.pages, &begin, &end);
-  int live = 0;
-  for (int e = begin + threadIdx.x; e < end; e += kPageThreads) live += p.refs[e] > 0 ? 1 : 0;
-  cta_exclusive(live, sums, &total);
-  const ClusterSum c = cluster_sum(total, &slot);
-  const int n = c.all;
-  // live pages below n, over the cluster: the rank at which those past n start
-  int low = 0;
-  for (int e = begin + threadIdx.x; e < end && e < n; e += kPageThreads) low += p.refs[e] > 0 ? 1 : 0;
-  cta_exclusive(low, sums, &total);
-  const int n_low = cluster_sum(total, &slot).all;
+  const PageRun run = page_run(p.pages);
+  int live = 0, n;
+  for (int e = run.begin; e < run.end; ++e) live += p.refs[e] > 0 ? 1 : 0;
+  int rank = cluster_exclusive(live, sums, &slot, &n);
+  // live pages below n: the rank at which those from n on start, known to n's thread
+  if (run.begin <= n && n < run.end) {
+    low = rank;
+    for (int e = run.begin; e < n; ++e) low += p.refs[e] > 0 ? 1 : 0;
+  }
+  cluster.sync();
+  const int n_low = n < p.pages ? *cluster.map_shared_rank(&low, n / pages_per_thread(p.pages) / kPageThreads) : n;
   const int moves = n - n_low;
-  int rank = c.before;  // live pages before this round of threads
-  for (int e0 = begin; e0 < end; e0 += kPageThreads) {
-    const int e = e0 + threadIdx.x;
-    const bool is_live = e < end && p.refs[e] > 0;
-    const int r = rank + cta_exclusive(is_live ? 1 : 0, sums, &total);
-    if (e < end) {
-      if (!is_live) {
-        p.map[e] = -1;
-        if (e < n) p.dst[e - r] = e;
-      } else if (e < n) {
-        p.map[e] = e;
-      } else {
-        p.src[r - n_low] = e;
-      }
+  for (int e = run.begin; e < run.end; ++e) {
+    if (p.refs[e] <= 0) {
+      p.map[e] = -1;
+      if (e < n) p.dst[e - rank] = e;
+      continue;
     }
-    rank += total;
+    if (e < n) p.map[e] = e;
+    else p.src[rank - n_low] = e;
+    ++rank;
   }
   __threadfence();
   cluster.sync();
