@@ -21,15 +21,17 @@
 // is cleared in shared memory, and every wait is bounded.
 //
 // What it measures: 4 requests of 256 rows, 32 query heads over 8, D = 128, over
-// 4,096 positions 92 us (0.75 PFLOP/s of the two products), with a window of
-// 2,048 56 us; one request of 256 rows of 64 heads over 8, 16,384 positions, 160 us
-// (0.86).  The weights' two halves make three products of two, so the tensor
+// 4,096 positions 91 us (0.76 PFLOP/s of the two products), with a window of
+// 2,048 56 us; one request of 256 rows of 64 heads over 8, 16,384 positions, 157 us
+// (0.87).  The weights' two halves make three products of two, so the tensor
 // cores bound it at 1.26 of the measured 1.89 PFLOP/s: a tile of both sets takes
 // 4,000 cycles, of which the products take 3,072; the rest is the softmax's
 // 1,700 cycles a set, which the other set's products do not hide altogether.
 // Beginning the second product at half of the weights cost 7 % (its issue then
 // waits inside the other set's turn); reading the scores twice, to hold half of
-// them in registers, cost 7 %.
+// them in registers, cost 7 %; finding the maximum along with the weights, which
+// are done again where the reference does not serve, cost 15 % (all scores stay
+// live, and registers spill).
 //
 // Warps: 0 loads pages, 1 issues the MMAs (a set's scores of tile t + 1 right
 // behind its second product of tile t, while the other set is in its softmax),
