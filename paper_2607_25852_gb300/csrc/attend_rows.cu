@@ -188,7 +188,8 @@ __global__ void __launch_bounds__((4 + 4 * kSets) * 32, 1)
   const uint32_t tmem = tmem_sh, tO = tmem + kSets * kTile;
   const uint32_t ring = smem_u32(smem);
 
-  // 4 warps x 32 x 104 + 8 x 32 x 200 = 64,512 = 384 x 168 registers
+  // 4 warps x 32 x 72 + 8 x 32 x 216 = 64,512 = 384 x 168 registers; with 88 and 208
+  // the softmax spills (91 -> 95 us), with 56 and 224 the other warps do
   if (warp >= 4) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     // ---- softmax ----
