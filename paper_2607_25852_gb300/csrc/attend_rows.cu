@@ -413,15 +413,20 @@ __global__ void __launch_bounds__((4 + 4 * kSets) * 32, 1)
         int done[kSets] = {0, 0}, segments[kSets] = {0, 0};  // a set's second products, segments
         RingPos kp{0, 0u}, vp{2, 0u};  // K0 K1 V0 K2 V1 ...
         auto wait = [&](uint64_t* bar, int use) { ok = ok && wait_phase(bar, (uint32_t)use & 1u, a.status); };
+        // What is added to these stays beside its use: hoisted out of the loops, two
+        // sets' addresses would take more registers than the warp has.
+        auto recompute = [](uint32_t& x, uint32_t& y) { asm volatile("" : "+r"(x), "+r"(y)); };
         // the scores of set h of the tile at kp; `last`: no other set's follow
         auto scores = [&](int h, bool last, bool queries_done) {
           if (h == 0) wait(&ctl.full[kp.slot], (int)kp.use);
           if (!ok) return;
           tc_fence_after();
-          const uint32_t key = lo_kq(ring + kp.slot * kSlotBytes), mine = q + h * ((kSetRows * 128) >> 4);
+          const uint32_t key = lo_kq(ring + kp.slot * kSlotBytes);
+          uint32_t mine = q + h * ((kSetRows * 128) >> 4), to = tmem + h * kTile;
+          recompute(mine, to);
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk)
-            umma_bf16(tmem + h * kTile, desc(mine + (kk >> 2) * kQHalf + (((kk & 3) * 32) >> 4), kHiKQ),
+            umma_bf16(to, desc(mine + (kk >> 2) * kQHalf + (((kk & 3) * 32) >> 4), kHiKQ),
                       desc(key + (((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4), kHiKQ), kScores, kk > 0 ? 1u : 0u);
           umma_commit(&s_full[h]);
           if (last) {
@@ -453,9 +458,11 @@ __global__ void __launch_bounds__((4 + 4 * kSets) * 32, 1)
               if (!ok) break;
               tc_fence_after();
               const uint32_t v = lo_v(ring + vp.slot * kSlotBytes, D == 128 ? kHalfBytes : 0);
+              uint32_t from = tmem + h * kTile, to = tO + h * D;
+              recompute(from, to);
 #pragma unroll
               for (int kk = 0; kk < 2 * (kTile / 16); ++kk)  // the upper halves, then the rests
-                umma_bf16_tmem(tO + h * D, tmem + h * kTile + 8 * kk,
+                umma_bf16_tmem(to, from + 8 * kk,
                                desc(v + (kk % (kTile / 16)) * (2048 >> 4), kHiV), kOutputs, kk > 0 || x > 0 ? 1u : 0u);
               ++done[h];
               if (x == ntiles - 1) {
