@@ -21,13 +21,13 @@
 // is cleared in shared memory, and every wait is bounded.
 //
 // What it measures: 4 requests of 256 rows, 32 query heads over 8, D = 128, over
-// 4,096 positions 91 us (0.76 PFLOP/s of the two products), with a window of
-// 2,048 56 us; one request of 256 rows of 64 heads over 8, 16,384 positions, 157 us
-// (0.87).  The weights' two halves make three products of two, so the tensor
+// 4,096 positions 90 us (0.76 PFLOP/s of the two products), with a window of
+// 2,048 55 us; one request of 256 rows of 64 heads over 8, 16,384 positions, 156 us
+// (0.88).  The weights' two halves make three products of two, so the tensor
 // cores bound it at 1.26 of the measured 1.89 PFLOP/s: a tile of both sets takes
 // 4,000 cycles, of which the products take 3,072; the rest is the softmax's
 // 1,700 cycles a set, which the other set's products do not hide altogether.
-// Beginning the second product at half of the weights cost 7 % (its issue then
+// Beginning the second product at half of the weights cost 5 % (its issue then
 // waits inside the other set's turn); reading the scores twice, to hold half of
 // them in registers, cost 7 %; finding the maximum along with the weights, which
 // are done again where the reference does not serve, cost 15 % (all scores stay
@@ -188,8 +188,9 @@ __global__ void __launch_bounds__((4 + 4 * kSets) * 32, 1)
   const uint32_t tmem = tmem_sh, tO = tmem + kSets * kTile;
   const uint32_t ring = smem_u32(smem);
 
-  // 4 warps x 32 x 72 + 8 x 32 x 216 = 64,512 = 384 x 168 registers; with 88 and 208
-  // the softmax spills (91 -> 95 us), with 56 and 224 the other warps do
+  // 4 warps x 32 x 72 + 8 x 32 x 216 = 64,512 = 384 x 168 registers: neither side
+  // spills (4 requests of 256 rows, 4,096 positions: 90 us; with 88 and 208 95, with
+  // 56 and 224 92)
   if (warp >= 4) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     // ---- softmax ----
@@ -395,7 +396,7 @@ __global__ void __launch_bounds__((4 + 4 * kSets) * 32, 1)
     }
   } else {
     // The first segment goes out before the registers move, for which the softmax
-    // waits: 64 requests of 32 rows of 64 heads 338 -> 327 us (in the kernel for few
+    // waits: 64 requests of 32 rows of 64 heads 3 % faster (in the kernel for few
     // columns the same cost 3 % at 17 rows).
     if (warp == 3 && lane == 0) list_first(a, share, ctl);
     __syncwarp();
