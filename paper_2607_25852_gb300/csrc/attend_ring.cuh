@@ -450,6 +450,7 @@ __device__ __forceinline__ void load_pages(const AttendLaunch& a, const TcPlan& 
     issued = (int)__reduce_max_sync(0xFFFFFFFFu, (unsigned)issued);
     for (int u = max(0, issued - t.slots); u < issued; ++u)
       wait_phase(&ctl.full[u % t.slots], (uint32_t)((u / t.slots) & 1), a.status);
+    __syncwarp();
   }
 }
 

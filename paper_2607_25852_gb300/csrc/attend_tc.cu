@@ -244,8 +244,8 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
     float neg_lowest = 0.0f;  // the negative of this set's lowest reference
     RingPos vp{2, 0u};  // the place of a tile's values
     auto wait = [&](uint64_t* bar, uint32_t parity) {
-      // a lane's own finding until the next vote
-      if (!failed) failed = !wait_phase(bar, parity & 1u, a.status);
+      // by vote: the lanes leave their loops together, before what a whole warp has to execute as one
+      if (!failed) failed = !__all_sync(0xFFFFFFFFu, wait_phase(bar, parity & 1u, a.status));
     };
     // The second product of unit u.  A wait by parity must not come two phases
     // early: with four barriers in turn that would be before unit u - 4 is done,
