@@ -323,7 +323,9 @@ __global__ void __launch_bounds__(kGenThreads, C <= 2 ? 2 : 1) attend_general_ke
       if (s.slot < 0) {
         if (a.lse) a.lse[out_index(a, s, tid)] = row_lse(sh_m[tid], sh_l[tid]);
       } else {
-        a.part_stat[(size_t)s.slot * a.ct + tid] = make_float2(sh_m[tid], sh_l[tid]);
+        // scores that are all NaN leave no maximum, but a sum: a part that saw something has a finite one
+        a.part_stat[(size_t)s.slot * a.ct + tid] =
+            make_float2(sh_l[tid] == 0.0f ? sh_m[tid] : fmaxf(sh_m[tid], kNoMax), sh_l[tid]);
       }
     }
     if (s.slot >= 0) {

@@ -86,6 +86,7 @@ __device__ __forceinline__ int place_position(const ItemTiles& t, int place) {
   return place < t.ns ? place : place - t.ns + t.w0;
 }
 
+constexpr float kNoMax = -3.0e38f;  // the maximum of a column whose scores have none so far
 constexpr int kNowhere = -(1 << 28);  // the position of rows that see nothing
 
 // A request's rows as spec_attend takes them: p is kNowhere where its rows see
@@ -437,8 +438,8 @@ __device__ void join_parts(const AttendLaunch& a, const Segment& s, int tid, int
       o = make_float4(o.x * old, o.y * old, o.z * old, o.w * old);
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) {
+        if (st[k].x == -INFINITY) continue;  // a part that saw nothing (or does not exist) adds nothing
         const float f = part_weight(st[k], mb);
-        if (f == 0.0f) continue;  // a part that saw nothing (or does not exist) adds nothing
         l = fmaf(st[k].y, f, l);
         o.x = fmaf(w[k].x, f, o.x);
         o.y = fmaf(w[k].y, f, o.y);

@@ -17,7 +17,6 @@ constexpr int kHalfBytes = kTile * 128;  // 64 elements of 128 positions
 constexpr int kMaxSlots = 12;
 constexpr int kSegRing = 4;
 constexpr int kBadRing = 32;      // tiles between the loader and the softmax: fewer than 2 kMaxSlots
-constexpr float kNoMax = -3.0e38f;  // the reference of a column that has seen nothing
 constexpr float kGrowth = 24.0f;  // log2 of how far weights may exceed 1
 
 struct TcPlan {
