@@ -398,6 +398,12 @@ def _ints(t, n, what, dtype=torch.int32):
     return t.data_ptr()
 
 
+def _int(n):
+    """A window, a number of sinks or a layer as the C ABI's int: what 32 bits do not hold stays as large or negative as
+    they can say, where ctypes would keep the low bits."""
+    return n if -1 <= n <= 0x7FFFFFFF else 0x7FFFFFFF if n > 0 else -1
+
+
 def spec_attend_workspace(B: int, K: int, q_heads: int, kv_heads: int, head_dim: int, dtype=torch.bfloat16) -> int:
     return library().spec_attend_workspace(B, K, q_heads, kv_heads, head_dim, F32 if dtype == torch.float32 else BF16)
 
@@ -429,10 +435,10 @@ def spec_attend(q, k_cache, v_cache, page_table, pos_base, B, K, out, ws, row_of
         lse = lse_out.data_ptr()
     table, max_pages = _table(page_table, B)
     code = library().spec_attend(
-        q_ptr, q_row, Hq, cache, layer, _ints(row_offsets, B + 1, "row_offsets"),
+        q_ptr, q_row, Hq, cache, _int(layer), _ints(row_offsets, B + 1, "row_offsets"),
         _ints(depth, B, "depth"), _ints(pos_base, B, "pos_base", torch.int64), table, max_pages, B, K,
-        D ** -0.5 if scale is None else scale, window, sinks, out.data_ptr(), lse, _ints(status, 1, "status"),
-        ws.data_ptr(), ws.nbytes, _stream_handle(stream))
+        D ** -0.5 if scale is None else scale, _int(window), _int(sinks), out.data_ptr(), lse,
+        _ints(status, 1, "status"), ws.data_ptr(), ws.nbytes, _stream_handle(stream))
     if code:
         raise SpecError(code, "spec_attend")
 
@@ -448,7 +454,7 @@ def spec_cache_append(k_new, v_new, k_cache, v_cache, page_table, pos_base, B, K
         raise ValueError("k_new, v_new: rows for every request")
     table, max_pages = _table(page_table, B)
     code = library().spec_cache_append(
-        cache, layer, k_ptr, k_row, v_ptr, v_row, _ints(row_offsets, B + 1, "row_offsets"),
+        cache, _int(layer), k_ptr, k_row, v_ptr, v_row, _ints(row_offsets, B + 1, "row_offsets"),
         _ints(depth, B, "depth"), _ints(pos_base, B, "pos_base", torch.int64), table, max_pages, B, K,
         _ints(status, 1, "status"), _stream_handle(stream))
     if code:
@@ -513,8 +519,8 @@ def spec_cache_release(page_table, page_refs, pos_base, page_size, accepted_len=
     table, max_pages = _table(page_table, B)
     code = library().spec_cache_release(
         table, _ints(page_refs, 1, "page_refs"), _ints(pos_base, B, "pos_base", torch.int64),
-        _ints(accepted_len, B, "accepted_len"), B, max_pages, page_refs.numel(), page_size, window, sinks,
-        _ints(status, 1, "status"), _stream_handle(stream))
+        _ints(accepted_len, B, "accepted_len"), B, max_pages, page_refs.numel(), page_size,
+        _int(window), _int(sinks), _ints(status, 1, "status"), _stream_handle(stream))
     if code:
         raise SpecError(code, "spec_cache_release")
 
