@@ -2,9 +2,11 @@
 buffers that ``spec_attend`` and the ``spec_cache_*`` calls share, and a round's
 calls on them.
 
-Every step runs in libspec's kernels on the current stream; nothing here waits
-for the device.  A round, with the arrays that the other entry points already
-have (``pos_base``, and ``row_offsets`` and ``depth`` from ``spec_allocate``):
+Every step runs in libspec's kernels on the current stream (a fork also copies
+the table); nothing here waits for the device, and no buffer changes its place,
+so every call may be part of a captured graph.  A round, with the arrays that the
+other entry points already have (``pos_base``, and ``row_offsets`` and ``depth``
+from ``spec_allocate``):
 
     cache.reserve(pos_base, depth, row_offsets)           # pages for the rows
     for layer in ...:
@@ -50,7 +52,7 @@ class PagedCache:
         self._pairs = max(requests * (drafts // page_size + 2), max(1, pages // 2))
         self._src, self._dst = torch.empty(self._pairs, **ints), torch.empty(self._pairs, **ints)
         self._counts = torch.zeros(2, **ints)
-        self._other_table = torch.empty_like(self.page_table)
+        self._old_table = torch.empty_like(self.page_table)
         self._cache_ws = cache_workspace(requests, drafts, page_size, device)
         self._attend_ws = attend_workspace(requests, drafts, q_heads, kv_heads, head_dim, dtype, device)
 
@@ -82,10 +84,12 @@ class PagedCache:
                            window=self.window, sinks=self.sinks, status=self.status, stream=stream)
 
     def fork(self, parent, stream=None):
-        """Request i becomes a copy of request parent[i] (int32 [B] on the device; -1: empty), sharing its pages."""
-        spec_cache_fork(self.page_table, self.page_refs, parent, self._other_table, self.page_refs,
-                        status=self.status, stream=stream)
-        self.page_table, self._other_table = self._other_table, self.page_table
+        """Request i becomes a copy of request parent[i] (int32 [B] on the device; -1: empty), sharing its pages.  The
+        new table takes the old one's place (the old one is copied aside first), so that captured calls find it."""
+        with torch.cuda.stream(stream):
+            self._old_table.copy_(self.page_table)
+        spec_cache_fork(self._old_table, self.page_refs, parent, self.page_table, self.page_refs, status=self.status,
+                        stream=stream)
 
     def compact(self, stream=None):
         """Moves the live pages to the lowest indices; page_map[old] is a page's new index."""
