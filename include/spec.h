@@ -586,10 +586,13 @@ typedef struct spec_cache {
  *                   keys count as invisible), a position past the table (its
  *                   request's rows are treated as seeing nothing), or
  *                   inconsistent offsets or depths (the request's rows are
- *                   not written) set SPEC_ERR_BAD_INPUT.
+ *                   not written) set SPEC_ERR_BAD_INPUT.  SPEC_ERR_TIMEOUT: a
+ *                   bounded wait inside the kernel gave up, and the call's
+ *                   results are void.
  *   ws, ws_bytes    spec_attend_workspace(...) bytes, 256-byte aligned,
  *                   zero-filled once before the first use; left ready for the
- *                   next call.  Calls that may overlap need separate ones.
+ *                   next call, after SPEC_ERR_TIMEOUT too.  Calls that may
+ *                   overlap need separate ones.
  * Limits: 1 <= B, 0 <= K <= SPEC_MAX_DRAFTS, q_heads a multiple of kv_heads
  * and at most SPEC_MAX_GROUP times it, max_pages * page_size <= 2^30.  A longer
  * prompt is fed in chunks of up to K + 1 = 256 rows.

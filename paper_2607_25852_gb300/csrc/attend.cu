@@ -330,11 +330,7 @@ __global__ void __launch_bounds__(kGenThreads, C <= 2 ? 2 : 1) attend_general_ke
     }
     if (s.slot >= 0) {
       __syncthreads();
-      if (tid == 0) {
-        __threadfence();
-        last = atomicAdd(a.arrived + s.first_cta, 1u) == (uint32_t)s.parts - 1 ? 1 : 0;
-        if (last) a.arrived[s.first_cta] = 0;
-      }
+      if (tid == 0) last = arrive_part(a, s) ? 1 : 0;
       __syncthreads();
       if (last) {
         __threadfence();

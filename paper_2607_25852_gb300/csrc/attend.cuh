@@ -375,6 +375,28 @@ __device__ __forceinline__ int part_slot(const Segment& s, int x) {
   return 2 * (s.first_cta + x * s.step) + (x == 0 ? 1 : 0);
 }
 
+// One thread, past the writing of a part: is it the item's last to arrive?  Then the
+// counter is back at zero for the next call.
+__device__ __forceinline__ bool arrive_part(const AttendLaunch& a, const Segment& s) {
+  __threadfence();
+  const bool last = atomicAdd(a.arrived + s.first_cta, 1u) == (uint32_t)s.parts - 1;
+  if (last) a.arrived[s.first_cta] = 0;
+  return last;
+}
+
+// One thread of a CTA whose wait gave up: the arrivals of the share's parts that it
+// leaves out, from segment `done` on.  So every part arrives once in every call, and
+// the counters are ready for the next one whatever became of this one.
+template <int TT>
+__device__ __noinline__ void arrive_for_rest(const AttendLaunch& a, const Share& share, int done) {
+  Walk<TT> walk(a, share);
+  Segment s;
+  for (int n = 0; walk.next(&s); ++n) {
+    if (n >= done && s.slot >= 0) arrive_part(a, s);
+    walk.advance();
+  }
+}
+
 // Where column c of a segment goes: packed row * Hq + query head.
 __device__ __forceinline__ long long out_index(const AttendLaunch& a, const Segment& s, int c) {
   const int col = s.col0 + c, j = group_row(a, col);

@@ -256,6 +256,8 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
       wait(&ctl.seg_full[n % kSegRing], n / kSegRing);
       if (named_or(1, kSoftThreads, failed)) {  // no one has left the last segment's end behind
         ctl.aborted = 1;
+        if (st == 0) arrive_for_rest<kTile>(a, share, n);
+        __syncwarp();
         break;
       }
       if (s.request < 0) break;
@@ -504,11 +506,7 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
       }
       if (!whole) {
         named_sync(1, kSoftThreads);
-        if (st == 0) {
-          __threadfence();
-          last_sh = atomicAdd(a.arrived + s.first_cta, 1u) == (uint32_t)s.parts - 1 ? 1 : 0;
-          if (last_sh) a.arrived[s.first_cta] = 0;
-        }
+        if (st == 0) last_sh = arrive_part(a, s) ? 1 : 0;
         named_sync(1, kSoftThreads);
         if (last_sh) {
           __threadfence();
