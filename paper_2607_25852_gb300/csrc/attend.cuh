@@ -106,9 +106,11 @@ __device__ __forceinline__ AttendRows attend_rows(const AttendLaunch& a, int i) 
   return o;
 }
 
-// Tiles of one key-value head of a request, over its column tiles.
+// Tiles of one key-value head of a request, over its column tiles.  (2^30 positions
+// make up to 2^24 tiles, 256 rows of 64 heads 512 column tiles.)
 struct HeadUnits {
-  int all, items, longest;  // tiles, column tiles, tiles of the longest
+  long long all;       // tiles
+  int items, longest;  // column tiles, tiles of the longest
 };
 template <int TT>
 __device__ __forceinline__ int item_units(const AttendLaunch& a, const AttendRows& r, int c0) {
@@ -131,8 +133,8 @@ __device__ __forceinline__ HeadUnits head_units(const AttendLaunch& a, const Att
 // `request`, whose first unit is `base`.
 struct Share {
   long long units, u0, u1, base;
+  long long per;   // units of one head of the request
   int ctas, cta;   // of the list, and this one's place among them
-  int per;         // units of one head of the request
   int request;
   AttendRows rows; // of the request
 };
@@ -169,7 +171,7 @@ __device__ void find_share(const AttendLaunch& a, Share* sh, ShareSums* sums) {
         per = head_units<TT>(a, r);
         if (r.bad && pass == 0 && blockIdx.x == 0) report(a.status, SPEC_ERR_BAD_INPUT);
       }
-      const long long mine = (long long)per.all * heads;
+      const long long mine = per.all * heads;
       // items are counted up to 4096 per request: exact where they are few
       const int my_items = min(per.items * heads, 4096);
       long long incl = mine;
@@ -217,7 +219,7 @@ __device__ void find_share(const AttendLaunch& a, Share* sh, ShareSums* sums) {
           const int k = c - (incl_items - my_items);  // the item's place in this thread's request
           if (k >= 0 && k < my_items) {
             const int h = k / per.items;
-            u0 = incl - mine + (long long)h * per.all;
+            u0 = incl - mine + h * per.all;
             int c0 = 0;
             for (int x = h * per.items; x < k; ++x, c0 += a.ct) u0 += item_units<TT>(a, r, c0);
             sh->u0 = u0;
@@ -240,7 +242,7 @@ __device__ void find_share(const AttendLaunch& a, Share* sh, ShareSums* sums) {
         // share leaves work for
         const int few = (int)ceilf(sqrtf((float)total * (float)items * a.part_tiles));
         ctas = max(1, min(ctas, few));
-        const int share = (int)((total + ctas - 1) / ctas);
+        const long long share = (total + ctas - 1) / ctas;
         ctas = (int)((total + share - 1) / share);
       }
       if (c < ctas) {

@@ -27,7 +27,7 @@ def lib(tmp_path_factory):
     return ctypes.CDLL(so)
 
 
-def shares(lib, pos, depth, K, G, Hkv, tile, ct, ctas, lists, stop=None, window=0, sinks=0, page_size=128, max_pages=1 << 20,
+def shares(lib, pos, depth, K, G, Hkv, tile, ct, ctas, lists, stop=None, window=0, sinks=0, page_size=128, max_pages=1 << 23,
            threads=256, part_cost=4, item_cost=4, part_tiles=6.0, arrived=None):
     """The listed segments, and the arrival counters after the call."""
     B, most = len(pos), 1 << 16
@@ -85,6 +85,10 @@ CASES = [  # pos, depth, G, Hkv, tile, columns per item, CTAs, lists
     ([4000] * 4, [255] * 4, 4, 8, 128, 256, 152, 8),
     ([900 * (i % 7) for i in range(700)], [i % 3 for i in range(700)], 3, 1, 64, 32, 304, 1),
     ([3000, 10, 90], [31, 0, 40], 64, 1, 64, 32, 152, 1),
+    # 2^33 tiles of one head: as far as positions, rows and heads of a group go
+    ([(1 << 30) - 256], [255], 64, 1, 64, 32, 152, 1),
+    ([(1 << 30) - 300, 7], [255, 255], 64, 2, 64, 32, 304, 2),
+    ([(1 << 30) - 256] * 3, [255] * 3, 64, 1, 128, 256, 152, 1),
 ]
 
 
