@@ -503,24 +503,20 @@ cudaError_t launch(const AttendLaunch& a, cudaStream_t stream) {
   t.chunk = a.grain;
   t.nchunk = kTile / t.chunk;
   constexpr int kSlot = (D / 64) * kHalfBytes, kQueries = kItemCols * D * 2;
-  // what the kernel's static shared memory takes, read once
-  static int static_smem = -1;
-  if (static_smem < 0) {
-    cudaFuncAttributes fa{};
-    const cudaError_t err = cudaFuncGetAttributes(&fa, attend_rows_kernel<D>);
-    if (err != cudaSuccess) return err;
-    static_smem = (int)fa.sharedSizeBytes;
-  }
+  static std::atomic<int> known;
+  int fixed;  // bytes of static shared memory
+  cudaError_t err = static_smem(attend_rows_kernel<D>, known, &fixed);
+  if (err != cudaSuccess) return err;
   // dynamic shared memory starts behind the static one, on a 1024-byte boundary
   // (1 KB of an SM's 228 KB is reserved per CTA)
-  const int limit = 227 * 1024, room = limit - (static_smem + 1023) / 1024 * 1024;
+  const int limit = 227 * 1024, room = limit - (fixed + 1023) / 1024 * 1024;
   t.slots = std::min((room - kQueries) / kSlot, kMaxSlots);
   t.q_off = t.slots * kSlot;
-  const int smem = t.q_off + kQueries + limit - room - static_smem;  // and the gap before it
+  const int smem = t.q_off + kQueries + limit - room - fixed;  // and the gap before it
   CUtensorMap tmK, tmV;
   if (!make_cache_map(&tmK, a.k, a, t.chunk) || !make_cache_map(&tmV, a.v, a, t.chunk)) return cudaErrorInvalidValue;
   static std::atomic<size_t> raised[kMaxDevices];
-  const cudaError_t err = raise_smem(attend_rows_kernel<D>, (size_t)smem, raised);
+  err = raise_smem(attend_rows_kernel<D>, (size_t)smem, raised);
   if (err != cudaSuccess) return err;
   return launch_after_previous(attend_rows_kernel<D>, dim3(a.ctas), dim3((4 + 4 * kSets) * 32), (size_t)smem, stream,
                                tmK, tmV, a, t);

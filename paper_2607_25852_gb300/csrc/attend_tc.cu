@@ -618,27 +618,23 @@ cudaError_t launch_variant(const AttendLaunch& a, cudaStream_t stream) {
   constexpr int kPerSm = two_per_sm(D, CG) ? 2 : 1;
   const int q_bytes = a.ct * D * 2, p_bytes = a.ct / 8 / H * kPChunkBytes, slot = (D / 64) * kHalfBytes;
   t.p_bytes = p_bytes;
-  // what the kernel's static shared memory takes, read once
-  static int static_smem = -1;
-  if (static_smem < 0) {
-    cudaFuncAttributes fa{};
-    const cudaError_t err = cudaFuncGetAttributes(&fa, attend_tc_kernel<D, CG, H>);
-    if (err != cudaSuccess) return err;
-    static_smem = (int)fa.sharedSizeBytes;
-  }
+  static std::atomic<int> known;
+  int fixed;  // bytes of static shared memory
+  cudaError_t err = static_smem(attend_tc_kernel<D, CG, H>, known, &fixed);
+  if (err != cudaSuccess) return err;
   // dynamic shared memory starts behind the static one, on a 1024-byte boundary
   // (1 KB of an SM's 228 KB is reserved per CTA)
   const int limit = 228 * 1024 / kPerSm - 1024;
-  const int room = limit - (static_smem + 1023) / 1024 * 1024;
+  const int room = limit - (fixed + 1023) / 1024 * 1024;
   t.slots = (room - QB * q_bytes - PB * p_bytes) / slot;
   if (t.slots > kMaxSlots) t.slots = kMaxSlots;
   t.q_off = t.slots * slot;
   t.p_off = t.q_off + QB * q_bytes;
-  const int smem = t.p_off + PB * p_bytes + limit - room - static_smem;  // and the gap before it
+  const int smem = t.p_off + PB * p_bytes + limit - room - fixed;  // and the gap before it
   CUtensorMap tmK, tmV;
   if (!make_cache_map(&tmK, a.k, a, t.chunk) || !make_cache_map(&tmV, a.v, a, t.chunk)) return cudaErrorInvalidValue;
   static std::atomic<size_t> raised[kMaxDevices];
-  const cudaError_t err = raise_smem(attend_tc_kernel<D, CG, H>, (size_t)smem, raised);
+  err = raise_smem(attend_tc_kernel<D, CG, H>, (size_t)smem, raised);
   if (err != cudaSuccess) return err;
   return launch_after_previous(attend_tc_kernel<D, CG, H>, dim3(a.ctas), dim3((4 + 4 * H) * 32), (size_t)smem, stream,
                                tmK, tmV, a, t);

@@ -128,7 +128,8 @@ __device__ __forceinline__ float warp_max(float x) {
 // Host side
 // ---------------------------------------------------------------------------
 inline PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() {
-  static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
+  static std::atomic<PFN_cuTensorMapEncodeTiled_v12000> known{nullptr};
+  PFN_cuTensorMapEncodeTiled_v12000 fn = known.load(std::memory_order_relaxed);
   if (!fn) {
     void* ptr = nullptr;
     cudaDriverEntryPointQueryResult q;
@@ -136,6 +137,7 @@ inline PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() {
             cudaSuccess &&
         q == cudaDriverEntryPointSuccess)
       fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(ptr);
+    known.store(fn, std::memory_order_relaxed);
   }
   return fn;
 }
@@ -152,6 +154,20 @@ inline int device_sms() {
   if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 1;
   if (kept) known[dev].store(sms, std::memory_order_relaxed);
   return sms;
+}
+
+// A kernel's static shared memory, asked for once: `known` is the kernel's own, 0
+// before that (no kernel that asks has none).
+template <typename Kernel>
+inline cudaError_t static_smem(Kernel kernel, std::atomic<int>& known, int* bytes) {
+  *bytes = known.load(std::memory_order_relaxed);
+  if (*bytes > 0) return cudaSuccess;
+  cudaFuncAttributes fa{};
+  const cudaError_t err = cudaFuncGetAttributes(&fa, kernel);
+  if (err != cudaSuccess) return err;
+  *bytes = (int)fa.sharedSizeBytes;
+  known.store(*bytes, std::memory_order_relaxed);
+  return cudaSuccess;
 }
 
 // Raises a kernel's dynamic shared memory limit, once per device and size:
