@@ -436,9 +436,10 @@ extern "C" int spec_attend(const void* q, int64_t q_row_stride, int q_heads, con
   a.table = page_table;
   a.rows = RowLayout{row_offsets, depth, pos_base, B, K};
   a.c2 = (float)(1.4426950408889634 * (double)scale);
-  // a window longer than the table hides nothing
-  a.window = (long long)window > (long long)max_pages * cache->page_size ? 0 : window;
-  a.sinks = sinks;
+  // a window longer than the table hides nothing, and sinks end with the table
+  const int table_end = max_pages * cache->page_size;
+  a.window = window > table_end ? 0 : window;
+  a.sinks = std::min(sinks, table_end);
   a.out = out;
   a.lse = lse_out;
   a.status = status;

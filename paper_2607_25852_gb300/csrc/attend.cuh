@@ -86,6 +86,11 @@ __device__ __forceinline__ int place_position(const ItemTiles& t, int place) {
   return place < t.ns ? place : place - t.ns + t.w0;
 }
 
+// And the place of a position, -1 if it has none.
+__device__ __forceinline__ int position_place(const ItemTiles& t, int pos) {
+  return pos < t.ns ? pos : pos < t.w0 ? -1 : pos - t.w0 + t.ns;
+}
+
 constexpr float kNoMax = -3.0e38f;  // the maximum of a column whose scores have none so far
 constexpr int kNowhere = -(1 << 28);  // the position of rows that see nothing
 

@@ -185,29 +185,33 @@ __device__ __forceinline__ void hide_values(uint8_t* tile, int y, bool any, bool
   }
 }
 
-// What was cleared in shared memory for the sake of rows that must not see it,
-// for a row (at position r) that does: the values at d, of the positions that
-// some of the item's rows see and some do not, that are not finite.  Rare, so a
-// plain loop over the cache.
-template <int D>
-__device__ __noinline__ float cleared_values(const AttendLaunch& a, const Segment& s, int r, int d) {
+// What was cleared in shared memory for the sake of rows that must not see it has
+// to be given back to those that do: calls f(position, its values) for the
+// positions of the segment that some of the item's rows see and some do not, in
+// order.  Those are the positions past the first row's own and, with a window,
+// those that it sees and the last row does not: at most twice as many as the item
+// has rows, however long the segment is.  Rare, so a plain loop over the cache,
+// which all threads walk alike.
+template <typename F>
+__device__ __forceinline__ void for_edge_values(const AttendLaunch& a, const Segment& s, F f) {
   const int p_first = s.p + group_row(a, s.col0), p_last = s.p + group_row(a, s.col0 + s.cols - 1);
-  float sum = 0.0f;
-  for (int x = 0; x < s.ntiles; ++x) {
-    for (int y = 0; y < kTile; ++y) {
-      const int pos = place_position(s.tiles, (s.tile0 + x) * kTile + y);
-      const bool any = pos <= p_last && (a.window == 0 || pos > p_first - a.window || pos < a.sinks);
-      const bool all = pos <= p_first && (a.window == 0 || pos > p_last - a.window || pos < a.sinks);
-      const bool seen = pos <= r && (a.window == 0 || pos > r - a.window || pos < a.sinks);
-      if (!any || all || !seen) continue;
-      const int page = a.table[(size_t)s.request * a.max_pages + pos / a.page_size];
-      if (page < 0 || page >= a.pages) continue;
-      const char* at = a.v + (int64_t)page * a.page_b + (int64_t)(pos % a.page_size) * a.token_b + s.head * a.head_b;
-      const float v = load_elem(reinterpret_cast<const __nv_bfloat16*>(at) + d);
-      if (!isfinite(v)) sum += v;
-    }
+  const int left = max(0, max(a.sinks, p_first - a.window + 1)), own = max(0, p_first + 1);
+  const int leaving = a.window > 0 ? max(0, min(p_first, p_last - a.window) - left + 1) : 0;
+  const int all = leaving + max(0, p_last - own + 1);
+#pragma unroll 1
+  for (int x = 0; x < all; ++x) {
+    const int pos = x < leaving ? left + x : own + x - leaving;
+    const int place = position_place(s.tiles, pos), tile = place / kTile - s.tile0;
+    if (place < 0 || tile < 0 || tile >= s.ntiles) continue;  // another segment's
+    const int page = a.table[(size_t)s.request * a.max_pages + pos / a.page_size];
+    if (page < 0 || page >= a.pages) continue;
+    f(pos, reinterpret_cast<const __nv_bfloat16*>(a.v + (int64_t)page * a.page_b +
+                                                  (int64_t)(pos % a.page_size) * a.token_b + s.head * a.head_b));
   }
-  return sum;
+}
+// Does a row at position r see position pos?
+__device__ __forceinline__ bool row_sees(const AttendLaunch& a, int r, int pos) {
+  return pos <= r && (a.window == 0 || pos > r - a.window || pos < a.sinks);
 }
 
 // An item's queries into shared memory, [64-element halves][column][128 bytes]

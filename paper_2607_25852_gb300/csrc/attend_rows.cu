@@ -361,12 +361,19 @@ __global__ void __launch_bounds__((4 + 4 * kSets) * 32, 1)
         tmem_ld32(my_o + d, o);
         if (!real) continue;
         if (poisoned) {
-          for (int k = 0; k < 32; ++k) {
-            const float add = cleared_values<D>(a, s, r, d + k);
+          for_edge_values(a, s, [&](int pos, const __nv_bfloat16* values) {
+            if (!row_sees(a, r, pos)) return;
 #pragma unroll
-            for (int y = 0; y < 32; ++y)
-              if (y == k) o[y] += add;
-          }
+            for (int k = 0; k < 32; k += 8) {
+              const uint4 w = __ldg(reinterpret_cast<const uint4*>(values + d + k));
+              const uint32_t e[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+              for (int y = 0; y < 4; ++y) {
+                if (bf16_not_finite(e[y])) o[k + 2 * y] += bf16_lo(e[y]);
+                if (bf16_not_finite(e[y] >> 16)) o[k + 2 * y + 1] += bf16_hi(e[y]);
+              }
+            }
+          });
         }
         if (whole) {
           store_row32<D>(a, out, d, o, inv);

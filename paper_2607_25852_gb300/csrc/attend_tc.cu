@@ -473,12 +473,14 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
 #pragma unroll
         for (int j = 0; j < 16; ++j) o[j] += rest[j];
         if (poisoned) {
-          for (int j = 0; j < 16; ++j) {
-            const float add = j < nc ? cleared_values<D>(a, s, sRow[hf * kSetCols + g * 8 + j], tl) : 0.0f;
+          const int* rows = sRow + hf * kSetCols + g * 8;
+          for_edge_values(a, s, [&](int pos, const __nv_bfloat16* values) {
+            const float add = load_elem(values + tl);
+            if (isfinite(add)) return;
 #pragma unroll
-            for (int k = 0; k < 16; ++k)
-              if (k == j) o[k] += add;
-          }
+            for (int j = 0; j < 16; ++j)
+              if (j < nc && row_sees(a, rows[j], pos)) o[j] += add;
+          });
         }
         if (whole) {
           __nv_bfloat16* row = staged + g * 8 * D + tl;

@@ -71,3 +71,23 @@ def test_a_window_hides_nan_keys(dtype, D, ps, K):
     t = torch.arange(4, 3000 - 900 + 1)
     c.k[c.table[0, t // ps].long().to(DEV), (t % ps).to(DEV)] = float("nan")
     check(c, *c.call(), want, torch.zeros((K + 1, 8), dtype=torch.bool))
+
+
+@pytest.mark.parametrize("dtype,D,ps,K", FORMS)
+@pytest.mark.parametrize("window,sinks", [(2, 0), (2, (1 << 31) - 1), (1, 1), (3, 2)])
+def test_infinite_values_beside_rows_before_the_first_position(window, sinks, dtype, D, ps, K):
+    """Some rows lie before position 0 and see nothing; an infinite value of position 1 reaches the rows that see it."""
+    if K < 3:
+        K = 3
+    c = Case([-2], [K], K, 8, 2, D, ps, dtype, window=window, sinks=sinks, seed=D + K)
+    want, want_lse, mass, big = ref.attend(c.q, c.k, c.v, c.table, c.pos, c.rows, ref.sqrt_scale(D), window, sinks)
+    c.v[int(c.table[0, 1 // ps]), 1 % ps, 1, 5] = float("inf")
+    hit = torch.zeros(want.shape, dtype=torch.bool)
+    for j in range(K + 1):
+        hit[j, 4:, 5] = 1 in ref.visible(j - 2, window, sinks)
+    out, lse = c.call()
+    tol, tol_lse = ref.bounds(want, mass, big, K + 1, D, dtype == BF16)
+    got, got_lse = out.cpu().double(), lse.cpu().double()
+    assert (~got[hit].isfinite()).all() and ((got - want).abs() <= tol)[~hit].all()
+    assert torch.equal(got_lse == -float("inf"), want_lse == -float("inf")) and (got_lse[:2] == -float("inf")).all()
+    assert ((got_lse - want_lse).abs() <= tol_lse)[2:].all() and int(c.status.item()) == 0
