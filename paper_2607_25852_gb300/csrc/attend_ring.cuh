@@ -338,6 +338,7 @@ __device__ __noinline__ void join_tc(const AttendLaunch& a, const Segment& s, co
 struct Control {
   uint64_t full[kMaxSlots], empty[kMaxSlots], q_full[2], q_free[2], seg_full[kSegRing], seg_free[kSegRing], drained;
   volatile int aborted;
+  volatile int loaded;     // tiles that the loader has come to
   int tile_bad[kBadRing];  // per tile: the boxes whose page is not one
   int2 page[2][16];        // a tile's boxes: page, first position in it
   Segment segs[kSegRing];
@@ -358,6 +359,29 @@ __device__ __forceinline__ void init_control(Control& ctl, int slots, int reader
   }
   mbar_init(&ctl.drained, 1);
   ctl.aborted = 0;
+  ctl.loaded = 0;
+}
+
+// wait_phase for what a segment's end gives back (a place in the list, the queries'
+// buffer): a segment may take longer than any fixed time, so the wait gives up once
+// the loader has come to no other tile for about a second, or the CTA has given up.
+__device__ __forceinline__ bool wait_segment(Control& ctl, uint64_t* bar, uint32_t parity, int32_t* status) {
+  if (mbar_try_wait(bar, parity)) return true;
+  uint64_t t0 = global_ns();
+  int loaded = ctl.loaded;
+  for (uint32_t it = 1; !mbar_try_wait(bar, parity); ++it) {
+    if ((it & 255u) != 0u) continue;
+    if (ctl.aborted) return false;
+    const uint64_t now = global_ns();
+    if (ctl.loaded != loaded) {
+      loaded = ctl.loaded;
+      t0 = now;
+    } else if (now - t0 > 1000000000ull) {
+      report(status, SPEC_ERR_TIMEOUT);
+      return false;
+    }
+  }
+  return true;
 }
 
 // The n-th segment of the share, for a reading warp.
@@ -428,7 +452,10 @@ __device__ __forceinline__ void load_pages(const AttendLaunch& a, const TcPlan& 
       const uint32_t bads = __ballot_sync(0xFFFFFFFFu, bad);
       if (bad) report(a.status, SPEC_ERR_BAD_INPUT);
       if (bad || !wanted) page = a.pages;  // past the map's last page: zeros are written, nothing is read
-      if (lane == 0) ctl.tile_bad[tiles % kBadRing] = (int)bads;
+      if (lane == 0) {
+        ctl.tile_bad[tiles % kBadRing] = (int)bads;
+        ctl.loaded = tiles;
+      }
       if (mine) ctl.page[tiles & 1][c] = make_int2(page, tok);
       __syncwarp();
       if (elect_one())
@@ -469,7 +496,8 @@ __device__ __forceinline__ void stage_queries(const AttendLaunch& a, Control& ct
     }
     if (s.request < 0 || __any_sync(0xFFFFFFFFu, ctl.aborted)) break;
     const int b = n % QB;
-    if (n >= QB && !__all_sync(0xFFFFFFFFu, wait_phase(&ctl.q_free[b], (uint32_t)(((n / QB) - 1) & 1), a.status))) {
+    if (n >= QB &&
+        !__all_sync(0xFFFFFFFFu, wait_segment(ctl, &ctl.q_free[b], (uint32_t)(((n / QB) - 1) & 1), a.status))) {
       ctl.aborted = 1;
       break;
     }
@@ -497,7 +525,7 @@ __device__ __forceinline__ void list_segments(const AttendLaunch& a, const Share
   }
   for (int n = N0; !ctl.aborted; ++n) {
     const int k = n % kSegRing;
-    if (n >= kSegRing && !wait_phase(&ctl.seg_free[k], (uint32_t)(((n / kSegRing) - 1) & 1), a.status)) {
+    if (n >= kSegRing && !wait_segment(ctl, &ctl.seg_free[k], (uint32_t)(((n / kSegRing) - 1) & 1), a.status)) {
       ctl.aborted = 1;
       break;
     }

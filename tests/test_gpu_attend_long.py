@@ -61,3 +61,31 @@ def test_a_value_that_is_not_finite_costs_no_walk_over_the_context(D, K, G, wind
     out, ms = call()
     assert (~out[hit].isfinite()).all() and torch.equal(out[~hit], clean[~hit])
     assert ms < 10 * clean_ms, (ms, clean_ms)
+
+
+@pytest.mark.parametrize("D,K,G,B,p", [(64, 0, 4, 320, 150_000_000), (128, 63, 4, 160, 80_000_000)])
+def test_a_segment_may_take_longer_than_a_wait(D, K, G, B, p):
+    """Items of more than a second each, parts of two or more per CTA (the waits are bounded to about a second).  All positions
+    hold the same few pages over and over, so that the keys come from the L2, and every request the same queries."""
+    ps, pages = 1 << 16, 8
+    g = torch.Generator(device=DEV).manual_seed(2)
+    k, v = (torch.randn((pages, ps, 1, D), device=DEV, generator=g).to(torch.bfloat16) for _ in range(2))
+    slots = (p + K) // ps + 1
+    table = (torch.arange(slots, dtype=torch.int32, device=DEV) % pages).repeat(B, 1)
+    q = torch.randn((K + 1, G, D), device=DEV, generator=g).to(torch.bfloat16).repeat(B, 1, 1)
+    out, lse = torch.zeros_like(q), torch.zeros(q.shape[:2], device=DEV)
+    ws = spec.attend_workspace(B, K, G, 1, D)
+    st = torch.zeros(1, dtype=torch.int32, device=DEV)
+    a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    a.record()
+    spec.spec_attend(q, k, v, table, torch.full((B,), p, dtype=torch.int64, device=DEV), B, K, out, ws, lse_out=lse, status=st)
+    b.record()
+    torch.cuda.synchronize()
+    print(f"{a.elapsed_time(b):.0f} ms")
+    assert int(st) == 0
+    # Every position is there as often as every other, give or take one of the p / (8 * 65,536) rounds of the pages.
+    # A thread's sum has a term per tile of 128 positions, with many rows one per 8 positions: as many roundings of 2^-24.
+    tol = pages * ps / p + (p / 128 if K == 0 else p / 8) * 2.0 ** -24 + 1e-4
+    x = torch.einsum("jhd,td->jht", q[:K + 1].double(), k.view(-1, D).double()) * D ** -0.5
+    want = torch.logsumexp(x, 2) + math.log(p / (pages * ps))
+    assert ((lse.view(B, K + 1, G).double() - want).abs() < tol).all()
