@@ -351,20 +351,22 @@ static int general_ctas_per_sm(int D, int dtype) {
 }
 
 struct AttendGeometry {
-  int ct;    // columns per item, the most of the kernels that may serve the shape
-  int ctas;  // most CTAs: two parts each
   size_t part_off, stat_off, bytes;
 };
 
-// The counters come first, so that their place does not depend on the kernel.
+// Room for the parts (two per CTA) of whichever kernel serves the shape: which one
+// does depends on the cache's pages and strides too.  The counters come first, as
+// many for every shape: a workspace may serve several in turn.
 static AttendGeometry attend_geometry(int cols, int D, int dtype) {
+  size_t columns = (size_t)2 * kAttendMaxSms * general_ctas_per_sm(D, dtype) * kGenCols;
+  if (attend_tc_may_serve(D, dtype)) {
+    const int ct = attend_tc_columns(cols);
+    columns = std::max(columns, (size_t)2 * kAttendMaxSms * attend_tc_ctas_per_sm(D, ct) * ct);
+  }
   AttendGeometry g{};
-  g.ct = dtype == SPEC_BF16 ? std::max(kGenCols, attend_tc_columns(cols)) : kGenCols;
-  g.ctas = kAttendMaxSms * 2;
-  const size_t slots = 2 * (size_t)g.ctas;
-  g.part_off = ((size_t)g.ctas * 4 + 255) / 256 * 256;
-  g.stat_off = g.part_off + (slots * g.ct * D * 4 + 255) / 256 * 256;
-  g.bytes = g.stat_off + (slots * g.ct * 8 + 255) / 256 * 256;
+  g.part_off = (2 * kAttendMaxSms * 4 + 255) / 256 * 256;
+  g.stat_off = g.part_off + (columns * D * 4 + 255) / 256 * 256;
+  g.bytes = g.stat_off + (columns * 8 + 255) / 256 * 256;
   return g;
 }
 

@@ -646,7 +646,7 @@ cudaError_t launch_variant(const AttendLaunch& a, cudaStream_t stream) {
 
 bool attend_tc_serves(int D, int dtype, int page_size, int64_t head_b, int64_t token_b, int64_t page_b) {
   const int64_t far = 1LL << 40;  // a tensor map's strides end there
-  return dtype == SPEC_BF16 && (D == 64 || D == 128) && page_size % 8 == 0 && head_b < far && token_b < far && page_b < far;
+  return attend_tc_may_serve(D, dtype) && page_size % 8 == 0 && head_b < far && token_b < far && page_b < far;
 }
 
 int attend_tc_grain(int page_size) { return std::min(page_size & -page_size, kTile); }

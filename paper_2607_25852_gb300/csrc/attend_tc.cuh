@@ -9,7 +9,9 @@ namespace spec {
 // fit TMEM; of the kernel for many rows, two sets of 128.
 constexpr int kTcMaxCols = 144, kRowsMaxCols = 256;
 
-// Whether the tensor-core kernels take a cache of this geometry (strides in bytes).
+// Whether the tensor-core kernels take a cache of this geometry (strides in bytes),
+// and whether they take any of this dimension and type.
+inline bool attend_tc_may_serve(int D, int dtype) { return dtype == SPEC_BF16 && (D == 64 || D == 128); }
 bool attend_tc_serves(int D, int dtype, int page_size, int64_t head_b, int64_t token_b, int64_t page_b);
 
 // Positions of one of their loads: the largest power of two that divides the page
