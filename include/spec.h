@@ -558,10 +558,14 @@ typedef struct spec_cache {
  *         (window == 0, or t > P - window, or t < sinks);
  *   out = sum_t exp(x_t - m) v_t / sum_t exp(x_t - m),  m = max_t x_t;
  *   lse = m + ln sum_t exp(x_t - m).
- * A row that sees no position (P < 0: pos_base = -1 marks an idle request of
- * a captured graph) gets out = 0 and lse = -inf.  The row's own key and value
- * are read from the cache (spec_cache_append comes first).  Keys and values
- * of invisible positions do not reach the result, whatever they hold.
+ * A row that sees no position (P < 0) gets out = 0 and lse = -inf.  So a
+ * request is idle, as a captured graph may need it, if all of its rows lie
+ * before position 0: pos_base + n_i < 0, which -(K + 1) gives whatever n_i is,
+ * and -1 only where n_i = 0.  spec_cache_append and spec_cache_reserve skip
+ * such rows likewise.
+ * The row's own key and value are read from the cache (spec_cache_append comes
+ * first).  Keys and values of invisible positions do not reach the result,
+ * whatever they hold.
  * Sums are held in fp32; with a bf16 cache of head_dim 64 or 128 the products
  * run on the tensor cores, with each weight exp(x - m) as a sum of two bf16
  * numbers (2^-17 relative) in the second one.

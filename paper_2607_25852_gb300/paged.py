@@ -15,6 +15,9 @@ from ``spec_allocate``):
     spec_verify(...); spec_commit(...)
     cache.commit(pos_base, accepted_len)                  # rejected drafts' pages go back
 
+A request idles in a round, with no page, no key and outputs of 0, if all of its
+rows lie before position 0: at pos_base = -(drafts + 1) whatever its depth.
+
 ``cache.fork`` shares pages between requests (parallel samples, beams),
 ``cache.compact`` moves the live pages to the low end, and
 ``cache.commit(pos_base)`` with 0 gives a finished request's pages back.
