@@ -565,10 +565,12 @@ typedef struct spec_cache {
  * such rows likewise.
  * The row's own key and value are read from the cache (spec_cache_append comes
  * first).  Keys and values of invisible positions do not reach the result,
- * whatever they hold.
+ * whatever they hold.  A visible key that is NaN makes the rows that see it NaN;
+ * a visible value that is not finite makes its element of them not finite
+ * (infinite or NaN), unless its weight underflows.
  * Sums are held in fp32; with a bf16 cache of head_dim 64 or 128 the products
  * run on the tensor cores, with each weight exp(x - m) as a sum of two bf16
- * numbers (2^-17 relative) in the second one.
+ * numbers (2^-16 relative) in the second one.
  * The result does not depend on the run: partial results of a request that
  * is split over CTAs are joined in a fixed order.
  * Arguments

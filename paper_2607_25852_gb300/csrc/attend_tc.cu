@@ -17,7 +17,8 @@
 // warps.
 // The sum of the weights is kept per thread, in fp32, and reduced once per
 // item.  For the second product a weight is the sum of two bf16 numbers, its
-// upper 8 bits and the rounded rest (2^-17 relative): one bf16 number would
+// upper 8 bits and the rounded rest (2^-16 relative: the rest is below 2^-7 of it,
+// and keeps 8 bits): one bf16 number would
 // put an error of the size of the result's own rounding on top of it.  The two
 // are columns of one product of twice the width, whose two results the item's
 // end adds: a product of 128 rows and 16 steps costs 65 cycles up to N = 32 and
