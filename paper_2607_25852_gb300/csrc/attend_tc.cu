@@ -37,13 +37,14 @@
 // (a value that some rows see and others do not is added back, row by row, in
 // the item's epilogue: only if it is not finite).
 //
-// Every mbarrier wait is bounded (about a second): a wait that gives up sets
-// SPEC_ERR_TIMEOUT and the kernel ends; the softmax warps, which meet at
-// barriers, leave together by a vote.
+// Every mbarrier wait is bounded (about a second; what a segment's end gives back,
+// a second in which no tile was loaded): a wait that gives up sets SPEC_ERR_TIMEOUT
+// and the kernel ends; the softmax warps, which meet at barriers, leave together by
+// a vote and arrive for the parts that the CTA leaves out.
 //
 // What it measures, 64 requests of 64 query heads over 8, D = 128, 4,096
-// positions each: 1 row 166 us (6.5 TB/s, 0.95 of the measured copy peak), 4 rows
-// 170, 8 rows 181, 12 rows 192 (5.6 TB/s), 17 rows 250 us (4.3 TB/s).  Up to 12
+// positions each: 1 row 167 us (6.4 TB/s, 0.95 of the measured copy peak), 4 rows
+// 171, 8 rows 184, 12 rows 195 (5.5 TB/s), 17 rows 249 us (4.3 TB/s).  Up to 12
 // rows HBM bounds it; at 17 the chain from scores to weights to output: a tile
 // takes 2.1 us where its bytes take 1.5, shared memory is 76 % busy (the MMAs'
 // operands 33, the softmax 31, arriving tiles 12) and two softmax warps per
@@ -665,7 +666,7 @@ int attend_tc_columns(int cols) {
 // in the variants of 16 / 32 / 96 / 144 columns: a token, D = 128: 166 / 165 / 168 /
 // 213; D = 64: 94 / 122 / 151 / 194; 8 rows, D = 128: - / - / 181 / 224.  17 rows (136
 // columns): 250 here, 328 in the kernel for many rows, whose second set holds 8
-// columns; 21 rows: 362 here as two items of 84, 323 there.
+// columns; 21 rows: 362 here as two items of 84, 305 there.
 cudaError_t launch_attend_tc(const AttendLaunch& a, cudaStream_t stream) {
   if (a.ct > kTcMaxCols) return launch_attend_rows(a, stream);
   if (a.ct <= 16) return a.D == 64 ? launch_variant<64, 2, 1>(a, stream) : launch_variant<128, 2, 1>(a, stream);

@@ -566,7 +566,7 @@ __device__ __forceinline__ void remap_entry(const CompactLaunch& p, long long x,
 
 // One cluster of 8 CTAs: count the live pages (n), rank those at or past n and
 // the holes below n, pair them by rank, move the counts, then rewrite the tables
-// (large ones in remap_kernel).  5.2 us (509 pages), 7.5 us (32,768 pages, 96 tables
+// (large ones in remap_kernel).  5.0 us (509 pages), 7.2 us (32,768 pages, 96 tables
 // of 384 slots); barriers and round trips bound it.
 __global__ void __cluster_dims__(kPageCluster, 1, 1) __launch_bounds__(kPageThreads)
     compact_kernel(const CompactLaunch p) {
