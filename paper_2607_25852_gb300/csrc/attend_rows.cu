@@ -327,6 +327,7 @@ __global__ void __launch_bounds__((4 + 4 * kSets) * 32, 1)
             wait(&ctl.full[vp.slot], vp.use);
             hide_values<D>(smem + vp.slot * kSlotBytes, tl, any, all, &poison);
             proxy_fence();
+            __syncwarp();
           }
         }
         vp.step(2, t.slots);
@@ -358,6 +359,7 @@ __global__ void __launch_bounds__((4 + 4 * kSets) * 32, 1)
 #pragma unroll 1
       for (int d = 0; active && d < D; d += 32) {
         float o[32];
+        __syncwarp();  // lanes without a column have skipped the last round's rest
         tmem_ld32(my_o + d, o);
         if (!real) continue;
         if (poisoned) {
@@ -384,8 +386,8 @@ __global__ void __launch_bounds__((4 + 4 * kSets) * 32, 1)
             part[(size_t)k * a.ct] = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
         }
       }
-      tc_fence_before();
       __syncwarp();
+      tc_fence_before();
       if (lane == 0 && active) mbar_arrive(&o_free[h]);
       if (!whole) {
         named_sync(1, kSoftThreads);

@@ -483,6 +483,7 @@ __global__ void __launch_bounds__((4 + 4 * H) * 32, two_per_sm(D, CG) ? 2 : 1)
             for (int j = 0; j < 16; ++j)
               if (j < nc && row_sees(a, rows[j], pos)) o[j] += add;
           });
+          __syncwarp();
         }
         if (whole) {
           __nv_bfloat16* row = staged + g * 8 * D + tl;
