@@ -21,6 +21,11 @@
  *   spec_markov_draft
  *                  the Markov head's sequential draw over a block (Section
  *                  3.2): a tensor-core contraction per position.
+ *   spec_attend, spec_cache_*, spec_rotary*
+ *                  the target's attention over a paged cache, the cache's pages,
+ *                  and rotary positions on the way into it.
+ *   spec_linear_*  linear attention with decays over a state per request.
+ *   spec_logprobs  log probabilities, ranks, entropy and alternatives of tokens.
  *   spec_graph_*, spec_select_round
  *                  a round per candidate budget as CUDA graphs, the budget
  *                  chosen on the device (Section 4.3).
@@ -726,6 +731,197 @@ int spec_cache_release(int32_t* page_table, int32_t* page_refs, const int64_t* p
 int spec_cache_compact(int32_t* page_table, int32_t* page_refs, int B, int max_pages, int pages,
                        int32_t* move_src_out, int32_t* move_dst_out, int32_t* page_map_out,
                        int32_t* counts_out, int32_t* status, cudaStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Rotary positions -- what stands between the target's projections and the
+ * paged cache.  Element pair d = 0 .. rotary_dim / 2 - 1 of a head, (a, b), in a
+ * row at position P = pos_base[i] + j becomes
+ *   amplitude * (a cos t - b sin t, b cos t + a sin t),  t = P frequencies[d].
+ * Pair d is elements (2 d, 2 d + 1) with `interleaved`, else (d, d + rotary_dim / 2);
+ * elements from rotary_dim on stay as they are.  The angle is exact to 2^-53 of
+ * itself before it is reduced to a turn, and rounded to fp32 after; results are
+ * rounded once.  Negated frequencies turn back.
+ *
+ * spec_rotary_frequencies -- the table for a base and a scaling.  Host only.
+ *   SPEC_ROTARY_PLAIN  f_d = base^(-2 d / rotary_dim)
+ *   SPEC_ROTARY_LINEAR f_d / factor: positions interpolated
+ *   SPEC_ROTARY_BASE   base * factor^(rotary_dim / (rotary_dim - 2)) for base: the
+ *                      slowest pair by the factor, the fastest not at all
+ *   SPEC_ROTARY_RAMP   with n = original_positions f_d / 2 pi turns over the trained
+ *                      length and w = clamp((n - low) / (high - low), 0, 1):
+ *                      w f_d + (1 - w) f_d / factor
+ *   factor >= 1 (not read without a scaling); original_positions, low and high
+ *   (0 < low < high) are read by SPEC_ROTARY_RAMP alone.
+ *   out             host fp64 [rotary_dim / 2].
+ * ---------------------------------------------------------------------- */
+#define SPEC_ROTARY_PLAIN 0
+#define SPEC_ROTARY_LINEAR 1
+#define SPEC_ROTARY_BASE 2
+#define SPEC_ROTARY_RAMP 3
+int spec_rotary_frequencies(int rotary_dim, double base, int scaling, double factor,
+                            int64_t original_positions, double low, double high, double* out);
+
+/* spec_rotary -- rows turned, with no cache.
+ *   x               device [R, heads, head_dim] of dtype, rows x_row_stride
+ *                   elements apart (a multiple of 16 bytes, 16-byte aligned;
+ *                   head_dim a multiple of 16 bytes): queries, or the queries and
+ *                   keys of a fused projection at once.
+ *   frequencies     device fp64 [rotary_dim / 2], radians per position; one that
+ *                   is not finite counts as 0 and sets SPEC_ERR_BAD_INPUT.
+ *   rotary_dim      even, 2 .. head_dim.  amplitude: finite.
+ *   row_offsets, depth, pos_base  as spec_attend.  A row before position 0 is
+ *                   skipped (not written); rows of inconsistent offsets or depths
+ *                   too, with SPEC_ERR_BAD_INPUT.
+ *   out             as x; may be x itself with the same stride (in place), else
+ *                   they do not overlap. */
+int spec_rotary(const void* x, int64_t x_row_stride, int heads, int head_dim, int dtype,
+                const double* frequencies, int rotary_dim, int interleaved, float amplitude,
+                const int32_t* row_offsets, const int32_t* depth, const int64_t* pos_base, int B,
+                int K, void* out, int64_t out_row_stride, int32_t* status, cudaStream_t stream);
+
+/* spec_rotary_append -- spec_rotary of the rows' queries and keys and
+ * spec_cache_append of the keys and values, in one pass: turned queries to q_out,
+ * turned keys and the values as they are to their pages.
+ *   q, q_out        as x and out of spec_rotary, of cache->dtype; both NULL with
+ *                   q_heads = 0 (keys and values alone).
+ *   k_new, v_new, page_table and what is skipped: as spec_cache_append.  The
+ *                   queries of a row whose key has no page are turned all the same. */
+int spec_rotary_append(const spec_cache* cache, int layer, const void* q, int64_t q_row_stride,
+                       int q_heads, const void* k_new, int64_t k_row_stride, const void* v_new,
+                       int64_t v_row_stride, const double* frequencies, int rotary_dim,
+                       int interleaved, float amplitude, const int32_t* row_offsets,
+                       const int32_t* depth, const int64_t* pos_base, const int32_t* page_table,
+                       int max_pages, int B, int K, void* q_out, int64_t q_out_row_stride,
+                       int32_t* status, cudaStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Linear attention with a decay per head, for the layers of a target that keep
+ * a state per request in place of keys and values.  For key-value head h with
+ * state S [key_dim, value_dim] and row j's decay l = exp(log_decay):
+ *   S_j = l_j S_{j-1} + k_j v_j^T,   out_j = scale q_j S_j
+ * (query head g reads the state of head g / (q_heads / kv_heads)).
+ *
+ * States.  fp32; element (layer l, slot s, head h, a, b) lies at
+ *   state + l * layer_stride + s * slot_stride + (h * key_dim + a) * value_dim + b
+ * (strides in elements, multiples of 4; state 16-byte aligned).  Request i starts
+ * from slot slots_in[i] (-1: from zeros) and its new state goes to slot
+ * slots_out[i] (-1: nowhere).  The two may be the same; several requests may start
+ * from one slot (parallel samples of a prompt).  No request's slots_out may be
+ * another's slots_in or slots_out in the same call.
+ * ---------------------------------------------------------------------- */
+typedef struct spec_states {
+  float* state;          /* device */
+  int32_t layers;        /* >= 1 */
+  int32_t slots;         /* >= 1 */
+  int32_t kv_heads;      /* >= 1 */
+  int32_t key_dim;       /* <= SPEC_MAX_HEAD_DIM */
+  int32_t value_dim;     /* <= SPEC_MAX_HEAD_DIM */
+  int64_t layer_stride, slot_stride;
+} spec_states;
+
+#define SPEC_MAX_LINEAR_ROWS (1 << 20) /* rows of a request in one call */
+
+/* ------------------------------------------------------------------------
+ * spec_linear_attend -- outputs of the packed rows, and with slots_out the
+ * states after them (a single token; a prompt of any length up to
+ * SPEC_MAX_LINEAR_ROWS).  A verification passes slots_out = NULL: the states stay
+ * until spec_verify has said which rows count, and spec_linear_commit takes those.
+ *   q               device [R, q_heads, key_dim] of dtype; k [R, kv_heads,
+ *                   key_dim]; v [R, kv_heads, value_dim]; rows q_row_stride,
+ *                   k_row_stride, v_row_stride elements apart (multiples of 16
+ *                   bytes, 16-byte aligned; key_dim and value_dim multiples of 16
+ *                   bytes): views of a fused projection will do.
+ *   log_decay       device fp32, row r's of head h at [r * decay_row_stride + h];
+ *                   decay_row_stride 0: one per head.  At most 0; -inf forgets
+ *                   everything before the row.  A value above 0 or NaN counts as 0
+ *                   and sets SPEC_ERR_BAD_INPUT.
+ *   slots_in        device int32 [B]; slots_out device int32 [B] or NULL.
+ *   row_offsets, depth  as spec_attend, with K up to SPEC_MAX_LINEAR_ROWS - 1.
+ *   pos_base        device int64 [B] or NULL (all rows count): rows before
+ *                   position 0 give out = 0 and change no state, so that a
+ *                   request idles at -(K + 1) as in spec_attend (its state goes
+ *                   from slots_in to slots_out as it is).
+ *   scale           finite.
+ *   out             device [R, q_heads, value_dim] of dtype, 16-byte aligned;
+ *                   rows that belong to no request are not written.
+ *   status          a slot out of range, inconsistent offsets or depths: nothing
+ *                   of that request is written and SPEC_ERR_BAD_INPUT is set.
+ *                   SPEC_ERR_TIMEOUT as spec_attend.
+ *   ws, ws_bytes    spec_linear_workspace(...) bytes, 256-byte aligned; no zeroing
+ *                   needed.  Calls that may overlap need separate ones.
+ * Sums and states are fp32.  With bf16 rows of key_dim and value_dim 64 or 128
+ * long calls run on the tensor cores, with the scores and the state as sums of two
+ * bf16 numbers (2^-16 relative) in the products that give out, and the weighted
+ * values as sums of three (2^-24) in those that make the state.
+ * The result does not depend on the run.  A key or value that is not finite makes
+ * its own and later rows' outputs and the state not finite where it enters them;
+ * earlier rows are not touched.
+ * Limits: 1 <= B, B (K + 1) <= 2^28, q_heads a multiple of kv_heads and at most
+ * SPEC_MAX_GROUP times it.
+ * ---------------------------------------------------------------------- */
+size_t spec_linear_workspace(int B, int K, int q_heads, int kv_heads, int key_dim, int value_dim,
+                             int dtype);
+int spec_linear_attend(const void* q, int64_t q_row_stride, int q_heads, const void* k,
+                       int64_t k_row_stride, const void* v, int64_t v_row_stride, int dtype,
+                       const float* log_decay, int64_t decay_row_stride, const spec_states* states,
+                       int layer, const int32_t* slots_in, const int32_t* slots_out,
+                       const int32_t* row_offsets, const int32_t* depth, const int64_t* pos_base,
+                       int B, int K, float scale, void* out, int32_t* status, void* ws,
+                       size_t ws_bytes, cudaStream_t stream);
+
+/* spec_linear_commit -- the states after the accepted rows: of request i's rows
+ * the first accepted_len[i] + 1 (accepted_len from spec_verify; NULL: all) enter the
+ * state of slots_in[i], which goes to slots_out[i].  Arguments as spec_linear_attend
+ * (slots_out required), with the rows' keys, values and decays as they were there.
+ * An accepted length outside [0, depth] sets SPEC_ERR_BAD_INPUT; that request's
+ * state is not written.
+ *   ws              spec_linear_workspace(...) bytes, for any q_heads. */
+int spec_linear_commit(const void* k, int64_t k_row_stride, const void* v, int64_t v_row_stride,
+                       int dtype, const float* log_decay, int64_t decay_row_stride,
+                       const spec_states* states, int layer, const int32_t* slots_in,
+                       const int32_t* slots_out, const int32_t* accepted_len,
+                       const int32_t* row_offsets, const int32_t* depth, const int64_t* pos_base,
+                       int B, int K, int32_t* status, void* ws, size_t ws_bytes,
+                       cudaStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * spec_logprobs -- what a serving interface reports beside the committed tokens
+ * (and for a prompt's): for row j of request i, j <= accepted_len[i], with
+ * p = softmax(l_j / t') (t' = temperature, or 1 when it is 0) and the token
+ * x = tokens[i][j]:
+ *   logprob = ln p(x); rank = 1 + the number of entries before x (a greater logit,
+ *   or an equal one at a lower index); entropy = -sum_v p_v ln p_v; and the top_n
+ *   entries of largest logit above -inf, in that order, with their ln p.
+ * Row j is the one that spec_verify's out_tokens[i][j] was drawn from or verified
+ * on, so its arrays serve as they are.
+ *   logits, row_offsets, depth  as spec_verify (logits device or host-mapped).
+ *   tokens          device int32 [B, K+1]; -1: no token (logprob -inf, rank 0).
+ *                   Another value outside [0, V) counts as -1 and sets
+ *                   SPEC_ERR_BAD_INPUT.
+ *   accepted_len    device int32 [B], or NULL: every row.  Outside [0, depth], or
+ *                   with inconsistent offsets or depths: SPEC_ERR_BAD_INPUT, and the
+ *                   request's rows count as not asked for.
+ *   top_n           0 .. SPEC_MAX_TOP.
+ *   logprob_out     device fp32 [B, K+1]; rank_out device int32 [B, K+1] or NULL;
+ *   entropy_out     device fp32 [B, K+1] or NULL.
+ *   top_tokens_out  device int32 [B, K+1, top_n], top_logprobs_out device fp32 of
+ *                   that shape; one may be NULL, both where top_n = 0.  Past the
+ *                   entries above -inf: -1 and -inf.
+ *   Rows not asked for get logprob -inf, rank 0, entropy 0, tokens -1; a row with a
+ *   NaN, a +inf or no finite logit too, with SPEC_ERR_BAD_INPUT.
+ *   ws, ws_bytes    spec_logprobs_workspace(B, K, V, top_n) bytes, 256-byte aligned,
+ *                   zero-filled once before its first use and left ready for the
+ *                   next call of these sizes.  Calls that may overlap, and other
+ *                   sizes, need separate ones.
+ * ---------------------------------------------------------------------- */
+#define SPEC_MAX_TOP 32
+size_t spec_logprobs_workspace(int B, int K, int V, int top_n);
+int spec_logprobs(const void* logits, int logits_dtype, const int32_t* row_offsets,
+                  const int32_t* depth, const int32_t* tokens, const int32_t* accepted_len, int B,
+                  int K, int V, float temperature, int top_n, float* logprob_out,
+                  int32_t* rank_out, float* entropy_out, int32_t* top_tokens_out,
+                  float* top_logprobs_out, int32_t* status, void* ws, size_t ws_bytes,
+                  cudaStream_t stream);
 
 /* ------------------------------------------------------------------------
  * spec_profile_stream_pass -- measurement aid.  The next spec_verify call

@@ -32,6 +32,10 @@ MAX_ALLOC_POSITIONS = 8192
 MAX_CANDIDATES = 64
 MAX_HEAD_DIM = 256
 MAX_GROUP = 64
+MAX_LINEAR_ROWS = 1 << 20
+MAX_TOP = 32
+
+ROTARY_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "ramp": 3}
 
 SHARD_STAT_BYTES = 32
 SHARD_DECISION_BYTES = 32
@@ -48,6 +52,8 @@ __all__ = [
     "spec_pointer_device_readable", "spec_check_bounded_wait", "spec_attend_workspace", "spec_attend",
     "attend_workspace", "spec_cache_append", "spec_cache_fork", "spec_cache_workspace", "cache_workspace",
     "spec_cache_reserve", "spec_cache_copy", "spec_cache_release", "spec_cache_compact",
+    "spec_rotary_frequencies", "spec_rotary", "spec_rotary_append", "spec_linear_workspace", "linear_workspace",
+    "spec_linear_attend", "spec_linear_commit", "spec_logprobs_workspace", "logprobs_workspace", "spec_logprobs",
 ]
 
 
@@ -537,6 +543,235 @@ def spec_cache_compact(page_table, page_refs, move_src_out, move_dst_out, page_m
         _ints(counts_out, 2, "counts_out"), _ints(status, 1, "status"), _stream_handle(stream))
     if code:
         raise SpecError(code, "spec_cache_compact")
+
+
+# ---------------------------------------------------------------------------
+# Rotary positions, linear attention, log probabilities
+# ---------------------------------------------------------------------------
+def _here(*tensors):
+    """Refuses tensors that the kernels could not read: all are on the current CUDA device."""
+    dev = torch.cuda.current_device() if tensors[0].is_cuda else -1
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.get_device() != dev):
+            raise ValueError("expected tensors on the current CUDA device")
+
+
+def _enough(t, n, what):
+    if t.shape[0] < n:
+        raise ValueError(f"{what}: rows for every request")
+
+
+def _floats(t, n, what, dtype=torch.float32):
+    """Pointer of a contiguous tensor of at least n entries (or of None)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() < n or not t.is_contiguous():
+        raise ValueError(f"{what}: expected contiguous {dtype} with at least {n} entries")
+    return t.data_ptr()
+
+
+def spec_rotary_frequencies(rotary_dim: int, base=10000.0, scaling="plain", factor=1.0, original_positions=0, low=1.0,
+                            high=32.0, device="cuda"):
+    """The frequencies (fp64 [rotary_dim / 2]) of a base and a scaling: "plain", "linear" (positions interpolated),
+    "base" (a larger base) or "ramp" (slow pairs interpolated, fast ones not); see spec.h."""
+    if scaling not in ROTARY_SCALINGS:
+        raise ValueError(f"scaling: one of {', '.join(ROTARY_SCALINGS)}")
+    out = (ctypes.c_double * max(1, rotary_dim // 2))()
+    _check(library().spec_rotary_frequencies(rotary_dim, base, ROTARY_SCALINGS[scaling], factor, original_positions,
+                                             low, high, out), "spec_rotary_frequencies")
+    return torch.tensor(list(out), dtype=torch.float64, device=device)
+
+
+def spec_rotary(x, frequencies, pos_base, B, K, out, interleaved=False, amplitude=1.0, row_offsets=None, depth=None,
+                status=None, stream=None):
+    """x [R, heads, head_dim] turned by its rows' positions into out (may be x itself); frequencies fp64
+    [rotary_dim / 2]; see spec.h."""
+    if x.dim() != 3 or out.shape != x.shape:
+        raise ValueError("x, out: expected [rows, heads, head_dim], the same shape")
+    _, heads, D = x.shape
+    x_ptr, x_row = _rows(x, heads, D, x.dtype, "x")
+    out_ptr, out_row = _rows(out, heads, D, x.dtype, "out")
+    if row_offsets is None:
+        _enough(x, B * (K + 1), "x")
+    freq = _floats(frequencies, 1, "frequencies", torch.float64)
+    offsets, depths = _ints(row_offsets, B + 1, "row_offsets"), _ints(depth, B, "depth")
+    pos, st, dtype = _ints(pos_base, B, "pos_base", torch.int64), _ints(status, 1, "status"), _dtype(x)
+    _here(x, out, frequencies, pos_base, row_offsets, depth, status)
+    code = library().spec_rotary(x_ptr, x_row, heads, D, dtype, freq, 2 * frequencies.numel(), interleaved, amplitude,
+                                 offsets, depths, pos, B, K, out_ptr, out_row, st, _stream_handle(stream))
+    if code:
+        raise SpecError(code, "spec_rotary")
+
+
+def spec_rotary_append(q, k_new, v_new, k_cache, v_cache, page_table, pos_base, B, K, frequencies, q_out,
+                       interleaved=False, amplitude=1.0, row_offsets=None, depth=None, layer=0, status=None,
+                       stream=None):
+    """q [R, q_heads, head_dim] turned into q_out (may be q itself; both None: keys and values alone), k_new turned and
+    v_new as it is [R, kv_heads, head_dim] into their pages; see spec.h."""
+    cache = _cache(k_cache, v_cache)
+    (H, D), dtype = k_cache.shape[-2:], k_cache.dtype
+    k_ptr, k_row = _rows(k_new, H, D, dtype, "k_new")
+    v_ptr, v_row = _rows(v_new, H, D, dtype, "v_new")
+    if (q is None) != (q_out is None):
+        raise ValueError("q, q_out: both or neither")
+    Hq, q_ptr, q_row, out_ptr, out_row = 0, None, 0, None, 0
+    if q is not None:
+        if q.dim() != 3 or q_out.shape != q.shape:
+            raise ValueError("q, q_out: expected [rows, q_heads, head_dim], the same shape")
+        Hq = q.shape[1]
+        q_ptr, q_row = _rows(q, Hq, D, dtype, "q")
+        out_ptr, out_row = _rows(q_out, Hq, D, dtype, "q_out")
+    if row_offsets is None:
+        for t, what in ((k_new, "k_new"), (v_new, "v_new"), (k_new if q is None else q, "q")):
+            _enough(t, B * (K + 1), what)
+    table, max_pages = _table(page_table, B)
+    freq = _floats(frequencies, 1, "frequencies", torch.float64)
+    offsets, depths = _ints(row_offsets, B + 1, "row_offsets"), _ints(depth, B, "depth")
+    pos, st = _ints(pos_base, B, "pos_base", torch.int64), _ints(status, 1, "status")
+    _here(k_new, v_new, q, q_out, k_cache, v_cache, page_table, frequencies, pos_base, row_offsets, depth, status)
+    code = library().spec_rotary_append(
+        cache, _int(layer), q_ptr, q_row, Hq, k_ptr, k_row, v_ptr, v_row, freq, 2 * frequencies.numel(), interleaved,
+        amplitude, offsets, depths, pos, table, max_pages, B, K, out_ptr, out_row, st, _stream_handle(stream))
+    if code:
+        raise SpecError(code, "spec_rotary_append")
+
+
+def spec_linear_workspace(B: int, K: int, q_heads: int, kv_heads: int, key_dim: int, value_dim: int,
+                          dtype=torch.bfloat16) -> int:
+    return library().spec_linear_workspace(B, K, q_heads, kv_heads, key_dim, value_dim,
+                                           F32 if dtype == torch.float32 else BF16)
+
+
+def linear_workspace(B: int, K: int, q_heads: int, kv_heads: int, key_dim: int, value_dim: int, dtype=torch.bfloat16,
+                     device="cuda"):
+    """A workspace for spec_linear_attend and spec_linear_commit."""
+    n = spec_linear_workspace(B, K, q_heads, kv_heads, key_dim, value_dim, dtype)
+    if n == 0:
+        raise SpecError(ERR_INVALID_ARG, "spec_linear_workspace")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _states(states):
+    """struct spec_states (its bytes) of a tensor [layers, slots, kv_heads, key_dim, value_dim] (or one layer's)."""
+    shape, stride = states.shape, states.stride()
+    if states.dtype != torch.float32 or len(shape) not in (4, 5):
+        raise ValueError("states: expected fp32 [layers, slots, kv_heads, key_dim, value_dim]")
+    H, Dk, Dv = shape[-3:]
+    if (Dv > 1 and stride[-1] != 1) or (Dk > 1 and stride[-2] != Dv) or (H > 1 and stride[-3] != Dk * Dv):
+        raise ValueError("states: a slot's states must be contiguous")
+    if len(shape) == 4:
+        return _native.pack_states(states.data_ptr(), 1, *shape, 0, stride[0])
+    return _native.pack_states(states.data_ptr(), *shape, *stride[:2])
+
+
+def _decay(log_decay, H, rows):
+    """Pointer and row stride of log decays [R, kv_heads], or [kv_heads] for all rows."""
+    shape, stride = log_decay.shape, log_decay.stride()
+    if log_decay.dtype != torch.float32 or len(shape) not in (1, 2) or shape[-1] != H or (H > 1 and stride[-1] != 1):
+        raise ValueError(f"log_decay: expected fp32 [rows, {H}] or [{H}]")
+    if len(shape) == 1:
+        return log_decay.data_ptr(), 0
+    if shape[0] < rows:
+        raise ValueError("log_decay: rows for every request")
+    return log_decay.data_ptr(), stride[0] if shape[0] > 1 else H
+
+
+def spec_linear_attend(q, k, v, log_decay, states, slots_in, slots_out, B, K, out, ws, row_offsets=None, depth=None,
+                       pos_base=None, scale=None, layer=0, status=None, stream=None):
+    """q [R, q_heads, key_dim], k [R, kv_heads, key_dim], v [R, kv_heads, value_dim], log_decay fp32 [R, kv_heads] or
+    [kv_heads]; states fp32 [layers, slots, kv_heads, key_dim, value_dim] (or one layer, 4 dimensions); slots_out None
+    leaves the states as they are; out [R, q_heads, value_dim]; scale 1 / sqrt(key_dim) if None; see spec.h."""
+    packed = _states(states)
+    H, Dk, Dv = states.shape[-3:]
+    if q.dim() != 3:
+        raise ValueError("q: expected [rows, q_heads, key_dim]")
+    Hq, dtype = q.shape[1], q.dtype
+    q_ptr, q_row = _rows(q, Hq, Dk, dtype, "q")
+    k_ptr, k_row = _rows(k, H, Dk, dtype, "k")
+    v_ptr, v_row = _rows(v, H, Dv, dtype, "v")
+    if out.shape != (q.shape[0], Hq, Dv) or out.dtype != dtype or not out.is_contiguous():
+        raise ValueError("out: expected q's rows and dtype, [rows, q_heads, value_dim], contiguous")
+    rows = q.shape[0] if row_offsets is not None else B * (K + 1)
+    for t, what in ((q, "q"), (k, "k"), (v, "v")):
+        _enough(t, rows, what)
+    g_ptr, g_row = _decay(log_decay, H, rows)
+    offsets, depths = _ints(row_offsets, B + 1, "row_offsets"), _ints(depth, B, "depth")
+    pos, st = _ints(pos_base, B, "pos_base", torch.int64), _ints(status, 1, "status")
+    s_in, s_out, kind = _ints(slots_in, B, "slots_in"), _ints(slots_out, B, "slots_out"), _dtype(q)
+    _here(q, k, v, log_decay, states, slots_in, slots_out, out, ws, row_offsets, depth, pos_base, status)
+    code = library().spec_linear_attend(
+        q_ptr, q_row, Hq, k_ptr, k_row, v_ptr, v_row, kind, g_ptr, g_row, packed, _int(layer), s_in, s_out, offsets,
+        depths, pos, B, K, Dk ** -0.5 if scale is None else scale, out.data_ptr(), st, ws.data_ptr(), ws.nbytes,
+        _stream_handle(stream))
+    if code:
+        raise SpecError(code, "spec_linear_attend")
+
+
+def spec_linear_commit(k, v, log_decay, states, slots_in, slots_out, accepted_len, B, K, ws, row_offsets=None,
+                       depth=None, pos_base=None, layer=0, status=None, stream=None):
+    """The first accepted_len + 1 rows (all with None) into the states; arguments as spec_linear_attend's."""
+    packed = _states(states)
+    H, Dk, Dv = states.shape[-3:]
+    dtype = k.dtype
+    k_ptr, k_row = _rows(k, H, Dk, dtype, "k")
+    v_ptr, v_row = _rows(v, H, Dv, dtype, "v")
+    rows = k.shape[0] if row_offsets is not None else B * (K + 1)
+    for t, what in ((k, "k"), (v, "v")):
+        _enough(t, rows, what)
+    g_ptr, g_row = _decay(log_decay, H, rows)
+    offsets, depths = _ints(row_offsets, B + 1, "row_offsets"), _ints(depth, B, "depth")
+    pos, st = _ints(pos_base, B, "pos_base", torch.int64), _ints(status, 1, "status")
+    s_in, s_out, kind = _ints(slots_in, B, "slots_in"), _ints(slots_out, B, "slots_out"), _dtype(k)
+    accepted = _ints(accepted_len, B, "accepted_len")
+    _here(k, v, log_decay, states, slots_in, slots_out, accepted_len, ws, row_offsets, depth, pos_base, status)
+    code = library().spec_linear_commit(
+        k_ptr, k_row, v_ptr, v_row, kind, g_ptr, g_row, packed, _int(layer), s_in, s_out, accepted, offsets, depths, pos,
+        B, K, st, ws.data_ptr(), ws.nbytes, _stream_handle(stream))
+    if code:
+        raise SpecError(code, "spec_linear_commit")
+
+
+def spec_logprobs_workspace(B: int, K: int, V: int, top_n: int) -> int:
+    return library().spec_logprobs_workspace(B, K, V, top_n)
+
+
+def logprobs_workspace(B: int, K: int, V: int, top_n: int, device="cuda"):
+    """A zero-filled workspace for spec_logprobs."""
+    n = spec_logprobs_workspace(B, K, V, top_n)
+    if n == 0:
+        raise SpecError(ERR_INVALID_ARG, "spec_logprobs_workspace")
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+def spec_logprobs(logits, tokens, B, K, V, logprob_out, ws, temperature=1.0, row_offsets=None, depth=None,
+                  accepted_len=None, rank_out=None, entropy_out=None, top_tokens_out=None, top_logprobs_out=None,
+                  status=None, stream=None):
+    """logits [R, V]; tokens int32 [B, K+1] (spec_verify's out_tokens); logprob_out fp32 [B, K+1]; top_tokens_out and
+    top_logprobs_out [B, K+1, n], either or both; see spec.h."""
+    if logits.dim() != 2 or logits.shape[1] != V or not logits.is_contiguous():
+        raise ValueError(f"logits: expected contiguous [rows, {V}]")
+    n, cells = 0, B * (K + 1)
+    if row_offsets is None:
+        _enough(logits, cells, "logits")
+    for t, what in ((top_tokens_out, "top_tokens_out"), (top_logprobs_out, "top_logprobs_out")):
+        if t is not None:
+            if t.dim() < 2 or (n and t.shape[-1] != n):
+                raise ValueError(f"{what}: expected [B, K+1, n], the same n")
+            n = t.shape[-1]
+    kind = _dtype(logits)
+    given, taken = _ints(tokens, cells, "tokens"), _ints(accepted_len, B, "accepted_len")
+    offsets, depths, st = _ints(row_offsets, B + 1, "row_offsets"), _ints(depth, B, "depth"), _ints(status, 1, "status")
+    lp, rank = _floats(logprob_out, cells, "logprob_out"), _ints(rank_out, cells, "rank_out")
+    entropy = _floats(entropy_out, cells, "entropy_out")
+    top, top_lp = _ints(top_tokens_out, cells * n, "top_tokens_out"), _floats(top_logprobs_out, cells * n,
+                                                                             "top_logprobs_out")
+    _here(tokens, accepted_len, row_offsets, depth, status, logprob_out, rank_out, entropy_out, top_tokens_out,
+          top_logprobs_out, ws)
+    code = library().spec_logprobs(
+        logits.data_ptr(), kind, offsets, depths, given, taken, B, K, V, temperature, n, lp, rank, entropy,
+        top, top_lp, st, ws.data_ptr(), ws.nbytes, _stream_handle(stream))
+    if code:
+        raise SpecError(code, "spec_logprobs")
 
 
 def spec_check_bounded_wait(status):

@@ -54,6 +54,17 @@ SIGNATURES = {
     "spec_attend": (_I, [_P, _L, _I, _P, _I, _P, _P, _P, _P, _I, _I, _I, ctypes.c_float, _I, _I, _P, _P, _P, _P, _SZ,
                          _P]),
     "spec_cache_append": (_I, [_P, _I, _P, _L, _P, _L, _P, _P, _P, _P, _I, _I, _I, _P, _P]),
+    "spec_rotary_frequencies": (_I, [_I, ctypes.c_double, _I, ctypes.c_double, _L, ctypes.c_double, ctypes.c_double, _P]),
+    "spec_rotary": (_I, [_P, _L, _I, _I, _I, _P, _I, _I, ctypes.c_float, _P, _P, _P, _I, _I, _P, _L, _P, _P]),
+    "spec_rotary_append": (_I, [_P, _I, _P, _L, _I, _P, _L, _P, _L, _P, _I, _I, ctypes.c_float, _P, _P, _P, _P, _I, _I,
+                                _I, _P, _L, _P, _P]),
+    "spec_linear_workspace": (_SZ, [_I, _I, _I, _I, _I, _I, _I]),
+    "spec_linear_attend": (_I, [_P, _L, _I, _P, _L, _P, _L, _I, _P, _L, _P, _I, _P, _P, _P, _P, _P, _I, _I,
+                                ctypes.c_float, _P, _P, _P, _SZ, _P]),
+    "spec_linear_commit": (_I, [_P, _L, _P, _L, _I, _P, _L, _P, _I, _P, _P, _P, _P, _P, _P, _I, _I, _P, _P, _SZ, _P]),
+    "spec_logprobs_workspace": (_SZ, [_I, _I, _I, _I]),
+    "spec_logprobs": (_I, [_P, _I, _P, _P, _P, _P, _I, _I, _I, ctypes.c_float, _I, _P, _P, _P, _P, _P, _P, _P, _SZ,
+                           _P]),
     "spec_cache_fork": (_I, [_P, _P, _P, _I, _I, _I, _I, _P, _P, _P, _P]),
     "spec_cache_workspace": (_SZ, [_I, _I, _I]),
     "spec_cache_reserve": (_I, [_P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _P, _P, _P, _P, _P, _P, _SZ, _P]),
@@ -70,8 +81,16 @@ class Cache(ctypes.Structure):
         (n, _L) for n in ("layer_stride", "page_stride", "token_stride", "head_stride")]
 
 
-# The bytes of a Cache from its fields in order: half of what building one takes.
+class States(ctypes.Structure):
+    """struct spec_states of include/spec.h."""
+    _fields_ = [("state", _P)] + [
+        (n, ctypes.c_int32) for n in ("layers", "slots", "kv_heads", "key_dim", "value_dim")] + [
+        (n, _L) for n in ("layer_stride", "slot_stride")]
+
+
+# The bytes of a Cache, and of a States, from its fields in order: half of what building one takes.
 pack_cache = struct.Struct("@PP6i4q").pack
+pack_states = struct.Struct("@P5i2q").pack
 
 
 _lib = None

@@ -1,0 +1,401 @@
+// linear.cu -- linear attention with a decay per head over the requests' states,
+// on the CUDA cores: single tokens, verification rounds, fp32 and odd sizes.
+//
+// For a head with state S [Dk x Dv], row j's decay l_j = exp(g_j):
+//   S_j = l_j S_{j-1} + k_j v_j^T,   o_j = scale q_j S_j.
+// With L_j = g_1 + .. + g_j over a block of rows this is, without a pass over the
+// state per row,
+//   o_i = scale (exp(L_i) q_i S_0 + sum_{j <= i} exp(L_i - L_j) (q_i k_j) v_j)
+//   S_n = exp(L_n) S_0 + sum_j exp(L_n - L_j) k_j v_j^T,
+// two multiply-adds per element of the state and row (one where the states stay).
+//
+// A CTA holds the state of a head, or some of its columns, in registers: 16-byte
+// loads, all in flight together, read once and written once.  Up to a dozen rows
+// that is bound by HBM.
+#include <cmath>
+
+#include <algorithm>
+
+#include "linear.cuh"
+#include "tensor_core.cuh"
+
+namespace spec {
+
+namespace {
+
+constexpr int kLinThreads = 256, kLinWarps = kLinThreads / 32;
+constexpr int kBlockRows = 8;
+
+template <typename T>
+__device__ __forceinline__ void unpack16(const uint4& w, float* f);
+template <>
+__device__ __forceinline__ void unpack16<float>(const uint4& w, float* f) {
+  f[0] = __uint_as_float(w.x), f[1] = __uint_as_float(w.y), f[2] = __uint_as_float(w.z), f[3] = __uint_as_float(w.w);
+}
+template <>
+__device__ __forceinline__ void unpack16<__nv_bfloat16>(const uint4& w, float* f) {
+  f[0] = bf16_lo(w.x), f[1] = bf16_hi(w.x), f[2] = bf16_lo(w.y), f[3] = bf16_hi(w.y);
+  f[4] = bf16_lo(w.z), f[5] = bf16_hi(w.z), f[6] = bf16_lo(w.w), f[7] = bf16_hi(w.w);
+}
+
+// Rows b0 .. b0 + n - 1, elements [0, width) of those at `from`, as floats to [kBlockRows][pitch];
+// rows past n and elements past width are 0.
+template <typename T>
+__device__ __forceinline__ void load_rows(const T* from, int64_t row_stride, int n, int width, int padded, float* to,
+                                          int pitch) {
+  constexpr int W = 16 / (int)sizeof(T);
+  const int vecs = (padded + W - 1) / W;
+  for (int x = threadIdx.x; x < kBlockRows * vecs; x += kLinThreads) {
+    const int r = x / vecs, d = (x - r * vecs) * W;
+    float f[W];
+    if (r < n && d < width) {
+      unpack16<T>(ldg_stream(from + r * row_stride + d), f);
+    } else {
+#pragma unroll
+      for (int y = 0; y < W; ++y) f[y] = 0.0f;
+    }
+#pragma unroll
+    for (int y = 0; y < W; y += 4)
+      *reinterpret_cast<float4*>(to + r * pitch + d + y) = make_float4(f[y], f[y + 1], f[y + 2], f[y + 3]);
+  }
+}
+
+__device__ __forceinline__ void store4(float* to, const float4& x) { *reinterpret_cast<float4*>(to) = x; }
+__device__ __forceinline__ void store4(__nv_bfloat16* to, const float4& x) {
+  const __nv_bfloat162 a = __floats2bfloat162_rn(x.x, x.y), b = __floats2bfloat162_rn(x.z, x.w);
+  *reinterpret_cast<uint2*>(to) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+}
+
+inline __host__ __device__ int key_pitch(int Dk) { return (Dk + 31) / 32 * 32 + 16; }  // rows 16 banks apart
+
+template <int S>
+inline size_t linear_smem(int Dk) {
+  return sizeof(float) * (2 * (size_t)kBlockRows * key_pitch(Dk) + (size_t)kBlockRows * S * (1 + kLinWarps));
+}
+
+// S columns of the state, KR of its rows per thread.
+template <typename T, int S, int KR>
+__global__ void __launch_bounds__(kLinThreads) linear_rows_kernel(const LinearLaunch p, int slices) {
+  constexpr int L = S / 4, KG = kLinThreads / L;  // threads across columns, groups of KR rows
+  extern __shared__ float4 smem4[];
+  __shared__ long long steps[kBlockRows];
+  __shared__ float score[kBlockRows][kBlockRows], weight[kBlockRows], first_weight[kBlockRows], all_weight;
+  const int pitch = key_pitch(p.Dk);
+  float* kb = reinterpret_cast<float*>(smem4);
+  float* qb = kb + kBlockRows * pitch;
+  float* vb = qb + kBlockRows * pitch;
+  float* red = vb + kBlockRows * S;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int i = (int)(blockIdx.x / (unsigned)(p.H * slices)), hs = (int)(blockIdx.x - (unsigned)i * (unsigned)(p.H * slices));
+  const int h = hs / slices, c0 = (hs - h * slices) * S;
+  const int col = (tid % L) * 4, kr0 = (tid / L) * KR;
+  const int columns = min(S, p.Dv - c0);
+  pdl_wait_prerequisites();
+  pdl_launch_dependents();
+  const LinearRequest r = linear_request(p, i);
+  if (!r.ok) {
+    if (hs == 0 && tid == 0) report(p.status, SPEC_ERR_BAD_INPUT);
+    return;
+  }
+  // ---- the state's part ----
+  const bool mine = col < columns;
+  float4 s[KR];
+  const int64_t at = ((int64_t)h * p.Dk + kr0) * p.Dv + c0 + col;
+#pragma unroll
+  for (int x = 0; x < KR; ++x) {
+    s[x] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (r.from >= 0 && mine && kr0 + x < p.Dk)
+      s[x] = *reinterpret_cast<const float4*>(p.state + r.from * p.slot_stride + at + (int64_t)x * p.Dv);
+  }
+  const T* k = static_cast<const T*>(p.k) + (int64_t)h * p.Dk;
+  const T* v = static_cast<const T*>(p.v) + (int64_t)h * p.Dv + c0;
+  T* out = static_cast<T*>(p.out);
+  if (p.q) {  // rows before position 0
+    for (long long x = tid; x < (long long)r.first * p.G * (columns / 4); x += kLinThreads) {
+      const int c = (int)(x % (columns / 4)), y = (int)(x / (columns / 4));
+      store4(out + ((int64_t)(r.row0 + y / p.G) * p.Hq + h * p.G + y % p.G) * p.Dv + c0 + 4 * c,
+             make_float4(0.0f, 0.0f, 0.0f, 0.0f));
+    }
+  }
+
+  for (int b0 = r.first; b0 < r.last; b0 += kBlockRows) {
+    const int n = min(kBlockRows, r.last - b0);
+    const int64_t row = r.row0 + b0;
+    __syncthreads();
+    load_rows<T>(k + row * p.k_row, p.k_row, n, p.Dk, pitch - 16, kb, pitch);
+    load_rows<T>(v + row * p.v_row, p.v_row, n, columns, S, vb, S);
+    if (warp == 0) {
+      long long g = 0;
+      if (lane < n) g = decay_steps(__ldg(p.log_decay + (row + lane) * p.decay_row + h), p.status);
+#pragma unroll
+      for (int o = 1; o < kBlockRows; o <<= 1) {
+        const long long y = __shfl_up_sync(0xFFFFFFFFu, g, o);
+        if (lane >= o) g += y;
+      }
+      const long long all = __shfl_sync(0xFFFFFFFFu, g, kBlockRows - 1);  // rows past n add 0
+      if (lane < kBlockRows) {
+        steps[lane] = g;
+        weight[lane] = exp2f(steps_float(all - g));
+        first_weight[lane] = exp2f(steps_float(g));
+      }
+      if (lane == 0) all_weight = exp2f(steps_float(all));
+    }
+    if (p.q) {
+      for (int g = 0; g < p.G; ++g) {
+        const T* q = static_cast<const T*>(p.q) + row * p.q_row + (int64_t)(h * p.G + g) * p.Dk;
+        if (g) __syncthreads();
+        load_rows<T>(q, p.q_row, n, p.Dk, pitch - 16, qb, pitch);
+        __syncthreads();
+        // ---- exp(L_i - L_j) (q_i k_j): four threads per pair ----
+        {
+          const int pair = tid >> 2, a = pair / kBlockRows, b = pair % kBlockRows;
+          float x = 0.0f;
+          for (int d = (tid & 3) * 4; d < pitch - 16; d += 16) {
+            const float4 y = *reinterpret_cast<const float4*>(qb + a * pitch + d);
+            const float4 z = *reinterpret_cast<const float4*>(kb + b * pitch + d);
+            x = fmaf(y.x, z.x, fmaf(y.y, z.y, fmaf(y.z, z.z, fmaf(y.w, z.w, x))));
+          }
+          x += __shfl_xor_sync(0xFFFFFFFFu, x, 1);
+          x += __shfl_xor_sync(0xFFFFFFFFu, x, 2);
+          if ((tid & 3) == 0) score[a][b] = b <= a ? x * exp2f(steps_float(steps[a] - steps[b])) : 0.0f;
+        }
+        // ---- q_i S_0: this thread's rows of the state, then all ----
+        float4 o[kBlockRows];
+#pragma unroll
+        for (int y = 0; y < kBlockRows; ++y) o[y] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int x = 0; x < KR; x += 4) {
+          if (kr0 + x >= pitch - 16) break;
+#pragma unroll
+          for (int y = 0; y < kBlockRows; ++y) {
+            if (y >= n) break;
+            const float4 z = *reinterpret_cast<const float4*>(qb + y * pitch + kr0 + x);
+            const float f[4] = {z.x, z.y, z.z, z.w};
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+              o[y].x = fmaf(f[t], s[x + t].x, o[y].x);
+              o[y].y = fmaf(f[t], s[x + t].y, o[y].y);
+              o[y].z = fmaf(f[t], s[x + t].z, o[y].z);
+              o[y].w = fmaf(f[t], s[x + t].w, o[y].w);
+            }
+          }
+        }
+#pragma unroll
+        for (int y = 0; y < kBlockRows; ++y) {
+          if (y >= n) break;
+#pragma unroll
+          for (int w = L; w < 32; w <<= 1) {
+            o[y].x += __shfl_xor_sync(0xFFFFFFFFu, o[y].x, w);
+            o[y].y += __shfl_xor_sync(0xFFFFFFFFu, o[y].y, w);
+            o[y].z += __shfl_xor_sync(0xFFFFFFFFu, o[y].z, w);
+            o[y].w += __shfl_xor_sync(0xFFFFFFFFu, o[y].w, w);
+          }
+          if (lane < L) *reinterpret_cast<float4*>(red + (warp * kBlockRows + y) * S + col) = o[y];
+        }
+        __syncthreads();
+        for (int x = tid; x < n * L; x += kLinThreads) {
+          const int y = x / L, c = (x - y * L) * 4;
+          if (c >= columns) continue;
+          float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f), b = a;
+#pragma unroll
+          for (int w = 0; w < kLinWarps; ++w) {
+            const float4 z = *reinterpret_cast<const float4*>(red + (w * kBlockRows + y) * S + c);
+            a.x += z.x, a.y += z.y, a.z += z.z, a.w += z.w;
+          }
+          for (int j = 0; j <= y; ++j) {  // no later row's value, whatever it holds
+            const float4 z = *reinterpret_cast<const float4*>(vb + j * S + c);
+            const float f = score[y][j];
+            b.x = fmaf(f, z.x, b.x), b.y = fmaf(f, z.y, b.y), b.z = fmaf(f, z.z, b.z), b.w = fmaf(f, z.w, b.w);
+          }
+          const float f = first_weight[y];
+          a.x = p.scale * fmaf(f, a.x, b.x), a.y = p.scale * fmaf(f, a.y, b.y);
+          a.z = p.scale * fmaf(f, a.z, b.z), a.w = p.scale * fmaf(f, a.w, b.w);
+          store4(out + ((row + y) * p.Hq + h * p.G + g) * p.Dv + c0 + c, a);
+        }
+      }
+    } else {
+      __syncthreads();
+    }
+    // ---- the state past the block ----
+    if (r.to < 0 && b0 + kBlockRows >= r.last) break;
+    const float f = all_weight;
+#pragma unroll
+    for (int x = 0; x < KR; ++x) s[x].x *= f, s[x].y *= f, s[x].z *= f, s[x].w *= f;
+    for (int j = 0; j < n; ++j) {
+      float4 z = *reinterpret_cast<const float4*>(vb + j * S + col);
+      const float w = weight[j];
+      z.x *= w, z.y *= w, z.z *= w, z.w *= w;
+#pragma unroll
+      for (int x = 0; x < KR; x += 4) {
+        if (kr0 + x >= pitch - 16) break;
+        const float4 y = *reinterpret_cast<const float4*>(kb + j * pitch + kr0 + x);
+        const float t[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          s[x + u].x = fmaf(t[u], z.x, s[x + u].x);
+          s[x + u].y = fmaf(t[u], z.y, s[x + u].y);
+          s[x + u].z = fmaf(t[u], z.z, s[x + u].z);
+          s[x + u].w = fmaf(t[u], z.w, s[x + u].w);
+        }
+      }
+    }
+  }
+  if (r.to >= 0 && mine) {
+#pragma unroll
+    for (int x = 0; x < KR; ++x)
+      if (kr0 + x < p.Dk)
+        *reinterpret_cast<float4*>(p.state + r.to * p.slot_stride + at + (int64_t)x * p.Dv) = s[x];
+  }
+}
+
+template <typename T, int S, int KR>
+cudaError_t launch_rows(const LinearLaunch& p, cudaStream_t stream) {
+  const int slices = (p.Dv + S - 1) / S;
+  const size_t smem = linear_smem<S>(p.Dk);
+  static std::atomic<size_t> raised[kMaxDevices];
+  const cudaError_t err = raise_smem(linear_rows_kernel<T, S, KR>, smem, raised);
+  if (err != cudaSuccess) return err;
+  return launch_after_previous(linear_rows_kernel<T, S, KR>, dim3((unsigned)((long long)p.rows.B * p.H * slices)),
+                               dim3(kLinThreads), smem, stream, p, slices);
+}
+
+// Wide parts where they leave an SM two CTAs to work on; the rows per thread, at most 16, follow.
+template <typename T>
+cudaError_t launch_rows(const LinearLaunch& p, cudaStream_t stream) {
+  const long long heads = (long long)p.rows.B * p.H;
+  const int sms = device_sms();
+  if (p.Dv > 64 && p.Dk <= 128 && heads * ((p.Dv + 127) / 128) >= 2LL * sms)
+    return p.Dk <= 64 ? launch_rows<T, 128, 8>(p, stream) : launch_rows<T, 128, 16>(p, stream);
+  if (p.Dv > 32 && heads * ((p.Dv + 63) / 64) >= 2LL * sms)
+    return p.Dk <= 64 ? launch_rows<T, 64, 4>(p, stream)
+                      : p.Dk <= 128 ? launch_rows<T, 64, 8>(p, stream) : launch_rows<T, 64, 16>(p, stream);
+  return p.Dk <= 128 ? launch_rows<T, 32, 4>(p, stream) : launch_rows<T, 32, 8>(p, stream);
+}
+
+bool linear_shape_ok(int B, int K, int q_heads, int kv_heads, int Dk, int Dv, int dtype) {
+  if (B < 1 || K < 0 || K >= SPEC_MAX_LINEAR_ROWS || (long long)B * (K + 1) > (1LL << 28)) return false;
+  if (dtype != SPEC_BF16 && dtype != SPEC_F32) return false;
+  const int e = element_size(dtype);
+  return kv_heads >= 1 && q_heads >= kv_heads && q_heads % kv_heads == 0 && q_heads / kv_heads <= SPEC_MAX_GROUP &&
+         Dk >= 1 && Dv >= 1 && Dk <= SPEC_MAX_HEAD_DIM && Dv <= SPEC_MAX_HEAD_DIM && Dk * e % 16 == 0 &&
+         Dv * e % 16 == 0 && (long long)B * kv_heads <= (1LL << 26) && q_heads <= (1 << 20);
+}
+
+bool states_ok(const spec_states* s) {
+  if (!s || !s->state || (reinterpret_cast<uintptr_t>(s->state) & 15u) != 0) return false;
+  if (s->layers < 1 || s->slots < 1 || s->kv_heads < 1 || s->kv_heads > (1 << 20) || s->key_dim < 1 ||
+      s->key_dim > SPEC_MAX_HEAD_DIM || s->value_dim < 1 || s->value_dim > SPEC_MAX_HEAD_DIM)
+    return false;
+  const int64_t size = (int64_t)s->kv_heads * s->key_dim * s->value_dim;
+  const int64_t strides[2] = {s->layer_stride, s->slot_stride};
+  const int32_t extent[2] = {s->layers, s->slots};
+  for (int k = 0; k < 2; ++k) {
+    if (extent[k] == 1) continue;  // never used
+    if (strides[k] < size || strides[k] > (INT64_MAX >> 4) / extent[k] || strides[k] % 4 != 0) return false;
+  }
+  return true;
+}
+
+bool linear_rows_ok(const void* p, int64_t stride, int64_t width, int64_t e) {
+  return p && (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && stride * e % 16 == 0 && stride >= width &&
+         stride <= (INT64_MAX >> 36);
+}
+
+int run_linear(const LinearLaunch& p, int dtype, void* ws, size_t ws_bytes, cudaStream_t stream) {
+  if (!ws || ws_bytes < spec_linear_workspace(p.rows.B, p.rows.K, p.Hq, p.H, p.Dk, p.Dv, dtype) ||
+      (reinterpret_cast<uintptr_t>(ws) & 255u) != 0)
+    return SPEC_ERR_WORKSPACE;
+  const cudaError_t err = dtype == SPEC_F32 ? launch_rows<float>(p, stream) : launch_rows<__nv_bfloat16>(p, stream);
+  return err == cudaSuccess && cudaGetLastError() == cudaSuccess ? SPEC_OK : SPEC_ERR_CUDA;
+}
+
+// What both calls have in common; false where an argument is refused.
+bool linear_common(LinearLaunch* p, const void* k, int64_t k_row_stride, const void* v, int64_t v_row_stride, int dtype,
+                   const float* log_decay, int64_t decay_row_stride, const spec_states* states, int layer,
+                   const int32_t* slots_in, const int32_t* row_offsets, const int32_t* depth, const int64_t* pos_base,
+                   int B, int K) {
+  const int64_t e = element_size(dtype);
+  if (layer < 0 || layer >= states->layers || !slots_in || !log_decay ||
+      (reinterpret_cast<uintptr_t>(log_decay) & 3u) != 0 ||
+      (decay_row_stride != 0 && (decay_row_stride < states->kv_heads || decay_row_stride > (INT64_MAX >> 36))))
+    return false;
+  if (!linear_rows_ok(k, k_row_stride, (int64_t)states->kv_heads * states->key_dim, e) ||
+      !linear_rows_ok(v, v_row_stride, (int64_t)states->kv_heads * states->value_dim, e))
+    return false;
+  p->k = k;
+  p->v = v;
+  p->k_row = k_row_stride;
+  p->v_row = v_row_stride;
+  p->H = p->Hq = states->kv_heads;
+  p->G = 1;
+  p->Dk = states->key_dim;
+  p->Dv = states->value_dim;
+  p->log_decay = log_decay;
+  p->decay_row = decay_row_stride;
+  p->state = states->state + (states->layers > 1 ? layer * states->layer_stride : 0);
+  p->slot_stride = states->slots > 1 ? states->slot_stride : 0;
+  p->slots = states->slots;
+  p->slots_in = slots_in;
+  p->rows = RowLayout{row_offsets, depth, pos_base, B, K};
+  return true;
+}
+
+}  // namespace
+
+}  // namespace spec
+
+extern "C" size_t spec_linear_workspace(int B, int K, int q_heads, int kv_heads, int key_dim, int value_dim,
+                                        int dtype) {
+  if (!spec::linear_shape_ok(B, K, q_heads, kv_heads, key_dim, value_dim, dtype)) return 0;
+  return 256;
+}
+
+extern "C" int spec_linear_attend(const void* q, int64_t q_row_stride, int q_heads, const void* k, int64_t k_row_stride,
+                                  const void* v, int64_t v_row_stride, int dtype, const float* log_decay,
+                                  int64_t decay_row_stride, const spec_states* states, int layer,
+                                  const int32_t* slots_in, const int32_t* slots_out, const int32_t* row_offsets,
+                                  const int32_t* depth, const int64_t* pos_base, int B, int K, float scale, void* out,
+                                  int32_t* status, void* ws, size_t ws_bytes, cudaStream_t stream) {
+  spec::NvtxRange range("spec_linear_attend");
+  using namespace spec;
+  if (!states_ok(states) ||
+      !linear_shape_ok(B, K, q_heads, states->kv_heads, states->key_dim, states->value_dim, dtype))
+    return SPEC_ERR_INVALID_ARG;
+  LinearLaunch p{};
+  if (!linear_common(&p, k, k_row_stride, v, v_row_stride, dtype, log_decay, decay_row_stride, states, layer, slots_in,
+                     row_offsets, depth, pos_base, B, K))
+    return SPEC_ERR_INVALID_ARG;
+  if (!linear_rows_ok(q, q_row_stride, (int64_t)q_heads * p.Dk, element_size(dtype)) || !out ||
+      (reinterpret_cast<uintptr_t>(out) & 15u) != 0 || !std::isfinite(scale))
+    return SPEC_ERR_INVALID_ARG;
+  p.q = q;
+  p.q_row = q_row_stride;
+  p.Hq = q_heads;
+  p.G = q_heads / p.H;
+  p.slots_out = slots_out;
+  p.scale = scale;
+  p.out = out;
+  p.status = status;
+  return run_linear(p, dtype, ws, ws_bytes, stream);
+}
+
+extern "C" int spec_linear_commit(const void* k, int64_t k_row_stride, const void* v, int64_t v_row_stride, int dtype,
+                                  const float* log_decay, int64_t decay_row_stride, const spec_states* states, int layer,
+                                  const int32_t* slots_in, const int32_t* slots_out, const int32_t* accepted_len,
+                                  const int32_t* row_offsets, const int32_t* depth, const int64_t* pos_base, int B,
+                                  int K, int32_t* status, void* ws, size_t ws_bytes, cudaStream_t stream) {
+  spec::NvtxRange range("spec_linear_commit");
+  using namespace spec;
+  if (!states_ok(states) ||
+      !linear_shape_ok(B, K, states->kv_heads, states->kv_heads, states->key_dim, states->value_dim, dtype))
+    return SPEC_ERR_INVALID_ARG;
+  LinearLaunch p{};
+  if (!slots_out ||
+      !linear_common(&p, k, k_row_stride, v, v_row_stride, dtype, log_decay, decay_row_stride, states, layer, slots_in,
+                     row_offsets, depth, pos_base, B, K))
+    return SPEC_ERR_INVALID_ARG;
+  p.slots_out = slots_out;
+  p.accepted = accepted_len;
+  p.status = status;
+  return run_linear(p, dtype, ws, ws_bytes, stream);
+}

@@ -16,7 +16,7 @@ struct RequestRows {
 struct RowLayout {
   const int32_t* row_offsets;  // [B + 1] or null
   const int32_t* depth;        // [B] or null
-  const int64_t* pos_base;     // [B]
+  const int64_t* pos_base;     // [B], or null: position 0
   int B, K;
 };
 
@@ -32,7 +32,7 @@ __device__ __forceinline__ RequestRows request_rows(const RowLayout& a, int i) {
     end = r.row0 + a.K + 1;
   }
   // far past any table (and far below 0) is all the same: sums with p do not overflow
-  const long long p = __ldg(reinterpret_cast<const long long*>(a.pos_base) + i), far = 1LL << 40;
+  const long long p = a.pos_base ? __ldg(reinterpret_cast<const long long*>(a.pos_base) + i) : 0, far = 1LL << 40;
   r.p = p > far ? far : p < -far ? -far : p;
   r.count = n + 1;
   r.ok = n >= 0 && n <= a.K && r.row0 >= 0 && end <= a.B * (a.K + 1) &&

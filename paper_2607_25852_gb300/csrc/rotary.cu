@@ -1,0 +1,337 @@
+// rotary.cu -- rotary positions: the rows' queries and keys turned by the angles
+// of their positions, the keys and the values straight into their pages.
+//
+// Element pair d of a head, (a, b), at position P becomes
+//   amplitude (a cos t - b sin t, b cos t + a sin t),  t = P f_d.
+// The angle is needed modulo a turn only, so f_d / 2 pi is rounded once to a
+// multiple of 2^-64 turns and multiplied by P in 64-bit integers: what overflows
+// is whole turns, and the product is exact (a position of 2^20 in fp32 loses the
+// angle's last 17 bits, and fp64 arithmetic is slow here).  cos and sin are then
+// CUDA's sincospif of the angle in half turns.
+//
+// A CTA takes a row: its first loads are in flight while its threads compute the
+// row's angles, one each, into shared memory for all heads.  Bound by HBM for
+// many rows, by two round trips (the row's position; its page and its data) and
+// the launch for few.
+#include <cmath>
+
+#include "paged.cuh"
+#include "tensor_core.cuh"
+
+namespace spec {
+
+namespace {
+
+constexpr int kRotaryThreads = 256;
+
+struct RotaryLaunch {
+  const char *x, *k_new, *v_new;  // k_new, v_new null without a cache
+  char *out, *k, *v;              // k and v of the layer
+  int64_t x_row, out_row, k_row, v_row;  // bytes between rows
+  int64_t page_b, token_b, head_b;
+  int heads, kv_heads, D;
+  int pairs;                      // rotary_dim / 2
+  int pages, page_size, max_pages;
+  bool in_place;                  // out is x: what is not turned stays
+  float amplitude;
+  const double* frequencies;
+  const int32_t* table;
+  RowLayout rows;
+  int32_t* status;
+};
+
+// W elements as one load or store.
+template <typename T, int W>
+struct alignas(sizeof(T) * W) Pack {
+  T e[W];
+};
+template <typename T, int W>
+__device__ __forceinline__ Pack<T, W> load_pack(const char* p) {
+  return *reinterpret_cast<const Pack<T, W>*>(p);
+}
+template <typename T, int W>
+__device__ __forceinline__ void store_pack(char* p, const Pack<T, W>& v) {
+  *reinterpret_cast<Pack<T, W>*>(p) = v;
+}
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ void from_float(float x, float* to) { *to = x; }
+__device__ __forceinline__ void from_float(float x, __nv_bfloat16* to) { *to = __float2bfloat16_rn(x); }
+
+// Cosine and sine, times the amplitude, of position P's turn of a pair.
+__device__ __forceinline__ float2 turn(double frequency, int64_t P, float amplitude, int32_t* status) {
+  double turns = frequency * 0.15915494309189533577;  // 1 / (2 pi)
+  turns -= rint(turns);
+  if (!(fabs(turns) <= 0.5)) {  // not finite
+    report(status, SPEC_ERR_BAD_INPUT);
+    turns = 0.0;
+  }
+  const int64_t step = __double2ll_rn(turns * 18446744073709551616.0);  // half a turn saturates, 2^-64 off
+  const int64_t phase = (int64_t)((uint64_t)P * (uint64_t)step);
+  float s, c;
+  sincospif((float)phase * 1.0842021724855044e-19f, &s, &c);  // 2^-63: in half turns
+  return make_float2(amplitude * c, amplitude * s);
+}
+
+// kInter: neighbouring elements are a pair, and a unit is one pack of W
+// elements.  Otherwise elements d and d + pairs are, and a unit is two packs of W
+// elements, one of each half (W divides the half), or one of those that stay.
+template <typename T, int W, bool kInter>
+__global__ void __launch_bounds__(kRotaryThreads) rotary_kernel(const RotaryLaunch p) {
+  __shared__ float cs[SPEC_MAX_HEAD_DIM / 2], sn[SPEC_MAX_HEAD_DIM / 2];
+  const int tid = threadIdx.x, K1 = p.rows.K + 1;
+  const int i = (int)(blockIdx.x / (unsigned)K1), j = (int)(blockIdx.x - (unsigned)i * (unsigned)K1);
+  pdl_wait_prerequisites();
+  pdl_launch_dependents();
+  const double frequency = tid < p.pairs ? __ldg(p.frequencies + tid) : 0.0;
+  const RequestRows q = request_rows(p.rows, i);
+  if (!q.ok) {
+    if (j == 0 && tid == 0) report(p.status, SPEC_ERR_BAD_INPUT);
+    return;
+  }
+  const int64_t pos = q.p + j;
+  if (j >= q.count || pos < 0) return;
+  const int64_t row = q.row0 + j;
+  const char* x = p.x + row * p.x_row;
+  char* out = p.out + row * p.out_row;
+
+  // ---- the keys' and values' place ----
+  char *k_to = nullptr, *v_to = nullptr;
+  if (p.k_new) {
+    int page = -1, slot = 0;
+    if (pos < (int64_t)p.max_pages * p.page_size) {
+      slot = (int)pos / p.page_size;
+      page = __ldg(p.table + (size_t)i * p.max_pages + slot);
+    }
+    if (page < 0 || page >= p.pages) {
+      if (tid == 0) report(p.status, SPEC_ERR_BAD_INPUT);
+    } else {
+      const int64_t at = (int64_t)page * p.page_b + (int64_t)((int)pos - slot * p.page_size) * p.token_b;
+      k_to = p.k + at;
+      v_to = p.v + at;
+    }
+  }
+
+  constexpr int E = (int)sizeof(T), kU = 2;  // units in flight per thread
+  const int turned = kInter ? (2 * p.pairs + W - 1) / W : p.pairs / W;  // a head's units with turned elements
+  const int units = kInter ? p.D / W : turned + (p.D - 2 * p.pairs) / W;
+  const int heads = p.heads + (k_to ? p.kv_heads : 0), total = heads * units;
+  // unit n: where it is read and written
+  auto place = [&](int n, int& u, const char*& from, char*& to) {
+    const int h = n / units;
+    u = n - h * units;
+    if (h < p.heads) {
+      from = x + (int64_t)h * p.D * E;
+      to = out + (int64_t)h * p.D * E;
+    } else {
+      from = p.k_new + row * p.k_row + (int64_t)(h - p.heads) * p.D * E;
+      to = k_to + (h - p.heads) * p.head_b;
+    }
+  };
+  const int first = kInter ? 0 : 2 * p.pairs - turned * W;  // a staying unit u begins at first + u W
+  bool angles = false;
+  for (int n0 = tid; n0 - tid < total || !angles; n0 += kU * kRotaryThreads) {
+    Pack<T, W> a[kU], b[kU];
+#pragma unroll
+    for (int y = 0; y < kU; ++y) {
+      const int n = n0 + y * kRotaryThreads;
+      if (n >= total) continue;
+      int u;
+      const char* from;
+      char* to;
+      place(n, u, from, to);
+      if (!kInter && u < turned) {
+        a[y] = load_pack<T, W>(from + (int64_t)u * W * E);
+        b[y] = load_pack<T, W>(from + (int64_t)(p.pairs + u * W) * E);
+      } else {
+        a[y] = load_pack<T, W>(from + (int64_t)(first + u * W) * E);
+      }
+    }
+    if (!angles) {  // the row's angles, a pair per thread, while the loads are under way
+      if (tid < p.pairs) {
+        const float2 t = turn(frequency, pos, p.amplitude, p.status);
+        cs[tid] = t.x;
+        sn[tid] = t.y;
+      }
+      __syncthreads();
+      angles = true;
+    }
+#pragma unroll
+    for (int y = 0; y < kU; ++y) {
+      const int n = n0 + y * kRotaryThreads;
+      if (n >= total) continue;
+      int u;
+      const char* from;
+      char* to;
+      place(n, u, from, to);
+      if (u >= turned) {
+        if (!(p.in_place && n < p.heads * units)) store_pack<T, W>(to + (int64_t)(first + u * W) * E, a[y]);
+        continue;
+      }
+      if (kInter) {
+#pragma unroll
+        for (int e = 0; e < W; e += 2) {
+          const int d = (u * W + e) / 2;
+          if (d >= p.pairs) break;  // the rest of this pack stays
+          const float v = to_float(a[y].e[e]), w = to_float(a[y].e[e + 1]), c = cs[d], s = sn[d];
+          from_float(fmaf(v, c, -w * s), &a[y].e[e]);
+          from_float(fmaf(w, c, v * s), &a[y].e[e + 1]);
+        }
+        store_pack<T, W>(to + (int64_t)u * W * E, a[y]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+          const float v = to_float(a[y].e[e]), w = to_float(b[y].e[e]), c = cs[u * W + e], s = sn[u * W + e];
+          from_float(fmaf(v, c, -w * s), &a[y].e[e]);
+          from_float(fmaf(w, c, v * s), &b[y].e[e]);
+        }
+        store_pack<T, W>(to + (int64_t)u * W * E, a[y]);
+        store_pack<T, W>(to + (int64_t)(p.pairs + u * W) * E, b[y]);
+      }
+    }
+  }
+  if (v_to) {
+    const int vec = p.D * E / 16, n = p.kv_heads * vec;
+    const char* v = p.v_new + row * p.v_row;
+    for (int y = tid; y < n; y += kRotaryThreads) {
+      const int h = y / vec;
+      *reinterpret_cast<uint4*>(v_to + h * p.head_b + (int64_t)(y - h * vec) * 16) = ldg_stream(v + (int64_t)y * 16);
+    }
+  }
+}
+
+template <typename T>
+cudaError_t launch_rotary(const RotaryLaunch& p, bool interleaved, cudaStream_t stream) {
+  const dim3 grid((unsigned)((long long)p.rows.B * (p.rows.K + 1))), block(kRotaryThreads);
+  constexpr int W = 16 / (int)sizeof(T);
+  if (interleaved) return launch_after_previous(rotary_kernel<T, W, true>, grid, block, 0, stream, p);
+  // the widest packs that divide the half that is turned
+  if (p.pairs % W == 0) return launch_after_previous(rotary_kernel<T, W, false>, grid, block, 0, stream, p);
+  if (p.pairs % (W / 2) == 0) return launch_after_previous(rotary_kernel<T, W / 2, false>, grid, block, 0, stream, p);
+  if (p.pairs % 2 == 0) return launch_after_previous(rotary_kernel<T, 2, false>, grid, block, 0, stream, p);
+  return launch_after_previous(rotary_kernel<T, 1, false>, grid, block, 0, stream, p);
+}
+
+bool rows_ok(const void* p, int64_t stride, int heads, int head_dim, int64_t e) {
+  return p && (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && stride * e % 16 == 0 &&
+         stride >= (int64_t)heads * head_dim && stride <= (INT64_MAX >> 32);
+}
+
+bool rotation_ok(const double* frequencies, int rotary_dim, int head_dim, float amplitude) {
+  return frequencies && rotary_dim >= 2 && rotary_dim % 2 == 0 && rotary_dim <= head_dim && std::isfinite(amplitude);
+}
+
+int run_rotary(const RotaryLaunch& p, int dtype, int interleaved, cudaStream_t stream) {
+  const cudaError_t err = dtype == SPEC_F32 ? launch_rotary<float>(p, interleaved != 0, stream)
+                                            : launch_rotary<__nv_bfloat16>(p, interleaved != 0, stream);
+  return err == cudaSuccess && cudaGetLastError() == cudaSuccess ? SPEC_OK : SPEC_ERR_CUDA;
+}
+
+}  // namespace
+
+}  // namespace spec
+
+extern "C" int spec_rotary_frequencies(int rotary_dim, double base, int scaling, double factor,
+                                       int64_t original_positions, double low, double high, double* out) {
+  using std::isfinite;
+  if (rotary_dim < 2 || rotary_dim % 2 != 0 || rotary_dim > SPEC_MAX_HEAD_DIM || !(base > 1.0) || !isfinite(base) || !out)
+    return SPEC_ERR_INVALID_ARG;
+  if (scaling < SPEC_ROTARY_PLAIN || scaling > SPEC_ROTARY_RAMP) return SPEC_ERR_INVALID_ARG;
+  if (scaling != SPEC_ROTARY_PLAIN && (!(factor >= 1.0) || !isfinite(factor))) return SPEC_ERR_INVALID_ARG;
+  if (scaling == SPEC_ROTARY_BASE && rotary_dim < 4) return SPEC_ERR_INVALID_ARG;
+  if (scaling == SPEC_ROTARY_RAMP && (original_positions < 1 || !(low > 0.0) || !(high > low) || !isfinite(high)))
+    return SPEC_ERR_INVALID_ARG;
+  if (scaling == SPEC_ROTARY_BASE) base *= std::pow(factor, (double)rotary_dim / (rotary_dim - 2));
+  for (int d = 0; d < rotary_dim / 2; ++d) {
+    double f = std::pow(base, -2.0 * d / rotary_dim);
+    if (scaling == SPEC_ROTARY_LINEAR) f /= factor;
+    if (scaling == SPEC_ROTARY_RAMP) {
+      const double turns = (double)original_positions * f / 6.283185307179586477;
+      const double keep = std::fmin(1.0, std::fmax(0.0, (turns - low) / (high - low)));
+      f = f * keep + f / factor * (1.0 - keep);
+    }
+    out[d] = f;
+  }
+  return SPEC_OK;
+}
+
+extern "C" int spec_rotary(const void* x, int64_t x_row_stride, int heads, int head_dim, int dtype,
+                           const double* frequencies, int rotary_dim, int interleaved, float amplitude,
+                           const int32_t* row_offsets, const int32_t* depth, const int64_t* pos_base, int B, int K,
+                           void* out, int64_t out_row_stride, int32_t* status, cudaStream_t stream) {
+  spec::NvtxRange range("spec_rotary");
+  using namespace spec;
+  if (!rows_shape_ok(B, K) || (dtype != SPEC_BF16 && dtype != SPEC_F32) || heads < 1 || heads > (1 << 16) ||
+      head_dim < 1 || head_dim > SPEC_MAX_HEAD_DIM || head_dim * element_size(dtype) % 16 != 0)
+    return SPEC_ERR_INVALID_ARG;
+  const int64_t e = element_size(dtype);
+  if (!rotation_ok(frequencies, rotary_dim, head_dim, amplitude) || !pos_base ||
+      !rows_ok(x, x_row_stride, heads, head_dim, e) || !rows_ok(out, out_row_stride, heads, head_dim, e))
+    return SPEC_ERR_INVALID_ARG;
+  if (out == x && out_row_stride != x_row_stride) return SPEC_ERR_INVALID_ARG;
+  RotaryLaunch p{};
+  p.x = static_cast<const char*>(x);
+  p.out = static_cast<char*>(out);
+  p.x_row = x_row_stride * e;
+  p.out_row = out_row_stride * e;
+  p.heads = heads;
+  p.D = head_dim;
+  p.pairs = rotary_dim / 2;
+  p.in_place = out == x;
+  p.amplitude = amplitude;
+  p.frequencies = frequencies;
+  p.rows = RowLayout{row_offsets, depth, pos_base, B, K};
+  p.status = status;
+  return run_rotary(p, dtype, interleaved, stream);
+}
+
+extern "C" int spec_rotary_append(const spec_cache* cache, int layer, const void* q, int64_t q_row_stride, int q_heads,
+                                  const void* k_new, int64_t k_row_stride, const void* v_new, int64_t v_row_stride,
+                                  const double* frequencies, int rotary_dim, int interleaved, float amplitude,
+                                  const int32_t* row_offsets, const int32_t* depth, const int64_t* pos_base,
+                                  const int32_t* page_table, int max_pages, int B, int K, void* q_out,
+                                  int64_t q_out_row_stride, int32_t* status, cudaStream_t stream) {
+  spec::NvtxRange range("spec_rotary_append");
+  using namespace spec;
+  if (!cache_ok(cache) || layer < 0 || layer >= cache->layers || !rows_shape_ok(B, K) ||
+      !table_shape_ok(B, max_pages, cache->pages, cache->page_size) || cache->kv_heads > (1 << 16))
+    return SPEC_ERR_INVALID_ARG;
+  const int64_t e = element_size(cache->dtype);
+  const int D = cache->head_dim;
+  if (!rotation_ok(frequencies, rotary_dim, D, amplitude) || !pos_base || !page_table ||
+      !rows_ok(k_new, k_row_stride, cache->kv_heads, D, e) || !rows_ok(v_new, v_row_stride, cache->kv_heads, D, e))
+    return SPEC_ERR_INVALID_ARG;
+  if (q_heads < 0 || q_heads > (1 << 16) || (q_heads == 0) != (q == nullptr) || (q_heads == 0) != (q_out == nullptr))
+    return SPEC_ERR_INVALID_ARG;
+  if (q_heads && (!rows_ok(q, q_row_stride, q_heads, D, e) || !rows_ok(q_out, q_out_row_stride, q_heads, D, e) ||
+                  (q == q_out && q_row_stride != q_out_row_stride)))
+    return SPEC_ERR_INVALID_ARG;
+  RotaryLaunch p{};
+  p.x = static_cast<const char*>(q);
+  p.out = static_cast<char*>(q_out);
+  p.x_row = q_row_stride * e;
+  p.out_row = q_out_row_stride * e;
+  p.k_new = static_cast<const char*>(k_new);
+  p.v_new = static_cast<const char*>(v_new);
+  p.k_row = k_row_stride * e;
+  p.v_row = v_row_stride * e;
+  p.k = static_cast<char*>(cache->k) + layer * cache->layer_stride * e;
+  p.v = static_cast<char*>(cache->v) + layer * cache->layer_stride * e;
+  p.page_b = cache->page_stride * e;
+  p.token_b = cache->token_stride * e;
+  p.head_b = cache->head_stride * e;
+  p.heads = q_heads;
+  p.kv_heads = cache->kv_heads;
+  p.D = D;
+  p.pairs = rotary_dim / 2;
+  p.pages = cache->pages;
+  p.page_size = cache->page_size;
+  p.max_pages = max_pages;
+  p.in_place = q == q_out;
+  p.amplitude = amplitude;
+  p.frequencies = frequencies;
+  p.table = page_table;
+  p.rows = RowLayout{row_offsets, depth, pos_base, B, K};
+  p.status = status;
+  return run_rotary(p, cache->dtype, interleaved, stream);
+}

@@ -10,7 +10,7 @@ from ``spec_allocate``):
 
     cache.reserve(pos_base, depth, row_offsets)           # pages for the rows
     for layer in ...:
-        cache.append(layer, k_new, v_new, pos_base, depth, row_offsets)
+        cache.append(layer, k_new, v_new, pos_base, depth, row_offsets)   # or append_rotary
         cache.attend(layer, q, pos_base, out, depth, row_offsets)
     spec_verify(...); spec_commit(...)
     cache.commit(pos_base, accepted_len)                  # rejected drafts' pages go back
@@ -25,7 +25,7 @@ rows lie before position 0: at pos_base = -(drafts + 1) whatever its depth.
 import torch
 
 from . import (MAX_DRAFTS, attend_workspace, cache_workspace, spec_attend, spec_cache_append, spec_cache_compact,
-               spec_cache_copy, spec_cache_fork, spec_cache_release, spec_cache_reserve)
+               spec_cache_copy, spec_cache_fork, spec_cache_release, spec_cache_reserve, spec_rotary_append)
 
 
 class PagedCache:
@@ -73,6 +73,14 @@ class PagedCache:
         """The rows' keys and values [R, kv_heads, head_dim] into their pages."""
         spec_cache_append(k_new, v_new, self.k, self.v, self.page_table, pos_base, self.B, self.K,
                           row_offsets=row_offsets, depth=depth, layer=layer, status=self.status, stream=stream)
+
+    def append_rotary(self, layer, q, k_new, v_new, pos_base, frequencies, q_out, depth=None, row_offsets=None,
+                      interleaved=False, amplitude=1.0, stream=None):
+        """append, with the queries (into q_out, which may be q) and the keys turned by their positions first;
+        frequencies from spec_rotary_frequencies."""
+        spec_rotary_append(q, k_new, v_new, self.k, self.v, self.page_table, pos_base, self.B, self.K, frequencies,
+                           q_out, interleaved=interleaved, amplitude=amplitude, row_offsets=row_offsets, depth=depth,
+                           layer=layer, status=self.status, stream=stream)
 
     def attend(self, layer, q, pos_base, out, depth=None, row_offsets=None, scale=None, lse_out=None, stream=None):
         """Attention of the rows' queries [R, q_heads, head_dim] over their requests' positions, into `out`."""

@@ -1,0 +1,346 @@
+"""spec_linear_attend and spec_linear_commit against the recurrence in 64 bits."""
+import math
+
+import pytest
+import torch
+
+import paper_2607_25852_gb300 as spec
+import rows_ref as ref
+from paper_2607_25852_gb300.states import LinearStates
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+class Case:
+    """Requests of `depth` + 1 rows; request i starts from slot start[i] of the pool (-1: zeros)."""
+
+    def __init__(self, depth, K, Hq, H, Dk, Dv, dtype=BF16, gate="row", start=None, seed=1, strong=2.0, fused=False):
+        g = torch.Generator().manual_seed(seed)
+        self.depth, self.K, self.B, self.dtype = depth, K, len(depth), dtype
+        self.Hq, self.H, self.Dk, self.Dv = Hq, H, Dk, Dv
+        self.offsets = [0]
+        for n in depth:
+            self.offsets.append(self.offsets[-1] + n + 1)
+        R = self.R = self.offsets[-1]
+        if fused:
+            w = Hq * Dk + H * Dk + H * Dv
+            rows = torch.randn((R + 1, w + 8), generator=g).to(dtype).to(DEV)
+            self.q = rows[:, :Hq * Dk].unflatten(1, (Hq, Dk))
+            self.k = rows[:, Hq * Dk:(Hq + H) * Dk].unflatten(1, (H, Dk))
+            self.v = rows[:, (Hq + H) * Dk:w].unflatten(1, (H, Dv))
+        else:
+            self.q, self.k, self.v = (torch.randn((R + 1, h, d), generator=g).to(dtype).to(DEV)
+                                      for h, d in ((Hq, Dk), (H, Dk), (H, Dv)))
+        if gate == "row":
+            self.decay = -torch.exp(torch.empty((R + 1, H)).uniform_(math.log(1e-3), math.log(strong), generator=g))
+        elif gate == "head":
+            self.decay = -torch.exp2(-1.0 - torch.arange(H) * 7.0 / H)
+        else:
+            self.decay = gate
+        self.slots = 2 * self.B + 1
+        self.states = torch.randn((2, self.slots, H, Dk, Dv), generator=g).to(DEV)
+        order = torch.randperm(self.slots, generator=g).tolist()
+        self.start = order[:self.B] if start is None else start
+        self.to = order[self.B:2 * self.B]
+        self.status = i32([0])
+        self.ws = spec.linear_workspace(self.B, K, Hq, H, Dk, Dv, dtype, DEV)
+        self.scale = Dk ** -0.5
+        self.pos = None
+
+    def at(self):
+        return dict(row_offsets=i32(self.offsets), depth=i32(self.depth), layer=1, status=self.status,
+                    pos_base=None if self.pos is None else torch.tensor(self.pos, device=DEV))
+
+    def attend(self, to="to", **kw):
+        out = torch.full((self.R + 1, self.Hq, self.Dv), 7.0, dtype=self.dtype, device=DEV)
+        slots_out = None if to is None else i32(self.to if to == "to" else to)
+        spec.spec_linear_attend(self.q, self.k, self.v, self.decay.to(DEV), self.states, i32(self.start), slots_out, self.B,
+                                self.K, out, self.ws, **{**self.at(), **kw})
+        return out
+
+    def commit(self, accepted, **kw):
+        spec.spec_linear_commit(self.k, self.v, self.decay.to(DEV), self.states, i32(self.start), i32(self.to),
+                                None if accepted is None else i32(accepted), self.B, self.K, self.ws,
+                                **{**self.at(), **kw})
+
+    def want(self, i, before, take=None):
+        rows = slice(self.offsets[i], self.offsets[i + 1])
+        g = self.decay if self.decay.dim() == 2 else self.decay.expand(self.R + 1, self.H)
+        first = before[1, self.start[i]] if self.start[i] >= 0 else torch.zeros_like(before[1, 0])
+        n = self.depth[i] + 1
+        skip = 0 if self.pos is None else min(n, max(0, -self.pos[i]))
+        out, state, o_size, s_size = ref.linear(
+            self.q[rows][skip:].cpu(), self.k[rows][skip:].cpu(), self.v[rows][skip:].cpu(), g[rows][skip:],
+            first.cpu(), self.scale, None if take is None else max(0, take - skip))
+        o_tol, s_tol = ref.linear_bounds(out, o_size, state, s_size, n, self.Dk, self.dtype)
+        pad = torch.zeros((skip,) + out.shape[1:], dtype=torch.float64)
+        return torch.cat([pad, out]), torch.cat([pad, o_tol]), state, s_tol
+
+    def check(self, out, before, accepted=None, states=True):
+        for i in range(self.B):
+            o, o_tol, s, s_tol = self.want(i, before, None if accepted is None else accepted[i] + 1)
+            if out is not None:
+                got = out[self.offsets[i]:self.offsets[i + 1]].cpu().double()
+                assert bool(((got - o).abs() <= o_tol).all()), (i, float(((got - o).abs() / o_tol).max()))
+            if states:
+                got = self.states[1, self.to[i]].cpu().double()
+                assert bool(((got - s).abs() <= s_tol).all()), (i, float(((got - s).abs() / s_tol).max()))
+        if out is not None:
+            assert bool((out[self.R] == 7).all())
+        touched = {(1, t) for t in self.to} if states else set()
+        for l in range(2):
+            for t in range(self.slots):
+                if (l, t) not in touched:
+                    assert torch.equal(self.states[l, t], before[l, t]), (l, t)
+
+
+SHAPES = [(4, 4, 128, 128), (4, 2, 64, 64), (8, 1, 64, 128), (2, 2, 128, 64)]
+ODD = [(3, 3, 72, 96), (2, 1, 8, 8), (4, 4, 32, 160), (1, 1, 256, 256), (6, 2, 200, 40)]
+
+
+@pytest.mark.parametrize("depth,K", [([0], 0), ([0] * 5, 0), ([7, 0, 3], 7), ([16, 8, 9], 16), ([40, 31, 0, 63], 63),
+                                     ([64, 130, 127], 200), ([300, 5], 300)])
+@pytest.mark.parametrize("shape", SHAPES + ODD)
+def test_rows(shape, depth, K):
+    c = Case(depth, K, *shape, start=None if len(depth) < 3 else [2, -1, 0, 3, 3][:len(depth)])
+    c.to = [s for s in range(c.slots) if s not in c.start][:c.B]
+    before = c.states.clone()
+    out = c.attend()
+    assert int(c.status) == 0
+    c.check(out, before)
+
+
+@pytest.mark.parametrize("gate", ["head", "row"])
+@pytest.mark.parametrize("depth,K", [([0, 0], 0), ([11, 4], 16), ([100, 70], 150)])
+@pytest.mark.parametrize("shape", [(2, 2, 128, 128), (4, 2, 64, 64), (3, 1, 36, 100)])
+def test_fp32(shape, depth, K, gate):
+    c = Case(depth, K, *shape, dtype=F32, gate=gate)
+    before = c.states.clone()
+    c.check(c.attend(), before)
+    assert int(c.status) == 0
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("K,depth,accepted", [(7, [7, 0, 4], [3, 0, 4]), (70, [70, 64, 0], [64, 0, 0])])
+def test_round(K, depth, accepted, dtype):
+    """A verification leaves the states; the commit takes the accepted rows, whatever the rejected ones hold."""
+    c = Case(depth, K, 4, 2, 128, 128, dtype=dtype, gate="head", fused=True)
+    before = c.states.clone()
+    out = c.attend(to=None)
+    c.check(out, before, states=False)
+    for i, a in enumerate(accepted):
+        c.k[c.offsets[i] + a + 1:c.offsets[i + 1]] = math.nan
+        c.v[c.offsets[i] + a + 1:c.offsets[i + 1]] = math.inf
+    c.commit(accepted)
+    assert int(c.status) == 0
+    for i, a in enumerate(accepted):
+        rows = slice(c.offsets[i] + a + 1, c.offsets[i + 1])
+        c.k[rows], c.v[rows] = 0.0, 0.0
+    c.check(None, before, accepted)
+
+
+@pytest.mark.parametrize("K", [3, 130])
+def test_in_place_and_shared_start(K):
+    """New states in the old ones' slots; two requests from one slot, into slots of their own."""
+    c = Case([K, K - 1, K], K, 2, 2, 64, 64)
+    c.to = list(c.start)
+    before = c.states.clone()
+    out = c.attend()
+    c.check(out, before)
+    c = Case([K, K - 1, K], K, 2, 2, 64, 64)
+    c.start[1] = c.start[0]
+    before = c.states.clone()
+    c.check(c.attend(), before)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("K", [6, 150])
+def test_strong_decays(K, dtype):
+    """Decays of nothing, of everything, and far below fp32's range, next to slow ones; sums of many strong ones."""
+    n = K + 1
+    g = torch.full((2 * n + 1, 3), -0.01)
+    g[:, 1] = -60.0
+    g[n // 2, 0] = -math.inf
+    g[n // 2 + 1, 2] = -1e30
+    g[3:5, 2] = 0.0
+    g[n:, 0] = -300.0
+    c = Case([K, K], K, 3, 3, 128, 128, dtype=dtype, gate=g)
+    before = c.states.clone()
+    out = c.attend()
+    assert int(c.status) == 0
+    c.check(out, before)
+    assert bool(torch.isfinite(out).all())
+
+
+def test_growth_is_refused():
+    g = torch.full((5, 2), -0.1)
+    g[1, 0], g[2, 1] = 0.5, math.nan
+    c = Case([3], 3, 2, 2, 64, 64, gate=g)
+    before = c.states.clone()
+    out = c.attend()
+    assert int(c.status) == spec.ERR_BAD_INPUT
+    c.decay[1, 0], c.decay[2, 1] = 0.0, 0.0
+    c.check(out, before)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("K,at", [(5, 3), (140, 70), (140, 130), (200, 64)])
+@pytest.mark.parametrize("what", ["k", "v"])
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+def test_not_finite(K, at, what, value, dtype):
+    """Rows before it are as if it were not there, rows from it on and the state are not finite where it enters."""
+    c = Case([K, K], K, 2, 2, 64, 64, dtype=dtype)
+    before = c.states.clone()
+    (c.k if what == "k" else c.v)[at, 1, 5] = value
+    out = c.attend()
+    c.k[at, 1], c.v[at, 1] = 0.0, 0.0
+    o, o_tol, s, s_tol = c.want(0, before)
+    got = out[:K + 1].cpu().double()
+    fine = torch.ones_like(o, dtype=torch.bool)
+    hit = slice(None) if what == "k" else 5
+    fine[at:, 1, hit] = False
+    if what == "v":  # the other elements of the row's product are what they were with the row
+        fine[at:, 1] = False
+    assert bool(((got - o).abs() <= o_tol)[fine].all())
+    assert not bool(torch.isfinite(got[at:, 1, hit]).any())
+    if what == "v":
+        assert bool(torch.isfinite(got[at:, 1, 6:]).all()) and bool(torch.isfinite(got[at:, 1, :5]).all())
+    state = c.states[1, c.to[0]].cpu()
+    assert bool(torch.isfinite(state[0]).all())
+    assert not bool(torch.isfinite(state[1][5] if what == "k" else state[1][:, 5]).any())
+    o, o_tol, s, s_tol = c.want(1, before)
+    assert bool(((out[K + 1:-1].cpu().double() - o).abs() <= o_tol).all())
+
+
+@pytest.mark.parametrize("K", [4, 100])
+def test_idle_and_early_rows(K):
+    """Rows before position 0 give 0 and change nothing; an idle request's state moves as it is."""
+    c = Case([K, K, K, K], K, 4, 2, 64, 128, start=[0, 1, -1, 2])
+    c.to = [4, 5, 6, 7]
+    c.pos = [-(K + 1), 3, -(K + 1), -2]
+    for i in (0, 2):
+        c.k[c.offsets[i]:c.offsets[i + 1]] = math.nan
+        c.q[c.offsets[i]:c.offsets[i + 1]] = math.nan
+    before = c.states.clone()
+    out = c.attend()
+    assert int(c.status) == 0
+    assert torch.equal(c.states[1, 4], before[1, 0]) and not bool(c.states[1, 6].any())
+    for i in (0, 2):
+        assert not bool(out[c.offsets[i]:c.offsets[i + 1]].any())
+        c.k[c.offsets[i]:c.offsets[i + 1]] = 0
+        c.q[c.offsets[i]:c.offsets[i + 1]] = 0
+    c.check(out, before)
+
+
+@pytest.mark.parametrize("K", [2, 90])
+def test_bad_requests(K):
+    """Slots out of range, depths that do not fit: nothing of these requests is written, the others are served."""
+    c = Case([K] * 5, K, 2, 2, 64, 64)
+    before = c.states.clone()
+    good_start, good_to = list(c.start), list(c.to)
+    c.start[1], c.to[2] = c.slots, -2
+    bad_depth = [K, K, K, K - 1, K]
+    out = c.attend(depth=i32(bad_depth))
+    assert int(c.status) == spec.ERR_BAD_INPUT
+    for i in (1, 2, 3):
+        assert bool((out[c.offsets[i]:c.offsets[i + 1]] == 7).all())
+        assert torch.equal(c.states[1, good_to[i]], before[1, good_to[i]])
+    c.start, c.to = good_start, good_to
+    for i in (0, 4):
+        o, o_tol, s, s_tol = c.want(i, before)
+        assert bool(((out[c.offsets[i]:c.offsets[i + 1]].cpu().double() - o).abs() <= o_tol).all())
+        assert bool(((c.states[1, c.to[i]].cpu().double() - s).abs() <= s_tol).all())
+    c.status.zero_()
+    kept = c.states.clone()
+    c.commit([0, K + 1, -1, 0, 0])
+    assert int(c.status) == spec.ERR_BAD_INPUT
+    for i in (1, 2):
+        assert torch.equal(c.states[1, c.to[i]], kept[1, c.to[i]])
+
+
+@pytest.mark.parametrize("depth,K,B", [([2000], 2000, 1), ([1500, 3, 900], 1999, 3)])
+def test_long(depth, K, B):
+    """Prompts long enough to be divided; the result does not depend on the run."""
+    c = Case(depth, K, 2, 1, 128, 128, strong=0.3)
+    before = c.states.clone()
+    out = c.attend()
+    assert int(c.status) == 0
+    c.check(out, before)
+    again, states = c.attend(), c.states.clone()
+    assert torch.equal(out, again)
+    c.states.copy_(before)
+    c.commit(None)
+    for i in range(B):
+        _, _, s, s_tol = c.want(i, before)
+        assert bool(((c.states[1, c.to[i]].cpu().double() - s).abs() <= s_tol).all())
+    del states
+
+
+def test_prompt_in_parts_is_the_prompt():
+    """One call, calls of 256 rows, and single tokens carry the same state."""
+    n, H, D = 600, 2, 64
+    c = Case([n - 1], n - 1, H, H, D, D, dtype=F32, start=[-1])
+    before = c.states.clone()
+    whole = c.attend()
+    st = LinearStates(1, H, H, D, D, 1, 256, F32)
+    out = torch.empty_like(whole[:n])
+    at = 0
+    for size in (256, 256, 60, 1, 1, 26):
+        rows = slice(at, at + size)
+        o = torch.empty((size, H, D), device=DEV)
+        st.attend(0, c.q[rows], c.k[rows], c.v[rows], c.decay[rows].to(DEV), o, update=True, K=size - 1)
+        out[rows] = o
+        at += size
+    assert at == n and int(st.status) == 0
+    o, o_tol, s, s_tol = c.want(0, before)
+    assert bool(((out.cpu().double() - o).abs() <= o_tol).all())
+    assert bool(((st.states[0, int(st.slots[0])].cpu().double() - s).abs() <= s_tol).all())
+
+
+def test_states_fork_in_a_graph():
+    """Parallel samples: a fork copies states, in a captured graph at every replay."""
+    H, D, B = 2, 64, 4
+    st = LinearStates(2, H, H, D, D, B, 3, BF16)
+    q, k, v = (torch.randn((B, H, D), device=DEV).to(BF16) for _ in range(3))
+    decay, out = torch.full((H,), -0.1, device=DEV), torch.empty((B, H, D), dtype=BF16, device=DEV)
+    parent = i32([0, 0, 2, -1])
+
+    def step():
+        for layer in range(2):
+            st.attend(layer, q, k, v, decay, out, update=True, K=0)
+        st.fork(parent)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        step()
+    model = torch.zeros((B, H, D, D), dtype=torch.float64)
+    kv = torch.einsum("bhd,bhe->bhde", k.cpu().double(), v.cpu().double())
+    for n in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        model = math.exp(-float(torch.tensor(0.1))) * model + kv
+        model = torch.stack([model[0], model[0], model[2], torch.zeros_like(model[0])])
+        for layer in range(2):
+            got = st.states[layer, st.slots.long()].cpu().double()
+            # three rows' products, each rounded and rescaled a few times
+            assert float((got - model).abs().max()) <= 16 * 2.0 ** -23 * float(model.abs().max())
+    assert int(st.status) == 0 and sorted(st.slots.tolist() + st._spare.tolist()) == list(range(2 * B))
+
+
+def test_another_stream():
+    c = Case([5, 90], 90, 2, 2, 64, 64)
+    before = c.states.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        out = c.attend()
+    side.synchronize()
+    c.check(out, before)
