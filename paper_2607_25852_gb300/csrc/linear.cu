@@ -16,7 +16,7 @@
 
 #include <algorithm>
 
-#include "linear.cuh"
+#include "linear_tc.cuh"
 #include "tensor_core.cuh"
 
 namespace spec {
@@ -301,10 +301,31 @@ bool linear_rows_ok(const void* p, int64_t stride, int64_t width, int64_t e) {
          stride <= (INT64_MAX >> 36);
 }
 
+// Segments' first states, and behind them their decays; at least 256 bytes.
+struct LinearGeometry {
+  LinearPlan plan;
+  size_t steps_off, bytes;
+};
+
+LinearGeometry linear_geometry(int B, int K, int q_heads, int kv_heads, int Dk, int Dv, int dtype) {
+  LinearGeometry g{};
+  g.plan.nseg = 1;
+  if (linear_tc_serves(K, Dk, Dv, dtype)) g.plan = linear_plan(B, K, q_heads, kv_heads);
+  g.plan.staged = g.plan.nseg > 1 || q_heads > kv_heads;
+  const size_t heads = linear_tc_serves(K, Dk, Dv, dtype) && g.plan.staged ? (size_t)B * kv_heads * g.plan.nseg : 0;
+  g.steps_off = heads * Dk * Dv * sizeof(float);
+  g.bytes = std::max<size_t>(256, g.steps_off + (heads * sizeof(long long) + 255) / 256 * 256);
+  return g;
+}
+
 int run_linear(const LinearLaunch& p, int dtype, void* ws, size_t ws_bytes, cudaStream_t stream) {
-  if (!ws || ws_bytes < spec_linear_workspace(p.rows.B, p.rows.K, p.Hq, p.H, p.Dk, p.Dv, dtype) ||
-      (reinterpret_cast<uintptr_t>(ws) & 255u) != 0)
-    return SPEC_ERR_WORKSPACE;
+  LinearGeometry g = linear_geometry(p.rows.B, p.rows.K, p.Hq, p.H, p.Dk, p.Dv, dtype);
+  if (!ws || ws_bytes < g.bytes || (reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return SPEC_ERR_WORKSPACE;
+  if (linear_tc_serves(p.rows.K, p.Dk, p.Dv, dtype)) {
+    g.plan.seg_state = static_cast<float*>(ws);
+    g.plan.seg_steps = reinterpret_cast<long long*>(static_cast<char*>(ws) + g.steps_off);
+    return launch_linear_tc(p, g.plan, stream) == cudaSuccess && cudaGetLastError() == cudaSuccess ? SPEC_OK : SPEC_ERR_CUDA;
+  }
   const cudaError_t err = dtype == SPEC_F32 ? launch_rows<float>(p, stream) : launch_rows<__nv_bfloat16>(p, stream);
   return err == cudaSuccess && cudaGetLastError() == cudaSuccess ? SPEC_OK : SPEC_ERR_CUDA;
 }
@@ -347,7 +368,9 @@ bool linear_common(LinearLaunch* p, const void* k, int64_t k_row_stride, const v
 extern "C" size_t spec_linear_workspace(int B, int K, int q_heads, int kv_heads, int key_dim, int value_dim,
                                         int dtype) {
   if (!spec::linear_shape_ok(B, K, q_heads, kv_heads, key_dim, value_dim, dtype)) return 0;
-  return 256;
+  // a commit's plan goes by the key-value heads
+  return std::max(spec::linear_geometry(B, K, q_heads, kv_heads, key_dim, value_dim, dtype).bytes,
+                  spec::linear_geometry(B, K, kv_heads, kv_heads, key_dim, value_dim, dtype).bytes);
 }
 
 extern "C" int spec_linear_attend(const void* q, int64_t q_row_stride, int q_heads, const void* k, int64_t k_row_stride,
