@@ -28,8 +28,12 @@
 // carries the state over them in order, and the segments' outputs then start from
 // their own states.
 //
-// Warps: 0 to 3 load (a chunk each in turn), 4 issues the MMAs, 5 sums the decays,
-// 8 to 11 make V', 12 to 19 keep the state, 20 to 27 make P and store O.
+// Warp 7 lists the chunks, with their decays summed up, in a ring of records that
+// all others go by.  2 and 3 load, 6 issues the MMAs, 8 to 11 make V', 12 to 19
+// keep the state, 0, 1, 4 and 5 (their lanes hold the scores) make P, 20 to 27
+// read O and store it by way of shared memory; where only states are made 20 to 23
+// make half of V'.  Loops stay rolled where registers allow: the roles' code
+// together does not fit the instruction caches otherwise.
 #include "attend_ring.cuh"
 #include "linear_tc.cuh"
 
@@ -38,10 +42,11 @@ namespace spec {
 namespace {
 
 constexpr int kHalf = kLinChunk * 128;  // 64 elements of a chunk's rows
-constexpr int kGRing = 4;               // chunks of decays
+constexpr int kRecords = 8;             // chunks listed ahead
 constexpr int kTS = 0, kTV = 128, kTU = 224, kTX = 352, kTO = 416;  // columns: S, V', U, scores and O1, O2
+constexpr int kTV1 = 352;                // the second V' where only states are made
 constexpr int kLinTmem = 512;
-constexpr int kOutThreads = 28 * 32, kSumThreads = 20 * 32;
+constexpr int kOutThreads = 28 * 32, kSumThreads = 24 * 32;
 
 enum LinPhase { kSegmentSums, kLastSegment, kAllSegments };
 
@@ -51,18 +56,31 @@ struct LinTcLaunch {
   int phase, heads;  // heads: items per request and segment
   long long items;
   int stages;
+  bool tma;  // the tensor maps are there
 };
 
-struct alignas(16) DecayChunk {
-  float hi[kLinChunk], lo[kLinChunk];      // L_i as a sum of two
-  float weight[kLinChunk], first[kLinChunk];  // exp(L_64 - L_j), exp(L_i)
-  float all;
+// A chunk: up to 64 rows of a request and head.  One without rows moves a state.
+struct alignas(16) Record {
+  float hi[kLinChunk], lo[kLinChunk];         // L_i as a sum of two
+  float weight[kLinChunk], first[kLinChunk];  // exp(L_64 - L_j), scale exp(L_i)
+  float row[kLinChunk / 2], column[kLinChunk / 2];  // exp(L_i - L_31) for i >= 32, exp(L_31 - L_j) for j < 32
+  float all;                                  // exp(L_64)
+  int rows, row0, h, hq;
+  int early;          // rows before position 0, right before row0
+  bool begins, ends;  // the item's first and last chunk
+  bool none;          // the list is over
+  const float* from;  // the item's first state; null: zeros
+  float* to;          // where its last goes; null: nowhere
 };
 
 struct LinControl {
-  uint64_t full[4], empty[4], g_full[kGRing], g_empty[kGRing];
-  uint64_t state_ready, weighted, sums, sums_read, scores, p_ready, out_ready, out_read, drained;
-  DecayChunk g[kGRing];
+  uint64_t full[4], empty[4], listed[kRecords], used[kRecords];
+  uint64_t state_ready, sums, sums_read, scores, p_ready, out_ready, out_read, drained;
+  // of even and odd chunks, as some warps may be a chunk ahead of others: V' there; where only states are made V'
+  // read; bad_row there
+  uint64_t weighted[2], read[2], noted[2];
+  uint64_t staged, stored;  // O in shared memory, and out of it
+  Record records[kRecords];
   int bad_row[2][128];
   int aborted;
   uint32_t tmem;
@@ -70,19 +88,18 @@ struct LinControl {
 
 // What a CTA works on at a time: rows of a request and head.
 struct LinItem {
-  const float* from;  // null: zeros
-  float* to;          // null: not stored
+  const float* from;
+  float* to;
   long long* steps;
-  int row0, n, h, hq;
-  int early;          // rows before position 0, right before row0
+  int row0, n, h, hq, early;
 };
 
-__device__ __forceinline__ bool lin_item(const LinTcLaunch& a, long long x, bool tell, LinItem* t) {
+__device__ __forceinline__ bool lin_item(const LinTcLaunch& a, long long x, LinItem* t) {
   const LinearLaunch& p = a.p;
   const int nseg = a.plan.nseg, seg = (int)(x % nseg), i = (int)(x / nseg / a.heads);
   const LinearRequest r = linear_request(p, i);
   if (!r.ok) {
-    if (tell && x == (long long)i * a.heads * nseg) report(p.status, SPEC_ERR_BAD_INPUT);
+    if (x == (long long)i * a.heads * nseg) report(p.status, SPEC_ERR_BAD_INPUT);
     return false;
   }
   const int rows = r.last - r.first, segs = max(1, (rows + a.plan.seg_rows - 1) / a.plan.seg_rows);
@@ -110,36 +127,57 @@ __device__ __forceinline__ bool lin_item(const LinTcLaunch& a, long long x, bool
   return true;
 }
 
-__device__ __forceinline__ void tmem_ld16(uint32_t addr, float (&v)[16]) {
-  uint32_t r[16];
+// 16 columns; not there before wait_ld().
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t (&r)[16]) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
-      "tcgen05.wait::ld.sync.aligned;"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
         "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
       : "r"(addr)
       : "memory");
+}
+__device__ __forceinline__ void tmem_ld8(uint32_t addr, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(addr)
+               : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_ld(uint32_t (&r)[N]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-  for (int k = 0; k < 16; ++k) v[k] = __uint_as_float(r[k]);
+  for (int k = 0; k < N; ++k) asm volatile("" : "+r"(r[k]));  // no use of them moves up
+}
+__device__ __forceinline__ void tmem_st8(uint32_t addr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(addr), "r"(r[0]), "r"(r[1]),
+               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st4(uint32_t addr, const uint32_t (&r)[4]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]),
+               "r"(r[3])
+               : "memory");
 }
 
 // Two numbers as bf16, rounded, and what is left of them.
-__device__ __forceinline__ uint32_t round_pair(float& x, float& y) {
+__device__ __forceinline__ uint32_t last_pair(f32x2 x) {
+  const float2 f = unpair(x);
   uint32_t b;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(b) : "f"(y), "f"(x));
-  const float2 rest = unpair(fma2(pair(bf16_lo(b), bf16_hi(b)), pair(-1.0f, -1.0f), pair(x, y)));
-  x = rest.x;
-  y = rest.y;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(b) : "f"(f.y), "f"(f.x));
   return b;
 }
-__device__ __forceinline__ uint32_t last_pair(float x, float y) {
-  uint32_t b;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(b) : "f"(y), "f"(x));
+__device__ __forceinline__ uint32_t round_pair(f32x2& x) {
+  const uint32_t b = last_pair(x);
+  x = fma2(pair(bf16_lo(b), bf16_hi(b)), pair(-1.0f, -1.0f), x);
   return b;
 }
+__device__ __forceinline__ f32x2 pair_of(uint32_t x, uint32_t y) { return pair(__uint_as_float(x), __uint_as_float(y)); }
 
 template <int DK, int DV, bool kOut>
-__global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1) linear_tc_kernel(const __grid_constant__ LinTcLaunch a) {
+__global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
+    linear_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                     const __grid_constant__ CUtensorMap tmV, const __grid_constant__ LinTcLaunch a) {
+  constexpr int kWeighers = kOut ? 4 : 8;  // warps that make V'
   constexpr int kKeyBytes = kLinChunk * DK * 2, kValueBytes = kLinChunk * DV * 2;
   constexpr int kKeyAt = kOut ? kKeyBytes : 0, kValueAt = kKeyAt + kKeyBytes, kStage = kValueAt + kValueBytes;
   extern __shared__ uint8_t smem_raw[];
@@ -147,20 +185,20 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1) linear_tc
   __shared__ LinControl ctl;
   const LinearLaunch& p = a.p;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const uint32_t ring = smem_u32(smem), pbuf = ring + a.stages * kStage;
-  uint8_t* pmem = smem + a.stages * kStage;
+  const uint32_t ring = smem_u32(smem);
+  uint8_t* pmem = smem + a.stages * kStage;  // P's two parts
+  uint8_t* omem = pmem + 2 * kHalf;          // O, row by row
 
   if (tid == 0) {
     for (int s = 0; s < a.stages; ++s) {
       mbar_init(&ctl.full[s], 1);
-      mbar_init(&ctl.empty[s], 1 + 4);
+      mbar_init(&ctl.empty[s], 1 + kWeighers);
     }
-    for (int s = 0; s < kGRing; ++s) {
-      mbar_init(&ctl.g_full[s], 1);
-      mbar_init(&ctl.g_empty[s], 4 + 8 + (kOut ? 8 : 0));
+    for (int s = 0; s < kRecords; ++s) {
+      mbar_init(&ctl.listed[s], 1);
+      mbar_init(&ctl.used[s], 2 + kWeighers + 8 + (kOut ? 4 + 8 : 0));
     }
     mbar_init(&ctl.state_ready, 8);
-    mbar_init(&ctl.weighted, 4);
     mbar_init(&ctl.sums, 1);
     mbar_init(&ctl.sums_read, 8);
     mbar_init(&ctl.scores, 1);
@@ -168,10 +206,17 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1) linear_tc
     mbar_init(&ctl.out_ready, 1);
     mbar_init(&ctl.out_read, 8);
     mbar_init(&ctl.drained, 1);
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(&ctl.weighted[s], kWeighers);
+      mbar_init(&ctl.noted[s], 4);
+      mbar_init(&ctl.read[s], 1);
+    }
+    mbar_init(&ctl.staged, 8);
+    mbar_init(&ctl.stored, 8);
     ctl.aborted = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 4) {
+  if (warp == 6) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl.tmem)),
                  "r"(kLinTmem)
                  : "memory");
@@ -202,63 +247,157 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1) linear_tc
   };
   bool ok = true;
   auto wait = [&](uint64_t* bar, uint32_t parity) { ok = __all_sync(0xFFFFFFFFu, ok && wait_one(bar, parity)); };
-  // calls f(item) for the CTA's items in turn
-  auto items = [&](bool tell, auto f) {
-    LinItem t;
-    for (long long x = blockIdx.x; ok && x < a.items; x += gridDim.x)
-      if (lin_item(a, x, tell, &t)) f(t);
+  // Record c, or null at the list's end; n counts those with rows, and a phase of
+  // most barriers is one of them.
+  uint32_t c = 0, n = 0;
+  auto next = [&]() -> const Record* {
+    wait(&ctl.listed[c % kRecords], c / kRecords);
+    const Record* r = &ctl.records[c % kRecords];
+    return ok && !r->none ? r : nullptr;
   };
-  uint32_t c = 0;  // chunks so far, of all items
-
-  if (warp < 4) {
-    // ---- loads: chunk c by warp c % stages ----
-    auto bring = [&](const __nv_bfloat16* from, int64_t stride, auto dim, uint32_t to, int rows) {
-      constexpr int kVecs = decltype(dim)::value / 8;
-#pragma unroll 4
-      for (int x = lane; x < kLinChunk * kVecs; x += 32) {
-        const int r = x / kVecs, v = x % kVecs;
-        const bool real = r < rows;
-        cp_async16(to + (v >> 3) * kHalf + r * 128 + (((v & 7) ^ (r & 7)) << 4), real ? from + r * stride + v * 8 : from, real);
-      }
-    };
-    if (warp < a.stages)
-      items(false, [&](const LinItem& t) {
-        const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(p.q) + t.row0 * p.q_row + (int64_t)t.hq * DK;
-        const __nv_bfloat16* k = static_cast<const __nv_bfloat16*>(p.k) + t.row0 * p.k_row + (int64_t)t.h * DK;
-        const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(p.v) + t.row0 * p.v_row + (int64_t)t.h * DV;
-        for (int x = 0; x < t.n && ok; x += kLinChunk, ++c) {
-          const int s = c % a.stages;
-          if (s != warp) continue;
-          const uint32_t use = c / a.stages;
-          if (use > 0) wait(&ctl.empty[s], use - 1);
+  auto done = [&]() {  // with record c, by the whole warp
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&ctl.used[c % kRecords]);
+    __syncwarp();
+    ++c;
+  };
+  // registers: 28 warps of 72 are split as 64, 64, 72, 104 twice, 48 twice per 4 warps; 24 of 80 as 40, 64, 80, 104
+  // twice, 80
+  const bool scorer = kOut && warp < 8 && (warp & 3) < 2;
+  if (warp < 8) {
+    if (kOut || warp >= 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    if (scorer) {
+      // ---- P: row d, half `set` of the columns ----
+      const int set = warp >> 2, quad = warp & 1, d = quad * 32 + lane;
+      const uint32_t from = tmem + kTX + ((uint32_t)(quad * 32) << 16) + 32 * set;
+      while (const Record* r = next()) {
+        if (r->rows > 0) {
+          wait(&ctl.scores, n);  // the last chunk's product has read P
           if (!ok) break;
-          const uint32_t at = ring + s * kStage;
-          const int rows = t.n - x;
-          if (kOut) bring(q + x * p.q_row, p.q_row, std::integral_constant<int, DK>{}, at, rows);
-          bring(k + x * p.k_row, p.k_row, std::integral_constant<int, DK>{}, at + kKeyAt, rows);
-          bring(v + x * p.v_row, p.v_row, std::integral_constant<int, DV>{}, at + kValueAt, rows);
-          asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
+          tc_fence_after();
+          const f32x2 minus = pair(-1.0f, -1.0f);
+          const f32x2 gh = pair(r->hi[d], r->hi[d]), gl = pair(r->lo[d], r->lo[d]);
+          const f32x2 mine = pair(r->row[lane], r->row[lane]);
+#pragma unroll 1
+          for (int half = 0; half < 2; ++half) {
+            const int j0 = 32 * set + 16 * half;
+            uint32_t w[16], hi[8], lo[8];
+            if (quad >= set) {
+              tmem_ld16(from + 16 * half, w);
+              wait_ld(w);
+            }
+            if (quad > set) {  // all columns before all rows: a product of two weights that are at most 1
+#pragma unroll
+              for (int y = 0; y < 8; y += 2) {
+                const float4 h = *reinterpret_cast<const float4*>(&r->column[j0 + 2 * y]);
+                f32x2 x = mul2(pair_of(w[2 * y], w[2 * y + 1]), mul2(mine, pair(h.x, h.y)));
+                hi[y] = round_pair(x), lo[y] = last_pair(x);
+                x = mul2(pair_of(w[2 * y + 2], w[2 * y + 3]), mul2(mine, pair(h.z, h.w)));
+                hi[y + 1] = round_pair(x), lo[y + 1] = last_pair(x);
+              }
+            } else if (quad == set) {
+#pragma unroll
+              for (int y = 0; y < 8; y += 2) {
+                const int j = j0 + 2 * y;
+                const float4 h = *reinterpret_cast<const float4*>(&r->hi[j]), l = *reinterpret_cast<const float4*>(&r->lo[j]);
+#pragma unroll
+                for (int z = 0; z < 2; ++z) {
+                  const float2 e = unpair(add2(fma2(z ? pair(h.z, h.w) : pair(h.x, h.y), minus, gh),
+                                               fma2(z ? pair(l.z, l.w) : pair(l.x, l.y), minus, gl)));
+                  const float s0 = __uint_as_float(w[2 * (y + z)]), s1 = __uint_as_float(w[2 * (y + z) + 1]);
+                  f32x2 x = pair(j + 2 * z <= d ? s0 * ex2_approx(e.x) : 0.0f, j + 2 * z + 1 <= d ? s1 * ex2_approx(e.y) : 0.0f);
+                  hi[y + z] = round_pair(x), lo[y + z] = last_pair(x);
+                }
+              }
+            } else {
+#pragma unroll
+              for (int y = 0; y < 8; ++y) hi[y] = lo[y] = 0u;
+            }
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              uint8_t* at = pmem + d * 128 + (((4 * set + 2 * half + y) ^ (d & 7)) << 4);
+              *reinterpret_cast<uint4*>(at) = make_uint4(hi[4 * y], hi[4 * y + 1], hi[4 * y + 2], hi[4 * y + 3]);
+              *reinterpret_cast<uint4*>(at + kHalf) = make_uint4(lo[4 * y], lo[4 * y + 1], lo[4 * y + 2], lo[4 * y + 3]);
+            }
+          }
+          tc_fence_before();
           proxy_fence();
           __syncwarp();
-          if (lane == 0) mbar_arrive(&ctl.full[s]);
+          if (lane == 0) mbar_arrive(&ctl.p_ready);
+          ++n;
         }
-      });
-  } else if (warp == 4) {
-    // ---- MMAs ----
-    if (elect_one()) {
-      constexpr uint32_t kScores = umma_idesc_bf16(128, kLinChunk);
-      constexpr uint32_t kOut1 = umma_idesc_bf16(128, kLinChunk) | kTransposeA;
-      constexpr uint32_t kSums = umma_idesc_bf16(128, DK) | kTransposeB;
-      auto need = [&](uint64_t* bar, uint32_t parity) { ok = ok && wait_one(bar, parity); };
-      LinItem t;
-      for (long long it = blockIdx.x; ok && it < a.items; it += gridDim.x) {
-        if (!lin_item(a, it, false, &t)) continue;
-        for (int x = 0; x < t.n && ok; x += kLinChunk, ++c) {
-          const int s = c % a.stages;
-          const uint32_t q = ring + s * kStage, k = q + kKeyAt, v = q + kValueAt;
-          need(&ctl.full[s], c / a.stages);
+        done();
+      }
+    } else if (warp == 2 || warp == 3) {
+      // ---- loads, every second chunk each: whole chunks by TMA, a request's last rows by plain copies, which put
+      // zeros behind them and read nothing there ----
+      auto copy = [&](const void* from, int64_t stride, int width, uint32_t to, int rows) {
+        const __nv_bfloat16* base = static_cast<const __nv_bfloat16*>(from);
+        const int vecs = width / 8;
+#pragma unroll 1
+        for (int x = lane; x < kLinChunk * vecs; x += 32) {
+          const int r = x / vecs, v = x % vecs;
+          const bool real = r < rows;
+          cp_async16(to + (v >> 3) * kHalf + r * 128 + (((v & 7) ^ (r & 7)) << 4), real ? base + r * stride + v * 8 : base, real);
+        }
+      };
+      auto bring = [&](const CUtensorMap* map, int width, int column, int row, int to, uint64_t* bar) {
+        for (int k = 0; k < width / 64; ++k) tma_load_2d(smem + to + k * kHalf, map, column + 64 * k, row, bar);
+      };
+      while (const Record* r = next()) {
+        const int rows = r->rows, row = r->row0, h = r->h, hq = r->hq;
+        const bool mine = rows > 0 ? (n & 1) == (uint32_t)(warp & 1) : warp == 2;
+        __syncwarp();
+        if (mine && lane == 0) mbar_arrive(&ctl.used[c % kRecords]);
+        __syncwarp();
+        ++c;
+        if (rows == 0) continue;
+        const int s = n % a.stages;
+        const uint32_t use = n / a.stages;
+        ++n;
+        if (!mine) continue;
+        if (use > 0) wait(&ctl.empty[s], use - 1);
+        if (!ok) break;
+        if (a.tma && rows == kLinChunk) {
+          if (lane == 0) {
+            mbar_expect_tx(&ctl.full[s], kStage);
+            if (kOut) bring(&tmQ, DK, hq * DK, row, s * kStage, &ctl.full[s]);
+            bring(&tmK, DK, h * DK, row, s * kStage + kKeyAt, &ctl.full[s]);
+            bring(&tmV, DV, h * DV, row, s * kStage + kValueAt, &ctl.full[s]);
+          }
+          __syncwarp();
+          continue;
+        }
+        const uint32_t at = ring + s * kStage;
+        if (kOut) copy(static_cast<const __nv_bfloat16*>(p.q) + row * p.q_row + (int64_t)hq * DK, p.q_row, DK, at, rows);
+        copy(static_cast<const __nv_bfloat16*>(p.k) + row * p.k_row + (int64_t)h * DK, p.k_row, DK, at + kKeyAt, rows);
+        copy(static_cast<const __nv_bfloat16*>(p.v) + row * p.v_row + (int64_t)h * DV, p.v_row, DV, at + kValueAt, rows);
+        asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
+        proxy_fence();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&ctl.full[s]);
+      }
+    } else if (warp == 6) {
+      // ---- MMAs ----
+      if (elect_one()) {
+        constexpr uint32_t kScores = umma_idesc_bf16(128, kLinChunk);
+        constexpr uint32_t kOut1 = umma_idesc_bf16(128, kLinChunk) | kTransposeA;
+        constexpr uint32_t kSums = umma_idesc_bf16(128, DK) | kTransposeB;
+        auto need = [&](uint64_t* bar, uint32_t parity) { ok = ok && wait_one(bar, parity); };
+        for (; ok; ++c) {
+          need(&ctl.listed[c % kRecords], c / kRecords);
+          if (!ok) break;
+          const int rows = ctl.records[c % kRecords].rows;
+          const bool none = ctl.records[c % kRecords].none;
+          mbar_arrive(&ctl.used[c % kRecords]);
+          if (none) break;
+          if (rows == 0) continue;
+          const int s = n % a.stages;
+          const uint32_t q = ring + s * kStage, k = q + kKeyAt, v = q + kValueAt, pbuf = ring + a.stages * kStage;
+          need(&ctl.full[s], n / a.stages);
           if (kOut) {
-            if (c > 0) need(&ctl.out_read, c - 1);
+            if (n > 0) need(&ctl.out_read, n - 1);
             if (!ok) break;
             tc_fence_after();
             // rows 64 to 127 of the scores are of what lies behind Q, and are not read
@@ -267,7 +406,7 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1) linear_tc
               umma_bf16(tmem + kTX, desc(lo_kq(q) + (((kk >> 2) * kHalf + (kk & 3) * 32) >> 4), kHiKQ),
                         desc(lo_kq(k) + (((kk >> 2) * kHalf + (kk & 3) * 32) >> 4), kHiKQ), kScores, kk > 0 ? 1u : 0u);
             umma_commit(&ctl.scores);
-            need(&ctl.state_ready, c);
+            need(&ctl.state_ready, n);
             if (!ok) break;
             tc_fence_after();
 #pragma unroll
@@ -277,17 +416,18 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1) linear_tc
                              kScores, kk > 0 ? 1u : 0u);
             }
           }
-          need(&ctl.weighted, c);
-          if (c > 0) need(&ctl.sums_read, c - 1);
+          need(&ctl.weighted[n & 1], n >> 1);
+          if (n > 0) need(&ctl.sums_read, n - 1);
           if (!ok) break;
           tc_fence_after();
 #pragma unroll
           for (int kk = 0; kk < 3 * (kLinChunk / 16); ++kk)
-            umma_bf16_tmem(tmem + kTU, tmem + kTV + 8 * kk, desc(lo_v(k, kHalf) + (kk % (kLinChunk / 16)) * (2048 >> 4), kHiV),
-                           kSums, kk > 0 ? 1u : 0u);
+            umma_bf16_tmem(tmem + kTU, tmem + (kOut || !(n & 1) ? kTV : kTV1) + 8 * kk,
+                           desc(lo_v(k, kHalf) + (kk % (kLinChunk / 16)) * (2048 >> 4), kHiV), kSums, kk > 0 ? 1u : 0u);
           umma_commit(&ctl.sums);
+          if (!kOut) umma_commit(&ctl.read[n & 1]);
           if (kOut) {
-            need(&ctl.p_ready, c);
+            need(&ctl.p_ready, n);
             if (!ok) break;
             tc_fence_after();
 #pragma unroll
@@ -299,234 +439,277 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1) linear_tc
             umma_commit(&ctl.out_ready);
           }
           umma_commit(&ctl.empty[s]);
+          ++n;
         }
+        // everything issued has completed before the tensor memory goes
+        umma_commit(&ctl.drained);
+        wait_phase(&ctl.drained, 0u, p.status);
       }
-      // everything issued has completed before the tensor memory goes
-      umma_commit(&ctl.drained);
-      wait_phase(&ctl.drained, 0u, p.status);
+      __syncwarp();
+    } else if (warp == 7) {
+      // ---- the list: a chunk's rows 2 lane and 2 lane + 1 per lane ----
+      LinItem t;
+      for (long long x = blockIdx.x; ok && x < a.items; x += gridDim.x) {
+        if (!lin_item(a, x, &t)) continue;
+        if (t.from) {  // the state is on its way to L2 while the items before are worked on
+          const char* line = reinterpret_cast<const char*>(t.from) + lane * 128;
+#pragma unroll 4
+          for (int y = 0; y < DK * DV * 4; y += 32 * 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(line + y));
+        }
+        long long total = 0;
+        const float* from = p.log_decay + t.row0 * p.decay_row + t.h;
+        auto row = [&](int r) { return r < t.n ? __ldg(from + r * p.decay_row) : 0.0f; };
+        float n0 = row(2 * lane), n1 = row(2 * lane + 1);
+        int x0 = 0;
+        do {
+          const long long d0 = decay_steps(n0, p.status), d1 = decay_steps(n1, p.status);
+          n0 = row(x0 + kLinChunk + 2 * lane), n1 = row(x0 + kLinChunk + 2 * lane + 1);
+          long long sum = d0 + d1;
+#pragma unroll
+          for (int o = 1; o < 32; o <<= 1) {
+            const long long y = __shfl_up_sync(0xFFFFFFFFu, sum, o);
+            if (lane >= o) sum += y;
+          }
+          const long long all = __shfl_sync(0xFFFFFFFFu, sum, 31), middle = __shfl_sync(0xFFFFFFFFu, sum, 15);  // L_64, L_31
+          total += all;
+          if (c >= kRecords) wait(&ctl.used[c % kRecords], c / kRecords - 1);
+          if (!ok) break;
+          Record& r = ctl.records[c % kRecords];
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const long long l = y ? sum : sum - d1;
+            const float hi = steps_float(l);
+            r.hi[2 * lane + y] = hi;
+            r.lo[2 * lane + y] = steps_float(l - __float2ll_rn(hi * 4294967296.0f));
+            r.weight[2 * lane + y] = exp2f(steps_float(all - l));
+            r.first[2 * lane + y] = p.scale * exp2f(hi);
+            (lane < 16 ? r.column[2 * lane + y] : r.row[2 * lane + y - 32]) = exp2f(steps_float(lane < 16 ? middle - l : l - middle));
+          }
+          if (lane == 0) {
+            r.all = exp2f(steps_float(all));
+            r.rows = min(kLinChunk, t.n - x0);
+            r.row0 = t.row0 + x0;
+            r.h = t.h;
+            r.hq = t.hq;
+            r.early = t.early;
+            r.begins = x0 == 0;
+            r.ends = x0 + kLinChunk >= t.n;
+            r.none = false;
+            r.from = t.from;
+            r.to = t.to;
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&ctl.listed[c % kRecords]);
+          __syncwarp();
+          ++c;
+          x0 += kLinChunk;
+        } while (x0 < t.n);
+        if (t.steps && lane == 0) *t.steps = total;
+      }
+      if (c >= kRecords) wait(&ctl.used[c % kRecords], c / kRecords - 1);
+      if (ok && lane == 0) {
+        ctl.records[c % kRecords].none = true;
+        mbar_arrive(&ctl.listed[c % kRecords]);
+      }
     }
-    __syncwarp();
-  } else if (warp == 5) {
-    // ---- decays: rows 2 lane and 2 lane + 1 of the chunk ----
-    items(true, [&](const LinItem& t) {
-      long long total = 0;
-      const float* from = p.log_decay + t.row0 * p.decay_row + t.h;
-      auto row = [&](int r) { return r < t.n ? __ldg(from + r * p.decay_row) : 0.0f; };
-      float n0 = row(2 * lane), n1 = row(2 * lane + 1);
-      for (int x = 0; x < t.n && ok; x += kLinChunk, ++c) {
-        const long long d0 = decay_steps(n0, p.status), d1 = decay_steps(n1, p.status);
-        n0 = row(x + kLinChunk + 2 * lane), n1 = row(x + kLinChunk + 2 * lane + 1);
-        long long sum = d0 + d1;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const long long y = __shfl_up_sync(0xFFFFFFFFu, sum, o);
-          if (lane >= o) sum += y;
-        }
-        const long long all = __shfl_sync(0xFFFFFFFFu, sum, 31);
-        total += all;
-        const int s = c % kGRing;
-        if (c >= kGRing) wait(&ctl.g_empty[s], c / kGRing - 1);
-        if (!ok) break;
-        DecayChunk& g = ctl.g[s];
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const long long l = y ? sum : sum - d1;
-          const float hi = steps_float(l);
-          g.hi[2 * lane + y] = hi;
-          g.lo[2 * lane + y] = steps_float(l - __float2ll_rn(hi * 4294967296.0f));
-          g.weight[2 * lane + y] = exp2f(steps_float(all - l));
-          g.first[2 * lane + y] = exp2f(hi);
-        }
-        if (lane == 0) g.all = exp2f(steps_float(all));
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&ctl.g_full[s]);
-      }
-      if (t.steps && lane == 0) *t.steps = total;
-    });
-  } else if (warp >= 8 && warp < 12) {
-    // ---- V': value `d` of the rows, weighted, in three parts ----
-    const int d = (warp & 3) * 32 + lane;
+  } else if (warp < 12 || (!kOut && warp >= 20)) {
+    // ---- V': value `d` of the rows (of half of them where there are two groups), weighted, in three parts ----
+    const int d = (warp & 3) * 32 + lane, group = warp >= 20;
     const bool mine = (warp & 3) * 32 < DV;
-    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, to = tmem + kTV + lanes;
-    items(false, [&](const LinItem& t) {
-      for (int x = 0; x < t.n && ok; x += kLinChunk, ++c) {
-        const int s = c % a.stages;
-        wait(&ctl.full[s], c / a.stages);
-        wait(&ctl.g_full[c % kGRing], c / kGRing);
-        if (c > 0) wait(&ctl.sums, c - 1);
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const int v8 = (d & 63) >> 3;
+    while (const Record* r = next()) {
+      if (r->rows > 0) {
+        const int s = n % a.stages;
+        const uint32_t to = tmem + (kOut || !(n & 1) ? kTV : kTV1) + lanes;
+        wait(&ctl.full[s], n / a.stages);
+        if (kOut && n > 0) wait(&ctl.sums, n - 1);
+        if (!kOut && n > 1) wait(&ctl.read[n & 1], (n >> 1) - 1);
         if (!ok) break;
         if (mine) {
           uint8_t* at = smem + s * kStage + kValueAt + (d >> 6) * kHalf + (d & 7) * 2;
-          const int v8 = (d & 63) >> 3;
-          const DecayChunk& g = ctl.g[c % kGRing];
-          float check = 0.0f;
+          f32x2 check = 0ull;
           tc_fence_after();
 #pragma unroll 1
-          for (int half = 0; half < 2; ++half) {
-            uint32_t part[3][16];
+          for (int g = kOut ? 0 : 4 * group; g < (kOut ? 8 : 4 * group + 4); ++g) {  // eight rows
+            uint32_t part[3][4];
 #pragma unroll
-            for (int y = 0; y < 16; ++y) {
-              const int r = half * 32 + 2 * y;
-              const float2 w = *reinterpret_cast<const float2*>(&g.weight[r]);
-              const uint16_t b0 = *reinterpret_cast<const uint16_t*>(at + r * 128 + ((v8 ^ (2 * y & 7)) << 4));
-              const uint16_t b1 = *reinterpret_cast<const uint16_t*>(at + (r + 1) * 128 + ((v8 ^ ((2 * y + 1) & 7)) << 4));
-              const float x0 = __uint_as_float((uint32_t)b0 << 16), x1 = __uint_as_float((uint32_t)b1 << 16);
-              check = fmaf(x0, 0.0f, fmaf(x1, 0.0f, check));
-              float y0 = x0 * w.x, y1 = x1 * w.y;
-              part[0][y] = round_pair(y0, y1);
-              part[1][y] = round_pair(y0, y1);
-              part[2][y] = last_pair(y0, y1);
+            for (int y = 0; y < 4; y += 2) {
+              const float4 w = *reinterpret_cast<const float4*>(&r->weight[8 * g + 2 * y]);
+#pragma unroll
+              for (int z = 0; z < 2; ++z) {
+                const int e = 2 * (y + z);
+                const uint16_t b0 = *reinterpret_cast<const uint16_t*>(at + (8 * g + e) * 128 + ((v8 ^ e) << 4));
+                const uint16_t b1 = *reinterpret_cast<const uint16_t*>(at + (8 * g + e + 1) * 128 + ((v8 ^ (e + 1)) << 4));
+                f32x2 x = pair(__uint_as_float((uint32_t)b0 << 16), __uint_as_float((uint32_t)b1 << 16));
+                if (kOut) check = fma2(x, 0ull, check);
+                x = mul2(x, z ? pair(w.z, w.w) : pair(w.x, w.y));
+                part[0][y + z] = round_pair(x);
+                part[1][y + z] = round_pair(x);
+                part[2][y + z] = last_pair(x);
+              }
             }
 #pragma unroll
-            for (int k = 0; k < 3; ++k) tmem_st16(to + 32 * k + 16 * half, part[k]);
+            for (int k = 0; k < 3; ++k) tmem_st4(to + 32 * k + 4 * g, part[k]);
           }
           if (kOut) {
             int bad = kLinChunk;
-            if (check != check) {  // rare: what is not finite goes, its first row is noted
-              for (int r = kLinChunk - 1; r >= 0; --r) {
-                uint16_t* e = reinterpret_cast<uint16_t*>(at + r * 128 + ((v8 ^ (r & 7)) << 4));
+            const float2 two = unpair(check);
+            if (two.x + two.y != 0.0f) {  // rare: what is not finite goes, its first row is noted
+#pragma unroll 1
+              for (int y = kLinChunk - 1; y >= 0; --y) {
+                uint16_t* e = reinterpret_cast<uint16_t*>(at + y * 128 + ((v8 ^ (y & 7)) << 4));
                 if (!bf16_not_finite(*e)) continue;
                 *e = 0;
-                bad = r;
+                bad = y;
               }
               proxy_fence();
             }
-            ctl.bad_row[c & 1][d] = bad;
+            ctl.bad_row[n & 1][d] = bad;
+            __syncwarp();
           }
           tmem_st_wait();
           tc_fence_before();
         }
         __syncwarp();
         if (lane == 0) {
-          mbar_arrive(&ctl.weighted);
+          mbar_arrive(&ctl.weighted[n & 1]);
+          if (kOut) mbar_arrive(&ctl.noted[n & 1]);
           mbar_arrive(&ctl.empty[s]);
-          mbar_arrive(&ctl.g_empty[c % kGRing]);
         }
+        ++n;
       }
-    });
-  } else if (warp >= 12 && warp < 20) {
-    // ---- the state: value d, keys of half kh ----
+      done();
+    }
+  } else if (warp < 20) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+    // ---- the state: value d, half kh of the keys ----
     constexpr int kKeys = DK / 2;
     const int d = (warp & 3) * 32 + lane, kh = (warp - 12) >> 2;
     const bool mine = (warp & 3) * 32 < DV;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t u = tmem + kTU + lanes + kh * kKeys, to = tmem + kTS + lanes + kh * (kKeys / 2);
-    float st[kKeys];
-    auto operand = [&]() {  // the state for the next chunk's product
-      if (mine) {
+    f32x2 st[kKeys / 2];
+    // 16 keys from k on as operand of the next chunk's product
+    auto operand = [&](int k) {
+      uint32_t hi[8], lo[8];
 #pragma unroll
-        for (int k = 0; k < kKeys; k += 32) {
-          uint32_t hi[16], lo[16];
-#pragma unroll
-          for (int y = 0; y < 16; ++y) {
-            float y0 = st[k + 2 * y], y1 = st[k + 2 * y + 1];
-            hi[y] = round_pair(y0, y1);
-            lo[y] = last_pair(y0, y1);
-          }
-          tmem_st16(to + k / 2, hi);
-          tmem_st16(to + DK / 2 + k / 2, lo);
-        }
-        tmem_st_wait();
-        tc_fence_before();
+      for (int y = 0; y < 8; ++y) {
+        f32x2 x = st[k / 2 + y];
+        hi[y] = round_pair(x);
+        lo[y] = last_pair(x);
       }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&ctl.state_ready);
+      tmem_st8(to + k / 2, hi);
+      tmem_st8(to + DK / 2 + k / 2, lo);
     };
-    items(false, [&](const LinItem& t) {
+    while (const Record* r = next()) {
+      const bool ends = r->ends;
+      if (r->begins) {
+        const float* from = r->from;
 #pragma unroll
-      for (int k = 0; k < kKeys; ++k) st[k] = t.from && mine ? __ldcg(t.from + (int64_t)(kh * kKeys + k) * DV + d) : 0.0f;
-      if (kOut && t.n > 0) operand();
-      for (int x = 0; x < t.n && ok; x += kLinChunk, ++c) {
-        wait(&ctl.g_full[c % kGRing], c / kGRing);
-        const float f = ctl.g[c % kGRing].all;
-        wait(&ctl.sums, c);  // O2 of the chunk, issued before, has read the operand as well
+        for (int k = 0; k < kKeys / 2; ++k) {
+          float x = 0.0f, y = 0.0f;
+          if (from && mine) {
+            x = __ldcg(from + (int64_t)(kh * kKeys + 2 * k) * DV + d);
+            y = __ldcg(from + (int64_t)(kh * kKeys + 2 * k + 1) * DV + d);
+          }
+          st[k] = pair(x, y);
+        }
+        if (kOut && r->rows > 0) {
+          __syncwarp();
+          if (mine) {
+#pragma unroll
+            for (int k = 0; k < kKeys; k += 16) operand(k);
+            tmem_st_wait();
+            tc_fence_before();
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&ctl.state_ready);
+          __syncwarp();
+        }
+      }
+      float* store = ends ? r->to : nullptr;
+      if (r->rows > 0) {
+        const f32x2 f = pair(r->all, r->all);
+        wait(&ctl.sums, n);  // O2 of the chunk, issued before, has read the operand as well
         if (!ok) break;
         tc_fence_after();
         if (mine) {
+          uint32_t w[2][16];
+          tmem_ld16(u, w[0]);
 #pragma unroll
           for (int k = 0; k < kKeys; k += 16) {
-            float w[16];
-            tmem_ld16(u + k, w);
+            uint32_t(&now)[16] = w[(k >> 4) & 1];
+            wait_ld(now);
+            if (k + 16 < kKeys) tmem_ld16(u + k + 16, w[((k >> 4) + 1) & 1]);
 #pragma unroll
-            for (int y = 0; y < 16; ++y) st[k + y] = fmaf(f, st[k + y], w[y]);
+            for (int y = 0; y < 8; ++y) st[k / 2 + y] = fma2(f, st[k / 2 + y], pair_of(now[2 * y], now[2 * y + 1]));
+            if (kOut && !ends) operand(k);
           }
+          if (kOut) tmem_st_wait();
           tc_fence_before();
         }
         __syncwarp();
         if (lane == 0) {
           mbar_arrive(&ctl.sums_read);
-          mbar_arrive(&ctl.g_empty[c % kGRing]);
+          if (kOut && !ends) mbar_arrive(&ctl.state_ready);
         }
-        if (kOut && x + kLinChunk < t.n) operand();
+        ++n;
       }
-      if (t.to && mine && ok) {
+      done();
+      if (store && mine) {
 #pragma unroll
-        for (int k = 0; k < kKeys; ++k) t.to[(int64_t)(kh * kKeys + k) * DV + d] = st[k];
+        for (int k = 0; k < kKeys / 2; ++k) {
+          const float2 x = unpair(st[k]);
+          store[(int64_t)(kh * kKeys + 2 * k) * DV + d] = x.x;
+          store[(int64_t)(kh * kKeys + 2 * k + 1) * DV + d] = x.y;
+        }
       }
-    });
-  } else if (kOut && warp >= 20) {
-    // ---- P, then O: half `set` of the columns ----
+    }
+  } else if (kOut) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+    // ---- O: value d, half `set` of the rows ----
     const int quad = warp & 3, set = (warp - 20) >> 2, d = quad * 32 + lane;
-    const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-    items(false, [&](const LinItem& t) {
-      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + ((int64_t)t.row0 * p.Hq + t.hq) * DV;
+    const uint32_t at = tmem + ((uint32_t)(quad * 32) << 16) + 32 * set;
+    constexpr int kVecs = DV / 8;
+    while (const Record* r = next()) {
       const int64_t out_row = (int64_t)p.Hq * DV;
-      for (long long x = tid - 20 * 32; x < (long long)t.early * (DV / 8); x += 256) {
-        const int r = (int)(x / (DV / 8)), v = (int)(x % (DV / 8));
-        *reinterpret_cast<uint4*>(out - (r + 1) * out_row + v * 8) = make_uint4(0u, 0u, 0u, 0u);
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + r->row0 * out_row + (int64_t)r->hq * DV;
+      if (r->begins && r->early > 0) {
+        for (long long x = tid - 20 * 32; x < (long long)r->early * kVecs; x += 256)
+          *reinterpret_cast<uint4*>(out - (x / kVecs + 1) * out_row + (x % kVecs) * 8) = make_uint4(0u, 0u, 0u, 0u);
+        __syncwarp();
       }
-      for (int x = 0; x < t.n && ok; x += kLinChunk, ++c) {
-        wait(&ctl.g_full[c % kGRing], c / kGRing);
-        const DecayChunk& g = ctl.g[c % kGRing];
-        wait(&ctl.scores, c);
-        if (!ok) break;
-        if (quad < 2) {  // row d of P
-          tc_fence_after();
-          uint32_t hi[16], lo[16];
-          if (quad >= set) {
-            float w[32];
-            tmem_ld32(tmem + kTX + lanes + 32 * set, w);
-            const float gh = g.hi[d], gl = g.lo[d];
-#pragma unroll
-            for (int y = 0; y < 16; ++y) {
-              const int j = 32 * set + 2 * y;
-              const float2 h = *reinterpret_cast<const float2*>(&g.hi[j]), l = *reinterpret_cast<const float2*>(&g.lo[j]);
-              float y0 = j <= d ? w[2 * y] * ex2_approx((gh - h.x) + (gl - l.x)) : 0.0f;
-              float y1 = j + 1 <= d ? w[2 * y + 1] * ex2_approx((gh - h.y) + (gl - l.y)) : 0.0f;
-              hi[y] = round_pair(y0, y1);
-              lo[y] = last_pair(y0, y1);
-            }
-          } else {
-#pragma unroll
-            for (int y = 0; y < 16; ++y) hi[y] = lo[y] = 0u;
-          }
-          tc_fence_before();
-#pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            uint8_t* at = pmem + d * 128 + (((4 * set + y) ^ (d & 7)) << 4);
-            *reinterpret_cast<uint4*>(at) = make_uint4(hi[4 * y], hi[4 * y + 1], hi[4 * y + 2], hi[4 * y + 3]);
-            *reinterpret_cast<uint4*>(at + kHalf) = make_uint4(lo[4 * y], lo[4 * y + 1], lo[4 * y + 2], lo[4 * y + 3]);
-          }
-          proxy_fence();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&ctl.p_ready);
-        }
-        wait(&ctl.weighted, c);  // whose finders note rows that are not finite
-        wait(&ctl.out_ready, c);
+      const int rows = r->rows;
+      if (rows > 0) {
+        wait(&ctl.noted[n & 1], n >> 1);
+        wait(&ctl.out_ready, n);
+        if (n > 0) wait(&ctl.stored, n - 1);
         if (!ok) break;
         if (quad * 32 < DV) {
           tc_fence_after();
-          const int bad = ctl.bad_row[c & 1][d];
+          const f32x2 scale = pair(p.scale, p.scale);
+          const int bad = ctl.bad_row[n & 1][d] - 32 * set;
+          uint16_t* to = reinterpret_cast<uint16_t*>(omem) + 32 * set * DV + d;
+#pragma unroll 1
+          for (int y = 0; y < 32; y += 8) {
+            uint32_t o1[8], o2[8];
+            tmem_ld8(at + kTX + y, o1);
+            tmem_ld8(at + kTO + y, o2);
+            wait_ld(o1);
+            wait_ld(o2);
 #pragma unroll
-          for (int y = 0; y < 32; y += 16) {
-            float o1[16], o2[16];
-            tmem_ld16(tmem + kTX + lanes + 32 * set + y, o1);
-            tmem_ld16(tmem + kTO + lanes + 32 * set + y, o2);
+            for (int k = 0; k < 8; k += 4) {
+              const float4 f = *reinterpret_cast<const float4*>(&r->first[32 * set + y + k]);
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
-              const int r = 32 * set + y + k;
-              const float o = p.scale * fmaf(g.first[r], o2[k], o1[k]);
-              if (x + r < t.n) out[(x + r) * out_row + d] = __float2bfloat16_rn(r >= bad ? __int_as_float(0x7FC00000) : o);
+              for (int z = 0; z < 2; ++z) {
+                const int e = k + 2 * z;
+                uint32_t b = last_pair(fma2(z ? pair(f.z, f.w) : pair(f.x, f.y), pair_of(o2[e], o2[e + 1]),
+                                            mul2(scale, pair_of(o1[e], o1[e + 1]))));
+                if (y + e + 1 >= bad) b = (y + e >= bad ? 0x7FC0u : b & 0xFFFFu) | 0x7FC00000u;
+                to[(y + e) * DV] = (uint16_t)b;
+                to[(y + e + 1) * DV] = (uint16_t)(b >> 16);
+              }
             }
           }
           tc_fence_before();
@@ -534,15 +717,31 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1) linear_tc
         __syncwarp();
         if (lane == 0) {
           mbar_arrive(&ctl.out_read);
-          mbar_arrive(&ctl.g_empty[c % kGRing]);
+          mbar_arrive(&ctl.staged);
         }
+        __syncwarp();
       }
-    });
+      done();
+      if (rows > 0) {
+        wait(&ctl.staged, n);
+        if (!ok) break;
+#pragma unroll
+        for (int y = 0; y < kLinChunk * kVecs / 256; ++y) {
+          const int e = y * 256 + tid - 20 * 32, x = e / kVecs, v = e % kVecs;
+          if (x < rows)
+            *reinterpret_cast<uint4*>(out + x * out_row + v * 8) = *reinterpret_cast<const uint4*>(omem + (x * kVecs + v) * 16);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&ctl.stored);
+        __syncwarp();
+        ++n;
+      }
+    }
   }
   __syncwarp();
   tc_fence_before();
   __syncthreads();
-  if (warp == 4) {
+  if (warp == 6) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kLinTmem) : "memory");
   }
@@ -584,6 +783,19 @@ __global__ void __launch_bounds__(256) linear_scan_kernel(const LinearLaunch p, 
   }
 }
 
+// Rows of `heads` heads of D, in boxes of 64 by 64.  Boxes are read only where all of their rows are a request's.
+bool make_rows_map(CUtensorMap* map, const void* base, long long rows, int64_t row_stride, int heads, int D) {
+  auto enc = tensor_map_encoder();
+  if (!enc || row_stride * 2 >= (1LL << 40)) return false;
+  cuuint64_t dims[2] = {(cuuint64_t)heads * D, (cuuint64_t)rows};
+  cuuint64_t strides[1] = {(cuuint64_t)row_stride * 2};
+  cuuint32_t box[2] = {64u, (cuuint32_t)kLinChunk}, estr[2] = {1u, 1u};
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             D == 64 ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B : CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int DK, int DV, bool kOut>
 cudaError_t launch_tc(const LinearLaunch& p, const LinearPlan& plan, int phase, cudaStream_t stream) {
   LinTcLaunch a{};
@@ -592,20 +804,24 @@ cudaError_t launch_tc(const LinearLaunch& p, const LinearPlan& plan, int phase, 
   a.phase = phase;
   a.heads = kOut ? p.Hq : p.H;
   a.items = (long long)p.rows.B * a.heads * plan.nseg;
-  constexpr int kStage = kLinChunk * 2 * ((kOut ? 2 : 1) * DK + DV), kP = kOut ? 2 * kHalf : 0;
+  const long long rows = (long long)p.rows.B * (p.rows.K + 1);
+  CUtensorMap tmQ{}, tmK{}, tmV{};
+  a.tma = (!kOut || make_rows_map(&tmQ, p.q, rows, p.q_row, p.Hq, DK)) && make_rows_map(&tmK, p.k, rows, p.k_row, p.H, DK) &&
+          make_rows_map(&tmV, p.v, rows, p.v_row, p.H, DV);
+  constexpr int kStage = kLinChunk * 2 * ((kOut ? 2 : 1) * DK + DV), kP = kOut ? 4 * kHalf : 0;  // P, and O
   static std::atomic<int> known;
   int fixed;
   cudaError_t err = static_smem(linear_tc_kernel<DK, DV, kOut>, known, &fixed);
   if (err != cudaSuccess) return err;
-  // dynamic shared memory from a 1024-byte boundary; 8 KB behind the last stage may be read (and not used)
-  const int room = 227 * 1024 - (fixed + 1023) / 1024 * 1024 - 1024 - kP - kHalf;
+  // dynamic shared memory from a 1024-byte boundary; what is read behind the last stage, and not used, is P's
+  const int room = 227 * 1024 - (fixed + 1023) / 1024 * 1024 - 1024 - kP;
   a.stages = std::min(4, room / kStage);
-  const size_t smem = (size_t)a.stages * kStage + kP + kHalf + 1024;
+  const size_t smem = (size_t)a.stages * kStage + kP + 1024;
   static std::atomic<size_t> raised[kMaxDevices];
   err = raise_smem(linear_tc_kernel<DK, DV, kOut>, smem, raised);
   if (err != cudaSuccess) return err;
   return launch_after_previous(linear_tc_kernel<DK, DV, kOut>, dim3((unsigned)std::min<long long>(a.items, device_sms())),
-                               dim3(kOut ? kOutThreads : kSumThreads), smem, stream, a);
+                               dim3(kOut ? kOutThreads : kSumThreads), smem, stream, tmQ, tmK, tmV, a);
 }
 
 template <int DK, int DV>

@@ -283,6 +283,31 @@ def test_long(depth, K, B):
     del states
 
 
+@pytest.mark.parametrize("shape", [(64, 32, 64, 64), (48, 48, 128, 128)])
+@pytest.mark.parametrize("Dk,Dv", [(128, 64), (64, 64), (64, 128), (128, 128)])
+def test_every_run_is_the_same(Dk, Dv):
+    """Warps that take part in a chunk and warps that do not (Dv = 64) keep step, call after call."""
+    c = Case([2500, 2000, 1111], 2500, 16, 16, Dk, Dv, start=[-1, 1, 2])
+    c.to = [4, 5, 6]
+    out, first = c.attend(), c.states.clone()
+    for _ in range(40):
+        again = c.attend()
+        c.commit(None)
+        assert int(c.status) == 0
+        assert torch.equal(out[:-1], again[:-1])
+        # both calls' states: the same sums in the same order
+        assert torch.equal(first, c.states)
+
+
+def test_many_heads(shape):
+    """More requests' heads than the device has SMs: each works on several in turn, of all lengths."""
+    c = Case([200, 64, 0, 130, 63, 191], 200, *shape)
+    before = c.states.clone()
+    out = c.attend()
+    assert int(c.status) == 0
+    c.check(out, before)
+
+
 def test_prompt_in_parts_is_the_prompt():
     """One call, calls of 256 rows, and single tokens carry the same state."""
     n, H, D = 600, 2, 64
