@@ -63,7 +63,6 @@ struct LinTcLaunch {
 struct alignas(16) Record {
   float hi[kLinChunk], lo[kLinChunk];         // L_i as a sum of two
   float weight[kLinChunk], first[kLinChunk];  // exp(L_64 - L_j), scale exp(L_i)
-  float row[kLinChunk / 2], column[kLinChunk / 2];  // exp(L_i - L_31) for i >= 32, exp(L_31 - L_j) for j < 32
   float all;                                  // exp(L_64)
   int rows, row0, h, hq;
   int early;          // rows before position 0, right before row0
@@ -231,17 +230,14 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
 
   // Waits end after a second without progress, or when another role has given up.
   auto wait_one = [&](uint64_t* bar, uint32_t parity) {
-    if (mbar_try_wait(bar, parity & 1u)) return true;
-    const uint64_t t0 = global_ns();
-    for (uint32_t it = 1; !mbar_try_wait(bar, parity & 1u); ++it) {
-      if ((it & 63u) == 0u) {
-        if (*(volatile int*)&ctl.aborted) return false;
-        if (global_ns() - t0 > 1000000000ull) {
-          report(p.status, SPEC_ERR_TIMEOUT);
-          *(volatile int*)&ctl.aborted = 1;
-          return false;
-        }
-      }
+    uint32_t began = 0;
+    for (uint32_t it = 0; !mbar_try_wait(bar, parity & 1u); ++it) {
+      if ((it & 63u) != 63u) continue;
+      uint32_t now;
+      asm volatile("mov.u32 %0, %%globaltimer_lo;" : "=r"(now));  // in ns
+      if (it == 63u) began = now;
+      if (now - began > 1000000000u) *(volatile int*)&ctl.aborted = 1;
+      if (*(volatile int*)&ctl.aborted) return false;
     }
     return true;
   };
@@ -278,25 +274,13 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
           tc_fence_after();
           const f32x2 minus = pair(-1.0f, -1.0f);
           const f32x2 gh = pair(r->hi[d], r->hi[d]), gl = pair(r->lo[d], r->lo[d]);
-          const f32x2 mine = pair(r->row[lane], r->row[lane]);
 #pragma unroll 1
           for (int half = 0; half < 2; ++half) {
             const int j0 = 32 * set + 16 * half;
             uint32_t w[16], hi[8], lo[8];
-            if (quad >= set) {
+            if (quad >= set) {  // (columns 32 to 63 are behind rows 0 to 31)
               tmem_ld16(from + 16 * half, w);
               wait_ld(w);
-            }
-            if (quad > set) {  // all columns before all rows: a product of two weights that are at most 1
-#pragma unroll
-              for (int y = 0; y < 8; y += 2) {
-                const float4 h = *reinterpret_cast<const float4*>(&r->column[j0 + 2 * y]);
-                f32x2 x = mul2(pair_of(w[2 * y], w[2 * y + 1]), mul2(mine, pair(h.x, h.y)));
-                hi[y] = round_pair(x), lo[y] = last_pair(x);
-                x = mul2(pair_of(w[2 * y + 2], w[2 * y + 3]), mul2(mine, pair(h.z, h.w)));
-                hi[y + 1] = round_pair(x), lo[y + 1] = last_pair(x);
-              }
-            } else if (quad == set) {
 #pragma unroll
               for (int y = 0; y < 8; y += 2) {
                 const int j = j0 + 2 * y;
@@ -385,6 +369,20 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
         constexpr uint32_t kOut1 = umma_idesc_bf16(128, kLinChunk) | kTransposeA;
         constexpr uint32_t kSums = umma_idesc_bf16(128, DK) | kTransposeB;
         auto need = [&](uint64_t* bar, uint32_t parity) { ok = ok && wait_one(bar, parity); };
+        // four products over 16 each: A and B in shared memory so many bytes apart, or A in tensor memory
+        auto four = [&](int to, uint32_t x, int x_step, uint32_t y, int y_step, uint32_t kind, bool fresh) {
+          const uint32_t x0 = x_step == 2048 ? lo_v(x, kHalf) : lo_kq(x), y0 = lo_kq(y);
+#pragma unroll
+          for (int m = 0; m < 4; ++m)
+            umma_bf16(tmem + to, desc(x0 + (m * x_step >> 4), x_step == 2048 ? kHiV : kHiKQ), desc(y0 + (m * y_step >> 4), kHiKQ),
+                      kind, m > 0 || !fresh ? 1u : 0u);
+        };
+        auto four_tmem = [&](int to, int x, uint32_t y0, int y_step, uint32_t kind, bool fresh) {
+#pragma unroll
+          for (int m = 0; m < 4; ++m)
+            umma_bf16_tmem(tmem + to, tmem + x + 8 * m, desc(y0 + (m * y_step >> 4), y_step == 2048 ? kHiV : kHiKQ), kind,
+                           m > 0 || !fresh ? 1u : 0u);
+        };
         for (; ok; ++c) {
           need(&ctl.listed[c % kRecords], c / kRecords);
           if (!ok) break;
@@ -401,41 +399,31 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
             if (!ok) break;
             tc_fence_after();
             // rows 64 to 127 of the scores are of what lies behind Q, and are not read
-#pragma unroll
-            for (int kk = 0; kk < DK / 16; ++kk)
-              umma_bf16(tmem + kTX, desc(lo_kq(q) + (((kk >> 2) * kHalf + (kk & 3) * 32) >> 4), kHiKQ),
-                        desc(lo_kq(k) + (((kk >> 2) * kHalf + (kk & 3) * 32) >> 4), kHiKQ), kScores, kk > 0 ? 1u : 0u);
+#pragma unroll 1
+            for (int h = 0; h < DK / 64; ++h) four(kTX, q + h * kHalf, 32, k + h * kHalf, 32, kScores, h == 0);
             umma_commit(&ctl.scores);
             need(&ctl.state_ready, n);
             if (!ok) break;
             tc_fence_after();
-#pragma unroll
-            for (int kk = 0; kk < 2 * (DK / 16); ++kk) {  // the upper parts, then the rests
-              const int y = kk % (DK / 16);
-              umma_bf16_tmem(tmem + kTO, tmem + kTS + 8 * kk, desc(lo_kq(q) + (((y >> 2) * kHalf + (y & 3) * 32) >> 4), kHiKQ),
-                             kScores, kk > 0 ? 1u : 0u);
-            }
+#pragma unroll 1
+            for (int h = 0; h < 2 * (DK / 64); ++h)  // the upper parts, then the rests
+              four_tmem(kTO, kTS + 32 * h, lo_kq(q + (h % (DK / 64)) * kHalf), 32, kScores, h == 0);
           }
           need(&ctl.weighted[n & 1], n >> 1);
           if (n > 0) need(&ctl.sums_read, n - 1);
           if (!ok) break;
           tc_fence_after();
-#pragma unroll
-          for (int kk = 0; kk < 3 * (kLinChunk / 16); ++kk)
-            umma_bf16_tmem(tmem + kTU, tmem + (kOut || !(n & 1) ? kTV : kTV1) + 8 * kk,
-                           desc(lo_v(k, kHalf) + (kk % (kLinChunk / 16)) * (2048 >> 4), kHiV), kSums, kk > 0 ? 1u : 0u);
+#pragma unroll 1
+          for (int h = 0; h < 3; ++h)
+            four_tmem(kTU, (kOut || !(n & 1) ? kTV : kTV1) + 32 * h, lo_v(k, kHalf), 2048, kSums, h == 0);
           umma_commit(&ctl.sums);
           if (!kOut) umma_commit(&ctl.read[n & 1]);
           if (kOut) {
             need(&ctl.p_ready, n);
             if (!ok) break;
             tc_fence_after();
-#pragma unroll
-            for (int kk = 0; kk < 2 * (kLinChunk / 16); ++kk) {
-              const int y = kk % (kLinChunk / 16);
-              umma_bf16(tmem + kTX, desc(lo_v(v, kHalf) + y * (2048 >> 4), kHiV),
-                        desc(lo_kq(pbuf + (kk / (kLinChunk / 16)) * kHalf) + ((y * 32) >> 4), kHiKQ), kOut1, kk > 0 ? 1u : 0u);
-            }
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) four(kTX, v, 2048, pbuf + h * kHalf, 32, kOut1, h == 0);
             umma_commit(&ctl.out_ready);
           }
           umma_commit(&ctl.empty[s]);
@@ -470,12 +458,12 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
             const long long y = __shfl_up_sync(0xFFFFFFFFu, sum, o);
             if (lane >= o) sum += y;
           }
-          const long long all = __shfl_sync(0xFFFFFFFFu, sum, 31), middle = __shfl_sync(0xFFFFFFFFu, sum, 15);  // L_64, L_31
+          const long long all = __shfl_sync(0xFFFFFFFFu, sum, 31);  // L_64
           total += all;
           if (c >= kRecords) wait(&ctl.used[c % kRecords], c / kRecords - 1);
           if (!ok) break;
           Record& r = ctl.records[c % kRecords];
-#pragma unroll
+#pragma unroll 1
           for (int y = 0; y < 2; ++y) {
             const long long l = y ? sum : sum - d1;
             const float hi = steps_float(l);
@@ -483,7 +471,6 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
             r.lo[2 * lane + y] = steps_float(l - __float2ll_rn(hi * 4294967296.0f));
             r.weight[2 * lane + y] = exp2f(steps_float(all - l));
             r.first[2 * lane + y] = p.scale * exp2f(hi);
-            (lane < 16 ? r.column[2 * lane + y] : r.row[2 * lane + y - 32]) = exp2f(steps_float(lane < 16 ? middle - l : l - middle));
           }
           if (lane == 0) {
             r.all = exp2f(steps_float(all));
@@ -741,6 +728,7 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
   __syncwarp();
   tc_fence_before();
   __syncthreads();
+  if (tid == 0 && ctl.aborted) report(p.status, SPEC_ERR_TIMEOUT);
   if (warp == 6) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kLinTmem) : "memory");

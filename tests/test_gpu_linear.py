@@ -283,7 +283,6 @@ def test_long(depth, K, B):
     del states
 
 
-@pytest.mark.parametrize("shape", [(64, 32, 64, 64), (48, 48, 128, 128)])
 @pytest.mark.parametrize("Dk,Dv", [(128, 64), (64, 64), (64, 128), (128, 128)])
 def test_every_run_is_the_same(Dk, Dv):
     """Warps that take part in a chunk and warps that do not (Dv = 64) keep step, call after call."""
@@ -299,6 +298,7 @@ def test_every_run_is_the_same(Dk, Dv):
         assert torch.equal(first, c.states)
 
 
+@pytest.mark.parametrize("shape", [(64, 32, 64, 64), (48, 48, 128, 128)])
 def test_many_heads(shape):
     """More requests' heads than the device has SMs: each works on several in turn, of all lengths."""
     c = Case([200, 64, 0, 130, 63, 191], 200, *shape)
