@@ -310,9 +310,9 @@ struct LinearGeometry {
 LinearGeometry linear_geometry(int B, int K, int q_heads, int kv_heads, int Dk, int Dv, int dtype) {
   LinearGeometry g{};
   g.plan.nseg = 1;
-  if (linear_tc_serves(K, Dk, Dv, dtype)) g.plan = linear_plan(B, K, q_heads, kv_heads);
+  if (linear_tc_serves(B, K, q_heads, Dk, Dv, dtype)) g.plan = linear_plan(B, K, q_heads, kv_heads);
   g.plan.staged = g.plan.nseg > 1 || q_heads > kv_heads;
-  const size_t heads = linear_tc_serves(K, Dk, Dv, dtype) && g.plan.staged ? (size_t)B * kv_heads * g.plan.nseg : 0;
+  const size_t heads = linear_tc_serves(B, K, q_heads, Dk, Dv, dtype) && g.plan.staged ? (size_t)B * kv_heads * g.plan.nseg : 0;
   g.steps_off = heads * Dk * Dv * sizeof(float);
   g.bytes = std::max<size_t>(256, g.steps_off + (heads * sizeof(long long) + 255) / 256 * 256);
   return g;
@@ -321,7 +321,7 @@ LinearGeometry linear_geometry(int B, int K, int q_heads, int kv_heads, int Dk, 
 int run_linear(const LinearLaunch& p, int dtype, void* ws, size_t ws_bytes, cudaStream_t stream) {
   LinearGeometry g = linear_geometry(p.rows.B, p.rows.K, p.Hq, p.H, p.Dk, p.Dv, dtype);
   if (!ws || ws_bytes < g.bytes || (reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return SPEC_ERR_WORKSPACE;
-  if (linear_tc_serves(p.rows.K, p.Dk, p.Dv, dtype)) {
+  if (linear_tc_serves(p.rows.B, p.rows.K, p.Hq, p.Dk, p.Dv, dtype)) {
     g.plan.seg_state = static_cast<float*>(ws);
     g.plan.seg_steps = reinterpret_cast<long long*>(static_cast<char*>(ws) + g.steps_off);
     return launch_linear_tc(p, g.plan, stream) == cudaSuccess && cudaGetLastError() == cudaSuccess ? SPEC_OK : SPEC_ERR_CUDA;

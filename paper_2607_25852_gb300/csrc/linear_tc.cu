@@ -53,9 +53,8 @@ enum LinPhase { kSegmentSums, kLastSegment, kAllSegments };
 struct LinTcLaunch {
   LinearLaunch p;
   LinearPlan plan;
-  int phase, heads;  // heads: items per request and segment
-  long long items;
-  int stages;
+  int phase;
+  uint32_t heads, items;  // heads: items per request and segment
   bool tma;  // the tensor maps are there
 };
 
@@ -85,6 +84,13 @@ struct LinControl {
   uint32_t tmem;
 };
 
+// Chunks in shared memory at a time (P and O take 32 KB of its 227, the rest 14).
+constexpr int lin_stage_bytes(int DK, int DV, bool out) { return kLinChunk * 2 * ((out ? 2 : 1) * DK + DV); }
+constexpr int lin_smem(int DK, int DV, bool out, int stages) {
+  return stages * lin_stage_bytes(DK, DV, out) + (out ? 4 * kHalf : 0) + 1024;
+}
+constexpr int lin_stages(int DK, int DV, bool out) { return lin_smem(DK, DV, out, 4) <= 213 * 1024 ? 4 : 3; }
+
 // What a CTA works on at a time: rows of a request and head.
 struct LinItem {
   const float* from;
@@ -93,25 +99,26 @@ struct LinItem {
   int row0, n, h, hq, early;
 };
 
-__device__ __forceinline__ bool lin_item(const LinTcLaunch& a, long long x, LinItem* t) {
+__device__ __forceinline__ bool lin_item(const LinTcLaunch& a, uint32_t x, LinItem* t) {
   const LinearLaunch& p = a.p;
-  const int nseg = a.plan.nseg, seg = (int)(x % nseg), i = (int)(x / nseg / a.heads);
+  const uint32_t nseg = a.plan.nseg, y = x / nseg, i = y / a.heads;
+  const int seg = (int)(x - y * nseg);
   const LinearRequest r = linear_request(p, i);
   if (!r.ok) {
-    if (x == (long long)i * a.heads * nseg) report(p.status, SPEC_ERR_BAD_INPUT);
+    if (x == i * a.heads * nseg) report(p.status, SPEC_ERR_BAD_INPUT);
     return false;
   }
   const int rows = r.last - r.first, segs = max(1, (rows + a.plan.seg_rows - 1) / a.plan.seg_rows);
   if (seg >= segs || (a.phase == kSegmentSums && seg == segs - 1) || (a.phase == kLastSegment && seg != segs - 1))
     return false;
   const int per = a.heads / p.H;  // 1 where states alone are made
-  t->hq = (int)(x / nseg - (long long)i * a.heads);
+  t->hq = (int)(y - i * a.heads);
   t->h = t->hq / per;
   const int first = r.first + seg * a.plan.seg_rows;
   t->row0 = r.row0 + first;
   t->n = min(a.plan.seg_rows, r.last - first);
   t->early = seg == 0 ? r.first : 0;
-  const int64_t size = (int64_t)p.Dk * p.Dv, head = (int64_t)(i * (int64_t)p.H + t->h) * nseg;
+  const int64_t size = (int64_t)p.Dk * p.Dv, head = ((int64_t)i * p.H + t->h) * nseg;
   t->steps = nullptr;
   if (a.phase == kSegmentSums) {
     t->from = nullptr;
@@ -179,17 +186,18 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
   constexpr int kWeighers = kOut ? 4 : 8;  // warps that make V'
   constexpr int kKeyBytes = kLinChunk * DK * 2, kValueBytes = kLinChunk * DV * 2;
   constexpr int kKeyAt = kOut ? kKeyBytes : 0, kValueAt = kKeyAt + kKeyBytes, kStage = kValueAt + kValueBytes;
+  constexpr int kStages = lin_stages(DK, DV, kOut);
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   __shared__ LinControl ctl;
   const LinearLaunch& p = a.p;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t ring = smem_u32(smem);
-  uint8_t* pmem = smem + a.stages * kStage;  // P's two parts
+  uint8_t* pmem = smem + kStages * kStage;  // P's two parts
   uint8_t* omem = pmem + 2 * kHalf;          // O, row by row
 
   if (tid == 0) {
-    for (int s = 0; s < a.stages; ++s) {
+    for (int s = 0; s < kStages; ++s) {
       mbar_init(&ctl.full[s], 1);
       mbar_init(&ctl.empty[s], 1 + kWeighers);
     }
@@ -337,8 +345,8 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
         __syncwarp();
         ++c;
         if (rows == 0) continue;
-        const int s = n % a.stages;
-        const uint32_t use = n / a.stages;
+        const int s = n % kStages;
+        const uint32_t use = n / kStages;
         ++n;
         if (!mine) continue;
         if (use > 0) wait(&ctl.empty[s], use - 1);
@@ -391,9 +399,9 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
           mbar_arrive(&ctl.used[c % kRecords]);
           if (none) break;
           if (rows == 0) continue;
-          const int s = n % a.stages;
-          const uint32_t q = ring + s * kStage, k = q + kKeyAt, v = q + kValueAt, pbuf = ring + a.stages * kStage;
-          need(&ctl.full[s], n / a.stages);
+          const int s = n % kStages;
+          const uint32_t q = ring + s * kStage, k = q + kKeyAt, v = q + kValueAt, pbuf = ring + kStages * kStage;
+          need(&ctl.full[s], n / kStages);
           if (kOut) {
             if (n > 0) need(&ctl.out_read, n - 1);
             if (!ok) break;
@@ -437,7 +445,7 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
     } else if (warp == 7) {
       // ---- the list: a chunk's rows 2 lane and 2 lane + 1 per lane ----
       LinItem t;
-      for (long long x = blockIdx.x; ok && x < a.items; x += gridDim.x) {
+      for (uint32_t x = blockIdx.x; ok && x < a.items; x += gridDim.x) {
         if (!lin_item(a, x, &t)) continue;
         if (t.from) {  // the state is on its way to L2 while the items before are worked on
           const char* line = reinterpret_cast<const char*>(t.from) + lane * 128;
@@ -507,9 +515,9 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
     const int v8 = (d & 63) >> 3;
     while (const Record* r = next()) {
       if (r->rows > 0) {
-        const int s = n % a.stages;
+        const int s = n % kStages;
         const uint32_t to = tmem + (kOut || !(n & 1) ? kTV : kTV1) + lanes;
-        wait(&ctl.full[s], n / a.stages);
+        wait(&ctl.full[s], n / kStages);
         if (kOut && n > 0) wait(&ctl.sums, n - 1);
         if (!kOut && n > 1) wait(&ctl.read[n & 1], (n >> 1) - 1);
         if (!ok) break;
@@ -590,66 +598,61 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
       tmem_st8(to + DK / 2 + k / 2, lo);
     };
     while (const Record* r = next()) {
-      const bool ends = r->ends;
-      if (r->begins) {
-        const float* from = r->from;
+      const bool ends = r->ends, begins = r->begins;
+      if (begins) {
+        const float* from = mine ? r->from : nullptr;
+        if (from) {
+          from += kh * kKeys * DV + d;
 #pragma unroll
-        for (int k = 0; k < kKeys / 2; ++k) {
-          float x = 0.0f, y = 0.0f;
-          if (from && mine) {
-            x = __ldcg(from + (int64_t)(kh * kKeys + 2 * k) * DV + d);
-            y = __ldcg(from + (int64_t)(kh * kKeys + 2 * k + 1) * DV + d);
-          }
-          st[k] = pair(x, y);
+          for (int k = 0; k < kKeys / 2; ++k) st[k] = pair(__ldcg(from + 2 * k * DV), __ldcg(from + (2 * k + 1) * DV));
+        } else {
+#pragma unroll
+          for (int k = 0; k < kKeys / 2; ++k) st[k] = 0ull;
         }
-        if (kOut && r->rows > 0) {
+      }
+      float* store = ends && mine ? r->to : nullptr;
+      if (r->rows > 0) {
+        const f32x2 f = pair(r->all, r->all);
+        // once for the first chunk's operand, once for the chunk's sums (and the next one's operand)
+#pragma unroll 1
+        for (int pass = kOut && begins ? 0 : 1; pass < 2; ++pass) {
+          if (pass) wait(&ctl.sums, n);  // O2 of the chunk, issued before, has read the operand as well
+          if (!ok) break;
+          const bool give = kOut && !(pass && ends);
           __syncwarp();
           if (mine) {
+            tc_fence_after();
 #pragma unroll
-            for (int k = 0; k < kKeys; k += 16) operand(k);
-            tmem_st_wait();
+            for (int k = 0; k < kKeys; k += 16) {
+              if (pass) {
+                uint32_t w[16];
+                tmem_ld16(u + k, w);
+                wait_ld(w);
+#pragma unroll
+                for (int y = 0; y < 8; ++y) st[k / 2 + y] = fma2(f, st[k / 2 + y], pair_of(w[2 * y], w[2 * y + 1]));
+              }
+              if (give) operand(k);
+            }
+            if (give) tmem_st_wait();
             tc_fence_before();
           }
           __syncwarp();
-          if (lane == 0) mbar_arrive(&ctl.state_ready);
-          __syncwarp();
-        }
-      }
-      float* store = ends ? r->to : nullptr;
-      if (r->rows > 0) {
-        const f32x2 f = pair(r->all, r->all);
-        wait(&ctl.sums, n);  // O2 of the chunk, issued before, has read the operand as well
-        if (!ok) break;
-        tc_fence_after();
-        if (mine) {
-          uint32_t w[2][16];
-          tmem_ld16(u, w[0]);
-#pragma unroll
-          for (int k = 0; k < kKeys; k += 16) {
-            uint32_t(&now)[16] = w[(k >> 4) & 1];
-            wait_ld(now);
-            if (k + 16 < kKeys) tmem_ld16(u + k + 16, w[((k >> 4) + 1) & 1]);
-#pragma unroll
-            for (int y = 0; y < 8; ++y) st[k / 2 + y] = fma2(f, st[k / 2 + y], pair_of(now[2 * y], now[2 * y + 1]));
-            if (kOut && !ends) operand(k);
+          if (lane == 0) {
+            if (pass) mbar_arrive(&ctl.sums_read);
+            if (give) mbar_arrive(&ctl.state_ready);
           }
-          if (kOut) tmem_st_wait();
-          tc_fence_before();
         }
-        __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(&ctl.sums_read);
-          if (kOut && !ends) mbar_arrive(&ctl.state_ready);
-        }
+        if (!ok) break;
         ++n;
       }
       done();
-      if (store && mine) {
+      if (store) {
+        store += kh * kKeys * DV + d;
 #pragma unroll
         for (int k = 0; k < kKeys / 2; ++k) {
           const float2 x = unpair(st[k]);
-          store[(int64_t)(kh * kKeys + 2 * k) * DV + d] = x.x;
-          store[(int64_t)(kh * kKeys + 2 * k + 1) * DV + d] = x.y;
+          store[2 * k * DV] = x.x;
+          store[(2 * k + 1) * DV] = x.y;
         }
       }
     }
@@ -791,24 +794,16 @@ cudaError_t launch_tc(const LinearLaunch& p, const LinearPlan& plan, int phase, 
   a.plan = plan;
   a.phase = phase;
   a.heads = kOut ? p.Hq : p.H;
-  a.items = (long long)p.rows.B * a.heads * plan.nseg;
+  a.items = (uint32_t)p.rows.B * a.heads * plan.nseg;  // below 2^31: linear_tc_serves()
   const long long rows = (long long)p.rows.B * (p.rows.K + 1);
   CUtensorMap tmQ{}, tmK{}, tmV{};
   a.tma = (!kOut || make_rows_map(&tmQ, p.q, rows, p.q_row, p.Hq, DK)) && make_rows_map(&tmK, p.k, rows, p.k_row, p.H, DK) &&
           make_rows_map(&tmV, p.v, rows, p.v_row, p.H, DV);
-  constexpr int kStage = kLinChunk * 2 * ((kOut ? 2 : 1) * DK + DV), kP = kOut ? 4 * kHalf : 0;  // P, and O
-  static std::atomic<int> known;
-  int fixed;
-  cudaError_t err = static_smem(linear_tc_kernel<DK, DV, kOut>, known, &fixed);
-  if (err != cudaSuccess) return err;
-  // dynamic shared memory from a 1024-byte boundary; what is read behind the last stage, and not used, is P's
-  const int room = 227 * 1024 - (fixed + 1023) / 1024 * 1024 - 1024 - kP;
-  a.stages = std::min(4, room / kStage);
-  const size_t smem = (size_t)a.stages * kStage + kP + 1024;
+  constexpr size_t smem = lin_smem(DK, DV, kOut, lin_stages(DK, DV, kOut));
   static std::atomic<size_t> raised[kMaxDevices];
-  err = raise_smem(linear_tc_kernel<DK, DV, kOut>, smem, raised);
+  const cudaError_t err = raise_smem(linear_tc_kernel<DK, DV, kOut>, smem, raised);
   if (err != cudaSuccess) return err;
-  return launch_after_previous(linear_tc_kernel<DK, DV, kOut>, dim3((unsigned)std::min<long long>(a.items, device_sms())),
+  return launch_after_previous(linear_tc_kernel<DK, DV, kOut>, dim3((unsigned)std::min<uint32_t>(a.items, device_sms())),
                                dim3(kOut ? kOutThreads : kSumThreads), smem, stream, tmQ, tmK, tmV, a);
 }
 

@@ -25,8 +25,8 @@ struct LinearPlan {
   long long* seg_steps;  // [B * H][nseg]
 };
 
-inline bool linear_tc_serves(int K, int Dk, int Dv, int dtype) {
-  return dtype == SPEC_BF16 && (Dk == 64 || Dk == 128) && (Dv == 64 || Dv == 128) && K + 1 > kLinTcRows;
+inline bool linear_tc_serves(int B, int K, int q_heads, int Dk, int Dv, int dtype) {
+  return (long long)B * q_heads * kLinMaxSegments < (1LL << 31) && dtype == SPEC_BF16 && (Dk == 64 || Dk == 128) && (Dv == 64 || Dv == 128) && K + 1 > kLinTcRows;
 }
 
 // The number of segments with the least work on the busiest SM, in chunks: a
