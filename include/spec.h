@@ -894,7 +894,7 @@ int spec_linear_commit(const void* k, int64_t k_row_stride, const void* v, int64
  *   entries of largest logit above -inf, in that order, with their ln p.
  * Row j is the one that spec_verify's out_tokens[i][j] was drawn from or verified
  * on, so its arrays serve as they are.
- *   logits, row_offsets, depth  as spec_verify (logits device or host-mapped).
+ *   logits, row_offsets, depth  as spec_verify, with logits on the device.
  *   tokens          device int32 [B, K+1]; -1: no token (logprob -inf, rank 0).
  *                   Another value outside [0, V) counts as -1 and sets
  *                   SPEC_ERR_BAD_INPUT.

@@ -765,7 +765,7 @@ def spec_logprobs(logits, tokens, B, K, V, logprob_out, ws, temperature=1.0, row
     entropy = _floats(entropy_out, cells, "entropy_out")
     top, top_lp = _ints(top_tokens_out, cells * n, "top_tokens_out"), _floats(top_logprobs_out, cells * n,
                                                                              "top_logprobs_out")
-    _here(tokens, accepted_len, row_offsets, depth, status, logprob_out, rank_out, entropy_out, top_tokens_out,
+    _here(logits, tokens, accepted_len, row_offsets, depth, status, logprob_out, rank_out, entropy_out, top_tokens_out,
           top_logprobs_out, ws)
     code = library().spec_logprobs(
         logits.data_ptr(), kind, offsets, depths, given, taken, B, K, V, temperature, n, lp, rank, entropy,

@@ -140,6 +140,13 @@ __device__ __forceinline__ f32x2 mul2(f32x2 x, f32x2 y) {
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
   return r;
 }
+// Two numbers as bf16, rounded.
+__device__ __forceinline__ uint32_t last_pair(f32x2 x) {
+  const float2 f = unpair(x);
+  uint32_t b;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(b) : "f"(f.y), "f"(f.x));
+  return b;
+}
 __device__ __forceinline__ float max3(float x, float y, float z) {
   float r;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));

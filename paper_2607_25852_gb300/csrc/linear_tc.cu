@@ -166,12 +166,6 @@ __device__ __forceinline__ void tmem_st4(uint32_t addr, const uint32_t (&r)[4]) 
 }
 
 // Two numbers as bf16, rounded, and what is left of them.
-__device__ __forceinline__ uint32_t last_pair(f32x2 x) {
-  const float2 f = unpair(x);
-  uint32_t b;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(b) : "f"(f.y), "f"(f.x));
-  return b;
-}
 __device__ __forceinline__ uint32_t round_pair(f32x2& x) {
   const uint32_t b = last_pair(x);
   x = fma2(pair(bf16_lo(b), bf16_hi(b)), pair(-1.0f, -1.0f), x);
