@@ -6,28 +6,29 @@
 //   s = sum_v 2^d_v,  e = sum_v d_v 2^d_v,
 //   ln p_v = ln 2 (c2 l_v - M - log2 s),  H = ln 2 (log2 s - e / s),
 // whose terms are non-negative but for M's rounding, so nothing cancels.  (Where M
-// is so large that the logits' own spacing is tens of binary orders, d_v is c2 (l_v - m).)
+// is beyond thousands of binary orders d_v is c2 (l_v - m), whose first step is exact near m.)
 // A token's rank counts the entries that come before it (greater, or equal with a
 // lower index); its logit is read first, so the count goes along, and only through
 // the vectors whose largest element reaches it.
 //
 // The alternatives come along too.  Each thread notes the largest element of each of
-// its 16-byte vectors.  After at most 16 rounds of 1,024 vectors, n values that are
-// known to be there (the four largest of each warp's lanes' maxima) give a bound
-// that the n-th best cannot be below; the few vectors that reach it are looked
-// through again, and what reaches it goes to a list as a 64-bit key that orders by
-// value and then by lower index.  A list that overflows, as many equal logits make
-// it, is replaced by n searches for the next best key.  So the order in which
-// threads append does not show.
+// its 16-byte vectors.  After at most 8 rounds (of 512 vectors; a span), the n-th
+// largest of the threads' maxima is a bound that the n-th best cannot be below; the
+// few vectors that reach it are looked through again, and what reaches it goes to a
+// list as a 64-bit key that orders by value and then by lower index.  A list that
+// overflows, as many equal logits make it, is replaced by n searches for the next
+// best key.  So the order in which lanes append does not show.
 //
 // The rows that are asked for, which only the device knows (of 64 requests of up to
 // 17 rows a third may be), are laid end to end and cut into equal shares, one per
 // CTA: a CTA has the end of a row, whole rows and the beginning of one.  So all
-// are busy to the end, and their pieces end at different times.  A warp of
-// its own brings the rounds by bulk copies into a ring in shared memory, ahead
-// across pieces.  The last
-// CTA to arrive at a row joins its pieces, in order.  Bound by HBM for many rows,
-// by the launch and three round trips for few.
+// are busy to the end, and their pieces end at different times.  Four warps go
+// through the rounds and do nothing else; one brings them by bulk copies into a
+// ring in shared memory; one looks for the best of a span and ends a piece while
+// the four are at the next: done by the four themselves, with barriers, that took
+// as long as the rounds did.  The last CTA to arrive at a row joins its pieces, in
+// order.  Bound by HBM and the exponentials for many rows, by the launch and three
+// round trips for few.
 #include <cfloat>
 #include <cmath>
 
@@ -40,18 +41,18 @@ namespace spec {
 
 namespace {
 
-constexpr int kLogThreads = 256, kLogWarps = kLogThreads / 32;
+constexpr int kLogWarps = 4, kLogThreads = kLogWarps * 32;  // that go through the rounds
 constexpr int kVecs = 4;             // 16-byte vectors per thread and round
 constexpr int kRoundVecs = kLogThreads * kVecs;
-constexpr int kLogStages = 4;        // rounds in shared memory
-constexpr int kCtasPerSm = 2;
-constexpr int kMaxPieces = 64;       // of a row
+constexpr int kLogStages = 3;        // rounds in shared memory
+constexpr int kCtasPerSm = 4;
+constexpr int kMaxPieces = 22;       // of a row
 constexpr int kMinShare = 256;       // vectors per CTA
-constexpr int kMaxListed = 1024;     // requests up to which only the rows asked for are gone through
-constexpr int kSpan = 16;            // rounds whose best are looked for together
-constexpr float kHuge = 1073741824.0f;  // 2^30: of |M|
-constexpr int kListCap = kMaxPieces * SPEC_MAX_TOP;  // what a join may have to look at
-constexpr int kListFull = 512;       // what a round may append to
+constexpr int kListCap = kMaxPieces * SPEC_MAX_TOP;  // keys that are looked at together: of all pieces, or of a span
+constexpr int kFoundCap = 256;       // vectors of a span
+constexpr int kMaxListed = 512;      // requests up to which only the rows asked for are gone through
+constexpr int kSpan = 8;             // rounds whose best are looked for together
+constexpr float kHuge = 8192.0f;     // of |M|
 typedef unsigned long long Key;      // 0: none
 
 struct alignas(16) LogPartial {
@@ -64,7 +65,7 @@ struct LogLaunch {
   const int32_t *tokens, *accepted;
   RowLayout rows;
   int V, n;
-  float c2;
+  float c2, inv_c2;
   float *logprob, *entropy, *top_logprobs;
   int32_t *rank, *top_tokens, *status;
   LogPartial* part;    // [row + CTA]: a row's pieces are consecutive CTAs', so no two are alike
@@ -113,6 +114,44 @@ __device__ __forceinline__ float largest<__nv_bfloat16>(const uint4& v) {
   const uint32_t m = max_pair_nan(max_pair_nan(v.x, v.y), max_pair_nan(v.z, v.w));
   return fmax_nan(bf16_lo(m), bf16_hi(m));
 }
+// Elements 2 k and 2 k + 1, not below `least` (in both types; a NaN becomes that too).
+template <typename T>
+__device__ __forceinline__ f32x2 pair_from(const uint4& v, int k, float least, uint32_t);
+template <>
+__device__ __forceinline__ f32x2 pair_from<float>(const uint4& v, int k, float least, uint32_t) {
+  return pair(fmaxf(element<float>(v, 2 * k), least), fmaxf(element<float>(v, 2 * k + 1), least));
+}
+template <>
+__device__ __forceinline__ f32x2 pair_from<__nv_bfloat16>(const uint4& v, int k, float, uint32_t least) {
+  uint32_t r;
+  asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(k == 0 ? v.x : k == 1 ? v.y : k == 2 ? v.z : v.w), "r"(least));
+  return pair(bf16_lo(r), bf16_hi(r));
+}
+// How many elements of a vector are at least `least`, a value of T.
+template <typename T>
+__device__ __forceinline__ int count_from(const uint4& v, float least);
+template <>
+__device__ __forceinline__ int count_from<float>(const uint4& v, float least) {
+  int n = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) n += element<float>(v, k) >= least ? 1 : 0;
+  return n;
+}
+template <>
+__device__ __forceinline__ int count_from<__nv_bfloat16>(const uint4& v, float least) {
+  const __nv_bfloat162 b = __float2bfloat162_rn(least);
+  auto two = [&](uint32_t w) { return __hge2(*reinterpret_cast<const __nv_bfloat162*>(&w), b); };  // 1 or 0 each
+  const __nv_bfloat162 n = __hadd2(__hadd2(two(v.x), two(v.y)), __hadd2(two(v.z), two(v.w)));
+  return (int)(__low2float(n) + __high2float(n));
+}
+// The next number of T above x (a number of T).
+template <typename T>
+__device__ __forceinline__ float next_above(float x) {
+  constexpr int kStep = sizeof(T) == 4 ? 1 : 0x10000;
+  const int b = __float_as_int(x);
+  return __int_as_float(x == 0.0f ? kStep : x > 0.0f ? min(b + kStep, 0x7F800000) : b - kStep);
+}
+
 // The difference of the references of two sums, at most 0 for b the larger.
 __device__ __forceinline__ float reference_step(float a, float b, float c2) {
   const float x = __fmul_rn(a, c2), y = __fmul_rn(b, c2);
@@ -137,34 +176,36 @@ __device__ __forceinline__ float warp_sum(float x) {
   return x;
 }
 
-// The n best of `count` keys in `list` to out[0 .. n), the best first.
-static __device__ __noinline__ void select_keys(const Key* list, int count, int n, Key* out) {
-  for (int x = threadIdx.x; x < n; x += kLogThreads)
-    if (x >= count) out[x] = 0;
-  for (int x = threadIdx.x; x < count; x += kLogThreads) {
+// The n best of `count` keys in `list` to out[0 .. n), the best first; one warp, which has written them.
+__device__ __forceinline__ void select_keys(const Key* list, int count, int n, Key* out) {
+  const int lane = threadIdx.x & 31;
+  __syncwarp();
+  if (lane < n) out[lane] = 0;
+  __syncwarp();
+#pragma unroll 1
+  for (int x = lane; x < count; x += 32) {
     const Key k = list[x];
     int before = 0;
 #pragma unroll 4
     for (int y = 0; y < count; ++y) before += list[y] > k ? 1 : 0;
     if (before < n) out[before] = k;
   }
+  __syncwarp();
 }
 
 struct LogShared {
   alignas(128) uint4 ring[kLogStages][kRoundVecs];
-  union {
-    uint16_t tops[kSpan * kVecs][kLogThreads];  // each thread's vectors' largest, as bf16, rounded up
-    Key joined[kListCap];
-  };
-  Key list[kListFull];
+  // two spans' vectors' largest, as bf16 rounded up, and threads' largest
+  alignas(16) uint16_t tops[2][kSpan * kVecs][kLogThreads];
+  float most[2][kLogThreads];
+  Key list[kListCap];
   Key best[SPEC_MAX_TOP];
-  Key warp_key[kLogWarps];
-  uint64_t full[kLogStages], empty[kLogStages];
+  uint64_t full[kLogStages], empty[kLogStages], span_full[2], span_empty[2];
   int asked[kMaxListed + 1];  // rows asked for of the requests before
-  float warp_top[kLogWarps * 4];
-  float m[kLogWarps], s[kLogWarps], e[kLogWarps];
-  int before[kLogWarps], sums[kLogWarps];
-  int count, last, aborted;
+  int found[kFoundCap];
+  float m[2][kLogWarps], s[2][kLogWarps], e[2][kLogWarps];  // of a piece that ends with the span
+  int before[2][kLogWarps], sums[kLogWarps];
+  int count, vectors, aborted;
 };
 
 // Rows of request i that are asked for; -1 where its arrays do not fit together.
@@ -187,22 +228,23 @@ __device__ __forceinline__ void write_nothing(const LogLaunch& p, long long r, i
   }
 }
 
-// The row's outputs from its sums and its best keys (in shared memory).
+// The row's outputs from its sums and its best keys, by one warp.
 __device__ __forceinline__ void write_row(const LogLaunch& p, long long r, float m, float s, float e, int before,
                                           int token, float given, const Key* best) {
+  const int lane = threadIdx.x & 31;
   if (before < 0 || m == -INFINITY) {
-    if (threadIdx.x == 0) report(p.status, SPEC_ERR_BAD_INPUT);
-    if (threadIdx.x < 32) write_nothing(p, r, threadIdx.x);
+    if (lane == 0) report(p.status, SPEC_ERR_BAD_INPUT);
+    write_nothing(p, r, lane);
     return;
   }
   constexpr float kLn2 = 0.693147180559945309f;
   const float norm = log2f(s), c2 = p.c2;
-  for (int x = threadIdx.x; x < p.n; x += kLogThreads) {
+  for (int x = lane; x < p.n; x += 32) {
     const Key k = best[x];
     if (p.top_tokens) p.top_tokens[r * p.n + x] = k ? key_index(k) : -1;
     if (p.top_logprobs) p.top_logprobs[r * p.n + x] = k ? kLn2 * (above_reference(key_value(k), m, c2) - norm) : -INFINITY;
   }
-  if (threadIdx.x == 0) {
+  if (lane == 0) {
     p.logprob[r] = token >= 0 ? kLn2 * (above_reference(given, m, c2) - norm) : -INFINITY;
     if (p.rank) p.rank[r] = token >= 0 ? before + 1 : 0;
     if (p.entropy) p.entropy[r] = kLn2 * (norm - e / s);
@@ -238,12 +280,13 @@ struct LogPiece {
   const T* row;
   int r, a;        // place in the outputs; place among the rows that are gone through
   int skip;        // elements of other rows in the row's first vector
-  int begin, end;  // vectors; nothing where the row is not asked for
+  int begin, end;  // vectors; none where the row is not asked for
   bool asked;
+  long long next;  // the next piece's position
 };
 
 template <typename T>
-__global__ void __launch_bounds__(kLogThreads + 32, kCtasPerSm) logprobs_kernel(const LogLaunch p) {
+__global__ void __launch_bounds__(kLogThreads + 64, kCtasPerSm) logprobs_kernel(const LogLaunch p) {
   constexpr int W = 16 / (int)sizeof(T);
   extern __shared__ uint4 smem_raw[];
   LogShared& sh = *reinterpret_cast<LogShared*>((reinterpret_cast<uintptr_t>(smem_raw) + 127) & ~(uintptr_t)127);
@@ -253,10 +296,15 @@ __global__ void __launch_bounds__(kLogThreads + 32, kCtasPerSm) logprobs_kernel(
       mbar_init(&sh.full[s], 1);
       mbar_init(&sh.empty[s], kLogWarps);
     }
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(&sh.span_full[s], kLogWarps);
+      mbar_init(&sh.span_empty[s], 1);
+    }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     sh.aborted = 0;
     sh.asked[0] = 0;
     sh.count = 0;
+    sh.vectors = 0;
   }
   pdl_wait_prerequisites();
   pdl_launch_dependents();
@@ -282,10 +330,8 @@ __global__ void __launch_bounds__(kLogThreads + 32, kCtasPerSm) logprobs_kernel(
         if (w < warp) sum += sh.sums[w];
       }
       if (i < B && tid < kLogThreads) sh.asked[i + 1] = rows + sum;
-      int all = 0;
 #pragma unroll
-      for (int w = 0; w < kLogWarps; ++w) all += sh.sums[w];
-      rows += all;
+      for (int w = 0; w < kLogWarps; ++w) rows += sh.sums[w];
       __syncthreads();
     }
   } else {
@@ -307,50 +353,44 @@ __global__ void __launch_bounds__(kLogThreads + 32, kCtasPerSm) logprobs_kernel(
       j = a - i * K1;
     }
   };
-  // ---- the others' outputs ----
-  const int cells = max(p.n, 1);
-  for (long long x = (long long)blockIdx.x * kLogThreads + tid; tid < kLogThreads && x < (long long)B * K1 * cells; x += (long long)gridDim.x * kLogThreads) {
-    const int r = (int)(x / cells), i = r / K1, j = r - i * K1;
-    const int n = listed ? sh.asked[i + 1] - sh.asked[i] : asked_rows(p, i);
-    if (n < 0 && j == 0) report(p.status, SPEC_ERR_BAD_INPUT);
-    if (j >= n) write_nothing(p, r, (int)(x - (long long)r * cells));
-  }
+
   // ---- this CTA's share: vectors at .. share_end - 1 of the rows laid end to end ----
   const int nv = (int)(((long long)p.V + 2 * W - 2) / W);  // a row's, its ends as misaligned as can be
   const long long total = (long long)rows * nv;
+  auto divide = [&](long long x, long long by) {  // (few pieces need 64 bits)
+    return total < (1LL << 31) ? (int)((uint32_t)x / (uint32_t)by) : (int)(x / by);
+  };
   const long long share = max(max((total + gridDim.x - 1) / gridDim.x, (long long)(nv / (kMaxPieces - 2) + 1)), (long long)kMinShare);
-  const long long share_end = min((blockIdx.x + 1) * share, total);
+  const long long share_begin = blockIdx.x * share, share_end = min(share_begin + share, total);
   // the piece at `pos`; false past the share
   auto piece_at = [&](long long pos, LogPiece<T>& t) {
     if (pos >= share_end) return false;
-    t.a = (int)(pos / nv);
+    t.a = divide(pos, nv);
     int i, j;
     place(t.a, i, j);
     t.r = i * K1 + j;
     t.begin = (int)(pos - (long long)t.a * nv);
-    t.end = (int)min((long long)nv, t.begin + (share_end - pos));
+    t.next = pos + min((long long)(nv - t.begin), share_end - pos);
     t.asked = listed || j < asked_rows(p, i);
     const int row0 = p.rows.row_offsets ? __ldg(p.rows.row_offsets + i) : i * K1;
     t.row = static_cast<const T*>(p.logits) + (t.asked ? (long long)(row0 + j) * p.V : 0);
     t.skip = (int)((reinterpret_cast<uintptr_t>(t.row) & 15u) / sizeof(T));
+    // a row may have one vector fewer than nv
+    t.end = t.asked ? min(t.begin + (int)(t.next - pos), (int)(((long long)p.V + t.skip + W - 1) / W)) : t.begin;
     return true;
   };
-  // its last vector: a row may have one fewer than nv
-  auto piece_end = [&](const LogPiece<T>& t) {
-    return t.asked ? min(t.end, (int)(((long long)p.V + t.skip + W - 1) / W)) : t.begin;
-  };
+  LogPiece<T> t;
 
   if (warp == kLogWarps) {
-    // ---- rounds, ahead of the others ----
+    // ---- brings the rounds, ahead of the others ----
     if (lane == 0) {
-      LogPiece<T> t;
       uint32_t brought = 0;
       bool ok = true;
-      for (long long pos = blockIdx.x * share; ok && piece_at(pos, t); pos += t.end - t.begin) {
+      for (long long pos = share_begin; ok && piece_at(pos, t); pos = t.next) {
         // whole vectors of the row; its ends are read where they are used
-        const int end = piece_end(t), inner = t.skip ? 1 : 0, outer = (int)(((long long)p.V + t.skip) / W);
-        for (int at = t.begin; at < end; at += kRoundVecs, ++brought) {
-          const int lo = max(at, inner), hi = min(min(at + kRoundVecs, end), outer), s = brought % kLogStages;
+        const int inner = t.skip ? 1 : 0, outer = (int)(((long long)p.V + t.skip) / W);
+        for (int at = t.begin; at < t.end; at += kRoundVecs, ++brought) {
+          const int lo = max(at, inner), hi = min(min(at + kRoundVecs, t.end), outer), s = brought % kLogStages;
           ok = brought < kLogStages || wait_phase(&sh.empty[s], (brought / kLogStages - 1) & 1u, p.status);
           if (!ok) break;
           const uint32_t bytes = hi > lo ? (uint32_t)(hi - lo) * 16u : 0u;
@@ -364,7 +404,7 @@ __global__ void __launch_bounds__(kLogThreads + 32, kCtasPerSm) logprobs_kernel(
         }
       }
       if (!ok) {
-        sh.aborted = 1;
+        *(volatile int*)&sh.aborted = 1;
         // the copies in flight end before the CTA does
         for (uint32_t y = brought - kLogStages; y < brought; ++y) wait_phase(&sh.full[y % kLogStages], (y / kLogStages) & 1u, p.status);
       }
@@ -372,311 +412,316 @@ __global__ void __launch_bounds__(kLogThreads + 32, kCtasPerSm) logprobs_kernel(
     return;
   }
 
-  uint32_t used = 0;
-  bool gone = false;
-  LogPiece<T> t, next{};
-  long long pos = blockIdx.x * share;
-  bool more = piece_at(pos, next);
-  // the next piece's token, and its logit, are loaded ahead
-  int next_token = more ? __ldg(p.tokens + next.r) : -1;
-  auto logit_of = [&](int token) { return next.asked && token >= 0 && token < p.V ? load_elem(next.row + token) : INFINITY; };
-  float next_given = more ? logit_of(next_token) : 0.0f;
-  while (more) {
-    t = next;
-    pos += t.end - t.begin;
-    t.end = piece_end(t);
-    int token = next_token;
-    const float given = next_given;
-    more = piece_at(pos, next);
-    if (more) next_token = __ldg(p.tokens + next.r);
-    bool logit_next = more;
-    if (!t.asked) {
-      if (logit_next) next_given = logit_of(next_token);
-      continue;
-    }
-    if (token < -1 || token >= p.V) {
-      if (t.begin == 0 && tid == 0) report(p.status, SPEC_ERR_BAD_INPUT);
-      token = -1;
-    }
-    const float above = __int_as_float(given == 0.0f  ? 1
-                                       : given > 0.0f ? min(__float_as_int(given) + 1, 0x7F800000)
-                                                      : __float_as_int(given) - 1);  // the next fp32 number
-    float m = -INFINITY, bound = -FLT_MAX, most_of_span = -INFINITY;
-    f32x2 s2 = 0ull, e2 = 0ull;
-    int before = 0;
-    bool bad = false;
-    const f32x2 c2 = pair(p.c2, p.c2);
+  // Waits by a whole warp; false, for all of the CTA soon, where one gave up.
+  auto wait = [&](uint64_t* bar, uint32_t parity) {
+    if (__all_sync(0xFFFFFFFFu, mbar_try_wait(bar, parity & 1u))) return true;
+    const bool there = !*(volatile int*)&sh.aborted && mbar_wait_slow(bar, parity & 1u, p.status);
+    if (__all_sync(0xFFFFFFFFu, there)) return true;
+    *(volatile int*)&sh.aborted = 1;
+    return false;
+  };
+  uint32_t spans = 0;
 
-    int span = t.begin, round = 0;  // the span's first vector, rounds of it done
-    for (int v0 = t.begin; v0 < t.end; v0 += kRoundVecs, ++used) {
-      // ---- a round's vectors ----
-      uint4 w[kVecs];
-      const int st = used % kLogStages;
-      bool there = !*(volatile int*)&sh.aborted && wait_phase(&sh.full[st], (used / kLogStages) & 1u, p.status);
-      const bool plain = v0 + kRoundVecs <= t.end && v0 * W >= t.skip && (v0 + kRoundVecs) * W - t.skip <= p.V;
-#pragma unroll
-      for (int u = 0; u < kVecs; ++u) {
-        w[u] = sh.ring[st][u * kLogThreads + tid];
-        if (!plain) {
-          const int v = v0 + u * kLogThreads + tid, first = v * W - t.skip;
-          if (v >= t.end || first < 0 || first + W > p.V) w[u] = row_end<T>(t.row, v < t.end ? first : p.V, p.V);
-        }
+  if (warp < kLogWarps) {
+    // ---- goes through the rounds ----
+    uint32_t used = 0;
+    for (long long pos = share_begin; piece_at(pos, t); pos = t.next) {
+      if (!t.asked) continue;
+      int token = __ldg(p.tokens + t.r);
+      if (token < -1 || token >= p.V) {
+        if (t.begin == 0 && tid == 0) report(p.status, SPEC_ERR_BAD_INPUT);
+        token = -1;
       }
-      float top[kVecs], most = -INFINITY;
-#pragma unroll
-      for (int u = 0; u < kVecs; ++u) {
-        top[u] = largest<T>(w[u]);
-        bad |= !(top[u] < INFINITY);
-        most = fmaxf(most, top[u]);
-      }
-      // ---- sums ----
-      if (most > m) {
-        const float d = reference_step(m, most, p.c2), f = exp2f(d);
-        e2 = mul2(pair(f, f), fma2(pair(d, d), s2, e2));
-        s2 = mul2(pair(f, f), s2);
-        m = most;
-      }
-      const float M = __fmul_rn(m, p.c2);
-      const bool huge = !(fabsf(M) < kHuge);  // or nothing above -inf
-      const f32x2 minus_M = pair(-M, -M);
-      auto add = [&](f32x2 x) {
-        float2 d = unpair(x);
-        d.x = fmaxf(d.x, -1000.0f), d.y = fmaxf(d.y, -1000.0f);  // -inf, and NaN where nothing is finite
-        const f32x2 y = pair(ex2_approx(d.x), ex2_approx(d.y));
-        s2 = add2(s2, y);
-        e2 = fma2(pair(d.x, d.y), y, e2);
-      };
-      if (!huge) {
-#pragma unroll
-        for (int u = 0; u < kVecs; ++u)
-#pragma unroll
-          for (int k = 0; k < W; k += 2) {
-            const float l0 = element<T>(w[u], k), l1 = element<T>(w[u], k + 1);
-            add(fma2(pair(l0, l1), c2, minus_M));
-          }
-      } else {
-#pragma unroll
-        for (int u = 0; u < kVecs; ++u)
-#pragma unroll
-          for (int k = 0; k < W; k += 2) {
-            const float l0 = element<T>(w[u], k), l1 = element<T>(w[u], k + 1);
-            add(pair((l0 - m) * p.c2, (l1 - m) * p.c2));
-          }
-      }
-      // ---- entries before the token: of `given` and more, behind the token of more than that ----
-      if (token >= 0) {
-#pragma unroll
-        for (int u = 0; u < kVecs; ++u) {
-          const int v = v0 + u * kLogThreads + tid, first = v * W - t.skip;
-          if (!(top[u] >= given) || v >= t.end) continue;
-          const float least = first + W <= token ? given : above;
-#pragma unroll
-          for (int k = 0; k < W; ++k) before += element<T>(w[u], k) >= least ? 1 : 0;
-          if (first <= token && first + W > token) {  // its own vector: those equal to it before it
-#pragma unroll
-            for (int k = 0; k < W; ++k) before += element<T>(w[u], k) == given && first + k < token ? 1 : 0;
-          }
-          // what is not the row's is -inf, before its first entry as well
-          if (first < 0 && given == -INFINITY) before += first;
-        }
-      }
-      if (logit_next) next_given = logit_of(next_token), logit_next = false;
-      if (p.n > 0) {
-#pragma unroll
-        for (int u = 0; u < kVecs; ++u) sh.tops[round * kVecs + u][tid] = rounded_up(top[u]);
-        most_of_span = fmaxf(most_of_span, most);
-      }
-      // the round's place in the ring is free
-      there = __all_sync(0xFFFFFFFFu, there);
-      if (lane == 0) mbar_arrive(&sh.empty[st]);
-      if (!there) sh.aborted = 1;
-      __syncwarp();
-      if (p.n == 0 || (++round < kSpan && v0 + kRoundVecs < t.end)) continue;
-
-      // ---- the span's candidates: a bound, and what reaches it ----
-      float lanes = most_of_span;
-      for (int k = 0; k < 4; ++k) {
-        const float y = warp_max(lanes);
-        if (lane == 0) sh.warp_top[warp * 4 + k] = y;
-        const uint32_t has = __ballot_sync(0xFFFFFFFFu, lanes == y);
-        if (lane == __ffs((int)has) - 1) lanes = -INFINITY;
-      }
-      named_sync(1, kLogThreads);
-      const float mine = sh.warp_top[lane];
-      int rank = 0;
-#pragma unroll 8
-      for (int o = 0; o < 32; ++o) {
-        const float y = sh.warp_top[o];
-        rank += y > mine || (y == mine && o < lane) ? 1 : 0;
-      }
-      const uint32_t nth = __ballot_sync(0xFFFFFFFFu, rank == p.n - 1);
-      bound = fmaxf(bound, __shfl_sync(0xFFFFFFFFu, mine, __ffs((int)nth) - 1));
-      // calls f(value, index) for this thread's elements of the span that reach the bound
-      auto candidates = [&](auto f) {
+      const float given = token >= 0 ? load_elem(t.row + token) : INFINITY;
+      const float above = next_above<T>(given);
+      float m = -INFINITY;
+      f32x2 s2 = 0ull, e2 = 0ull;
+      int before = 0;
+      bool bad = false;
+      const f32x2 c2 = pair(p.c2, p.c2);
+      int v0 = t.begin;
+      do {  // a span
+        const int buffer = spans & 1;
+        if (spans >= 2 && !wait(&sh.span_empty[buffer], (spans >> 1) - 1)) return;
+        float most_of_span = -INFINITY;
+        int round = 0;
 #pragma unroll 1
-        for (int y0 = 0; y0 < round * kVecs; y0 += 4) {
-          uint32_t reach = 0;
+        for (; round < kSpan && v0 < t.end; ++round, v0 += kRoundVecs, ++used) {
+          // ---- a round's vectors ----
+          uint4 w[kVecs];
+          const int st = used % kLogStages;
+          if (!wait(&sh.full[st], used / kLogStages)) return;
+          const bool plain = v0 + kRoundVecs <= t.end && v0 * W >= t.skip && (v0 + kRoundVecs) * W - t.skip <= p.V;
 #pragma unroll
-          for (int y = 0; y < 4; ++y)
-            reach |= __uint_as_float((uint32_t)sh.tops[y0 + y][tid] << 16) >= bound ? 1u << y : 0u;
+          for (int u = 0; u < kVecs; ++u) {
+            w[u] = sh.ring[st][u * kLogThreads + tid];
+            if (!plain) {
+              const int v = v0 + u * kLogThreads + tid, first = v * W - t.skip;
+              if (v >= t.end || first < 0 || first + W > p.V) w[u] = row_end<T>(t.row, v < t.end ? first : p.V, p.V);
+            }
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sh.empty[st]);
+          float top[kVecs], most = -INFINITY;
+#pragma unroll
+          for (int u = 0; u < kVecs; ++u) {
+            top[u] = largest<T>(w[u]);
+            bad |= !(top[u] < INFINITY);
+            most = fmaxf(most, top[u]);
+          }
+          // ---- sums ----
+          if (most > m) {
+            const float d = reference_step(m, most, p.c2), f = exp2f(d);
+            e2 = mul2(pair(f, f), fma2(pair(d, d), s2, e2));
+            s2 = mul2(pair(f, f), s2);
+            m = most;
+          }
+          const float M = __fmul_rn(m, p.c2);
+          if (fabsf(M) < kHuge) {
+            const f32x2 minus_M = pair(-M, -M);
+            // what is 1,000 binary orders below the largest, and -inf, counts as that: 0 times a number
+            const float low = m - 1000.0f * p.inv_c2;
+            const uint32_t low2 = last_pair(pair(low, low));
+#pragma unroll
+            for (int u = 0; u < kVecs; ++u)
+#pragma unroll
+              for (int k = 0; k < W / 2; ++k) {
+                const f32x2 d = fma2(pair_from<T>(w[u], k, low, low2), c2, minus_M);
+                const float2 x = unpair(d);
+                const f32x2 y = pair(ex2_approx(x.x), ex2_approx(x.y));
+                s2 = add2(s2, y);
+                e2 = fma2(d, y, e2);
+              }
+          } else if (m > -INFINITY) {
 #pragma unroll 1
-          for (; reach; reach &= reach - 1) {
-            const int first = (span + (y0 + __ffs((int)reach) - 1) * kLogThreads + tid) * W - t.skip;
-            const uint4 v = first >= 0 && first + W <= p.V ? __ldg(reinterpret_cast<const uint4*>(t.row + first))
-                                                           : row_end<T>(t.row, first, p.V);
+            for (int u = 0; u < kVecs; ++u)
 #pragma unroll
-            for (int k = 0; k < W; ++k)
-              if (element<T>(v, k) >= bound) f(element<T>(v, k), first + k);
+              for (int k = 0; k < W; ++k) {
+                const float x = fmaxf((element<T>(w[u], k) - m) * p.c2, -1000.0f);
+                const f32x2 y = pair(ex2_approx(x), 0.0f);
+                s2 = add2(s2, y);
+                e2 = fma2(pair(x, 0.0f), y, e2);
+              }
+          }
+          // ---- entries before the token: of `given` and more, behind the token of more than that ----
+          if (token >= 0) {
+#pragma unroll
+            for (int u = 0; u < kVecs; ++u) {
+              const int v = v0 + u * kLogThreads + tid, first = v * W - t.skip;
+              if (!(top[u] >= given) || v >= t.end) continue;
+              before += count_from<T>(w[u], first + W <= token ? given : above);
+              if (first <= token && first + W > token) {  // its own vector: those equal to it before it
+#pragma unroll
+                for (int k = 0; k < W; ++k) before += element<T>(w[u], k) == given && first + k < token ? 1 : 0;
+              }
+              // what is not the row's is -inf, before its first entry as well
+              if (first < 0 && given == -INFINITY) before += first;
+            }
+          }
+          if (p.n > 0) {
+#pragma unroll
+            for (int u = 0; u < kVecs; ++u) sh.tops[buffer][round * kVecs + u][tid] = rounded_up(top[u]);
+            most_of_span = fmaxf(most_of_span, most);
           }
         }
-      };
-      bool full = false;
-      candidates([&](float l, int k) {
-        const int slot = atomicAdd(&sh.count, 1);
-        if (slot < kListFull) sh.list[slot] = make_key(l, k);
-        else full = true;
-      });
-      if (named_or(1, kLogThreads, full)) {
-        // too many: the n best of the spans before (by their indices), and the n best of this one, one after another
-        const int start = span * W - t.skip;
-        Key old[kListFull / kLogThreads];
-#pragma unroll
-        for (int y = 0; y < kListFull / kLogThreads; ++y) {
-          old[y] = sh.list[y * kLogThreads + tid];
-          if (key_index(old[y]) >= start) old[y] = 0;
+        sh.most[buffer][tid] = most_of_span;
+        if (v0 >= t.end) {  // the piece's sums
+          const float top = warp_max(m);
+          float2 half = unpair(s2);
+          float s = half.x + half.y;
+          half = unpair(e2);
+          float e = half.x + half.y;
+          move_sums(top, m, s, e, p.c2);
+          s = warp_sum(s);
+          e = warp_sum(e);
+          before = __reduce_add_sync(0xFFFFFFFFu, before);
+          bad = __any_sync(0xFFFFFFFFu, bad);
+          if (lane == 0) {
+            sh.m[buffer][warp] = top;
+            sh.s[buffer][warp] = s;
+            sh.e[buffer][warp] = e;
+            sh.before[buffer][warp] = bad ? -1 : before;
+          }
         }
-        named_sync(1, kLogThreads);
-        if (tid == 0) sh.count = 0;
-        named_sync(1, kLogThreads);
-#pragma unroll
-        for (int y = 0; y < kListFull / kLogThreads; ++y)
-          if (old[y]) sh.list[atomicAdd(&sh.count, 1)] = old[y];
-        named_sync(1, kLogThreads);
-        int kept = sh.count;  // at most n, from the span before
-        Key last = ~(Key)0;
-        for (int y = 0; y < p.n; ++y) {
-          Key next = 0;
-          candidates([&](float l, int k) {
-            const Key key = make_key(l, k);
-            if (key < last && key > next) next = key;
-          });
-#pragma unroll 1
-          for (int o = 16; o > 0; o >>= 1) next = max(next, __shfl_xor_sync(0xFFFFFFFFu, next, o));
-          if (lane == 0) sh.warp_key[warp] = next;
-          named_sync(1, kLogThreads);
-#pragma unroll 1
-          for (int w = 0; w < kLogWarps; ++w) next = max(next, sh.warp_key[w]);
-          named_sync(1, kLogThreads);
-          last = next;
-          if (last == 0) break;
-          if (tid == 0) sh.list[kept] = last;
-          ++kept;
-        }
-        if (tid == 0) sh.count = kept;
-        named_sync(1, kLogThreads);
-      }
-      const int listed_now = sh.count, kept = min(listed_now, p.n);
-      select_keys(sh.list, listed_now, p.n, sh.best);
-      named_sync(1, kLogThreads);
-      if (tid < kept) sh.list[tid] = sh.best[tid];
-      if (tid == 0) sh.count = kept;
-      if (kept == p.n) bound = fmaxf(bound, key_value(sh.best[p.n - 1]));
-      named_sync(1, kLogThreads);
-      span = v0 + kRoundVecs;
-      round = 0;
-      most_of_span = -INFINITY;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.span_full[buffer]);
+        ++spans;
+      } while (v0 < t.end);
     }
-    if (sh.aborted) gone = true;
-    if (logit_next) next_given = logit_of(next_token);
-    // the CTAs that have a piece of the row
-    const int b0 = (int)((long long)t.a * nv / share), b1 = (int)(((long long)(t.a + 1) * nv - 1) / share), pieces = b1 - b0 + 1;
+    return;
+  }
+
+  // ---- the last warp: outputs of rows that are not asked for, the best of spans, the ends of pieces ----
+  const int cells = max(p.n, 1);
+  for (long long x = (long long)blockIdx.x * 32 + lane; x < (long long)B * K1 * cells; x += (long long)gridDim.x * 32) {
+    const int r = (int)(x / cells), i = r / K1, j = r - i * K1;
+    const int n = listed ? sh.asked[i + 1] - sh.asked[i] : asked_rows(p, i);
+    if (n < 0 && j == 0) report(p.status, SPEC_ERR_BAD_INPUT);
+    if (j >= n) write_nothing(p, r, (int)(x - (long long)r * cells));
+  }
+  for (long long pos = share_begin; piece_at(pos, t); pos = t.next) {
+    if (!t.asked) continue;
+    int token = __ldg(p.tokens + t.r);
+    if (token < -1 || token >= p.V) token = -1;
+    const float given = token >= 0 ? load_elem(t.row + token) : INFINITY;
+    float bound = -FLT_MAX;
+    int kept = 0;  // keys in the list: the best so far
+    int v0 = t.begin, buffer;
+    for (;;) {
+      buffer = spans & 1;
+      const int span = v0, rounds = min(kSpan, (t.end - v0 + kRoundVecs - 1) / kRoundVecs);
+      v0 += kSpan * kRoundVecs;
+      if (!wait(&sh.span_full[buffer], spans >> 1)) return;
+      ++spans;
+      if (p.n > 0 && rounds > 0) {
+        // ---- a bound: the n-th best of the spans before, or the n-th largest of the threads' maxima ----
+        float most[kLogWarps], reached = -FLT_MAX;
+#pragma unroll
+        for (int y = 0; y < kLogWarps; ++y) most[y] = sh.most[buffer][y * 32 + lane];
+#pragma unroll 1
+        for (int k = kept < p.n ? 0 : p.n; k < p.n; ++k) {
+          float mine = most[0];
+#pragma unroll
+          for (int y = 1; y < kLogWarps; ++y) mine = fmaxf(mine, most[y]);
+          reached = warp_max(mine);
+          const uint32_t has = __ballot_sync(0xFFFFFFFFu, mine == reached);
+          if (lane == __ffs((int)has) - 1) {
+            bool gone = false;
+#pragma unroll
+            for (int y = 0; y < kLogWarps; ++y)
+              if (!gone && most[y] == reached) most[y] = -INFINITY, gone = true;
+          }
+        }
+        bound = fmaxf(bound, reached);
+        // ---- the vectors that reach it ----
+        auto vectors = [&](auto f) {  // calls f(vector of the span)
+#pragma unroll 1
+          for (int slot = 0; slot < rounds * kVecs; slot += 2) {
+            // 8 of 128 threads per lane, two slots at a time
+            const uint4 v = *reinterpret_cast<const uint4*>(&sh.tops[buffer][slot + (lane >> 4)][(lane & 15) * 8]);
+            if (!(largest<__nv_bfloat16>(v) >= bound)) continue;
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+              if (element<__nv_bfloat16>(v, k) >= bound) f((slot + (lane >> 4)) * kLogThreads + (lane & 15) * 8 + k);
+          }
+          __syncwarp();
+        };
+        auto entries = [&](int x, auto f) {  // calls f(key) for what reaches the bound in vector x
+          const int first = (span + x) * W - t.skip;
+          const uint4 v = first >= 0 && first + W <= p.V ? __ldg(reinterpret_cast<const uint4*>(t.row + first))
+                                                         : row_end<T>(t.row, first, p.V);
+#pragma unroll
+          for (int k = 0; k < W; ++k)
+            if (element<T>(v, k) >= bound) f(make_key(element<T>(v, k), first + k));
+        };
+        vectors([&](int x) {
+          const int at = atomicAdd(&sh.vectors, 1);
+          if (at < kFoundCap) sh.found[at] = x;
+        });
+        const int found = sh.vectors;
+        __syncwarp();
+        if (lane == 0) sh.vectors = 0, sh.count = kept;
+        __syncwarp();
+        int keys = kListCap + 1;
+        if (found <= kFoundCap) {
+#pragma unroll 1
+          for (int x = lane; x < found; x += 32)
+            entries(sh.found[x], [&](Key k) {
+              const int at = atomicAdd(&sh.count, 1);
+              if (at < kListCap) sh.list[at] = k;
+            });
+          __syncwarp();
+          keys = sh.count;
+        }
+        if (keys > kListCap) {
+          // ---- too many: this span's n best one after another, behind those of the spans before ----
+          Key last = ~(Key)0;
+          keys = kept;
+#pragma unroll 1
+          for (int y = 0; y < p.n; ++y) {
+            Key next = 0;
+            vectors([&](int x) {
+              entries(x, [&](Key k) {
+                if (k < last && k > next) next = k;
+              });
+            });
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) next = max(next, __shfl_xor_sync(0xFFFFFFFFu, next, o));
+            if (next == 0) break;
+            last = next;
+            if (lane == 0) sh.list[keys] = next;
+            ++keys;
+          }
+        }
+        select_keys(sh.list, keys, p.n, sh.best);
+        kept = min(keys, p.n);
+        if (lane < kept) sh.list[lane] = sh.best[lane];
+        if (kept == p.n) bound = fmaxf(bound, key_value(sh.best[p.n - 1]));
+        __syncwarp();
+      }
+      if (v0 >= t.end) break;
+      if (lane == 0) mbar_arrive(&sh.span_empty[buffer]);
+    }
 
     // ---- the piece's sums and best ----
-    const float warp_m = warp_max(m);
-    if (lane == 0) sh.m[warp] = warp_m;
-    // a span's end has left the best there, in order
-    const int found = sh.count;
-    const size_t x = (size_t)t.a + blockIdx.x;
-    if (tid < p.n) (pieces > 1 ? p.part_keys + x * p.n : sh.best)[tid] = tid < found ? sh.list[tid] : 0;
-    if (named_or(1, kLogThreads, gone)) break;
-    if (tid == 0) sh.count = 0;  // for the next piece, whose appends come after another barrier
-    float all_m = sh.m[0];
-#pragma unroll
-    for (int w = 1; w < kLogWarps; ++w) all_m = fmaxf(all_m, sh.m[w]);
-    float2 half = unpair(s2);
-    float s = half.x + half.y;
-    half = unpair(e2);
-    float e = half.x + half.y;
-    move_sums(all_m, m, s, e, p.c2);
-    m = all_m;
-    s = warp_sum(s);
-    e = warp_sum(e);
-    before = __reduce_add_sync(0xFFFFFFFFu, before);
-    bad = __any_sync(0xFFFFFFFFu, bad);
-    if (lane == 0) {
-      sh.s[warp] = s;
-      sh.e[warp] = e;
-      sh.before[warp] = bad ? -1 : before;
+    if (p.n > 0 && kept < p.n) {
+      if (lane >= kept && lane < p.n) sh.best[lane] = 0;
+      __syncwarp();
     }
-    named_sync(1, kLogThreads);
-    s = sh.s[0], e = sh.e[0], before = sh.before[0];
-#pragma unroll
-    for (int w = 1; w < kLogWarps; ++w) {
-      s += sh.s[w];
-      e += sh.e[w];
-      before = before < 0 || sh.before[w] < 0 ? -1 : before + sh.before[w];
-    }
+    float m = lane < kLogWarps ? sh.m[buffer][lane] : -INFINITY, s = 0.0f, e = 0.0f;
+    int before = 0;
+    if (lane < kLogWarps) s = sh.s[buffer][lane], e = sh.e[buffer][lane], before = sh.before[buffer][lane];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sh.span_empty[buffer]);
+    auto join = [&]() {  // the lanes' sums
+      const float top = warp_max(m);
+      move_sums(top, m, s, e, p.c2);
+      m = top;
+      s = warp_sum(s);
+      e = warp_sum(e);
+      const bool bad = __any_sync(0xFFFFFFFFu, before < 0);
+      before = __reduce_add_sync(0xFFFFFFFFu, before);
+      if (bad) before = -1;
+    };
+    join();
+    // the CTAs that have a piece of the row
+    const int b0 = divide((long long)t.a * nv, share), b1 = divide((long long)(t.a + 1) * nv - 1, share), pieces = b1 - b0 + 1;
     if (pieces > 1) {
-      if (tid == 0) {
-        p.part[x] = LogPartial{m, s, e, before};
-        __threadfence();  // and what the others wrote before the barrier
-        sh.last = atomicAdd(p.arrived + t.a, 1u) == (uint32_t)pieces - 1;
-        __threadfence();
-      }
-      named_sync(1, kLogThreads);
-      if (!sh.last) continue;
-
-      // ---- the last CTA of the row joins the pieces: one or two per lane, every warp the same ----
-      if (tid == 0) p.arrived[t.a] = 0;
-      const LogPartial* parts = p.part + t.a + b0;
-      uint4 v[2];
-#pragma unroll
-      for (int y = 0; y < 2; ++y)
-        v[y] = lane + 32 * y < pieces ? __ldcg(reinterpret_cast<const uint4*>(parts + lane + 32 * y))
-                                      : make_uint4(0xFF800000u, 0u, 0u, 0u);
-      Key least = 0;
+      const size_t x = (size_t)t.a + blockIdx.x;
+      if (lane < p.n) p.part_keys[x * p.n + lane] = sh.best[lane];
+      if (lane == 0) p.part[x] = LogPartial{m, s, e, before};
+      __threadfence();
+      __syncwarp();
+      int last = 0;
+      if (lane == 0) last = atomicAdd(p.arrived + t.a, 1u) == (uint32_t)pieces - 1;
+      if (!__shfl_sync(0xFFFFFFFFu, last, 0)) continue;
+      // ---- the last CTA of the row joins the pieces, one per lane ----
+      __threadfence();
+      if (lane == 0) p.arrived[t.a] = 0;
+      const uint4 v = lane < pieces ? __ldcg(reinterpret_cast<const uint4*>(p.part + t.a + b0 + lane))
+                                    : make_uint4(0xFF800000u, 0u, 0u, 0u);
       const Key* keys = p.part_keys + ((size_t)t.a + b0) * p.n;
       if (p.n) {
         // what is below some piece's n-th best is not among the n best
-        for (int y = lane; y < pieces; y += 32) least = max(least, __ldcg(keys + (size_t)y * p.n + p.n - 1));
+        Key least = lane < pieces ? __ldcg(keys + (size_t)lane * p.n + p.n - 1) : 0;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) least = max(least, __shfl_xor_sync(0xFFFFFFFFu, least, o));
-        for (int y = tid; y < pieces * p.n; y += kLogThreads) {
+        if (lane == 0) sh.count = 0;
+        __syncwarp();
+#pragma unroll 4
+        for (int y = lane; y < pieces * p.n; y += 32) {
           const Key k = __ldcg(keys + y);
-          if (k != 0 && k >= least) sh.joined[atomicAdd(&sh.count, 1)] = k;
+          if (k != 0 && k >= least) sh.list[atomicAdd(&sh.count, 1)] = k;
         }
+        __syncwarp();
+        const int count = sh.count;
+        select_keys(sh.list, count, p.n, sh.best);
       }
-      m = warp_max(fmaxf(__uint_as_float(v[0].x), __uint_as_float(v[1].x)));
-      float part_s[2], part_e[2];
-#pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        part_s[y] = __uint_as_float(v[y].y), part_e[y] = __uint_as_float(v[y].z);
-        move_sums(m, __uint_as_float(v[y].x), part_s[y], part_e[y], p.c2);
-      }
-      s = warp_sum(part_s[0] + part_s[1]);
-      e = warp_sum(part_e[0] + part_e[1]);
-      bad = __any_sync(0xFFFFFFFFu, (int)v[0].w < 0 || (int)v[1].w < 0);
-      before = __reduce_add_sync(0xFFFFFFFFu, (int)v[0].w + (int)v[1].w);
-      if (bad) before = -1;
-      if (p.n) {
-        named_sync(1, kLogThreads);
-        select_keys(sh.joined, sh.count, p.n, sh.best);
-        named_sync(1, kLogThreads);
-        if (tid == 0) sh.count = 0;
-      }
+      m = __uint_as_float(v.x), s = __uint_as_float(v.y), e = __uint_as_float(v.z), before = (int)v.w;
+      join();
     }
     write_row(p, t.r, m, s, e, before, token, given, sh.best);
-    named_sync(1, kLogThreads);
+    __syncwarp();
   }
 }
 
@@ -707,7 +752,7 @@ cudaError_t launch_logprobs(const LogLaunch& p, int ctas, cudaStream_t stream) {
   static std::atomic<size_t> raised[kMaxDevices];
   const cudaError_t err = raise_smem(logprobs_kernel<T>, smem, raised);
   if (err != cudaSuccess) return err;
-  return launch_after_previous(logprobs_kernel<T>, dim3((unsigned)ctas), dim3(kLogThreads + 32), smem, stream, p);
+  return launch_after_previous(logprobs_kernel<T>, dim3((unsigned)ctas), dim3(kLogThreads + 64), smem, stream, p);
 }
 
 }  // namespace
@@ -743,6 +788,7 @@ extern "C" int spec_logprobs(const void* logits, int logits_dtype, const int32_t
   p.V = V;
   p.n = top_n;
   p.c2 = (float)(1.4426950408889634 / (temperature > 0.0f ? (double)temperature : 1.0));
+  p.inv_c2 = 1.0f / p.c2;
   p.logprob = logprob_out;
   p.entropy = entropy_out;
   p.top_logprobs = top_logprobs_out;
