@@ -493,7 +493,7 @@ __global__ void __launch_bounds__(kLogThreads + 64, kCtasPerSm) logprobs_kernel(
                 e2 = fma2(d, y, e2);
               }
           } else if (m > -INFINITY) {
-#pragma unroll 1
+#pragma unroll
             for (int u = 0; u < kVecs; ++u)
 #pragma unroll
               for (int k = 0; k < W; ++k) {
