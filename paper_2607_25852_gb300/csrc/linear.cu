@@ -16,6 +16,7 @@
 
 #include <algorithm>
 
+#include "linear_few.cuh"
 #include "linear_tc.cuh"
 #include "tensor_core.cuh"
 
@@ -76,7 +77,7 @@ inline size_t linear_smem(int Dk) {
 // S columns of the state, KR of its rows per thread.
 template <typename T, int S, int KR>
 __global__ void __launch_bounds__(kLinThreads) linear_rows_kernel(const LinearLaunch p, int slices) {
-  constexpr int L = S / 4, KG = kLinThreads / L;  // threads across columns, groups of KR rows
+  constexpr int L = S / 4;  // threads across columns
   extern __shared__ float4 smem4[];
   __shared__ long long steps[kBlockRows];
   __shared__ float score[kBlockRows][kBlockRows], weight[kBlockRows], first_weight[kBlockRows], all_weight;
@@ -326,7 +327,10 @@ int run_linear(const LinearLaunch& p, int dtype, void* ws, size_t ws_bytes, cuda
     g.plan.seg_steps = reinterpret_cast<long long*>(static_cast<char*>(ws) + g.steps_off);
     return launch_linear_tc(p, g.plan, stream) == cudaSuccess && cudaGetLastError() == cudaSuccess ? SPEC_OK : SPEC_ERR_CUDA;
   }
-  const cudaError_t err = dtype == SPEC_F32 ? launch_rows<float>(p, stream) : launch_rows<__nv_bfloat16>(p, stream);
+  const bool few = linear_few_serves(p.rows.B, p.rows.K, p.Hq, p.H, p.Dk, p.Dv, dtype, device_sms());
+  const cudaError_t err = few                 ? launch_linear_few(p, dtype, stream)
+                          : dtype == SPEC_F32 ? launch_rows<float>(p, stream)
+                                              : launch_rows<__nv_bfloat16>(p, stream);
   return err == cudaSuccess && cudaGetLastError() == cudaSuccess ? SPEC_OK : SPEC_ERR_CUDA;
 }
 
