@@ -352,6 +352,7 @@ def spec_shard_finish(races, S, decisions, B, K, V, temperature, seeds, request_
 # do on the host counts: pointers go to ctypes as integers, and the current
 # stream comes from torch's own accessor where it has one.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream_handle(stream):
@@ -359,7 +360,7 @@ def _stream_handle(stream):
         return stream.cuda_stream
     if _raw_stream is None:
         return torch.cuda.current_stream().cuda_stream
-    return _raw_stream(torch.cuda.current_device())
+    return _raw_stream(_current_device())
 
 
 def _cache(k, v):
@@ -548,11 +549,13 @@ def spec_cache_compact(page_table, page_refs, move_src_out, move_dst_out, page_m
 # ---------------------------------------------------------------------------
 # Rotary positions, linear attention, log probabilities
 # ---------------------------------------------------------------------------
-def _here(*tensors):
+def _here(first, *others):
     """Refuses tensors that the kernels could not read: all are on the current CUDA device."""
-    dev = torch.cuda.current_device() if tensors[0].is_cuda else -1
-    for t in tensors:
-        if t is not None and (not t.is_cuda or t.get_device() != dev):
+    dev = first.get_device()
+    if dev < 0 or dev != _current_device():
+        raise ValueError("expected tensors on the current CUDA device")
+    for t in others:
+        if t is not None and t.get_device() != dev:
             raise ValueError("expected tensors on the current CUDA device")
 
 

@@ -9,7 +9,7 @@
 // 16 keys by four values of the state per thread (heads of 128), in registers for
 // all rows of the head.  Up to three states are in flight per SM while one is
 // worked on.  The rows' products with the state are summed over the warps through
-// shared memory, four rows at a time.
+// shared memory, four or eight rows at a time.
 //
 // Bound by HBM for up to about eight rows, by the rows' passes beyond.
 #include "attend_ring.cuh"
@@ -20,7 +20,6 @@ namespace spec {
 namespace {
 
 constexpr int kFewThreads = 256, kFewWarps = kFewThreads / 32;  // and a warp that brings
-constexpr int kPass = 4;      // rows per pass
 constexpr int kMaxStages = 4;
 
 struct FewLaunch {
@@ -86,7 +85,7 @@ __device__ __forceinline__ void store_four(__nv_bfloat16* to, f32x2 a, f32x2 b) 
   *reinterpret_cast<uint2*>(to) = make_uint2(last_pair(a), last_pair(b));
 }
 
-template <typename T, int DK, int DV>
+template <typename T, int DK, int DV, int kPass>
 __global__ void __launch_bounds__(kFewThreads + 32, 1) linear_few_kernel(const __grid_constant__ FewLaunch a) {
   constexpr int L = DV / 4, KG = kFewThreads / L, KR = DK / KG;  // threads across values, groups of KR keys
   constexpr int W = 16 / (int)sizeof(T);
@@ -221,11 +220,16 @@ __global__ void __launch_bounds__(kFewThreads + 32, 1) linear_few_kernel(const _
     const T* qs = reinterpret_cast<const T*>(smem + s * a.stage_bytes + a.rows_off);
     const T* ks = reinterpret_cast<const T*>(smem + s * a.stage_bytes + a.rows_off + a.k_off);
     const T* vs = reinterpret_cast<const T*>(smem + s * a.stage_bytes + a.rows_off + a.v_off);
-    f32x2 st[KR][2];
+    f32x2 st[KR / 2][4];  // pairs of keys
 #pragma unroll
-    for (int x = 0; x < KR; ++x) {
-      st[x][0] = st[x][1] = 0ull;
-      if (!t.fresh) row_four(state + (kr0 + x) * DV + col, st[x]);
+    for (int x = 0; x < KR; x += 2) {
+      float4 w = make_float4(0.0f, 0.0f, 0.0f, 0.0f), y = w;
+      if (!t.fresh) {
+        w = *reinterpret_cast<const float4*>(state + (kr0 + x) * DV + col);
+        y = *reinterpret_cast<const float4*>(state + (kr0 + x + 1) * DV + col);
+      }
+      st[x / 2][0] = pair(w.x, y.x), st[x / 2][1] = pair(w.y, y.y);
+      st[x / 2][2] = pair(w.z, y.z), st[x / 2][3] = pair(w.w, y.w);
     }
     if (p.q) {
       for (int x = tid; x < t.early * p.G * L; x += kFewThreads) {  // rows before position 0
@@ -258,29 +262,25 @@ __global__ void __launch_bounds__(kFewThreads + 32, 1) linear_few_kernel(const _
 #pragma unroll 1
         for (int y0 = 0; y0 < n; y0 += kPass) {
           // ---- rows y0 .. y0 + 3 times the state, this thread's keys ----
-          f32x2 o[kPass][2];
 #pragma unroll
           for (int y = 0; y < kPass; ++y) {
-            o[y][0] = o[y][1] = 0ull;
-            if (y0 + y >= n) continue;
+            if (y0 + y >= n) break;
+            f32x2 o[4] = {0ull, 0ull, 0ull, 0ull};  // of even and odd keys
 #pragma unroll
             for (int x = 0; x < KR; x += 4) {
               f32x2 f[2];
               row_four(q + (y0 + y) * DK + kr0 + x, f);
-              const float2 f0 = unpair(f[0]), f1 = unpair(f[1]);
 #pragma unroll
-              for (int z = 0; z < 2; ++z) {
-                o[y][z] = fma2(pair(f0.x, f0.x), st[x][z], o[y][z]);
-                o[y][z] = fma2(pair(f0.y, f0.y), st[x + 1][z], o[y][z]);
-                o[y][z] = fma2(pair(f1.x, f1.x), st[x + 2][z], o[y][z]);
-                o[y][z] = fma2(pair(f1.y, f1.y), st[x + 3][z], o[y][z]);
-              }
+              for (int z = 0; z < 4; ++z) o[z] = fma2(f[1], st[x / 2 + 1][z], fma2(f[0], st[x / 2][z], o[z]));
             }
-            if (L < 32) {
+            float v[4];
 #pragma unroll
-              for (int z = 0; z < 2; ++z) o[y][z] = add2(o[y][z], __shfl_xor_sync(0xFFFFFFFFu, o[y][z], 16));
+            for (int z = 0; z < 4; ++z) {
+              const float2 two = unpair(o[z]);
+              v[z] = two.x + two.y;
+              if (L < 32) v[z] += __shfl_xor_sync(0xFFFFFFFFu, v[z], 16);
             }
-            if (lane < L) store_four(&red[warp][y][col], o[y][0], o[y][1]);
+            if (lane < L) *reinterpret_cast<float4*>(&red[warp][y][col]) = make_float4(v[0], v[1], v[2], v[3]);
           }
           named_sync(1, kFewThreads);
           // ---- all of the state, and the block's own rows ----
@@ -309,29 +309,34 @@ __global__ void __launch_bounds__(kFewThreads + 32, 1) linear_few_kernel(const _
     if (t.to) {
       const f32x2 f = pair(t.all, t.all);
 #pragma unroll
-      for (int x = 0; x < KR; ++x) st[x][0] = mul2(st[x][0], f), st[x][1] = mul2(st[x][1], f);
+      for (int x = 0; x < KR / 2; ++x)
+#pragma unroll
+        for (int z = 0; z < 4; ++z) st[x][z] = mul2(st[x][z], f);
 #pragma unroll 1
       for (int j = 0; j < n; ++j) {
         f32x2 w[2];
         row_four(vs + j * DV + col, w);
-        const f32x2 m = pair(t.weight[j], t.weight[j]);
-        w[0] = mul2(m, w[0]), w[1] = mul2(m, w[1]);
+        const float2 w0 = unpair(w[0]), w1 = unpair(w[1]);
+        const float m = t.weight[j], v[4] = {m * w0.x, m * w0.y, m * w1.x, m * w1.y};
 #pragma unroll
         for (int x = 0; x < KR; x += 4) {
           f32x2 k[2];
           row_four(ks + j * DK + kr0 + x, k);
-          const float2 k0 = unpair(k[0]), k1 = unpair(k[1]);
 #pragma unroll
-          for (int z = 0; z < 2; ++z) {
-            st[x][z] = fma2(pair(k0.x, k0.x), w[z], st[x][z]);
-            st[x + 1][z] = fma2(pair(k0.y, k0.y), w[z], st[x + 1][z]);
-            st[x + 2][z] = fma2(pair(k1.x, k1.x), w[z], st[x + 2][z]);
-            st[x + 3][z] = fma2(pair(k1.y, k1.y), w[z], st[x + 3][z]);
+          for (int z = 0; z < 4; ++z) {
+            st[x / 2][z] = fma2(k[0], pair(v[z], v[z]), st[x / 2][z]);
+            st[x / 2 + 1][z] = fma2(k[1], pair(v[z], v[z]), st[x / 2 + 1][z]);
           }
         }
       }
 #pragma unroll
-      for (int x = 0; x < KR; ++x) store_four(state + (kr0 + x) * DV + col, st[x][0], st[x][1]);
+      for (int x = 0; x < KR; x += 2) {
+        float2 w[4];
+#pragma unroll
+        for (int z = 0; z < 4; ++z) w[z] = unpair(st[x / 2][z]);
+        *reinterpret_cast<float4*>(state + (kr0 + x) * DV + col) = make_float4(w[0].x, w[1].x, w[2].x, w[3].x);
+        *reinterpret_cast<float4*>(state + (kr0 + x + 1) * DV + col) = make_float4(w[0].y, w[1].y, w[2].y, w[3].y);
+      }
       proxy_fence();
     }
     __syncwarp();
@@ -339,8 +344,8 @@ __global__ void __launch_bounds__(kFewThreads + 32, 1) linear_few_kernel(const _
   }
 }
 
-template <typename T, int DK, int DV>
-cudaError_t launch_few(const LinearLaunch& p, cudaStream_t stream) {
+template <typename T, int DK, int DV, int kPass>
+cudaError_t launch_pass(const LinearLaunch& p, cudaStream_t stream) {
   FewLaunch a{};
   a.p = p;
   a.heads = (uint32_t)p.rows.B * (uint32_t)p.H;
@@ -351,16 +356,22 @@ cudaError_t launch_few(const LinearLaunch& p, cudaStream_t stream) {
   a.stage_bytes = (a.rows_off + a.v_off + (p.rows.K + 1) * DV * (int)sizeof(T) + 127) / 128 * 128;
   static std::atomic<int> known;
   int fixed;
-  cudaError_t err = static_smem(linear_few_kernel<T, DK, DV>, known, &fixed);
+  cudaError_t err = static_smem(linear_few_kernel<T, DK, DV, kPass>, known, &fixed);
   if (err != cudaSuccess) return err;
   const int room = 227 * 1024 - (fixed + 1023) / 1024 * 1024 - 128;
   a.stages = std::min(kMaxStages, room / a.stage_bytes);
   const size_t smem = (size_t)a.stages * a.stage_bytes + 128;
   static std::atomic<size_t> raised[kMaxDevices];
-  err = raise_smem(linear_few_kernel<T, DK, DV>, smem, raised);
+  err = raise_smem(linear_few_kernel<T, DK, DV, kPass>, smem, raised);
   if (err != cudaSuccess) return err;
-  return launch_after_previous(linear_few_kernel<T, DK, DV>, dim3(std::min<uint32_t>(a.heads, device_sms())),
+  return launch_after_previous(linear_few_kernel<T, DK, DV, kPass>, dim3(std::min<uint32_t>(a.heads, device_sms())),
                                dim3(kFewThreads + 32), smem, stream, a);
+}
+
+// Up to four rows leave room for a third state of 64 KB.
+template <typename T, int DK, int DV>
+cudaError_t launch_few(const LinearLaunch& p, cudaStream_t stream) {
+  return p.rows.K < 4 || !p.q ? launch_pass<T, DK, DV, 4>(p, stream) : launch_pass<T, DK, DV, 8>(p, stream);
 }
 
 template <typename T>

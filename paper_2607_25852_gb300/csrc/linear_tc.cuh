@@ -9,7 +9,7 @@
 namespace spec {
 
 constexpr int kLinChunk = 64;      // rows that a pass over the state takes
-constexpr int kLinTcRows = 32;     // calls of more rows per request go to the tensor cores
+constexpr int kLinTcRows = 11;     // calls of more rows per request go to the tensor cores
 constexpr int kLinMaxSegments = 32;
 constexpr int kLinSms = 152;       // the device that plans are made for (a workspace's size must not depend on the one it is asked on)
 

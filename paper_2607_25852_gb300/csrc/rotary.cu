@@ -9,10 +9,12 @@
 // angle's last 17 bits, and fp64 arithmetic is slow here).  cos and sin are then
 // CUDA's sincospif of the angle in half turns.
 //
-// A CTA takes a row: its first loads are in flight while its threads compute the
-// row's angles, one each, into shared memory for all heads.  Bound by HBM for
-// many rows, by two round trips (the row's position; its page and its data) and
-// the launch for few.
+// A CTA takes up to 8 rows: a thread each finds their places, all compute their
+// angles, and then a thread has the same elements of every few heads, row after
+// row, with their angles in registers.  (A row per CTA spent 700 instructions per
+// warp on three vectors: 16 rows' chunks of 256, 100 MB, 43 us.)  Bound by HBM for
+// many rows, by three round trips (position, page, data) and the launch for few.
+#include <algorithm>
 #include <cmath>
 
 #include "paged.cuh"
@@ -23,6 +25,7 @@ namespace spec {
 namespace {
 
 constexpr int kRotaryThreads = 256;
+constexpr int kRotaryRows = 8;  // of a CTA, at most
 
 struct RotaryLaunch {
   const char *x, *k_new, *v_new;  // k_new, v_new null without a cache
@@ -31,6 +34,7 @@ struct RotaryLaunch {
   int64_t page_b, token_b, head_b;
   int heads, kv_heads, D;
   int pairs;                      // rotary_dim / 2
+  int batch;                      // rows of a CTA
   int pages, page_size, max_pages;
   bool in_place;                  // out is x: what is not turned stays
   float amplitude;
@@ -73,136 +77,126 @@ __device__ __forceinline__ float2 turn(double frequency, int64_t P, float amplit
   return make_float2(amplitude * c, amplitude * s);
 }
 
+struct RowPlace {
+  int64_t row, pos;  // row -1: skipped
+  int64_t at;        // the key's and value's bytes into the layer; -1: nowhere
+};
+
+__device__ __forceinline__ RowPlace row_place(const RotaryLaunch& p, unsigned r) {
+  const unsigned K1 = (unsigned)p.rows.K + 1;
+  RowPlace t{-1, 0, -1};
+  if (r >= (unsigned)p.rows.B * K1) return t;
+  const int i = (int)(r / K1), j = (int)(r - (unsigned)i * K1);
+  const RequestRows q = request_rows(p.rows, i);
+  if (!q.ok) {
+    if (j == 0) report(p.status, SPEC_ERR_BAD_INPUT);
+    return t;
+  }
+  t.pos = q.p + j;
+  if (j >= q.count || t.pos < 0) return t;
+  t.row = q.row0 + j;
+  if (!p.k_new) return t;
+  int page = -1, slot = 0;
+  if (t.pos < (int64_t)p.max_pages * p.page_size) {
+    slot = (int)t.pos / p.page_size;
+    page = __ldg(p.table + (size_t)i * p.max_pages + slot);
+  }
+  if (page >= 0 && page < p.pages)
+    t.at = (int64_t)page * p.page_b + (int64_t)((int)t.pos - slot * p.page_size) * p.token_b;
+  else
+    report(p.status, SPEC_ERR_BAD_INPUT);
+  return t;
+}
+
 // kInter: neighbouring elements are a pair, and a unit is one pack of W
 // elements.  Otherwise elements d and d + pairs are, and a unit is two packs of W
 // elements, one of each half (W divides the half), or one of those that stay.
 template <typename T, int W, bool kInter>
-__global__ void __launch_bounds__(kRotaryThreads) rotary_kernel(const RotaryLaunch p) {
-  __shared__ float cs[SPEC_MAX_HEAD_DIM / 2], sn[SPEC_MAX_HEAD_DIM / 2];
-  const int tid = threadIdx.x, K1 = p.rows.K + 1;
-  const int i = (int)(blockIdx.x / (unsigned)K1), j = (int)(blockIdx.x - (unsigned)i * (unsigned)K1);
+__global__ void __launch_bounds__(kRotaryThreads, 4) rotary_kernel(const RotaryLaunch p) {
+  constexpr int E = (int)sizeof(T), kU = kInter ? 3 : W * (int)sizeof(T) == 16 ? 1 : 2;  // heads in flight
+  constexpr int kPairs = kInter ? (W + 1) / 2 : W;
+  __shared__ alignas(16) float cs[kRotaryRows][SPEC_MAX_HEAD_DIM / 2], sn[kRotaryRows][SPEC_MAX_HEAD_DIM / 2];
+  __shared__ RowPlace places[kRotaryRows];
+  const int tid = threadIdx.x;
   pdl_wait_prerequisites();
   pdl_launch_dependents();
-  const double frequency = tid < p.pairs ? __ldg(p.frequencies + tid) : 0.0;
-  const RequestRows q = request_rows(p.rows, i);
-  if (!q.ok) {
-    if (j == 0 && tid == 0) report(p.status, SPEC_ERR_BAD_INPUT);
-    return;
-  }
-  const int64_t pos = q.p + j;
-  if (j >= q.count || pos < 0) return;
-  const int64_t row = q.row0 + j;
-  const char* x = p.x + row * p.x_row;
-  char* out = p.out + row * p.out_row;
-
-  // ---- the keys' and values' place ----
-  char *k_to = nullptr, *v_to = nullptr;
-  if (p.k_new) {
-    int page = -1, slot = 0;
-    if (pos < (int64_t)p.max_pages * p.page_size) {
-      slot = (int)pos / p.page_size;
-      page = __ldg(p.table + (size_t)i * p.max_pages + slot);
-    }
-    if (page < 0 || page >= p.pages) {
-      if (tid == 0) report(p.status, SPEC_ERR_BAD_INPUT);
-    } else {
-      const int64_t at = (int64_t)page * p.page_b + (int64_t)((int)pos - slot * p.page_size) * p.token_b;
-      k_to = p.k + at;
-      v_to = p.v + at;
-    }
-  }
-
-  constexpr int E = (int)sizeof(T), kU = 2;  // units in flight per thread
+  if (tid < p.batch) places[tid] = row_place(p, blockIdx.x * (unsigned)p.batch + tid);
+  // ---- a thread has unit u of every hstep-th head ----
   const int turned = kInter ? (2 * p.pairs + W - 1) / W : p.pairs / W;  // a head's units with turned elements
   const int units = kInter ? p.D / W : turned + (p.D - 2 * p.pairs) / W;
-  const int heads = p.heads + (k_to ? p.kv_heads : 0), total = heads * units;
-  // unit n: where it is read and written
-  auto place = [&](int n, int& u, const char*& from, char*& to) {
-    const int h = n / units;
-    u = n - h * units;
-    if (h < p.heads) {
-      from = x + (int64_t)h * p.D * E;
-      to = out + (int64_t)h * p.D * E;
-    } else {
-      from = p.k_new + row * p.k_row + (int64_t)(h - p.heads) * p.D * E;
-      to = k_to + (h - p.heads) * p.head_b;
-    }
-  };
-  const int first = kInter ? 0 : 2 * p.pairs - turned * W;  // a staying unit u begins at first + u W
-  bool angles = false;
-  for (int n0 = tid; n0 - tid < total || !angles; n0 += kU * kRotaryThreads) {
-    Pack<T, W> a[kU], b[kU];
-#pragma unroll
-    for (int y = 0; y < kU; ++y) {
-      const int n = n0 + y * kRotaryThreads;
-      if (n >= total) continue;
-      int u;
-      const char* from;
-      char* to;
-      place(n, u, from, to);
-      if (!kInter && u < turned) {
-        a[y] = load_pack<T, W>(from + (int64_t)u * W * E);
-        b[y] = load_pack<T, W>(from + (int64_t)(p.pairs + u * W) * E);
-      } else {
-        a[y] = load_pack<T, W>(from + (int64_t)(first + u * W) * E);
-      }
-    }
-    if (!angles) {  // the row's angles, a pair per thread, while the loads are under way
-      if (tid < p.pairs) {
-        const float2 t = turn(frequency, pos, p.amplitude, p.status);
-        cs[tid] = t.x;
-        sn[tid] = t.y;
-      }
-      __syncthreads();
-      angles = true;
-    }
-#pragma unroll
-    for (int y = 0; y < kU; ++y) {
-      const int n = n0 + y * kRotaryThreads;
-      if (n >= total) continue;
-      int u;
-      const char* from;
-      char* to;
-      place(n, u, from, to);
-      if (u >= turned) {
-        if (!(p.in_place && n < p.heads * units)) store_pack<T, W>(to + (int64_t)(first + u * W) * E, a[y]);
-        continue;
-      }
-      if (kInter) {
-#pragma unroll
-        for (int e = 0; e < W; e += 2) {
-          const int d = (u * W + e) / 2;
-          if (d >= p.pairs) break;  // the rest of this pack stays
-          const float v = to_float(a[y].e[e]), w = to_float(a[y].e[e + 1]), c = cs[d], s = sn[d];
-          from_float(fmaf(v, c, -w * s), &a[y].e[e]);
-          from_float(fmaf(w, c, v * s), &a[y].e[e + 1]);
-        }
-        store_pack<T, W>(to + (int64_t)u * W * E, a[y]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < W; ++e) {
-          const float v = to_float(a[y].e[e]), w = to_float(b[y].e[e]), c = cs[u * W + e], s = sn[u * W + e];
-          from_float(fmaf(v, c, -w * s), &a[y].e[e]);
-          from_float(fmaf(w, c, v * s), &b[y].e[e]);
-        }
-        store_pack<T, W>(to + (int64_t)u * W * E, a[y]);
-        store_pack<T, W>(to + (int64_t)(p.pairs + u * W) * E, b[y]);
-      }
-    }
+  const int hstep = kRotaryThreads / units, h0 = tid / units, u = tid - h0 * units;
+  const int heads = h0 < hstep ? p.heads + (p.k_new ? p.kv_heads : 0) : 0;
+  const bool turns = u < turned;
+  const int at0 = (kInter || turns ? u * W : 2 * p.pairs + (u - turned) * W) * E;  // within a head
+  const int at1 = (p.pairs + u * W) * E, head = p.D * E;
+  const int vecs = head / 16, vstep = kRotaryThreads / vecs, v0 = tid / vecs, vu = (tid - v0 * vecs) * 16;
+  const int values = p.k_new && v0 < vstep ? p.kv_heads : 0;
+  __syncthreads();
+  for (int x = tid; x < p.batch * p.pairs; x += kRotaryThreads) {
+    const int y = x / p.pairs, d = x - y * p.pairs;
+    if (places[y].row < 0) continue;
+    const float2 t = turn(__ldg(p.frequencies + d), places[y].pos, p.amplitude, p.status);
+    cs[y][d] = t.x;
+    sn[y][d] = t.y;
   }
-  if (v_to) {
-    const int vec = p.D * E / 16, n = p.kv_heads * vec;
-    const char* v = p.v_new + row * p.v_row;
-    for (int y = tid; y < n; y += kRotaryThreads) {
-      const int h = y / vec;
-      *reinterpret_cast<uint4*>(v_to + h * p.head_b + (int64_t)(y - h * vec) * 16) = ldg_stream(v + (int64_t)y * 16);
+  __syncthreads();
+#pragma unroll 1
+  for (int y = 0; y < p.batch; ++y) {
+    const int64_t row = places[y].row, at = places[y].at;
+    if (row < 0) continue;
+    const char *x = p.x + row * p.x_row, *k_from = p.k_new + row * p.k_row, *v_from = p.v_new + row * p.v_row;
+    char *out = p.out + row * p.out_row, *k_to = p.k + at, *v_to = p.v + at;
+    Pack<T, W> a[kU], b[kU];
+    auto load = [&](int h, Pack<T, W>& a, Pack<T, W>& b) {
+      const char* from = h < p.heads ? x + h * head : k_from + (h - p.heads) * head;
+      a = load_pack<T, W>(from + at0);
+      if (!kInter && turns) b = load_pack<T, W>(from + at1);
+    };
+#pragma unroll
+    for (int z = 0; z < kU; ++z)
+      if (h0 + z * hstep < heads) load(h0 + z * hstep, a[z], b[z]);
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if (v0 < values) v = ldg_stream(v_from + v0 * head + vu);
+    float c[kPairs], s[kPairs];
+#pragma unroll
+    for (int e = 0; e < kPairs; ++e) c[e] = cs[y][(u * kPairs + e) & (SPEC_MAX_HEAD_DIM / 2 - 1)], s[e] = sn[y][(u * kPairs + e) & (SPEC_MAX_HEAD_DIM / 2 - 1)];
+#pragma unroll 1
+    for (int h = h0; h < heads; h += kU * hstep) {
+#pragma unroll
+      for (int z = 0; z < kU; ++z) {
+        const int w = h + z * hstep;
+        if (w >= heads) break;
+        if (w >= p.heads && at < 0) break;
+        char* to = w < p.heads ? out + w * head : k_to + (w - p.heads) * p.head_b;
+        if (!turns) {
+          if (!(p.in_place && w < p.heads)) store_pack<T, W>(to + at0, a[z]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < kPairs; ++e) {
+            if (kInter && u * kPairs + e >= p.pairs) break;  // the rest of this pack stays
+            T *f = &a[z].e[kInter ? 2 * e % W : e], *g = kInter ? &a[z].e[(2 * e + 1) % W] : &b[z].e[e];
+            const float f0 = to_float(*f), g0 = to_float(*g);
+            from_float(fmaf(f0, c[e], -g0 * s[e]), f);
+            from_float(fmaf(g0, c[e], f0 * s[e]), g);
+          }
+          store_pack<T, W>(to + at0, a[z]);
+          if (!kInter) store_pack<T, W>(to + at1, b[z]);
+        }
+        if (w + kU * hstep < heads) load(w + kU * hstep, a[z], b[z]);
+      }
+    }
+    if (at < 0) continue;
+    for (int h = v0; h < values; h += vstep) {
+      if (h > v0) v = ldg_stream(v_from + h * head + vu);
+      *reinterpret_cast<uint4*>(v_to + h * p.head_b + vu) = v;
     }
   }
 }
 
 template <typename T>
 cudaError_t launch_rotary(const RotaryLaunch& p, bool interleaved, cudaStream_t stream) {
-  const dim3 grid((unsigned)((long long)p.rows.B * (p.rows.K + 1))), block(kRotaryThreads);
+  const long long rows = (long long)p.rows.B * (p.rows.K + 1);
+  const dim3 grid((unsigned)((rows + p.batch - 1) / p.batch)), block(kRotaryThreads);
   constexpr int W = 16 / (int)sizeof(T);
   if (interleaved) return launch_after_previous(rotary_kernel<T, W, true>, grid, block, 0, stream, p);
   // the widest packs that divide the half that is turned
@@ -221,7 +215,9 @@ bool rotation_ok(const double* frequencies, int rotary_dim, int head_dim, float 
   return frequencies && rotary_dim >= 2 && rotary_dim % 2 == 0 && rotary_dim <= head_dim && std::isfinite(amplitude);
 }
 
-int run_rotary(const RotaryLaunch& p, int dtype, int interleaved, cudaStream_t stream) {
+int run_rotary(RotaryLaunch& p, int dtype, int interleaved, cudaStream_t stream) {
+  // one row per CTA while there are no more than six CTAs' worth per SM
+  p.batch = (int)std::min<long long>(kRotaryRows, std::max<long long>(1, (long long)p.rows.B * (p.rows.K + 1) / (6 * device_sms())));
   const cudaError_t err = dtype == SPEC_F32 ? launch_rotary<float>(p, interleaved != 0, stream)
                                             : launch_rotary<__nv_bfloat16>(p, interleaved != 0, stream);
   return err == cudaSuccess && cudaGetLastError() == cudaSuccess ? SPEC_OK : SPEC_ERR_CUDA;
