@@ -738,9 +738,10 @@ int spec_cache_compact(int32_t* page_table, int32_t* page_refs, int B, int max_p
  * row at position P = pos_base[i] + j becomes
  *   amplitude * (a cos t - b sin t, b cos t + a sin t),  t = P frequencies[d].
  * Pair d is elements (2 d, 2 d + 1) with `interleaved`, else (d, d + rotary_dim / 2);
- * elements from rotary_dim on stay as they are.  The angle is exact to 2^-53 of
- * itself before it is reduced to a turn, and rounded to fp32 after; results are
- * rounded once.  Negated frequencies turn back.
+ * elements from rotary_dim on stay as they are.  frequencies[d] / 2 pi is rounded to
+ * 2^-52 of itself and to 2^-64; its product with P is exact, and what is left of it
+ * within a turn is rounded to fp32.  Results are rounded once.  Negated frequencies
+ * turn back.
  *
  * spec_rotary_frequencies -- the table for a base and a scaling.  Host only.
  *   SPEC_ROTARY_PLAIN  f_d = base^(-2 d / rotary_dim)
@@ -771,7 +772,7 @@ int spec_rotary_frequencies(int rotary_dim, double base, int scaling, double fac
  *   rotary_dim      even, 2 .. head_dim.  amplitude: finite.
  *   row_offsets, depth, pos_base  as spec_attend.  A row before position 0 is
  *                   skipped (not written); rows of inconsistent offsets or depths
- *                   too, with SPEC_ERR_BAD_INPUT.
+ *                   too, and rows past position 2^32 - 1, with SPEC_ERR_BAD_INPUT.
  *   out             as x; may be x itself with the same stride (in place), else
  *                   they do not overlap. */
 int spec_rotary(const void* x, int64_t x_row_stride, int heads, int head_dim, int dtype,

@@ -94,6 +94,10 @@ __device__ __forceinline__ RowPlace row_place(const RotaryLaunch& p, unsigned r)
   }
   t.pos = q.p + j;
   if (j >= q.count || t.pos < 0) return t;
+  if (t.pos >> 32) {
+    report(p.status, SPEC_ERR_BAD_INPUT);
+    return t;
+  }
   t.row = q.row0 + j;
   if (!p.k_new) return t;
   int page = -1, slot = 0;

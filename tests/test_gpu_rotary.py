@@ -175,3 +175,83 @@ def test_paged_cache_captured():
                     check(out[2 * i + j], *ref.rotate(q[2 * i + j].cpu(), p + j, f.tolist(), False, 1.0), F32)
         pos += 2
     assert int(c.status) == 0
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,D,rot,inter,out_of_place", [
+    (BF16, 6, 2, 128, 128, False, True), (BF16, 3, 1, 80, 50, True, False), (F32, 5, 5, 64, 32, False, True),
+    (BF16, 40, 8, 64, 64, True, False)])
+def test_many_ragged_rows(dtype, Hq, Hkv, D, rot, inter, out_of_place):
+    """Thousands of rows: several to a CTA, of different requests, bad and early rows and pages among them."""
+    B, K, ps = 211, 40, 16
+    g = torch.Generator().manual_seed(Hq)
+    depth = torch.randint(0, K + 1, (B,), generator=g).tolist()
+    pos = torch.randint(0, 400, (B,), generator=g).tolist()
+    pos[3], pos[50], pos[77] = -5, -K - 1, (1 << 40) + 12345
+    rows = paged_ref.Rows(depth, K)
+    need = [max(0, p + n) // ps + 1 if p < 1 << 20 else 0 for p, n in zip(pos, depth)]
+    pages = sum(need) + 3
+    table = paged_ref.random_table(B, need, pages, 32, g)
+    table[8, pos[8] // ps] = pages  # out of range
+    given = list(depth)
+    given[120] = depth[120] + 1     # does not fit its rows
+    q, k, v = (torch.randn((rows.R, h, D), generator=g).to(dtype).to(DEV) for h in (Hq, Hkv, Hkv))
+    caches = [torch.full((1, pages, ps, Hkv, D), 3.0, dtype=dtype, device=DEV) for _ in range(2)]
+    f = spec.spec_rotary_frequencies(rot, 10000.0)
+    at = dict(row_offsets=i32(rows.offsets), depth=i32(given), status=i32([0]))
+    out = torch.full(q.shape, 7.0, dtype=dtype, device=DEV) if out_of_place else q.clone()
+    blank = out.clone()
+    where, td = torch.tensor(pos, device=DEV), table.to(DEV)
+    spec.spec_rotary_append(q if out_of_place else out, k, v, caches[0], caches[1], td, where, B, K, f, out,
+                            interleaved=inter, **at)
+    assert int(at["status"]) == spec.ERR_BAD_INPUT
+    want = blank.cpu().double()
+    err = torch.zeros_like(want)
+    kept = [torch.full((pages, ps, Hkv, D), 3.0, dtype=torch.float64) for _ in range(2)]
+    kept_err = torch.zeros_like(kept[0])
+    qc, kc, vc = q.cpu(), k.cpu(), v.cpu()
+    for i in range(B):
+        if i == 120:
+            continue
+        for j in range(depth[i] + 1):
+            r, p = rows.offsets[i] + j, pos[i] + j
+            if not 0 <= p < 1 << 32:
+                continue
+            want[r], err[r] = ref.rotate(qc[r], p, f.tolist(), inter, 1.0)
+            page = int(table[i, p // ps]) if p // ps < table.shape[1] else -1
+            if 0 <= page < pages:
+                kept[0][page, p % ps], kept_err[page, p % ps] = ref.rotate(kc[r], p, f.tolist(), inter, 1.0)
+                kept[1][page, p % ps] = vc[r].double()
+    check(out, want, err, dtype)
+    check(caches[0][0], kept[0], kept_err, dtype)
+    assert torch.equal(caches[1][0].cpu().double(), kept[1])
+
+
+def test_many_rows_captured_on_a_stream():
+    """Positions and depths that change between replays; what lies behind the last row stays."""
+    B, K, H, D = 130, 31, 2, 64
+    x = torch.randn((B * (K + 1) + 4, H, D), device=DEV)
+    out = torch.full(x.shape, 5.0, device=DEV)
+    f = spec.spec_rotary_frequencies(D)
+    pos, depth, offsets = torch.zeros(B, dtype=torch.int64, device=DEV), i32([0] * B), i32([0] * (B + 1))
+    status, side, graph = i32([0]), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        spec.spec_rotary(x, f, pos, B, K, out, row_offsets=offsets, depth=depth, status=status)
+    for step in range(3):
+        n = [(5 * i + 11 * step) % (K + 1) for i in range(B)]
+        rows = paged_ref.Rows(n, K)
+        where = [(1 << 20) * step + 7 * i for i in range(B)]
+        pos.copy_(torch.tensor(where))
+        depth.copy_(i32(n))
+        offsets.copy_(i32(rows.offsets))
+        out.fill_(5.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert int(status) == 0 and bool((out[rows.R:] == 5).all())
+        xc = x.cpu()
+        want, err = xc.double(), torch.zeros(x.shape, dtype=torch.float64)
+        for i in range(B):
+            for j in range(n[i] + 1):
+                r = rows.offsets[i] + j
+                want[r], err[r] = ref.rotate(xc[r], where[i] + j, f.tolist(), False, 1.0)
+        check(out[:rows.R], want[:rows.R], err[:rows.R], F32)
