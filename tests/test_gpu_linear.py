@@ -369,3 +369,148 @@ def test_another_stream():
         out = c.attend()
     side.synchronize()
     c.check(out, before)
+
+
+# Many requests of a few rows: from two heads' states per SM on, CTAs that stay and bring states by bulk copies.
+FEW = [(8, 8, 128, 128), (16, 8, 64, 64), (32, 8, 64, 128), (8, 8, 128, 64)]
+
+
+def few(shape, K, dtype=BF16, B=40, seed=2, **kw):
+    g = torch.Generator().manual_seed(seed)
+    return Case(torch.randint(0, K + 1, (B,), generator=g).tolist(), K, *shape, dtype=dtype, seed=seed, **kw)
+
+
+@pytest.mark.parametrize("dtype,K", [(BF16, 0), (BF16, 2), (BF16, 7), (BF16, 10), (F32, 0), (F32, 1), (F32, 7)])
+@pytest.mark.parametrize("shape", FEW)
+def test_many_requests(shape, K, dtype):
+    """Starts that are shared, fresh or in place, all in one call; then the same round by a commit."""
+    c = few(shape, K, dtype)
+    c.start[3] = c.start[5] = c.start[8]
+    c.start[4] = -1
+    c.to[6], c.to[20] = c.start[6], c.start[20]
+    before = c.states.clone()
+    out = c.attend()
+    assert int(c.status) == 0
+    c.check(out, before)
+    c.states.copy_(before)
+    assert torch.equal(c.attend(to=None), out)
+    assert torch.equal(c.states, before)
+    accepted = [(7 * i) % (n + 1) for i, n in enumerate(c.depth)]
+    for i, a in enumerate(accepted):
+        c.k[c.offsets[i] + a + 1:c.offsets[i + 1]] = math.nan
+        c.v[c.offsets[i] + a + 1:c.offsets[i + 1]] = -math.inf
+        c.decay[c.offsets[i] + a + 1:c.offsets[i + 1]] = math.nan  # a rejected row's decay is not looked at
+    c.commit(accepted)
+    assert int(c.status) == 0
+    for i, a in enumerate(accepted):
+        for x in (c.k, c.v, c.decay):
+            x[c.offsets[i] + a + 1:c.offsets[i + 1]] = 0
+    c.check(None, before, accepted)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("shape", FEW)
+def test_many_requests_early_and_idle(shape, dtype):
+    c = few(shape, 3, dtype)
+    c.pos = [(-4, -1, 5, -2, 0)[i % 5] for i in range(c.B)]
+    for i in range(0, c.B, 5):  # idle, whatever their rows hold
+        c.k[c.offsets[i]:c.offsets[i + 1]] = math.nan
+        c.q[c.offsets[i]:c.offsets[i + 1]] = math.inf
+    c.start[0] = -1
+    before = c.states.clone()
+    out = c.attend()
+    assert int(c.status) == 0
+    assert not bool(c.states[1, c.to[0]].any()) and torch.equal(c.states[1, c.to[5]], before[1, c.start[5]])
+    for i in range(0, c.B, 5):
+        assert not bool(out[c.offsets[i]:c.offsets[i + 1]].any())
+        c.k[c.offsets[i]:c.offsets[i + 1]] = 0
+        c.q[c.offsets[i]:c.offsets[i + 1]] = 0
+    c.check(out, before)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_many_requests_bad_ones(dtype):
+    """Bad slots, depths and accepted lengths among good requests, which are served (one's state, to slot -1, goes
+    nowhere); growth and NaN stay where they are."""
+    c = few(FEW[0], 3, dtype)
+    before, start, to = c.states.clone(), list(c.start), list(c.to)
+    bad = {1: "start", 2: "to", 7: "depth", 39: "start"}
+    depth = list(c.depth)
+    for i, what in bad.items():
+        if what == "start":
+            c.start[i] = (c.slots, -7)[i == 39]
+        elif what == "to":
+            c.to[i] = -1
+        else:
+            depth[i] = depth[i] + 1
+    c.decay[c.offsets[9], 4] = 0.25
+    c.v[c.offsets[11], 2, 3] = math.nan
+    out = c.attend(depth=i32(depth))
+    assert int(c.status) == spec.ERR_BAD_INPUT
+    c.decay[c.offsets[9], 4] = 0
+    c.start, c.to = start, to
+    for i in range(c.B):
+        rows = slice(c.offsets[i], c.offsets[i + 1])
+        got, state = out[rows].cpu().double(), c.states[1, to[i]].cpu().double()
+        if i in bad:
+            assert torch.equal(c.states[1, to[i]], before[1, to[i]])
+        if i in bad and i != 2:
+            assert bool((got == 7).all())
+            continue
+        heads = [h for h in range(c.H) if (i, h) != (11, 2)]
+        o, o_tol, s, s_tol = c.want(i, before)
+        assert bool(((got - o).abs() <= o_tol)[:, heads].all())
+        assert i == 2 or bool(((state - s).abs() <= s_tol)[heads].all())
+    s = c.states[1, to[11], 2]
+    assert bool(s[:, 3].isnan().all()) and bool(torch.isfinite(s[:, :3]).all()) and bool(torch.isfinite(s[:, 4:]).all())
+    c.v[c.offsets[11], 2, 3] = 0
+    c.status.zero_()
+    c.states.copy_(before)
+    c.commit([n + (i == 1) - (i == 2) * (n + 1) for i, n in enumerate(c.depth)])
+    assert int(c.status) == spec.ERR_BAD_INPUT
+    for i in range(c.B):
+        state = c.states[1, to[i]].cpu().double()
+        if i in (1, 2):
+            assert torch.equal(c.states[1, to[i]], before[1, to[i]])
+        else:
+            _, _, s, s_tol = c.want(i, before)
+            assert bool(((state - s).abs() <= s_tol).all())
+
+
+@pytest.mark.parametrize("K", [3, 40])
+def test_captured_round(K):
+    """A verification and its commit in a graph on a stream of its own, replayed as rows, accepted lengths and slots
+    change; another graph shares the workspace."""
+    c = few((8, 8, 64, 64), K, B=48)
+    accepted, start, to = i32([0] * c.B), i32(c.start), i32(c.to)
+    out = torch.zeros((c.R + 1, c.Hq, c.Dv), dtype=c.dtype, device=DEV)
+    decay, at = c.decay.to(DEV), c.at()
+
+    def verify():
+        spec.spec_linear_attend(c.q, c.k, c.v, decay, c.states, start, None, c.B, K, out, c.ws, **at)
+
+    def commit():
+        spec.spec_linear_commit(c.k, c.v, decay, c.states, start, to, accepted, c.B, K, c.ws, **at)
+    graphs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+    for graph, call in zip(graphs, (verify, commit)):
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.graph(graph, stream=side):
+            call()
+    for step in range(3):
+        before = c.states.clone()
+        kept = [(step + 3 * i) % (n + 1) for i, n in enumerate(c.depth)]
+        accepted.copy_(i32(kept))
+        graphs[0].replay()
+        graphs[1].replay()
+        torch.cuda.synchronize()
+        assert int(c.status) == 0
+        for i in range(c.B):
+            o, o_tol, s, s_tol = c.want(i, before, kept[i] + 1)
+            got = out[c.offsets[i]:c.offsets[i + 1]].cpu().double()
+            assert bool(((got - o).abs() <= o_tol).all())
+            assert bool(((c.states[1, c.to[i]].cpu().double() - s).abs() <= s_tol).all())
+        c.q.copy_(torch.randn(c.q.shape, device=DEV))
+        c.start, c.to = c.to, c.start  # the next round starts from this one's states
+        start.copy_(i32(c.start))
+        to.copy_(i32(c.to))

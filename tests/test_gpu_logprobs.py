@@ -174,3 +174,68 @@ def test_unaligned_view_graph_and_stream():
         for i in range(B):
             plain.check_row(i, 0, logits[i].cpu(), int(tokens[i, 0]), 0.9, 6)
     assert int(plain.status) == 0
+
+
+@pytest.mark.parametrize("B,K,V,n", [(700, 2, 611, 3), (513, 0, 2500, 0), (1500, 1, 33, 32)])
+def test_many_requests(B, K, V, n):
+    """More requests than a CTA lists; bad ones among them, whose rows the others' places do not depend on."""
+    g = torch.Generator().manual_seed(B)
+    depth = torch.randint(0, K + 1, (B,), generator=g).tolist()
+    offsets = [0]
+    for d in depth:
+        offsets.append(offsets[-1] + d + 1)
+    logits = torch.randn((offsets[-1], V), generator=g).to(BF16)
+    tokens = torch.randint(0, V, (B, K + 1), generator=g)
+    accepted = [int(torch.randint(0, d + 1, (1,), generator=g)) for d in depth]
+    given = list(accepted)
+    bad = {2, B // 2, B - 1}
+    for i in bad:
+        given[i] = depth[i] + 1
+    call = Call(logits.to(DEV), tokens.to(torch.int32).to(DEV), B, K, n, 0.8, i32(offsets), i32(depth), i32(given))
+    assert int(call.status) == spec.ERR_BAD_INPUT
+    for i in range(B):
+        for j in range(K + 1):
+            if i in bad or j > accepted[i]:
+                call.nothing(i, j)
+            elif i % 23 == 0 or i > B - 5:
+                call.check_row(i, j, logits[offsets[i] + j], int(tokens[i, j]), 0.8, n)
+    x = logits.double() / 0.8
+    lse = torch.logsumexp(x, 1)
+    got = call.lp.cpu().double()
+    for i in range(B):
+        if i not in bad:
+            for j in range(accepted[i] + 1):
+                r = offsets[i] + j
+                want = float(x[r, tokens[i, j]] - lse[r])
+                assert abs(float(got[i, j]) - want) <= ref.logprob_bound(logits[r], 0.8, want)
+
+
+@pytest.mark.parametrize("V,B,K,n", [(40961, 12, 4, 32), (201088, 3, 0, 32), (201089, 1, 16, 20)])
+def test_captured_rounds(V, B, K, n):
+    """Rows in many pieces that end inside spans; other accepted lengths, other tokens, other logits at each replay."""
+    g = torch.Generator().manual_seed(V)
+    R = B * (K + 1)
+    logits = (torch.randn((R, V), generator=g) * 2).to(BF16).to(DEV)
+    tokens, accepted = i32([[0] * (K + 1)] * B), i32([0] * B)
+    call = Call(logits, tokens, B, K, n, 1.0, accepted=accepted)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        call.run()
+    for step in range(3):
+        kept = [(i + step * (K + 1) // 2) % (K + 1) for i in range(B)]
+        accepted.copy_(i32(kept))
+        tokens.copy_(torch.randint(0, V, (B, K + 1), generator=g))
+        if step == 2:
+            logits.copy_(logits.flip(0).roll(1234, 1))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert int(call.status) == 0
+        rows, picked = logits.cpu(), tokens.tolist()
+        for i in range(B):
+            for j in range(K + 1):
+                if j <= kept[i]:
+                    if (i + j) % 3 == 0:
+                        call.check_row(i, j, rows[i * (K + 1) + j], picked[i][j], 1.0, n)
+                else:
+                    call.nothing(i, j)
