@@ -808,8 +808,7 @@ cudaError_t launch_phases(const LinearLaunch& p, const LinearPlan& plan, cudaStr
     if (err != cudaSuccess) return err;
   }
   if (plan.staged) {
-    const cudaError_t err = launch_after_previous(linear_scan_kernel, dim3((unsigned)(p.rows.B * p.H), (unsigned)(DK * DV / 1024)), dim3(256),
-                                0, stream, p, plan);
+    const cudaError_t err = launch_linear_scan(p, plan, stream);
     if (err != cudaSuccess) return err;
   }
   return p.q ? launch_tc<DK, DV, true>(p, plan, kAllSegments, stream)
@@ -817,6 +816,11 @@ cudaError_t launch_phases(const LinearLaunch& p, const LinearPlan& plan, cudaStr
 }
 
 }  // namespace
+
+cudaError_t launch_linear_scan(const LinearLaunch& p, const LinearPlan& plan, cudaStream_t stream) {
+  return launch_after_previous(linear_scan_kernel, dim3((unsigned)(p.rows.B * p.H), (unsigned)((p.Dk * p.Dv + 1023) / 1024)),
+                               dim3(256), 0, stream, p, plan);
+}
 
 cudaError_t launch_linear_tc(const LinearLaunch& p, const LinearPlan& plan, cudaStream_t stream) {
   if (p.Dk == 64) return p.Dv == 64 ? launch_phases<64, 64>(p, plan, stream) : launch_phases<64, 128>(p, plan, stream);

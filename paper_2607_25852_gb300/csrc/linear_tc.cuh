@@ -56,4 +56,7 @@ inline LinearPlan linear_plan(int B, int K, int q_heads, int kv_heads) {
 // p.q null: states only.
 cudaError_t launch_linear_tc(const LinearLaunch& p, const LinearPlan& plan, cudaStream_t stream);
 
+// The segments' first states out of the sums of those before them and the request's own.
+cudaError_t launch_linear_scan(const LinearLaunch& p, const LinearPlan& plan, cudaStream_t stream);
+
 }  // namespace spec

@@ -514,3 +514,41 @@ def test_captured_round(K):
         c.start, c.to = c.to, c.start  # the next round starts from this one's states
         start.copy_(i32(c.start))
         to.copy_(i32(c.to))
+
+
+@pytest.mark.parametrize("dtype,shape", [(F32, (2, 2, 64, 64)), (F32, (6, 2, 128, 128)), (BF16, (3, 1, 72, 96)), (BF16, (4, 2, 256, 40))])
+@pytest.mark.parametrize("K", [47, 200])
+def test_parts_of_long_calls(K, shape, dtype):
+    """Odd sizes and fp32 divided along the rows: in place, from a shared slot, from zeros, some rows before position 0,
+    an idle request, one too long for its rows; then the same rows by a commit of some of them."""
+    c = Case([K, K - 20, K, 15, K, K, 2], K, *shape, dtype=dtype)
+    c.start[5] = c.start[1]
+    c.start[2] = -1
+    c.to[0] = c.start[0]
+    c.pos = [0, 1000, -30, 7, -(K + 1), 0, -1]
+    bad, bad_depth = 5, list(c.depth)
+    bad_depth[bad] -= 1
+    c.q[c.offsets[4]:c.offsets[5]] = math.nan
+    before = c.states.clone()
+    out = c.attend(depth=i32(bad_depth))
+    assert int(c.status) == spec.ERR_BAD_INPUT
+    assert bool((out[c.offsets[bad]:c.offsets[bad + 1]] == 7).all())
+    assert torch.equal(c.states[1, c.to[bad]], before[1, c.to[bad]])
+    c.q[c.offsets[4]:c.offsets[5]] = 0
+    c.status.zero_()
+    c.states.copy_(before)
+    again = c.attend()
+    assert int(c.status) == 0
+    c.check(again, before)
+    served = [i for i in range(c.B) if i != bad]
+    for i in served:
+        assert torch.equal(out[c.offsets[i]:c.offsets[i + 1]], again[c.offsets[i]:c.offsets[i + 1]])
+    accepted = [n // (i + 1) for i, n in enumerate(c.depth)]
+    c.states.copy_(before)
+    for i, a in enumerate(accepted):
+        c.k[c.offsets[i] + a + 1:c.offsets[i + 1]] = math.nan
+    c.commit(accepted)
+    assert int(c.status) == 0
+    for i, a in enumerate(accepted):
+        c.k[c.offsets[i] + a + 1:c.offsets[i + 1]] = 0
+    c.check(None, before, accepted)
