@@ -9,7 +9,7 @@
 // memory, i.e. transposed, so that each operand is where it arises:
 //   scores [i x j]   = Q K^T        Q and K as they lie in shared memory
 //   O2^T   [v x i]   = S^T Q^T      S^T from tensor memory
-//   U^T    [v x k]   = V'^T K       V'^T from tensor memory, K as it lies
+//   U^T    [v x k]   = V'^T K       V' from shared memory, K as it lies
 //   O1^T   [v x i]   = V^T P^T      V as it lies, P from shared memory
 // The state itself stays in fp32 registers: thread (v, half of k) adds U to it and
 // stores it as operand for the next chunk in two bf16 numbers (2^-16 relative);
@@ -29,11 +29,21 @@
 // their own states.
 //
 // Warp 7 lists the chunks, with their decays summed up, in a ring of records that
-// all others go by.  2 and 3 load, 6 issues the MMAs, 8 to 11 make V', 12 to 19
-// keep the state, 0, 1, 4 and 5 (their lanes hold the scores) make P, 20 to 27
-// read O and store it by way of shared memory; where only states are made 20 to 23
-// make half of V'.  Loops stay rolled where registers allow: the roles' code
-// together does not fit the instruction caches otherwise.
+// all others go by.  2 and 3 load, 6 issues the MMAs, 8 to 11 and 28 to 31 (20 to 23
+// where only states are made) make V', 12 to 19 keep the state, 0, 1, 4 and 5 (their
+// lanes hold the scores) make P, 20 to 27 read O and store it by way of shared memory.
+// U is made in two halves, which the state's two groups of warps take as they come, and
+// before O2, whose operand they write behind it.
+//
+// What bounds it: of the 4,800 cycles of a chunk of heads of 128 the tensor cores work
+// 1,850.  The MMAs' thread is never idle: their issue takes those, and what is between
+// them as much, as every role's code is fetched again and again (62 KB together, 81 % of
+// requests hit the instruction cache).  So loops stay rolled where registers allow: a
+// variant with other code in the loops, but no more work, hit 68 % and took 198 us for
+// 169.  Two threads that issue MMAs took 206, a table of steps in place of the code 314.
+// Measured: 4 requests of 4,096 rows of 38 heads of 128 164 us (4.0 TB/s), 2 of 16,384 of
+// 32 heads 523 (in segments), 64 of 256 of 32 heads 180 (4.5 TB/s), 64 of 64 73 (5.5).
+// (With V' by four warps by way of tensor memory 185, 542, 197 and 95.)
 #include "attend_ring.cuh"
 #include "linear_tc.cuh"
 
@@ -43,10 +53,11 @@ namespace {
 
 constexpr int kHalf = kLinChunk * 128;  // 64 elements of a chunk's rows
 constexpr int kRecords = 8;             // chunks listed ahead
-constexpr int kTS = 0, kTV = 128, kTU = 224, kTX = 352, kTO = 416;  // columns: S, V', U, scores and O1, O2
-constexpr int kTV1 = 352;                // the second V' where only states are made
+constexpr int kTS = 0, kTU = 128;       // columns: S, U
+constexpr int kTX = 256, kTO = 320;     // scores and then O1, O2, of even chunks; those of odd ones 128 on
 constexpr int kLinTmem = 512;
-constexpr int kOutThreads = 28 * 32, kSumThreads = 24 * 32;
+constexpr int kOutThreads = 32 * 32, kSumThreads = 24 * 32;
+constexpr int kWeighers = 8;            // warps that make V'
 
 enum LinPhase { kSegmentSums, kLastSegment, kAllSegments };
 
@@ -72,22 +83,25 @@ struct alignas(16) Record {
 };
 
 struct LinControl {
-  uint64_t full[4], empty[4], listed[kRecords], used[kRecords];
-  uint64_t state_ready, sums, sums_read, scores, p_ready, out_ready, out_read, drained;
+  uint64_t full[4], empty[4], q_empty[4], listed[kRecords], used[kRecords];
+  uint64_t state_ready, operand_read, scores, p_ready, drained;
+  uint64_t sums[2], sums_read[2];  // U of half of the keys there, and read
   // of even and odd chunks, as some warps may be a chunk ahead of others: V' there; where only states are made V'
-  // read; bad_row there
-  uint64_t weighted[2], read[2], noted[2];
+  // read; O there and read.  Of every fourth: bad_row there
+  uint64_t weighted[2], read[2], out_ready[2], out_read[2], noted[4];
   uint64_t staged, stored;  // O in shared memory, and out of it
   Record records[kRecords];
-  int bad_row[2][128];
+  unsigned long long bad_row[4][128];  // chunk << 8 | 255 - the first row that is not finite, of every fourth chunk
   int aborted;
   uint32_t tmem;
 };
 
-// Chunks in shared memory at a time (P and O take 32 KB of its 227, the rest 14).
-constexpr int lin_stage_bytes(int DK, int DV, bool out) { return kLinChunk * 2 * ((out ? 2 : 1) * DK + DV); }
+// In shared memory: the chunks' K and V (V' is not the only reader of V), their Q, which
+// are free again earlier, V' (twice where only states are made), P's two parts, and O.
+constexpr int lin_q_stages(int DK) { return DK == 64 ? 4 : 2; }
 constexpr int lin_smem(int DK, int DV, bool out, int stages) {
-  return stages * lin_stage_bytes(DK, DV, out) + (out ? 4 * kHalf : 0) + 1024;
+  // (a product over 128 values of 64 reads what lies behind them: P, or nothing)
+  return kLinChunk * 2 * (stages * (DK + DV) + (out ? lin_q_stages(DK) * DK + 4 * DV + 128 : 6 * DV + 64)) + 1024;
 }
 constexpr int lin_stages(int DK, int DV, bool out) { return lin_smem(DK, DV, out, 4) <= 213 * 1024 ? 4 : 3; }
 
@@ -159,12 +173,6 @@ __device__ __forceinline__ void tmem_st8(uint32_t addr, const uint32_t (&r)[8]) 
                "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                : "memory");
 }
-__device__ __forceinline__ void tmem_st4(uint32_t addr, const uint32_t (&r)[4]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]),
-               "r"(r[3])
-               : "memory");
-}
-
 // Two numbers as bf16, rounded, and what is left of them.
 __device__ __forceinline__ uint32_t round_pair(f32x2& x) {
   const uint32_t b = last_pair(x);
@@ -177,20 +185,22 @@ template <int DK, int DV, bool kOut>
 __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
     linear_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                      const __grid_constant__ CUtensorMap tmV, const __grid_constant__ LinTcLaunch a) {
-  constexpr int kWeighers = kOut ? 4 : 8;  // warps that make V'
   constexpr int kKeyBytes = kLinChunk * DK * 2, kValueBytes = kLinChunk * DV * 2;
-  constexpr int kKeyAt = kOut ? kKeyBytes : 0, kValueAt = kKeyAt + kKeyBytes, kStage = kValueAt + kValueBytes;
-  constexpr int kStages = lin_stages(DK, DV, kOut);
+  constexpr int kValueAt = kKeyBytes, kStage = kKeyBytes + kValueBytes;
+  constexpr int kStages = lin_stages(DK, DV, kOut), kQueries = kOut ? lin_q_stages(DK) : 1;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   __shared__ LinControl ctl;
   const LinearLaunch& p = a.p;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t ring = smem_u32(smem);
-  uint8_t* pmem = smem + kStages * kStage;  // P's two parts
-  uint8_t* omem = pmem + 2 * kHalf;          // O, row by row
+  constexpr int kQueryAt = kStages * kStage, kWeightedAt = kQueryAt + (kOut ? kQueries * kKeyBytes : 0);
+  uint8_t* pmem = smem + kWeightedAt + 3 * kValueBytes;  // P's two parts
+  uint8_t* omem = pmem + 2 * kHalf;                       // O, row by row
 
+  for (int x = tid; x < 4 * 128; x += blockDim.x) ctl.bad_row[x >> 7][x & 127] = 0;
   if (tid == 0) {
+    for (int s = 0; s < kQueries; ++s) mbar_init(&ctl.q_empty[s], 1);
     for (int s = 0; s < kStages; ++s) {
       mbar_init(&ctl.full[s], 1);
       mbar_init(&ctl.empty[s], 1 + kWeighers);
@@ -200,18 +210,19 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
       mbar_init(&ctl.used[s], 2 + kWeighers + 8 + (kOut ? 4 + 8 : 0));
     }
     mbar_init(&ctl.state_ready, 8);
-    mbar_init(&ctl.sums, 1);
-    mbar_init(&ctl.sums_read, 8);
+    mbar_init(&ctl.operand_read, 1);
     mbar_init(&ctl.scores, 1);
     mbar_init(&ctl.p_ready, 4);
-    mbar_init(&ctl.out_ready, 1);
-    mbar_init(&ctl.out_read, 8);
     mbar_init(&ctl.drained, 1);
     for (int s = 0; s < 2; ++s) {
       mbar_init(&ctl.weighted[s], kWeighers);
-      mbar_init(&ctl.noted[s], 4);
+      mbar_init(&ctl.sums[s], 1);
+      mbar_init(&ctl.sums_read[s], 4);
       mbar_init(&ctl.read[s], 1);
+      mbar_init(&ctl.out_ready[s], 1);
+      mbar_init(&ctl.out_read[s], 8);
     }
+    for (int s = 0; s < 4; ++s) mbar_init(&ctl.noted[s], kWeighers);
     mbar_init(&ctl.staged, 8);
     mbar_init(&ctl.stored, 8);
     ctl.aborted = 0;
@@ -259,11 +270,12 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
     __syncwarp();
     ++c;
   };
-  // registers: 28 warps of 72 are split as 64, 64, 72, 104 twice, 48 twice per 4 warps; 24 of 80 as 40, 64, 80, 104
-  // twice, 80
+  // registers: 32 warps of 64 are split as 56, 56, 48, 104 twice, 48 three times per 4 warps; 24 of 80 as 40, 64, 80,
+  // 104 twice, 80
   const bool scorer = kOut && warp < 8 && (warp & 3) < 2;
   if (warp < 8) {
-    if (kOut || warp >= 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    if (kOut) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    else if (warp >= 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     else asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
     if (scorer) {
       // ---- P: row d, half `set` of the columns ----
@@ -277,14 +289,14 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
           const f32x2 minus = pair(-1.0f, -1.0f);
           const f32x2 gh = pair(r->hi[d], r->hi[d]), gl = pair(r->lo[d], r->lo[d]);
 #pragma unroll 1
-          for (int half = 0; half < 2; ++half) {
-            const int j0 = 32 * set + 16 * half;
-            uint32_t w[16], hi[8], lo[8];
+          for (int part = 0; part < 4; ++part) {  // eight columns
+            const int j0 = 32 * set + 8 * part;
+            uint32_t w[8], hi[4] = {0u, 0u, 0u, 0u}, lo[4] = {0u, 0u, 0u, 0u};
             if (quad >= set) {  // (columns 32 to 63 are behind rows 0 to 31)
-              tmem_ld16(from + 16 * half, w);
+              tmem_ld8(from + 128 * (n & 1) + 8 * part, w);
               wait_ld(w);
 #pragma unroll
-              for (int y = 0; y < 8; y += 2) {
+              for (int y = 0; y < 4; y += 2) {
                 const int j = j0 + 2 * y;
                 const float4 h = *reinterpret_cast<const float4*>(&r->hi[j]), l = *reinterpret_cast<const float4*>(&r->lo[j]);
 #pragma unroll
@@ -296,16 +308,10 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
                   hi[y + z] = round_pair(x), lo[y + z] = last_pair(x);
                 }
               }
-            } else {
-#pragma unroll
-              for (int y = 0; y < 8; ++y) hi[y] = lo[y] = 0u;
             }
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-              uint8_t* at = pmem + d * 128 + (((4 * set + 2 * half + y) ^ (d & 7)) << 4);
-              *reinterpret_cast<uint4*>(at) = make_uint4(hi[4 * y], hi[4 * y + 1], hi[4 * y + 2], hi[4 * y + 3]);
-              *reinterpret_cast<uint4*>(at + kHalf) = make_uint4(lo[4 * y], lo[4 * y + 1], lo[4 * y + 2], lo[4 * y + 3]);
-            }
+            uint8_t* at = pmem + d * 128 + (((4 * set + part) ^ (d & 7)) << 4);
+            *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+            *reinterpret_cast<uint4*>(at + kHalf) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
           }
           tc_fence_before();
           proxy_fence();
@@ -339,25 +345,27 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
         __syncwarp();
         ++c;
         if (rows == 0) continue;
-        const int s = n % kStages;
-        const uint32_t use = n / kStages;
-        ++n;
+        const uint32_t chunk = n++;
         if (!mine) continue;
+        const int s = chunk % kStages;
+        const uint32_t use = chunk / kStages;
         if (use > 0) wait(&ctl.empty[s], use - 1);
+        const int to_q = kQueryAt + (kOut ? (int)(chunk % kQueries) * kKeyBytes : 0);
+        if (kOut && chunk >= kQueries) wait(&ctl.q_empty[chunk % kQueries], chunk / kQueries - 1);
         if (!ok) break;
         if (a.tma && rows == kLinChunk) {
           if (lane == 0) {
-            mbar_expect_tx(&ctl.full[s], kStage);
-            if (kOut) bring(&tmQ, DK, hq * DK, row, s * kStage, &ctl.full[s]);
-            bring(&tmK, DK, h * DK, row, s * kStage + kKeyAt, &ctl.full[s]);
+            mbar_expect_tx(&ctl.full[s], kStage + (kOut ? kKeyBytes : 0));
+            if (kOut) bring(&tmQ, DK, hq * DK, row, to_q, &ctl.full[s]);
+            bring(&tmK, DK, h * DK, row, s * kStage, &ctl.full[s]);
             bring(&tmV, DV, h * DV, row, s * kStage + kValueAt, &ctl.full[s]);
           }
           __syncwarp();
           continue;
         }
         const uint32_t at = ring + s * kStage;
-        if (kOut) copy(static_cast<const __nv_bfloat16*>(p.q) + row * p.q_row + (int64_t)hq * DK, p.q_row, DK, at, rows);
-        copy(static_cast<const __nv_bfloat16*>(p.k) + row * p.k_row + (int64_t)h * DK, p.k_row, DK, at + kKeyAt, rows);
+        if (kOut) copy(static_cast<const __nv_bfloat16*>(p.q) + row * p.q_row + (int64_t)hq * DK, p.q_row, DK, ring + to_q, rows);
+        copy(static_cast<const __nv_bfloat16*>(p.k) + row * p.k_row + (int64_t)h * DK, p.k_row, DK, at, rows);
         copy(static_cast<const __nv_bfloat16*>(p.v) + row * p.v_row + (int64_t)h * DV, p.v_row, DV, at + kValueAt, rows);
         asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
         proxy_fence();
@@ -369,7 +377,7 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
       if (elect_one()) {
         constexpr uint32_t kScores = umma_idesc_bf16(128, kLinChunk);
         constexpr uint32_t kOut1 = umma_idesc_bf16(128, kLinChunk) | kTransposeA;
-        constexpr uint32_t kSums = umma_idesc_bf16(128, DK) | kTransposeB;
+        constexpr uint32_t kSums = umma_idesc_bf16(128, 64) | kTransposeA | kTransposeB;
         auto need = [&](uint64_t* bar, uint32_t parity) { ok = ok && wait_one(bar, parity); };
         // four products over 16 each: A and B in shared memory so many bytes apart, or A in tensor memory
         auto four = [&](int to, uint32_t x, int x_step, uint32_t y, int y_step, uint32_t kind, bool fresh) {
@@ -379,11 +387,16 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
             umma_bf16(tmem + to, desc(x0 + (m * x_step >> 4), x_step == 2048 ? kHiV : kHiKQ), desc(y0 + (m * y_step >> 4), kHiKQ),
                       kind, m > 0 || !fresh ? 1u : 0u);
         };
-        auto four_tmem = [&](int to, int x, uint32_t y0, int y_step, uint32_t kind, bool fresh) {
+        auto four_tmem = [&](int to, int x, uint32_t y, uint32_t kind, bool fresh) {
 #pragma unroll
           for (int m = 0; m < 4; ++m)
-            umma_bf16_tmem(tmem + to, tmem + x + 8 * m, desc(y0 + (m * y_step >> 4), y_step == 2048 ? kHiV : kHiKQ), kind,
-                           m > 0 || !fresh ? 1u : 0u);
+            umma_bf16_tmem(tmem + to, tmem + x + 8 * m, desc(lo_kq(y) + (m * 32 >> 4), kHiKQ), kind, m > 0 || !fresh ? 1u : 0u);
+        };
+        auto four_rows = [&](int to, uint32_t x, uint32_t y, uint32_t kind, bool fresh) {  // both transposed
+#pragma unroll
+          for (int m = 0; m < 4; ++m)
+            umma_bf16(tmem + to, desc(lo_v(x, kHalf) + (m * 2048 >> 4), kHiV), desc(lo_v(y, kHalf) + (m * 2048 >> 4), kHiV), kind,
+                      m > 0 || !fresh ? 1u : 0u);
         };
         for (; ok; ++c) {
           need(&ctl.listed[c % kRecords], c / kRecords);
@@ -394,39 +407,53 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
           if (none) break;
           if (rows == 0) continue;
           const int s = n % kStages;
-          const uint32_t q = ring + s * kStage, k = q + kKeyAt, v = q + kValueAt, pbuf = ring + kStages * kStage;
+          const uint32_t k = ring + s * kStage, v = k + kValueAt, pbuf = smem_u32(pmem), half = n & 1;
+          const uint32_t q = ring + kQueryAt + (kOut ? n % kQueries * kKeyBytes : 0);
+          const int tx = kTX + 128 * half, to = kTO + 128 * half;
           need(&ctl.full[s], n / kStages);
           if (kOut) {
-            if (n > 0) need(&ctl.out_read, n - 1);
+            if (n > 1) need(&ctl.out_read[half], (n >> 1) - 1);
             if (!ok) break;
             tc_fence_after();
             // rows 64 to 127 of the scores are of what lies behind Q, and are not read
 #pragma unroll 1
-            for (int h = 0; h < DK / 64; ++h) four(kTX, q + h * kHalf, 32, k + h * kHalf, 32, kScores, h == 0);
+            for (int h = 0; h < DK / 64; ++h) four(tx, q + h * kHalf, 32, k + h * kHalf, 32, kScores, h == 0);
             umma_commit(&ctl.scores);
+          }
+          // the state's half of the keys takes U while the other's is made, and S' while the rest is
+          need(&ctl.weighted[half], n >> 1);
+#pragma unroll 1
+          for (int x = 0; x < 2; ++x) {
+            if (n > 0) need(&ctl.sums_read[x], n - 1);
+            if (n > 0 && DK == 64 && x == 0) need(&ctl.sums_read[1], n - 1);  // one product makes both halves
+            if (!ok) break;
+            tc_fence_after();
+            if (x < DK / 64) {
+#pragma unroll 1
+              for (int h = 0; h < 3; ++h)
+                four_rows(kTU + 64 * x, ring + kWeightedAt + ((kOut ? 0 : 3 * half) + h) * kValueBytes, k + x * kHalf, kSums, h == 0);
+            }
+            umma_commit(&ctl.sums[x]);
+          }
+          if (!ok) break;
+          if (!kOut) umma_commit(&ctl.read[half]);
+          if (kOut) {
             need(&ctl.state_ready, n);
             if (!ok) break;
             tc_fence_after();
 #pragma unroll 1
             for (int h = 0; h < 2 * (DK / 64); ++h)  // the upper parts, then the rests
-              four_tmem(kTO, kTS + 32 * h, lo_kq(q + (h % (DK / 64)) * kHalf), 32, kScores, h == 0);
+              four_tmem(to, kTS + 32 * h, q + (h % (DK / 64)) * kHalf, kScores, h == 0);
+            umma_commit(&ctl.operand_read);
+            umma_commit(&ctl.q_empty[n % kQueries]);
           }
-          need(&ctl.weighted[n & 1], n >> 1);
-          if (n > 0) need(&ctl.sums_read, n - 1);
-          if (!ok) break;
-          tc_fence_after();
-#pragma unroll 1
-          for (int h = 0; h < 3; ++h)
-            four_tmem(kTU, (kOut || !(n & 1) ? kTV : kTV1) + 32 * h, lo_v(k, kHalf), 2048, kSums, h == 0);
-          umma_commit(&ctl.sums);
-          if (!kOut) umma_commit(&ctl.read[n & 1]);
           if (kOut) {
             need(&ctl.p_ready, n);
             if (!ok) break;
             tc_fence_after();
 #pragma unroll 1
-            for (int h = 0; h < 2; ++h) four(kTX, v, 2048, pbuf + h * kHalf, 32, kOut1, h == 0);
-            umma_commit(&ctl.out_ready);
+            for (int h = 0; h < 2; ++h) four(tx, v, 2048, pbuf + h * kHalf, 32, kOut1, h == 0);
+            umma_commit(&ctl.out_ready[half]);
           }
           umma_commit(&ctl.empty[s]);
           ++n;
@@ -501,69 +528,60 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
         mbar_arrive(&ctl.listed[c % kRecords]);
       }
     }
-  } else if (warp < 12 || (!kOut && warp >= 20)) {
-    // ---- V': value `d` of the rows (of half of them where there are two groups), weighted, in three parts ----
-    const int d = (warp & 3) * 32 + lane, group = warp >= 20;
-    const bool mine = (warp & 3) * 32 < DV;
-    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const int v8 = (d & 63) >> 3;
+  } else if (warp < 12 || warp >= (kOut ? 28 : 20)) {
+    if (kOut) asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+    // ---- V': half of the rows, weighted, in three parts; eight values at a time ----
+    constexpr int kVecs = DV / 8, kStep = 128 / kVecs, kPasses = kLinChunk / 2 / kStep;
+    const int t = (warp & 3) * 32 + lane, v8 = t % kVecs, r0 = t / kVecs + (warp >= 20 ? kLinChunk / 2 : 0);
+    const int at = (v8 >> 3) * kHalf + r0 * 128 + (((v8 & 7) ^ (r0 & 7)) << 4);
     while (const Record* r = next()) {
       if (r->rows > 0) {
         const int s = n % kStages;
-        const uint32_t to = tmem + (kOut || !(n & 1) ? kTV : kTV1) + lanes;
+        uint8_t* from = smem + s * kStage + kValueAt + at;
+        uint8_t* to = smem + kWeightedAt + (kOut ? 0 : 3 * (n & 1) * kValueBytes) + at;
         wait(&ctl.full[s], n / kStages);
-        if (kOut && n > 0) wait(&ctl.sums, n - 1);
+        if (kOut && n > 0) wait(&ctl.sums[1], n - 1);
         if (!kOut && n > 1) wait(&ctl.read[n & 1], (n >> 1) - 1);
         if (!ok) break;
-        if (mine) {
-          uint8_t* at = smem + s * kStage + kValueAt + (d >> 6) * kHalf + (d & 7) * 2;
-          f32x2 check = 0ull;
-          tc_fence_after();
+        f32x2 check = 0ull;
 #pragma unroll 1
-          for (int g = kOut ? 0 : 4 * group; g < (kOut ? 8 : 4 * group + 4); ++g) {  // eight rows
-            uint32_t part[3][4];
+        for (int g = 0; g < kPasses; ++g) {
+          const uint4 b = *reinterpret_cast<const uint4*>(from + g * kStep * 128);
+          const float f = r->weight[r0 + g * kStep];
+          const f32x2 weight = pair(f, f);
+          const uint32_t two[4] = {b.x, b.y, b.z, b.w};
+          uint32_t part[3][4];
 #pragma unroll
-            for (int y = 0; y < 4; y += 2) {
-              const float4 w = *reinterpret_cast<const float4*>(&r->weight[8 * g + 2 * y]);
-#pragma unroll
-              for (int z = 0; z < 2; ++z) {
-                const int e = 2 * (y + z);
-                const uint16_t b0 = *reinterpret_cast<const uint16_t*>(at + (8 * g + e) * 128 + ((v8 ^ e) << 4));
-                const uint16_t b1 = *reinterpret_cast<const uint16_t*>(at + (8 * g + e + 1) * 128 + ((v8 ^ (e + 1)) << 4));
-                f32x2 x = pair(__uint_as_float((uint32_t)b0 << 16), __uint_as_float((uint32_t)b1 << 16));
-                if (kOut) check = fma2(x, 0ull, check);
-                x = mul2(x, z ? pair(w.z, w.w) : pair(w.x, w.y));
-                part[0][y + z] = round_pair(x);
-                part[1][y + z] = round_pair(x);
-                part[2][y + z] = last_pair(x);
-              }
-            }
-#pragma unroll
-            for (int k = 0; k < 3; ++k) tmem_st4(to + 32 * k + 4 * g, part[k]);
+          for (int y = 0; y < 4; ++y) {
+            f32x2 x = pair(bf16_lo(two[y]), bf16_hi(two[y]));
+            if (kOut) check = fma2(x, 0ull, check);
+            x = mul2(x, weight);
+            part[0][y] = round_pair(x);
+            part[1][y] = round_pair(x);
+            part[2][y] = last_pair(x);
           }
-          if (kOut) {
-            int bad = kLinChunk;
-            const float2 two = unpair(check);
-            if (two.x + two.y != 0.0f) {  // rare: what is not finite goes, its first row is noted
-#pragma unroll 1
-              for (int y = kLinChunk - 1; y >= 0; --y) {
-                uint16_t* e = reinterpret_cast<uint16_t*>(at + y * 128 + ((v8 ^ (y & 7)) << 4));
-                if (!bf16_not_finite(*e)) continue;
-                *e = 0;
-                bad = y;
-              }
-              proxy_fence();
-            }
-            ctl.bad_row[n & 1][d] = bad;
-            __syncwarp();
-          }
-          tmem_st_wait();
-          tc_fence_before();
+#pragma unroll
+          for (int k = 0; k < 3; ++k)
+            *reinterpret_cast<uint4*>(to + k * kValueBytes + g * kStep * 128) = make_uint4(part[k][0], part[k][1], part[k][2], part[k][3]);
         }
+        if (kOut) {
+          const float2 two = unpair(check);
+          if (two.x + two.y != 0.0f) {  // rare: what is not finite goes, its first row is noted
+#pragma unroll 1
+            for (int x = 0; x < 8 * kPasses; ++x) {
+              const int g = x >> 3, e = x & 7;
+              uint16_t* value = reinterpret_cast<uint16_t*>(from + g * kStep * 128) + e;
+              if (!bf16_not_finite(*value)) continue;
+              *value = 0;
+              atomicMax(&ctl.bad_row[n & 3][v8 * 8 + e], (unsigned long long)(n + 1) << 8 | (255u - (r0 + g * kStep)));
+            }
+          }
+        }
+        proxy_fence();
         __syncwarp();
         if (lane == 0) {
           mbar_arrive(&ctl.weighted[n & 1]);
-          if (kOut) mbar_arrive(&ctl.noted[n & 1]);
+          if (kOut) mbar_arrive(&ctl.noted[n & 3]);
           mbar_arrive(&ctl.empty[s]);
         }
         ++n;
@@ -610,31 +628,38 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
         // once for the first chunk's operand, once for the chunk's sums (and the next one's operand)
 #pragma unroll 1
         for (int pass = kOut && begins ? 0 : 1; pass < 2; ++pass) {
-          if (pass) wait(&ctl.sums, n);  // O2 of the chunk, issued before, has read the operand as well
-          if (!ok) break;
-          const bool give = kOut && !(pass && ends);
-          __syncwarp();
-          if (mine) {
-            tc_fence_after();
+          if (pass) {
+            wait(&ctl.sums[kh], n);
+            if (!ok) break;
+            __syncwarp();
+            if (mine) {
+              tc_fence_after();
 #pragma unroll
-            for (int k = 0; k < kKeys; k += 16) {
-              if (pass) {
+              for (int k = 0; k < kKeys; k += 16) {
                 uint32_t w[16];
                 tmem_ld16(u + k, w);
                 wait_ld(w);
 #pragma unroll
                 for (int y = 0; y < 8; ++y) st[k / 2 + y] = fma2(f, st[k / 2 + y], pair_of(w[2 * y], w[2 * y + 1]));
               }
-              if (give) operand(k);
+              tc_fence_before();
             }
-            if (give) tmem_st_wait();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&ctl.sums_read[kh]);
+          }
+          if (!kOut || (pass && ends)) continue;
+          if (n + pass > 0) wait(&ctl.operand_read, n + pass - 1);
+          if (!ok) break;
+          __syncwarp();
+          if (mine) {
+            tc_fence_after();
+#pragma unroll
+            for (int k = 0; k < kKeys; k += 16) operand(k);
+            tmem_st_wait();
             tc_fence_before();
           }
           __syncwarp();
-          if (lane == 0) {
-            if (pass) mbar_arrive(&ctl.sums_read);
-            if (give) mbar_arrive(&ctl.state_ready);
-          }
+          if (lane == 0) mbar_arrive(&ctl.state_ready);
         }
         if (!ok) break;
         ++n;
@@ -654,7 +679,7 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
     // ---- O: value d, half `set` of the rows ----
     const int quad = warp & 3, set = (warp - 20) >> 2, d = quad * 32 + lane;
-    const uint32_t at = tmem + ((uint32_t)(quad * 32) << 16) + 32 * set;
+    const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16) + 32 * set;
     constexpr int kVecs = DV / 8;
     while (const Record* r = next()) {
       const int64_t out_row = (int64_t)p.Hq * DV;
@@ -666,14 +691,16 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
       }
       const int rows = r->rows;
       if (rows > 0) {
-        wait(&ctl.noted[n & 1], n >> 1);
-        wait(&ctl.out_ready, n);
+        wait(&ctl.noted[n & 3], n >> 2);
+        wait(&ctl.out_ready[n & 1], n >> 1);
         if (n > 0) wait(&ctl.stored, n - 1);
         if (!ok) break;
         if (quad * 32 < DV) {
           tc_fence_after();
           const f32x2 scale = pair(p.scale, p.scale);
-          const int bad = ctl.bad_row[n & 1][d] - 32 * set;
+          const uint32_t at = lanes + 128 * (n & 1);
+          const unsigned long long noted = ctl.bad_row[n & 3][d];
+          const int bad = ((noted >> 8) == n + 1ull ? 255 - (int)(noted & 255) : kLinChunk) - 32 * set;
           uint16_t* to = reinterpret_cast<uint16_t*>(omem) + 32 * set * DV + d;
 #pragma unroll 1
           for (int y = 0; y < 32; y += 8) {
@@ -700,7 +727,7 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
         }
         __syncwarp();
         if (lane == 0) {
-          mbar_arrive(&ctl.out_read);
+          mbar_arrive(&ctl.out_read[n & 1]);
           mbar_arrive(&ctl.staged);
         }
         __syncwarp();
