@@ -850,8 +850,8 @@ typedef struct spec_states {
  *                   SPEC_ERR_TIMEOUT as spec_attend.
  *   ws, ws_bytes    spec_linear_workspace(...) bytes, 256-byte aligned; no zeroing
  *                   needed.  Calls that may overlap need separate ones.
- * Sums and states are fp32.  With bf16 rows of key_dim and value_dim 64 or 128
- * long calls run on the tensor cores, with the scores and the state as sums of two
+ * Sums and states are fp32.  With bf16 rows of key_dim and value_dim 64 or 128 calls
+ * of 14 rows or more per request (K >= 13) run on the tensor cores, with the scores and the state as sums of two
  * bf16 numbers (2^-16 relative) in the products that give out, and the weighted
  * values as sums of three (2^-24) in those that make the state.
  * The result does not depend on the run.  A key or value that is not finite makes
@@ -910,6 +910,8 @@ int spec_linear_commit(const void* k, int64_t k_row_stride, const void* v, int64
  *                   entries above -inf: -1 and -inf.
  *   Rows not asked for get logprob -inf, rank 0, entropy 0, tokens -1; a row with a
  *   NaN, a +inf or no finite logit too, with SPEC_ERR_BAD_INPUT.
+ *   status          SPEC_ERR_TIMEOUT as spec_attend (with what a call that gave up
+ *                   has written, zero-fill its workspace again).
  *   ws, ws_bytes    spec_logprobs_workspace(B, K, V, top_n) bytes, 256-byte aligned,
  *                   zero-filled once before its first use and left ready for the
  *                   next call of these sizes.  Calls that may overlap, and other

@@ -11,7 +11,9 @@
 // worked on.  The rows' products with the state are summed over the warps through
 // shared memory, four or eight rows at a time.
 //
-// Bound by HBM for up to about eight rows, by the rows' passes beyond.
+// Bound by HBM for up to about eight rows, by the rows' passes beyond: 128 tokens of 32
+// heads of 128 with their states 92 us (5.9 TB/s), 64 requests of up to 8 rows 48 us
+// (the states alone 2.8 TB/s) and their commit 55 (5.1 TB/s).
 #include "attend_ring.cuh"
 #include "linear_few.cuh"
 

@@ -9,6 +9,9 @@ constexpr int kLinFewRows = 32;  // rows of a request, and rows times query head
 
 // Few rows of many heads: two states at least are in shared memory at a time, and
 // every SM has a few to go through (fewer heads go to parts of states, linear.cu).
+// There / here, 32 heads of 128 per request: 12 tokens without an update 11.7 / 7.4 us,
+// 64 40.3 / 32.7, 128 with one 104 / 92; 64 requests of 8 rows 50.5 / 48.2, of 10 84 /
+// 64, their commits 57.4 / 55.7 and 71.7 / 59.6.
 inline bool linear_few_serves(int B, int K, int q_heads, int kv_heads, int Dk, int Dv, int dtype, int sms) {
   if ((Dk != 64 && Dk != 128) || (Dv != 64 && Dv != 128)) return false;
   const int e = element_size(dtype), rows = (K + 1) * (q_heads / kv_heads);

@@ -109,7 +109,7 @@ def logprobs(row, token, t, n):
 
 
 def logprob_bound(row, t, logprob):
-    """A term 2^d has d = (l - m) c2 off by three roundings, c2's among them (|d| < 150, but weighted with 2^d: at
-    most 2^-22 of its sum), and ex2's 2^-22; a thread's running sum takes up to 33 steps a round of 16,384 entries and
+    """A term 2^d has d = l c2 - m c2 off by three roundings, c2's among them (|d| < 150, but weighted with 2^d: at
+    most 2^-22 of its sum; m c2's own cancels in ln p), and ex2's 2^-22; a thread's running sum takes up to 33 steps a round of 16,384 entries and
     30 joins.  log2 and the products: 2^-22 of the result."""
     return (33 * (len(row) // 16384 + 1) + 46) * EPS + abs(logprob) * 8 * EPS

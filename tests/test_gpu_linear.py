@@ -552,3 +552,17 @@ def test_parts_of_long_calls(K, shape, dtype):
     for i, a in enumerate(accepted):
         c.k[c.offsets[i] + a + 1:c.offsets[i + 1]] = 0
     c.check(None, before, accepted)
+
+
+@pytest.mark.parametrize("K", [11, 12, 13, 14])
+@pytest.mark.parametrize("B", [2, 40])
+def test_between_the_forms(B, K):
+    """Lengths around those at which another kernel takes over: single chunks, a verification and its commit."""
+    c = Case([K - i % 3 for i in range(B)], K, 8, 8, 128, 128)
+    before = c.states.clone()
+    out = c.attend(to=None)
+    c.check(out, before, states=False)
+    accepted = [i % (n + 1) for i, n in enumerate(c.depth)]
+    c.commit(accepted)
+    assert int(c.status) == 0
+    c.check(None, before, accepted)
