@@ -848,8 +848,9 @@ typedef struct spec_states {
  *   status          a slot out of range, inconsistent offsets or depths: nothing
  *                   of that request is written and SPEC_ERR_BAD_INPUT is set.
  *                   SPEC_ERR_TIMEOUT as spec_attend.
- *   ws, ws_bytes    spec_linear_workspace(...) bytes, 256-byte aligned; no zeroing
- *                   needed.  Calls that may overlap need separate ones.
+ *   ws, ws_bytes    spec_linear_workspace(...) bytes, for this K or a larger one,
+ *                   256-byte aligned; no zeroing needed.  Calls that may overlap
+ *                   need separate ones.
  * Sums and states are fp32.  With bf16 rows of key_dim and value_dim 64 or 128 calls
  * of 14 rows or more per request (K >= 13) run on the tensor cores, with the scores and the state as sums of two
  * bf16 numbers (2^-16 relative) in the products that give out, and the weighted

@@ -379,13 +379,13 @@ cudaError_t launch_rows(const LinearLaunch& p, const LinearPlan& plan, cudaStrea
 // 6 of them.  1 / 3 / 8 / 16 segments: 3 requests of 201 rows of 32 heads of 128 in fp32
 // 111 / 94 / 101 / 118 us (3 taken), one of 501 169 / 129 / 80 / 84 (73 with 10, taken),
 // 16 requests of 256 rows of 16 heads of 64 106 / 152 / 159 / 186 (1 taken).
-LinearPlan linear_rows_plan(int B, int K, int q_heads, int kv_heads, int Dk, int Dv) {
+LinearPlan linear_rows_plan(int B, int K, int q_heads, int kv_heads, int Dk, int Dv, int max_segments) {
   LinearPlan best{};
   best.nseg = 1;
   const long long blocks = (K + kBlockRows) / kBlockRows, heads = (long long)B * kv_heads, queries = (long long)B * q_heads;
   best.seg_rows = (int)(blocks * kBlockRows);
   double least = rows_cost(heads, Dk, Dv, kLinSms).cost * (double)blocks * (q_heads / kv_heads + 0.5);
-  for (int n = 2; n <= kLinMaxSegments && queries * n <= 64 * kLinSms; ++n) {
+  for (int n = 2; n <= max_segments && queries * n <= 64 * kLinSms; ++n) {
     const long long per = (blocks + n - 1) / n;
     if (per < 2) break;
     const double cost = (rows_cost(queries * n, Dk, Dv, kLinSms).cost * 1.5 +
@@ -428,25 +428,31 @@ bool linear_rows_ok(const void* p, int64_t stride, int64_t width, int64_t e) {
          stride <= (INT64_MAX >> 36);
 }
 
-// Segments' first states, and behind them their decays; at least 256 bytes.
+// Segments' first states, and behind them their decays; at least 256 bytes.  The best plan for a length may want more
+// than that for a longer one: a workspace for the longer one serves as well, with the best plan of those that fit.
 struct LinearGeometry {
   LinearPlan plan;
   size_t steps_off, bytes;
 };
 
-LinearGeometry linear_geometry(int B, int K, int q_heads, int kv_heads, int Dk, int Dv, int dtype) {
+LinearGeometry linear_geometry(int B, int K, int q_heads, int kv_heads, int Dk, int Dv, int dtype, size_t limit = SIZE_MAX) {
   LinearGeometry g{};
+  const auto bytes = [&](size_t heads) {
+    return std::max<size_t>(256, heads * Dk * Dv * sizeof(float) + (heads * sizeof(long long) + 255) / 256 * 256);
+  };
+  int most = kLinMaxSegments;
+  while (most > 1 && bytes((size_t)B * kv_heads * most) > limit) --most;
   const bool tc = linear_tc_serves(B, K, q_heads, Dk, Dv, dtype);
-  g.plan = tc ? linear_plan(B, K, q_heads, kv_heads) : linear_rows_plan(B, K, q_heads, kv_heads, Dk, Dv);
+  g.plan = tc ? linear_plan(B, K, q_heads, kv_heads, most) : linear_rows_plan(B, K, q_heads, kv_heads, Dk, Dv, most);
   g.plan.staged = g.plan.nseg > 1 || (tc && q_heads > kv_heads);
   const size_t heads = g.plan.staged ? (size_t)B * kv_heads * g.plan.nseg : 0;
   g.steps_off = heads * Dk * Dv * sizeof(float);
-  g.bytes = std::max<size_t>(256, g.steps_off + (heads * sizeof(long long) + 255) / 256 * 256);
+  g.bytes = bytes(heads);
   return g;
 }
 
 int run_linear(const LinearLaunch& p, int dtype, void* ws, size_t ws_bytes, cudaStream_t stream) {
-  LinearGeometry g = linear_geometry(p.rows.B, p.rows.K, p.Hq, p.H, p.Dk, p.Dv, dtype);
+  LinearGeometry g = linear_geometry(p.rows.B, p.rows.K, p.Hq, p.H, p.Dk, p.Dv, dtype, ws_bytes);
   if (!ws || ws_bytes < g.bytes || (reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return SPEC_ERR_WORKSPACE;
   g.plan.seg_state = static_cast<float*>(ws);
   g.plan.seg_steps = reinterpret_cast<long long*>(static_cast<char*>(ws) + g.steps_off);

@@ -36,13 +36,13 @@ inline bool linear_tc_serves(int B, int K, int q_heads, int Dk, int Dv, int dtyp
 // segment's sums take about 0.6 of its outputs' time, another launch and the scan
 // about 6 chunks.  Whole / in segments: two prompts of 16,384 rows of 32 heads of 128
 // 602 / 523 us, one of 4,096 of 8 heads of 64 142 / 29.
-inline LinearPlan linear_plan(int B, int K, int q_heads, int kv_heads) {
+inline LinearPlan linear_plan(int B, int K, int q_heads, int kv_heads, int max_segments) {
   LinearPlan best{};
   best.nseg = 1;
   const long long chunks = (K + kLinChunk) / kLinChunk;
   best.seg_rows = (int)(chunks * kLinChunk);
   double least = 0.0;
-  for (int n = 1; n <= kLinMaxSegments; ++n) {
+  for (int n = 1; n <= max_segments; ++n) {
     const long long per = (chunks + n - 1) / n;
     if (n > 1 && per < 4) break;
     const long long outs = ((long long)B * q_heads * n + kLinSms - 1) / kLinSms;

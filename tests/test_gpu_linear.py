@@ -566,3 +566,22 @@ def test_between_the_forms(B, K):
     c.commit(accepted)
     assert int(c.status) == 0
     c.check(None, before, accepted)
+
+
+@pytest.mark.parametrize("dtype,Hq,H,D", [(F32, 32, 32, 64), (BF16, 8, 2, 128), (F32, 3, 1, 96), (BF16, 4, 4, 64)])
+def test_shorter_calls_in_the_same_workspace(dtype, Hq, H, D):
+    """Calls of fewer rows than the workspace was made for, whose own best division would want a larger one."""
+    rows = 700
+    st = LinearStates(1, Hq, H, D, D, 1, rows, dtype)
+    g = torch.Generator().manual_seed(4)
+    for n in (1, 9, 17, 63, 64, 65, 127, 200, 255, 256, 300, 384, 449, 511, 512, 640, 700):
+        q, k, v = (torch.randn((n, h, D), generator=g).to(dtype) for h in (Hq, H, H))
+        decay = -torch.rand((n, H), generator=g)
+        st.states.zero_()
+        out = torch.empty((n, Hq, D), dtype=dtype, device=DEV)
+        st.attend(0, q.to(DEV), k.to(DEV), v.to(DEV), decay.to(DEV), out, update=True, K=n - 1)
+        o, state, o_size, s_size = ref.linear(q, k, v, decay, torch.zeros((H, D, D)), D ** -0.5)
+        o_tol, s_tol = ref.linear_bounds(o, o_size, state, s_size, n, D, dtype)
+        assert int(st.status) == 0
+        assert bool(((out.cpu().double() - o).abs() <= o_tol).all())
+        assert bool(((st.states[0, int(st.slots[0])].cpu().double() - state).abs() <= s_tol).all())
