@@ -852,7 +852,7 @@ typedef struct spec_states {
  *                   256-byte aligned; no zeroing needed.  Calls that may overlap
  *                   need separate ones.
  * Sums and states are fp32.  With bf16 rows of key_dim and value_dim 64 or 128 calls
- * of 14 rows or more per request (K >= 13) run on the tensor cores, with the scores and the state as sums of two
+ * of 12 rows or more per request (K >= 11) run on the tensor cores, with the scores and the state as sums of two
  * bf16 numbers (2^-16 relative) in the products that give out, and the weighted
  * values as sums of three (2^-24) in those that make the state.
  * The result does not depend on the run.  A key or value that is not finite makes
