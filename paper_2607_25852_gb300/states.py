@@ -56,9 +56,13 @@ class LinearStates:
                            pos_base=pos_base, layer=layer, status=self.status, stream=stream)
 
     def fork(self, parent, stream=None):
-        """Request i becomes a copy of request parent[i] (int32 [B] on the device; -1: zero states)."""
+        """Request i becomes a copy of request parent[i] (int32 [B] on the device; -1: zero states; another that is no
+        request's sets ERR_BAD_INPUT, and what its states are then is not said)."""
+        if parent.shape != self.slots.shape:
+            raise ValueError(f"parent: expected one of each of the {self.B} requests")
         with torch.cuda.stream(stream):
-            start = torch.where(parent >= 0, self.slots[parent.clamp(min=0).long()], -1)
+            start = self.slots[parent.clamp(0, self.B - 1).long()]
+            start = start.masked_fill(parent < 0, -1).masked_fill((parent < -1) | (parent >= self.B), 2 * self.B)
             for layer in range(self.layers):
                 spec_linear_commit(self._no_k, self._no_v, self._no_decay, self.states, start, self._spare, None, self.B,
                                    0, self._ws, pos_base=self._no_rows, layer=layer, status=self.status)

@@ -585,3 +585,20 @@ def test_shorter_calls_in_the_same_workspace(dtype, Hq, H, D):
         assert int(st.status) == 0
         assert bool(((out.cpu().double() - o).abs() <= o_tol).all())
         assert bool(((st.states[0, int(st.slots[0])].cpu().double() - state).abs() <= s_tol).all())
+
+
+def test_fork_from_no_request():
+    """A parent that is no request's is reported; the others' states move, and the next calls go on."""
+    st = LinearStates(2, 1, 1, 64, 64, 4, 1, F32)
+    st.states.copy_(torch.arange(2 * 8, device=DEV).view(2, 8, 1, 1, 1).expand_as(st.states))
+    st.fork(i32([3, 4, -2, -1]))
+    assert int(st.status) == spec.ERR_BAD_INPUT
+    assert sorted(st.slots.tolist() + st._spare.tolist()) == list(range(8))
+    for layer in range(2):
+        assert bool((st.states[layer, st.slots[0]] == 8 * layer + 3).all()) and not bool(st.states[layer, st.slots[3]].any())
+    with pytest.raises(ValueError):
+        st.fork(i32([0, 1]))
+    st.status.zero_()
+    st.fork(i32([0, 0, 0, 0]))
+    assert int(st.status) == 0
+    assert bool((st.states[1, st.slots.long()] == 11).all())
