@@ -903,6 +903,7 @@ int spec_linear_commit(const void* k, int64_t k_row_stride, const void* v, int64
  *   accepted_len    device int32 [B], or NULL: every row.  Outside [0, depth], or
  *                   with inconsistent offsets or depths: SPEC_ERR_BAD_INPUT, and the
  *                   request's rows count as not asked for.
+ *   temperature     as spec_verify, and above 0 at least FLT_MIN.
  *   top_n           0 .. SPEC_MAX_TOP.
  *   logprob_out     device fp32 [B, K+1]; rank_out device int32 [B, K+1] or NULL;
  *   entropy_out     device fp32 [B, K+1] or NULL.

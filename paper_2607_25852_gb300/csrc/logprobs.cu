@@ -248,15 +248,17 @@ __device__ __forceinline__ void write_row(const LogLaunch& p, long long r, float
   }
   constexpr float kLn2 = 0.693147180559945309f;
   const float norm = log2f(s), c2 = p.c2;
+  // roundings of a probability near 1 stay on this side of it
+  auto log_of = [&](float l) { return fminf(kLn2 * (above_reference(l, m, c2) - norm), 0.0f); };
   for (int x = lane; x < p.n; x += 32) {
     const Key k = best[x];
     if (p.top_tokens) p.top_tokens[r * p.n + x] = k ? key_index(k) : -1;
-    if (p.top_logprobs) p.top_logprobs[r * p.n + x] = k ? kLn2 * (above_reference(key_value(k), m, c2) - norm) : -INFINITY;
+    if (p.top_logprobs) p.top_logprobs[r * p.n + x] = k ? log_of(key_value(k)) : -INFINITY;
   }
   if (lane == 0) {
-    p.logprob[r] = token >= 0 ? kLn2 * (above_reference(given, m, c2) - norm) : -INFINITY;
+    p.logprob[r] = token >= 0 ? log_of(given) : -INFINITY;
     if (p.rank) p.rank[r] = token >= 0 ? before + 1 : 0;
-    if (p.entropy) p.entropy[r] = kLn2 * (norm - e / s);
+    if (p.entropy) p.entropy[r] = fmaxf(kLn2 * (norm - e / s), 0.0f);
   }
 }
 
@@ -785,7 +787,7 @@ extern "C" int spec_logprobs(const void* logits, int logits_dtype, const int32_t
   if (!logits || !tokens || !logprob_out || (top_n > 0 && !top_tokens_out && !top_logprobs_out))
     return SPEC_ERR_INVALID_ARG;
   if (reinterpret_cast<uintptr_t>(logits) % element_size(logits_dtype) != 0 || !(temperature >= 0.0f) ||
-      std::isinf(temperature))
+      std::isinf(temperature) || (temperature > 0.0f && temperature < FLT_MIN))  // log2(e) / t is finite
     return SPEC_ERR_INVALID_ARG;
   const LogGeometry g = logprobs_geometry(B, K, V, top_n);
   if (!ws || ws_bytes < g.bytes || (reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return SPEC_ERR_WORKSPACE;

@@ -239,3 +239,22 @@ def test_captured_rounds(V, B, K, n):
                         call.check_row(i, j, rows[i * (K + 1) + j], picked[i][j], 1.0, n)
                 else:
                     call.nothing(i, j)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("t", [2.0 ** -126, 1e-30, 1e-3, 1e30, 3e38])
+def test_extreme_temperatures(t, dtype):
+    """From a distribution that is one entry's to a flat one."""
+    V = 5001
+    g = torch.Generator().manual_seed(12)
+    row = torch.randn((1, V), generator=g).to(dtype)
+    best = int(row[0].float().argmax())
+    for token in (best, 17):
+        call = Call(row.to(DEV), i32([[token]]), 1, 0, 3, t)
+        assert int(call.status) == 0
+        want = float(torch.log_softmax(row[0].double() / t, 0)[token])
+        got = float(call.lp[0, 0])
+        # where its binary logarithm is beyond fp32's range a log probability is -inf
+        assert (want / math.log(2) < -3.4e38 and got == -math.inf) or abs(got - want) <= ref.logprob_bound(row[0], t, want), (got, want)
+        assert float(call.entropy[0, 0]) >= 0 and float(call.entropy[0, 0]) < 1.001 * math.log(V)
+        assert int(call.top[0, 0, 0]) == best

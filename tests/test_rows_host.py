@@ -223,3 +223,17 @@ def test_reference_recurrence():
             f = math.exp(float(d[j + 1:i + 1].double().sum()))
             o += f * float(q[i, 0].double() @ k[j, 0].double()) * v[j, 0].double()
         assert torch.allclose(out[i, 0], 0.5 * o, rtol=1e-12)
+
+
+def test_logprobs_refuses_denormal_temperatures(lib):
+    """Their reciprocal is not finite."""
+    for t, code in ((1e-39, 1), (2.0 ** -149, 1)):
+        assert lib.spec_logprobs(DUMMY, 0, None, None, DUMMY, None, 1, 0, 100, t, 0, DUMMY, None, None, None, None, None,
+                                 DUMMY, 1 << 20, STREAM) == code
+
+
+def test_fork_refuses_another_shape():
+    from paper_2607_25852_gb300.states import LinearStates
+    st = LinearStates(1, 1, 1, 64, 64, 3, 1, device="cpu")
+    with pytest.raises(ValueError, match="parent"):
+        st.fork(torch.zeros(2, dtype=torch.int32))
