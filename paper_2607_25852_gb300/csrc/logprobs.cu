@@ -62,6 +62,7 @@ constexpr int kFoundCap = 256;       // vectors of a span
 constexpr int kMaxListed = 512;
 constexpr int kSpan = 8;             // rounds whose best are looked for together
 constexpr float kHuge = 8192.0f;     // of |M|: below it M's rounding, and so the largest d, is at most 2^-11
+constexpr float kLowest = -3.0e38f;  // rounds to a finite number in both types
 typedef unsigned long long Key;      // 0: none
 
 struct alignas(16) LogPartial {
@@ -248,8 +249,11 @@ __device__ __forceinline__ void write_row(const LogLaunch& p, long long r, float
   }
   constexpr float kLn2 = 0.693147180559945309f;
   const float norm = log2f(s), c2 = p.c2;
-  // roundings of a probability near 1 stay on this side of it
-  auto log_of = [&](float l) { return fminf(kLn2 * (above_reference(l, m, c2) - norm), 0.0f); };
+  // roundings of a probability near 1 stay on this side of it (a NaN would stay one)
+  auto log_of = [&](float l) {
+    const float x = kLn2 * (above_reference(l, m, c2) - norm);
+    return x > 0.0f ? 0.0f : x;
+  };
   for (int x = lane; x < p.n; x += 32) {
     const Key k = best[x];
     if (p.top_tokens) p.top_tokens[r * p.n + x] = k ? key_index(k) : -1;
@@ -258,7 +262,8 @@ __device__ __forceinline__ void write_row(const LogLaunch& p, long long r, float
   if (lane == 0) {
     p.logprob[r] = token >= 0 ? log_of(given) : -INFINITY;
     if (p.rank) p.rank[r] = token >= 0 ? before + 1 : 0;
-    if (p.entropy) p.entropy[r] = fmaxf(kLn2 * (norm - e / s), 0.0f);
+    const float x = kLn2 * (norm - e / s);
+    if (p.entropy) p.entropy[r] = x < 0.0f ? 0.0f : x;
   }
 }
 
@@ -488,10 +493,10 @@ __global__ void __launch_bounds__(kLogThreads + 64, kCtasPerSm) logprobs_kernel(
             m = most;
           }
           const float M = __fmul_rn(m, p.c2);
-          if (fabsf(M) < kHuge) {
+          // what is 1,000 binary orders below the largest, and -inf, counts as that: 0 times a number
+          const float low = m - 1000.0f * p.inv_c2;
+          if (fabsf(M) < kHuge && low > kLowest) {
             const f32x2 minus_M = pair(-M, -M);
-            // what is 1,000 binary orders below the largest, and -inf, counts as that: 0 times a number
-            const float low = m - 1000.0f * p.inv_c2;
             const uint32_t low2 = last_pair(pair(low, low));
 #pragma unroll
             for (int u = 0; u < kVecs; ++u)
@@ -503,12 +508,12 @@ __global__ void __launch_bounds__(kLogThreads + 64, kCtasPerSm) logprobs_kernel(
                 s2 = add2(s2, y);
                 e2 = fma2(d, y, e2);
               }
-          } else if (m > -INFINITY) {
+          } else if (m > -INFINITY) {  // M is huge, or temperatures put those orders outside the type
 #pragma unroll
             for (int u = 0; u < kVecs; ++u)
 #pragma unroll
               for (int k = 0; k < W; ++k) {
-                const float x = fmaxf((element<T>(w[u], k) - m) * p.c2, -1000.0f);
+                const float x = fmaxf(above_reference(element<T>(w[u], k), m, p.c2), -1000.0f);
                 const f32x2 y = pair(ex2_approx(x), 0.0f);
                 s2 = add2(s2, y);
                 e2 = fma2(pair(x, 0.0f), y, e2);

@@ -258,3 +258,26 @@ def test_extreme_temperatures(t, dtype):
         assert (want / math.log(2) < -3.4e38 and got == -math.inf) or abs(got - want) <= ref.logprob_bound(row[0], t, want), (got, want)
         assert float(call.entropy[0, 0]) >= 0 and float(call.entropy[0, 0]) < 1.001 * math.log(V)
         assert int(call.top[0, 0, 0]) == best
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("t", [2.0 ** -126, 1e-3, 1e30, 1e35, 4e35, 6e35, 1e37, 3.4028234e38])
+@pytest.mark.parametrize("kind", ["finite", "masked", "wide"])
+def test_entropy_at_extreme_temperatures(t, kind, dtype):
+    """Also where 1,000 binary orders below the largest logit lie outside the type: entries at -inf, and what fills a
+    row's last vector, are no part of the sum.  Logits of the whole range stay what they are beside such a temperature."""
+    for V in (5001, 40003):
+        g = torch.Generator().manual_seed(13)
+        row = torch.randn(V, generator=g) if kind != "wide" else torch.empty(V).uniform_(-1.0, 1.0, generator=g) * 3e38
+        if kind == "masked":
+            row[torch.rand(V, generator=g) < 0.4] = -math.inf
+        row = row.to(dtype)
+        best = int(row.float().argmax())
+        call = Call(row[None].to(DEV), i32([[best]]), 1, 0, 4, t)
+        assert int(call.status) == 0
+        _, _, entropy, top, _ = ref.logprobs(row, best, t, 4)
+        # c2 = log2(e) / t below the smallest normal number is off by up to 2^-150, with logits of up to 2^128 on both
+        # sides of a difference 2^-21 in all
+        tol = 2 * (1 + entropy) * ref.logprob_bound(row, t, entropy) + (2.0 ** -21 if kind == "wide" else 0.0)
+        assert abs(float(call.entropy[0, 0]) - entropy) <= tol, (float(call.entropy[0, 0]), entropy)
+        assert call.top[0, 0].tolist() == top
