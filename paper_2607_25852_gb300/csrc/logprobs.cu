@@ -162,10 +162,15 @@ __device__ __forceinline__ float next_above(float x) {
   return __int_as_float(x == 0.0f ? kStep : x > 0.0f ? min(b + kStep, 0x7F800000) : b - kStep);
 }
 
-// The difference of the references of two sums, at most 0 for b the larger.
+// The difference of the references of the sums of a and of b, a at most b.  Below kHuge a reference is the rounded
+// product with c2, beyond it the exact one: where one is of each kind, the rounding of the first counts.
 __device__ __forceinline__ float reference_step(float a, float b, float c2) {
   const float x = __fmul_rn(a, c2), y = __fmul_rn(b, c2);
-  const float d = fabsf(x) < kHuge && fabsf(y) < kHuge ? x - y : a == b ? 0.0f : (a - b) * c2;
+  const bool small_a = fabsf(x) < kHuge, small_b = fabsf(y) < kHuge;
+  float d = a == b ? 0.0f : (a - b) * c2;
+  if (small_a && small_b) d = x - y;
+  else if (small_a) d += fmaf(-a, c2, x);
+  else if (small_b) d += fmaf(b, c2, -y);
   return fmaxf(d, -1000.0f);  // -inf, and NaN of two that are -inf
 }
 // c2 l_v - M for the reference of m.

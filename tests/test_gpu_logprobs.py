@@ -281,3 +281,21 @@ def test_entropy_at_extreme_temperatures(t, kind, dtype):
         tol = 2 * (1 + entropy) * ref.logprob_bound(row, t, entropy) + (2.0 ** -21 if kind == "wide" else 0.0)
         assert abs(float(call.entropy[0, 0]) - entropy) <= tol, (float(call.entropy[0, 0]), entropy)
         assert call.top[0, 0].tolist() == top
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("t,V", [(1.0, 5001), (0.01, 5001), (0.01, 201088), (100.0, 40003)])
+def test_sums_of_two_references(t, V, sign):
+    """The largest logits around 8,192 binary orders on either side: below that a sum is relative to its largest logit's
+    rounded product with log2(e) / t, beyond it to the exact one, and sums of both kinds meet in a row.  (In bf16 such
+    logits are 32 binary orders apart, and only the largest counts.)"""
+    n = 8
+    g = torch.Generator().manual_seed(V)
+    row = sign * 8192 * math.log(2) * t + t * torch.empty(V).uniform_(-1.0, 1.0, generator=g)
+    # some have the border within a thread's own elements, some between threads, some between a row's pieces
+    for r in (row, row.sort()[0], row.sort(descending=True)[0]):
+        tokens = [0, int(r.argmax()), V - 1]
+        call = Call(r.repeat(3, 1).to(DEV), i32([[x] for x in tokens]), 3, 0, n, t)
+        assert int(call.status) == 0
+        for i, token in enumerate(tokens):
+            call.check_row(i, 0, r, token, t, n)
