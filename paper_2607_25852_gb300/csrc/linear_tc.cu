@@ -207,7 +207,7 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
     }
     for (int s = 0; s < kRecords; ++s) {
       mbar_init(&ctl.listed[s], 1);
-      mbar_init(&ctl.used[s], 2 + kWeighers + 8 + (kOut ? 4 + 8 : 0));
+      mbar_init(&ctl.used[s], 3 + kWeighers + 8 + (kOut ? 4 + 8 : 0));  // all that read it
     }
     mbar_init(&ctl.state_ready, 8);
     mbar_init(&ctl.operand_read, 1);
@@ -338,14 +338,10 @@ __global__ void __launch_bounds__(kOut ? kOutThreads : kSumThreads, 1)
       };
       while (const Record* r = next()) {
         const int rows = r->rows, row = r->row0, h = r->h, hq = r->hq;
-        const bool mine = rows > 0 ? (n & 1) == (uint32_t)(warp & 1) : warp == 2;
-        __syncwarp();
-        if (mine && lane == 0) mbar_arrive(&ctl.used[c % kRecords]);
-        __syncwarp();
-        ++c;
+        done();  // both read every record, to count the chunks
         if (rows == 0) continue;
         const uint32_t chunk = n++;
-        if (!mine) continue;
+        if ((chunk & 1) != (uint32_t)(warp & 1)) continue;
         const int s = chunk % kStages;
         const uint32_t use = chunk / kStages;
         if (use > 0) wait(&ctl.empty[s], use - 1);

@@ -602,3 +602,30 @@ def test_fork_from_no_request():
     st.fork(i32([0, 0, 0, 0]))
     assert int(st.status) == 0
     assert bool((st.states[1, st.slots.long()] == 11).all())
+
+
+@pytest.mark.parametrize("K", [11, 63])
+def test_many_idle_requests_before_live_ones(K):
+    """Chunks without rows, many more than are listed ahead, one after another, with a few requests behind them and some
+    between: outputs and states by one call, states by a commit, on the tensor cores."""
+    B, H, D = 120, 32, 64
+    c = Case([K] * B, K, H, H, D, D)
+    live = {0, 61, 62, 114, 116, 117, 118, 119}
+    c.pos = [5 if i in live else -(K + 1) for i in range(B)]
+    for i in range(B):
+        if i not in live:
+            c.k[c.offsets[i]:c.offsets[i + 1]] = math.nan
+    before = c.states.clone()
+    for call in (c.attend, lambda: c.commit(None)):
+        c.states.copy_(before)
+        c.states[1, c.to] = 9.0
+        out = call()
+        assert int(c.status) == 0
+        for i in range(B):
+            if i not in live:
+                assert torch.equal(c.states[1, c.to[i]], before[1, c.start[i]])
+                assert out is None or not bool(out[c.offsets[i]:c.offsets[i + 1]].any())
+                continue
+            o, o_tol, s, s_tol = c.want(i, before)
+            assert bool(((c.states[1, c.to[i]].cpu().double() - s).abs() <= s_tol).all())
+            assert out is None or bool(((out[c.offsets[i]:c.offsets[i + 1]].cpu().double() - o).abs() <= o_tol).all())
