@@ -55,3 +55,32 @@ def test_every_reader_arrives_for_every_record():
         assert "continue" not in re.sub(r"if \(!kOut \|\| \(pass && ends\)\) continue;|if \(!bf16_not_finite\(\*value\)\) continue;",
                                         "", before)
         assert not re.search(r"(?<!if \(!ok\) )break;", before)
+
+
+def in_flight(ahead, stages):
+    """A loading warp's chunks that may still be on their way where it gives up at its next one, every stage filled as
+    early as the ring lets it: chunk x once x - stages was read, and those are read in order."""
+    return [x for x in range(ahead - 2, -1, -2) if x + stages >= ahead]
+
+
+def test_copies_in_flight_end_before_the_cta():
+    """Where a wait gives up the boxes that the loading warps have sent are waited for, with a limit, before the CTA
+    ends; the MMAs' products by their thread."""
+    source = roles()
+    loop = source["---- loads,"]
+    loop = loop[loop.index("while (const Record* r = next())"):]
+    # noted after the last wait that may give up, before the first box
+    assert loop.index("if (!ok) break;") < loop.index("ctl.sent[warp & 1] = chunk + 1;") < loop.index("bring(&tmQ")
+    end = source["---- O: value"]
+    end = end[end.index("__syncthreads();"):]
+    drain = re.search(r"for \(uint32_t x = 0; x < 4; \+\+x\) \{\s*const uint32_t sent = ctl\.sent\[x & 1\], y = 1 \+ \(x & 2\);\s*"
+                      r"if \(y <= sent\) wait_phase\(&ctl\.full\[\(sent - y\) % kStages\], \(sent - y\) / kStages & 1u, p\.status\);", end)
+    assert drain and "if (tid == 0 && ctl.aborted) {" in end[:drain.start()]
+    for stages in (3, 4):
+        for ahead in range(2, 40):  # `sent` is ahead - 1
+            waited = [ahead - 1 - y for y in (1, 3) if y <= ahead - 1]
+            assert set(in_flight(ahead, stages)) <= set(waited)
+            # none of their barriers is two uses on, where the wait would be for another chunk: the other warp's chunks
+            # end below ahead + stages, as nothing from `ahead` on is read, and this warp's below `ahead`
+            assert all(x + 2 * stages >= ahead + stages or (x + 2 * stages - ahead) % 2 == 0 for x in waited)
+    assert "wait_phase(&ctl.drained, 0u, p.status);" in source["---- MMAs"]
