@@ -196,3 +196,50 @@ def test_calls_at_once():
             torch.cuda.synchronize()
             for (_, result), w in zip(calls, want):
                 assert all(torch.equal(a, b) for a, b in zip(result, w)) and int(result[-1]) == 0
+
+
+def test_calls_at_once_write_everything():
+    """As above, with every output of the calls, the new states among them, set to something else before."""
+    g = torch.Generator().manual_seed(7)
+
+    def make(B, K, H, dk, V, n, dtype):
+        R = B * (K + 1)
+        q, k, v = (torch.randn((R, H, dk), generator=g).to(dtype).to(DEV) for _ in range(3))
+        decay = (-torch.rand((R, H), generator=g)).to(DEV)
+        states = torch.randn((2 * B, H, dk, dk), generator=g).to(DEV)
+        start, to = torch.arange(B, dtype=torch.int32, device=DEV), torch.arange(B, 2 * B, dtype=torch.int32, device=DEV)
+        ws, lws = spec.linear_workspace(B, K, H, H, dk, dk, dtype, DEV), spec.logprobs_workspace(B, K, V, n, DEV)
+        logits = torch.randn((R, V), generator=g).to(dtype).to(DEV)
+        tokens = torch.randint(0, V, (B, K + 1), generator=g).to(torch.int32).to(DEV)
+        freq, pos = spec.spec_rotary_frequencies(dk), torch.arange(B, device=DEV) * 37
+        turned, out = torch.empty_like(q), torch.empty_like(v)
+        lp, status = torch.empty((B, K + 1), device=DEV), i32([0])
+        top = torch.empty((B, K + 1, n), dtype=torch.int32, device=DEV)
+
+        def call():
+            spec.spec_rotary(q, freq, pos, B, K, turned, status=status)
+            spec.spec_linear_attend(turned, k, v, decay, states, start, to, B, K, out, ws, status=status)
+            spec.spec_logprobs(logits, tokens, B, K, V, lp, lws, top_tokens_out=top, status=status)
+        def spoil():
+            for x in (turned, out, states[B:], lp):
+                x.fill_(77.0)
+            top.fill_(-9)
+        return call, spoil, (turned, out, states, lp, top, status)
+    for sizes in [((40, 3, 8, 64, 3000, 4, torch.bfloat16), (2, 255, 8, 128, 500, 2, torch.bfloat16)),
+                  ((3, 200, 4, 64, 900, 8, F32), (70, 0, 16, 128, 5000, 3, F32))]:
+        calls = [make(*s) for s in sizes]
+        want = []
+        for call, spoil, result in calls:
+            spoil()
+            call()
+            torch.cuda.synchronize()
+            want.append([x.clone() for x in result])
+        streams = [torch.cuda.Stream() for _ in calls]
+        for _ in range(5):
+            for stream, (call, spoil, _) in zip(streams, calls):
+                with torch.cuda.stream(stream):
+                    spoil()
+                    call()
+            torch.cuda.synchronize()
+            for (_, _, result), w in zip(calls, want):
+                assert all(torch.equal(a, b) for a, b in zip(result, w)) and int(result[-1]) == 0

@@ -629,3 +629,49 @@ def test_many_idle_requests_before_live_ones(K):
             o, o_tol, s, s_tol = c.want(i, before)
             assert bool(((c.states[1, c.to[i]].cpu().double() - s).abs() <= s_tol).all())
             assert out is None or bool(((out[c.offsets[i]:c.offsets[i + 1]].cpu().double() - o).abs() <= o_tol).all())
+
+
+@pytest.mark.parametrize("depth,K,shape,dtype", [
+    ([2500, 2000, 1111], 2500, (16, 16, 128, 128), BF16),  # the tensor cores, in segments
+    ([100] * 20, 100, (16, 16, 64, 128), BF16),            # and whole, more heads than SMs
+    ([2000], 2000, (2, 1, 128, 128), BF16),                # query heads in groups
+    ([7, 3] * 20, 7, (8, 8, 128, 128), BF16),              # few rows of many heads
+    ([150, 60, 201], 201, (4, 2, 72, 96), F32),            # the CUDA cores, in segments
+    ([5, 1], 5, (2, 2, 256, 256), BF16)])                  # and whole
+def test_every_run_leaves_the_same_states(depth, K, shape, dtype):
+    """A call writes all of its outputs and states, the same at every run; a commit of all rows the same states."""
+    c = Case(depth, K, *shape, dtype=dtype)
+    before = c.states.clone()
+    at = torch.tensor(c.to, device=DEV)
+    first = None
+    for run in range(12):
+        c.states[1, at] = float(run)
+        out = c.attend()
+        attended = c.states.clone()
+        c.states[1, at] = -float(run)
+        c.commit(None)
+        assert int(c.status) == 0
+        if first is None:
+            first = out, attended, c.states.clone()
+            c.check(out, before)
+        assert torch.equal(out, first[0])
+        assert torch.equal(attended, first[1])
+        assert torch.equal(c.states, first[2])
+
+
+@pytest.mark.parametrize("K,B", [(16, 24), (80, 24), (300, 5)])
+@pytest.mark.parametrize("shape", [(16, 4, 128, 128), (8, 2, 64, 64), (6, 2, 128, 64)])
+def test_groups_in_place(shape, K, B):
+    """Query heads in groups, many requests, new states in the old ones' slots, on the tensor cores: a head's outputs
+    are those of the old state whichever of its group is done first.  Some start from zeros, some from a shared slot."""
+    c = Case([(7 * i + 5) % K + 1 for i in range(B)], K, *shape)
+    c.to = list(c.start)
+    c.start[3] = -1
+    spare = next(s for s in range(c.slots) if s not in c.start + c.to)
+    c.start[1] = c.start[2] = spare
+    before = c.states.clone()
+    for _ in range(3):
+        c.states.copy_(before)
+        out = c.attend()
+        assert int(c.status) == 0
+        c.check(out, before)
