@@ -253,10 +253,12 @@ __device__ __forceinline__ void write_row(const LogLaunch& p, long long r, float
     return;
   }
   constexpr float kLn2 = 0.693147180559945309f;
-  const float norm = log2f(s), c2 = p.c2;
-  // roundings of a probability near 1 stay on this side of it (a NaN would stay one)
+  const float norm = log2f(s), c2 = p.c2, M = __fmul_rn(m, c2);
+  // above_reference less log2 s, in halves: of a logit near the type's lowest value ln p is in fp32's range where log2 p is
+  // not.  Roundings of a probability near 1 stay on this side of it (a NaN would stay one).
   auto log_of = [&](float l) {
-    const float x = kLn2 * (above_reference(l, m, c2) - norm);
+    const float half = fabsf(M) < kHuge ? fmaf(0.5f * l, c2, -0.5f * M) : (0.5f * l - 0.5f * m) * c2;
+    const float x = 2.0f * (kLn2 * (half - 0.5f * norm));
     return x > 0.0f ? 0.0f : x;
   };
   for (int x = lane; x < p.n; x += 32) {

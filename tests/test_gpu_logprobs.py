@@ -299,3 +299,33 @@ def test_sums_of_two_references(t, V, sign):
         assert int(call.status) == 0
         for i, token in enumerate(tokens):
             call.check_row(i, 0, r, token, t, n)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("t", [1.0, 1.3, 7.0, 1e5])
+@pytest.mark.parametrize("kind", ["masked", "all_masked", "wide"])
+def test_masks_of_the_lowest_value(kind, t, dtype):
+    """Entries at the type's lowest value are entries like others: ln p of them is what it is, where it is in fp32's
+    range, as a token's and among the alternatives; logits of the whole range likewise."""
+    V, n = 3001, 32
+    g = torch.Generator().manual_seed(14)
+    row = torch.randn(V, generator=g)
+    if kind == "wide":
+        row = torch.empty(V).uniform_(-1.0, 1.0, generator=g) * 3.3e38
+    row = row.to(dtype)
+    if kind == "masked":
+        row[torch.randperm(V, generator=g)[7:]] = torch.finfo(dtype).min
+    elif kind == "all_masked":
+        row.fill_(torch.finfo(dtype).min)
+    for token in (0, int(row.argmin()), int(row.argmax()), V - 1):
+        call = Call(row[None].to(DEV), i32([[token]]), 1, 0, n, t)
+        assert int(call.status) == 0
+        lp, rank, entropy, best, best_lp = ref.logprobs(row, token, t, n)
+
+        def same(got, want):
+            # fp32's largest number is 2^128 - 2^104: what is at -2^128 or below is -inf in it
+            return got == -math.inf if want <= -2.0 ** 128 else abs(got - want) <= ref.logprob_bound(row, t, want)
+        assert same(float(call.lp[0, 0]), lp) and int(call.rank[0, 0]) == rank
+        assert abs(float(call.entropy[0, 0]) - entropy) <= 2 * (1 + entropy) * ref.logprob_bound(row, t, entropy)
+        assert call.top[0, 0].tolist() == best
+        assert all(same(a, b) for a, b in zip(call.top_lp[0, 0].tolist(), best_lp))
