@@ -774,7 +774,10 @@ int spec_rotary_frequencies(int rotary_dim, double base, int scaling, double fac
  *                   skipped (not written); rows of inconsistent offsets or depths
  *                   too, and rows past position 2^32 - 1, with SPEC_ERR_BAD_INPUT.
  *   out             as x; may be x itself with the same stride (in place), else
- *                   they do not overlap. */
+ *                   they do not overlap.
+ * Limits: 1 <= B, 0 <= K <= SPEC_MAX_DRAFTS, B (K + 1) <= 2^28.  A longer prompt is
+ * passed in calls of up to K + 1 = 256 rows, or in one as several requests of so many,
+ * each with its own pos_base (and, with a cache, the same row of the table). */
 int spec_rotary(const void* x, int64_t x_row_stride, int heads, int head_dim, int dtype,
                 const double* frequencies, int rotary_dim, int interleaved, float amplitude,
                 const int32_t* row_offsets, const int32_t* depth, const int64_t* pos_base, int B,
@@ -834,8 +837,9 @@ typedef struct spec_states {
  *                   bytes): views of a fused projection will do.
  *   log_decay       device fp32, row r's of head h at [r * decay_row_stride + h];
  *                   decay_row_stride 0: one per head.  At most 0; -inf forgets
- *                   everything before the row.  A value above 0 or NaN counts as 0
- *                   and sets SPEC_ERR_BAD_INPUT.
+ *                   what is finite of everything before the row (0 times the rest
+ *                   stays NaN; slot -1 begins anew).  A value above 0 or NaN counts
+ *                   as 0 and sets SPEC_ERR_BAD_INPUT.
  *   slots_in        device int32 [B]; slots_out device int32 [B] or NULL.
  *   row_offsets, depth  as spec_attend, with K up to SPEC_MAX_LINEAR_ROWS - 1.
  *   pos_base        device int64 [B] or NULL (all rows count): rows before
@@ -852,9 +856,11 @@ typedef struct spec_states {
  *                   256-byte aligned; no zeroing needed.  Calls that may overlap
  *                   need separate ones.
  * Sums and states are fp32.  With bf16 rows of key_dim and value_dim 64 or 128 calls
- * of 12 rows or more per request (K >= 11) run on the tensor cores, with the scores and the state as sums of two
- * bf16 numbers (2^-16 relative) in the products that give out, and the weighted
- * values as sums of three (2^-24) in those that make the state.
+ * of 12 rows or more per request (K >= 11) run on the tensor cores, with the scores
+ * and the state as sums of two bf16 numbers (2^-16 relative) in the products that
+ * give out, and the weighted values as sums of three (2^-24) in those that make the
+ * state; scores and states beyond bf16's largest number, 3.39e38, make outputs that
+ * are not finite there.
  * The result does not depend on the run.  A key or value that is not finite makes
  * its own and later rows' outputs and the state not finite where it enters them;
  * earlier rows are not touched.
@@ -911,13 +917,16 @@ int spec_linear_commit(const void* k, int64_t k_row_stride, const void* v, int64
  *                   that shape; one may be NULL, both where top_n = 0.  Past the
  *                   entries above -inf: -1 and -inf.
  *   Rows not asked for get logprob -inf, rank 0, entropy 0, tokens -1; a row with a
- *   NaN, a +inf or no finite logit too, with SPEC_ERR_BAD_INPUT.
+ *   NaN, a +inf or no finite logit too, with SPEC_ERR_BAD_INPUT.  A log probability
+ *   below fp32's range is -inf.
  *   status          SPEC_ERR_TIMEOUT as spec_attend (with what a call that gave up
  *                   has written, zero-fill its workspace again).
  *   ws, ws_bytes    spec_logprobs_workspace(B, K, V, top_n) bytes, 256-byte aligned,
  *                   zero-filled once before its first use and left ready for the
  *                   next call of these sizes.  Calls that may overlap, and other
  *                   sizes, need separate ones.
+ * Limits: 1 <= B, 0 <= K <= SPEC_MAX_DRAFTS, B (K + 1) <= 2^28, V < SPEC_MAX_VOCAB.  A
+ * longer prompt's rows are asked for as several requests of up to K + 1 = 256.
  * ---------------------------------------------------------------------- */
 #define SPEC_MAX_TOP 32
 size_t spec_logprobs_workspace(int B, int K, int V, int top_n);

@@ -18,7 +18,8 @@
 // 8 heads of 128 668 -> 82 us).  One token of 16 heads of 128 3.8 us, 64 requests of 8
 // rows of 8 heads of 256 77 us (3.6 TB/s).  Few rows are bound by HBM's latency, many by
 // the issue of FMAs and of the loads from shared memory that feed them: 64 requests of
-// 256 rows of 16 heads of 64 take 411 us, 24 TFLOP/s.
+// 256 rows of 16 heads of 64 take 411 us, 24 TFLOP/s.  (Two instances with 16 rows of
+// the state per thread keep 8 and 24 bytes on the stack.)
 #include <cmath>
 
 #include <algorithm>

@@ -8,8 +8,8 @@ namespace spec {
 constexpr int kLinFewRows = 32;  // rows of a request, and rows times query heads per key-value head, at most
 
 // Few rows of many heads: two states at least are in shared memory at a time, and
-// every SM has a few to go through (fewer heads go to parts of states, linear.cu).
-// There / here, 32 heads of 128 per request: 12 tokens without an update 11.7 / 7.4 us,
+// every SM has a few to go through (fewer heads go by parts of states, linear.cu).
+// By parts of states / here, 32 heads of 128 per request: 12 tokens without an update 11.7 / 7.4 us,
 // 64 40.3 / 32.7, 128 with one 104 / 92; 64 requests of 8 rows 50.5 / 48.2, of 10 84 /
 // 64, their commits 57.4 / 55.7 and 71.7 / 59.6.  Query heads in groups go one after
 // another in both; 64 requests of 8 states, 2 / 4 / 8 query heads each: one row 18.0 / 15.3,

@@ -43,7 +43,8 @@
 // 169.  Two threads that issue MMAs took 206, a table of steps in place of the code 314.
 // Measured: 4 requests of 4,096 rows of 38 heads of 128 164 us (4.0 TB/s), 2 of 16,384 of
 // 32 heads 523 (in segments), 64 of 256 of 32 heads 180 (4.5 TB/s), 64 of 64 73 (5.5).
-// (With V' by four warps by way of tensor memory 185, 542, 197 and 95.)
+// (With V' by four warps by way of tensor memory 185, 542, 197 and 95.)  Registers
+// end at 64 and 80 a thread: five of the eight instances keep 8 to 16 bytes on the stack.
 #include "attend_ring.cuh"
 #include "linear_tc.cuh"
 

@@ -11,7 +11,9 @@ namespace spec {
 constexpr int kLinChunk = 64;      // rows that a pass over the state takes
 // Calls of more rows per request go to the tensor cores.  CUDA cores / tensor cores, 32 heads of 128: 64 requests of 10
 // rows 65 / 60 us, of 12 72 / 60, of 17 114 / 61, commits of 12 62 / 61; 12 requests of 10 16.1 / 17.2, of 12 17.9 / 17.3,
-// of 17 27.3 / 17.4, commits of 17 15.5 / 16.8; one of 12 6.5 / 9.7, of 17 9.2 / 9.8.
+// of 17 27.3 / 17.4, commits of 17 15.5 / 16.8; one of 12 6.5 / 9.7, of 17 9.2 / 9.8.  The rule goes by the rows alone,
+// so that from 12 to about 17 rows calls of few heads take up to 3.2 us longer than they would on the CUDA cores, and 64
+// requests of 10 rows 5 us longer than here.
 constexpr int kLinTcRows = 11;
 constexpr int kLinMaxSegments = 32;
 constexpr int kLinSms = 152;       // the device that plans are made for (a workspace's size must not depend on the one it is asked on)

@@ -6,7 +6,8 @@
 //   s = sum_v 2^d_v,  e = sum_v d_v 2^d_v,
 //   ln p_v = ln 2 (c2 l_v - M - log2 s),  H = ln 2 (log2 s - e / s),
 // whose terms are non-negative but for M's rounding, so nothing cancels.  (Where M
-// is beyond thousands of binary orders d_v is c2 (l_v - m), whose first step is exact near m.)
+// is beyond thousands of binary orders d_v is c2 (l_v - m), whose first step is exact near m;
+// sums of both kinds are joined with M's rounding.)
 // A token's rank counts the entries that come before it (greater, or equal with a
 // lower index); its logit is read first, so the count goes along, and only through
 // the vectors whose largest element reaches it.
@@ -27,9 +28,11 @@
 // ring in shared memory; one looks for the best of a span and ends a piece while
 // the four are at the next: done by the four themselves, with barriers, that took
 // as long as the rounds did.  The last CTA to arrive at a row joins its pieces, in
-// order.  Bound by the issue of about 14 instructions an entry (the exponentials' unit
-// alone would take 14 us of 54, HBM 18) for many rows, by a chain of round trips for
-// few: 587 rows of 201,088 with 8 alternatives 89 us after an L2 flush, 76 without
+// order.  No unit bounds many rows: of a round's 54 us the issue of about 14 instructions
+// an entry takes 23, HBM 18, the exponentials 14; what is left are waits, for the vectors
+// of a round and along each thread's two chains of sums, and the calls' begin and end
+// (issue active 59 % of the SMs' active cycles, 44 % of all).  Few rows are bound by a
+// chain of round trips.  587 rows of 201,088 with 8 alternatives 89 us after an L2 flush, 76 without
 // alternatives (3.1 TB/s); one row 19 us then.
 #include <cfloat>
 #include <cmath>

@@ -56,8 +56,9 @@ class LinearStates:
                            pos_base=pos_base, layer=layer, status=self.status, stream=stream)
 
     def fork(self, parent, stream=None):
-        """Request i becomes a copy of request parent[i] (int32 [B] on the device; -1: zero states; another that is no
-        request's sets ERR_BAD_INPUT, and what its states are then is not said)."""
+        """Request i becomes a copy of request parent[i] (int32 [B] on the device; -1: zero states, as for a request that
+        begins; another that is no request's sets ERR_BAD_INPUT, and what its states are then is not said).  All
+        requests' states move, those of requests that stay what they are among them."""
         if parent.shape != self.slots.shape:
             raise ValueError(f"parent: expected one of each of the {self.B} requests")
         with torch.cuda.stream(stream):
